@@ -455,6 +455,119 @@ adadsf_status adadsf_decode_step(const adadsf_model_cfg *cfg, const adadsf_model
                                  int C_max, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Serving from a paged cache. A layer that keeps r_l T tokens caches another
+ * number of keys and values in every layer and sequence; pages of a fixed
+ * number of tokens, handed out by the caller from one pool, hold them
+ * without reserving the longest. (The paper has no counterpart.)
+ *
+ * adadsf_paged_cache: the pool. k, v: [n_pages][n_kv_heads][page_size]
+ * [head_dim] in cfg->dtype (ADADSF_KV_SAME) or as int8 (ADADSF_KV_I8), whose
+ * fp32 scales k_scale, v_scale are [n_pages][n_kv_heads][page_size] (one a
+ * token and head; NULL for ADADSF_KV_SAME). page_size: 16, 32, 64 or 128.
+ * A value is stored as round(x * (127 / m)), ties to even, with scale m / 127,
+ * m the largest |x| of its head's vector, and stands for that number times
+ * its scale. Vectors with m < 2^-100 are stored as zeros; one that holds an
+ * infinity or a NaN gets a NaN scale (every feature reads back as NaN).
+ *
+ * adadsf_paged_batch: B sequences. starts [B+1] (non-decreasing, starts[0]
+ * >= 0, starts[B] <= n_rows), lens [B] and table [B][max_pages] are device int32.
+ * Sequence b has lens[b] tokens in the cache, the token at place p in slot
+ * p % page_size of page table[b][p / page_size]; the batch addresses its
+ * last n_b = starts[b+1] - starts[b] ones: packed row starts[b] + i is the
+ * token at place lens[b] - n_b + i. max_new: host bound, n_b <= max_new.
+ * Entries of table past a sequence's last page are not read, nor are slots
+ * past its last token. Sequences must not share pages that a call writes.
+ * Counts that break these rules, and page numbers outside [0, n_pages), set
+ * the device error word (adadsf_sync_check: ADADSF_ERR_INVALID_ARG); such
+ * counts are clamped, tokens of such pages read as zeros (keys included) and are not
+ * written. A row whose place is negative (n_b > lens[b]) has no token: it
+ * is not written, reads back as zeros and attends to nothing.
+ * Every count lives on the device, so launches depend on B, n_rows, max_new
+ * and max_pages only and one captured graph serves growing sequences.
+ * ---------------------------------------------------------------------- */
+typedef enum { ADADSF_KV_SAME = 0, ADADSF_KV_I8 = 1 } adadsf_kv_store;
+
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int32_t n_pages, page_size;
+  int32_t store;         /* adadsf_kv_store */
+} adadsf_paged_cache;
+
+typedef struct {
+  const int32_t *starts, *lens, *table;
+  int64_t n_rows;        /* packed rows (0: calls return at once) */
+  int32_t B, max_new, max_pages;
+} adadsf_paged_batch;
+
+/* (cos, sin) pairs of positions 0 .. n_pos - 1: tab_dev fp32
+ * [n_pos][rotary_dim / 2][2], pair i turning by pos * rope_theta^(-2 i /
+ * rotary_dim). */
+adadsf_status adadsf_rope_table(const adadsf_model_cfg *cfg, int n_pos, float *tab_dev, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary, quantisation and cache write of the batch's rows. qkv_dev
+ * [n_rows, q+2kv] (cfg->dtype), not yet rotated; pos_dev [n_rows] int32 (or
+ * NULL: the row's place): its original position, in [0, n_pos) (else the
+ * device error word is set and the position clamped); tab_dev as
+ * adadsf_rope_table writes it (unused when cfg->rotary_dim is 0). Feature i <
+ * rotary_dim / 2 of a query or key head pairs with i + rotary_dim / 2. q_out_dev (NULL: not
+ * wanted) [n_rows, q] receives the rotated queries, the pages the rotated
+ * keys and the values. Rotation in fp32 and one rounding to what is stored,
+ * whole numbers included. ws: at least 256 bytes (the device error word).
+ * ---------------------------------------------------------------------- */
+adadsf_status adadsf_paged_append(const adadsf_model_cfg *cfg, const adadsf_paged_cache *cache,
+                                  const adadsf_paged_batch *batch, const void *qkv_dev, const float *tab_dev,
+                                  int n_pos, const int32_t *pos_dev, void *q_out_dev, void *ws, size_t ws_bytes,
+                                  void *stream);
+
+/* The batch's tokens read back: k_out_dev, v_out_dev [n_rows, kv] in cfg->dtype
+ * (what the stored numbers stand for, rounded once). ws: at least 256 bytes. */
+adadsf_status adadsf_paged_read(const adadsf_model_cfg *cfg, const adadsf_paged_cache *cache,
+                                const adadsf_paged_batch *batch, void *k_out_dev, void *v_out_dev, void *ws,
+                                size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Attention of the batch's rows over their sequences' pages: per query head h,
+ * softmax(q K^T / sqrt(head_dim)) V over the tokens at places up to the row's
+ * own, key/value head h / (n_heads / n_kv_heads). q_dev: rows of q features
+ * (rotated), ld_q elements apart (a multiple of 16 bytes, >= q; rows of a
+ * qkv matrix will do); out_dev [n_rows, q]. cfg->dtype. A row without any
+ * visible token gets zeros. The new tokens' keys and values must be in the
+ * pages (adadsf_paged_append).
+ * ws: adadsf_paged_attention_workspace_size bytes, zero-filled before first
+ * use; it may serve batches of any smaller workspace size.
+ * ---------------------------------------------------------------------- */
+size_t adadsf_paged_attention_workspace_size(const adadsf_model_cfg *cfg, const adadsf_paged_cache *cache,
+                                             const adadsf_paged_batch *batch);
+adadsf_status adadsf_paged_attention(const adadsf_model_cfg *cfg, const adadsf_paged_cache *cache,
+                                     const adadsf_paged_batch *batch, const void *q_dev, int64_t ld_q, void *out_dev,
+                                     void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * The next token of each of B rows of logits. logits_dev: rows of V values
+ * (`dtype`) ld_logits elements apart. Per row, with m its largest logit:
+ *   z_i = (l_i - m) (1 / temperature), w_i = exp(z_i) rounded to a multiple
+ *   of 2^-40 (whole numbers: sums do not depend on their order);
+ *   tokens ranked by logit, equal ones by index, are kept while their rank
+ *   is below top_k, the weight ranked before them is below top_p times the
+ *   weight of the first top_k, and exp(z_i) >= min_p; the first always;
+ *   the token is the first, by index, whose running kept weight exceeds
+ *   floor(u * kept weight).
+ * u_dev [B]: given random numbers in [0, 1). temperature_dev, top_p_dev, min_p_dev
+ * (fp32) and top_k_dev (int32), [B] each, NULL for 1, 1, 0 and 0: top_k <= 0
+ * or >= V, top_p >= 1 and min_p <= 0 (or NaN) keep all; a temperature that is
+ * not above 0 takes the first of the ranking. token_dev [B] int32;
+ * logprob_dev (NULL or fp32 [B]): z_i minus the logarithm of the kept weight (0 without
+ * a temperature). Logits of -infinity or NaN are never drawn; a row of nothing
+ * else gives token -1 and logprob -infinity. V up to 397312.
+ * ---------------------------------------------------------------------- */
+adadsf_status adadsf_sample(const void *logits_dev, int64_t ld_logits, int B, int V, int dtype,
+                            const float *temperature_dev, const int32_t *top_k_dev, const float *top_p_dev,
+                            const float *min_p_dev, const float *u_dev, int32_t *token_dev, float *logprob_dev,
+                            void *stream);
+
+/* ------------------------------------------------------------------------
  * Synchronises `stream`, then reads and clears the device error word at the
  * start of `ws`: ADADSF_ERR_DEVICE_TIMEOUT if a kernel gave up waiting,
  * ADADSF_ERR_INVALID_ARG if a kernel met an out-of-range index,
@@ -490,6 +603,10 @@ typedef enum {
   ADADSF_KERNEL_DECIDE,        /* decode: keep decision of each new token (with the router and norm for at most 16 bf16 sequences; inside the norm launch when another step runs on one stream) */
   ADADSF_KERNEL_KV_CACHE,      /* decode cache: fill (prefill), thresholds */
   ADADSF_KERNEL_ALIGN,         /* alignment objective and router gradient (Eqs. 9-10) */
+  ADADSF_KERNEL_PAGED_APPEND,  /* rotary + write of new tokens into a paged cache */
+  ADADSF_KERNEL_PAGED_READ,    /* paged cache read back */
+  ADADSF_KERNEL_PAGED_ATTENTION,
+  ADADSF_KERNEL_SAMPLE,        /* next tokens from logits */
   ADADSF_KERNEL_COUNT
 } adadsf_kernel_kind;
 

@@ -27,6 +27,7 @@ ALLOC_RAW, ALLOC_ROUND = 1, 2
 FLAG_GATE_SIGMOID = 1
 FLAG_FOLDED_NORMS = 2
 FLAG_GATHERED_QKV = 4
+KV_SAME, KV_I8 = 0, 1
 
 TORCH_DTYPE = {F32: torch.float32, BF16: torch.bfloat16}
 DTYPE_CODE = {torch.float32: F32, torch.bfloat16: BF16}
@@ -57,6 +58,18 @@ class LaunchRecord(ctypes.Structure):
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("store", ctypes.c_int32)]
+
+
+class _PagedBatch(ctypes.Structure):
+    _fields_ = [("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("n_rows", ctypes.c_int64), ("B", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
 class AdadsfError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"adadsf status {status}: {msg}")
@@ -76,6 +89,7 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, sz, f64, u32 = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t,
                                       ctypes.c_double, ctypes.c_uint)
+        ppc, ppb = ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedBatch)
         pcfg, plw, pmw = ctypes.POINTER(ModelCfg), ctypes.POINTER(LayerWeights), ctypes.POINTER(ModelWeights)
         sig = {
             "adadsf_last_error": (ctypes.c_char_p, []),
@@ -106,6 +120,12 @@ def lib() -> ctypes.CDLL:
             "adadsf_prefill": (i32, [pcfg, pmw, vp, i32, i32, vp, vp, vp, vp, sz, i32, vp, sz, vp]),
             "adadsf_decode_workspace_size": (sz, [pcfg, i32, i32]),
             "adadsf_decode_step": (i32, [pcfg, pmw, vp, i32, vp, vp, vp, sz, i32, vp, sz, vp]),
+            "adadsf_rope_table": (i32, [pcfg, i32, vp, vp]),
+            "adadsf_paged_append": (i32, [pcfg, ppc, ppb, vp, vp, i32, vp, vp, vp, sz, vp]),
+            "adadsf_paged_read": (i32, [pcfg, ppc, ppb, vp, vp, vp, sz, vp]),
+            "adadsf_paged_attention_workspace_size": (sz, [pcfg, ppc, ppb]),
+            "adadsf_paged_attention": (i32, [pcfg, ppc, ppb, vp, i64, vp, vp, sz, vp]),
+            "adadsf_sample": (i32, [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]),
             "adadsf_sync_check": (i32, [vp, sz, vp]),
             "adadsf_selftest_bounded_wait": (i32, [vp, sz, i32, vp]),
             "adadsf_profile_begin": (i32, [i32]),
@@ -458,6 +478,154 @@ def adadsf_decode_step(model: DeviceModel, ids: torch.Tensor, hidden_out: torch.
     _check(lib().adadsf_decode_step(ctypes.byref(model.cfg), ctypes.byref(model.struct), _p(ids), B,
                                     _p(hidden_out), _p(kept_out), _p(cache), cache.numel(), int(C_max), _p(ws),
                                     ws.numel(), _s(stream)))
+
+
+# --------------------------------------------------------------------- paged cache
+class PagedCache:
+    """Pool of pages of keys and values (adadsf_paged_cache in
+    include/adadsf.h): k, v [n_pages, n_kv_heads, page_size, head_dim] in the
+    config's type, or int8 with fp32 scales [n_pages, n_kv_heads, page_size]."""
+
+    def __init__(self, cfg: ModelCfg, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        i8 = k.dtype == torch.int8
+        for name, t in (("k", k), ("v", v)):
+            _dev(t, name)
+            if t.dim() != 4 or t.shape != k.shape or t.shape[1] != cfg.n_kv_heads or t.shape[3] != cfg.head_dim:
+                raise ValueError(f"{name} must be [n_pages, {cfg.n_kv_heads}, page_size, {cfg.head_dim}]")
+            if t.dtype != (torch.int8 if i8 else TORCH_DTYPE[cfg.dtype]):
+                raise ValueError(f"{name} is {t.dtype}: the config's type or int8, the same for k and v")
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if (t is not None) != i8:
+                raise ValueError(f"{name}: scales belong to an int8 cache")
+            if i8:
+                _dev(t, name)
+                if t.dtype != torch.float32 or t.shape != k.shape[:3]:
+                    raise ValueError(f"{name} must be float32 {tuple(k.shape[:3])}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.page_size = int(k.shape[0]), int(k.shape[2])
+        self.struct = _PagedCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if i8 else None,
+                                  v_scale.data_ptr() if i8 else None, self.n_pages, self.page_size,
+                                  KV_I8 if i8 else KV_SAME)
+        self.ref = ctypes.byref(self.struct)
+
+
+def paged_cache(cfg: ModelCfg, n_pages: int, page_size: int, store: int = KV_SAME, device=None) -> PagedCache:
+    """A pool of n_pages zeroed pages of page_size tokens."""
+    shape = (int(n_pages), cfg.n_kv_heads, int(page_size), cfg.head_dim)
+    dtype = torch.int8 if store == KV_I8 else TORCH_DTYPE[cfg.dtype]
+    kv = [torch.zeros(shape, dtype=dtype, device=device or "cuda") for _ in range(2)]
+    scales = [torch.zeros(shape[:3], dtype=torch.float32, device=device or "cuda") for _ in range(2)] if store == KV_I8 else []
+    return PagedCache(cfg, *kv, *scales)
+
+
+class PagedBatch:
+    """The sequences of a call over a paged cache (adadsf_paged_batch): int32
+    device tensors starts (B + 1,), lens (B,) and table (B, max_pages), whose
+    contents may change between calls; n_rows packed rows, at most max_new of
+    one sequence."""
+
+    def __init__(self, starts: torch.Tensor, lens: torch.Tensor, table: torch.Tensor, n_rows: int, max_new: int):
+        B = lens.numel()
+        for name, t, shape in (("starts", starts, (B + 1,)), ("lens", lens, (B,)), ("table", table, (B, table.shape[-1]))):
+            _dev(t, name)
+            if t.dtype != torch.int32 or tuple(t.shape) != shape:
+                raise ValueError(f"{name} must be int32 {shape}")
+        self.starts, self.lens, self.table = starts, lens, table
+        self.n_rows, self.max_new = int(n_rows), int(max_new)
+        self.struct = _PagedBatch(starts.data_ptr(), lens.data_ptr(), table.data_ptr(), self.n_rows, B, self.max_new,
+                                  int(table.shape[1]))
+        self.ref = ctypes.byref(self.struct)
+
+
+def _rows(t: torch.Tensor, name: str, n_rows: int, cols: int, dtype: torch.dtype):
+    _dev(t, name)
+    if t.dtype != dtype or t.numel() != n_rows * cols:
+        raise ValueError(f"{name} must be {n_rows} rows of {cols} of {dtype}")
+
+
+def adadsf_rope_table(cfg: ModelCfg, n_pos: int, device=None, stream=None) -> torch.Tensor:
+    """(cos, sin) of positions 0 .. n_pos - 1: fp32 (n_pos, rotary_dim / 2, 2)."""
+    tab = torch.empty(int(n_pos), cfg.rotary_dim // 2, 2, dtype=torch.float32, device=device or "cuda")
+    _check(lib().adadsf_rope_table(ctypes.byref(cfg), int(n_pos), tab.data_ptr(), _s(stream)))
+    return tab
+
+
+def adadsf_paged_append(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, qkv: torch.Tensor,
+                        tab: Optional[torch.Tensor], pos: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Rotates the batch's rows of qkv (n_rows, q + 2 kv), writes keys and
+    values to their pages and the rotated queries to q_out."""
+    n, q, kv = batch.n_rows, cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+    _rows(qkv, "qkv", n, q + 2 * kv, TORCH_DTYPE[cfg.dtype])
+    if pos is not None:
+        _rows(pos, "pos", n, 1, torch.int32)
+    if q_out is not None:
+        _rows(q_out, "q_out", n, q, TORCH_DTYPE[cfg.dtype])
+    if tab is not None:
+        _rows(tab, "tab", tab.shape[0], cfg.rotary_dim, torch.float32)
+    if ws is None:
+        ws = workspace(256, qkv.device)
+    _check(lib().adadsf_paged_append(ctypes.byref(cfg), cache.ref, batch.ref, qkv.data_ptr(),
+                                     None if tab is None else tab.data_ptr(), 0 if tab is None else tab.shape[0],
+                                     None if pos is None else pos.data_ptr(),
+                                     None if q_out is None else q_out.data_ptr(), ws.data_ptr(), ws.numel(), _s(stream)))
+
+
+def adadsf_paged_read(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, k_out: torch.Tensor, v_out: torch.Tensor,
+                      ws: Optional[torch.Tensor] = None, stream=None):
+    """Reads the batch's cached tokens back as rows (n_rows, kv)."""
+    kv = cfg.n_kv_heads * cfg.head_dim
+    _rows(k_out, "k_out", batch.n_rows, kv, TORCH_DTYPE[cfg.dtype])
+    _rows(v_out, "v_out", batch.n_rows, kv, TORCH_DTYPE[cfg.dtype])
+    if ws is None:
+        ws = workspace(256, k_out.device)
+    _check(lib().adadsf_paged_read(ctypes.byref(cfg), cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(),
+                                   ws.data_ptr(), ws.numel(), _s(stream)))
+
+
+def adadsf_paged_attention_workspace_size(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch) -> int:
+    n = lib().adadsf_paged_attention_workspace_size(ctypes.byref(cfg), cache.ref, batch.ref)
+    if n == 0:
+        raise AdadsfError(ERR_INVALID_ARG, adadsf_last_error())
+    return n
+
+
+def adadsf_paged_attention(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, q: torch.Tensor, out: torch.Tensor,
+                           ws: Optional[torch.Tensor] = None, stream=None):
+    """Causal attention of the batch's rows over their pages. q: (n_rows, q)
+    with unit stride along a row (a slice of a wider matrix will do)."""
+    n, width = batch.n_rows, cfg.n_heads * cfg.head_dim
+    if not q.is_cuda or q.dtype != TORCH_DTYPE[cfg.dtype] or tuple(q.shape) != (n, width) or (n and q.stride(1) != 1):
+        raise ValueError(f"q must be a CUDA tensor ({n}, {width}) of {TORCH_DTYPE[cfg.dtype]} with unit stride along a row")
+    _rows(out, "out", n, width, TORCH_DTYPE[cfg.dtype])
+    if ws is None:
+        ws = workspace(adadsf_paged_attention_workspace_size(cfg, cache, batch), q.device)
+    _check(lib().adadsf_paged_attention(ctypes.byref(cfg), cache.ref, batch.ref, q.data_ptr(),
+                                        q.stride(0) if n > 1 else width, out.data_ptr(), ws.data_ptr(), ws.numel(),
+                                        _s(stream)))
+
+
+def adadsf_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor,
+                  temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                  top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                  logprob: Optional[torch.Tensor] = None, stream=None):
+    """The next token (int32) of each row of logits (B, V) from the random
+    numbers u (B,); every setting is a (B,) tensor or None."""
+    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in DTYPE_CODE or (logits.numel() and logits.stride(1) != 1):
+        raise ValueError("logits must be a CUDA tensor (B, V) of float32 or bfloat16 with unit stride along a row")
+    B, V = logits.shape
+    ptr = []
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("u", u, torch.float32),
+                           ("token", token, torch.int32), ("logprob", logprob, torch.float32)):
+        if t is None:
+            ptr.append(None)
+            continue
+        _rows(t, name, B, 1, dtype)
+        ptr.append(t.data_ptr())
+    _check(lib().adadsf_sample(logits.data_ptr(), logits.stride(0) if B > 1 else V, B, V, DTYPE_CODE[logits.dtype], *ptr,
+                               _s(stream)))
 
 
 def adadsf_sync_check(ws: torch.Tensor, stream=None) -> int:

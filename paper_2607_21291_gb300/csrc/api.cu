@@ -1584,6 +1584,163 @@ adadsf_status adadsf_decode_step(const adadsf_model_cfg* cfg, const adadsf_model
   return ADADSF_OK;
 }
 
+// ---------------------------------------------------------------- serving from a paged cache
+static adadsf_status paged_view(const adadsf_model_cfg* cfg, const adadsf_paged_cache* c, const adadsf_paged_batch* b,
+                                bool pointers, Paged* p) {
+  TRY(check_cfg(cfg));
+  if (!c || !b) return fail(ADADSF_ERR_INVALID_ARG, "cache or batch is NULL");
+  if (c->store != ADADSF_KV_SAME && c->store != ADADSF_KV_I8)
+    return fail(ADADSF_ERR_INVALID_ARG, "store %d is neither ADADSF_KV_SAME nor ADADSF_KV_I8", c->store);
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128)
+    return fail(ADADSF_ERR_UNSUPPORTED, "page_size=%d must be 16, 32, 64 or 128", c->page_size);
+  if (c->n_pages <= 0) return fail(ADADSF_ERR_INVALID_ARG, "n_pages=%d must be positive", c->n_pages);
+  if ((int64_t)c->n_pages * cfg->n_kv_heads > INT32_MAX)
+    return fail(ADADSF_ERR_UNSUPPORTED, "n_pages * n_kv_heads exceeds 2^31 - 1");
+  if (b->B < 0 || b->n_rows < 0 || b->max_new < 0 || b->max_pages <= 0)
+    return fail(ADADSF_ERR_INVALID_ARG, "need B, n_rows, max_new >= 0 and max_pages > 0 (B=%d n_rows=%lld max_new=%d max_pages=%d)",
+                b->B, (long long)b->n_rows, b->max_new, b->max_pages);
+  if (b->n_rows > (int64_t)1 << 30) return fail(ADADSF_ERR_UNSUPPORTED, "n_rows exceeds 2^30");
+  if ((int64_t)b->max_pages * c->page_size > (int64_t)1 << 30)
+    return fail(ADADSF_ERR_UNSUPPORTED, "max_pages * page_size exceeds 2^30");
+  if (pointers && b->n_rows > 0) {
+    NEED_PTR(c->k, "cache k");
+    NEED_PTR(c->v, "cache v");
+    if (c->store == ADADSF_KV_I8) {
+      NEED_PTR(c->k_scale, "cache k_scale");
+      NEED_PTR(c->v_scale, "cache v_scale");
+    }
+    if (b->B == 0) return fail(ADADSF_ERR_INVALID_ARG, "n_rows=%lld rows of no sequence", (long long)b->n_rows);
+    if (!b->starts || !b->lens || !b->table) return fail(ADADSF_ERR_INVALID_ARG, "batch starts, lens or table is NULL");
+    if ((reinterpret_cast<uintptr_t>(b->starts) | reinterpret_cast<uintptr_t>(b->lens) |
+         reinterpret_cast<uintptr_t>(b->table)) & 3u)
+      return fail(ADADSF_ERR_INVALID_ARG, "batch starts, lens or table misaligned");
+  }
+  *p = Paged{};
+  p->k = c->k; p->v = c->v;
+  p->ks = c->k_scale; p->vs = c->v_scale;
+  p->n_pages = c->n_pages;
+  p->page_log2 = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
+  p->i8 = c->store == ADADSF_KV_I8;
+  p->starts = b->starts; p->lens = b->lens; p->table = b->table;
+  p->n_rows = b->n_rows;
+  p->B = b->B; p->max_new = b->max_new; p->max_pages = b->max_pages;
+  p->Hq = cfg->n_heads; p->Hkv = cfg->n_kv_heads; p->hd = cfg->head_dim;
+  return ADADSF_OK;
+}
+
+adadsf_status adadsf_rope_table(const adadsf_model_cfg* cfg, int n_pos, float* tab_dev, void* stream) {
+  TRY(check_cfg(cfg));
+  if (n_pos < 0 || n_pos > 1 << 24) return fail(ADADSF_ERR_INVALID_ARG, "n_pos=%d out of range", n_pos);
+  if (n_pos == 0 || cfg->rotary_dim == 0) return ADADSF_OK;
+  NEED_PTR(tab_dev, "tab_dev");
+  Dev dev;
+  TRY(device_info(&dev, stream, nullptr));
+  return launch(dev, ADADSF_KERNEL_ROPE_TABLE, false, 0, rope_bytes(cfg, n_pos),
+                CALL(rope_table(reinterpret_cast<float2*>(tab_dev), n_pos, cfg->rotary_dim, cfg->rope_theta, dev),
+                     "rotary table"));
+}
+
+adadsf_status adadsf_paged_append(const adadsf_model_cfg* cfg, const adadsf_paged_cache* cache,
+                                  const adadsf_paged_batch* batch, const void* qkv_dev, const float* tab_dev, int n_pos,
+                                  const int32_t* pos_dev, void* q_out_dev, void* ws, size_t ws_bytes, void* stream) {
+  Paged p;
+  TRY(paged_view(cfg, cache, batch, true, &p));
+  TRY(check_ws(ws, ws_bytes, kErrBytes));
+  if (p.n_rows == 0) return ADADSF_OK;
+  NEED_PTR(qkv_dev, "qkv_dev");
+  if (cfg->rotary_dim > 0) {
+    NEED_PTR(tab_dev, "tab_dev");
+    if (n_pos <= 0) return fail(ADADSF_ERR_INVALID_ARG, "n_pos=%d must be positive", n_pos);
+  }
+  if (pos_dev && (reinterpret_cast<uintptr_t>(pos_dev) & 3u)) return fail(ADADSF_ERR_INVALID_ARG, "pos_dev misaligned");
+  if (q_out_dev && !aligned16(q_out_dev)) return fail(ADADSF_ERR_INVALID_ARG, "q_out_dev is not 16-byte aligned");
+  Dev dev;
+  TRY(device_info(&dev, stream, ws));
+  const double es = elem_size(cfg->dtype), kv = 2.0 * p.Hkv * p.hd, q = q_out_dev ? (double)p.Hq * p.hd : 0.0;
+  return launch(dev, ADADSF_KERNEL_PAGED_APPEND, false, 0,
+                p.n_rows * ((2.0 * q + kv) * es + (p.i8 ? kv + 8.0 * p.Hkv : kv * es)),
+                CALL(paged_append(cfg->dtype, p, qkv_dev, reinterpret_cast<const float2*>(tab_dev), cfg->rotary_dim / 2,
+                                  n_pos, pos_dev, q_out_dev, dev),
+                     "paged append"));
+}
+
+adadsf_status adadsf_paged_read(const adadsf_model_cfg* cfg, const adadsf_paged_cache* cache,
+                                const adadsf_paged_batch* batch, void* k_out_dev, void* v_out_dev, void* ws,
+                                size_t ws_bytes, void* stream) {
+  Paged p;
+  TRY(paged_view(cfg, cache, batch, true, &p));
+  TRY(check_ws(ws, ws_bytes, kErrBytes));
+  if (p.n_rows == 0) return ADADSF_OK;
+  NEED_PTR(k_out_dev, "k_out_dev");
+  NEED_PTR(v_out_dev, "v_out_dev");
+  Dev dev;
+  TRY(device_info(&dev, stream, ws));
+  const double es = elem_size(cfg->dtype), kv = 2.0 * p.Hkv * p.hd;
+  return launch(dev, ADADSF_KERNEL_PAGED_READ, false, 0,
+                p.n_rows * (kv * es + (p.i8 ? kv + 8.0 * p.Hkv : kv * es)),
+                CALL(paged_read(cfg->dtype, p, k_out_dev, v_out_dev, dev), "paged read"));
+}
+
+size_t adadsf_paged_attention_workspace_size(const adadsf_model_cfg* cfg, const adadsf_paged_cache* cache,
+                                             const adadsf_paged_batch* batch) {
+  Paged p;
+  if (paged_view(cfg, cache, batch, false, &p) != ADADSF_OK) return 0;
+  return kErrBytes + kSyncBytes + align256(paged_attention_scratch(cfg->dtype, p));
+}
+
+adadsf_status adadsf_paged_attention(const adadsf_model_cfg* cfg, const adadsf_paged_cache* cache,
+                                     const adadsf_paged_batch* batch, const void* q_dev, int64_t ld_q, void* out_dev,
+                                     void* ws, size_t ws_bytes, void* stream) {
+  Paged p;
+  TRY(paged_view(cfg, cache, batch, true, &p));
+  const int q = p.Hq * p.hd, vec = cfg->dtype == ADADSF_BF16 ? 8 : 4;
+  if (ld_q < q || ld_q % vec)
+    return fail(ADADSF_ERR_INVALID_ARG, "ld_q=%lld must be a multiple of %d and at least %d", (long long)ld_q, vec, q);
+  TRY(check_ws(ws, ws_bytes, adadsf_paged_attention_workspace_size(cfg, cache, batch)));
+  if (p.n_rows == 0) return ADADSF_OK;
+  NEED_PTR(q_dev, "q_dev");
+  NEED_PTR(out_dev, "out_dev");
+  Dev dev;
+  TRY(device_info(&dev, stream, ws));
+  // the counts live on the device: work is what the host can bound it by
+  const double es = elem_size(cfg->dtype), span = (double)p.max_pages * cache->page_size;
+  return launch(dev, ADADSF_KERNEL_PAGED_ATTENTION, false, 4.0 * p.n_rows * q * span,
+                2.0 * p.n_rows * q * es + p.B * span * 2.0 * p.Hkv * (p.i8 ? p.hd + 4.0 : p.hd * es),
+                CALL(paged_attention(cfg->dtype, p, q_dev, ld_q, out_dev, at<int>(ws, kErrBytes),
+                                     at<char>(ws, kErrBytes + kSyncBytes), dev),
+                     "paged attention"));
+}
+
+adadsf_status adadsf_sample(const void* logits_dev, int64_t ld_logits, int B, int V, int dtype,
+                            const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev,
+                            const float* min_p_dev, const float* u_dev, int32_t* token_dev, float* logprob_dev,
+                            void* stream) {
+  if (dtype != ADADSF_F32 && dtype != ADADSF_BF16) return fail(ADADSF_ERR_INVALID_ARG, "dtype %d unknown", dtype);
+  if (B < 0 || V <= 0 || ld_logits < V)
+    return fail(ADADSF_ERR_INVALID_ARG, "need B >= 0, V > 0 and ld_logits >= V (B=%d V=%d ld_logits=%lld)", B, V,
+                (long long)ld_logits);
+  if (V > kSampleMaxV) return fail(ADADSF_ERR_UNSUPPORTED, "V=%d exceeds %d", V, kSampleMaxV);
+  if (B > 1 << 24) return fail(ADADSF_ERR_UNSUPPORTED, "B=%d exceeds 2^24", B);
+  if (B == 0) return ADADSF_OK;
+  if (!logits_dev || (reinterpret_cast<uintptr_t>(logits_dev) & (elem_size(dtype) - 1)))
+    return fail(ADADSF_ERR_INVALID_ARG, "logits_dev is NULL or misaligned");
+  if (!u_dev || !token_dev) return fail(ADADSF_ERR_INVALID_ARG, "u_dev or token_dev is NULL");
+  if ((reinterpret_cast<uintptr_t>(temperature_dev) | reinterpret_cast<uintptr_t>(top_k_dev) |
+       reinterpret_cast<uintptr_t>(top_p_dev) | reinterpret_cast<uintptr_t>(min_p_dev) |
+       reinterpret_cast<uintptr_t>(u_dev) | reinterpret_cast<uintptr_t>(token_dev) |
+       reinterpret_cast<uintptr_t>(logprob_dev)) & 3u)
+    return fail(ADADSF_ERR_INVALID_ARG, "a row's settings or outputs are misaligned");
+  Dev dev;
+  TRY(device_info(&dev, stream, nullptr));
+  Sample a;
+  a.logits = logits_dev; a.ld = ld_logits;
+  a.B = B; a.V = V;
+  a.temperature = temperature_dev; a.top_k = top_k_dev; a.top_p = top_p_dev; a.min_p = min_p_dev; a.u = u_dev;
+  a.token = token_dev; a.logprob = logprob_dev;
+  return launch(dev, ADADSF_KERNEL_SAMPLE, false, 0, (double)B * V * elem_size(dtype),
+                CALL(sample(dtype, a, dev), "sampling"));
+}
+
 adadsf_status adadsf_sync_check(void* ws, size_t ws_bytes, void* stream) {
   TRY(check_ws(ws, ws_bytes, kErrBytes));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -1651,7 +1808,8 @@ const char* adadsf_kernel_name(int kind) {
   static const char* names[ADADSF_KERNEL_COUNT] = {
       "embed", "router", "topk", "positions", "gather_norm", "gemm_qkv", "rope_table", "rope",
       "attention", "gemm_o", "norm2", "gemm_up", "gemm_down", "stats", "final_norm", "copy",
-      "linear", "selftest", "gemm_qkv_up", "gemm_o_down", "topk_gather_norm", "decide", "kv_cache", "align"};
+      "linear", "selftest", "gemm_qkv_up", "gemm_o_down", "topk_gather_norm", "decide", "kv_cache", "align",
+      "paged_append", "paged_read", "paged_attention", "sample"};
   return (kind >= 0 && kind < ADADSF_KERNEL_COUNT) ? names[kind] : "unknown";
 }
 

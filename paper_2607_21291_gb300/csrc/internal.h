@@ -269,4 +269,35 @@ struct DecodeAttn {
 cudaError_t decode_attention(int dtype, const DecodeAttn& a, const Dev& dev);
 cudaError_t decode_advance(int32_t* hdr, const Dev& dev);
 
+// A paged cache and a batch over it (adadsf_paged_cache, adadsf_paged_batch).
+struct Paged {
+  void *k, *v;
+  float *ks, *vs;                        // i8 only
+  int n_pages, page_log2;
+  bool i8;
+  const int32_t *starts, *lens, *table;
+  int64_t n_rows;
+  int B, max_new, max_pages;
+  int Hq, Hkv, hd;
+};
+// paged_cache.cu
+cudaError_t paged_append(int dtype, const Paged& p, const void* qkv, const float2* tab, int half, int n_pos,
+                         const int32_t* pos, void* q_out, const Dev& dev);
+cudaError_t paged_read(int dtype, const Paged& p, void* k_out, void* v_out, const Dev& dev);
+// paged_attention.cu
+// scratch: paged_attention_scratch bytes; sync: the workspace's synchronisation area.
+size_t paged_attention_scratch(int dtype, const Paged& p);
+cudaError_t paged_attention(int dtype, const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch,
+                            const Dev& dev);
+// sample.cu
+struct Sample {
+  const void* logits; int64_t ld;
+  int B, V;
+  const float* temperature; const int32_t* top_k; const float *top_p, *min_p, *u;   // all but u may be null
+  int32_t* token;
+  float* logprob;                        // or null
+};
+constexpr int kSampleMaxV = 397312;
+cudaError_t sample(int dtype, const Sample& a, const Dev& dev);
+
 }  // namespace adadsf

@@ -1,0 +1,334 @@
+// The next token of a row of logits by temperature, top-k, top-p, min-p and a given
+// random number (adadsf_sample).
+//
+// A cluster of CTAs holds one row in shared memory as ordered 32-bit keys (larger
+// key = larger logit), each CTA a contiguous slice, each thread a contiguous chunk of
+// it (an odd number of words, so that a warp's chunks spread over the banks), so logits
+// are read from memory once. Kept tokens are a prefix of the descending order, so a
+// cut (key, number of equal ones kept) describes them. Cuts come from a radix
+// search over 11, 11 and 10 bits: a histogram per CTA, of counts (top-k) or of
+// weights (top-p), every CTA then adds up all of them through distributed shared
+// memory and finds the same bin. Weights are whole multiples of 2^-40 of the
+// largest, so their sums do not depend on order, and neither does the token.
+#include <math.h>
+
+#include "common.cuh"
+
+namespace adadsf {
+namespace {
+
+constexpr int kSmThreads = 512;
+constexpr int kSmWarps = kSmThreads / 32;
+constexpr int kSmBins = 2048;
+constexpr int kSmMostChunk = 97;          // words of a thread: 8 x 512 x 97 tokens
+constexpr int kSmMostCluster = 8;
+constexpr int kSmSmem = kSmThreads * kSmMostChunk * 4;
+static_assert(kSmMostCluster * kSmThreads * kSmMostChunk == kSampleMaxV, "the limit that the header states");
+constexpr uint32_t kSmNone = 0x007fffffu; // key of -infinity; padding lies below it
+constexpr float kSmUnit = 1099511627776.f;   // 2^40
+
+typedef unsigned long long u64;
+
+__device__ __forceinline__ uint32_t key_of(float x) {
+  uint32_t u = __float_as_uint(x);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return kSmNone;   // NaN: never drawn
+  if (u == 0x80000000u) u = 0;                           // -0 equals 0
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
+}
+__device__ __forceinline__ uint4 ld_cluster_u32x4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(addr)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ u64 ld_cluster_u64(uint32_t addr) {
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+struct SampleShared {
+  uint32_t lo[kSmBins], hi[kSmBins];   // histogram: counts in lo, or weights in (lo, hi)
+  u64 warp[kSmWarps];                  // block scan
+  u64 total;                           // this CTA's total, read by the cluster
+  u64 found_before, found_in, found_all;
+  uint32_t found_bin;
+  uint32_t most;                       // this CTA's largest key, read by the cluster
+  uint32_t index;                      // written by the CTA that finds it
+};
+
+// Sum of v over the block's threads before this one; *all: over all of them.
+__device__ __forceinline__ u64 block_before(u64 v, SampleShared& s, u64* all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u64 inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const u64 up = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += up;
+  }
+  __syncthreads();   // the last call's sums are read
+  if (lane == 31) s.warp[warp] = inc;
+  __syncthreads();
+  u64 base = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < kSmWarps; ++w) {
+    const u64 t = s.warp[w];
+    base += w < warp ? t : 0;
+    sum += t;
+  }
+  *all = sum;
+  return base + inc - v;
+}
+
+// The same over the cluster's threads, CTAs in order of their slices.
+__device__ __forceinline__ u64 cluster_before(u64 v, SampleShared& s, u64* all) {
+  u64 mine;
+  u64 before = block_before(v, s, &mine);
+  const uint32_t n = cluster_nctarank(), rank = cluster_ctarank();
+  if (threadIdx.x == 0) s.total = mine;
+  cluster_sync();
+  u64 sum = 0;
+  for (uint32_t c = 0; c < n; ++c) {
+    const u64 t = ld_cluster_u64(map_to_cta(smem_u32(&s.total), c));
+    if (c < rank) before += t;
+    sum += t;
+  }
+  cluster_sync();   // read by all: the next call may write
+  *all = sum;
+  return before;
+}
+
+// Adds up the cluster's histograms, whose bins run from the largest keys down, and finds the
+// first bin that takes the running sum, from `base` on, to `target` or more. frac < 1: the
+// target is frac times the sum of all bins (at least 1). Results in s.found_*.
+template <bool WEIGHTS>
+__device__ __forceinline__ void find_bin(SampleShared& s, u64 base, double target, double frac) {
+  const uint32_t n = cluster_nctarank();
+  cluster_sync();   // every CTA's histogram is complete
+  const int b0 = 4 * threadIdx.x;
+  u64 v[4] = {0, 0, 0, 0};
+  for (uint32_t c = 0; c < n; ++c) {
+    const uint4 lo = ld_cluster_u32x4(map_to_cta(smem_u32(s.lo + b0), c));
+    v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+    if (WEIGHTS) {
+      const uint4 hi = ld_cluster_u32x4(map_to_cta(smem_u32(s.hi + b0), c));
+      v[0] += (u64)hi.x << 32; v[1] += (u64)hi.y << 32; v[2] += (u64)hi.z << 32; v[3] += (u64)hi.w << 32;
+    }
+  }
+  u64 all;
+  u64 run = base + block_before(v[0] + v[1] + v[2] + v[3], s, &all);
+  if (frac < 1.0) target = fmax(frac * (double)all, 1.0);
+  if (threadIdx.x == 0) s.found_all = all;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((double)run < target && (double)(run + v[i]) >= target) {
+      s.found_bin = b0 + i;
+      s.found_before = run;
+      s.found_in = v[i];
+    }
+    run += v[i];
+  }
+  cluster_sync();   // histograms are read, and the results of this CTA visible
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, int chunk) {
+  extern __shared__ __align__(16) uint32_t keys[];   // [kSmThreads][chunk]
+  __shared__ __align__(16) SampleShared s;
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x, lane = tid & 31;
+  const uint32_t n_cta = cluster_nctarank(), rank = cluster_ctarank();
+  const int row = blockIdx.x / n_cta;
+  const int slice = kSmThreads * chunk, i0 = (int)rank * slice;
+  const T* x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+  uint32_t most = 0;
+  for (int i = tid; i < slice; i += kSmThreads) {
+    const uint32_t k = i0 + i < a.V ? key_of(Elem<T>::to_f(x[i0 + i])) : 0u;
+    keys[i] = k;
+    most = max(most, k);
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (lane == 0) s.warp[tid >> 5] = most;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 0; w < kSmWarps; ++w) most = max(most, (uint32_t)s.warp[w]);
+    s.most = most;
+    s.index = 0xffffffffu;
+  }
+  cluster_sync();
+  for (uint32_t c = 0; c < n_cta; ++c) most = max(most, ld_cluster_u32(map_to_cta(smem_u32(&s.most), c)));
+
+  const uint32_t* own = keys + tid * chunk;
+  const int own0 = i0 + tid * chunk;
+  const float t = a.temperature ? a.temperature[row] : 1.f;
+  const float inv = 1.f / t, top = value_of(most);
+  auto logit_of = [&](uint32_t k) { return k == most ? 0.f : __fmul_rn(__fsub_rn(value_of(k), top), inv); };
+  auto chance = [&](uint32_t k) -> float {   // exp(z), 0 for what is never drawn
+    if (k <= kSmNone) return 0.f;
+    const float w = expf(logit_of(k));
+    return w >= 0.f ? w : 0.f;               // NaN (an infinite logit under an infinite temperature)
+  };
+  auto weight = [&](float w) { return __float2ull_rn(w * kSmUnit); };
+  // index of the n-th (from 1) key equal to k in the order of the vocabulary, in every CTA
+  auto nth = [&](uint32_t k, u64 n) -> uint32_t {
+    int c = 0;
+    for (int i = 0; i < chunk; ++i) c += own[i] == k;
+    u64 all;
+    u64 before = cluster_before((u64)c, s, &all);
+    if (before < n && n <= before + c) {
+      int i = -1;
+      while (before < n) before += own[++i] == k;
+      for (uint32_t q = 0; q < n_cta; ++q) st_cluster_u32(map_to_cta(smem_u32(&s.index), q), (uint32_t)(own0 + i));
+    }
+    cluster_sync();
+    return s.index;
+  };
+
+  if (most <= kSmNone) {   // nothing to draw
+    cluster_sync();        // no CTA leaves while another reads its shared memory
+    if (rank == 0 && tid == 0) {
+      a.token[row] = -1;
+      if (a.logprob) a.logprob[row] = -INFINITY;
+    }
+    return;
+  }
+  if (!(t > 0.f)) {
+    const uint32_t i = nth(most, 1);
+    if (rank == 0 && tid == 0) {
+      a.token[row] = (int32_t)i;
+      if (a.logprob) a.logprob[row] = 0.f;
+    }
+    return;
+  }
+
+  // ---- the cut: keys above cut_key, and the first cut_ties of those equal to it
+  uint32_t cut_key = 0;
+  u64 cut_ties = ~0ull;       // ~0: all
+  bool some_ties = false;     // fewer than there are
+  const int shifts[3] = {21, 10, 0}, masks[3] = {0x7ff, 0x7ff, 0x3ff};
+  const int k = a.top_k ? a.top_k[row] : 0;
+  if (k > 0 && k < a.V) {
+    uint32_t prefix = 0;
+    u64 above = 0;
+    for (int lv = 0; lv < 3; ++lv) {
+      for (int i = tid; i < kSmBins; i += kSmThreads) s.lo[i] = 0;
+      __syncthreads();
+      for (int i = 0; i < chunk; ++i) {
+        const uint32_t key = own[i];
+        if (lv == 0 || (key >> shifts[lv - 1]) == prefix)
+          atomicAdd(&s.lo[kSmBins - 1 - ((key >> shifts[lv]) & masks[lv])], 1u);
+      }
+      find_bin<false>(s, above, (double)k, 1.0);
+      prefix = (prefix << (lv == 2 ? 10 : 11)) | (kSmBins - 1 - s.found_bin);
+      above = s.found_before;
+      cut_ties = (u64)k - above;
+      some_ties = cut_ties < s.found_in;
+    }
+    cut_key = prefix;
+  }
+  const float top_p = a.top_p ? a.top_p[row] : 1.f;
+  if (top_p < 1.f) {
+    const uint32_t k_key = cut_key;
+    const u64 k_ties = cut_ties;
+    uint32_t prefix = 0;
+    double target = 0.0;
+    u64 before = 0;
+    for (int lv = 0; lv < 3; ++lv) {
+      for (int i = tid; i < kSmBins; i += kSmThreads) s.lo[i] = s.hi[i] = 0;
+      __syncthreads();
+      auto add = [&](uint32_t key, u64 w) {
+        const int bin = kSmBins - 1 - ((key >> shifts[lv]) & masks[lv]);
+        const uint32_t lo = (uint32_t)w;
+        uint32_t hi = (uint32_t)(w >> 32);
+        if (lo) hi += atomicAdd(&s.lo[bin], lo) > 0xffffffffu - lo;   // the carry
+        if (hi) atomicAdd(&s.hi[bin], hi);
+      };
+      auto at_level = [&](uint32_t key) { return lv == 0 || (key >> shifts[lv - 1]) == prefix; };
+      for (int i = 0; i < chunk; ++i) {
+        const uint32_t key = own[i];
+        if (at_level(key) && (key > k_key || (key == k_key && k_ties == ~0ull))) add(key, weight(chance(key)));
+      }
+      // the kept ones among the equals of top-k's last
+      if (rank == 0 && tid == 0 && k_ties != ~0ull && at_level(k_key)) add(k_key, k_ties * weight(chance(k_key)));
+      find_bin<true>(s, before, target, lv == 0 ? (double)top_p : 1.0);
+      if (lv == 0) target = fmax((double)top_p * (double)s.found_all, 1.0);
+      prefix = (prefix << (lv == 2 ? 10 : 11)) | (kSmBins - 1 - s.found_bin);
+      before = s.found_before;
+    }
+    const u64 one = weight(chance(prefix));
+    if (one > 0) {
+      // the fewest equals whose weight takes the sum to the target
+      u64 n = (u64)fmax(ceil((target - (double)before) / (double)one), 1.0);
+      while (n > 1 && (double)(before + (n - 1) * one) >= target) --n;
+      while ((double)(before + n * one) < target) ++n;
+      const u64 there = s.found_in / one;
+      if (n < there || prefix != k_key) some_ties = n < there;
+      cut_key = prefix;
+      cut_ties = n < there ? n : there;
+      if (!some_ties) cut_ties = ~0ull;
+    }
+  }
+  uint32_t last = 0xffffffffu;   // equals of cut_key are kept up to this index
+  if (some_ties) last = nth(cut_key, cut_ties);
+
+  // ---- the draw
+  const float floor_p = a.min_p ? a.min_p[row] : 0.f;
+  const float min_p = floor_p > 0.f ? fminf(floor_p, 1.f) : 0.f;
+  auto kept = [&](int i) -> u64 {
+    const uint32_t key = own[i];
+    if (key < cut_key || (key == cut_key && (uint32_t)(own0 + i) > last)) return 0;
+    const float w = chance(key);
+    return w < min_p ? 0 : weight(w);
+  };
+  u64 sum = 0, all;
+  for (int i = 0; i < chunk; ++i) sum += kept(i);
+  u64 before = cluster_before(sum, s, &all);
+  const double mark_d = (double)a.u[row] * (double)all;
+  u64 mark = mark_d > 0.0 ? (u64)mark_d : 0;
+  if (mark > all - 1) mark = all - 1;
+  if (before <= mark && mark < before + sum) {
+    int i = 0;
+    for (;; ++i) {
+      before += kept(i);
+      if (before > mark) break;
+    }
+    a.token[row] = own0 + i;
+    if (a.logprob) {
+      const float rest = (float)((double)(all - (u64)kSmUnit) / (double)kSmUnit);
+      a.logprob[row] = logit_of(own[i]) - log1pf(rest);
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t sample(int dtype, const Sample& a, const Dev& dev) {
+  const int n_cta = a.V > 4096 ? kSmMostCluster : 1;
+  int chunk = (a.V + n_cta * kSmThreads - 1) / (n_cta * kSmThreads);
+  chunk |= 1;
+  if (chunk > kSmMostChunk || (int64_t)a.B * n_cta > INT32_MAX) return cudaErrorInvalidValue;
+  auto run = [&](auto t) -> cudaError_t {
+    using T = decltype(t);
+    const cudaError_t e = allow_smem<sample_kernel<T>, kSmSmem>();
+    if (e != cudaSuccess) return e;
+    return launch_pdl_cluster(sample_kernel<T>, dim3((unsigned)(a.B * n_cta)), dim3(kSmThreads),
+                              (size_t)kSmThreads * chunk * 4, dev.stream, n_cta, a, chunk);
+  };
+  return dtype == kBF16 ? run(bf16()) : run(0.f);
+}
+
+}  // namespace adadsf
