@@ -1397,6 +1397,20 @@ bool make_tmap_bf16_k(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t c
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tmap_pages(CUtensorMap* m, const void* pool, const Paged& p, bool i8, uint32_t box_rows) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t es = i8 ? 1 : 2, page = (cuuint64_t)1 << p.page_log2;
+  cuuint64_t dims[3] = {(cuuint64_t)p.hd, page, (cuuint64_t)p.n_pages * p.Hkv};
+  cuuint64_t strides[2] = {p.hd * es, page * p.hd * es};
+  cuuint32_t box[3] = {(cuuint32_t)(i8 ? p.hd : 64), (cuuint32_t)std::min<cuuint64_t>(page, box_rows), 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, i8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(pool), dims,
+            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            box[0] * es == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace {
 
 bool make_tmap(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint64_t ld,

@@ -280,6 +280,9 @@ struct Paged {
   int B, max_new, max_pages;
   int Hq, Hkv, hd;
 };
+// Tensor map of a pool of pages as [n_pages Hkv][page][hd]: boxes of min(page, box_rows)
+// rows of 64 features (bf16, 128-byte swizzle) or a whole head (8-bit, 128- or 64-byte swizzle).
+bool make_tmap_pages(CUtensorMap* m, const void* pool, const Paged& p, bool i8, uint32_t box_rows);
 // paged_cache.cu
 cudaError_t paged_append(int dtype, const Paged& p, const void* qkv, const float2* tab, int half, int n_pos,
                          const int32_t* pos, void* q_out, const Dev& dev);
@@ -289,6 +292,9 @@ cudaError_t paged_read(int dtype, const Paged& p, void* k_out, void* v_out, cons
 size_t paged_attention_scratch(int dtype, const Paged& p);
 cudaError_t paged_attention(int dtype, const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch,
                             const Dev& dev);
+// paged_rows.cu -- bf16, few new tokens a sequence: 16 packed rows a tile.
+size_t paged_rows_scratch(const Paged& p);
+cudaError_t paged_rows(const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch, const Dev& dev);
 // sample.cu
 struct Sample {
   const void* logits; int64_t ld;

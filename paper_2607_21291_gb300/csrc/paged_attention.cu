@@ -10,6 +10,7 @@ namespace adadsf {
 namespace {
 
 constexpr int kPaThreads = 128;
+constexpr int kPaFewRows = 64;   // packed rows of a sequence up to which paged_rows.cu runs
 
 template <typename T, int HD, bool I8>
 __global__ void __launch_bounds__(kPaThreads)
@@ -79,9 +80,12 @@ __global__ void __launch_bounds__(kPaThreads)
 
 }  // namespace
 
-size_t paged_attention_scratch(int, const Paged&) { return 0; }
+size_t paged_attention_scratch(int dtype, const Paged& p) { return dtype == kBF16 ? paged_rows_scratch(p) : 0; }
 
-cudaError_t paged_attention(int dtype, const Paged& p, const void* q, int64_t ld_q, void* out, int*, void*, const Dev& dev) {
+cudaError_t paged_attention(int dtype, const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch,
+                            const Dev& dev) {
+  if (dtype == kBF16 && (int64_t)p.max_new * (p.Hq / p.Hkv) <= kPaFewRows)
+    return paged_rows(p, q, ld_q, out, sync, scratch, dev);
   const int64_t blocks = (p.n_rows * p.Hq + kPaThreads / 32 - 1) / (kPaThreads / 32);
   if (blocks > INT32_MAX) return cudaErrorInvalidValue;
   auto run = [&](auto t, auto hd, auto i8) {
