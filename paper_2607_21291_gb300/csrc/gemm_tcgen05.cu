@@ -1411,6 +1411,19 @@ bool make_tmap_pages(CUtensorMap* m, const void* pool, const Paged& p, bool i8, 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tmap_heads(CUtensorMap* m, const void* q, const Paged& p, int64_t ld_q, int tokens) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t G = p.Hq / p.Hkv, hd = p.hd;
+  cuuint64_t dims[4] = {hd, G, (cuuint64_t)p.Hkv, (cuuint64_t)p.n_rows};
+  cuuint64_t strides[3] = {hd * 2, G * hd * 2, (cuuint64_t)ld_q * 2};
+  cuuint32_t box[4] = {64, (cuuint32_t)G, 1, (cuuint32_t)tokens};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(q), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace {
 
 bool make_tmap(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint64_t ld,

@@ -280,6 +280,8 @@ struct Paged {
   int B, max_new, max_pages;
   int Hq, Hkv, hd;
 };
+// Tensor map of query rows as [n_rows][Hkv][G][hd]: boxes of `tokens` rows of a group's 64 features.
+bool make_tmap_heads(CUtensorMap* m, const void* q, const Paged& p, int64_t ld_q, int tokens);
 // Tensor map of a pool of pages as [n_pages Hkv][page][hd]: boxes of min(page, box_rows)
 // rows of 64 features (bf16, 128-byte swizzle) or a whole head (8-bit, 128- or 64-byte swizzle).
 bool make_tmap_pages(CUtensorMap* m, const void* pool, const Paged& p, bool i8, uint32_t box_rows);
@@ -295,6 +297,10 @@ cudaError_t paged_attention(int dtype, const Paged& p, const void* q, int64_t ld
 // paged_rows.cu -- bf16, few new tokens a sequence: 16 packed rows a tile.
 size_t paged_rows_scratch(const Paged& p);
 cudaError_t paged_rows(const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch, const Dev& dev);
+// paged_tc.cu -- bf16, chunks of new tokens, on tcgen05 (at most 128 query heads a key/value head).
+bool paged_tc_takes(const Paged& p);
+size_t paged_tc_scratch(const Paged& p);
+cudaError_t paged_tc(const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch, const Dev& dev);
 // sample.cu
 struct Sample {
   const void* logits; int64_t ld;

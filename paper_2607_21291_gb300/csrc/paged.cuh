@@ -50,4 +50,109 @@ __device__ __forceinline__ int64_t paged_vec(const Paged& p, int page, int place
   return (((int64_t)page * p.Hkv + h) << p.page_log2) + (place & ((1 << p.page_log2) - 1));
 }
 
+// A line of tiles of keys, shared out in equal pieces. Sequence b's items run group of rows by
+// group of rows, key/value heads inside; an item has as many tiles as its last row sees keys,
+// at least one. CUT: rows of a group (`groups`, `tokens`) and keys of a tile (KEYS).
+// A warp keeps 32 sequences at a time, one a lane.
+struct PagedItem {
+  int b, h, grp, n, len, tiles, seen;  // seen: keys that its last row sees
+  int64_t row0, u0;                    // first packed row of the sequence, first tile on the line
+};
+template <class CUT>
+struct PagedLine {
+  CUT cut;
+  int64_t base, end;      // of this chunk of sequences on the line
+  int b0;
+  PagedSeq q;             // this lane's sequence
+  int64_t mine, at;       // its tiles, and their place on the line
+  int b, grp;             // the group that item() found last, and its place
+  int64_t x;
+
+  static __device__ __forceinline__ int tiles_of(int seen) { return seen <= CUT::KEYS ? 1 : (seen + CUT::KEYS - 1) / CUT::KEYS; }
+  // keys that the last row of group g sees
+  __device__ __forceinline__ int seen_of(int n, int len, int g) const { return max(0, len - n + min(n, cut.tokens(g))); }
+  __device__ __forceinline__ void load(const Paged& p, int b_first, int64_t from, int lane, int* err) {
+    b0 = b_first;
+    b = -1;
+    base = from;
+    q = PagedSeq{0, 0, 0};
+    mine = 0;
+    if (b0 + lane < p.B) {
+      q = paged_seq(p, b0 + lane, err);
+      const int groups = cut.groups(q.n);
+      for (int g = 0; g < groups; ++g) mine += tiles_of(seen_of(q.n, q.len, g));
+      mine *= p.Hkv;
+    }
+    int64_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += up;
+    }
+    at = base + inc - mine;
+    end = base + __shfl_sync(0xffffffffu, inc, 31);
+  }
+  // the line's length, and [first, last) of CTA `cta` of `ctas` in pieces of *per tiles, `least` or more
+  __device__ __forceinline__ void piece(const Paged& p, int least, int cta, int ctas, int lane, int* err, int64_t* per,
+                                        int64_t* first, int64_t* last) {
+    int64_t all = 0;
+    for (int c = 0; c < p.B; c += 32) {
+      load(p, c, all, lane, err);
+      all = end;
+    }
+    *per = max((int64_t)least, (all + ctas - 1) / ctas);
+    *first = min(all, cta * *per);
+    *last = min(all, *first + *per);
+    if (*first < base) load(p, 0, 0, lane, err);
+  }
+  // the item that holds tile u (below the line's length; calls with rising u)
+  __device__ __forceinline__ PagedItem item(const Paged& p, int64_t u, int lane, int* err) {
+    while (u >= end) load(p, b0 + 32, end, lane, err);
+    const int l = __ffs(__ballot_sync(0xffffffffu, u >= at && u < at + mine)) - 1;
+    PagedItem it;
+    it.b = b0 + l;
+    it.n = __shfl_sync(0xffffffffu, q.n, l);
+    it.len = __shfl_sync(0xffffffffu, q.len, l);
+    it.row0 = __shfl_sync(0xffffffffu, q.row0, l);
+    const int64_t from = __shfl_sync(0xffffffffu, at, l);
+    if (b != it.b) {
+      b = it.b;
+      grp = 0;
+      x = from;
+    }
+    for (;; ++grp) {
+      it.seen = seen_of(it.n, it.len, grp);
+      it.tiles = tiles_of(it.seen);
+      const int64_t all = (int64_t)it.tiles * p.Hkv;
+      if (u < x + all) break;
+      x += all;
+    }
+    it.grp = grp;
+    it.h = (int)((u - x) / it.tiles);
+    it.u0 = x + (int64_t)it.h * it.tiles;
+    return it;
+  }
+};
+
+// 2^x on the SFU (relative error about 2^-22, denormal results flushed).
+__device__ __forceinline__ float paged_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two 8-bit numbers (the low bytes of t's halves) as bf16, exactly: with b a number's low seven
+// bits and s its top one, (128 + b) - (s ? 256 : 128).
+__device__ __forceinline__ uint32_t bf16_of_i8(uint32_t t) {
+  const uint32_t b = (t & 0x007f007fu) | 0x43004300u, s = (t & 0x00800080u) | 0x43004300u;
+  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&b), *reinterpret_cast<const __nv_bfloat162*>(&s));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+      : "memory");
+}
+
 }  // namespace adadsf

@@ -2,6 +2,7 @@
 // splitting the head, walks the visible keys with an online softmax in fp32.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "paged.cuh"
@@ -80,12 +81,13 @@ __global__ void __launch_bounds__(kPaThreads)
 
 }  // namespace
 
-size_t paged_attention_scratch(int dtype, const Paged& p) { return dtype == kBF16 ? paged_rows_scratch(p) : 0; }
+size_t paged_attention_scratch(int dtype, const Paged& p) { return dtype == kBF16 ? std::max(paged_rows_scratch(p), paged_tc_scratch(p)) : 0; }
 
 cudaError_t paged_attention(int dtype, const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch,
                             const Dev& dev) {
   if (dtype == kBF16 && (int64_t)p.max_new * (p.Hq / p.Hkv) <= kPaFewRows)
     return paged_rows(p, q, ld_q, out, sync, scratch, dev);
+  if (dtype == kBF16 && paged_tc_takes(p)) return paged_tc(p, q, ld_q, out, sync, scratch, dev);
   const int64_t blocks = (p.n_rows * p.Hq + kPaThreads / 32 - 1) / (kPaThreads / 32);
   if (blocks > INT32_MAX) return cudaErrorInvalidValue;
   auto run = [&](auto t, auto hd, auto i8) {

@@ -13,9 +13,8 @@
 //   O (16 x hd) += P (16 x 16) V          P as bf16 and a bf16 of what that leaves: reading is
 //                                         what takes the time, and rounded weights would add
 //                                         an error as large as the output's rounding
-// 8-bit numbers become bf16 exactly in registers: with b the offset byte's low seven bits and
-// s its top one, bf16(128 + b) - bf16(128 << s) needs two logic operations and a
-// subtraction for two numbers. Key scales multiply scores, value scales weights.
+// 8-bit numbers become bf16 exactly in registers (bf16_of_i8: a byte permutation, two logic
+// operations and a subtraction for two). Key scales multiply scores, value scales weights.
 //
 // All tiles of all (sequence, row tile, key/value head) items lie on one line that is cut
 // into equal pieces, one per CTA: any mix of lengths fills the machine. An item cut in
@@ -52,11 +51,6 @@ struct PrCfg {
   static_assert(SCALES <= 1024 && 2 * MERGE <= 2 * TILE, "two warps' O fit the stage they free");
 };
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
@@ -72,81 +66,12 @@ __device__ __forceinline__ float2 lds_f2(uint32_t a) {
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
   return v;
 }
-// Two 8-bit numbers (the low bytes of t's halves) as bf16.
-__device__ __forceinline__ uint32_t bf16_of_i8(uint32_t t) {
-  const uint32_t b = (t & 0x007f007fu) | 0x43004300u, s = (t & 0x00800080u) | 0x43004300u;
-  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&b), *reinterpret_cast<const __nv_bfloat162*>(&s));
-  return *reinterpret_cast<const uint32_t*>(&d);
-}
-
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
-      : "memory");
-}
-
-// The line of tiles. Sequence b's items run row tile by row tile, heads inside; an
-// item has as many tiles as its last row sees keys, at least one. A warp keeps 32 sequences
-// at a time, one a lane.
-struct PrItem {
-  int b, h, rt, n, len, tiles, seen;   // seen: keys that its last row sees
-  int64_t row0, u0;                    // first packed row of the sequence, first tile on the line
-};
-struct PrLine {
-  int64_t base, end;      // of this chunk of sequences on the line
-  int b0;
-  PagedSeq q;             // this lane's sequence
-  int64_t mine, at;       // its tiles, and their place on the line
-
-  static __device__ __forceinline__ int tiles_of(int seen) { return seen <= kPrTK ? 1 : (seen + kPrTK - 1) / kPrTK; }
-  // keys that the last row of row tile rt sees
-  static __device__ __forceinline__ int seen_of(const PagedSeq& q, int rt, int G) {
-    return max(0, q.len - q.n + min(q.n, ((rt + 1) * kPrRows - 1) / G + 1));
-  }
-  __device__ __forceinline__ void load(const Paged& p, int b_first, int64_t from, int G, int lane, int* err) {
-    b0 = b_first;
-    base = from;
-    q = PagedSeq{0, 0, 0};
-    mine = 0;
-    if (b0 + lane < p.B) {
-      q = paged_seq(p, b0 + lane, err);
-      const int nrt = (q.n * G + kPrRows - 1) / kPrRows;
-      for (int rt = 0; rt < nrt; ++rt) mine += tiles_of(seen_of(q, rt, G));
-      mine *= p.Hkv;
-    }
-    int64_t inc = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += up;
-    }
-    at = base + inc - mine;
-    end = base + __shfl_sync(0xffffffffu, inc, 31);
-  }
-  // the item that holds tile u (below the line's length)
-  __device__ __forceinline__ PrItem item(const Paged& p, int64_t u, int G, int lane, int* err) {
-    while (u >= end) load(p, b0 + 32, end, G, lane, err);
-    const unsigned has = __ballot_sync(0xffffffffu, u >= at && u < at + mine);
-    const int l = __ffs(has) - 1;
-    PrItem it;
-    it.b = b0 + l;
-    PagedSeq s;
-    s.n = it.n = __shfl_sync(0xffffffffu, q.n, l);
-    s.len = it.len = __shfl_sync(0xffffffffu, q.len, l);
-    s.row0 = it.row0 = __shfl_sync(0xffffffffu, q.row0, l);
-    int64_t x = __shfl_sync(0xffffffffu, at, l);
-    for (it.rt = 0;; ++it.rt) {
-      it.seen = seen_of(s, it.rt, G);
-      it.tiles = tiles_of(it.seen);
-      if (u < x + (int64_t)it.tiles * p.Hkv) break;
-      x += (int64_t)it.tiles * p.Hkv;
-    }
-    it.h = (int)((u - x) / it.tiles);
-    it.u0 = x + (int64_t)it.h * it.tiles;
-    return it;
-  }
+// Groups of 16 packed rows, tiles of 64 keys.
+struct PrCut {
+  static constexpr int KEYS = kPrTK;
+  int G;
+  __device__ __forceinline__ int groups(int n) const { return (n * G + kPrRows - 1) / kPrRows; }
+  __device__ __forceinline__ int tokens(int g) const { return ((g + 1) * kPrRows - 1) / G + 1; }
 };
 
 template <int HD, bool I8>
@@ -183,17 +108,10 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
   pdl_wait();
   pdl_trigger();
   // this CTA's piece of the line
-  PrLine line;
-  int64_t all = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 32) {
-    line.load(p, b0, all, G, lane, err);
-    all = line.end;
-  }
-  int64_t per = (all + gridDim.x - 1) / gridDim.x;
-  if (per < kPrMinTiles) per = kPrMinTiles;
-  const int64_t ua = min(all, (int64_t)blockIdx.x * per), ub = min(all, ua + per);
+  PagedLine<PrCut> line{PrCut{G}};
+  int64_t per, ua, ub;
+  line.piece(p, kPrMinTiles, (int)blockIdx.x, (int)gridDim.x, lane, err, &per, &ua, &ub);
   if (ua >= ub) return;
-  if (ua < line.base) line.load(p, 0, 0, G, lane, err);
 
   if (warp == kPrWarps) {
     // ------------------------------------------------------------ producer
@@ -201,7 +119,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
     int issued = 0;
     bool ok = true;
     for (int64_t u = ua; ok && u < ub;) {
-      const PrItem it = line.item(p, u, G, lane, err);
+      const PagedItem it = line.item(p, u, lane, err);
       const int t1 = (int)(min(ub, it.u0 + it.tiles) - it.u0);
       int t = (int)(u - it.u0);
       u = it.u0 + t1;
@@ -267,7 +185,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
   const int mi = lane >> 3, mr = lane & 7;   // ldmatrix: this lane's matrix and row
   int taken = 0;
   for (int64_t u = ua; u < ub;) {
-    const PrItem it = line.item(p, u, G, lane, err);
+    const PagedItem it = line.item(p, u, lane, err);
     const int t1 = (int)(min(ub, it.u0 + it.tiles) - it.u0), t0 = (int)(u - it.u0);
     u = it.u0 + t1;
     // rows gid and gid + 8: their token and head, and the keys that they see
@@ -277,7 +195,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
     bool live[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int x = it.rt * kPrRows + gid + 8 * r, i = x / G, g = x - i * G;
+      const int x = it.grp * kPrRows + gid + 8 * r, i = x / G, g = x - i * G;
       live[r] = i < it.n;
       lim[r] = live[r] ? it.len - it.n + i + 1 : 0;
       src[r] = q + (it.row0 + i) * ld_q + (it.h * G + g) * HD;
@@ -324,7 +242,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
 #pragma unroll
     for (int j = 0; j < NT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
     // keys that every row of the item sees: tiles below need no mask
-    const int open = it.len - it.n + it.rt * kPrRows / G + 1;
+    const int open = it.len - it.n + it.grp * kPrRows / G + 1;
     bool ok = true;
     int st = 0;
     for (int t = t0; t < t1; ++t, ++taken) {
@@ -394,7 +312,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
           const float mn = fmaxf(m_r[r], mx);
           base[r] = mn == -INFINITY ? 0.f : mn;
-          corr[r] = ex2(m_r[r] - base[r]);
+          corr[r] = paged_ex2(m_r[r] - base[r]);
           m_r[r] = mn;
         }
         uint32_t pa[4], pl[4];   // weights: bf16, and what that leaves
@@ -403,7 +321,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           float sum = 0.f;
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt) {
-            float p0 = ex2(sc[nt][2 * r] - base[r]), p1 = ex2(sc[nt][2 * r + 1] - base[r]);
+            float p0 = paged_ex2(sc[nt][2 * r] - base[r]), p1 = paged_ex2(sc[nt][2 * r + 1] - base[r]);
             sum += p0 + p1;
             if (I8) {   // a masked key's scale may be anything
               p0 = p0 > 0.f ? p0 * vsc[nt].x : 0.f;
@@ -529,8 +447,8 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float mn = fmaxf(m_r[r], ml[r].x), b = mn == -INFINITY ? 0.f : mn;
-        mine[r] = ex2(m_r[r] - b);
-        theirs[r] = ex2(ml[r].x - b);
+        mine[r] = paged_ex2(m_r[r] - b);
+        theirs[r] = paged_ex2(ml[r].x - b);
         l_r[r] = l_r[r] * mine[r] + ml[r].y * theirs[r];
         m_r[r] = mn;
       }
