@@ -51,12 +51,30 @@ __device__ __forceinline__ int64_t paged_vec(const Paged& p, int page, int place
 }
 
 // A line of tiles of keys, shared out in equal pieces. Sequence b's items run group of rows by
-// group of rows, key/value heads inside; an item has as many tiles as its last row sees keys,
-// at least one. CUT: rows of a group (`groups`, `tokens`) and keys of a tile (KEYS).
+// group of rows, key/value heads inside. An item takes PAD places (what its start and
+// end cost) and then one for each tile of the keys that its last row sees (at least one). The places
+// of a piece are its CTA's work; items of at most WHOLE tiles are not cut, they go to the
+// CTA that has their first tile. CUT: rows of a group (groups, tokens), keys of a tile (KEYS), PAD, WHOLE.
 // A warp keeps 32 sequences at a time, one a lane.
+template <class CUT>
 struct PagedItem {
   int b, h, grp, n, len, tiles, seen;  // seen: keys that its last row sees
-  int64_t row0, u0;                    // first packed row of the sequence, first tile on the line
+  int64_t row0, at0;                   // first packed row of the sequence, place of the first tile
+  // its tiles [j0, j1) in the piece [ua, ub)
+  __device__ __forceinline__ void in(int64_t ua, int64_t ub, int* j0, int* j1) const {
+    if (tiles <= CUT::WHOLE) {
+      *j0 = 0;
+      *j1 = at0 >= ua && at0 < ub ? tiles : 0;
+    } else {
+      *j0 = (int)max((int64_t)0, ua - at0);
+      *j1 = (int)min((int64_t)tiles, ub - at0);
+    }
+  }
+  // the CTAs that have its first tile and tile number `last` (the same where it is not cut)
+  __device__ __forceinline__ int first_cta(int64_t per) const { return (int)(at0 / per); }
+  __device__ __forceinline__ int last_cta(int64_t per, int last) const {
+    return (int)((tiles <= CUT::WHOLE ? at0 : at0 + last) / per);
+  }
 };
 template <class CUT>
 struct PagedLine {
@@ -80,7 +98,7 @@ struct PagedLine {
     if (b0 + lane < p.B) {
       q = paged_seq(p, b0 + lane, err);
       const int groups = cut.groups(q.n);
-      for (int g = 0; g < groups; ++g) mine += tiles_of(seen_of(q.n, q.len, g));
+      for (int g = 0; g < groups; ++g) mine += CUT::PAD + tiles_of(seen_of(q.n, q.len, g));
       mine *= p.Hkv;
     }
     int64_t inc = mine;
@@ -92,7 +110,7 @@ struct PagedLine {
     at = base + inc - mine;
     end = base + __shfl_sync(0xffffffffu, inc, 31);
   }
-  // the line's length, and [first, last) of CTA `cta` of `ctas` in pieces of *per tiles, `least` or more
+  // [first, last) of CTA `cta` of `ctas` in pieces of *per places, `least` or more
   __device__ __forceinline__ void piece(const Paged& p, int least, int cta, int ctas, int lane, int* err, int64_t* per,
                                         int64_t* first, int64_t* last) {
     int64_t all = 0;
@@ -105,11 +123,12 @@ struct PagedLine {
     *last = min(all, *first + *per);
     if (*first < base) load(p, 0, 0, lane, err);
   }
-  // the item that holds tile u (below the line's length; calls with rising u)
-  __device__ __forceinline__ PagedItem item(const Paged& p, int64_t u, int lane, int* err) {
+  // the item that holds place *u (below the line's length; calls with rising *u), which moves past it
+  __device__ __forceinline__ PagedItem<CUT> item(const Paged& p, int64_t* to, int lane, int* err) {
+    const int64_t u = *to;
     while (u >= end) load(p, b0 + 32, end, lane, err);
     const int l = __ffs(__ballot_sync(0xffffffffu, u >= at && u < at + mine)) - 1;
-    PagedItem it;
+    PagedItem<CUT> it;
     it.b = b0 + l;
     it.n = __shfl_sync(0xffffffffu, q.n, l);
     it.len = __shfl_sync(0xffffffffu, q.len, l);
@@ -123,13 +142,14 @@ struct PagedLine {
     for (;; ++grp) {
       it.seen = seen_of(it.n, it.len, grp);
       it.tiles = tiles_of(it.seen);
-      const int64_t all = (int64_t)it.tiles * p.Hkv;
+      const int64_t all = (int64_t)(CUT::PAD + it.tiles) * p.Hkv;
       if (u < x + all) break;
       x += all;
     }
     it.grp = grp;
-    it.h = (int)((u - x) / it.tiles);
-    it.u0 = x + (int64_t)it.h * it.tiles;
+    it.h = (int)((u - x) / (CUT::PAD + it.tiles));
+    it.at0 = x + (int64_t)it.h * (CUT::PAD + it.tiles) + CUT::PAD;
+    *to = it.at0 + it.tiles;
     return it;
   }
 };

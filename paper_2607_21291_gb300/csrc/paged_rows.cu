@@ -36,7 +36,9 @@ constexpr int kPrWarps = 4;               // consumer warps, 16 keys of a tile e
 constexpr int kPrThreads = 32 * (kPrWarps + 1);
 constexpr int kPrPerSm = 2;               // CTAs an SM
 constexpr int kPrMaxCtas = 160 * kPrPerSm;
-constexpr int kPrMinTiles = 4;            // fewest tiles of a piece
+constexpr int kPrPad = 2;                 // an item's start and end, in tiles
+constexpr int kPrWhole = 8;               // tiles up to which an item is not cut
+constexpr int kPrMin = 4;                 // fewest places of a piece
 
 template <int HD, bool I8>
 struct PrCfg {
@@ -68,7 +70,7 @@ __device__ __forceinline__ float2 lds_f2(uint32_t a) {
 }
 // Groups of 16 packed rows, tiles of 64 keys.
 struct PrCut {
-  static constexpr int KEYS = kPrTK;
+  static constexpr int KEYS = kPrTK, PAD = kPrPad, WHOLE = kPrWhole;
   int G;
   __device__ __forceinline__ int groups(int n) const { return (n * G + kPrRows - 1) / kPrRows; }
   __device__ __forceinline__ int tokens(int g) const { return ((g + 1) * kPrRows - 1) / G + 1; }
@@ -110,7 +112,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
   // this CTA's piece of the line
   PagedLine<PrCut> line{PrCut{G}};
   int64_t per, ua, ub;
-  line.piece(p, kPrMinTiles, (int)blockIdx.x, (int)gridDim.x, lane, err, &per, &ua, &ub);
+  line.piece(p, kPrMin, (int)blockIdx.x, (int)gridDim.x, lane, err, &per, &ua, &ub);
   if (ua >= ub) return;
 
   if (warp == kPrWarps) {
@@ -119,11 +121,10 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
     int issued = 0;
     bool ok = true;
     for (int64_t u = ua; ok && u < ub;) {
-      const PagedItem it = line.item(p, u, lane, err);
-      const int t1 = (int)(min(ub, it.u0 + it.tiles) - it.u0);
-      int t = (int)(u - it.u0);
-      u = it.u0 + t1;
-      if (it.seen == 0) continue;
+      const PagedItem<PrCut> it = line.item(p, &u, lane, err);
+      int t, t1;
+      it.in(ua, ub, &t, &t1);
+      if (it.seen == 0 || t >= t1) continue;
       const int32_t* tab = p.table + (int64_t)it.b * p.max_pages;
       // a lane's page of tile t; pages past the last visible key are not looked at
       auto page_of = [&](int t) {
@@ -185,9 +186,10 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
   const int mi = lane >> 3, mr = lane & 7;   // ldmatrix: this lane's matrix and row
   int taken = 0;
   for (int64_t u = ua; u < ub;) {
-    const PagedItem it = line.item(p, u, lane, err);
-    const int t1 = (int)(min(ub, it.u0 + it.tiles) - it.u0), t0 = (int)(u - it.u0);
-    u = it.u0 + t1;
+    const PagedItem<PrCut> it = line.item(p, &u, lane, err);
+    int t0, t1;
+    it.in(ua, ub, &t0, &t1);
+    if (t0 >= t1) continue;
     // rows gid and gid + 8: their token and head, and the keys that they see
     const bf16* src[2];
     bf16* dst[2];
@@ -481,7 +483,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
     if (warp != 0) continue;
 
     // warp 0 holds the piece's result
-    const int first = (int)(it.u0 / per), last = (int)((it.u0 + it.tiles - 1) / per);
+    const int first = it.first_cta(per), last = it.last_cta(per, it.tiles - 1);
     if (first != last) {
       const int me = (int)blockIdx.x;
       auto slot_of = [&](int cta) { return parts + ((int64_t)cta * 2 + (cta == first ? 1 : 0)) * SLOT; };
@@ -553,7 +555,7 @@ cudaError_t launch_rows(const Paged& p, const void* q, int64_t ld_q, void* out, 
   const int64_t span = ((int64_t)p.max_pages << p.page_log2) / kPrTK + 1;
   const int64_t row_tiles = std::min<int64_t>((int64_t)p.B * ((p.max_new * (int64_t)G + kPrRows - 1) / kPrRows),
                                               p.n_rows * G);
-  const int64_t most = std::max<int64_t>(1, (row_tiles * p.Hkv * span + kPrMinTiles - 1) / kPrMinTiles);
+  const int64_t most = std::max<int64_t>(1, (row_tiles * p.Hkv * (span + kPrPad) + kPrMin - 1) / kPrMin);
   const int64_t room = std::min(dev.num_sms * kPrPerSm, kPrMaxCtas);
   return launch_pdl(paged_rows_kernel<HD, I8>, dim3((unsigned)std::min(most, room)), dim3(kPrThreads), (size_t)C::SMEM,
                     dev.stream, tk, tv, p, static_cast<const bf16*>(q), ld_q, static_cast<bf16*>(out),

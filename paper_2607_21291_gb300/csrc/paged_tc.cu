@@ -37,11 +37,9 @@ namespace {
 constexpr int kPtRows = 128;            // lanes of a row tile
 constexpr int kPtKB = 128;              // keys of a block
 constexpr int kPtMaxCtas = 160;
-constexpr int kPtMinTiles = 3;          // fewest blocks of a piece
-#ifndef PT_FINE
-#define PT_FINE 2048
-#endif
-constexpr int kPtFine = PT_FINE;           // keys up to which weights enter in two parts
+constexpr int kPtPad = 2;               // an item's start and end, in blocks
+constexpr int kPtWhole = 4;             // blocks up to which an item is not cut
+constexpr int kPtFine = 2048;           // keys up to which weights enter in two parts
 constexpr float kPtRescale = 8.f;       // O rescaled only when the row maximum grows by > 2^8
 
 template <int HD, bool I8>
@@ -52,12 +50,17 @@ struct PtCfg {
   static constexpr int HS = HD / 64;                // 64-feature slabs
   static constexpr int SLAB = 128 * 128;            // 128 rows of 128 bytes
   static constexpr int TILE = HS * SLAB;            // Q tile, K block or V block
-  static constexpr int DATA = (2 + KST + VST) * TILE;
+  // 8-bit numbers on their way: halves of a block's keys (or values), 64 rows of HD bytes as they lie
+  static constexpr int GST = I8 ? (HD == 64 ? 6 : 3) : 0;
+  static constexpr int GSTN = GST ? GST : 1;
+  static constexpr int GHALF = 64 * HD;
+  static constexpr int DATA = (2 + KST + VST) * TILE + GST * GHALF;
   // key and value scales of eight blocks: they are written up to KST blocks ahead of the one that the softmax reads
   static constexpr int SC = 8;
   static_assert(KST + 1 <= SC, "scales");
-  static constexpr int SCALES = I8 ? SC * 2 * kPtKB * 4 : 0;
-  static constexpr int NBARS = 2 + 2 * KST + 3 * VST + 8 + 1 + SC + 4;
+  static constexpr int SCW = 2 * kPtKB + 4;          // words of a block: keys, values, marks of keys that are NaN
+  static constexpr int SCALES = I8 ? SC * SCW * 4 : 0;
+  static constexpr int NBARS = 2 + 2 * KST + 3 * VST + 8 + 1 + SC + 4 + 2 * GST;
   static constexpr int TAIL = 512;
   static constexpr int RAW = DATA + SCALES + TAIL + 1024;
   static constexpr int SMEM = RAW > 232448 ? 232448 : RAW < 120 * 1024 ? 120 * 1024 : RAW;   // one CTA an SM: TMEM is allocated in full
@@ -70,7 +73,7 @@ struct PtCfg {
 
 // Groups of two row tiles, blocks of 128 keys.
 struct PtCut {
-  static constexpr int KEYS = kPtKB;
+  static constexpr int KEYS = kPtKB, PAD = kPtPad, WHOLE = kPtWhole;
   int R;
   __device__ __forceinline__ int groups(int n) const { return (n + 2 * R - 1) / (2 * R); }
   __device__ __forceinline__ int tokens(int g) const { return (g + 1) * 2 * R; }
@@ -78,12 +81,13 @@ struct PtCut {
 
 // A piece of an item on a CTA: blocks j0 .. j1 - 1; nb[t]: blocks that tile t takes in all.
 struct PtWork {
-  PagedItem it;
+  PagedItem<PtCut> it;
   int j0, j1, two, nb[2];
   int t0;      // first token
+  bool mine;   // whether the piece has the item's start
   __device__ __forceinline__ int open(int t, int R) const { return it.len - it.n + t0 + t * R + 1; }   // keys that its first row sees
 };
-__device__ __forceinline__ PtWork pt_work(const PagedItem& it, int64_t u, int64_t ub, int R) {
+__device__ __forceinline__ PtWork pt_work(const PagedItem<PtCut>& it, int64_t ua, int64_t ub, int R) {
   PtWork w;
   w.it = it;
   w.t0 = it.grp * 2 * R;
@@ -91,8 +95,9 @@ __device__ __forceinline__ PtWork pt_work(const PagedItem& it, int64_t u, int64_
   const int seen0 = max(0, it.len - it.n + min(it.n, w.t0 + R));
   w.nb[0] = (seen0 + kPtKB - 1) / kPtKB;
   w.nb[1] = w.two ? (it.seen + kPtKB - 1) / kPtKB : 0;
-  w.j0 = (int)(u - it.u0);
-  w.j1 = min((int)(min(ub, it.u0 + it.tiles) - it.u0), w.two ? w.nb[1] : w.nb[0]);
+  it.in(ua, ub, &w.j0, &w.j1);
+  w.mine = w.j0 == 0 && w.j1 > 0;
+  w.j1 = min(w.j1, w.two ? w.nb[1] : w.nb[0]);
   return w;
 }
 
@@ -141,10 +146,34 @@ __device__ __forceinline__ void commit(uint32_t bar, uint32_t lead) {
       "r"(lead)
       : "memory");
 }
-template <int N>
-__device__ __forceinline__ void more_registers() { __syncwarp(); asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void fewer_registers() { __syncwarp(); asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// Waits that poll: a suspended thread is woken late (all of the kernel's waits with a suspension
+// of up to 100 us took 430 us where these take 404, at 2048 tokens on 14336 of 28 heads).
+__device__ __forceinline__ bool try_now(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool wait_now(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* err, unsigned long long timeout_ns) {
+  if (try_now(bar, parity)) return true;
+  const unsigned long long t0 = globaltimer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (try_now(bar, parity)) return true;
+    if ((it & 63u) == 0) {
+      if (*abort_flag) return false;
+      if (globaltimer_ns() - t0 > timeout_ns) {
+        *abort_flag = 1;
+        set_device_error(err, DEVERR_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
 
 template <int HD, bool I8>
 __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
@@ -159,14 +188,15 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
     if (threadIdx.x == 0) set_device_error(err, DEVERR_TIMEOUT);
     return;
   }
-  const uint32_t sQ = smem_u32(smem), sK0 = sQ + 2 * C::TILE, sV0 = sK0 + KST * C::TILE;
-  float* scales = reinterpret_cast<float*>(smem + C::DATA);           // [SC][key, value][128]
+  const uint32_t sQ = smem_u32(smem), sK0 = sQ + 2 * C::TILE, sV0 = sK0 + KST * C::TILE, sG0 = sV0 + VST * C::TILE;
+  float* scales = reinterpret_cast<float*>(smem + C::DATA);           // [SC][SCW]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::DATA + C::SCALES);
   const uint32_t q_full = smem_u32(bars), q_empty = q_full + 8;
   const uint32_t k_full0 = q_empty + 8, k_empty0 = k_full0 + 8 * KST;
   const uint32_t v_full0 = k_empty0 + 8 * KST, v_empty0 = v_full0 + 8 * VST, v_ok0 = v_empty0 + 8 * VST;
   const uint32_t s_full0 = v_ok0 + 8 * VST, p_full0 = s_full0 + 16, o_done0 = p_full0 + 16, o_free0 = o_done0 + 16;
   const uint32_t drain = o_free0 + 16, sc_full0 = drain + 8, wrote0 = sc_full0 + 8 * C::SC, told0 = wrote0 + 16;
+  const uint32_t g_full0 = told0 + 16, g_empty0 = g_full0 + 8 * C::GST;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::NBARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* last_s = abort_flag + 1;      // [2] whether this CTA joins the tile's pieces
@@ -194,6 +224,10 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
     }
     mbar_init(drain, 1);
     for (int i = 0; i < C::SC; ++i) mbar_init(sc_full0 + 8 * i, 4);
+    for (int i = 0; i < C::GST; ++i) {
+      mbar_init(g_full0 + 8 * i, 1);
+      mbar_init(g_empty0 + 8 * i, 4);
+    }
     for (int t = 0; t < 2; ++t) {
       mbar_init(wrote0 + 8 * t, 4);
       mbar_init(told0 + 8 * t, 1);
@@ -218,8 +252,8 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
 
   PagedLine<PtCut> line{PtCut{R}};
   int64_t per, ua, ub;
-  line.piece(p, kPtMinTiles, (int)blockIdx.x, (int)gridDim.x, lane, err, &per, &ua, &ub);
-  auto wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_bounded(bar, parity, abort_flag, err, timeout_ns); };
+  line.piece(p, kPtPad + 1, (int)blockIdx.x, (int)gridDim.x, lane, err, &per, &ua, &ub);
+  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_now(bar, parity, abort_flag, err, timeout_ns); };
   auto all_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
   // a lane waits for its warp
   auto warp_wait = [&](uint32_t bar, uint32_t parity) {
@@ -229,16 +263,14 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
   };
 
   if (warp < 4) {
-    fewer_registers<I8 ? 64 : 80>();
     if (warp == 0) {
       // ------------------------------------------------------------ TMA
-      const int box = 1 << p.page_log2, boxes = kPtKB / box;
-      int items = 0, issued = 0;
+      const int box = I8 ? min(1 << p.page_log2, 64) : 1 << p.page_log2, boxes = kPtKB / box;   // rows of a copy, copies of a block
+      int items = 0, issued = 0, copied = 0;
       bool ok = true;
       for (int64_t u = ua; ok && u < ub;) {
-        const PagedItem it = line.item(p, u, lane, err);
-        const PtWork w = pt_work(it, u, ub, R);
-        u = min(ub, it.u0 + it.tiles);
+        const PagedItem<PtCut> it = line.item(p, &u, lane, err);
+        const PtWork w = pt_work(it, ua, ub, R);
         if (w.j0 >= w.j1) continue;
         if (items > 0 && !warp_wait(q_empty, (items - 1) & 1)) break;
         if (lane == 0) {
@@ -248,7 +280,6 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
               tma_load_4d(sQ + t * C::TILE + s * C::SLAB, &tq, s * 64, 0, it.h, (int)(it.row0 + w.t0 + t * R), q_full);
         }
         ++items;
-        if (I8) continue;
         const int32_t* tab = p.table + (int64_t)it.b * p.max_pages;
         auto page_of = [&](int j) {
           const int place = j * kPtKB + lane * box;
@@ -263,12 +294,31 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
           const bool there = (unsigned)page < (unsigned)p.n_pages;
           if (want && !there) set_device_error(err, DEVERR_INDEX);
           const int z = there ? page * p.Hkv + it.h : p.n_pages * p.Hkv;   // out of the pool: filled with zeros
-          const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xffffffffu, want)) * box * C::HS * 128);
+          const unsigned wants = __ballot_sync(0xffffffffu, want);
+          const int r = place & ((1 << p.page_log2) - 1);
+          if (I8) {
+            // keys, then values, in halves: half h is the copies of lanes boxes / 2 h ..
+            const int half = boxes / 2, mine = lane >= half, at = lane - mine * half;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int st = copied % C::GSTN;
+              const unsigned part = (v & 1) ? wants >> half : wants & ((1u << half) - 1);
+              ok = ok && all_wait(g_empty0 + 8 * st, ((copied / C::GSTN) & 1) ^ 1);
+              if (!ok) break;
+              if (lane == 0) mbar_arrive_expect_tx(g_full0 + 8 * st, (uint32_t)(__popc(part) * box * HD));
+              __syncwarp();
+              if (want && mine == (v & 1)) tma_load_3d(sG0 + st * C::GHALF + at * box * HD, v < 2 ? &tk : &tv, 0, r, z, g_full0 + 8 * st);
+              ++copied;
+            }
+            if (!ok) break;
+            continue;
+          }
+          const uint32_t bytes = (uint32_t)(__popc(wants) * box * C::HS * 128);
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
             const int n_st = v ? VST : KST, st = issued % n_st;
             const uint32_t full = (v ? v_full0 : k_full0) + 8 * st, empty = (v ? v_empty0 : k_empty0) + 8 * st;
-            if (!warp_wait(empty, ((issued / n_st) & 1) ^ 1)) { ok = false; break; }
+            if (!all_wait(empty, ((issued / n_st) & 1) ^ 1)) { ok = false; break; }
             if (lane == 0) mbar_arrive_expect_tx(full, bytes);
             __syncwarp();
             if (want)
@@ -284,7 +334,12 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
       // drain: what was copied last into each place has landed
       if (lane == 0) {
         if (items > 0) mbar_wait_drain(q_full, (items - 1) & 1, timeout_ns);
-        if (!I8)
+        if (I8)
+          for (int st = 0; st < C::GST && st < copied; ++st) {
+            const int last = st + ((copied - 1 - st) / C::GSTN) * C::GSTN;
+            mbar_wait_drain(g_full0 + 8 * st, (uint32_t)((last / C::GSTN) & 1), timeout_ns);
+          }
+        else
           for (int v = 0; v < 2; ++v) {
             const int n_st = v ? VST : KST;
             for (int st = 0; st < n_st && st < issued; ++st) {
@@ -312,19 +367,18 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
         const uint32_t v0 = v_low + vslot * (C::TILE >> 4), to = tmem_base + C::TO + t * HD, tp = tmem_base + t * kPtKB;
 #pragma unroll
         for (int kk = 0; kk < kPtKB / 16; ++kk)
-          mma_ts(to, tp + kk * 8, v0 + kk * 128, idesc_o, (acc || kk > 0) ? 1u : 0u, lead);
+          mma_ts(to, tp + (kk >> 1) * 32 + (kk & 1) * 8, v0 + kk * 128, idesc_o, (acc || kk > 0) ? 1u : 0u, lead);
         if (fine)
 #pragma unroll
-          for (int kk = 0; kk < kPtKB / 16; ++kk) mma_ts(to, tp + 64 + kk * 8, v0 + kk * 128, idesc_o, 1u, lead);
+          for (int kk = 0; kk < kPtKB / 16; ++kk) mma_ts(to, tp + (kk >> 1) * 32 + 16 + (kk & 1) * 8, v0 + kk * 128, idesc_o, 1u, lead);
         commit(o_done0 + 8 * t, lead);
       };
       int kc = 0, vc = 0, items = 0;
       int pc[2] = {0, 0}, oc[2] = {0, 0};   // P blocks taken, pieces finished, per tile
       bool ok = true;
       for (int64_t u = ua; ok && u < ub;) {
-        const PagedItem it = line.item(p, u, lane, err);
-        const PtWork w = pt_work(it, u, ub, R);
-        u = min(ub, it.u0 + it.tiles);
+        const PagedItem<PtCut> it = line.item(p, &u, lane, err);
+        const PtWork w = pt_work(it, ua, ub, R);
         if (w.j0 >= w.j1) continue;
         const bool fine = it.seen <= kPtFine;
         auto k_wait = [&](int c) { return all_wait(k_full0 + 8 * (c % KST), (c / KST) & 1); };
@@ -387,9 +441,8 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
       int vc = 0;
       bool ok = true;
       for (int64_t u = ua; ok && u < ub;) {
-        const PagedItem it = line.item(p, u, lane, err);
-        const PtWork w = pt_work(it, u, ub, R);
-        u = min(ub, it.u0 + it.tiles);
+        const PagedItem<PtCut> it = line.item(p, &u, lane, err);
+        const PtWork w = pt_work(it, ua, ub, R);
         const int open = w.open(0, R);
         for (int j = w.j0; j < w.j1; ++j, ++vc) {
           const int st = vc % VST;
@@ -431,7 +484,7 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
     }
   } else if (warp < 12) {
     // -------------------------------------------------------------- softmax
-    more_registers<I8 ? 168 : 208>();
+
     const int t = (warp - 4) >> 2;                   // tile
     const int r = (warp & 3) * 32 + lane;            // its row = TMEM lane
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
@@ -441,15 +494,14 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
     int sc = 0, blocks = 0, cut = 0;   // S blocks taken, blocks passed, pieces of cut items
     bool ok = true;
     for (int64_t u = ua; ok && u < ub;) {
-      const PagedItem it = line.item(p, u, lane, err);
-      const PtWork w = pt_work(it, u, ub, R);
-      u = min(ub, it.u0 + it.tiles);
+      const PagedItem<PtCut> it = line.item(p, &u, lane, err);
+      const PtWork w = pt_work(it, ua, ub, R);
       const int i = w.t0 + t * R + ti;
       const bool live = ti < R && i < it.n;
       const int lim = live ? it.len - it.n + i + 1 : 0;   // keys that the row sees
       bf16* dst = out + ((it.row0 + i) * p.Hq + it.h * G + gi) * HD;
       const int j1 = min(w.j1, w.nb[t]);
-      if (w.nb[t] == 0 && w.j0 == 0 && live && (t == 0 || w.two))   // a tile without keys
+      if (w.nb[t] == 0 && w.mine && live && (t == 0 || w.two))   // a tile without keys
         for (int e = 0; e < HD; e += 8) *reinterpret_cast<uint4*>(dst + e) = make_uint4(0, 0, 0, 0);
       if (w.j0 >= j1) {
         blocks += max(0, w.j1 - w.j0);
@@ -460,35 +512,57 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
       float m = -INFINITY, l = 0.f;
       for (int j = w.j0; j < j1; ++j) {
         const int at_sc = (blocks + j - w.j0) % C::SC;
-        const float4* ks4 = reinterpret_cast<const float4*>(scales + at_sc * 2 * kPtKB);
+        const float4* ks4 = reinterpret_cast<const float4*>(scales + at_sc * C::SCW);
         const float4* vs4 = ks4 + kPtKB / 4;
         if (I8 && !all_wait(sc_full0 + 8 * at_sc, (blocks + j - w.j0) / C::SC & 1)) { ok = false; break; }
         if (!all_wait(s_full0 + 8 * t, sc & 1)) { ok = false; break; }
         ++sc;
         tc_fence_after();
-        uint32_t s[kPtKB];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, s + 32 * c);
-        tmem_ld_wait();
-        if (I8) {   // the scale of the scores is in the key scales
-#pragma unroll
-          for (int k = 0; k < kPtKB; k += 4) {
-            const float4 f = ks4[k / 4];
-            const float2 a = __fmul2_rn(make_float2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), make_float2(f.x, f.y));
-            const float2 b = __fmul2_rn(make_float2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), make_float2(f.z, f.w));
-            s[k] = __float_as_uint(a.x); s[k + 1] = __float_as_uint(a.y);
-            s[k + 2] = __float_as_uint(b.x); s[k + 3] = __float_as_uint(b.y);
-          }
-        }
-        const bool masked = (j + 1) * kPtKB > open;
-        if (masked) {
+        const uint4 marks = I8 ? reinterpret_cast<const uint4*>(vs4)[kPtKB / 4] : make_uint4(0, 0, 0, 0);
+        if ((j + 1) * kPtKB > open || (marks.x | marks.y | marks.z | marks.w)) {
+          // keys that the row does not see: -infinity
           const int left = lim - j * kPtKB;
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t z[32];
+            tmem_ld32(tS + 32 * c, z);
+            tmem_ld_wait();
 #pragma unroll
-          for (int k = 0; k < kPtKB; ++k) s[k] = k < left ? s[k] : 0xff800000u;
+            for (int k = 0; k < 32; ++k) {
+              if (I8 && ((c == 0 ? marks.x : c == 1 ? marks.y : c == 2 ? marks.z : marks.w) >> k & 1)) z[k] = 0x7fc00000u;
+              z[k] = 32 * c + k < left ? z[k] : 0xff800000u;
+            }
+            tmem_st32(tS + 32 * c, z);
+          }
+          tmem_st_wait();
         }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        constexpr int MW = I8 ? 32 : 64;   // scores read at once
+#pragma unroll 1
+        for (int c = 0; c < kPtKB; c += MW) {
+          uint32_t s[MW];
 #pragma unroll
-        for (int k = 0; k < kPtKB; k += 2) mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+          for (int i = 0; i < MW; i += 32) tmem_ld32(tS + c + i, s + i);
+          tmem_ld_wait();
+#pragma unroll
+          for (int k = 0; k < MW; k += 4) {
+            float4 y = make_float4(__uint_as_float(s[k]), __uint_as_float(s[k + 1]), __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
+            if (I8) {   // the scale of the scores is in the key scales
+              const float4 f = ks4[(c + k) / 4];
+              const float2 u0 = __fmul2_rn(make_float2(y.x, y.y), make_float2(f.x, f.y));
+              const float2 u1 = __fmul2_rn(make_float2(y.z, y.w), make_float2(f.z, f.w));
+              y = make_float4(u0.x, u0.y, u1.x, u1.y);
+            }
+            mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], y.x, y.y);
+            mx[((k >> 1) + 1) & 3] = max3(mx[((k >> 1) + 1) & 3], y.z, y.w);
+            if (I8) {
+              s[k] = __float_as_uint(y.x); s[k + 1] = __float_as_uint(y.y);
+              s[k + 2] = __float_as_uint(y.z); s[k + 3] = __float_as_uint(y.w);
+            }
+          }
+          if (I8) tmem_st32(tS + c, s);
+        }
+        if (I8) tmem_st_wait();
         float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         if (!I8) top *= scale_log2;
         // O is stable: its last product was issued before S_t(j), which is complete
@@ -509,42 +583,40 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
         if (grow) m = top;
         const float base = m == -INFINITY ? 0.f : m;
         const float2 scale2 = make_float2(scale_log2, scale_log2), neg2 = make_float2(-base, -base);
-        // weights and their sum; FINE: what their rounding leaves, too
-        auto weigh = [&](auto fine_c, auto masked_c) {
-          constexpr bool FINE = decltype(fine_c)::value, MASKED = decltype(masked_c)::value;
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        // weights of 32 keys from their scores, over them: bf16 pairs, then what the rounding leaves
+        auto weigh = [&](int c, const uint32_t (&z)[32]) {
+          uint32_t hi[16];
+          float2 e[16];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t hi[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const int at = 32 * c + 2 * k;
-              const float2 y = make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]));
-              const float2 x = I8 ? __fadd2_rn(y, neg2) : __ffma2_rn(y, scale2, neg2);
-              float2 e = make_float2(paged_ex2(x.x), paged_ex2(x.y));
-              sum[k & 1] = __fadd2_rn(sum[k & 1], e);
-              if (I8) {
-                const float4 f = vs4[at / 4];
-                const float2 y2 = __fmul2_rn(e, (at & 2) ? make_float2(f.z, f.w) : make_float2(f.x, f.y));
-                // a masked key's scale may be anything
-                e = MASKED ? make_float2(e.x > 0.f ? y2.x : 0.f, e.y > 0.f ? y2.y : 0.f) : y2;
-              }
-              hi[k] = pack_bf16x2(e.x, e.y);
-              if (FINE)
-                s[16 * c + k] = pack_bf16x2(e.x - __uint_as_float(hi[k] << 16), e.y - __uint_as_float(hi[k] & 0xffff0000u));
+          for (int k = 0; k < 16; ++k) {
+            float2 y = make_float2(__uint_as_float(z[2 * k]), __uint_as_float(z[2 * k + 1]));
+            y = I8 ? __fadd2_rn(y, neg2) : __ffma2_rn(y, scale2, neg2);
+            e[k] = make_float2(paged_ex2(y.x), paged_ex2(y.y));
+            sum[k & 1] = __fadd2_rn(sum[k & 1], e[k]);
+            if (I8) {
+              const float4 f = vs4[8 * c + k / 2];
+              e[k] = __fmul2_rn(e[k], (k & 1) ? make_float2(f.z, f.w) : make_float2(f.x, f.y));
             }
-            tmem_st16(tS + 16 * c, hi);
-            if (FINE) tmem_st16(tS + 64 + 16 * c, s + 16 * c);
+            hi[k] = pack_bf16x2(e[k].x, e[k].y);
           }
-          l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+          tmem_st16(tS + 32 * c, hi);
+          if (fine) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+              hi[k] = pack_bf16x2(e[k].x - __uint_as_float(hi[k] << 16), e[k].y - __uint_as_float(hi[k] & 0xffff0000u));
+            tmem_st16(tS + 32 * c + 16, hi);
+          }
         };
-        if (fine) {
-          if (I8 && masked) weigh(std::true_type(), std::true_type());
-          else weigh(std::true_type(), std::false_type());
-        } else {
-          if (I8 && masked) weigh(std::false_type(), std::true_type());
-          else weigh(std::false_type(), std::false_type());
+        // read again piece by piece: the loop is short enough for the instruction caches
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          uint32_t z[32];
+          tmem_ld32(tS + 32 * c, z);
+          tmem_ld_wait();
+          weigh(c, z);
         }
+        l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -555,14 +627,14 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
       if (!warp_wait(o_done0 + 8 * t, (sc - 1) & 1)) { ok = false; break; }
       tc_fence_after();
       // ---- the piece's result: out, or a partial
-      const int first = (int)(it.u0 / per), last = (int)((it.u0 + w.nb[t] - 1) / per);
+      const int first = it.first_cta(per), last = it.last_cta(per, w.nb[t] - 1);
       auto part_of = [&](int cta) {   // this tile's O [HD / 4][128] float4, then (m, l)
         return parts + ((int64_t)cta * 2 + (cta == first ? 1 : 0)) * C::PART + t * (kPtRows * HD + 2 * kPtRows);
       };
       auto flag_of = [&](int cta) {
         return reinterpret_cast<int*>(parts + ((int64_t)cta * 2 + (cta == first ? 1 : 0)) * C::PART + 2 * (kPtRows * HD + 2 * kPtRows)) + t;
       };
-      int odd = I8 ? 0 : *(volatile int*)odd_s;   // set by this item's V or an earlier one's: a look too many costs time only
+      int odd = *(volatile int*)odd_s;   // set by this item's V or an earlier one's: a look too many costs time only
       bool join = false;
       if (first != last) {
         float4* po = reinterpret_cast<float4*>(part_of((int)blockIdx.x));
@@ -623,7 +695,7 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
           float mm = -INFINITY, ll = 0.f;
           for (int c = first; c <= last; ++c) {
             mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(part_of(c) + kPtRows * HD) + r).x);
-            odd |= I8 ? 0 : __ldcg(flag_of(c));
+            odd |= __ldcg(flag_of(c));
           }
           const float base = mm == -INFINITY ? 0.f : mm;
           for (int c = first; c <= last; ++c) {
@@ -660,14 +732,17 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
           }
         }
       }
-      if (!I8 && odd && live && (first == last || join)) {
+      if (odd && live && (first == last || join)) {
         // infinities and NaN among the values of the item's own new tokens: to the rows that see them
+#pragma unroll 1
         for (int j = max(w.open(0, R), 0); j < lim; ++j) {
           const int page = p.table[(int64_t)it.b * p.max_pages + (j >> p.page_log2)];
           if ((unsigned)page >= (unsigned)p.n_pages) continue;
-          const bf16* v = static_cast<const bf16*>(p.v) + paged_vec(p, page, j, it.h) * HD;
+          const int64_t vec = paged_vec(p, page, j, it.h);
+          if (I8 && p.vs[vec] < INFINITY) continue;
+#pragma unroll 1
           for (int e = 0; e < HD; ++e) {
-            const float x = __bfloat162float(v[e]);
+            const float x = I8 ? NAN : __bfloat162float(static_cast<const bf16*>(p.v)[vec * HD + e]);
             if (!(fabsf(x) < INFINITY)) dst[e] = __float2bfloat16_rn(__bfloat162float(dst[e]) + x);
           }
         }
@@ -675,100 +750,97 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
     }
   } else if (I8) {
     // -------------------------------------------------------------- 8-bit blocks to bf16
-    // a lane's 16 bytes: chunk `chunk` of one key in 16; eight lanes of a store phase hit
-    // all banks (two keys, four chunks two apart, swizzled by key)
-    fewer_registers<112>();
+    // A lane takes 16 bytes of a key at a time and stores 32. Eight lanes of a load or a store phase have
+    // four neighbouring chunks of two keys r and r ^ 5, which in either swizzle hit all banks.
     constexpr int CH = HD / 16;                       // 16-byte chunks of a key
-    constexpr int KPI = 32 / CH;                      // keys a warp reads at once: 4 (hd 128) or 8
-    constexpr int STEPS = kPtKB / (4 * KPI);          // per block: 8 or 4
+    constexpr int STEPS = 16 * CH / 32;               // a warp's 16 keys of a half: 4 or 2
     const int cw = warp - 12;
     const int chunk = HD == 128 ? (lane & 3) + 4 * (lane >> 4) : lane & 3;
-    const int sub = HD == 128 ? (lane >> 2) & 3 : lane >> 2;
-    int blocks = 0;
+    const int sub = lane >> 2;                        // hd 64: eight keys at once; hd 128: four
+    int blocks = 0, taken = 0;
     bool ok = true;
     for (int64_t u = ua; ok && u < ub;) {
-      const PagedItem it = line.item(p, u, lane, err);
-      const PtWork w = pt_work(it, u, ub, R);
-      u = min(ub, it.u0 + it.tiles);
+      const PagedItem<PtCut> it = line.item(p, &u, lane, err);
+      const PtWork w = pt_work(it, ua, ub, R);
       if (w.j0 >= w.j1) continue;
       const int32_t* tab = p.table + (int64_t)it.b * p.max_pages;
-      // lanes 0-7: pages of the block's eight runs of 16 keys
-      auto page_of = [&](int j) {
-        const int place = j * kPtKB + (lane & 7) * 16;
-        int page = place < it.seen ? tab[place >> p.page_log2] : -1;
-        if (place < it.seen && (unsigned)page >= (unsigned)p.n_pages) {
-          set_device_error(err, DEVERR_INDEX);
-          page = -1;
-        }
-        return page;
+      const int open = w.open(0, R);
+      const int id = cw * 32 + lane;   // the key whose scales this thread brings
+      // its vector in block j, or -1
+      auto vec_of = [&](int j) -> int64_t {
+        const int place = j * kPtKB + id;
+        if (place >= it.seen) return -1;
+        const int page = tab[place >> p.page_log2];
+        return (unsigned)page < (unsigned)p.n_pages ? paged_vec(p, page, place, it.h) : -1;
       };
-      auto key_of = [&](int step) { return step * 4 * KPI + cw * KPI + sub; };   // 4 KPI = 16 or 32 keys a step
-      auto fetch = [&](uint4 (&x)[STEPS], const void* pool, int j, int pages) {
+      // half a block to bf16: 64 keys from key 64 h on of a tile; keys past the last visible one: values
+      // of any finite kind will do (their weights are zero), and what lies there was loaded as numbers
+      auto turn = [&](uint32_t tile, int h) {
+        const int st = taken % C::GSTN;
+        if (!all_wait(g_full0 + 8 * st, (taken / C::GSTN) & 1)) return false;
+        const uint8_t* from = smem + (sG0 - sQ) + st * C::GHALF;
+        uint8_t* to = smem + (tile - sQ) + (chunk >> 2) * C::SLAB;
+        const int c = (2 * chunk) & 7;
 #pragma unroll
         for (int k = 0; k < STEPS; ++k) {
-          const int key = key_of(k), place = j * kPtKB + key;
-          const int page = __shfl_sync(0xffffffffu, pages, key >> 4);
-          x[k] = page >= 0 && place < it.seen
-                     ? __ldg(reinterpret_cast<const uint4*>(static_cast<const int8_t*>(pool) + paged_vec(p, page, place, it.h) * HD) + chunk)
-                     : make_uint4(0, 0, 0, 0);
-        }
-      };
-      auto put = [&](const uint4 (&x)[STEPS], uint32_t tile) {
-        uint8_t* t8 = smem + (tile - sQ);
-#pragma unroll
-        for (int k = 0; k < STEPS; ++k) {
-          const int key = key_of(k);
-          const uint32_t in[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+          const int low = HD == 128 ? (2 * (k & 1) + ((sub >> 1) & 1)) ^ ((sub & 1) * 5) : ((sub >> 1) & 3) ^ ((sub & 1) * 5);
+          const int key = cw * 16 + (HD == 128 ? k >> 1 : k) * 8 + low;
+          const uint4 x = HD == 128 ? *reinterpret_cast<const uint4*>(from + key * 128 + ((chunk ^ (key & 7)) << 4))
+                                    : *reinterpret_cast<const uint4*>(from + key * 64 + ((chunk ^ ((key >> 1) & 3)) << 4));
+          const uint32_t in[4] = {x.x, x.y, x.z, x.w};
           uint32_t y[8];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             y[2 * i] = bf16_of_i8(__byte_perm(in[i], 0, 0x4140));
             y[2 * i + 1] = bf16_of_i8(__byte_perm(in[i], 0, 0x4342));
           }
-          uint8_t* row = t8 + (chunk >> 2) * C::SLAB + key * 128;
-          const int c = (2 * chunk) & 7;
+          uint8_t* row = to + (h * 64 + key) * 128;
           *reinterpret_cast<uint4*>(row + ((c ^ (key & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
           *reinterpret_cast<uint4*>(row + (((c + 1) ^ (key & 7)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(g_empty0 + 8 * st);
+        ++taken;
+        return true;
       };
-      uint4 kx[STEPS], vx[STEPS];
-      float ksc, vsc;
-      // thread `id` of the 128 brings the scales of key `id`
-      const int id = cw * 32 + lane;
-      auto fetch_scales = [&](int j, int pages) {
-        const int place = j * kPtKB + id;
-        const int page = __shfl_sync(0xffffffffu, pages, id >> 4);
-        const bool is = page >= 0 && place < it.seen;
-        const int64_t vec = is ? paged_vec(p, page, place, it.h) : 0;
-        ksc = is ? __ldg(p.ks + vec) * scale_log2 : 0.f;
-        vsc = is ? __ldg(p.vs + vec) : 0.f;
-      };
-      int pages = page_of(w.j0);
-      fetch(kx, p.k, w.j0, pages);
-      fetch_scales(w.j0, pages);
+      int64_t vec = vec_of(w.j0), vec_next = w.j0 + 1 < w.j1 ? vec_of(w.j0 + 1) : -1;
+      float ksc = vec >= 0 ? __ldg(p.ks + vec) : 0.f, vsc = vec >= 0 ? __ldg(p.vs + vec) : 0.f;
+#pragma unroll 1
       for (int j = w.j0; j < w.j1; ++j, ++blocks) {
-        fetch(vx, p.v, j, pages);
         const int kst = blocks % KST, vst = blocks % VST;
-        if (!warp_wait(k_empty0 + 8 * kst, ((blocks / KST) & 1) ^ 1)) { ok = false; break; }
-        scales[blocks % C::SC * 2 * kPtKB + id] = ksc;
-        scales[blocks % C::SC * 2 * kPtKB + kPtKB + id] = vsc;
-        put(kx, sK0 + kst * C::TILE);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(sc_full0 + 8 * (blocks % C::SC));
-          mbar_arrive(k_full0 + 8 * kst);
+        if (!all_wait(k_empty0 + 8 * kst, ((blocks / KST) & 1) ^ 1)) { ok = false; break; }
+        // A masked score is -infinity before its scale, which therefore is a positive number: any
+        // for a key of zeros, and for one whose scale is NaN (it held an infinity or a NaN), which
+        // is marked. Such a value, where not every row sees it, is taken out and given to the rows that
+        // see it at the end.
+        const bool bad_k = !(ksc < INFINITY), bad_v = !(vsc < INFINITY) && j * kPtKB + id >= open;
+        if (bad_v) atomicOr(odd_s, 1);
+        float* sc = scales + blocks % C::SC * C::SCW;
+        sc[id] = bad_k || ksc == 0.f ? scale_log2 : ksc * scale_log2;
+        sc[kPtKB + id] = bad_v ? 0.f : vsc;
+        const unsigned marks = __ballot_sync(0xffffffffu, bad_k);
+        if (lane == 0) reinterpret_cast<uint32_t*>(sc + 2 * kPtKB)[cw] = marks;
+        // the next block's scales, its page asked for a block ahead of them
+        vec = vec_next;
+        vec_next = j + 2 < w.j1 ? vec_of(j + 2) : -1;
+        ksc = vec >= 0 ? __ldg(p.ks + vec) : 0.f;
+        vsc = vec >= 0 ? __ldg(p.vs + vec) : 0.f;
+        // keys, then values: one copy of the code for both and their halves
+#pragma unroll 1
+        for (int v = 0; v < 4; ++v) {
+          if (v == 2) ok = all_wait(v_empty0 + 8 * vst, ((blocks / VST) & 1) ^ 1);
+          ok = ok && turn(v < 2 ? sK0 + kst * C::TILE : sV0 + vst * C::TILE, v & 1);
+          if (!ok) break;
+          if (v & 1) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              if (v == 1) mbar_arrive(sc_full0 + 8 * (blocks % C::SC));
+              mbar_arrive(v == 1 ? k_full0 + 8 * kst : v_full0 + 8 * vst);
+            }
+          }
         }
-        if (j + 1 < w.j1) {
-          pages = page_of(j + 1);
-          fetch(kx, p.k, j + 1, pages);
-          fetch_scales(j + 1, pages);
-        }
-        if (!warp_wait(v_empty0 + 8 * vst, ((blocks / VST) & 1) ^ 1)) { ok = false; break; }
-        put(vx, sV0 + vst * C::TILE);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(v_full0 + 8 * vst);
+        if (!ok) break;
       }
     }
   }
@@ -790,11 +862,12 @@ cudaError_t launch_tc(const Paged& p, const void* q, int64_t ld_q, void* out, in
   const int G = p.Hq / p.Hkv, R = kPtRows / G;
   CUtensorMap tq, tk, tv;
   if (!make_tmap_heads(&tq, q, p, ld_q, R)) return cudaErrorInvalidValue;
-  if (I8) tk = tv = tq;   // not used
-  else if (!make_tmap_pages(&tk, p.k, p, false, kPtKB) || !make_tmap_pages(&tv, p.v, p, false, kPtKB)) return cudaErrorInvalidValue;
+  const uint32_t box = I8 ? kPtKB / 2 : kPtKB;
+  if (!make_tmap_pages(&tk, p.k, p, I8, box) || !make_tmap_pages(&tv, p.v, p, I8, box)) return cudaErrorInvalidValue;
+  // no more CTAs than pieces of the least size that any counts could make
   const int64_t span = ((int64_t)p.max_pages << p.page_log2) / kPtKB + 1;
   const int64_t groups = std::min<int64_t>((int64_t)p.B * ((p.max_new + 2 * R - 1) / (2 * R)), p.n_rows);
-  const int64_t most = std::max<int64_t>(1, (groups * p.Hkv * span + kPtMinTiles - 1) / kPtMinTiles);
+  const int64_t most = std::max<int64_t>(1, (groups * p.Hkv * (span + kPtPad) + kPtPad) / (kPtPad + 1));
   return launch_pdl(paged_tc_kernel<HD, I8>, dim3((unsigned)std::min<int64_t>(most, std::min(dev.num_sms, kPtMaxCtas))),
                     dim3(C::THREADS), (size_t)C::SMEM, dev.stream, tq, tk, tv, p, static_cast<bf16*>(out),
                     1.4426950408889634f / sqrtf((float)HD), sync, static_cast<float*>(scratch), dev.err, kWaitTimeoutNs);

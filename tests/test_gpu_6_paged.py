@@ -501,3 +501,69 @@ def test_binding_refuses(A):
         A.adadsf_paged_append(cfg, cache, batch, z(2, 500), None)
     with pytest.raises(A.AdadsfError):
         A.adadsf_paged_append(cfg, cache, batch, z(2, 512), None)                 # a rotary model needs its table
+
+
+# ------------------------------------------------------------------ long contexts of chunks, masked infinities
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("heads", [(28, 4, 128, "bf16"), (12, 12, 64, "bf16")], ids=str)
+def test_attention_long_chunks(A, heads, store):
+    """Chunks over more keys than those whose weights enter the products in two parts: a
+    weight then is one bf16 (off by 2^-8 of itself at most, as the output's rounding is),
+    which the bound of this test adds to the others."""
+    w = World(A, shape_of(*heads), store, 64, [(40, 5000), (150, 2300), (1, 4097), (300, 700)], seed=15)
+    q = queries(w)
+    ref, bound = attend64(w, q)
+    got = attend(A, w, q).double()
+    a = bound / (2.0 ** -8 + 2.0 ** -17)      # at least softmax |V|
+    assert ((got - ref).abs() <= bound + (2.0 ** -8 + 2.0 ** -16) * a).all()
+
+
+def _spoil(w, what, b, place, feature):
+    """Makes a cached key or value of sequence b hold an infinity or a NaN, in the pool and in the
+    reference; an 8-bit vector becomes NaN as a whole (a NaN scale, numbers zero)."""
+    page, slot = int(w.table[b, place // w.page]), place % w.page
+    pool, scale, ref = (w.k, w.ks, w.K) if what[0] == "k" else (w.v, w.vs, w.V)
+    bad = {"inf": math.inf, "-inf": -math.inf, "nan": math.nan}[what[1]]
+    if scale is not None:
+        pool[page, 1, slot] = 0
+        scale[page, 1, slot] = math.nan
+        ref[b][place, 1] = math.nan
+    else:
+        pool[page, 1, slot, feature] = bad
+        ref[b][place, 1, feature] = bad
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("new", [1, 3, 60, 200])
+@pytest.mark.parametrize("heads", [(28, 4, 128, "bf16"), (8, 8, 64, "bf16"), (8, 2, 128, "bf16"), (8, 8, 64, "f32")], ids=str)
+def test_attention_infinities_of_later_tokens(A, heads, new, store):
+    """Infinities and NaN in keys and values of new tokens and of old ones: rows that do not
+    see them are as if they were not there, rows that see them are infinite or NaN
+    where the formula is."""
+    w = World(A, shape_of(*heads), store, 32, [(new, 300), (new, new), (new, 150)], seed=new)
+    clean = [[x.clone() for x in t] for t in (w.K, w.V)]
+    _spoil(w, ("v", "inf"), 0, 299, 5)
+    _spoil(w, ("v", "nan"), 1, new - 1, 63)
+    if new > 2:
+        _spoil(w, ("v", "-inf"), 0, 298, 17)
+        _spoil(w, ("v", "inf"), 1, new // 2, 0)
+        _spoil(w, ("k", "nan"), 2, 150 - new // 3, 9)
+    q = queries(w, scale=0.5)
+    out = attend(A, w, q).double().reshape(w.n_rows, w.shape.n_heads, w.shape.head_dim)
+    bad = [w.K, w.V]
+    w.K, w.V = clean
+    ref, bound = (t.reshape(out.shape) for t in attend64(w, q))
+    G, r = w.shape.n_heads // w.shape.n_kv_heads, 0
+    for b, (n, l) in enumerate(w.seqs):
+        for i in range(n):
+            seen = max(0, l - n + i + 1)
+            mine = slice(G, 2 * G)                                         # the query heads of key/value head 1
+            want = torch.ones(w.shape.n_heads, w.shape.head_dim, dtype=torch.bool, device="cuda")
+            if not torch.isfinite(bad[0][b][:seen, 1]).all():
+                want[mine] = False
+            else:
+                want[mine] = torch.isfinite(bad[1][b][:seen, 1]).all(0)
+            got = torch.isfinite(out[r])
+            assert torch.equal(got, want), (b, i)
+            assert ((out[r] - ref[r]).abs()[want] <= bound[r][want]).all(), (b, i)
+            r += 1
