@@ -5,12 +5,17 @@
 // key = larger logit), each CTA a contiguous slice, each thread a contiguous chunk of
 // it (an odd number of words, so that a warp's chunks spread over the banks), so logits
 // are read from memory once. Kept tokens are a prefix of the descending order, so a
-// cut (key, number of equal ones kept) describes them. Cuts come from a radix
-// search over 11, 11 and 10 bits: a histogram per CTA, of counts (top-k) or of
-// weights (top-p), every CTA then adds up all of them through distributed shared
-// memory and finds the same bin. Weights are whole multiples of 2^-40 of the
-// largest, so their sums do not depend on order, and neither does the token.
+// cut (key, number of equal ones kept) describes them. A cut is found by histograms of counts
+// (top-k) or of weights (top-p): every CTA makes its own, then adds up all of them through distributed
+// shared memory and finds the same bin. The first histogram's bins are even in the logits'
+// distance from the largest (bins of the keys' leading bits, four to an octave, put the bulk of a row
+// into a few of them, and its atomics into one queue), the next ones' even in the keys of the bin
+// found, down to one key. Weights are whole multiples of 2^-40 of the largest, so
+// their sums do not depend on order, and neither does the token.
+// A row is bound by latency: four to eight rounds over the cluster, each about a microsecond and a half.
 #include <math.h>
+
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -22,9 +27,11 @@ constexpr int kSmWarps = kSmThreads / 32;
 constexpr int kSmBins = 2048;
 constexpr int kSmMostChunk = 97;          // words of a thread: 8 x 512 x 97 tokens
 constexpr int kSmMostCluster = 8;
-constexpr int kSmSmem = kSmThreads * kSmMostChunk * 4;
+constexpr int kSmSmem = kSmThreads * kSmMostChunk * 4 + 16;
 static_assert(kSmMostCluster * kSmThreads * kSmMostChunk == kSampleMaxV, "the limit that the header states");
 constexpr uint32_t kSmNone = 0x007fffffu; // key of -infinity; padding lies below it
+constexpr float kSmCountBins = 2047.f / 40.f;   // first bins: a logit unit, and a unit of z (weights end at 28)
+constexpr float kSmWeightBins = 2047.f / 28.f;
 constexpr float kSmUnit = 1099511627776.f;   // 2^40
 
 typedef unsigned long long u64;
@@ -144,9 +151,21 @@ __device__ __forceinline__ void find_bin(SampleShared& s, u64 base, double targe
   cluster_sync();   // histograms are read, and the results of this CTA visible
 }
 
+// Four consecutive elements, 16 or 8 aligned bytes.
+__device__ __forceinline__ uint4 keys_of4(const float* p) {
+  const float4 v = *reinterpret_cast<const float4*>(p);
+  return make_uint4(key_of(v.x), key_of(v.y), key_of(v.z), key_of(v.w));
+}
+__device__ __forceinline__ uint4 keys_of4(const bf16* p) {
+  float f[4];
+  load4(p, f);
+  return make_uint4(key_of(f[0]), key_of(f[1]), key_of(f[2]), key_of(f[3]));
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, int chunk) {
-  extern __shared__ __align__(16) uint32_t keys[];   // [kSmThreads][chunk]
+  constexpr int KS = sizeof(T) == 2 ? 16 : 0;        // bits of a key that its type leaves alone
+  extern __shared__ __align__(16) uint32_t raw[];    // [kSmThreads][chunk], shifted by up to three words
   __shared__ __align__(16) SampleShared s;
   pdl_wait();
   pdl_trigger();
@@ -154,13 +173,27 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   const uint32_t n_cta = cluster_nctarank(), rank = cluster_ctarank();
   const int row = blockIdx.x / n_cta;
   const int slice = kSmThreads * chunk, i0 = (int)rank * slice;
-  const T* x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+  const T* x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld + i0;
+  // groups of four elements that are aligned in memory, aligned in shared memory too
+  const int shift = (int)((reinterpret_cast<uintptr_t>(x) / sizeof(T)) & 3);
+  uint32_t* keys = raw + shift;
+  const int there = min(max(a.V - i0, 0), slice);
   uint32_t most = 0;
-  for (int i = tid; i < slice; i += kSmThreads) {
-    const uint32_t k = i0 + i < a.V ? key_of(Elem<T>::to_f(x[i0 + i])) : 0u;
-    keys[i] = k;
-    most = max(most, k);
+#pragma unroll 4
+  for (int g = tid; 4 * g < there + shift; g += kSmThreads) {
+    const int i = 4 * g - shift;
+    if (i >= 0 && i + 4 <= there) {
+      const uint4 k = keys_of4(x + i);
+      *reinterpret_cast<uint4*>(raw + 4 * g) = k;
+      most = max(max(most, max(k.x, k.y)), max(k.z, k.w));
+    } else {
+      for (int e = max(i, 0); e < min(i + 4, there); ++e) {
+        keys[e] = key_of(Elem<T>::to_f(x[e]));
+        most = max(most, keys[e]);
+      }
+    }
   }
+  for (int i = there + tid; i < slice; i += kSmThreads) keys[i] = 0;
   most = __reduce_max_sync(0xffffffffu, most);
   if (lane == 0) s.warp[tid >> 5] = most;
   __syncthreads();
@@ -219,68 +252,103 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   uint32_t cut_key = 0;
   u64 cut_ties = ~0ull;       // ~0: all
   bool some_ties = false;     // fewer than there are
-  const int shifts[3] = {21, 10, 0}, masks[3] = {0x7ff, 0x7ff, 0x3ff};
+  // One search. key_in: whether a key takes part; more: weight of `more_key` beside those (0: none). In: the target, or
+  // frac < 1 of the whole (see find_bin), which it leaves in target. Out: the key, and in s.found_*.
+  auto search = [&](auto weights_c, auto key_in, uint32_t more_key, u64 more, double& target, double frac) -> uint32_t {
+    constexpr bool W = decltype(weights_c)::value;
+    const float per = W ? kSmWeightBins : kSmCountBins;
+    auto bin0 = [&](uint32_t k) -> int {   // falls with the key, slowly or not at all
+      if (k == most) return 0;
+      if (k <= kSmNone) return kSmBins - 1;
+      const float d = W ? -logit_of(k) : __fsub_rn(top, value_of(k));
+      return (int)fminf(__fmul_rn(d, per), (float)(kSmBins - 1));   // NaN: the last one
+    };
+    auto add = [&](int bin, u64 w) {
+      const uint32_t lo = (uint32_t)w;
+      uint32_t hi = (uint32_t)(w >> 32);
+      if (W) {
+        if (lo) hi += atomicAdd(&s.lo[bin], lo) > 0xffffffffu - lo;   // the carry
+        if (hi) atomicAdd(&s.hi[bin], hi);
+      } else {
+        atomicAdd(&s.lo[bin], lo);
+      }
+    };
+    auto clear = [&] {
+      for (int i = tid; i < kSmBins; i += kSmThreads) {
+        s.lo[i] = 0;
+        if (W) s.hi[i] = 0;
+      }
+      __syncthreads();
+    };
+    clear();
+    for (int i = 0; i < chunk; ++i) {
+      const uint32_t k = own[i];
+      if (!key_in(k)) continue;
+      if (W) {
+        const u64 w = weight(chance(k));
+        if (w) add(bin0(k), w);
+      } else {
+        add(bin0(k), 1);
+      }
+    }
+    if (more && rank == 0 && tid == 0) add(bin0(more_key), more);
+    find_bin<W>(s, 0, target, frac);
+    if (frac < 1.0) target = fmax(frac * (double)s.found_all, 1.0);
+    // keys that can lie in the bin, with room for roundings
+    const int bin = (int)s.found_bin;
+    const float unit = W ? t / per : 1.f / per;
+    const float far = top - (float)(bin + 1) * unit, near = top - (float)bin * unit;
+    const float room = 1e-5f * (fabsf(top) + fabsf(far) + (float)(bin + 2) * unit);
+    uint32_t lo = far - room > -INFINITY && bin < kSmBins - 1 ? key_of(far - room) : 0u;
+    uint32_t hi = near + room < INFINITY && bin > 0 ? min(key_of(near + room), most) : most;
+    lo >>= KS;
+    hi >>= KS;
+    while (lo < hi) {
+      const int bits = max(0, 32 - __clz(hi - lo) - 11);   // (hi - lo) >> bits is below kSmBins
+      auto at = [&](uint32_t k) { return (k >> KS) >= lo && (k >> KS) <= hi && bin0(k) == bin; };
+      const u64 before = s.found_before;
+      __syncthreads();
+      clear();
+      for (int i = 0; i < chunk; ++i) {
+        const uint32_t k = own[i];
+        if (key_in(k) && at(k)) add((int)((hi - (k >> KS)) >> bits), W ? weight(chance(k)) : 1);
+      }
+      if (more && rank == 0 && tid == 0 && at(more_key)) add((int)((hi - (more_key >> KS)) >> bits), more);
+      find_bin<W>(s, before, target, 1.0);
+      hi -= s.found_bin << bits;
+      if (hi - lo > (1u << bits) - 1) lo = hi - ((1u << bits) - 1);
+    }
+    // a key whose low bits are its type's: zeros above 0, ones below
+    return KS == 0 ? hi : (hi & (0x80000000u >> KS)) ? hi << KS : (hi << KS) | ((1u << KS) - 1);
+  };
   const int k = a.top_k ? a.top_k[row] : 0;
   if (k > 0 && k < a.V) {
-    uint32_t prefix = 0;
-    u64 above = 0;
-    for (int lv = 0; lv < 3; ++lv) {
-      for (int i = tid; i < kSmBins; i += kSmThreads) s.lo[i] = 0;
-      __syncthreads();
-      for (int i = 0; i < chunk; ++i) {
-        const uint32_t key = own[i];
-        if (lv == 0 || (key >> shifts[lv - 1]) == prefix)
-          atomicAdd(&s.lo[kSmBins - 1 - ((key >> shifts[lv]) & masks[lv])], 1u);
-      }
-      find_bin<false>(s, above, (double)k, 1.0);
-      prefix = (prefix << (lv == 2 ? 10 : 11)) | (kSmBins - 1 - s.found_bin);
-      above = s.found_before;
-      cut_ties = (u64)k - above;
-      some_ties = cut_ties < s.found_in;
-    }
-    cut_key = prefix;
+    double target = (double)k;
+    cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, target, 1.0);
+    cut_ties = (u64)k - s.found_before;
+    some_ties = cut_ties < s.found_in;
+    __syncthreads();
   }
   const float top_p = a.top_p ? a.top_p[row] : 1.f;
   if (top_p < 1.f) {
     const uint32_t k_key = cut_key;
     const u64 k_ties = cut_ties;
-    uint32_t prefix = 0;
     double target = 0.0;
-    u64 before = 0;
-    for (int lv = 0; lv < 3; ++lv) {
-      for (int i = tid; i < kSmBins; i += kSmThreads) s.lo[i] = s.hi[i] = 0;
-      __syncthreads();
-      auto add = [&](uint32_t key, u64 w) {
-        const int bin = kSmBins - 1 - ((key >> shifts[lv]) & masks[lv]);
-        const uint32_t lo = (uint32_t)w;
-        uint32_t hi = (uint32_t)(w >> 32);
-        if (lo) hi += atomicAdd(&s.lo[bin], lo) > 0xffffffffu - lo;   // the carry
-        if (hi) atomicAdd(&s.hi[bin], hi);
-      };
-      auto at_level = [&](uint32_t key) { return lv == 0 || (key >> shifts[lv - 1]) == prefix; };
-      for (int i = 0; i < chunk; ++i) {
-        const uint32_t key = own[i];
-        if (at_level(key) && (key > k_key || (key == k_key && k_ties == ~0ull))) add(key, weight(chance(key)));
-      }
-      // the kept ones among the equals of top-k's last
-      if (rank == 0 && tid == 0 && k_ties != ~0ull && at_level(k_key)) add(k_key, k_ties * weight(chance(k_key)));
-      find_bin<true>(s, before, target, lv == 0 ? (double)top_p : 1.0);
-      if (lv == 0) target = fmax((double)top_p * (double)s.found_all, 1.0);
-      prefix = (prefix << (lv == 2 ? 10 : 11)) | (kSmBins - 1 - s.found_bin);
-      before = s.found_before;
-    }
-    const u64 one = weight(chance(prefix));
+    // of the equals of top-k's last, the kept ones
+    const uint32_t key = search(std::true_type(), [&](uint32_t q) { return q > k_key || (q == k_key && k_ties == ~0ull); }, k_key,
+                                k_ties == ~0ull ? 0 : k_ties * weight(chance(k_key)), target, (double)top_p);
+    const u64 one = weight(chance(key)), before = s.found_before;
     if (one > 0) {
       // the fewest equals whose weight takes the sum to the target
       u64 n = (u64)fmax(ceil((target - (double)before) / (double)one), 1.0);
       while (n > 1 && (double)(before + (n - 1) * one) >= target) --n;
       while ((double)(before + n * one) < target) ++n;
-      const u64 there = s.found_in / one;
-      if (n < there || prefix != k_key) some_ties = n < there;
-      cut_key = prefix;
-      cut_ties = n < there ? n : there;
-      if (!some_ties) cut_ties = ~0ull;
+      const u64 all = s.found_in / one;
+      if (n < all || key != k_key) some_ties = n < all;
+      cut_key = key;
+      cut_ties = n < all ? n : all;
     }
+    __syncthreads();
   }
   uint32_t last = 0xffffffffu;   // equals of cut_key are kept up to this index
   if (some_ties) last = nth(cut_key, cut_ties);
@@ -295,6 +363,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     return w < min_p ? 0 : weight(w);
   };
   u64 sum = 0, all;
+#pragma unroll 4
   for (int i = 0; i < chunk; ++i) sum += kept(i);
   u64 before = cluster_before(sum, s, &all);
   const double mark_d = (double)a.u[row] * (double)all;
@@ -326,7 +395,7 @@ cudaError_t sample(int dtype, const Sample& a, const Dev& dev) {
     const cudaError_t e = allow_smem<sample_kernel<T>, kSmSmem>();
     if (e != cudaSuccess) return e;
     return launch_pdl_cluster(sample_kernel<T>, dim3((unsigned)(a.B * n_cta)), dim3(kSmThreads),
-                              (size_t)kSmThreads * chunk * 4, dev.stream, n_cta, a, chunk);
+                              (size_t)kSmThreads * chunk * 4 + 16, dev.stream, n_cta, a, chunk);
   };
   return dtype == kBF16 ? run(bf16()) : run(0.f);
 }
