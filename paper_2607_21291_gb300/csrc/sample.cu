@@ -24,14 +24,17 @@ namespace {
 
 constexpr int kSmThreads = 512;
 constexpr int kSmWarps = kSmThreads / 32;
-constexpr int kSmBins = 2048;
+constexpr int kSmBinsLog2 = 9, kSmBins = 1 << kSmBinsLog2;
+static_assert(kSmBins == kSmThreads, "a thread a bin");
 constexpr int kSmMostChunk = 97;          // words of a thread: 8 x 512 x 97 tokens
 constexpr int kSmMostCluster = 8;
 constexpr int kSmSmem = kSmThreads * kSmMostChunk * 4 + 16;
 static_assert(kSmMostCluster * kSmThreads * kSmMostChunk == kSampleMaxV, "the limit that the header states");
 constexpr uint32_t kSmNone = 0x007fffffu; // key of -infinity; padding lies below it
-constexpr float kSmCountBins = 2047.f / 40.f;   // first bins: a logit unit, and a unit of z (weights end at 28)
-constexpr float kSmWeightBins = 2047.f / 28.f;
+// First bins: the last takes what lies further from the largest logit (or from z = 0), most of a row as
+// a rule, which threads sum up for themselves before they add it.
+// A cut that lies there is looked for in a second set of bins, to kSmEnd (weights end at 28).
+constexpr float kSmFar = 10.f, kSmEnd = 32.f;
 constexpr float kSmUnit = 1099511627776.f;   // 2^40
 
 typedef unsigned long long u64;
@@ -44,14 +47,6 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
-}
-__device__ __forceinline__ uint4 ld_cluster_u32x4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(addr)
-               : "memory");
-  return v;
 }
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   uint32_t v;
@@ -68,10 +63,13 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
 }
 
 struct SampleShared {
-  uint32_t lo[kSmBins], hi[kSmBins];   // histogram: counts in lo, or weights in (lo, hi)
+  // Histograms: counts in lo, or weights in (lo, hi). Rounds over the cluster take turns with two of
+  // everything that other CTAs read, so one barrier a round is enough.
+  uint32_t lo[2][kSmBins], hi[2][kSmBins];
+  u64 total[2];                        // this CTA's total
+  u64 bins[2][kSmBins];                // sums over the cluster of this CTA's share of the bins
   u64 warp[kSmWarps];                  // block scan
-  u64 total;                           // this CTA's total, read by the cluster
-  u64 found_before, found_in, found_all;
+  u64 found_before, found_in, found_all, found_target;
   uint32_t found_bin;
   uint32_t most;                       // this CTA's largest key, read by the cluster
   uint32_t index;                      // written by the CTA that finds it
@@ -100,55 +98,72 @@ __device__ __forceinline__ u64 block_before(u64 v, SampleShared& s, u64* all) {
   return base + inc - v;
 }
 
-// The same over the cluster's threads, CTAs in order of their slices.
-__device__ __forceinline__ u64 cluster_before(u64 v, SampleShared& s, u64* all) {
+// The same over the cluster's threads, CTAs in order of their slices. A round of the cluster.
+__device__ __forceinline__ u64 cluster_before(u64 v, SampleShared& s, int& round, u64* all) {
   u64 mine;
   u64 before = block_before(v, s, &mine);
   const uint32_t n = cluster_nctarank(), rank = cluster_ctarank();
-  if (threadIdx.x == 0) s.total = mine;
+  const int q = round++ & 1;
+  if (threadIdx.x == 0) s.total[q] = mine;
   cluster_sync();
   u64 sum = 0;
-  for (uint32_t c = 0; c < n; ++c) {
-    const u64 t = ld_cluster_u64(map_to_cta(smem_u32(&s.total), c));
+#pragma unroll
+  for (uint32_t c = 0; c < kSmMostCluster; ++c) {
+    const u64 t = c < n ? ld_cluster_u64(map_to_cta(smem_u32(&s.total[q]), c)) : 0;
     if (c < rank) before += t;
     sum += t;
   }
-  cluster_sync();   // read by all: the next call may write
   *all = sum;
   return before;
 }
 
-// Adds up the cluster's histograms, whose bins run from the largest keys down, and finds the
+// The smallest whole number whose double is `target` or more: compared with it, whole sums need no doubles.
+__device__ __forceinline__ u64 whole_target(double target) {
+  u64 v = (u64)ceil(target);
+  while (v > 0 && (double)(v - 1) >= target) --v;
+  return v;
+}
+
+// Adds up the cluster's histograms number `q`, whose bins run from the largest keys down, and finds the
 // first bin that takes the running sum, from `base` on, to `target` or more. frac < 1: the
-// target is frac times the sum of all bins (at least 1). Results in s.found_*.
+// target is frac times the sum of all bins (at least 1), left in s.found_target. Results in s.found_*.
+// Each CTA adds up a share of the bins and all read the sums (every CTA reading every histogram took 8 us
+// a round, 11-bit ones 25: 16 words a thread cross the cluster's network slowly).
 template <bool WEIGHTS>
-__device__ __forceinline__ void find_bin(SampleShared& s, u64 base, double target, double frac) {
-  const uint32_t n = cluster_nctarank();
+__device__ __forceinline__ void find_bin(SampleShared& s, int q, u64 base, u64 target, double frac) {
+  const uint32_t n = cluster_nctarank(), rank = cluster_ctarank();   // 1, 2, 4 or 8
+  const uint32_t share = kSmBins / n;
+  const int tid = threadIdx.x;
   cluster_sync();   // every CTA's histogram is complete
-  const int b0 = 4 * threadIdx.x;
-  u64 v[4] = {0, 0, 0, 0};
-  for (uint32_t c = 0; c < n; ++c) {
-    const uint4 lo = ld_cluster_u32x4(map_to_cta(smem_u32(s.lo + b0), c));
-    v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
-    if (WEIGHTS) {
-      const uint4 hi = ld_cluster_u32x4(map_to_cta(smem_u32(s.hi + b0), c));
-      v[0] += (u64)hi.x << 32; v[1] += (u64)hi.y << 32; v[2] += (u64)hi.z << 32; v[3] += (u64)hi.w << 32;
-    }
+  u64 v;
+  if (n > 1) {
+    const uint32_t c = tid & (n - 1), bin = rank * share + tid / n;
+    v = ld_cluster_u32(map_to_cta(smem_u32(&s.lo[q][bin]), c));
+    if (WEIGHTS) v += (u64)ld_cluster_u32(map_to_cta(smem_u32(&s.hi[q][bin]), c)) << 32;
+    for (uint32_t o = 1; o < n; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (c == 0) s.bins[q][tid / n] = v;
+    cluster_sync();
+    v = ld_cluster_u64(map_to_cta(smem_u32(&s.bins[q][tid & (share - 1)]), tid / share));
+  } else {
+    v = s.lo[q][tid];
+    if (WEIGHTS) v += (u64)s.hi[q][tid] << 32;
   }
   u64 all;
-  u64 run = base + block_before(v[0] + v[1] + v[2] + v[3], s, &all);
-  if (frac < 1.0) target = fmax(frac * (double)all, 1.0);
-  if (threadIdx.x == 0) s.found_all = all;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((double)run < target && (double)(run + v[i]) >= target) {
-      s.found_bin = b0 + i;
-      s.found_before = run;
-      s.found_in = v[i];
+  const u64 run = base + block_before(v, s, &all);
+  if (frac < 1.0) {
+    if (tid == 0) {
+      s.found_all = all;
+      s.found_target = whole_target(fmax(frac * (double)all, 1.0));
     }
-    run += v[i];
+    __syncthreads();
+    target = s.found_target;
   }
-  cluster_sync();   // histograms are read, and the results of this CTA visible
+  if (run < target && run + v >= target) {
+    s.found_bin = tid;
+    s.found_before = run;
+    s.found_in = v;
+  }
+  __syncthreads();
 }
 
 // Four consecutive elements, 16 or 8 aligned bytes.
@@ -206,7 +221,6 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   for (uint32_t c = 0; c < n_cta; ++c) most = max(most, ld_cluster_u32(map_to_cta(smem_u32(&s.most), c)));
 
   const uint32_t* own = keys + tid * chunk;
-  const int own0 = i0 + tid * chunk;
   const float t = a.temperature ? a.temperature[row] : 1.f;
   const float inv = 1.f / t, top = value_of(most);
   auto logit_of = [&](uint32_t k) { return k == most ? 0.f : __fmul_rn(__fsub_rn(value_of(k), top), inv); };
@@ -215,28 +229,53 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     const float w = expf(logit_of(k));
     return w >= 0.f ? w : 0.f;               // NaN (an infinite logit under an infinite temperature)
   };
-  auto weight = [&](float w) { return __float2ull_rn(w * kSmUnit); };
+  // w 2^40 to the nearest whole number: a float of 2^24 or more is one, shifted
+  auto weight = [&](float w) -> u64 {
+    const float y = w * kSmUnit;
+    const uint32_t bits = __float_as_uint(y);
+    return y < 16777216.f ? (u64)__float2uint_rn(y) : (u64)((bits & 0x7fffffu) | 0x800000u) << ((bits >> 23) - 150);
+  };
+  int round = 0;
+  // Where, in the slice, a running sum passes `mark`, if that is in this warp's part: `before` and `sum` are
+  // each thread's, value(i) the summands. The warp takes the thread's chunk 32 at a time. -1: elsewhere.
+  auto walk = [&](u64 before, u64 sum, u64 mark, auto value) -> int {
+    const unsigned has = __ballot_sync(0xffffffffu, before <= mark && mark < before + sum);
+    if (!has) return -1;
+    const int from = __ffs(has) - 1;
+    u64 run = __shfl_sync(0xffffffffu, before, from);
+    const int first = ((tid & ~31) + from) * chunk;
+    for (int i = 0;; i += 32) {
+      u64 inc = i + lane < chunk ? value(first + i + lane) : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, run + inc > mark);
+      if (past) return first + i + __ffs(past) - 1;
+      if (i + 32 >= chunk) return first + chunk - 1;   // not reached: the sums say that it is here
+      run += __shfl_sync(0xffffffffu, inc, 31);
+    }
+  };
   // index of the n-th (from 1) key equal to k in the order of the vocabulary, in every CTA
   auto nth = [&](uint32_t k, u64 n) -> uint32_t {
     int c = 0;
+#pragma unroll 4
     for (int i = 0; i < chunk; ++i) c += own[i] == k;
     u64 all;
-    u64 before = cluster_before((u64)c, s, &all);
-    if (before < n && n <= before + c) {
-      int i = -1;
-      while (before < n) before += own[++i] == k;
-      for (uint32_t q = 0; q < n_cta; ++q) st_cluster_u32(map_to_cta(smem_u32(&s.index), q), (uint32_t)(own0 + i));
-    }
+    const u64 before = cluster_before((u64)c, s, round, &all);
+    const int i = walk(before, (u64)c, n - 1, [&](int i) -> u64 { return keys[i] == k; });
+    if (i >= 0 && lane < (int)n_cta) st_cluster_u32(map_to_cta(smem_u32(&s.index), lane), (uint32_t)(i0 + i));
     cluster_sync();
     return s.index;
   };
 
   if (most <= kSmNone) {   // nothing to draw
-    cluster_sync();        // no CTA leaves while another reads its shared memory
     if (rank == 0 && tid == 0) {
       a.token[row] = -1;
       if (a.logprob) a.logprob[row] = -INFINITY;
     }
+    cluster_sync();        // no CTA leaves while another reads its shared memory
     return;
   }
   if (!(t > 0.f)) {
@@ -252,69 +291,77 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   uint32_t cut_key = 0;
   u64 cut_ties = ~0ull;       // ~0: all
   bool some_ties = false;     // fewer than there are
-  // One search. key_in: whether a key takes part; more: weight of `more_key` beside those (0: none). In: the target, or
-  // frac < 1 of the whole (see find_bin), which it leaves in target. Out: the key, and in s.found_*.
-  auto search = [&](auto weights_c, auto key_in, uint32_t more_key, u64 more, double& target, double frac) -> uint32_t {
+  // One search. key_in: whether a key takes part; more: weight of `more_key` beside those (0: none); target: as
+  // find_bin takes it. Out: the key, and in s.found_* the sums before and of it.
+  auto search = [&](auto weights_c, auto key_in, uint32_t more_key, u64 more, u64 target, double frac) -> uint32_t {
     constexpr bool W = decltype(weights_c)::value;
-    const float per = W ? kSmWeightBins : kSmCountBins;
+    constexpr float kNear = (kSmBins - 1) / kSmFar, kBeyond = (kSmBins - 1) / (kSmEnd - kSmFar);
+    bool beyond = false;   // the second set, of the first one's last bin; other keys: -1
     auto bin0 = [&](uint32_t k) -> int {   // falls with the key, slowly or not at all
-      if (k == most) return 0;
-      if (k <= kSmNone) return kSmBins - 1;
-      const float d = W ? -logit_of(k) : __fsub_rn(top, value_of(k));
-      return (int)fminf(__fmul_rn(d, per), (float)(kSmBins - 1));   // NaN: the last one
+      const float d = k == most ? 0.f : k <= kSmNone ? INFINITY : W ? -logit_of(k) : __fsub_rn(top, value_of(k));
+      const int bin = (int)fminf(__fmul_rn(d, kNear), (float)(kSmBins - 1));   // NaN: the last one
+      if (!beyond) return bin;
+      if (bin < kSmBins - 1) return -1;
+      const float e = __fsub_rn(d, kSmFar);
+      return e < 0.f ? 0 : (int)fminf(__fmul_rn(e, kBeyond), (float)(kSmBins - 1));
     };
-    auto add = [&](int bin, u64 w) {
-      const uint32_t lo = (uint32_t)w;
-      uint32_t hi = (uint32_t)(w >> 32);
-      if (W) {
-        if (lo) hi += atomicAdd(&s.lo[bin], lo) > 0xffffffffu - lo;   // the carry
-        if (hi) atomicAdd(&s.hi[bin], hi);
-      } else {
-        atomicAdd(&s.lo[bin], lo);
-      }
-    };
-    auto clear = [&] {
-      for (int i = tid; i < kSmBins; i += kSmThreads) {
-        s.lo[i] = 0;
-        if (W) s.hi[i] = 0;
-      }
+    // the histogram of the next round: bin_of(key) < 0 takes no part
+    auto count = [&](auto bin_of) -> int {
+      const int q = round++ & 1;
+      s.lo[q][tid] = 0;
+      if (W) s.hi[q][tid] = 0;
       __syncthreads();
-    };
-    clear();
-    for (int i = 0; i < chunk; ++i) {
-      const uint32_t k = own[i];
-      if (!key_in(k)) continue;
-      if (W) {
-        const u64 w = weight(chance(k));
-        if (w) add(bin0(k), w);
-      } else {
-        add(bin0(k), 1);
+      auto put = [&](int bin, u64 w) {
+        if (!W) {
+          atomicAdd(&s.lo[q][bin], (uint32_t)w);
+          return;
+        }
+        const uint32_t lo = (uint32_t)w;
+        const uint32_t hi = (uint32_t)(w >> 32) + (lo && atomicAdd(&s.lo[q][bin], lo) > 0xffffffffu - lo);
+        if (hi) atomicAdd(&s.hi[q][bin], hi);
+      };
+      u64 rest = 0;   // of the last bin
+#pragma unroll 2
+      for (int i = 0; i < chunk; ++i) {
+        const uint32_t k = own[i];
+        const int bin = key_in(k) ? bin_of(k) : -1;
+        if (bin < 0) continue;
+        const u64 w = W ? weight(chance(k)) : 1;
+        if (bin == kSmBins - 1) rest += w;   // most of a row in the first round
+        else put(bin, w);
       }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+      if (lane == 0 && rest) put(kSmBins - 1, rest);
+      if (W && more && rank == 0 && tid == 0) {
+        const int bin = bin_of(more_key);
+        if (bin >= 0) put(bin, more);
+      }
+      return q;
+    };
+    find_bin<W>(s, count(bin0), 0, target, frac);
+    if (frac < 1.0) target = s.found_target;
+    if (s.found_bin == kSmBins - 1) {
+      const u64 before = s.found_before;
+      beyond = true;
+      find_bin<W>(s, count(bin0), before, target, 1.0);
     }
-    if (more && rank == 0 && tid == 0) add(bin0(more_key), more);
-    find_bin<W>(s, 0, target, frac);
-    if (frac < 1.0) target = fmax(frac * (double)s.found_all, 1.0);
     // keys that can lie in the bin, with room for roundings
     const int bin = (int)s.found_bin;
-    const float unit = W ? t / per : 1.f / per;
-    const float far = top - (float)(bin + 1) * unit, near = top - (float)bin * unit;
-    const float room = 1e-5f * (fabsf(top) + fabsf(far) + (float)(bin + 2) * unit);
+    const float per = beyond ? kBeyond : kNear, from = beyond ? kSmFar : 0.f, unit = W ? t : 1.f;
+    const float far = top - unit * (from + (float)(bin + 1) / per), near = top - unit * (from + (float)bin / per);
+    const float room = 1e-5f * (fabsf(top) + fabsf(far) + unit * (from + (float)(bin + 2) / per));
     uint32_t lo = far - room > -INFINITY && bin < kSmBins - 1 ? key_of(far - room) : 0u;
-    uint32_t hi = near + room < INFINITY && bin > 0 ? min(key_of(near + room), most) : most;
+    uint32_t hi = near + room < INFINITY && (bin > 0 || beyond) ? min(key_of(near + room), most) : most;
     lo >>= KS;
     hi >>= KS;
     while (lo < hi) {
-      const int bits = max(0, 32 - __clz(hi - lo) - 11);   // (hi - lo) >> bits is below kSmBins
-      auto at = [&](uint32_t k) { return (k >> KS) >= lo && (k >> KS) <= hi && bin0(k) == bin; };
+      const int bits = max(0, 32 - __clz(hi - lo) - kSmBinsLog2);   // (hi - lo) >> bits is below kSmBins
       const u64 before = s.found_before;
-      __syncthreads();
-      clear();
-      for (int i = 0; i < chunk; ++i) {
-        const uint32_t k = own[i];
-        if (key_in(k) && at(k)) add((int)((hi - (k >> KS)) >> bits), W ? weight(chance(k)) : 1);
-      }
-      if (more && rank == 0 && tid == 0 && at(more_key)) add((int)((hi - (more_key >> KS)) >> bits), more);
-      find_bin<W>(s, before, target, 1.0);
+      const int q = count([&](uint32_t k) -> int {
+        return (k >> KS) >= lo && (k >> KS) <= hi && bin0(k) == bin ? (int)((hi - (k >> KS)) >> bits) : -1;
+      });
+      find_bin<W>(s, q, before, target, 1.0);
       hi -= s.found_bin << bits;
       if (hi - lo > (1u << bits) - 1) lo = hi - ((1u << bits) - 1);
     }
@@ -323,8 +370,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   };
   const int k = a.top_k ? a.top_k[row] : 0;
   if (k > 0 && k < a.V) {
-    double target = (double)k;
-    cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, target, 1.0);
+    cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, (u64)k, 1.0);
     cut_ties = (u64)k - s.found_before;
     some_ties = cut_ties < s.found_in;
     __syncthreads();
@@ -333,16 +379,13 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   if (top_p < 1.f) {
     const uint32_t k_key = cut_key;
     const u64 k_ties = cut_ties;
-    double target = 0.0;
     // of the equals of top-k's last, the kept ones
     const uint32_t key = search(std::true_type(), [&](uint32_t q) { return q > k_key || (q == k_key && k_ties == ~0ull); }, k_key,
-                                k_ties == ~0ull ? 0 : k_ties * weight(chance(k_key)), target, (double)top_p);
+                                k_ties == ~0ull ? 0 : k_ties * weight(chance(k_key)), 0, (double)top_p);
     const u64 one = weight(chance(key)), before = s.found_before;
     if (one > 0) {
       // the fewest equals whose weight takes the sum to the target
-      u64 n = (u64)fmax(ceil((target - (double)before) / (double)one), 1.0);
-      while (n > 1 && (double)(before + (n - 1) * one) >= target) --n;
-      while ((double)(before + n * one) < target) ++n;
+      const u64 n = (s.found_target - before + one - 1) / one;   // at least 1: `before` is below the target
       const u64 all = s.found_in / one;
       if (n < all || key != k_key) some_ties = n < all;
       cut_key = key;
@@ -351,36 +394,41 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     __syncthreads();
   }
   uint32_t last = 0xffffffffu;   // equals of cut_key are kept up to this index
+  const uint32_t last_key = cut_key;
   if (some_ties) last = nth(cut_key, cut_ties);
 
   // ---- the draw
   const float floor_p = a.min_p ? a.min_p[row] : 0.f;
   const float min_p = floor_p > 0.f ? fminf(floor_p, 1.f) : 0.f;
+  // keys below this weigh nothing, or less than min_p: exp(z) >= min_p asks for a z that is a little
+  // above its logarithm at most, with room for the logarithm's and the other roundings
+  {
+    const float z = min_p > 0.f ? fmaxf(logf(min_p), -28.5f) : -28.5f;
+    const float low = top + t * z - 1e-5f * (fabsf(top) + 2.f * t * fabsf(z) + t);
+    if (low > -INFINITY) cut_key = max(cut_key, min(key_of(low), most));
+  }
   auto kept = [&](int i) -> u64 {
-    const uint32_t key = own[i];
-    if (key < cut_key || (key == cut_key && (uint32_t)(own0 + i) > last)) return 0;
+    const uint32_t key = keys[i];
+    if (key < cut_key || (key == last_key && (uint32_t)(i0 + i) > last)) return 0;
     const float w = chance(key);
     return w < min_p ? 0 : weight(w);
   };
   u64 sum = 0, all;
-#pragma unroll 4
-  for (int i = 0; i < chunk; ++i) sum += kept(i);
-  u64 before = cluster_before(sum, s, &all);
+#pragma unroll 2
+  for (int i = 0; i < chunk; ++i) sum += kept(tid * chunk + i);
+  const u64 before = cluster_before(sum, s, round, &all);
   const double mark_d = (double)a.u[row] * (double)all;
   u64 mark = mark_d > 0.0 ? (u64)mark_d : 0;
   if (mark > all - 1) mark = all - 1;
-  if (before <= mark && mark < before + sum) {
-    int i = 0;
-    for (;; ++i) {
-      before += kept(i);
-      if (before > mark) break;
-    }
-    a.token[row] = own0 + i;
+  const int i = walk(before, sum, mark, kept);
+  if (i >= 0 && lane == 0) {
+    a.token[row] = i0 + i;
     if (a.logprob) {
       const float rest = (float)((double)(all - (u64)kSmUnit) / (double)kSmUnit);
-      a.logprob[row] = logit_of(own[i]) - log1pf(rest);
+      a.logprob[row] = logit_of(keys[i]) - log1pf(rest);
     }
   }
+  cluster_sync();   // no CTA leaves while another reads its shared memory
 }
 
 }  // namespace
