@@ -29,12 +29,12 @@ static_assert(kSmBins == kSmThreads, "a thread a bin");
 constexpr int kSmMostChunk = 97;          // words of a thread: 8 x 512 x 97 tokens
 constexpr int kSmMostCluster = 8;
 constexpr int kSmSmem = kSmThreads * kSmMostChunk * 4 + 16;
+static_assert((uint64_t)kSmThreads * kSmMostChunk << 14 < 1ull << 31, "14 bits of every key of a CTA, and top-k's equals' upper ones");
 static_assert(kSmMostCluster * kSmThreads * kSmMostChunk == kSampleMaxV, "the limit that the header states");
-constexpr uint32_t kSmNone = 0x007fffffu; // key of -infinity; padding lies below it
-// First bins: the last takes what lies further from the largest logit (or from z = 0), most of a row as
-// a rule, which threads sum up for themselves before they add it.
-// A cut that lies there is looked for in a second set of bins, to kSmEnd (weights end at 28).
-constexpr float kSmFar = 10.f, kSmEnd = 32.f;
+constexpr uint32_t kSmNone = 0x007fffffu; // key of -infinity, of NaN and of padding
+// First bins: even in the distance from the largest logit (or from z = 0) to this, the last one takes the
+// rest (weights end at 28).
+constexpr float kSmEnd = 32.f, kSmBinsPer = (kSmBins - 1) / kSmEnd;
 constexpr float kSmUnit = 1099511627776.f;   // 2^40
 
 typedef unsigned long long u64;
@@ -63,9 +63,10 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
 }
 
 struct SampleShared {
-  // Histograms: counts in lo, or weights in (lo, hi). Rounds over the cluster take turns with two of
-  // everything that other CTAs read, so one barrier a round is enough.
-  uint32_t lo[2][kSmBins], hi[2][kSmBins];
+  // Histograms: counts in part 0, or weights in 14, 14 and the other bits: a CTA's keys do not fill a word with
+  // 14 bits each, so that an addition needs no carry and nothing waits for it. Rounds over the cluster
+  // take turns with two of everything that other CTAs read, so one barrier a round is enough.
+  uint32_t part[2][3][kSmBins];
   u64 total[2];                        // this CTA's total
   u64 bins[2][kSmBins];                // sums over the cluster of this CTA's share of the bins
   u64 warp[kSmWarps];                  // block scan
@@ -138,15 +139,18 @@ __device__ __forceinline__ void find_bin(SampleShared& s, int q, u64 base, u64 t
   u64 v;
   if (n > 1) {
     const uint32_t c = tid & (n - 1), bin = rank * share + tid / n;
-    v = ld_cluster_u32(map_to_cta(smem_u32(&s.lo[q][bin]), c));
-    if (WEIGHTS) v += (u64)ld_cluster_u32(map_to_cta(smem_u32(&s.hi[q][bin]), c)) << 32;
+    v = ld_cluster_u32(map_to_cta(smem_u32(&s.part[q][0][bin]), c));
+    if (WEIGHTS) {
+      v += (u64)ld_cluster_u32(map_to_cta(smem_u32(&s.part[q][1][bin]), c)) << 14;
+      v += (u64)ld_cluster_u32(map_to_cta(smem_u32(&s.part[q][2][bin]), c)) << 28;
+    }
     for (uint32_t o = 1; o < n; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if (c == 0) s.bins[q][tid / n] = v;
     cluster_sync();
     v = ld_cluster_u64(map_to_cta(smem_u32(&s.bins[q][tid & (share - 1)]), tid / share));
   } else {
-    v = s.lo[q][tid];
-    if (WEIGHTS) v += (u64)s.hi[q][tid] << 32;
+    v = s.part[q][0][tid];
+    if (WEIGHTS) v += ((u64)s.part[q][1][tid] << 14) + ((u64)s.part[q][2][tid] << 28);
   }
   u64 all;
   const u64 run = base + block_before(v, s, &all);
@@ -208,7 +212,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       }
     }
   }
-  for (int i = there + tid; i < slice; i += kSmThreads) keys[i] = 0;
+  for (int i = there + tid; i < slice; i += kSmThreads) keys[i] = kSmNone;
   most = __reduce_max_sync(0xffffffffu, most);
   if (lane == 0) s.warp[tid >> 5] = most;
   __syncthreads();
@@ -236,6 +240,53 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     return y < 16777216.f ? (u64)__float2uint_rn(y) : (u64)((bits & 0x7fffffu) | 0x800000u) << ((bits >> 23) - 150);
   };
   int round = 0;
+  const int k = a.top_k ? a.top_k[row] : 0;
+  const float top_p = a.top_p ? a.top_p[row] : 1.f;
+  const float floor_p = a.min_p ? a.min_p[row] : 0.f;
+  const bool by_k = k > 0 && k < a.V, by_p = top_p < 1.f;
+  // The first round of a search leaves the keys that can be kept, from low_key on: a bit for each of the
+  // thread's, and only those are looked at again.
+  uint32_t low_key = 0, can[4] = {0, 0, 0, 0};
+  auto mark_from = [&](uint32_t low) {
+    low_key = low;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t m = 0;
+      const int n = min(32, chunk - 32 * w);
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) m |= (uint32_t)(own[32 * w + i] >= low) << i;
+      can[w] = m;
+    }
+  };
+  // Whether the marked keys are few enough to go to one by one.
+  auto sparse = [&] {
+    return low_key && !__any_sync(0xffffffffu, 3 * (__popc(can[0]) + __popc(can[1]) + __popc(can[2]) + __popc(can[3])) > chunk);
+  };
+  // f(i, the key) for the thread's keys that can be kept: one by one, or in groups whose loads and
+  // arithmetic overlap: then from the values g(key) of four, with those below low_key among them.
+  auto each = [&](auto g, auto f) {
+    if (sparse()) {
+#pragma unroll 1
+      for (int w = 0; w < 4; ++w)
+        for (uint32_t m = w == 0 ? can[0] : w == 1 ? can[1] : w == 2 ? can[2] : can[3]; m; m &= m - 1)
+          f(g(32 * w + __ffs(m) - 1, own[32 * w + __ffs(m) - 1]));
+      return;
+    }
+    int i = 0;
+#pragma unroll 1
+    for (; i + 4 <= chunk; i += 4) {
+      const auto a0 = g(i, own[i]);
+      const auto a1 = g(i + 1, own[i + 1]);
+      const auto a2 = g(i + 2, own[i + 2]);
+      const auto a3 = g(i + 3, own[i + 3]);
+      f(a0);
+      f(a1);
+      f(a2);
+      f(a3);
+    }
+#pragma unroll 1
+    for (; i < chunk; ++i) f(g(i, own[i]));
+  };
   // Where, in the slice, a running sum passes `mark`, if that is in this warp's part: `before` and `sum` are
   // each thread's, value(i) the summands. The warp takes the thread's chunk 32 at a time. -1: elsewhere.
   auto walk = [&](u64 before, u64 sum, u64 mark, auto value) -> int {
@@ -260,8 +311,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   // index of the n-th (from 1) key equal to k in the order of the vocabulary, in every CTA
   auto nth = [&](uint32_t k, u64 n) -> uint32_t {
     int c = 0;
-#pragma unroll 4
-    for (int i = 0; i < chunk; ++i) c += own[i] == k;
+    each([&](int, uint32_t key) { return (int)(key == k); }, [&](int one) { c += one; });
     u64 all;
     const u64 before = cluster_before((u64)c, s, round, &all);
     const int i = walk(before, (u64)c, n - 1, [&](int i) -> u64 { return keys[i] == k; });
@@ -295,44 +345,32 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   // find_bin takes it. Out: the key, and in s.found_* the sums before and of it.
   auto search = [&](auto weights_c, auto key_in, uint32_t more_key, u64 more, u64 target, double frac) -> uint32_t {
     constexpr bool W = decltype(weights_c)::value;
-    constexpr float kNear = (kSmBins - 1) / kSmFar, kBeyond = (kSmBins - 1) / (kSmEnd - kSmFar);
-    bool beyond = false;   // the second set, of the first one's last bin; other keys: -1
+    const float from = fminf(top, 3.4e38f), per = kSmBinsPer;
     auto bin0 = [&](uint32_t k) -> int {   // falls with the key, slowly or not at all
-      const float d = k == most ? 0.f : k <= kSmNone ? INFINITY : W ? -logit_of(k) : __fsub_rn(top, value_of(k));
-      const int bin = (int)fminf(__fmul_rn(d, kNear), (float)(kSmBins - 1));   // NaN: the last one
-      if (!beyond) return bin;
-      if (bin < kSmBins - 1) return -1;
-      const float e = __fsub_rn(d, kSmFar);
-      return e < 0.f ? 0 : (int)fminf(__fmul_rn(e, kBeyond), (float)(kSmBins - 1));
+      const float d = __fsub_rn(from, value_of(k)), e = W ? __fmul_rn(d, inv) : d;
+      return (int)fminf(fmaxf(__fmul_rn(e, per), 0.f), (float)(kSmBins - 1));   // NaN (0 times infinity): 0
     };
     // the histogram of the next round: bin_of(key) < 0 takes no part
     auto count = [&](auto bin_of) -> int {
       const int q = round++ & 1;
-      s.lo[q][tid] = 0;
-      if (W) s.hi[q][tid] = 0;
+#pragma unroll
+      for (int i = 0; i < (W ? 3 : 1); ++i) s.part[q][i][tid] = 0;
       __syncthreads();
       auto put = [&](int bin, u64 w) {
         if (!W) {
-          atomicAdd(&s.lo[q][bin], (uint32_t)w);
+          atomicAdd(&s.part[q][0][bin], 1u);
           return;
         }
-        const uint32_t lo = (uint32_t)w;
-        const uint32_t hi = (uint32_t)(w >> 32) + (lo && atomicAdd(&s.lo[q][bin], lo) > 0xffffffffu - lo);
-        if (hi) atomicAdd(&s.hi[q][bin], hi);
+        const uint32_t p0 = (uint32_t)w & 0x3fffu, p1 = (uint32_t)(w >> 14) & 0x3fffu, p2 = (uint32_t)(w >> 28);
+        if (p0) atomicAdd(&s.part[q][0][bin], p0);
+        if (p1) atomicAdd(&s.part[q][1][bin], p1);
+        if (p2) atomicAdd(&s.part[q][2][bin], p2);
       };
-      u64 rest = 0;   // of the last bin
-#pragma unroll 2
-      for (int i = 0; i < chunk; ++i) {
-        const uint32_t k = own[i];
-        const int bin = key_in(k) ? bin_of(k) : -1;
-        if (bin < 0) continue;
-        const u64 w = W ? weight(chance(k)) : 1;
-        if (bin == kSmBins - 1) rest += w;   // most of a row in the first round
-        else put(bin, w);
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
-      if (lane == 0 && rest) put(kSmBins - 1, rest);
+      struct Put { int bin; u64 w; };
+      each([&](int, uint32_t key) {
+        const int bin = key_in(key) ? bin_of(key) : -1;
+        return Put{bin, W ? (bin >= 0 ? weight(chance(key)) : 0) : 1};
+      }, [&](const Put& a) { if (a.bin >= 0) put(a.bin, a.w); });
       if (W && more && rank == 0 && tid == 0) {
         const int bin = bin_of(more_key);
         if (bin >= 0) put(bin, more);
@@ -341,18 +379,14 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     };
     find_bin<W>(s, count(bin0), 0, target, frac);
     if (frac < 1.0) target = s.found_target;
-    if (s.found_bin == kSmBins - 1) {
-      const u64 before = s.found_before;
-      beyond = true;
-      find_bin<W>(s, count(bin0), before, target, 1.0);
-    }
     // keys that can lie in the bin, with room for roundings
     const int bin = (int)s.found_bin;
-    const float per = beyond ? kBeyond : kNear, from = beyond ? kSmFar : 0.f, unit = W ? t : 1.f;
-    const float far = top - unit * (from + (float)(bin + 1) / per), near = top - unit * (from + (float)bin / per);
-    const float room = 1e-5f * (fabsf(top) + fabsf(far) + unit * (from + (float)(bin + 2) / per));
+    const float unit = W ? t / per : 1.f / per;
+    const float far = top - (float)(bin + 1) * unit, near = top - (float)bin * unit;
+    const float room = 1e-5f * (fabsf(top) + fabsf(far) + (float)(bin + 2) * unit);
     uint32_t lo = far - room > -INFINITY && bin < kSmBins - 1 ? key_of(far - room) : 0u;
-    uint32_t hi = near + room < INFINITY && (bin > 0 || beyond) ? min(key_of(near + room), most) : most;
+    uint32_t hi = near + room < INFINITY && bin > 0 ? min(key_of(near + room), most) : most;
+    if (lo > low_key) mark_from(min(lo, most));
     lo >>= KS;
     hi >>= KS;
     while (lo < hi) {
@@ -368,15 +402,13 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     // a key whose low bits are its type's: zeros above 0, ones below
     return KS == 0 ? hi : (hi & (0x80000000u >> KS)) ? hi << KS : (hi << KS) | ((1u << KS) - 1);
   };
-  const int k = a.top_k ? a.top_k[row] : 0;
-  if (k > 0 && k < a.V) {
+  if (by_k) {
     cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, (u64)k, 1.0);
     cut_ties = (u64)k - s.found_before;
     some_ties = cut_ties < s.found_in;
     __syncthreads();
   }
-  const float top_p = a.top_p ? a.top_p[row] : 1.f;
-  if (top_p < 1.f) {
+  if (by_p) {
     const uint32_t k_key = cut_key;
     const u64 k_ties = cut_ties;
     // of the equals of top-k's last, the kept ones
@@ -398,29 +430,26 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   if (some_ties) last = nth(cut_key, cut_ties);
 
   // ---- the draw
-  const float floor_p = a.min_p ? a.min_p[row] : 0.f;
   const float min_p = floor_p > 0.f ? fminf(floor_p, 1.f) : 0.f;
   // keys below this weigh nothing, or less than min_p: exp(z) >= min_p asks for a z that is a little
-  // above its logarithm at most, with room for the logarithm's and the other roundings
+  // below its logarithm at least, with room for the logarithm's and the other roundings
   {
     const float z = min_p > 0.f ? fmaxf(logf(min_p), -28.5f) : -28.5f;
     const float low = top + t * z - 1e-5f * (fabsf(top) + 2.f * t * fabsf(z) + t);
     if (low > -INFINITY) cut_key = max(cut_key, min(key_of(low), most));
   }
-  auto kept = [&](int i) -> u64 {
-    const uint32_t key = keys[i];
+  auto kept = [&](int i, uint32_t key) -> u64 {   // number i of the slice
     if (key < cut_key || (key == last_key && (uint32_t)(i0 + i) > last)) return 0;
     const float w = chance(key);
     return w < min_p ? 0 : weight(w);
   };
   u64 sum = 0, all;
-#pragma unroll 2
-  for (int i = 0; i < chunk; ++i) sum += kept(tid * chunk + i);
+  each([&](int i, uint32_t key) { return kept(tid * chunk + i, key); }, [&](u64 w) { sum += w; });
   const u64 before = cluster_before(sum, s, round, &all);
   const double mark_d = (double)a.u[row] * (double)all;
   u64 mark = mark_d > 0.0 ? (u64)mark_d : 0;
   if (mark > all - 1) mark = all - 1;
-  const int i = walk(before, sum, mark, kept);
+  const int i = walk(before, sum, mark, [&](int i) { return kept(i, keys[i]); });
   if (i >= 0 && lane == 0) {
     a.token[row] = i0 + i;
     if (a.logprob) {
