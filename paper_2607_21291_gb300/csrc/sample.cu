@@ -244,48 +244,40 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   const float top_p = a.top_p ? a.top_p[row] : 1.f;
   const float floor_p = a.min_p ? a.min_p[row] : 0.f;
   const bool by_k = k > 0 && k < a.V, by_p = top_p < 1.f;
-  // The first round of a search leaves the keys that can be kept, from low_key on: a bit for each of the
-  // thread's, and only those are looked at again.
-  uint32_t low_key = 0, can[4] = {0, 0, 0, 0};
-  auto mark_from = [&](uint32_t low) {
-    low_key = low;
+  // The first round of a search leaves the keys that can be kept, from low_key on, and among them the ones of
+  // the bin that it found (keys from low to high): a bit for each of the thread's. Only those are looked at again.
+  uint32_t low_key = 0, can[4] = {0, 0, 0, 0}, in_bin[4] = {0, 0, 0, 0};
+  auto mark_keys = [&](uint32_t low, uint32_t high) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      uint32_t m = 0;
+      uint32_t above = 0, in = 0;
       const int n = min(32, chunk - 32 * w);
 #pragma unroll 4
-      for (int i = 0; i < n; ++i) m |= (uint32_t)(own[32 * w + i] >= low) << i;
-      can[w] = m;
+      for (int i = 0; i < n; ++i) {
+        const uint32_t k = own[32 * w + i];
+        above |= (uint32_t)(k >= low) << i;
+        in |= (uint32_t)(k >= low && k <= high) << i;
+      }
+      can[w] = above;
+      in_bin[w] = in;
     }
+    low_key = low;
   };
-  // Whether the marked keys are few enough to go to one by one.
-  auto sparse = [&] {
-    return low_key && !__any_sync(0xffffffffu, 3 * (__popc(can[0]) + __popc(can[1]) + __popc(can[2]) + __popc(can[3])) > chunk);
-  };
-  // f(i, the key) for the thread's keys that can be kept: one by one, or in groups whose loads and
-  // arithmetic overlap: then from the values g(key) of four, with those below low_key among them.
-  auto each = [&](auto g, auto f) {
-    if (sparse()) {
+  // f(g(i, own[i])) for the marked keys one by one
+  auto each_of = [&](const uint32_t (&marks)[4], auto g, auto f) {
 #pragma unroll 1
-      for (int w = 0; w < 4; ++w)
-        for (uint32_t m = w == 0 ? can[0] : w == 1 ? can[1] : w == 2 ? can[2] : can[3]; m; m &= m - 1)
-          f(g(32 * w + __ffs(m) - 1, own[32 * w + __ffs(m) - 1]));
+    for (int w = 0; w < 4; ++w)
+      for (uint32_t m = w == 0 ? marks[0] : w == 1 ? marks[1] : w == 2 ? marks[2] : marks[3]; m; m &= m - 1)
+        f(g(32 * w + __ffs(m) - 1, own[32 * w + __ffs(m) - 1]));
+  };
+  // The same for the thread's keys that can be kept, where they are few, or for all of them.
+  auto each = [&](auto g, auto f) {
+    if (low_key && !__any_sync(0xffffffffu, 3 * (__popc(can[0]) + __popc(can[1]) + __popc(can[2]) + __popc(can[3])) > chunk)) {
+      each_of(can, g, f);
       return;
     }
-    int i = 0;
-#pragma unroll 1
-    for (; i + 4 <= chunk; i += 4) {
-      const auto a0 = g(i, own[i]);
-      const auto a1 = g(i + 1, own[i + 1]);
-      const auto a2 = g(i + 2, own[i + 2]);
-      const auto a3 = g(i + 3, own[i + 3]);
-      f(a0);
-      f(a1);
-      f(a2);
-      f(a3);
-    }
-#pragma unroll 1
-    for (; i < chunk; ++i) f(g(i, own[i]));
+#pragma unroll 2
+    for (int i = 0; i < chunk; ++i) f(g(i, own[i]));
   };
   // Where, in the slice, a running sum passes `mark`, if that is in this warp's part: `before` and `sum` are
   // each thread's, value(i) the summands. The warp takes the thread's chunk 32 at a time. -1: elsewhere.
@@ -343,41 +335,54 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   bool some_ties = false;     // fewer than there are
   // One search. key_in: whether a key takes part; more: weight of `more_key` beside those (0: none); target: as
   // find_bin takes it. Out: the key, and in s.found_* the sums before and of it.
-  auto search = [&](auto weights_c, auto key_in, uint32_t more_key, u64 more, u64 target, double frac) -> uint32_t {
+  // Weights of keys below tail_key go into the last bin together.
+  auto search = [&](auto weights_c, auto key_in, uint32_t more_key, u64 more, u64 target, double frac, uint32_t tail_key) -> uint32_t {
     constexpr bool W = decltype(weights_c)::value;
     const float from = fminf(top, 3.4e38f), per = kSmBinsPer;
     auto bin0 = [&](uint32_t k) -> int {   // falls with the key, slowly or not at all
       const float d = __fsub_rn(from, value_of(k)), e = W ? __fmul_rn(d, inv) : d;
       return (int)fminf(fmaxf(__fmul_rn(e, per), 0.f), (float)(kSmBins - 1));   // NaN (0 times infinity): 0
     };
-    // the histogram of the next round: bin_of(key) < 0 takes no part
-    auto count = [&](auto bin_of) -> int {
+    struct Put { int bin; u64 w; };   // bin < 0: takes no part
+    auto put = [&](int q, const Put& a) {
+      if (a.bin < 0) return;
+      if (!W) {
+        atomicAdd(&s.part[q][0][a.bin], 1u);
+        return;
+      }
+      const uint32_t p0 = (uint32_t)a.w & 0x3fffu, p1 = (uint32_t)(a.w >> 14) & 0x3fffu, p2 = (uint32_t)(a.w >> 28);
+      atomicAdd(&s.part[q][0][a.bin], p0);
+      atomicAdd(&s.part[q][1][a.bin], p1);
+      if (p2) atomicAdd(&s.part[q][2][a.bin], p2);
+    };
+    auto clear = [&]() -> int {   // the histogram of the next round
       const int q = round++ & 1;
 #pragma unroll
       for (int i = 0; i < (W ? 3 : 1); ++i) s.part[q][i][tid] = 0;
       __syncthreads();
-      auto put = [&](int bin, u64 w) {
-        if (!W) {
-          atomicAdd(&s.part[q][0][bin], 1u);
-          return;
-        }
-        const uint32_t p0 = (uint32_t)w & 0x3fffu, p1 = (uint32_t)(w >> 14) & 0x3fffu, p2 = (uint32_t)(w >> 28);
-        if (p0) atomicAdd(&s.part[q][0][bin], p0);
-        if (p1) atomicAdd(&s.part[q][1][bin], p1);
-        if (p2) atomicAdd(&s.part[q][2][bin], p2);
-      };
-      struct Put { int bin; u64 w; };
-      each([&](int, uint32_t key) {
-        const int bin = key_in(key) ? bin_of(key) : -1;
-        return Put{bin, W ? (bin >= 0 ? weight(chance(key)) : 0) : 1};
-      }, [&](const Put& a) { if (a.bin >= 0) put(a.bin, a.w); });
-      if (W && more && rank == 0 && tid == 0) {
-        const int bin = bin_of(more_key);
-        if (bin >= 0) put(bin, more);
-      }
       return q;
     };
-    find_bin<W>(s, count(bin0), 0, target, frac);
+    int q = clear();
+    u64 rest = 0;
+    auto first = [&](uint32_t key) {
+      if (!key_in(key)) return;
+      const u64 w = W ? weight(chance(key)) : 1;
+      if (W && key < tail_key) rest += w;
+      else put(q, Put{bin0(key), w});
+    };
+    if (low_key) {
+      each_of(can, [&](int, uint32_t key) { return key; }, first);
+    } else {
+#pragma unroll 2
+      for (int i = 0; i < chunk; ++i) first(own[i]);
+    }
+    if (W) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+      if (lane == 0) put(q, Put{kSmBins - 1, rest});
+      if (more && rank == 0 && tid == 0) put(q, Put{bin0(more_key), more});
+    }
+    find_bin<W>(s, q, 0, target, frac);
     if (frac < 1.0) target = s.found_target;
     // keys that can lie in the bin, with room for roundings
     const int bin = (int)s.found_bin;
@@ -386,15 +391,21 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     const float room = 1e-5f * (fabsf(top) + fabsf(far) + (float)(bin + 2) * unit);
     uint32_t lo = far - room > -INFINITY && bin < kSmBins - 1 ? key_of(far - room) : 0u;
     uint32_t hi = near + room < INFINITY && bin > 0 ? min(key_of(near + room), most) : most;
-    if (lo > low_key) mark_from(min(lo, most));
     lo >>= KS;
     hi >>= KS;
+    mark_keys(min(max(lo << KS, low_key), most), hi << KS | ((1u << KS) - 1));
     while (lo < hi) {
       const int bits = max(0, 32 - __clz(hi - lo) - kSmBinsLog2);   // (hi - lo) >> bits is below kSmBins
       const u64 before = s.found_before;
-      const int q = count([&](uint32_t k) -> int {
+      auto bin_of = [&](uint32_t k) -> int {
         return (k >> KS) >= lo && (k >> KS) <= hi && bin0(k) == bin ? (int)((hi - (k >> KS)) >> bits) : -1;
-      });
+      };
+      q = clear();
+      each_of(in_bin, [&](int, uint32_t key) {
+        const int at = key_in(key) ? bin_of(key) : -1;
+        return Put{at, W && at >= 0 ? weight(chance(key)) : 1};
+      }, [&](const Put& a) { put(q, a); });
+      if (W && more && rank == 0 && tid == 0) put(q, Put{bin_of(more_key), more});
       find_bin<W>(s, q, before, target, 1.0);
       hi -= s.found_bin << bits;
       if (hi - lo > (1u << bits) - 1) lo = hi - ((1u << bits) - 1);
@@ -403,7 +414,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     return KS == 0 ? hi : (hi & (0x80000000u >> KS)) ? hi << KS : (hi << KS) | ((1u << KS) - 1);
   };
   if (by_k) {
-    cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, (u64)k, 1.0);
+    cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, (u64)k, 1.0, 0);
     cut_ties = (u64)k - s.found_before;
     some_ties = cut_ties < s.found_in;
     __syncthreads();
@@ -411,9 +422,12 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   if (by_p) {
     const uint32_t k_key = cut_key;
     const u64 k_ties = cut_ties;
+    // All logits below this one together weigh less than 1 - top_p of the largest: the cut lies above.
+    const float tail = top + t * (logf((1.f - top_p) / (float)a.V) - 0.01f);
+    const uint32_t tail_key = top_p > 0.f && tail - 1e-5f * fabsf(top) > -INFINITY ? min(key_of(tail - 1e-5f * fabsf(top)), most) : 0u;
     // of the equals of top-k's last, the kept ones
     const uint32_t key = search(std::true_type(), [&](uint32_t q) { return q > k_key || (q == k_key && k_ties == ~0ull); }, k_key,
-                                k_ties == ~0ull ? 0 : k_ties * weight(chance(k_key)), 0, (double)top_p);
+                                k_ties == ~0ull ? 0 : k_ties * weight(chance(k_key)), 0, (double)top_p, tail_key);
     const u64 one = weight(chance(key)), before = s.found_before;
     if (one > 0) {
       // the fewest equals whose weight takes the sum to the target
