@@ -172,13 +172,13 @@ __device__ __forceinline__ void find_bin(SampleShared& s, int q, u64 base, u64 t
 
 // Four consecutive elements, 16 or 8 aligned bytes.
 __device__ __forceinline__ uint4 keys_of4(const float* p) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
+  const float4 v = __ldg(reinterpret_cast<const float4*>(p));
   return make_uint4(key_of(v.x), key_of(v.y), key_of(v.z), key_of(v.w));
 }
 __device__ __forceinline__ uint4 keys_of4(const bf16* p) {
-  float f[4];
-  load4(p, f);
-  return make_uint4(key_of(f[0]), key_of(f[1]), key_of(f[2]), key_of(f[3]));
+  const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+  return make_uint4(key_of(__uint_as_float(v.x << 16)), key_of(__uint_as_float(v.x & 0xffff0000u)),
+                    key_of(__uint_as_float(v.y << 16)), key_of(__uint_as_float(v.y & 0xffff0000u)));
 }
 
 template <typename T>
@@ -198,18 +198,18 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   uint32_t* keys = raw + shift;
   const int there = min(max(a.V - i0, 0), slice);
   uint32_t most = 0;
-#pragma unroll 4
-  for (int g = tid; 4 * g < there + shift; g += kSmThreads) {
-    const int i = 4 * g - shift;
-    if (i >= 0 && i + 4 <= there) {
-      const uint4 k = keys_of4(x + i);
-      *reinterpret_cast<uint4*>(raw + 4 * g) = k;
-      most = max(max(most, max(k.x, k.y)), max(k.z, k.w));
-    } else {
-      for (int e = max(i, 0); e < min(i + 4, there); ++e) {
-        keys[e] = key_of(Elem<T>::to_f(x[e]));
-        most = max(most, keys[e]);
-      }
+  const int g0 = shift ? 1 : 0, g1 = (there + shift) / 4;   // whole groups
+#pragma unroll 8
+  for (int g = g0 + tid; g < g1; g += kSmThreads) {
+    const uint4 k = keys_of4(x + 4 * g - shift);
+    *reinterpret_cast<uint4*>(raw + 4 * g) = k;
+    most = max(max(most, max(k.x, k.y)), max(k.z, k.w));
+  }
+  if (tid < 8) {   // up to three elements on either side
+    const int i = tid < 4 ? tid : max(4 * g1 - shift, 4 * g0 - shift) + tid - 4;
+    if (tid < 4 ? i < 4 * g0 - shift && i < there : i < there) {
+      keys[i] = key_of(Elem<T>::to_f(x[i]));
+      most = max(most, keys[i]);
     }
   }
   for (int i = there + tid; i < slice; i += kSmThreads) keys[i] = kSmNone;
