@@ -301,6 +301,9 @@ cudaError_t paged_rows(const Paged& p, const void* q, int64_t ld_q, void* out, i
 bool paged_tc_takes(const Paged& p);
 size_t paged_tc_scratch(const Paged& p);
 cudaError_t paged_tc(const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch, const Dev& dev);
+// paged_f32.cu -- fp32 models.
+size_t paged_f32_scratch(const Paged& p);
+cudaError_t paged_f32(const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch, const Dev& dev);
 // sample.cu
 struct Sample {
   const void* logits; int64_t ld;

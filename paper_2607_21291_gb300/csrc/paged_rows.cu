@@ -72,8 +72,8 @@ __device__ __forceinline__ float2 lds_f2(uint32_t a) {
 struct PrCut {
   static constexpr int KEYS = kPrTK, PAD = kPrPad, WHOLE = kPrWhole;
   int G;
-  __device__ __forceinline__ int groups(int n) const { return (n * G + kPrRows - 1) / kPrRows; }
-  __device__ __forceinline__ int tokens(int g) const { return ((g + 1) * kPrRows - 1) / G + 1; }
+  __device__ __forceinline__ int groups(int n) const { return (int)(((int64_t)n * G + kPrRows - 1) / kPrRows); }
+  __device__ __forceinline__ int tokens(int g) const { return (int)((((int64_t)g + 1) * kPrRows - 1) / G) + 1; }
 };
 
 template <int HD, bool I8>
