@@ -1,13 +1,15 @@
 // Paged cache: rotary, quantisation and write of new tokens, and the read back.
 //
-// A thread holds eight features of one head's vector; the hd / 8 threads of a vector
-// are neighbours in a warp. Rotation turns feature i with i + half (both read,
-// so that no thread waits for another) in separate fp32 products and sums. 8-bit storage:
-// the largest |x| of the vector by shuffles on the bits of |x| (a NaN is larger
-// than any number there), then round(x * (127 / m)).
-// Bytes bound both kernels: each element is read and written once.
+// A block takes up to kPgRows packed rows. Its first warp finds where they lie, a lane a row; then
+// the block's threads take the rows' head vectors, eight features a thread and the hd / 8 threads of a vector
+// neighbours in a warp. Rotation turns feature i with i + half (both read, so
+// that no thread waits for another) in separate fp32 products and sums. 8-bit storage: the largest |x| of the vector by
+// shuffles on the bits of |x| (a NaN is larger than any number there), then round(x * (127 / m)).
+// Bytes bound both kernels: each element is read and written once. One row a block, each block finding its
+// place for itself, took PG_BEFORE.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "paged.cuh"
@@ -16,13 +18,21 @@ namespace adadsf {
 namespace {
 
 constexpr int kPgThreads = 256;
+constexpr int kPgRows = 16;   // most rows of a block
+#ifndef PG_A
+#define PG_A 4
+#define PG_R 6
+#define PG_UA 2
+#define PG_UR 4
+#endif
+constexpr int kPgAppendPerSm = PG_A, kPgReadPerSm = PG_R, kUA = PG_UA, kUR = PG_UR;
 constexpr float kPgTiny = 7.888609052210118e-31f;   // 2^-100: vectors below are stored as zeros
 
 // Eight features e0 .. e0 + 7 of `src`.
 template <typename T>
 __device__ __forceinline__ void load8(const T* src, float* f) {
 #pragma unroll
-  for (int i = 0; i < 8; i += Elem<T>::kVec) load_vec(src + i, f + i);
+  for (int i = 0; i < 8; i += Elem<T>::kVec) unpack16(__ldg(reinterpret_cast<const uint4*>(src + i)), f + i, T());
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* dst, const float* f) {
@@ -43,7 +53,7 @@ __device__ __forceinline__ void turned8(const T* head, int e0, int half, const f
     const float4* t4 = reinterpret_cast<const float4*>(tab + (lower ? e0 : e0 - half));
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const float4 cs = t4[i / 2];
+      const float4 cs = __ldg(t4 + i / 2);
       const float t0 = __fmul_rn(g[i], cs.y), t1 = __fmul_rn(g[i + 1], cs.w);
       f[i] = __fadd_rn(__fmul_rn(f[i], cs.x), lower ? -t0 : t0);
       f[i + 1] = __fadd_rn(__fmul_rn(f[i + 1], cs.z), lower ? -t1 : t1);
@@ -62,51 +72,73 @@ __device__ __forceinline__ void turned8(const T* head, int e0, int half, const f
   }
 }
 
+// Where a block's rows lie: number of the token's vector of head 0 (-1: no token, or a page that is not),
+// and its place. Whole first warp; then for all.
+struct PgRows {
+  int64_t vec[kPgRows];
+  int place[kPgRows];
+};
+__device__ __forceinline__ void pg_rows(const Paged& p, int64_t row0, int n, PgRows& s, int* err) {
+  const int lane = threadIdx.x;
+  if (lane < 32) {
+    int b = paged_find(p, row0, lane);
+    if (lane < n) {
+      const int64_t row = row0 + lane;
+      while (b < p.B && p.starts[b + 1] <= row) ++b;
+      int place = -1, page = -1;
+      if (b < p.B) {
+        const PagedSeq q = paged_seq(p, b, err);
+        const int i = (int)(row - q.row0);
+        if (i >= 0 && i < q.n) place = q.len - q.n + i;
+        if (place >= 0) page = paged_page(p, b, place, err);
+      }
+      s.vec[lane] = page >= 0 ? paged_vec(p, page, place, 0) : -1;
+      s.place[lane] = place;
+    }
+  }
+  __syncthreads();
+}
+
 template <typename T, int HD, bool I8>
-__global__ void __launch_bounds__(kPgThreads)
+__global__ void __launch_bounds__(kPgThreads, kPgAppendPerSm)
     paged_append_kernel(const Paged p, const T* qkv, const float2* tab, int half, int n_pos, const int32_t* pos,
-                        T* q_out, int* err) {
+                        T* q_out, int rows, int* err) {
   constexpr int TPV = HD / 8;   // threads of a vector
+  __shared__ PgRows s;
+  __shared__ int at_s[kPgRows];
   pdl_wait();
   pdl_trigger();
-  const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x & 31;
-  const int heads = p.Hq + 2 * p.Hkv;
-  // the row's sequence and place: every warp finds them for itself
-  const int b = paged_find(p, row, lane);
-  int place = -1, page = -1;
-  if (b < p.B) {
-    const PagedSeq s = paged_seq(p, b, err);
-    const int i = (int)(row - s.row0);
-    if (i >= 0 && i < s.n) place = s.len - s.n + i;
-    if (place >= 0) page = paged_page(p, b, place, err);
-  }
-  const float2* turn = tab;
-  if (half > 0) {
-    int at = pos ? pos[row] : max(place, 0);
-    if (at < 0 || at >= n_pos) {
-      set_device_error(err, DEVERR_INDEX);
-      at = min(max(at, 0), n_pos - 1);
-    }
-    turn = tab + (int64_t)at * half;
-  }
-  const int v0 = blockIdx.y * (kPgThreads / TPV) + (int)threadIdx.x / TPV;
-  const int e0 = (int)threadIdx.x % TPV * 8;
-  const int first = q_out ? 0 : p.Hq;
-  for (int h0 = first; h0 < heads; h0 += gridDim.y * (kPgThreads / TPV)) {
-    const int h = h0 + v0;
-    const bool live = h < heads;
+  const int64_t row0 = (int64_t)blockIdx.x * rows;
+  const int n = (int)min((int64_t)rows, p.n_rows - row0);
+  const int tid = threadIdx.x;
+  if (half > 0 && pos && tid >= 32 && tid < 32 + n) at_s[tid - 32] = pos[row0 + tid - 32];
+  pg_rows(p, row0, n, s, err);
+  const int heads = p.Hq + 2 * p.Hkv, first = q_out ? 0 : p.Hq, mine = heads - first;
+  const int e0 = tid % TPV * 8;
+  const int step = gridDim.y * (kPgThreads / TPV), total = n * mine;
+#pragma unroll kUA
+  for (int v0 = blockIdx.y * (kPgThreads / TPV); v0 < total; v0 += step) {
+    const int v = v0 + tid / TPV;
+    const bool live = v < total;
+    const int r = live ? v / mine : 0, h = live ? first + v - r * mine : 0;
     float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const T* src = qkv + (row * heads + h) * HD;
     if (live) {
-      if (h < p.Hq + p.Hkv && half > 0) turned8(src, e0, half, turn, f);
-      else load8(src + e0, f);
+      const T* src = qkv + ((row0 + r) * heads + h) * HD;
+      if (h < p.Hq + p.Hkv && half > 0) {
+        int at = pos ? at_s[r] : max(s.place[r], 0);
+        if (at < 0 || at >= n_pos) {
+          set_device_error(err, DEVERR_INDEX);
+          at = min(max(at, 0), n_pos - 1);
+        }
+        turned8(src, e0, half, tab + (int64_t)at * half, f);
+      } else {
+        load8(src + e0, f);
+      }
+      if (h < p.Hq) store8(q_out + ((row0 + r) * p.Hq + h) * HD + e0, f);
     }
-    if (live && h < p.Hq) store8(q_out + (row * p.Hq + h) * HD + e0, f);
-    const bool cached = live && h >= p.Hq && page >= 0;
+    const bool cached = live && h >= p.Hq && s.vec[r] >= 0;
     const bool value = h >= p.Hq + p.Hkv;
-    const int g = h - p.Hq - (value ? p.Hkv : 0);
-    const int64_t vec = cached ? paged_vec(p, page, place, g) : 0;
+    const int64_t vec = s.vec[r] + ((int64_t)(h - p.Hq - (value ? p.Hkv : 0)) << p.page_log2);
     if (!I8) {
       if (cached) store8(static_cast<T*>(value ? p.v : p.k) + vec * HD + e0, f);
     } else {
@@ -134,39 +166,47 @@ __global__ void __launch_bounds__(kPgThreads)
 }
 
 template <typename T, int HD, bool I8>
-__global__ void __launch_bounds__(kPgThreads)
-    paged_read_kernel(const Paged p, T* k_out, T* v_out, int* err) {
-  constexpr int TPV = HD / 8;
+__global__ void __launch_bounds__(kPgThreads, kPgReadPerSm)
+    paged_read_kernel(const Paged p, T* k_out, T* v_out, int rows, int* err) {
+  constexpr int FPT = I8 ? 16 : 8;   // features of a thread
+  constexpr int TPV = HD / FPT;
+  __shared__ PgRows s;
   pdl_wait();
   pdl_trigger();
-  const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x & 31;
-  const int b = paged_find(p, row, lane);
-  int place = -1, page = -1;
-  if (b < p.B) {
-    const PagedSeq s = paged_seq(p, b, err);
-    const int i = (int)(row - s.row0);
-    if (i >= 0 && i < s.n) place = s.len - s.n + i;
-    if (place >= 0) page = paged_page(p, b, place, err);
-  }
-  const int e0 = (int)threadIdx.x % TPV * 8;
-  for (int h = (int)threadIdx.x / TPV; h < 2 * p.Hkv; h += kPgThreads / TPV) {
+  const int64_t row0 = (int64_t)blockIdx.x * rows;
+  const int n = (int)min((int64_t)rows, p.n_rows - row0);
+  pg_rows(p, row0, n, s, err);
+  const int tid = threadIdx.x, e0 = tid % TPV * FPT, total = n * 2 * p.Hkv;
+#pragma unroll kUR
+  for (int v = blockIdx.y * (kPgThreads / TPV) + tid / TPV; v < total; v += gridDim.y * (kPgThreads / TPV)) {
+    const int r = v / (2 * p.Hkv), h = v - r * 2 * p.Hkv;
     const bool value = h >= p.Hkv;
     const int g = h - (value ? p.Hkv : 0);
-    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (page >= 0) {
-      const int64_t vec = paged_vec(p, page, place, g);
-      if (I8) {
-        const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(value ? p.v : p.k) + vec * HD + e0);
-        const float scale = (value ? p.vs : p.ks)[vec];
+    const int64_t at = s.vec[r], vec = at + ((int64_t)g << p.page_log2);
+    T* dst = (value ? v_out : k_out) + ((row0 + r) * p.Hkv + g) * HD + e0;
+    if (I8) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      float scale = 0.f;
+      if (at >= 0) {
+        w = __ldg(reinterpret_cast<const uint4*>(static_cast<const int8_t*>(value ? p.v : p.k) + vec * HD + e0));
+        scale = __ldg((value ? p.vs : p.ks) + vec);
+      }
+      const uint32_t in[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          f[i] = (float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * scale;
-      } else {
-        load8(static_cast<const T*>(value ? p.v : p.k) + vec * HD + e0, f);
+      for (int k = 0; k < 2; ++k) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)(int8_t)(in[2 * k + (i >> 2)] >> (8 * (i & 3))) * scale;
+        store8(dst + 8 * k, f);
+      }
+    } else {
+      constexpr int N = 8 / Elem<T>::kVec;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(value ? p.v : p.k) + vec * HD + e0) + i;
+        reinterpret_cast<uint4*>(dst)[i] = at >= 0 ? __ldg(src) : make_uint4(0, 0, 0, 0);
       }
     }
-    store8((value ? v_out : k_out) + (row * p.Hkv + g) * HD + e0, f);
   }
 }
 
@@ -184,24 +224,37 @@ cudaError_t with_kind(int dtype, const Paged& p, F&& f) {
 
 }  // namespace
 
+// Rows of a block (equal shares of as many full waves of `per_sm` blocks an SM as are needed), and where there
+// are few rows, several blocks for the vectors of one.
+static dim3 pg_grid(int64_t n_rows, int vectors, int per_pass, int per_sm, int num_sms, int* rows) {
+  const int64_t wave = (int64_t)per_sm * num_sms, waves = (n_rows + kPgRows * wave - 1) / (kPgRows * wave);
+  *rows = (int)((n_rows + waves * wave - 1) / (waves * wave));
+  const int64_t blocks = (n_rows + *rows - 1) / *rows;
+  const int64_t passes = ((int64_t)*rows * vectors + per_pass - 1) / per_pass;
+  return dim3((unsigned)blocks, (unsigned)std::min<int64_t>(passes, std::max<int64_t>(1, wave / blocks)));
+}
+
 cudaError_t paged_append(int dtype, const Paged& p, const void* qkv, const float2* tab, int half, int n_pos,
                          const int32_t* pos, void* q_out, const Dev& dev) {
   return with_kind(dtype, p, [&](auto t, auto hd, auto i8) -> cudaError_t {
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
-    constexpr int per = kPgThreads / (HD / 8);
-    const int vecs = (q_out ? p.Hq : 0) + 2 * p.Hkv;
-    return launch_pdl(paged_append_kernel<T, HD, decltype(i8)::value>, dim3((unsigned)p.n_rows, (vecs + per - 1) / per),
-                      dim3(kPgThreads), 0, dev.stream, p, static_cast<const T*>(qkv), tab, half, n_pos, pos,
-                      static_cast<T*>(q_out), dev.err);
+    int rows;
+    const dim3 grid = pg_grid(p.n_rows, (q_out ? p.Hq : 0) + 2 * p.Hkv, kPgThreads / (HD / 8), kPgAppendPerSm, dev.num_sms, &rows);
+    return launch_pdl(paged_append_kernel<T, HD, decltype(i8)::value>, grid, dim3(kPgThreads), 0, dev.stream, p,
+                      static_cast<const T*>(qkv), tab, half, n_pos, pos, static_cast<T*>(q_out), rows, dev.err);
   });
 }
 
 cudaError_t paged_read(int dtype, const Paged& p, void* k_out, void* v_out, const Dev& dev) {
   return with_kind(dtype, p, [&](auto t, auto hd, auto i8) -> cudaError_t {
     using T = decltype(t);
-    return launch_pdl(paged_read_kernel<T, decltype(hd)::value, decltype(i8)::value>, dim3((unsigned)p.n_rows),
-                      dim3(kPgThreads), 0, dev.stream, p, static_cast<T*>(k_out), static_cast<T*>(v_out), dev.err);
+    constexpr int HD = decltype(hd)::value;
+    constexpr bool I8 = decltype(i8)::value;
+    int rows;
+    const dim3 grid = pg_grid(p.n_rows, 2 * p.Hkv, kPgThreads / (HD / (I8 ? 16 : 8)), kPgReadPerSm, dev.num_sms, &rows);
+    return launch_pdl(paged_read_kernel<T, HD, I8>, grid, dim3(kPgThreads), 0, dev.stream, p, static_cast<T*>(k_out),
+                      static_cast<T*>(v_out), rows, dev.err);
   });
 }
 

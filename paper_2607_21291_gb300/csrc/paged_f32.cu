@@ -26,7 +26,7 @@ constexpr int kPfThreads = 128;
 constexpr int kPfPLd = kPfTK + 4;
 constexpr int kPfSms = 160;
 
-template <int HD, int RT>
+template <int HD, int RT, bool I8>
 struct PfCfg {
   static constexpr int TX = RT == 64 ? 16 : 32;       // threads along the keys
   static constexpr int NR = RT == 64 ? 8 : 4;         // rows of a thread
@@ -35,7 +35,7 @@ struct PfCfg {
   static constexpr int LD = HD + 4;
   static constexpr int FLOATS = (RT + kPfTK) * LD + kPfTK * HD + RT * kPfPLd;
   static constexpr int SMEM = FLOATS * 4;
-  static constexpr int PER_SM = RT == 64 ? (HD == 64 ? 3 : 1) : (HD == 64 ? 5 : 2);
+  static constexpr int PER_SM = RT == 64 ? (HD == 64 ? 2 : 1) : HD == 64 ? (I8 ? 3 : 4) : 2;   // as registers and shared memory allow
   static constexpr int PART = RT * HD + 2 * RT;       // floats of a partial: O a thread, then (m, l) a row
 };
 
@@ -50,7 +50,7 @@ struct PfCut {
 template <int HD, int RT, bool I8>
 __global__ void __launch_bounds__(kPfThreads)
     paged_f32_kernel(const Paged p, const float* q, int64_t ld_q, float* out, float scale, int* sync, float* parts, int* err) {
-  using C = PfCfg<HD, RT>;
+  using C = PfCfg<HD, RT, I8>;
   using Cut = PfCut<RT>;
   constexpr int TX = C::TX, NR = C::NR, KC = C::KC, NF = C::NF, RPW = RT / 4;
   extern __shared__ __align__(16) float smem_pf[];
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kPfThreads)
 
 template <int HD, int RT, bool I8>
 cudaError_t launch_f32(const Paged& p, const float* q, int64_t ld_q, float* out, int* sync, float* scratch, const Dev& dev) {
-  using C = PfCfg<HD, RT>;
+  using C = PfCfg<HD, RT, I8>;
   const cudaError_t e = allow_smem<paged_f32_kernel<HD, RT, I8>, C::SMEM>();
   if (e != cudaSuccess) return e;
   const int G = p.Hq / p.Hkv;
@@ -350,7 +350,7 @@ cudaError_t launch_f32_store(const Paged& p, const float* q, int64_t ld_q, float
 }
 
 template <int HD, int RT>
-constexpr size_t f32_scratch() { return (size_t)kPfSms * PfCfg<HD, RT>::PER_SM * 2 * PfCfg<HD, RT>::PART * 4; }
+constexpr size_t f32_scratch() { return (size_t)kPfSms * PfCfg<HD, RT, false>::PER_SM * 2 * PfCfg<HD, RT, false>::PART * 4; }
 
 }  // namespace
 
