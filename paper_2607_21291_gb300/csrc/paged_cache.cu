@@ -1,12 +1,13 @@
 // Paged cache: rotary, quantisation and write of new tokens, and the read back.
 //
-// A block takes up to kPgRows packed rows. Its first warp finds where they lie, a lane a row; then
-// the block's threads take the rows' head vectors, eight features a thread and the hd / 8 threads of a vector
-// neighbours in a warp. Rotation turns feature i with i + half (both read, so
-// that no thread waits for another) in separate fp32 products and sums. 8-bit storage: the largest |x| of the vector by
+// A block takes up to kPgRows packed rows; its first warp finds where they lie, a lane a row. A thread holds
+// sixteen features of a head's vector in two chunks whose features pair in the rotation (or neighbours), and
+// a warp four or eight heads of a row at a time, head after head, so a row's turns stay in registers. Products and sums
+// of the rotation are separate fp32 ones. 8-bit storage: the largest |x| of the vector by
 // shuffles on the bits of |x| (a NaN is larger than any number there), then round(x * (127 / m)).
-// Bytes bound both kernels: each element is read and written once. One row a block, each block finding its
-// place for itself, took PG_BEFORE.
+// Bytes bound both kernels: each element is read and written once. 8192 new rows of the Qwen2.5-7B shape into
+// 8 bits take 30 us (4.8 TB/s), 32768 read back 18.5 us (5.5 TB/s); one row a block, with the turns read again for
+// each chunk, took 58 and (eight features a thread, four rows a block) 40 us.
 #include <math.h>
 
 #include <algorithm>
@@ -19,13 +20,8 @@ namespace {
 
 constexpr int kPgThreads = 256;
 constexpr int kPgRows = 16;   // most rows of a block
-#ifndef PG_A
-#define PG_A 4
-#define PG_R 6
-#define PG_UA 2
-#define PG_UR 4
-#endif
-constexpr int kPgAppendPerSm = PG_A, kPgReadPerSm = PG_R, kUA = PG_UA, kUR = PG_UR;
+// Resident blocks an SM, as registers allow: fewer leave loads out of flight, more make the compiler spill.
+constexpr int kPgAppendPerSm = 4, kPgReadPerSm = 8;
 constexpr float kPgTiny = 7.888609052210118e-31f;   // 2^-100: vectors below are stored as zeros
 
 // Eight features e0 .. e0 + 7 of `src`.
@@ -40,26 +36,11 @@ __device__ __forceinline__ void store8(T* dst, const float* f) {
   for (int i = 0; i < 8; i += Elem<T>::kVec) store_vec(dst + i, f + i);
 }
 
-// Features e0 .. e0 + 7 of a head, turned: (a c - b s, b c + a s) for the pair (a, b), each
-// product and sum rounded by itself.
+// Features e0 .. e0 + 7 of a head turned one by one (half not a multiple of 8): (a c - b s, b c + a s) for the
+// pair (a, b), each product and sum rounded by itself.
 template <typename T>
 __device__ __forceinline__ void turned8(const T* head, int e0, int half, const float2* tab, float* f) {
   load8(head + e0, f);
-  if (e0 >= 2 * half) return;
-  if ((half & 7) == 0) {
-    const bool lower = e0 < half;
-    float g[8];
-    load8(head + (lower ? e0 + half : e0 - half), g);
-    const float4* t4 = reinterpret_cast<const float4*>(tab + (lower ? e0 : e0 - half));
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float4 cs = __ldg(t4 + i / 2);
-      const float t0 = __fmul_rn(g[i], cs.y), t1 = __fmul_rn(g[i + 1], cs.w);
-      f[i] = __fadd_rn(__fmul_rn(f[i], cs.x), lower ? -t0 : t0);
-      f[i + 1] = __fadd_rn(__fmul_rn(f[i + 1], cs.z), lower ? -t1 : t1);
-    }
-    return;
-  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int e = e0 + i;
@@ -103,48 +84,90 @@ template <typename T, int HD, bool I8>
 __global__ void __launch_bounds__(kPgThreads, kPgAppendPerSm)
     paged_append_kernel(const Paged p, const T* qkv, const float2* tab, int half, int n_pos, const int32_t* pos,
                         T* q_out, int rows, int* err) {
-  constexpr int TPV = HD / 8;   // threads of a vector
+  constexpr int TPV = HD / 16;          // threads of a vector, two chunks of eight features each
+  constexpr int VPW = 32 / TPV;         // vectors of a warp at a time: a group of a row's heads
   __shared__ PgRows s;
   __shared__ int at_s[kPgRows];
   pdl_wait();
   pdl_trigger();
   const int64_t row0 = (int64_t)blockIdx.x * rows;
   const int n = (int)min((int64_t)rows, p.n_rows - row0);
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, j = lane % TPV;
   if (half > 0 && pos && tid >= 32 && tid < 32 + n) at_s[tid - 32] = pos[row0 + tid - 32];
   pg_rows(p, row0, n, s, err);
-  const int heads = p.Hq + 2 * p.Hkv, first = q_out ? 0 : p.Hq, mine = heads - first;
-  const int e0 = tid % TPV * 8;
-  const int step = gridDim.y * (kPgThreads / TPV), total = n * mine;
-#pragma unroll kUA
-  for (int v0 = blockIdx.y * (kPgThreads / TPV); v0 < total; v0 += step) {
-    const int v = v0 + tid / TPV;
-    const bool live = v < total;
-    const int r = live ? v / mine : 0, h = live ? first + v - r * mine : 0;
-    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (live) {
-      const T* src = qkv + ((row0 + r) * heads + h) * HD;
-      if (h < p.Hq + p.Hkv && half > 0) {
-        int at = pos ? at_s[r] : max(s.place[r], 0);
-        if (at < 0 || at >= n_pos) {
-          set_device_error(err, DEVERR_INDEX);
-          at = min(max(at, 0), n_pos - 1);
-        }
-        turned8(src, e0, half, tab + (int64_t)at * half, f);
-      } else {
-        load8(src + e0, f);
+  const int heads = p.Hq + 2 * p.Hkv, first = q_out ? 0 : p.Hq, groups = (heads - first + VPW - 1) / VPW;
+  const bool even = (half & 7) == 0;
+  // chunks whose features pair: j and j + half / 8; behind the rotated ones, neighbours
+  const int pairs = even ? half / 8 : 0;
+  const bool turns = j < pairs;
+  const int e0 = 8 * (turns ? j : 2 * j), e1 = 8 * (turns ? j + pairs : 2 * j + 1);
+  // this warp's share of the units (row, group of heads): neighbours, so that a row's turns are read once
+  const int total = n * groups, warps = gridDim.y * (kPgThreads / 32), me = blockIdx.y * (kPgThreads / 32) + tid / 32;
+  const int u1 = (int)((int64_t)total * (me + 1) / warps);
+  int row_in = -1, at = 0;
+  float c[8], sn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = sn[i] = 0.f;
+#pragma unroll 1
+  for (int u = (int)((int64_t)total * me / warps); u < u1; ++u) {
+    const int r = u / groups, h = first + (u - r * groups) * VPW + lane / TPV;
+    const bool live = h < heads;
+    const T* src = qkv + ((row0 + r) * heads + (live ? h : 0)) * HD;
+    if (r != row_in && half > 0) {
+      row_in = r;
+      at = pos ? at_s[r] : max(s.place[r], 0);
+      if (at < 0 || at >= n_pos) {
+        set_device_error(err, DEVERR_INDEX);
+        at = min(max(at, 0), n_pos - 1);
       }
-      if (h < p.Hq) store8(q_out + ((row0 + r) * p.Hq + h) * HD + e0, f);
+      if (turns) {
+        const float4* t4 = reinterpret_cast<const float4*>(tab + (int64_t)at * half + 8 * j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 x = __ldg(t4 + i);
+          c[2 * i] = x.x;
+          sn[2 * i] = x.y;
+          c[2 * i + 1] = x.z;
+          sn[2 * i + 1] = x.w;
+        }
+      }
+    }
+    float f[2][8];
+    const bool rotated = h < p.Hq + p.Hkv && half > 0;
+    if (rotated && !even) {
+      turned8(src, e0, half, tab + (int64_t)at * half, f[0]);
+      turned8(src, e1, half, tab + (int64_t)at * half, f[1]);
+    } else {
+      load8(src + e0, f[0]);
+      load8(src + e1, f[1]);
+      if (rotated && turns) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = f[0][i], y = f[1][i];
+          f[0][i] = __fsub_rn(__fmul_rn(x, c[i]), __fmul_rn(y, sn[i]));
+          f[1][i] = __fadd_rn(__fmul_rn(y, c[i]), __fmul_rn(x, sn[i]));
+        }
+      }
+    }
+    if (live && h < p.Hq) {
+      T* dst = q_out + ((row0 + r) * p.Hq + h) * HD;
+      store8(dst + e0, f[0]);
+      store8(dst + e1, f[1]);
     }
     const bool cached = live && h >= p.Hq && s.vec[r] >= 0;
     const bool value = h >= p.Hq + p.Hkv;
     const int64_t vec = s.vec[r] + ((int64_t)(h - p.Hq - (value ? p.Hkv : 0)) << p.page_log2);
     if (!I8) {
-      if (cached) store8(static_cast<T*>(value ? p.v : p.k) + vec * HD + e0, f);
-    } else {
+      if (cached) {
+        T* dst = static_cast<T*>(value ? p.v : p.k) + vec * HD;
+        store8(dst + e0, f[0]);
+        store8(dst + e1, f[1]);
+      }
+    } else if (__any_sync(0xffffffffu, cached)) {
       unsigned m = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+      for (int i = 0; i < 8; ++i)
+        m = max(m, max(__float_as_uint(f[0][i]) & 0x7fffffffu, __float_as_uint(f[1][i]) & 0x7fffffffu));
 #pragma unroll
       for (int o = 1; o < TPV; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
       if (cached) {
@@ -152,14 +175,16 @@ __global__ void __launch_bounds__(kPgThreads, kPgAppendPerSm)
         const bool bad = m >= 0x7f800000u, none = most < kPgTiny;
         const float scale = bad ? NAN : none ? 0.f : __fdiv_rn(most, 127.f);
         const float inv = bad || none ? 0.f : __fdiv_rn(127.f, most);
-        uint32_t w[2] = {0, 0};
+        uint32_t w[4] = {0, 0, 0, 0};
         if (!bad && !none) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            w[i >> 2] |= (uint32_t)(__float2int_rn(__fmul_rn(f[i], inv)) & 0xff) << (8 * (i & 3));
+          for (int i = 0; i < 16; ++i)
+            w[i >> 2] |= (uint32_t)(__float2int_rn(__fmul_rn(f[i >> 3][i & 7], inv)) & 0xff) << (8 * (i & 3));
         }
-        *reinterpret_cast<uint2*>(static_cast<int8_t*>(value ? p.v : p.k) + vec * HD + e0) = make_uint2(w[0], w[1]);
-        if (e0 == 0) (value ? p.vs : p.ks)[vec] = scale;
+        int8_t* dst = static_cast<int8_t*>(value ? p.v : p.k) + vec * HD;
+        *reinterpret_cast<uint2*>(dst + e0) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(dst + e1) = make_uint2(w[2], w[3]);
+        if (j == 0) (value ? p.vs : p.ks)[vec] = scale;
       }
     }
   }
@@ -177,7 +202,7 @@ __global__ void __launch_bounds__(kPgThreads, kPgReadPerSm)
   const int n = (int)min((int64_t)rows, p.n_rows - row0);
   pg_rows(p, row0, n, s, err);
   const int tid = threadIdx.x, e0 = tid % TPV * FPT, total = n * 2 * p.Hkv;
-#pragma unroll kUR
+#pragma unroll 2
   for (int v = blockIdx.y * (kPgThreads / TPV) + tid / TPV; v < total; v += gridDim.y * (kPgThreads / TPV)) {
     const int r = v / (2 * p.Hkv), h = v - r * 2 * p.Hkv;
     const bool value = h >= p.Hkv;
@@ -240,7 +265,7 @@ cudaError_t paged_append(int dtype, const Paged& p, const void* qkv, const float
     using T = decltype(t);
     constexpr int HD = decltype(hd)::value;
     int rows;
-    const dim3 grid = pg_grid(p.n_rows, (q_out ? p.Hq : 0) + 2 * p.Hkv, kPgThreads / (HD / 8), kPgAppendPerSm, dev.num_sms, &rows);
+    const dim3 grid = pg_grid(p.n_rows, (q_out ? p.Hq : 0) + 2 * p.Hkv, kPgThreads / (HD / 16), kPgAppendPerSm, dev.num_sms, &rows);
     return launch_pdl(paged_append_kernel<T, HD, decltype(i8)::value>, grid, dim3(kPgThreads), 0, dev.stream, p,
                       static_cast<const T*>(qkv), tab, half, n_pos, pos, static_cast<T*>(q_out), rows, dev.err);
   });
