@@ -154,6 +154,35 @@ struct PagedLine {
   }
 };
 
+// Waits that poll: a suspended thread is woken late (all of the kernel's waits with a suspension
+// of up to 100 us took 430 us where these take 404, at 2048 tokens on 14336 of 28 heads).
+__device__ __forceinline__ bool paged_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool paged_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* err, unsigned long long timeout_ns) {
+  if (paged_try(bar, parity)) return true;
+  const unsigned long long t0 = globaltimer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (paged_try(bar, parity)) return true;
+    if ((it & 63u) == 0) {
+      if (*abort_flag) return false;
+      if (globaltimer_ns() - t0 > timeout_ns) {
+        *abort_flag = 1;
+        set_device_error(err, DEVERR_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+
 // 2^x on the SFU (relative error about 2^-22, denormal results flushed).
 __device__ __forceinline__ float paged_ex2(float x) {
   float y;

@@ -20,7 +20,12 @@
 // into equal pieces, one per CTA: any mix of lengths fills the machine. An item cut in
 // pieces leaves fp32 partials in the workspace; the CTA that finishes last joins them in the
 // order of the pieces (a counter in the synchronisation area, left at zero), so the
-// result does not depend on which one that is.
+// result does not depend on which one that is. Its four warps take a quarter of the features
+// each: one single token on 131071 cached has 77 pieces a head to join (95 us with one warp).
+//
+// Measured, 28 query heads on 4 of 128: 8 single tokens on 32767 cached 89 us, 6.0 TB/s (89% of
+// a plain copy); 8-bit numbers 95 us, 2.9 TB/s, bound by the instructions that make them
+// bf16; 16 on up to 4096 in 8 bits 22 us; one on 131071 69 us; 256 on 300 43 us.
 #include <math.h>
 
 #include <algorithm>
@@ -30,11 +35,10 @@
 namespace adadsf {
 namespace {
 
-constexpr int kPrTK = 64;                 // keys of a tile
 constexpr int kPrRows = 16;               // packed rows of an item
-constexpr int kPrWarps = 4;               // consumer warps, 16 keys of a tile each
+constexpr int kPrWarps = 4;               // consumer warps, a quarter of a tile's keys each
 constexpr int kPrThreads = 32 * (kPrWarps + 1);
-constexpr int kPrPerSm = 2;               // CTAs an SM
+constexpr int kPrPerSm = 2;               // CTAs an SM (three, of 128 registers a thread: 8 to 10% slower)
 constexpr int kPrMaxCtas = 160 * kPrPerSm;
 constexpr int kPrPad = 2;                 // an item's start and end, in tiles
 constexpr int kPrWhole = 8;               // tiles up to which an item is not cut
@@ -42,13 +46,16 @@ constexpr int kPrMin = 4;                 // fewest places of a piece
 
 template <int HD, bool I8>
 struct PrCfg {
+  static constexpr int KPW = 16;                           // keys of a warp's step, a quarter of a tile (32: longer code, no faster)
+  static constexpr int TK = kPrWarps * KPW;                // keys of a tile
   static constexpr int STAGES = I8 || HD == 64 ? 5 : 3;
   static constexpr int SLABS = I8 ? 1 : HD / 64;           // 128-byte (8-bit, hd 64: 64-byte) wide parts of a row
   static constexpr int ROWB = I8 ? HD : 128;               // bytes of a row in a slab
-  static constexpr int TILE = SLABS * kPrTK * ROWB;        // K or V of a stage
-  static constexpr int SCALES = I8 ? 2 * kPrTK * 4 : 0;    // K scales, V scales
+  static constexpr int TILE = SLABS * TK * ROWB;           // K or V of a stage
+  static constexpr int SCALES = I8 ? 2 * TK * 4 : 0;       // K scales, V scales
   static constexpr int STAGE = 2 * TILE + (I8 ? 1024 : 0);  // tiles stay 1024-byte aligned
-  static constexpr int SMEM = STAGES * STAGE + 1024;
+  static constexpr int QF = HD / 32 * 2 * 32 * 16;         // the item's queries as A operands
+  static constexpr int SMEM = STAGES * STAGE + QF + 1024;
   static constexpr int MERGE = HD / 8 * 32 * 16;           // one warp's O
   static_assert(SCALES <= 1024 && 2 * MERGE <= 2 * TILE, "two warps' O fit the stage they free");
 };
@@ -68,9 +75,10 @@ __device__ __forceinline__ float2 lds_f2(uint32_t a) {
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
   return v;
 }
-// Groups of 16 packed rows, tiles of 64 keys.
+// Groups of 16 packed rows, tiles of TK keys.
+template <int TK>
 struct PrCut {
-  static constexpr int KEYS = kPrTK, PAD = kPrPad, WHOLE = kPrWhole;
+  static constexpr int KEYS = TK, PAD = kPrPad, WHOLE = kPrWhole;
   int G;
   __device__ __forceinline__ int groups(int n) const { return (int)(((int64_t)n * G + kPrRows - 1) / kPrRows); }
   __device__ __forceinline__ int tokens(int g) const { return (int)((((int64_t)g + 1) * kPrRows - 1) / G) + 1; }
@@ -82,12 +90,14 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
                       const bf16* q, int64_t ld_q, bf16* out, float scale_log2, int* sync, float* parts, int* err,
                       unsigned long long timeout_ns) {
   using C = PrCfg<HD, I8>;
+  using Cut = PrCut<C::TK>;
+  constexpr int KPW = C::KPW, TK = C::TK, KT = KPW / 8;   // a warp's keys of a tile, in n tiles
   constexpr int NT = HD / 8;                    // n tiles of the output
   constexpr int SLOT = kPrRows * HD + 64;       // floats of a partial: O (per lane and n tile), then (m, l)
   extern __shared__ __align__(1024) uint8_t dsm[];
   __shared__ __align__(8) uint64_t bars[2 * C::STAGES];
   __shared__ float2 ml_s[2][kPrRows];           // (m, l) of the merging warps
-  __shared__ int abort_s, failed_s;
+  __shared__ int abort_s, failed_s, done_s;
   const uint32_t ring = (smem_u32(dsm) + 1023u) & ~1023u;
   uint8_t* ring_p = dsm + (ring - smem_u32(dsm));
   const uint32_t full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[C::STAGES]);
@@ -110,25 +120,25 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
   pdl_wait();
   pdl_trigger();
   // this CTA's piece of the line
-  PagedLine<PrCut> line{PrCut{G}};
+  PagedLine<Cut> line{Cut{G}};
   int64_t per, ua, ub;
   line.piece(p, kPrMin, (int)blockIdx.x, (int)gridDim.x, lane, err, &per, &ua, &ub);
   if (ua >= ub) return;
 
   if (warp == kPrWarps) {
     // ------------------------------------------------------------ producer
-    const int box = min(1 << p.page_log2, kPrTK), boxes = kPrTK / box;   // rows of a copy, copies of a tile
+    const int box = min(1 << p.page_log2, TK), boxes = TK / box;   // rows of a copy, copies of a tile
     int issued = 0;
     bool ok = true;
     for (int64_t u = ua; ok && u < ub;) {
-      const PagedItem<PrCut> it = line.item(p, &u, lane, err);
+      const PagedItem<Cut> it = line.item(p, &u, lane, err);
       int t, t1;
       it.in(ua, ub, &t, &t1);
       if (it.seen == 0 || t >= t1) continue;
       const int32_t* tab = p.table + (int64_t)it.b * p.max_pages;
       // a lane's page of tile t; pages past the last visible key are not looked at
       auto page_of = [&](int t) {
-        const int place = t * kPrTK + lane * box;
+        const int place = t * TK + lane * box;
         return lane < boxes && place < it.seen ? tab[place >> p.page_log2] : 0;
       };
       int next = page_of(t);
@@ -136,18 +146,18 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
         const int st = issued % C::STAGES;
         const int page = next;
         if (t + 1 < t1) next = page_of(t + 1);
-        const int place = t * kPrTK + lane * box;
+        const int place = t * TK + lane * box;
         const bool want = lane < boxes && place < it.seen;
         const bool there = (unsigned)page < (unsigned)p.n_pages;
         if (want && !there) set_device_error(err, DEVERR_INDEX);
         int w = 0;
-        if (lane == 0) w = mbar_wait_bounded(empty0 + 8 * st, ((issued / C::STAGES) & 1) ^ 1, abort_flag, err, timeout_ns);
+        if (lane == 0) w = paged_wait(empty0 + 8 * st, ((issued / C::STAGES) & 1) ^ 1, abort_flag, err, timeout_ns);
         if (!__shfl_sync(0xffffffffu, w, 0)) { ok = false; break; }
         const uint32_t dk = ring + st * C::STAGE, ds = dk + 2 * C::TILE, fb = full0 + 8 * st;
         const unsigned wants = __ballot_sync(0xffffffffu, want), good = __ballot_sync(0xffffffffu, want && there);
         if (I8 && want && !there) {   // a page that is not: zeros, scales too
           float* sc = reinterpret_cast<float*>(ring_p + st * C::STAGE + 2 * C::TILE);
-          for (int i = 0; i < box; ++i) sc[lane * box + i] = sc[kPrTK + lane * box + i] = 0.f;
+          for (int i = 0; i < box; ++i) sc[lane * box + i] = sc[TK + lane * box + i] = 0.f;
         }
         __syncwarp();
         if (lane == 0)
@@ -160,14 +170,14 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           const int r = place & ((1 << p.page_log2) - 1);
 #pragma unroll
           for (int x = 0; x < C::SLABS; ++x) {
-            const uint32_t o = x * kPrTK * C::ROWB + lane * box * C::ROWB;
+            const uint32_t o = x * TK * C::ROWB + lane * box * C::ROWB;
             tma_load_3d(dk + o, &tk, x * 64, r, z, fb);
             tma_load_3d(dk + C::TILE + o, &tv, x * 64, r, z, fb);
           }
           if (I8 && there) {
             const int64_t vec = ((int64_t)z << p.page_log2) + r;
             bulk_load(ds + lane * box * 4, p.ks + vec, box * 4, fb);
-            bulk_load(ds + kPrTK * 4 + lane * box * 4, p.vs + vec, box * 4, fb);
+            bulk_load(ds + TK * 4 + lane * box * 4, p.vs + vec, box * 4, fb);
           }
         }
         ++issued;
@@ -186,7 +196,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
   const int mi = lane >> 3, mr = lane & 7;   // ldmatrix: this lane's matrix and row
   int taken = 0;
   for (int64_t u = ua; u < ub;) {
-    const PagedItem<PrCut> it = line.item(p, &u, lane, err);
+    const PagedItem<Cut> it = line.item(p, &u, lane, err);
     int t0, t1;
     it.in(ua, ub, &t0, &t1);
     if (t0 >= t1) continue;
@@ -211,34 +221,20 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
             *reinterpret_cast<uint4*>(dst[r] + e) = make_uint4(0, 0, 0, 0);
       continue;
     }
-    // Q as A operands: word w of a lane's chunk pairs the features that its keys' chunk pairs
-    uint32_t qa[HD / 16][4];
-    if (I8) {
-      // k step 4 i + w: features 16 c + 4 w .. + 3 of chunk c = (HD / 64) tig + i
+    // Q as A operands in shared memory (registers for them would cost a CTA an SM): part n of a lane is a 16-byte
+    // chunk of row gid or gid + 8 whose words pair with those of the keys' chunks (bf16: chunk 2 tig + i of slab s;
+    // 8 bits: halves of 16 features)
+    constexpr int QN = HD / 32;
+    uint4* sq = reinterpret_cast<uint4*>(ring_p + C::STAGES * C::STAGE);
 #pragma unroll
-      for (int i = 0; i < HD / 64; ++i)
+    for (int n = 0; n < QN; ++n) {
+      if (n % kPrWarps != warp) continue;
+      const int at = I8 ? 16 * (HD / 64 * tig + n / 2) + 8 * (n & 1) : 64 * (n / 2) + 8 * (2 * tig + (n & 1));
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const uint4* s4 = reinterpret_cast<const uint4*>(src[r] + 16 * (HD / 64 * tig + i));
-          const uint4 a = live[r] ? s4[0] : make_uint4(0, 0, 0, 0), b = live[r] ? s4[1] : make_uint4(0, 0, 0, 0);
-          qa[4 * i][r] = a.x; qa[4 * i][2 + r] = a.y;
-          qa[4 * i + 1][r] = a.z; qa[4 * i + 1][2 + r] = a.w;
-          qa[4 * i + 2][r] = b.x; qa[4 * i + 2][2 + r] = b.y;
-          qa[4 * i + 3][r] = b.z; qa[4 * i + 3][2 + r] = b.w;
-        }
-    } else {
-      // k steps 4 s + 2 i, + 1: features 64 s + 8 c .. + 7 of chunk c = 2 tig + i
-#pragma unroll
-      for (int s = 0; s < HD / 64; ++s)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const uint4 a = live[r] ? *reinterpret_cast<const uint4*>(src[r] + 64 * s + 8 * (2 * tig + i)) : make_uint4(0, 0, 0, 0);
-            qa[4 * s + 2 * i][r] = a.x; qa[4 * s + 2 * i][2 + r] = a.y;
-            qa[4 * s + 2 * i + 1][r] = a.z; qa[4 * s + 2 * i + 1][2 + r] = a.w;
-          }
+      for (int r = 0; r < 2; ++r)
+        sq[(2 * n + r) * 32 + lane] = live[r] ? *reinterpret_cast<const uint4*>(src[r] + at) : make_uint4(0, 0, 0, 0);
     }
+    named_bar_sync(1, 32 * kPrWarps);
     float o[NT][4];
     float m_r[2] = {-INFINITY, -INFINITY}, l_r[2] = {0.f, 0.f};
 #pragma unroll
@@ -249,46 +245,47 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
     int st = 0;
     for (int t = t0; t < t1; ++t, ++taken) {
       st = taken % C::STAGES;
-      ok = mbar_wait_bounded(full0 + 8 * st, (taken / C::STAGES) & 1, abort_flag, err, timeout_ns);
+      ok = paged_wait(full0 + 8 * st, (taken / C::STAGES) & 1, abort_flag, err, timeout_ns);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      const uint32_t kt = ring + st * C::STAGE, vt = kt + C::TILE, ks = kt + 2 * C::TILE, vs = ks + kPrTK * 4;
-      const int kw = warp * 16;                             // this warp's keys within the tile
-      const int j0 = t * kPrTK + kw;
+      const uint32_t kt = ring + st * C::STAGE, vt = kt + C::TILE, ks = kt + 2 * C::TILE, vs = ks + TK * 4;
+      const int kw = warp * KPW;                            // this warp's keys within the tile
+      const int j0 = t * TK + kw;
       if (j0 < it.seen) {
-        float sc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        float sc[KT][4];
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          const int row = kw + 8 * nt + gid;
-          if (I8) {
+        for (int nt = 0; nt < KT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+        // a loop: the tile's code is long for the instruction caches
+#pragma unroll 2
+        for (int n = 0; n < QN; n += 2) {
+          const uint4 a0 = sq[(2 * n) * 32 + lane], a1 = sq[(2 * n + 1) * 32 + lane];
+          const uint4 a2 = sq[(2 * n + 2) * 32 + lane], a3 = sq[(2 * n + 3) * 32 + lane];
 #pragma unroll
-            for (int i = 0; i < HD / 64; ++i) {
-              const int c = HD / 64 * tig + i;
+          for (int nt = 0; nt < KT; ++nt) {
+            const int row = kw + 8 * nt + gid;
+            if (I8) {
+              const int c = HD / 64 * tig + n / 2;
               const uint4 k4 = HD == 128 ? lds128(kt + row * 128 + ((c ^ (row & 7)) << 4))
                                          : lds128(kt + row * 64 + ((c ^ ((row >> 1) & 3)) << 4));
-              const uint32_t kw4[4] = {k4.x, k4.y, k4.z, k4.w};
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const uint32_t b0 = bf16_of_i8(__byte_perm(kw4[w], 0, 0x4140)), b1 = bf16_of_i8(__byte_perm(kw4[w], 0, 0x4342));
-                mma_16816(sc[nt], qa[4 * i + w][0], qa[4 * i + w][1], qa[4 * i + w][2], qa[4 * i + w][3], b0, b1);
-              }
+              auto half = [&](uint32_t w, uint32_t sel) { return bf16_of_i8(__byte_perm(w, 0, sel)); };
+              mma_16816(sc[nt], a0.x, a1.x, a0.y, a1.y, half(k4.x, 0x4140), half(k4.x, 0x4342));
+              mma_16816(sc[nt], a0.z, a1.z, a0.w, a1.w, half(k4.y, 0x4140), half(k4.y, 0x4342));
+              mma_16816(sc[nt], a2.x, a3.x, a2.y, a3.y, half(k4.z, 0x4140), half(k4.z, 0x4342));
+              mma_16816(sc[nt], a2.z, a3.z, a2.w, a3.w, half(k4.w, 0x4140), half(k4.w, 0x4342));
+            } else {
+              const uint32_t at = kt + (n / 2) * TK * 128 + row * 128;
+              const uint4 k4 = lds128(at + (((2 * tig) ^ (row & 7)) << 4)), k5 = lds128(at + (((2 * tig + 1) ^ (row & 7)) << 4));
+              mma_16816(sc[nt], a0.x, a1.x, a0.y, a1.y, k4.x, k4.y);
+              mma_16816(sc[nt], a0.z, a1.z, a0.w, a1.w, k4.z, k4.w);
+              mma_16816(sc[nt], a2.x, a3.x, a2.y, a3.y, k5.x, k5.y);
+              mma_16816(sc[nt], a2.z, a3.z, a2.w, a3.w, k5.z, k5.w);
             }
-          } else {
-#pragma unroll
-            for (int s = 0; s < HD / 64; ++s)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint4 k4 = lds128(kt + s * kPrTK * 128 + row * 128 + (((2 * tig + i) ^ (row & 7)) << 4));
-                const int k0 = 4 * s + 2 * i;
-                mma_16816(sc[nt], qa[k0][0], qa[k0][1], qa[k0][2], qa[k0][3], k4.x, k4.y);
-                mma_16816(sc[nt], qa[k0 + 1][0], qa[k0 + 1][1], qa[k0 + 1][2], qa[k0 + 1][3], k4.z, k4.w);
-              }
           }
         }
-        // online softmax over the warp's 16 keys; score [nt][2 r + e] is row gid + 8 r, key j0 + 8 nt + 2 tig + e
-        float2 vsc[2];
+        // online softmax over the warp's keys; score [nt][2 r + e] is row gid + 8 r, key j0 + 8 nt + 2 tig + e
+        float2 vsc[KT];
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int nt = 0; nt < KT; ++nt) {
           float2 k2 = make_float2(scale_log2, scale_log2);
           if (I8) {
             const float2 kk = lds_f2(ks + 4 * (kw + 8 * nt + 2 * tig));
@@ -298,10 +295,10 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           }
           sc[nt][0] *= k2.x; sc[nt][1] *= k2.y; sc[nt][2] *= k2.x; sc[nt][3] *= k2.y;
         }
-        const bool masked = j0 + 16 > open;
+        const bool masked = j0 + KPW > open;
         if (masked) {
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
+          for (int nt = 0; nt < KT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (j0 + 8 * nt + 2 * tig + (e & 1) >= lim[e >> 1]) sc[nt][e] = -INFINITY;
@@ -309,7 +306,9 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
         float corr[2], base[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float mx = fmaxf(fmaxf(sc[0][2 * r], sc[0][2 * r + 1]), fmaxf(sc[1][2 * r], sc[1][2 * r + 1]));
+          float mx = fmaxf(sc[0][2 * r], sc[0][2 * r + 1]);
+#pragma unroll
+          for (int nt = 1; nt < KT; ++nt) mx = fmaxf(mx, fmaxf(sc[nt][2 * r], sc[nt][2 * r + 1]));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
           const float mn = fmaxf(m_r[r], mx);
@@ -317,12 +316,12 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           corr[r] = paged_ex2(m_r[r] - base[r]);
           m_r[r] = mn;
         }
-        uint32_t pa[4], pl[4];   // weights: bf16, and what that leaves
+        uint32_t pa[2 * KT], pl[2 * KT];   // weights: bf16, and what that leaves
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float sum = 0.f;
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt) {
+          for (int nt = 0; nt < KT; ++nt) {
             float p0 = paged_ex2(sc[nt][2 * r] - base[r]), p1 = paged_ex2(sc[nt][2 * r + 1] - base[r]);
             sum += p0 + p1;
             if (I8) {   // a masked key's scale may be anything
@@ -394,28 +393,29 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           for (int np = 0; np < HD / 16; ++np) {
             uint32_t vb[4];
             const int row = kw + (mi & 1) * 8 + mr, col = np * 16 + (mi >> 1) * 8;
-            ldmatrix_x4_trans(vt + (col >> 6) * kPrTK * 128 + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4), vb);
+            ldmatrix_x4_trans(vt + (col >> 6) * TK * 128 + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4), vb);
             if (masked) { vb[0] &= keep0; vb[1] &= keep1; vb[2] &= keep0; vb[3] &= keep1; }
             mma_16816(o[2 * np], pa[0], pa[1], pa[2], pa[3], vb[0], vb[1]);
             mma_16816(o[2 * np + 1], pa[0], pa[1], pa[2], pa[3], vb[2], vb[3]);
             mma_16816(o[2 * np], pl[0], pl[1], pl[2], pl[3], vb[0], vb[1]);
             mma_16816(o[2 * np + 1], pl[0], pl[1], pl[2], pl[3], vb[2], vb[3]);
           }
-          for (int key = max(open, j0); key < min(it.seen, j0 + 16); ++key) {
+          for (int key = max(open, j0); key < min(it.seen, j0 + KPW); ++key) {
             const int x = key - j0, row = kw + x;
             float w[2];   // the weight as the products take it
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
               const int from = (lane & 28) | ((x & 7) >> 1);
-              const uint32_t hi = __shfl_sync(0xffffffffu, x < 8 ? pa[r] : pa[2 + r], from);
-              const uint32_t lo = __shfl_sync(0xffffffffu, x < 8 ? pl[r] : pl[2 + r], from);
+              uint32_t hi = x < 8 ? pa[r] : pa[2 + r], lo = x < 8 ? pl[r] : pl[2 + r];
+              hi = __shfl_sync(0xffffffffu, hi, from);
+              lo = __shfl_sync(0xffffffffu, lo, from);
               w[r] = (x & 1) ? __uint_as_float(hi & 0xffff0000u) + __uint_as_float(lo & 0xffff0000u)
                              : __uint_as_float(hi << 16) + __uint_as_float(lo << 16);
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               const uint32_t two = *reinterpret_cast<const uint32_t*>(
-                  ring_p + (vt - ring) + (j >> 3) * kPrTK * 128 + row * 128 + (((j & 7) ^ (row & 7)) << 4) + 4 * tig);
+                  ring_p + (vt - ring) + (j >> 3) * TK * 128 + row * 128 + (((j & 7) ^ (row & 7)) << 4) + 4 * tig);
               const float v0 = __uint_as_float(two << 16), v1 = __uint_as_float(two & 0xffff0000u);
               if (key < lim[0]) { o[j][0] = fmaf(w[0], v0, o[j][0]); o[j][1] = fmaf(w[0], v1, o[j][1]); }
               if (key < lim[1]) { o[j][2] = fmaf(w[1], v0, o[j][2]); o[j][3] = fmaf(w[1], v1, o[j][3]); }
@@ -480,64 +480,107 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // written by threads, next by a copy
     __syncwarp();
     if (lane == 0) mbar_arrive(empty0 + 8 * st);
-    if (warp != 0) continue;
-
     // warp 0 holds the piece's result
-    const int first = it.first_cta(per), last = it.last_cta(per, it.tiles - 1);
-    if (first != last) {
-      const int me = (int)blockIdx.x;
-      auto slot_of = [&](int cta) { return parts + ((int64_t)cta * 2 + (cta == first ? 1 : 0)) * SLOT; };
-      float4* po = reinterpret_cast<float4*>(slot_of(me));
+    // a row's 1 / l; a row without a key is zero, and one whose keys are all -inf or one of them NaN is NaN
+    auto inv_of = [&](int r) { return l_r[r] > 0.f ? 1.f / l_r[r] : lim[r] > 0 ? l_r[r] / l_r[r] : 0.f; };
+    if (t0 == 0 && t1 == it.tiles) {
+      if (warp != 0) continue;
+      if (I8) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) __stcg(po + j * 32 + lane, make_float4(o[j][0], o[j][1], o[j][2], o[j][3]));
-      float2* pm = reinterpret_cast<float2*>(slot_of(me) + kPrRows * HD);
+        for (int r = 0; r < 2; ++r) {
+          if (!live[r]) continue;
+          const float inv = inv_of(r);
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int j = 0; j < NT; j += 8) {
+              float f[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) f[k] = o[j + k][2 * r + e] * inv;
+              store_vec(dst[r] + NT * (2 * tig + e) + j, f);
+            }
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          if (!live[r]) continue;
+          const float inv = inv_of(r);
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            *reinterpret_cast<uint32_t*>(dst[r] + 8 * j + 2 * tig) = pack_bf16x2(o[j][2 * r] * inv, o[j][2 * r + 1] * inv);
+        }
+      }
+      continue;
+    }
+    const int first = it.first_cta(per), last = it.last_cta(per, it.tiles - 1);
+    auto slot_of = [&](int cta) { return parts + ((int64_t)cta * 2 + (cta == first ? 1 : 0)) * SLOT; };
+    if (warp == 0) {
+      float* mine = slot_of((int)blockIdx.x);
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        __stcg(reinterpret_cast<float4*>(mine) + j * 32 + lane, make_float4(o[j][0], o[j][1], o[j][2], o[j][3]));
       if (tig == 0) {
-        __stcg(pm + gid, make_float2(m_r[0], l_r[0]));
-        __stcg(pm + gid + 8, make_float2(m_r[1], l_r[1]));
+        __stcg(reinterpret_cast<float2*>(mine + kPrRows * HD) + gid, make_float2(m_r[0], l_r[0]));
+        __stcg(reinterpret_cast<float2*>(mine + kPrRows * HD) + gid + 8, make_float2(m_r[1], l_r[1]));
       }
       __threadfence();
       __syncwarp();
-      int done = 0;
-      if (lane == 0) done = atomicAdd(sync + first, 1) == last - first;
-      if (!__shfl_sync(0xffffffffu, done, 0)) continue;
-      __threadfence();
-      if (lane == 0) sync[first] = 0;
-      m_r[0] = m_r[1] = -INFINITY;
-      l_r[0] = l_r[1] = 0.f;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-      for (int c = first; c <= last; ++c) {
-        const float4* xo = reinterpret_cast<const float4*>(slot_of(c));
-        const float2* xm = reinterpret_cast<const float2*>(slot_of(c) + kPrRows * HD);
-        float4 x[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) x[j] = __ldcg(xo + j * 32 + lane);
-        const float2 ml[2] = {__ldcg(xm + gid), __ldcg(xm + gid + 8)};
-        float mine[2], theirs[2];
-        join_ml(ml, mine, theirs);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) join_o(j, x[j], mine, theirs);
+      if (lane == 0) {
+        const int done = atomicAdd(sync + first, 1) == last - first;
+        if (done) sync[first] = 0;
+        *(volatile int*)&done_s = done;
+        __threadfence();
       }
     }
+    named_bar_sync(1, 32 * kPrWarps);
+    const bool done = *(volatile int*)&done_s != 0;
+    named_bar_sync(1, 32 * kPrWarps);   // read before the next item's
+    if (!done) continue;
+    // the last one to finish joins the pieces, a quarter of the n tiles a warp, four pieces at a time
+    __threadfence();
+    constexpr int NW = NT / kPrWarps;
+    float4 sum[NW];
+#pragma unroll
+    for (int j = 0; j < NW; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    m_r[0] = m_r[1] = -INFINITY;
+    l_r[0] = l_r[1] = 0.f;
+    for (int c = first; c <= last; c += 4) {
+      float4 x[4][NW];
+      float2 ml[4][2];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float* from = slot_of(min(c + k, last));
+#pragma unroll
+        for (int j = 0; j < NW; ++j) x[k][j] = __ldcg(reinterpret_cast<const float4*>(from) + (warp * NW + j) * 32 + lane);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) ml[k][r] = __ldcg(reinterpret_cast<const float2*>(from + kPrRows * HD) + gid + 8 * r);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (c + k > last) break;
+        float mine[2], theirs[2];
+        join_ml(ml[k], mine, theirs);
+#pragma unroll
+        for (int j = 0; j < NW; ++j)
+          sum[j] = make_float4(sum[j].x * mine[0] + x[k][j].x * theirs[0], sum[j].y * mine[0] + x[k][j].y * theirs[0],
+                               sum[j].z * mine[1] + x[k][j].z * theirs[1], sum[j].w * mine[1] + x[k][j].w * theirs[1]);
+      }
+    }
+    // n tile j: features 8 j + 2 tig + e, or (8 bits) NT (2 tig + e) + j
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       if (!live[r]) continue;
-      const float inv = l_r[r] > 0.f ? 1.f / l_r[r] : lim[r] > 0 ? l_r[r] / l_r[r] : 0.f;
-      if (I8) {
-        // features NT (2 tig + e) + j
+      const float inv = inv_of(r);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int j = 0; j < NT; j += 8) {
-            float f[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = o[j + k][2 * r + e] * inv;
-            store_vec(dst[r] + NT * (2 * tig + e) + j, f);
-          }
-      } else {
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          *reinterpret_cast<uint32_t*>(dst[r] + 8 * j + 2 * tig) = pack_bf16x2(o[j][2 * r] * inv, o[j][2 * r + 1] * inv);
+      for (int j = 0; j < NW; ++j) {
+        const float a = (r ? sum[j].z : sum[j].x) * inv, b = (r ? sum[j].w : sum[j].y) * inv;
+        bf16* to = dst[r] + (I8 ? NT * 2 * tig + warp * NW + j : 8 * (warp * NW + j) + 2 * tig);
+        if (I8) {
+          to[0] = __float2bfloat16_rn(a);
+          to[NT] = __float2bfloat16_rn(b);
+        } else {
+          *reinterpret_cast<uint32_t*>(to) = pack_bf16x2(a, b);
+        }
       }
     }
   }
@@ -549,10 +592,10 @@ cudaError_t launch_rows(const Paged& p, const void* q, int64_t ld_q, void* out, 
   const cudaError_t e = allow_smem<paged_rows_kernel<HD, I8>, C::SMEM>();
   if (e != cudaSuccess) return e;
   CUtensorMap tk, tv;
-  if (!make_tmap_pages(&tk, p.k, p, I8, kPrTK) || !make_tmap_pages(&tv, p.v, p, I8, kPrTK)) return cudaErrorInvalidValue;
+  if (!make_tmap_pages(&tk, p.k, p, I8, C::TK) || !make_tmap_pages(&tv, p.v, p, I8, C::TK)) return cudaErrorInvalidValue;
   // no more CTAs than pieces of the fewest tiles that any counts could make
   const int G = p.Hq / p.Hkv;
-  const int64_t span = ((int64_t)p.max_pages << p.page_log2) / kPrTK + 1;
+  const int64_t span = ((int64_t)p.max_pages << p.page_log2) / C::TK + 1;
   const int64_t row_tiles = std::min<int64_t>((int64_t)p.B * ((p.max_new * (int64_t)G + kPrRows - 1) / kPrRows),
                                               p.n_rows * G);
   const int64_t most = std::max<int64_t>(1, (row_tiles * p.Hkv * (span + kPrPad) + kPrMin - 1) / kPrMin);

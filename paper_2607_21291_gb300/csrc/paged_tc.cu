@@ -146,35 +146,6 @@ __device__ __forceinline__ void commit(uint32_t bar, uint32_t lead) {
       "r"(lead)
       : "memory");
 }
-// Waits that poll: a suspended thread is woken late (all of the kernel's waits with a suspension
-// of up to 100 us took 430 us where these take 404, at 2048 tokens on 14336 of 28 heads).
-__device__ __forceinline__ bool try_now(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool wait_now(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* err, unsigned long long timeout_ns) {
-  if (try_now(bar, parity)) return true;
-  const unsigned long long t0 = globaltimer_ns();
-  for (uint32_t it = 1;; ++it) {
-    if (try_now(bar, parity)) return true;
-    if ((it & 63u) == 0) {
-      if (*abort_flag) return false;
-      if (globaltimer_ns() - t0 > timeout_ns) {
-        *abort_flag = 1;
-        set_device_error(err, DEVERR_TIMEOUT);
-        return false;
-      }
-    }
-  }
-}
-
 template <int HD, bool I8>
 __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
     paged_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
@@ -253,7 +224,7 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
   PagedLine<PtCut> line{PtCut{R}};
   int64_t per, ua, ub;
   line.piece(p, kPtPad + 1, (int)blockIdx.x, (int)gridDim.x, lane, err, &per, &ua, &ub);
-  auto wait = [&](uint32_t bar, uint32_t parity) { return wait_now(bar, parity, abort_flag, err, timeout_ns); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return paged_wait(bar, parity, abort_flag, err, timeout_ns); };
   auto all_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
   // a lane waits for its warp
   auto warp_wait = [&](uint32_t bar, uint32_t parity) {
