@@ -464,9 +464,9 @@ adadsf_status adadsf_decode_step(const adadsf_model_cfg *cfg, const adadsf_model
  * [head_dim] in cfg->dtype (ADADSF_KV_SAME) or as int8 (ADADSF_KV_I8), whose
  * fp32 scales k_scale, v_scale are [n_pages][n_kv_heads][page_size] (one a
  * token and head; NULL for ADADSF_KV_SAME). page_size: 16, 32, 64 or 128.
- * A value is stored as round(x * (127 / m)), ties to even, with scale m / 127,
- * m the largest |x| of its head's vector, and stands for that number times
- * its scale. Vectors with m < 2^-100 are stored as zeros; one that holds an
+ * A value is stored as round(x * ((1 / m) * 127)), in fp32, ties to even, with
+ * scale m / 127, m the largest |x| of its head's vector, and stands for that
+ * number times its scale. Vectors with m < 2^-100 are stored as zeros; one that holds an
  * infinity or a NaN gets a NaN scale (every feature reads back as NaN).
  *
  * adadsf_paged_batch: B sequences. starts [B+1] (non-decreasing, starts[0]

@@ -4,7 +4,7 @@
 // sixteen features of a head's vector in two chunks whose features pair in the rotation (or neighbours), and
 // a warp four or eight heads of a row at a time, head after head, so a row's turns stay in registers. Products and sums
 // of the rotation are separate fp32 ones. 8-bit storage: the largest |x| of the vector by
-// shuffles on the bits of |x| (a NaN is larger than any number there), then round(x * (127 / m)).
+// shuffles on the bits of |x| (a NaN is larger than any number there), then round(x * (127 (1 / m))).
 // Bytes bound both kernels: each element is read and written once. 8192 new rows of the Qwen2.5-7B shape into
 // 8 bits take 30 us (4.8 TB/s), 32768 read back 18.5 us (5.5 TB/s); one row a block, with the turns read again for
 // each chunk, took 58 and (eight features a thread, four rows a block) 40 us.
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kPgThreads, kPgAppendPerSm)
         const float most = __uint_as_float(m);
         const bool bad = m >= 0x7f800000u, none = most < kPgTiny;
         const float scale = bad ? NAN : none ? 0.f : __fdiv_rn(most, 127.f);
-        const float inv = bad || none ? 0.f : __fdiv_rn(127.f, most);
+        const float inv = bad || none ? 0.f : __fmul_rn(__frcp_rn(most), 127.f);   // a reciprocal for the products, not a division
         uint32_t w[4] = {0, 0, 0, 0};
         if (!bad && !none) {
 #pragma unroll

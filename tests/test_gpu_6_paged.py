@@ -303,12 +303,12 @@ def test_attention_reports_bad_counts(A, heads, store, new):
 
 # ------------------------------------------------------------------ write and read back
 def quantised64(x):
-    """(whole numbers, scale) by the header's rule: 32-bit quotients, the product rounded to
-    32 bits, then to the nearest whole number, ties to even."""
+    """(whole numbers, scale) by the header's rule: a 32-bit reciprocal and products, then
+    the nearest whole number, ties to even."""
     m = np.abs(x).max(-1)
     live = m >= np.float32(2.0 ** -100)
     with np.errstate(divide="ignore", invalid="ignore"):
-        inv = np.where(live, np.float32(127) / m, np.float32(0)).astype(np.float32)
+        inv = np.where(live, np.float32(1) / m * np.float32(127), np.float32(0)).astype(np.float32)
     s = np.where(live, m / np.float32(127), np.float32(0)).astype(np.float32)
     return np.rint(x * inv[..., None]).astype(np.int64), s
 
