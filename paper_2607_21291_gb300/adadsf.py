@@ -149,10 +149,13 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-def _s(stream) -> ctypes.c_void_p:
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+def _s(stream) -> int:
+    """The stream's handle; None is the current one (without making a Stream object of it: 2 us of a call's 10)."""
+    if stream is not None:
+        return stream.cuda_stream
+    if not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _dev(t: torch.Tensor, name: str):
@@ -539,8 +542,8 @@ class PagedBatch:
 
 
 def _rows(t: torch.Tensor, name: str, n_rows: int, cols: int, dtype: torch.dtype):
-    _dev(t, name)
-    if t.dtype != dtype or t.numel() != n_rows * cols:
+    if not (t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.numel() == n_rows * cols):
+        _dev(t, name)
         raise ValueError(f"{name} must be {n_rows} rows of {cols} of {dtype}")
 
 
@@ -556,12 +559,13 @@ def adadsf_paged_append(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, qkv
                         q_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Rotates the batch's rows of qkv (n_rows, q + 2 kv), writes keys and
     values to their pages and the rotated queries to q_out."""
-    n, q, kv = batch.n_rows, cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
-    _rows(qkv, "qkv", n, q + 2 * kv, TORCH_DTYPE[cfg.dtype])
+    hd, n, dtype = cfg.head_dim, batch.n_rows, TORCH_DTYPE[cfg.dtype]
+    q, kv = cfg.n_heads * hd, cfg.n_kv_heads * hd
+    _rows(qkv, "qkv", n, q + 2 * kv, dtype)
     if pos is not None:
         _rows(pos, "pos", n, 1, torch.int32)
     if q_out is not None:
-        _rows(q_out, "q_out", n, q, TORCH_DTYPE[cfg.dtype])
+        _rows(q_out, "q_out", n, q, dtype)
     if tab is not None:
         _rows(tab, "tab", tab.shape[0], cfg.rotary_dim, torch.float32)
     if ws is None:
@@ -575,9 +579,9 @@ def adadsf_paged_append(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, qkv
 def adadsf_paged_read(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, k_out: torch.Tensor, v_out: torch.Tensor,
                       ws: Optional[torch.Tensor] = None, stream=None):
     """Reads the batch's cached tokens back as rows (n_rows, kv)."""
-    kv = cfg.n_kv_heads * cfg.head_dim
-    _rows(k_out, "k_out", batch.n_rows, kv, TORCH_DTYPE[cfg.dtype])
-    _rows(v_out, "v_out", batch.n_rows, kv, TORCH_DTYPE[cfg.dtype])
+    kv, dtype = cfg.n_kv_heads * cfg.head_dim, TORCH_DTYPE[cfg.dtype]
+    _rows(k_out, "k_out", batch.n_rows, kv, dtype)
+    _rows(v_out, "v_out", batch.n_rows, kv, dtype)
     if ws is None:
         ws = workspace(256, k_out.device)
     _check(lib().adadsf_paged_read(ctypes.byref(cfg), cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(),
@@ -595,10 +599,10 @@ def adadsf_paged_attention(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, 
                            ws: Optional[torch.Tensor] = None, stream=None):
     """Causal attention of the batch's rows over their pages. q: (n_rows, q)
     with unit stride along a row (a slice of a wider matrix will do)."""
-    n, width = batch.n_rows, cfg.n_heads * cfg.head_dim
-    if not q.is_cuda or q.dtype != TORCH_DTYPE[cfg.dtype] or tuple(q.shape) != (n, width) or (n and q.stride(1) != 1):
-        raise ValueError(f"q must be a CUDA tensor ({n}, {width}) of {TORCH_DTYPE[cfg.dtype]} with unit stride along a row")
-    _rows(out, "out", n, width, TORCH_DTYPE[cfg.dtype])
+    n, width, dtype = batch.n_rows, cfg.n_heads * cfg.head_dim, TORCH_DTYPE[cfg.dtype]
+    if not q.is_cuda or q.dtype is not dtype or q.shape != (n, width) or (n and q.stride(1) != 1):
+        raise ValueError(f"q must be a CUDA tensor ({n}, {width}) of {dtype} with unit stride along a row")
+    _rows(out, "out", n, width, dtype)
     if ws is None:
         ws = workspace(adadsf_paged_attention_workspace_size(cfg, cache, batch), q.device)
     _check(lib().adadsf_paged_attention(ctypes.byref(cfg), cache.ref, batch.ref, q.data_ptr(),
@@ -615,16 +619,16 @@ def adadsf_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor,
     if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in DTYPE_CODE or (logits.numel() and logits.stride(1) != 1):
         raise ValueError("logits must be a CUDA tensor (B, V) of float32 or bfloat16 with unit stride along a row")
     B, V = logits.shape
-    ptr = []
-    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("u", u, torch.float32),
-                           ("token", token, torch.int32), ("logprob", logprob, torch.float32)):
+
+    def ptr(t, name, dtype=torch.float32):
         if t is None:
-            ptr.append(None)
-            continue
+            return None
         _rows(t, name, B, 1, dtype)
-        ptr.append(t.data_ptr())
-    _check(lib().adadsf_sample(logits.data_ptr(), logits.stride(0) if B > 1 else V, B, V, DTYPE_CODE[logits.dtype], *ptr,
+        return t.data_ptr()
+
+    _check(lib().adadsf_sample(logits.data_ptr(), logits.stride(0) if B > 1 else V, B, V, DTYPE_CODE[logits.dtype],
+                               ptr(temperature, "temperature"), ptr(top_k, "top_k", torch.int32), ptr(top_p, "top_p"),
+                               ptr(min_p, "min_p"), ptr(u, "u"), ptr(token, "token", torch.int32), ptr(logprob, "logprob"),
                                _s(stream)))
 
 
