@@ -22,6 +22,8 @@
 namespace adadsf {
 namespace {
 
+typedef unsigned long long u64;
+
 constexpr int kSmThreads = 512;
 constexpr int kSmWarps = kSmThreads / 32;
 constexpr int kSmBinsLog2 = 9, kSmBins = 1 << kSmBinsLog2;
@@ -31,13 +33,13 @@ constexpr int kSmMostCluster = 8;
 constexpr int kSmSmem = kSmThreads * kSmMostChunk * 4 + 16;
 static_assert((uint64_t)kSmThreads * kSmMostChunk << 14 < 1ull << 31, "14 bits of every key of a CTA, and top-k's equals' upper ones");
 static_assert(kSmMostCluster * kSmThreads * kSmMostChunk == kSampleMaxV, "the limit that the header states");
+// Keys that a search leaves are gathered in one CTA where they are this few.
+constexpr int kSmList = 3 * kSmThreads;
 constexpr uint32_t kSmNone = 0x007fffffu; // key of -infinity, of NaN and of padding
 // First bins: even in the distance from the largest logit (or from z = 0) to this, the last one takes the
 // rest (weights end at 28).
 constexpr float kSmEnd = 32.f, kSmBinsPer = (kSmBins - 1) / kSmEnd;
 constexpr float kSmUnit = 1099511627776.f;   // 2^40
-
-typedef unsigned long long u64;
 
 __device__ __forceinline__ uint32_t key_of(float x) {
   uint32_t u = __float_as_uint(x);
@@ -46,7 +48,19 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t key) {
-  return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
+  return __uint_as_float((~(uint32_t)((int32_t)key >> 31) | 0x80000000u) ^ key);
+}
+// A weight w in [0, 1] as whole multiples of 2^-40, to the nearest one, ties to even: hi 2^20 + lo, hi and lo up to 2^20. Sums
+// with 2^3 and 2^-17 round to multiples of 2^-20 and 2^-40 and leave them in their low bits: no conversions,
+// which go through a unit a sixteenth as wide, nor 64-bit shifts.
+struct SmWeight {
+  uint32_t hi, lo;
+  __device__ __forceinline__ u64 whole() const { return ((u64)hi << 20) + lo; }
+};
+__device__ __forceinline__ SmWeight weight_of(float w) {
+  const float a = __fadd_rz(w, 8.f), rest = __fsub_rn(w, __fsub_rn(a, 8.f));   // below 2^-20, exact
+  const float b = __fadd_rn(rest, 7.62939453125e-06f);
+  return SmWeight{__float_as_uint(a) - 0x41000000u, __float_as_uint(b) - 0x37000000u};
 }
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   uint32_t v;
@@ -66,13 +80,13 @@ struct SampleShared {
   // Histograms: counts in part 0, or weights in 14, 14 and the other bits: a CTA's keys do not fill a word with
   // 14 bits each, so that an addition needs no carry and nothing waits for it. Rounds over the cluster
   // take turns with two of everything that other CTAs read, so one barrier a round is enough.
-  uint32_t part[2][3][kSmBins];
+  uint32_t part[2][3][kSmBins];        // or the gathered keys, as they come in
   u64 total[2];                        // this CTA's total
-  u64 bins[2][kSmBins];                // sums over the cluster of this CTA's share of the bins
+  u64 bins[2][kSmBins];                // sums over the cluster of this CTA's share of the bins, or the gathered keys' indices
   u64 warp[kSmWarps];                  // block scan
   u64 found_before, found_in, found_all, found_target;
   uint32_t found_bin;
-  uint32_t most;                       // this CTA's largest key, read by the cluster
+  uint32_t most, least;                // this CTA's largest key, the smallest of its warps' largest ones; read by the cluster
   uint32_t index;                      // written by the CTA that finds it
 };
 
@@ -99,11 +113,18 @@ __device__ __forceinline__ u64 block_before(u64 v, SampleShared& s, u64* all) {
   return base + inc - v;
 }
 
-// The same over the cluster's threads, CTAs in order of their slices. A round of the cluster.
-__device__ __forceinline__ u64 cluster_before(u64 v, SampleShared& s, int& round, u64* all) {
+// The CTAs that hold the row's keys: a cluster, or one.
+__device__ __forceinline__ void row_sync(uint32_t n) {
+  if (n > 1) cluster_sync();
+  else __syncthreads();
+}
+
+// block_before over the threads of n CTAs in order of their slices. A round of the cluster.
+__device__ __forceinline__ u64 row_before(u64 v, SampleShared& s, int& round, u64* all, uint32_t n, uint32_t rank) {
   u64 mine;
   u64 before = block_before(v, s, &mine);
-  const uint32_t n = cluster_nctarank(), rank = cluster_ctarank();
+  *all = mine;
+  if (n == 1) return before;
   const int q = round++ & 1;
   if (threadIdx.x == 0) s.total[q] = mine;
   cluster_sync();
@@ -131,11 +152,10 @@ __device__ __forceinline__ u64 whole_target(double target) {
 // Each CTA adds up a share of the bins and all read the sums (every CTA reading every histogram took 8 us
 // a round, 11-bit ones 25: 16 words a thread cross the cluster's network slowly).
 template <bool WEIGHTS>
-__device__ __forceinline__ void find_bin(SampleShared& s, int q, u64 base, u64 target, double frac) {
-  const uint32_t n = cluster_nctarank(), rank = cluster_ctarank();   // 1, 2, 4 or 8
+__device__ __forceinline__ void find_bin(SampleShared& s, int q, u64 base, u64 target, double frac, uint32_t n, uint32_t rank) {
   const uint32_t share = kSmBins / n;
   const int tid = threadIdx.x;
-  cluster_sync();   // every CTA's histogram is complete
+  row_sync(n);   // every CTA's histogram is complete
   u64 v;
   if (n > 1) {
     const uint32_t c = tid & (n - 1), bin = rank * share + tid / n;
@@ -189,13 +209,14 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31;
-  const uint32_t n_cta = cluster_nctarank(), rank = cluster_ctarank();
+  uint32_t n_cta = cluster_nctarank(), rank = cluster_ctarank();   // 1 or 8; once the row's keys are gathered, 1 and 0
   const int row = blockIdx.x / n_cta;
   const int slice = kSmThreads * chunk, i0 = (int)rank * slice;
   const T* x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld + i0;
   // groups of four elements that are aligned in memory, aligned in shared memory too
   const int shift = (int)((reinterpret_cast<uintptr_t>(x) / sizeof(T)) & 3);
   uint32_t* keys = raw + shift;
+  const uint32_t* index = nullptr;     // of gathered keys
   const int there = min(max(a.V - i0, 0), slice);
   uint32_t most = 0;
   const int g0 = shift ? 1 : 0, g1 = (there + shift) / 4;   // whole groups
@@ -217,12 +238,21 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   if (lane == 0) s.warp[tid >> 5] = most;
   __syncthreads();
   if (tid == 0) {
-    for (int w = 0; w < kSmWarps; ++w) most = max(most, (uint32_t)s.warp[w]);
+    uint32_t least = most;
+    for (int w = 1; w < kSmWarps; ++w) {
+      most = max(most, (uint32_t)s.warp[w]);
+      least = min(least, (uint32_t)s.warp[w]);
+    }
     s.most = most;
+    s.least = least;
     s.index = 0xffffffffu;
   }
   cluster_sync();
-  for (uint32_t c = 0; c < n_cta; ++c) most = max(most, ld_cluster_u32(map_to_cta(smem_u32(&s.most), c)));
+  uint32_t least = 0xffffffffu;
+  for (uint32_t c = 0; c < n_cta; ++c) {
+    most = max(most, ld_cluster_u32(map_to_cta(smem_u32(&s.most), c)));
+    least = min(least, ld_cluster_u32(map_to_cta(smem_u32(&s.least), c)));
+  }
 
   const uint32_t* own = keys + tid * chunk;
   const float t = a.temperature ? a.temperature[row] : 1.f;
@@ -233,12 +263,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     const float w = expf(logit_of(k));
     return w >= 0.f ? w : 0.f;               // NaN (an infinite logit under an infinite temperature)
   };
-  // w 2^40 to the nearest whole number: a float of 2^24 or more is one, shifted
-  auto weight = [&](float w) -> u64 {
-    const float y = w * kSmUnit;
-    const uint32_t bits = __float_as_uint(y);
-    return y < 16777216.f ? (u64)__float2uint_rn(y) : (u64)((bits & 0x7fffffu) | 0x800000u) << ((bits >> 23) - 150);
-  };
+  auto weight = [&](float w) -> u64 { return weight_of(w).whole(); };
   int round = 0;
   const int k = a.top_k ? a.top_k[row] : 0;
   const float top_p = a.top_p ? a.top_p[row] : 1.f;
@@ -247,6 +272,17 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   // The first round of a search leaves the keys that can be kept, from low_key on, and among them the ones of
   // the bin that it found (keys from low to high): a bit for each of the thread's. Only those are looked at again.
   uint32_t low_key = 0, can[4] = {0, 0, 0, 0}, in_bin[4] = {0, 0, 0, 0};
+  auto mark_from = [&](uint32_t low) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t above = 0;
+      const int n = min(32, chunk - 32 * w);
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) above |= (uint32_t)(own[32 * w + i] >= low) << i;
+      can[w] = above;
+    }
+    low_key = low;
+  };
   auto mark_keys = [&](uint32_t low, uint32_t high) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -300,15 +336,41 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       run += __shfl_sync(0xffffffffu, inc, 31);
     }
   };
+  auto index_of = [&](int i) -> uint32_t { return index ? index[i] : (uint32_t)(i0 + i); };   // of number i of the slice
+  // Where the keys that can be kept are few, they move to the first CTA in the vocabulary's order, which goes on alone: its
+  // rounds need no cluster and take a third of the time. false: the others, which are done. Marks are to be made again.
+  auto gather = [&]() -> bool {
+    if (n_cta == 1) return true;
+    const int mine = __popc(can[0]) + __popc(can[1]) + __popc(can[2]) + __popc(can[3]);
+    u64 all;
+    uint32_t at = (uint32_t)row_before((u64)mine, s, round, &all, n_cta, rank);
+    if (all > kSmList) return true;
+    const uint32_t to_key = map_to_cta(smem_u32(&s.part[0][0][0]), 0), to_index = map_to_cta(smem_u32(&s.bins[0][0]), 0);
+    each_of(can, [&](int i, uint32_t key) { return make_uint2(key, (uint32_t)(i0 + tid * chunk + i)); }, [&](const uint2& a) {
+      st_cluster_u32(to_key + 4 * at, a.x);
+      st_cluster_u32(to_index + 4 * at, a.y);
+      ++at;
+    });
+    cluster_sync();
+    if (rank != 0) return false;
+    n_cta = 1;
+    chunk = ((int)all + kSmThreads - 1) / kSmThreads | 1;
+    keys = raw;
+    for (int i = tid; i < kSmThreads * chunk; i += kSmThreads) keys[i] = i < (int)all ? (&s.part[0][0][0])[i] : kSmNone;
+    own = keys + tid * chunk;
+    index = reinterpret_cast<const uint32_t*>(&s.bins[0][0]);
+    __syncthreads();
+    return true;
+  };
   // index of the n-th (from 1) key equal to k in the order of the vocabulary, in every CTA
   auto nth = [&](uint32_t k, u64 n) -> uint32_t {
     int c = 0;
     each([&](int, uint32_t key) { return (int)(key == k); }, [&](int one) { c += one; });
     u64 all;
-    const u64 before = cluster_before((u64)c, s, round, &all);
+    const u64 before = row_before((u64)c, s, round, &all, n_cta, rank);
     const int i = walk(before, (u64)c, n - 1, [&](int i) -> u64 { return keys[i] == k; });
-    if (i >= 0 && lane < (int)n_cta) st_cluster_u32(map_to_cta(smem_u32(&s.index), lane), (uint32_t)(i0 + i));
-    cluster_sync();
+    if (i >= 0 && lane < (int)n_cta) st_cluster_u32(map_to_cta(smem_u32(&s.index), lane), index_of(i));
+    row_sync(n_cta);
     return s.index;
   };
 
@@ -333,6 +395,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   uint32_t cut_key = 0;
   u64 cut_ties = ~0ull;       // ~0: all
   bool some_ties = false;     // fewer than there are
+  bool gone = false;          // the keys went to another CTA
   // One search. key_in: whether a key takes part; more: weight of `more_key` beside those (0: none); target: as
   // find_bin takes it. Out: the key, and in s.found_* the sums before and of it.
   // Weights of keys below tail_key go into the last bin together.
@@ -341,16 +404,17 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     const float from = fminf(top, 3.4e38f), per = kSmBinsPer;
     auto bin0 = [&](uint32_t k) -> int {   // falls with the key, slowly or not at all
       const float d = __fsub_rn(from, value_of(k)), e = W ? __fmul_rn(d, inv) : d;
-      return (int)fminf(fmaxf(__fmul_rn(e, per), 0.f), (float)(kSmBins - 1));   // NaN (0 times infinity): 0
+      const float at = fminf(fmaxf(__fmul_rn(e, per), 0.f), (float)(kSmBins - 1));   // NaN (0 times infinity): 0
+      return (int)(__float_as_uint(__fadd_rz(at, 8388608.f)) & 0x7fffffu);          // whole part, without a conversion
     };
-    struct Put { int bin; u64 w; };   // bin < 0: takes no part
+    struct Put { int bin; SmWeight w; };   // bin < 0: takes no part
     auto put = [&](int q, const Put& a) {
       if (a.bin < 0) return;
       if (!W) {
         atomicAdd(&s.part[q][0][a.bin], 1u);
         return;
       }
-      const uint32_t p0 = (uint32_t)a.w & 0x3fffu, p1 = (uint32_t)(a.w >> 14) & 0x3fffu, p2 = (uint32_t)(a.w >> 28);
+      const uint32_t p0 = a.w.lo & 0x3fffu, p1 = (a.w.lo >> 14) + ((a.w.hi & 0xffu) << 6), p2 = a.w.hi >> 8;
       atomicAdd(&s.part[q][0][a.bin], p0);
       atomicAdd(&s.part[q][1][a.bin], p1);
       if (p2) atomicAdd(&s.part[q][2][a.bin], p2);
@@ -362,13 +426,23 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       __syncthreads();
       return q;
     };
+    auto put_whole = [&](int q, int bin, u64 w) {   // any weight
+      if (bin < 0) return;
+      atomicAdd(&s.part[q][0][bin], (uint32_t)w & 0x3fffu);
+      atomicAdd(&s.part[q][1][bin], (uint32_t)(w >> 14) & 0x3fffu);
+      atomicAdd(&s.part[q][2][bin], (uint32_t)(w >> 28));
+    };
     int q = clear();
-    u64 rest = 0;
+    uint32_t rest_hi = 0, rest_lo = 0;
     auto first = [&](uint32_t key) {
       if (!key_in(key)) return;
-      const u64 w = W ? weight(chance(key)) : 1;
-      if (W && key < tail_key) rest += w;
-      else put(q, Put{bin0(key), w});
+      const SmWeight w = W ? weight_of(chance(key)) : SmWeight{0, 1};
+      if (W && key < tail_key) {
+        rest_hi += w.hi;
+        rest_lo += w.lo;
+      } else {
+        put(q, Put{bin0(key), w});
+      }
     };
     if (low_key) {
       each_of(can, [&](int, uint32_t key) { return key; }, first);
@@ -377,12 +451,13 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       for (int i = 0; i < chunk; ++i) first(own[i]);
     }
     if (W) {
+      u64 rest = ((u64)rest_hi << 20) + rest_lo;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
-      if (lane == 0) put(q, Put{kSmBins - 1, rest});
-      if (more && rank == 0 && tid == 0) put(q, Put{bin0(more_key), more});
+      if (lane == 0) put_whole(q, kSmBins - 1, rest);
+      if (more && rank == 0 && tid == 0) put_whole(q, bin0(more_key), more);
     }
-    find_bin<W>(s, q, 0, target, frac);
+    find_bin<W>(s, q, 0, target, frac, n_cta, rank);
     if (frac < 1.0) target = s.found_target;
     // keys that can lie in the bin, with room for roundings
     const int bin = (int)s.found_bin;
@@ -393,7 +468,15 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     uint32_t hi = near + room < INFINITY && bin > 0 ? min(key_of(near + room), most) : most;
     lo >>= KS;
     hi >>= KS;
-    mark_keys(min(max(lo << KS, low_key), most), hi << KS | ((1u << KS) - 1));
+    const uint32_t low = min(max(lo << KS, low_key), most), high = hi << KS | ((1u << KS) - 1);
+    mark_keys(low, high);
+    if (n_cta > 1 && (W || s.found_before + s.found_in <= kSmList)) {
+      if (!gather()) {
+        gone = true;
+        return 0;
+      }
+      if (n_cta == 1) mark_keys(low, high);
+    }
     while (lo < hi) {
       const int bits = max(0, 32 - __clz(hi - lo) - kSmBinsLog2);   // (hi - lo) >> bits is below kSmBins
       const u64 before = s.found_before;
@@ -403,10 +486,10 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       q = clear();
       each_of(in_bin, [&](int, uint32_t key) {
         const int at = key_in(key) ? bin_of(key) : -1;
-        return Put{at, W && at >= 0 ? weight(chance(key)) : 1};
+        return Put{at, W && at >= 0 ? weight_of(chance(key)) : SmWeight{0, 1}};
       }, [&](const Put& a) { put(q, a); });
-      if (W && more && rank == 0 && tid == 0) put(q, Put{bin_of(more_key), more});
-      find_bin<W>(s, q, before, target, 1.0);
+      if (W && more && rank == 0 && tid == 0) put_whole(q, bin_of(more_key), more);
+      find_bin<W>(s, q, before, target, 1.0, n_cta, rank);
       hi -= s.found_bin << bits;
       if (hi - lo > (1u << bits) - 1) lo = hi - ((1u << bits) - 1);
     }
@@ -414,7 +497,14 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     return KS == 0 ? hi : (hi & (0x80000000u >> KS)) ? hi << KS : (hi << KS) | ((1u << KS) - 1);
   };
   if (by_k) {
+    // Every warp has a key that is not below `least`: the k largest are not either.
+    if (n_cta > 1 && k <= (int)n_cta * kSmWarps && least > kSmNone) {
+      mark_from(least);
+      if (!gather()) return;
+      if (n_cta == 1) mark_from(least);
+    }
     cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, (u64)k, 1.0, 0);
+    if (gone) return;
     cut_ties = (u64)k - s.found_before;
     some_ties = cut_ties < s.found_in;
     __syncthreads();
@@ -428,6 +518,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     // of the equals of top-k's last, the kept ones
     const uint32_t key = search(std::true_type(), [&](uint32_t q) { return q > k_key || (q == k_key && k_ties == ~0ull); }, k_key,
                                 k_ties == ~0ull ? 0 : k_ties * weight(chance(k_key)), 0, (double)top_p, tail_key);
+    if (gone) return;
     const u64 one = weight(chance(key)), before = s.found_before;
     if (one > 0) {
       // the fewest equals whose weight takes the sum to the target
@@ -452,26 +543,31 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     const float low = top + t * z - 1e-5f * (fabsf(top) + 2.f * t * fabsf(z) + t);
     if (low > -INFINITY) cut_key = max(cut_key, min(key_of(low), most));
   }
-  auto kept = [&](int i, uint32_t key) -> u64 {   // number i of the slice
-    if (key < cut_key || (key == last_key && (uint32_t)(i0 + i) > last)) return 0;
+  auto kept = [&](int i, uint32_t key) -> SmWeight {   // number i of the slice
+    if (key < cut_key || (key == last_key && index_of(i) > last)) return SmWeight{0, 0};
     const float w = chance(key);
-    return w < min_p ? 0 : weight(w);
+    return weight_of(w < min_p ? 0.f : w);
   };
-  u64 sum = 0, all;
-  each([&](int i, uint32_t key) { return kept(tid * chunk + i, key); }, [&](u64 w) { sum += w; });
-  const u64 before = cluster_before(sum, s, round, &all);
+  uint32_t sum_hi = 0, sum_lo = 0;
+  each([&](int i, uint32_t key) { return kept(tid * chunk + i, key); }, [&](const SmWeight& w) {
+    sum_hi += w.hi;
+    sum_lo += w.lo;
+  });
+  const u64 sum = ((u64)sum_hi << 20) + sum_lo;
+  u64 all;
+  const u64 before = row_before(sum, s, round, &all, n_cta, rank);
   const double mark_d = (double)a.u[row] * (double)all;
   u64 mark = mark_d > 0.0 ? (u64)mark_d : 0;
   if (mark > all - 1) mark = all - 1;
-  const int i = walk(before, sum, mark, [&](int i) { return kept(i, keys[i]); });
+  const int i = walk(before, sum, mark, [&](int i) { return kept(i, keys[i]).whole(); });
   if (i >= 0 && lane == 0) {
-    a.token[row] = i0 + i;
+    a.token[row] = (int32_t)index_of(i);
     if (a.logprob) {
       const float rest = (float)((double)(all - (u64)kSmUnit) / (double)kSmUnit);
       a.logprob[row] = logit_of(keys[i]) - log1pf(rest);
     }
   }
-  cluster_sync();   // no CTA leaves while another reads its shared memory
+  row_sync(n_cta);   // no CTA leaves while another reads its shared memory
 }
 
 }  // namespace
