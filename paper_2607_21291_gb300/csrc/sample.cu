@@ -128,15 +128,16 @@ __device__ __forceinline__ u64 row_before(u64 v, SampleShared& s, int& round, u6
   const int q = round++ & 1;
   if (threadIdx.x == 0) s.total[q] = mine;
   cluster_sync();
-  u64 sum = 0;
+  const uint32_t lane = threadIdx.x & 31;
+  const u64 t = lane < n ? ld_cluster_u64(map_to_cta(smem_u32(&s.total[q]), lane)) : 0;
+  u64 lower = lane < rank ? t : 0, sum = t;
 #pragma unroll
-  for (uint32_t c = 0; c < kSmMostCluster; ++c) {
-    const u64 t = c < n ? ld_cluster_u64(map_to_cta(smem_u32(&s.total[q]), c)) : 0;
-    if (c < rank) before += t;
-    sum += t;
+  for (int o = 1; o < kSmMostCluster; o <<= 1) {   // the first lanes, a CTA each
+    lower += __shfl_xor_sync(0xffffffffu, lower, o);
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
   }
-  *all = sum;
-  return before;
+  *all = __shfl_sync(0xffffffffu, sum, 0);
+  return before + __shfl_sync(0xffffffffu, lower, 0);
 }
 
 // The smallest whole number whose double is `target` or more: compared with it, whole sums need no doubles.
@@ -248,20 +249,26 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     s.index = 0xffffffffu;
   }
   cluster_sync();
-  uint32_t least = 0xffffffffu;
-  for (uint32_t c = 0; c < n_cta; ++c) {
-    most = max(most, ld_cluster_u32(map_to_cta(smem_u32(&s.most), c)));
-    least = min(least, ld_cluster_u32(map_to_cta(smem_u32(&s.least), c)));
-  }
+  // a lane a CTA: loads from other CTAs one behind the other take a third of a microsecond each
+  most = __reduce_max_sync(0xffffffffu, lane < (int)n_cta ? ld_cluster_u32(map_to_cta(smem_u32(&s.most), lane)) : 0u);
+  const uint32_t least = __reduce_min_sync(0xffffffffu, lane < (int)n_cta ? ld_cluster_u32(map_to_cta(smem_u32(&s.least), lane)) : ~0u);
 
   const uint32_t* own = keys + tid * chunk;
   const float t = a.temperature ? a.temperature[row] : 1.f;
   const float inv = 1.f / t, top = value_of(most);
   auto logit_of = [&](uint32_t k) { return k == most ? 0.f : __fmul_rn(__fsub_rn(value_of(k), top), inv); };
-  auto chance = [&](uint32_t k) -> float {   // exp(z), 0 for what is never drawn
-    if (k <= kSmNone) return 0.f;
-    const float w = expf(logit_of(k));
-    return w >= 0.f ? w : 0.f;               // NaN (an infinite logit under an infinite temperature)
+  // exp(z): 0 of kSmNone, whose z is -infinity or NaN, as it is of an infinite logit under an infinite temperature
+  auto chance = [&](uint32_t k) -> float { return fmaxf(expf(logit_of(k)), 0.f); };
+  // f(i, keys i to i + 3) over the thread's keys, behind the last one kSmNone, where one is `low` or above: four chains
+  // of arithmetic side by side
+  auto by_four = [&](uint32_t low, auto f) {
+#pragma unroll 1
+    for (int i = 0; i < chunk; i += 4) {
+      uint32_t k4[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k4[j] = i + j < chunk ? own[i + j] : kSmNone;
+      if (max(max(k4[0], k4[1]), max(k4[2], k4[3])) >= low) f(i, k4);
+    }
   };
   auto weight = [&](float w) -> u64 { return weight_of(w).whole(); };
   int round = 0;
@@ -306,14 +313,8 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       for (uint32_t m = w == 0 ? marks[0] : w == 1 ? marks[1] : w == 2 ? marks[2] : marks[3]; m; m &= m - 1)
         f(g(32 * w + __ffs(m) - 1, own[32 * w + __ffs(m) - 1]));
   };
-  // The same for the thread's keys that can be kept, where they are few, or for all of them.
-  auto each = [&](auto g, auto f) {
-    if (low_key && !__any_sync(0xffffffffu, 3 * (__popc(can[0]) + __popc(can[1]) + __popc(can[2]) + __popc(can[3])) > chunk)) {
-      each_of(can, g, f);
-      return;
-    }
-#pragma unroll 2
-    for (int i = 0; i < chunk; ++i) f(g(i, own[i]));
+  auto few = [&]() {   // whether the warp's keys that can be kept are few
+    return low_key && !__any_sync(0xffffffffu, 3 * (__popc(can[0]) + __popc(can[1]) + __popc(can[2]) + __popc(can[3])) > chunk);
   };
   // Where, in the slice, a running sum passes `mark`, if that is in this warp's part: `before` and `sum` are
   // each thread's, value(i) the summands. The warp takes the thread's chunk 32 at a time. -1: elsewhere.
@@ -365,7 +366,12 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   // index of the n-th (from 1) key equal to k in the order of the vocabulary, in every CTA
   auto nth = [&](uint32_t k, u64 n) -> uint32_t {
     int c = 0;
-    each([&](int, uint32_t key) { return (int)(key == k); }, [&](int one) { c += one; });
+    if (few()) {
+      each_of(can, [&](int, uint32_t key) { return (int)(key == k); }, [&](int one) { c += one; });
+    } else {
+#pragma unroll 4
+      for (int i = 0; i < chunk; ++i) c += own[i] == k;
+    }
     u64 all;
     const u64 before = row_before((u64)c, s, round, &all, n_cta, rank);
     const int i = walk(before, (u64)c, n - 1, [&](int i) -> u64 { return keys[i] == k; });
@@ -396,10 +402,10 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   u64 cut_ties = ~0ull;       // ~0: all
   bool some_ties = false;     // fewer than there are
   bool gone = false;          // the keys went to another CTA
-  // One search. key_in: whether a key takes part; more: weight of `more_key` beside those (0: none); target: as
+  // One search. key_in: whether a key takes part, none below least_in does; more: weight of `more_key` beside those (0: none); target: as
   // find_bin takes it. Out: the key, and in s.found_* the sums before and of it.
   // Weights of keys below tail_key go into the last bin together.
-  auto search = [&](auto weights_c, auto key_in, uint32_t more_key, u64 more, u64 target, double frac, uint32_t tail_key) -> uint32_t {
+  auto search = [&](auto weights_c, auto key_in, uint32_t least_in, uint32_t more_key, u64 more, u64 target, double frac, uint32_t tail_key) -> uint32_t {
     constexpr bool W = decltype(weights_c)::value;
     const float from = fminf(top, 3.4e38f), per = kSmBinsPer;
     auto bin0 = [&](uint32_t k) -> int {   // falls with the key, slowly or not at all
@@ -434,21 +440,25 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     };
     int q = clear();
     uint32_t rest_hi = 0, rest_lo = 0;
-    auto first = [&](uint32_t key) {
-      if (!key_in(key)) return;
-      const SmWeight w = W ? weight_of(chance(key)) : SmWeight{0, 1};
-      if (W && key < tail_key) {
-        rest_hi += w.hi;
-        rest_lo += w.lo;
-      } else {
-        put(q, Put{bin0(key), w});
+    auto first = [&](uint32_t key, const SmWeight& w) {
+      const bool in = key_in(key), tail = W && key < tail_key;
+      if (W) {
+        rest_hi += in && tail ? w.hi : 0;
+        rest_lo += in && tail ? w.lo : 0;
       }
+      if (in && !tail) put(q, Put{bin0(key), w});
     };
+    auto worth = [&](uint32_t key) { return W ? weight_of(chance(key)) : SmWeight{0, 1}; };
     if (low_key) {
-      each_of(can, [&](int, uint32_t key) { return key; }, first);
+      each_of(can, [&](int, uint32_t key) { return key; }, [&](uint32_t key) { first(key, worth(key)); });
     } else {
-#pragma unroll 2
-      for (int i = 0; i < chunk; ++i) first(own[i]);
+      by_four(least_in, [&](int, const uint32_t (&k4)[4]) {
+        SmWeight w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = worth(k4[j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) first(k4[j], w[j]);
+      });
     }
     if (W) {
       u64 rest = ((u64)rest_hi << 20) + rest_lo;
@@ -503,7 +513,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       if (!gather()) return;
       if (n_cta == 1) mark_from(least);
     }
-    cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, (u64)k, 1.0, 0);
+    cut_key = search(std::false_type(), [](uint32_t) { return true; }, 0, 0, 0, (u64)k, 1.0, 0);
     if (gone) return;
     cut_ties = (u64)k - s.found_before;
     some_ties = cut_ties < s.found_in;
@@ -516,7 +526,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     const float tail = top + t * (logf((1.f - top_p) / (float)a.V) - 0.01f);
     const uint32_t tail_key = top_p > 0.f && tail - 1e-5f * fabsf(top) > -INFINITY ? min(key_of(tail - 1e-5f * fabsf(top)), most) : 0u;
     // of the equals of top-k's last, the kept ones
-    const uint32_t key = search(std::true_type(), [&](uint32_t q) { return q > k_key || (q == k_key && k_ties == ~0ull); }, k_key,
+    const uint32_t key = search(std::true_type(), [&](uint32_t q) { return q > k_key || (q == k_key && k_ties == ~0ull); }, k_key, k_key,
                                 k_ties == ~0ull ? 0 : k_ties * weight(chance(k_key)), 0, (double)top_p, tail_key);
     if (gone) return;
     const u64 one = weight(chance(key)), before = s.found_before;
@@ -543,16 +553,26 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     const float low = top + t * z - 1e-5f * (fabsf(top) + 2.f * t * fabsf(z) + t);
     if (low > -INFINITY) cut_key = max(cut_key, min(key_of(low), most));
   }
+  const bool ties = last != 0xffffffffu;
   auto kept = [&](int i, uint32_t key) -> SmWeight {   // number i of the slice
-    if (key < cut_key || (key == last_key && index_of(i) > last)) return SmWeight{0, 0};
     const float w = chance(key);
-    return weight_of(w < min_p ? 0.f : w);
+    bool drop = key < cut_key || w < min_p;
+    if (ties && key == last_key) drop |= index_of(i) > last;
+    return weight_of(drop ? 0.f : w);
   };
   uint32_t sum_hi = 0, sum_lo = 0;
-  each([&](int i, uint32_t key) { return kept(tid * chunk + i, key); }, [&](const SmWeight& w) {
+  auto add = [&](const SmWeight& w) {
     sum_hi += w.hi;
     sum_lo += w.lo;
-  });
+  };
+  if (few()) {
+    each_of(can, [&](int i, uint32_t key) { return kept(tid * chunk + i, key); }, add);
+  } else {
+    by_four(cut_key, [&](int i, const uint32_t (&k4)[4]) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) add(kept(tid * chunk + i + j, k4[j]));
+    });
+  }
   const u64 sum = ((u64)sum_hi << 20) + sum_lo;
   u64 all;
   const u64 before = row_before(sum, s, round, &all, n_cta, rank);
