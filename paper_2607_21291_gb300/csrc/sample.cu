@@ -102,15 +102,15 @@ __device__ __forceinline__ u64 block_before(u64 v, SampleShared& s, u64* all) {
   __syncthreads();   // the last call's sums are read
   if (lane == 31) s.warp[warp] = inc;
   __syncthreads();
-  u64 base = 0, sum = 0;
+  u64 sums = lane < kSmWarps ? s.warp[lane] : 0;
 #pragma unroll
-  for (int w = 0; w < kSmWarps; ++w) {
-    const u64 t = s.warp[w];
-    base += w < warp ? t : 0;
-    sum += t;
+  for (int o = 1; o < kSmWarps; o <<= 1) {
+    const u64 up = __shfl_up_sync(0xffffffffu, sums, o);
+    if (lane >= o) sums += up;
   }
-  *all = sum;
-  return base + inc - v;
+  *all = __shfl_sync(0xffffffffu, sums, kSmWarps - 1);
+  const u64 base = __shfl_sync(0xffffffffu, sums, warp ? warp - 1 : 0);
+  return (warp ? base : 0) + inc - v;
 }
 
 // The CTAs that hold the row's keys: a cluster, or one.
