@@ -42,10 +42,9 @@ constexpr float kSmEnd = 32.f, kSmBinsPer = (kSmBins - 1) / kSmEnd;
 constexpr float kSmUnit = 1099511627776.f;   // 2^40
 
 __device__ __forceinline__ uint32_t key_of(float x) {
-  uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return kSmNone;   // NaN: never drawn
-  if (u == 0x80000000u) u = 0;                           // -0 equals 0
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+  // -0 equals 0; a NaN is never drawn, as -infinity is not
+  const uint32_t u = __float_as_uint(fmaxf(__fadd_rn(x, 0.f), -INFINITY));
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float((~(uint32_t)((int32_t)key >> 31) | 0x80000000u) ^ key);
@@ -54,14 +53,16 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 // with 2^3 and 2^-17 round to multiples of 2^-20 and 2^-40 and leave them in their low bits: no conversions,
 // which go through a unit a sixteenth as wide, nor 64-bit shifts.
 struct SmWeight {
-  uint32_t hi, lo;
-  __device__ __forceinline__ u64 whole() const { return ((u64)hi << 20) + lo; }
+  uint32_t a, b;   // bits of the two sums
+  __device__ __forceinline__ uint32_t hi() const { return a - 0x41000000u; }
+  __device__ __forceinline__ uint32_t lo() const { return b - 0x37000000u; }
+  __device__ __forceinline__ u64 whole() const { return ((u64)hi() << 20) + lo(); }
 };
 __device__ __forceinline__ SmWeight weight_of(float w) {
   const float a = __fadd_rz(w, 8.f), rest = __fsub_rn(w, __fsub_rn(a, 8.f));   // below 2^-20, exact
-  const float b = __fadd_rn(rest, 7.62939453125e-06f);
-  return SmWeight{__float_as_uint(a) - 0x41000000u, __float_as_uint(b) - 0x37000000u};
+  return SmWeight{__float_as_uint(a), __float_as_uint(__fadd_rn(rest, 7.62939453125e-06f))};
 }
+
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
         atomicAdd(&s.part[q][0][a.bin], 1u);
         return;
       }
-      const uint32_t p0 = a.w.lo & 0x3fffu, p1 = (a.w.lo >> 14) + ((a.w.hi & 0xffu) << 6), p2 = a.w.hi >> 8;
+      const uint32_t lo = a.w.lo(), hi = a.w.hi(), p0 = lo & 0x3fffu, p1 = (lo >> 14) + ((hi & 0xffu) << 6), p2 = hi >> 8;
       atomicAdd(&s.part[q][0][a.bin], p0);
       atomicAdd(&s.part[q][1][a.bin], p1);
       if (p2) atomicAdd(&s.part[q][2][a.bin], p2);
@@ -443,12 +444,12 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     auto first = [&](uint32_t key, const SmWeight& w) {
       const bool in = key_in(key), tail = W && key < tail_key;
       if (W) {
-        rest_hi += in && tail ? w.hi : 0;
-        rest_lo += in && tail ? w.lo : 0;
+        rest_hi += in && tail ? w.hi() : 0;
+        rest_lo += in && tail ? w.lo() : 0;
       }
       if (in && !tail) put(q, Put{bin0(key), w});
     };
-    auto worth = [&](uint32_t key) { return W ? weight_of(chance(key)) : SmWeight{0, 1}; };
+    auto worth = [&](uint32_t key) { return W ? weight_of(chance(key)) : SmWeight{0, 0}; };
     if (low_key) {
       each_of(can, [&](int, uint32_t key) { return key; }, [&](uint32_t key) { first(key, worth(key)); });
     } else {
@@ -496,7 +497,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       q = clear();
       each_of(in_bin, [&](int, uint32_t key) {
         const int at = key_in(key) ? bin_of(key) : -1;
-        return Put{at, W && at >= 0 ? weight_of(chance(key)) : SmWeight{0, 1}};
+        return Put{at, W && at >= 0 ? weight_of(chance(key)) : SmWeight{0, 0}};
       }, [&](const Put& a) { put(q, a); });
       if (W && more && rank == 0 && tid == 0) put_whole(q, bin_of(more_key), more);
       find_bin<W>(s, q, before, target, 1.0, n_cta, rank);
@@ -560,10 +561,12 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
     if (ties && key == last_key) drop |= index_of(i) > last;
     return weight_of(drop ? 0.f : w);
   };
-  uint32_t sum_hi = 0, sum_lo = 0;
+  SmWeight some = {0, 0};   // bits added up, and how many
+  uint32_t n_some = 0;
   auto add = [&](const SmWeight& w) {
-    sum_hi += w.hi;
-    sum_lo += w.lo;
+    some.a += w.a;
+    some.b += w.b;
+    ++n_some;
   };
   if (few()) {
     each_of(can, [&](int i, uint32_t key) { return kept(tid * chunk + i, key); }, add);
@@ -573,7 +576,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       for (int j = 0; j < 4; ++j) add(kept(tid * chunk + i + j, k4[j]));
     });
   }
-  const u64 sum = ((u64)sum_hi << 20) + sum_lo;
+  const u64 sum = ((u64)(some.a - n_some * 0x41000000u) << 20) + (some.b - n_some * 0x37000000u);
   u64 all;
   const u64 before = row_before(sum, s, round, &all, n_cta, rank);
   const double mark_d = (double)a.u[row] * (double)all;
