@@ -482,6 +482,8 @@ adadsf_status adadsf_decode_step(const adadsf_model_cfg *cfg, const adadsf_model
  * counts are clamped, tokens of such pages read as zeros (keys included) and are not
  * written. A row whose place is negative (n_b > lens[b]) has no token: it
  * is not written, reads back as zeros and attends to nothing.
+ * Rows of no sequence (before starts[0], from starts[B] on) are not written to
+ * pages and read back as zeros; adadsf_paged_attention leaves them as they are.
  * Every count lives on the device, so launches depend on B, n_rows, max_new
  * and max_pages only and one captured graph serves growing sequences.
  * ---------------------------------------------------------------------- */

@@ -24,6 +24,13 @@
 // Weights enter the product as bf16. Where a row sees few keys their rounding does not average
 // out, so items of at most kPtFine keys add a second product with what the rounding left.
 // Every wait is bounded in time (device error word on give-up).
+//
+// Measured, 28 query heads on 4 of 128: 2048 tokens on 14336 cached 402 us, 1121 TFLOP/s (58% of a plain product's;
+// about 60 us of it do not grow with the cache, the slope is 1270). The chain softmax, product, next scores of a tile
+// bounds it: the tensor cores are busy 38% of the time, with only products issued they would reach 1500. 8-bit caches
+// take 648 us: conversion and scales share the schedulers with the softmax (420 us without the work of both, 546 and
+// 626 without either; scales read again instead of scaled scores written back were slower, 673). 7 ragged
+// chunks of 777 on up to 3001 in 8 bits, 12 query heads on 2: 126 us; 128 tokens on 100: 13.6 us.
 #include <math.h>
 
 #include <algorithm>

@@ -12,7 +12,12 @@
 // into a few of them, and its atomics into one queue), the next ones' even in the keys of the bin
 // found, down to one key. Weights are whole multiples of 2^-40 of the largest, so
 // their sums do not depend on order, and neither does the token.
-// A row is bound by latency: four to eight rounds over the cluster, each about a microsecond and a half.
+// For top-k up to the number of warps, keys below the smallest of the warps' largest ones are out at once. When
+// few keys are left (kSmList), they move to one CTA, whose rounds take a third of the time of the cluster's.
+// Few rows are bound by the latency of those rounds (two to eight, 2 us each over the cluster), many
+// rows by the instructions of the passes over the keys, half of them comparisons and logic on a pipe of half
+// rate. Measured: one row of 50304 bf16 5 us greedy, 11 with top-k 50, 15 with top-p 0.9; 16 rows of 152064 fp32 of
+// mixed settings 31 us; 256 of 151936 bf16 173 us (54 greedy, 82 with top-k 50, 272 with top-p 0.9).
 #include <math.h>
 
 #include <type_traits>
