@@ -7,7 +7,7 @@
 // keys and take turns: while one tile's softmax runs, the tensor cores work for the
 // other. Items lie on one line of blocks cut into equal pieces, one per SM (see PagedLine), so chunks
 // of any mix of lengths, and few rows over a long cache, fill the machine. Pieces of a cut
-// item leave fp32 partials; the one that finishes last joins them in order.
+// item leave fp32 partials; the one that finishes last joins them in order (many of them in two steps).
 //   warp 0      TMA: Q tiles of the item; bf16 caches: K and V blocks, a box a page
 //   warp 1      issues S_t = Q_t K^T (M = N = 128) into TMEM and, once the tile's softmax has
 //               written P_t over S_t, O_t += P_t V: P_t from TMEM, V as it lies in the pages (an
@@ -25,11 +25,12 @@
 // out, so items of at most kPtFine keys add a second product with what the rounding left.
 // Every wait is bounded in time (device error word on give-up).
 //
-// Measured, 28 query heads on 4 of 128: 2048 tokens on 14336 cached 402 us, 1121 TFLOP/s (58% of a plain product's;
-// about 60 us of it do not grow with the cache, the slope is 1270). The chain softmax, product, next scores of a tile
+// Measured, 28 query heads on 4 of 128: 2048 tokens on 14336 cached 392 us, 1150 TFLOP/s (60% of a plain product's;
+// about 50 us of it do not grow with the cache, the slope is 1270). The chain softmax, product, next scores of a tile
 // bounds it: the tensor cores are busy 38% of the time, with only products issued they would reach 1500. 8-bit caches
-// take 648 us: conversion and scales share the schedulers with the softmax (420 us without the work of both, 546 and
-// 626 without either; scales read again instead of scaled scores written back were slower, 673). 7 ragged
+// take 659 us: conversion and scales share the schedulers with the softmax (a fifth
+// less without the conversion, a third less without the scales besides; scales read again instead of scaled scores written back
+// were 4% slower). 7 ragged
 // chunks of 777 on up to 3001 in 8 bits, 12 query heads on 2: 126 us; 128 tokens on 100: 13.6 us.
 #include <math.h>
 
@@ -47,6 +48,9 @@ constexpr int kPtMaxCtas = 160;
 constexpr int kPtPad = 2;               // an item's start and end, in blocks
 constexpr int kPtWhole = 4;             // blocks up to which an item is not cut
 constexpr int kPtFine = 2048;           // keys up to which weights enter in two parts
+constexpr int kPtJoin = 8;              // pieces that are joined at a time
+constexpr int kPtGroups = 512;          // first counter of such groups
+static_assert(2 * kPtMaxCtas <= kPtGroups && (kPtGroups + 4 * kPtMaxCtas) * 4 <= (int)kSyncBytes, "counters");
 constexpr float kPtRescale = 8.f;       // O rescaled only when the row maximum grows by > 2^8
 
 template <int HD, bool I8>
@@ -629,9 +633,8 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
         __stcg(reinterpret_cast<float2*>(part_of((int)blockIdx.x) + kPtRows * HD) + r, make_float2(m, l));
         if (r == 0) __stcg(flag_of((int)blockIdx.x), odd);
       }
-      float inv = 0.f;
       if (first == last) {
-        inv = 1.f / l;
+        const float inv = 1.f / l;
 #pragma unroll 1
         for (int c = 0; c < HD / 32; ++c) {
           uint32_t o[32];
@@ -651,64 +654,92 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(o_free0 + 8 * t);
       if (first != last) {
-        __threadfence();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(wrote0 + 8 * t);
-        if (r < 32) {   // the tile's first warp counts the piece
-          if (!warp_wait(wrote0 + 8 * t, cut & 1)) { ok = false; break; }
-          if (lane == 0) {
-            __threadfence();
-            const int done = atomicAdd(sync + 2 * first + t, 1) == last - first;
-            if (done) sync[2 * first + t] = 0;
-            last_s[t] = done;
-            __threadfence();
-            mbar_arrive(told0 + 8 * t);
+        // Whether this is the last of n CTAs that come here for the tile; all of the tile's threads.
+        auto finish = [&](int* counter, int n) {
+          __threadfence();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(wrote0 + 8 * t);
+          if (r < 32) {   // the tile's first warp counts
+            if (!warp_wait(wrote0 + 8 * t, cut & 1)) return ok = false;
+            if (lane == 0) {
+              __threadfence();
+              const int done = atomicAdd(counter, 1) == n - 1;
+              if (done) *counter = 0;
+              last_s[t] = done;
+              __threadfence();
+              mbar_arrive(told0 + 8 * t);
+            }
           }
-        }
-        if (!warp_wait(told0 + 8 * t, cut & 1)) { ok = false; break; }
-        ++cut;
-        join = last_s[t] != 0;
-        if (join) {
+          if (!warp_wait(told0 + 8 * t, cut & 1)) return ok = false;
+          ++cut;
+          return last_s[t] != 0;
+        };
+        // Partials of CTAs from, from + step, .. to, in this order, into the first one's place, or divided by their sum into the output.
+        auto merge = [&](int from, int step, int to, bool out) {
           __threadfence();
           float mm = -INFINITY, ll = 0.f;
-          for (int c = first; c <= last; ++c) {
+          for (int c = from; c <= to; c += step) {
             mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(part_of(c) + kPtRows * HD) + r).x);
             odd |= __ldcg(flag_of(c));
           }
           const float base = mm == -INFINITY ? 0.f : mm;
-          for (int c = first; c <= last; ++c) {
+          for (int c = from; c <= to; c += step) {
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_of(c) + kPtRows * HD) + r);
             ll += ml.y * paged_ex2(ml.x - base);
           }
-          inv = 1.f / ll;
+          const float by = out ? 1.f / ll : 1.f;
+          if (live) {
 #pragma unroll 1
-          for (int e = 0; e < HD; e += 32) {
-            float v[32];
+            for (int e = 0; e < HD; e += 32) {
+              float v[32];
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = 0.f;
-#pragma unroll 1
-            for (int c = first; c <= last; ++c) {
-              const float* po = part_of(c);
-              const float f = paged_ex2(__ldcg(reinterpret_cast<const float2*>(po + kPtRows * HD) + r).x - base) * inv;
-              float4 x[8];
+              for (int k = 0; k < 32; ++k) v[k] = 0.f;
+#pragma unroll(I8 ? 1 : 2)
+              for (int c = from; c <= to; c += step) {
+                const float* po = part_of(c);
+                const float f = paged_ex2(__ldcg(reinterpret_cast<const float2*>(po + kPtRows * HD) + r).x - base) * by;
+                float4 x[8];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4*>(po) + (e / 4 + k) * kPtRows + r);
+                for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4*>(po) + (e / 4 + k) * kPtRows + r);
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                v[4 * k] = fmaf(x[k].x, f, v[4 * k]);
-                v[4 * k + 1] = fmaf(x[k].y, f, v[4 * k + 1]);
-                v[4 * k + 2] = fmaf(x[k].z, f, v[4 * k + 2]);
-                v[4 * k + 3] = fmaf(x[k].w, f, v[4 * k + 3]);
+                for (int k = 0; k < 8; ++k) {
+                  v[4 * k] = fmaf(x[k].x, f, v[4 * k]);
+                  v[4 * k + 1] = fmaf(x[k].y, f, v[4 * k + 1]);
+                  v[4 * k + 2] = fmaf(x[k].z, f, v[4 * k + 2]);
+                  v[4 * k + 3] = fmaf(x[k].w, f, v[4 * k + 3]);
+                }
+              }
+              if (out) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] = lim > 0 ? v[k] : 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) store_vec(dst + e + 8 * k, v + 8 * k);
+              } else {
+                float4* po = reinterpret_cast<float4*>(part_of(from));
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                  __stcg(po + (e / 4 + k) * kPtRows + r, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
               }
             }
-            if (live) {
-#pragma unroll
-              for (int k = 0; k < 32; ++k) v[k] = lim > 0 ? v[k] : 0.f;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) store_vec(dst + e + 8 * k, v + 8 * k);
-            }
           }
+          if (!out) {
+            __stcg(reinterpret_cast<float2*>(part_of(from) + kPtRows * HD) + r, make_float2(mm, ll));
+            if (r == 0) __stcg(flag_of(from), odd);
+          }
+        };
+        // Many pieces: by kPtJoin first, then these. One CTA reads 64 KB a tile and piece, 1.7 us: 12 tokens on 20000 cached of 28
+        // heads on 4, in 38 pieces a head, took 73 us in one step, 48 in two; 13 pieces are faster in one.
+        const int me = (int)blockIdx.x, pieces = last - first + 1;
+        const int step = pieces > 2 * kPtJoin ? kPtJoin : 1;
+        bool on = true;
+        if (step > 1) {
+          const int lead = first + (me - first) / kPtJoin * kPtJoin, end = min(lead + kPtJoin - 1, last);
+          on = finish(sync + kPtGroups + (2 * lead + (lead == first)) * 2 + t, end - lead + 1);
+          if (on && end > lead) merge(lead, 1, end, false);
         }
+        if (on) join = finish(sync + 2 * first + t, (pieces + step - 1) / step);
+        if (!ok) break;
+        if (join) merge(first, step, last, true);
       }
       if (odd && live && (first == last || join)) {
         // infinities and NaN among the values of the item's own new tokens: to the rows that see them

@@ -518,6 +518,22 @@ def test_attention_long_chunks(A, heads, store):
     assert ((got - ref).abs() <= bound + (2.0 ** -8 + 2.0 ** -16) * a).all()
 
 
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("heads,seqs", [((28, 4, 128, "bf16"), [(20, 20000)]), ((16, 1, 64, "bf16"), [(8, 30011)]),
+                                        ((7, 1, 128, "bf16"), [(30, 9001), (1, 300), (25, 9500)])], ids=str)
+def test_attention_many_pieces(A, heads, seqs, store):
+    """Few rows over many keys: tens of CTAs share an item, and their pieces are joined in
+    two steps. The bound is that of long chunks; a second call with the same workspace gives the same bits."""
+    w = World(A, shape_of(*heads), store, 128, seqs, seed=16)
+    q = queries(w)
+    ref, bound = attend64(w, q)
+    a = bound / (2.0 ** -8 + 2.0 ** -17)
+    ws = A.workspace(A.adadsf_paged_attention_workspace_size(w.cfg, w.cache, w.batch))
+    got = attend(A, w, q, ws)
+    assert ((got.double() - ref).abs() <= bound + (2.0 ** -8 + 2.0 ** -16) * a).all()
+    assert torch.equal(attend(A, w, q, ws), got)
+
+
 def _spoil(w, what, b, place, feature):
     """Makes a cached key or value of sequence b hold an infinity or a NaN, in the pool and in the
     reference; an 8-bit vector becomes NaN as a whole (a NaN scale, numbers zero)."""
