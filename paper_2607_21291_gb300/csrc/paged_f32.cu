@@ -300,17 +300,28 @@ __global__ void __launch_bounds__(kPfThreads)
 #pragma unroll
         for (int c = 0; c < NF; ++c) o[i][c] = 0.f;
       }
+      // maxima first: the sums of one piece then wait for no other's, and loads of several are in flight
+#pragma unroll 4
+      for (int cta = first; cta <= last; ++cta)
+#pragma unroll
+        for (int i = 0; i < NR; ++i) m[i] = fmaxf(m[i], __ldcg(reinterpret_cast<const float2*>(part_of(cta) + RT * HD) + row_of(i)).x);
+#pragma unroll 2
       for (int cta = first; cta <= last; ++cta) {
         const float* po2 = part_of(cta);
+        float x[NR][NF];
+        float2 ml[NR];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          const float2 ml = __ldcg(reinterpret_cast<const float2*>(po2 + RT * HD) + row_of(i));
-          const float m_new = fmaxf(m[i], ml.x), base = m_new == -INFINITY ? 0.f : m_new;
-          const float a = expf(m[i] - base), b = expf(ml.x - base);
-          l[i] = l[i] * a + ml.y * b;
-          m[i] = m_new;
+          ml[i] = __ldcg(reinterpret_cast<const float2*>(po2 + RT * HD) + row_of(i));
 #pragma unroll
-          for (int c = 0; c < NF; ++c) o[i][c] = o[i][c] * a + __ldcg(po2 + (i * NF + c) * kPfThreads + tid) * b;
+          for (int c = 0; c < NF; ++c) x[i][c] = __ldcg(po2 + (i * NF + c) * kPfThreads + tid);
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          const float f = expf(ml[i].x - (m[i] == -INFINITY ? 0.f : m[i]));
+          l[i] += ml[i].y * f;
+#pragma unroll
+          for (int c = 0; c < NF; ++c) o[i][c] += x[i][c] * f;
         }
       }
     }

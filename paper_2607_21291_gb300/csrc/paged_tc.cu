@@ -27,7 +27,7 @@
 //
 // Measured, 28 query heads on 4 of 128: 2048 tokens on 14336 cached 392 us, 1150 TFLOP/s (60% of a plain product's;
 // about 50 us of it do not grow with the cache, the slope is 1270). The chain softmax, product, next scores of a tile
-// bounds it: the tensor cores are busy 38% of the time, with only products issued they would reach 1500. 8-bit caches
+// bounds it: the tensor cores are busy 45% of the time, with only products issued they would reach 1500. 8-bit caches
 // take 659 us: conversion and scales share the schedulers with the softmax (a fifth
 // less without the conversion, a third less without the scales besides; scales read again instead of scaled scores written back
 // were 4% slower). 7 ragged
