@@ -103,6 +103,30 @@ def test_settings(A, V, dtype):
         check_row(x[b], int(token[b]), float(logprob[b]), *per[b], u[b])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [4097, 20000, 152064])
+def test_few_and_many_survivors(A, V, dtype):
+    """Cuts that leave a handful to thousands of tokens, around the sizes where a row's search changes
+    its way: ties by the hundred, rows sorted either way (all likely tokens in one part of
+    the row), rows of which a hundred tokens are not masked, alone or in every part."""
+    g = torch.Generator().manual_seed(V + 1)
+    kinds = [torch.randn(V, generator=g) * 2, torch.round(torch.randn(V, generator=g) * 8) / 4]
+    kinds += [kinds[0].sort().values, kinds[1].sort(descending=True).values]
+    few = torch.full((V,), -math.inf)
+    few[torch.randperm(V, generator=g)[:100]] = torch.randn(100, generator=g)
+    here = torch.full((V,), -math.inf)
+    here[V // 2:V // 2 + 100] = torch.randn(100, generator=g)
+    kinds += [few, here]
+    per = [(t, k, p, f) for k in (1, 2, 127, 128, 129, 700, 0) for t, p, f in ((1.0, 1.0, 0.0), (0.6, 0.9, 0.0), (1.5, 0.97, 0.02))]
+    rows = [(x, s) for x in kinds for s in per]
+    logits = torch.stack([x for x, _ in rows]).to(dtype).cuda()
+    u = torch.rand(len(rows), generator=g).tolist()
+    token, logprob = draw(A, logits, u, *[[s[i] for _, s in rows] for i in range(4)])
+    x = logits.double().cpu().numpy()
+    for b, (_, s) in enumerate(rows):
+        check_row(x[b], int(token[b]), float(logprob[b]), *s, u[b])
+
+
 def test_defaults_and_many_rows(A):
     """No settings at all, more rows than fit the machine at once, rows of a wider
     matrix that start at odd places."""
