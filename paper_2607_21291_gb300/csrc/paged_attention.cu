@@ -5,15 +5,18 @@
 
 namespace adadsf {
 
-// Packed rows (tokens x query heads of a group) of a sequence up to which paged_rows.cu runs: it reads the cache
-// once per 16 of them. us at 8 sequences of 4096 cached keys, 28 query heads on 4, that kernel and the one
-// on tcgen05: 28 rows (4 tokens) 31 and 45, 63 rows (9 tokens) 47 and 46.
-constexpr int kFewRows = 64;
-// Beyond them it runs while 16 rows of a key/value head make no more items than these, and these and their tiles of 64
-// keys no more steps: few items in many pieces cost the other kernel their joining. us, that kernel and the one
-// on tcgen05, 28 heads on 4: 32 tokens on 300 13 and 16, on 4096 26 and 39; 64 on 0 14 and 13; 128 on 300 (224 items) 26
-// and 20; 20 on 20000 (11268 steps) 51 and 54; 12 heads of 64: 100 on 500 13 and 18, in 8 bits 13 and 23.
-constexpr int64_t kFewItems = 128, kFewSteps = 8192;
+// Which bf16 calls paged_rows.cu takes, by packed rows of a sequence (tokens x query heads of a group), items (16 rows of
+// a key/value head) and steps (an item's tiles of 64 keys), as the host can bound them. It reads the cache
+// once per 16 rows: up to 16 always. Beyond, while its steps take less than what paged_tc.cu
+// needs besides its products (joining, and blocks of 128 rows that are not full), that is up to kFewSteps steps times features
+// (four times that of 8-bit caches for two items a head, which convert a key no slower than the other kernel), for up to
+// kFewRows rows, or for few items, which the other kernel would cut in many pieces. us, this kernel and that one:
+//   28 heads of 128 on 4    8 sequences of 4096, 4 tokens 28 and 39, 6 tokens 35 and 39, 9 tokens 43 and 40; 64 of 300, 9
+//                           tokens 36 and 25; 16 of 16000, 4 tokens 157 and 115, in 8 bits 172 and 194, 6 tokens 251 and 193
+//     one sequence          32 tokens on 300 13 and 16, on 4096 26 and 39; 64 on none 14 and 13; 128 on 300 26 and 20
+//   12 heads of 64          32 sequences of 700, 32 tokens 41 and 55, 64 tokens 68 and 56; one of 500, 100 tokens 13 and 18
+constexpr int kAnyRows = 16, kFewRows = 48;
+constexpr int64_t kFewItems = 128, kFewSteps = 1 << 20;
 
 size_t paged_attention_scratch(int dtype, const Paged& p) {
   return dtype == kBF16 ? std::max(paged_rows_scratch(p), paged_tc_scratch(p)) : paged_f32_scratch(p);
@@ -22,11 +25,11 @@ size_t paged_attention_scratch(int dtype, const Paged& p) {
 cudaError_t paged_attention(int dtype, const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch,
                             const Dev& dev) {
   if (dtype == kF32) return paged_f32(p, q, ld_q, out, sync, scratch, dev);
-  const int64_t G = p.Hq / p.Hkv;
-  const int64_t items = p.Hkv * std::min(p.B * ((p.max_new * G + 15) / 16), p.n_rows * G / 16 + p.B);   // at most
+  const int64_t G = p.Hq / p.Hkv, rows = p.max_new * G;
+  const int64_t items = std::min<int64_t>(p.Hkv * std::min(p.B * ((rows + 15) / 16), p.n_rows * G / 16 + p.B), 1 << 24);
   const int64_t steps = items * ((((int64_t)p.max_pages << p.page_log2) + 63) / 64);
   // a group of more heads than a row tile of tcgen05 has lanes stays with the rows
-  if (p.max_new * G <= kFewRows || (items <= kFewItems && steps <= kFewSteps) || !paged_tc_takes(p))
+  if (rows <= kAnyRows || (steps * p.hd <= kFewSteps * (p.i8 && rows <= 32 ? 4 : 1) && (rows <= kFewRows || items <= kFewItems)) || !paged_tc_takes(p))
     return paged_rows(p, q, ld_q, out, sync, scratch, dev);
   return paged_tc(p, q, ld_q, out, sync, scratch, dev);
 }

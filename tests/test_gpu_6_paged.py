@@ -519,6 +519,19 @@ def test_attention_long_chunks(A, heads, store):
 
 
 @pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("heads", [(28, 4, 128, "bf16"), (12, 2, 128, "bf16"), (16, 1, 64, "bf16"), (12, 12, 64, "bf16")], ids=str)
+def test_attention_many_odd_chunks(A, heads, store):
+    """Chunks around whole row tiles (128 rows: R tokens of a group's heads) and pairs of them, over
+    lengths around whole blocks of keys, enough of them to be taken as chunks."""
+    R = 128 // (heads[0] // heads[1])
+    new = [R - 1, R, R + 1, 2 * R - 1, 2 * R, 2 * R + 1, 4 * R + 1, 1, 0]
+    seqs = [(n, n + more) for k, n in enumerate(new) for more in (0, (127, 128, 129, 1, 256)[k % 5] + k)]
+    w = World(A, shape_of(*heads), store, 32, seqs + [(R, R - 3)] * 4, seed=17)
+    q = queries(w)
+    check_attention(A, w, q, attend(A, w, q))
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
 @pytest.mark.parametrize("heads,seqs", [((28, 4, 128, "bf16"), [(20, 20000)]), ((16, 1, 64, "bf16"), [(8, 30011)]),
                                         ((7, 1, 128, "bf16"), [(30, 9001), (1, 300), (25, 9500)])], ids=str)
 def test_attention_many_pieces(A, heads, seqs, store):
