@@ -156,6 +156,7 @@ __device__ __forceinline__ u64 whole_target(double target) {
 // Adds up the cluster's histograms number `q`, whose bins run from the largest keys down, and finds the
 // first bin that takes the running sum, from `base` on, to `target` or more. frac < 1: the
 // target is frac times the sum of all bins (at least 1), left in s.found_target. Results in s.found_*.
+// Where no bin does, it is the last one, which leaves everything in.
 // Each CTA adds up a share of the bins and all read the sums (every CTA reading every histogram took 8 us
 // a round, 11-bit ones 25: 16 words a thread cross the cluster's network slowly).
 template <bool WEIGHTS>
@@ -189,7 +190,7 @@ __device__ __forceinline__ void find_bin(SampleShared& s, int q, u64 base, u64 t
     __syncthreads();
     target = s.found_target;
   }
-  if (run < target && run + v >= target) {
+  if (run < target && (run + v >= target || tid == kSmBins - 1)) {
     s.found_bin = tid;
     s.found_before = run;
     s.found_in = v;
@@ -506,7 +507,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
       }, [&](const Put& a) { put(q, a); });
       if (W && more && rank == 0 && tid == 0) put_whole(q, bin_of(more_key), more);
       find_bin<W>(s, q, before, target, 1.0, n_cta, rank);
-      hi -= s.found_bin << bits;
+      hi -= min(s.found_bin << bits, hi - lo);
       if (hi - lo > (1u << bits) - 1) lo = hi - ((1u << bits) - 1);
     }
     // a key whose low bits are its type's: zeros above 0, ones below
@@ -528,8 +529,9 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   if (by_p) {
     const uint32_t k_key = cut_key;
     const u64 k_ties = cut_ties;
-    // All logits below this one together weigh less than 1 - top_p of the largest: the cut lies above.
-    const float tail = top + t * (logf((1.f - top_p) / (float)a.V) - 0.01f);
+    // All logits below this one together weigh less than 1 - top_p of the largest: the cut lies above. In whole units a
+    // weight is at most twice what it was (below half a unit it is 0), so each has half of its share; the rest is room for roundings.
+    const float tail = top + t * (logf((1.f - top_p) / (2.f * (float)a.V)) - 0.01f);
     const uint32_t tail_key = top_p > 0.f && tail - 1e-5f * fabsf(top) > -INFINITY ? min(key_of(tail - 1e-5f * fabsf(top)), most) : 0u;
     // of the equals of top-k's last, the kept ones
     const uint32_t key = search(std::true_type(), [&](uint32_t q) { return q > k_key || (q == k_key && k_ties == ~0ull); }, k_key, k_key,
@@ -557,7 +559,8 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const Sample a, i
   {
     const float z = min_p > 0.f ? fmaxf(logf(min_p), -28.5f) : -28.5f;
     const float low = top + t * z - 1e-5f * (fabsf(top) + 2.f * t * fabsf(z) + t);
-    if (low > -INFINITY) cut_key = max(cut_key, min(key_of(low), most));
+    if (low > -INFINITY) cut_key = max(cut_key, key_of(low));
+    cut_key = min(cut_key, most);   // the first is always kept
   }
   const bool ties = last != 0xffffffffu;
   auto kept = [&](int i, uint32_t key) -> SmWeight {   // number i of the slice

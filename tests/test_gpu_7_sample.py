@@ -266,3 +266,48 @@ def test_refusals(A):
         A.adadsf_sample(x, u, t.long())
     with pytest.raises(ValueError):
         A.adadsf_sample(x, u, t, top_k=u)
+
+
+# Weights in units of 2^-40 that round up by up to the factor of two that rounding has, and top_p so close to 1 that the
+# cut falls among them.
+NEAR_ONE = [1 - 2.0 ** -24, 1 - 2.0 ** -23, 1 - 2.0 ** -22, 1 - 3.5e-7, 1 - 2.0 ** -21, 1 - 2.0 ** -20, 0.999998, 0.999994, 0.9999]
+
+
+@pytest.mark.parametrize("at", ["first", "middle", "last"])
+@pytest.mark.parametrize("dtype,V,low,high", [
+    (torch.float32, 50304, math.log(2.56) - 40 * math.log(2), 0.0), (torch.float32, 152064, math.log(2.53) - 40 * math.log(2), 0.0),
+    (torch.float32, 152064, math.log(0.55) - 40 * math.log(2), 0.0), (torch.float32, 397312, math.log(0.52) - 40 * math.log(2), 0.0),
+    (torch.float32, 4096, math.log(0.7) - 40 * math.log(2), 0.0), (torch.float32, 152064, -0.5, 27.5), (torch.float32, 152064, 0.0, 28.0),
+    (torch.bfloat16, 152064, 0.0, 28.0), (torch.bfloat16, 151936, 0.0, 27.5), (torch.bfloat16, 397312, 0.0, 28.0),
+    (torch.bfloat16, 50304, 0.0, 26.75)], ids=str)
+def test_cut_in_a_flat_tail(A, dtype, V, low, high, at):
+    """One large logit above equal ones that weigh a unit or a few: kept are the large one and the first of
+    the others, as many as top_p asks for in whole units, and the draw goes by exact sums. With a temperature
+    of 1/2 and half the distances too. What is drawn is written in any case."""
+    u = [0.0, 0.25, 0.75, 1 - 2.0 ** -24]
+    rows = [(p, x, t) for p in NEAR_ONE for x in u for t in (1.0, 0.5)]
+    x = torch.full((len(rows), V), low, dtype=torch.float32)
+    top = {"first": 0, "middle": V // 3, "last": V - 1}[at]
+    x[:, top] = high
+    x = (x * torch.tensor([[t] for _, _, t in rows])).to(dtype)
+    other = (top + 1) % V
+    z = (x[:, other].double() - x[:, top].double()).numpy() / np.array([t for _, _, t in rows])
+    token, logprob = draw(A, x.cuda(), [r[1] for r in rows], [r[2] for r in rows], None, [r[0] for r in rows])
+    for b, (p, v, _) in enumerate(rows):
+        units = math.exp(z[b]) * 2.0 ** 40
+        w = round(units)
+        assert abs(units - w) < 0.49                                  # clear of a tie
+        p, v, one = float(np.float32(p)), float(np.float32(v)), 2 ** 40
+        total = one + w * (V - 1)
+        n = 0 if w == 0 else min(V - 1, max(0, math.ceil((p * total - one) / w)))   # others kept
+        kept = one + n * w
+        mark = int(v * kept)
+        before = min(n, top)                                          # kept others ahead of the large one
+        if w and mark < before * w:
+            want = mark // w
+        elif mark < before * w + one:
+            want = top
+        else:
+            want = top + 1 + (mark - before * w - one) // w
+        assert token[b] == want, (p, v, w, n, token[b], want)
+        assert abs(logprob[b] - ((0.0 if want == top else z[b]) - math.log(kept / one))) <= 1e-4
