@@ -507,6 +507,7 @@ class PagedCache:
                     raise ValueError(f"{name} must be float32 {tuple(k.shape[:3])}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.page_size = int(k.shape[0]), int(k.shape[2])
+        self.n_kv_heads, self.head_dim, self.dtype = cfg.n_kv_heads, cfg.head_dim, None if i8 else cfg.dtype   # int8 is for either
         self.struct = _PagedCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if i8 else None,
                                   v_scale.data_ptr() if i8 else None, self.n_pages, self.page_size,
                                   KV_I8 if i8 else KV_SAME)
@@ -547,6 +548,12 @@ def _rows(t: torch.Tensor, name: str, n_rows: int, cols: int, dtype: torch.dtype
         raise ValueError(f"{name} must be {n_rows} rows of {cols} of {dtype}")
 
 
+def _fits(cfg: ModelCfg, cache: PagedCache):
+    if cfg.n_kv_heads != cache.n_kv_heads or cfg.head_dim != cache.head_dim or cache.dtype not in (cfg.dtype, None):
+        raise ValueError(f"the cache is for {cache.n_kv_heads} heads of {cache.head_dim} of type {cache.dtype}, the "
+                         f"configuration has {cfg.n_kv_heads} of {cfg.head_dim} of type {cfg.dtype}")
+
+
 def adadsf_rope_table(cfg: ModelCfg, n_pos: int, device=None, stream=None) -> torch.Tensor:
     """(cos, sin) of positions 0 .. n_pos - 1: fp32 (n_pos, rotary_dim / 2, 2)."""
     tab = torch.empty(int(n_pos), cfg.rotary_dim // 2, 2, dtype=torch.float32, device=device or "cuda")
@@ -559,6 +566,7 @@ def adadsf_paged_append(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, qkv
                         q_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Rotates the batch's rows of qkv (n_rows, q + 2 kv), writes keys and
     values to their pages and the rotated queries to q_out."""
+    _fits(cfg, cache)
     hd, n, dtype = cfg.head_dim, batch.n_rows, TORCH_DTYPE[cfg.dtype]
     q, kv = cfg.n_heads * hd, cfg.n_kv_heads * hd
     _rows(qkv, "qkv", n, q + 2 * kv, dtype)
@@ -579,6 +587,7 @@ def adadsf_paged_append(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, qkv
 def adadsf_paged_read(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, k_out: torch.Tensor, v_out: torch.Tensor,
                       ws: Optional[torch.Tensor] = None, stream=None):
     """Reads the batch's cached tokens back as rows (n_rows, kv)."""
+    _fits(cfg, cache)
     kv, dtype = cfg.n_kv_heads * cfg.head_dim, TORCH_DTYPE[cfg.dtype]
     _rows(k_out, "k_out", batch.n_rows, kv, dtype)
     _rows(v_out, "v_out", batch.n_rows, kv, dtype)
@@ -599,6 +608,7 @@ def adadsf_paged_attention(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, 
                            ws: Optional[torch.Tensor] = None, stream=None):
     """Causal attention of the batch's rows over their pages. q: (n_rows, q)
     with unit stride along a row (a slice of a wider matrix will do)."""
+    _fits(cfg, cache)
     n, width, dtype = batch.n_rows, cfg.n_heads * cfg.head_dim, TORCH_DTYPE[cfg.dtype]
     if not q.is_cuda or q.dtype is not dtype or q.shape != (n, width) or (n and q.stride(1) != 1):
         raise ValueError(f"q must be a CUDA tensor ({n}, {width}) of {dtype} with unit stride along a row")

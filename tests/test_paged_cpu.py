@@ -111,3 +111,31 @@ def test_rope_table(A):
     f = A.lib().adadsf_rope_table
     assert f(ctypes.byref(cfg), -1, P, None) == f(ctypes.byref(cfg), 4, None, None) == A.ERR_INVALID_ARG
     assert f(ctypes.byref(cfg), 0, None, None) == A.OK
+
+
+def test_a_cache_of_another_shape_is_refused(A, monkeypatch):
+    """A cache that was made for other key/value heads, another head size or type than the call's configuration is refused
+    by the binding before anything else is looked at: its pages would be read and written out of bounds."""
+    import torch
+    monkeypatch.setattr(A, "_dev", lambda t, name: None)   # host tensors will do: nothing is launched
+    shape = S.QWEN25_1_5B
+    cfg = A.make_cfg(shape)
+    i32 = dict(dtype=torch.int32)
+    b = A.PagedBatch(torch.zeros(2, **i32), torch.zeros(1, **i32), torch.zeros(1, 4, **i32), 1, 1)
+    x = torch.zeros(1, shape.qkv_dim, dtype=torch.bfloat16)
+    q, kv = x[:, :shape.q_dim], x[:, :shape.kv_dim]
+    for store in (A.KV_SAME, A.KV_I8):
+        c = A.paged_cache(cfg, 3, 16, store, device="cpu")
+        others = [shape.replace(n_kv_heads=4), shape.replace(n_kv_heads=1), shape.replace(head_dim=64)]
+        if store == A.KV_SAME:
+            others.append(shape.replace(dtype="f32"))
+        for other in others:
+            wrong = A.make_cfg(other)
+            for call in (lambda: A.adadsf_paged_append(wrong, c, b, x, None, None, q, ws=x),
+                         lambda: A.adadsf_paged_read(wrong, c, b, kv, kv, ws=x),
+                         lambda: A.adadsf_paged_attention(wrong, c, b, q, q, ws=x),
+                         lambda: A.adadsf_paged_attention(wrong, c, b, q, q)):
+                with pytest.raises(ValueError, match="cache"):
+                    call()
+    with pytest.raises(ValueError, match="k_out"):           # an 8-bit cache serves either type: only the operand is wrong
+        A.adadsf_paged_read(A.make_cfg(shape.replace(dtype="f32")), A.paged_cache(cfg, 3, 16, A.KV_I8, device="cpu"), b, kv, kv, ws=x)
