@@ -324,15 +324,26 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           for (int nt = 0; nt < KT; ++nt) {
             float p0 = paged_ex2(sc[nt][2 * r] - base[r]), p1 = paged_ex2(sc[nt][2 * r + 1] - base[r]);
             sum += p0 + p1;
-            if (I8) {   // a masked key's scale may be anything
-              p0 = p0 > 0.f ? p0 * vsc[nt].x : 0.f;
-              p1 = p1 > 0.f ? p1 * vsc[nt].y : 0.f;
+            if (I8) {
+              p0 *= vsc[nt].x;
+              p1 *= vsc[nt].y;
             }
             const uint32_t two = pack_bf16x2(p0, p1);
             pa[2 * nt + r] = two;
             pl[2 * nt + r] = pack_bf16x2(p0 - __uint_as_float(two << 16), p1 - __uint_as_float(two & 0xffff0000u));
           }
           l_r[r] = l_r[r] * corr[r] + sum;
+        }
+        if (I8 && masked) {   // the scale of a key that a row does not see may be anything, and zero times it is not always zero
+#pragma unroll
+          for (int nt = 0; nt < KT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const int key = j0 + 8 * nt + 2 * tig;
+              const uint32_t sees = (key < lim[r] ? 0xffffu : 0u) | (key + 1 < lim[r] ? 0xffff0000u : 0u);
+              pa[2 * nt + r] &= sees;
+              pl[2 * nt + r] &= sees;
+            }
         }
         if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
 #pragma unroll

@@ -596,3 +596,33 @@ def test_attention_infinities_of_later_tokens(A, heads, new, store):
             assert torch.equal(got, want), (b, i)
             assert ((out[r] - ref[r]).abs()[want] <= bound[r][want]).all(), (b, i)
             r += 1
+
+
+@pytest.mark.parametrize("new", [1, 3, 200])
+@pytest.mark.parametrize("heads", [(28, 4, 128, "bf16"), (12, 12, 64, "bf16"), (8, 8, 64, "f32")], ids=str)
+def test_attention_nan_scale_of_no_weight(A, heads, new):
+    """8 bits: a visible token whose value has a NaN scale makes the row NaN however small its weight is, also where
+    that is 0 in 32 bits; rows that do not see it are as without it."""
+    w = World(A, shape_of(*heads), "i8", 32, [(new, 300), (new, 150 + new), (new, 200 + new)], seed=18)
+    q = queries(w).abs()
+    G, hd = w.shape.n_heads // w.shape.n_kv_heads, w.shape.head_dim
+    clean = [[x.clone() for x in t] for t in (w.K, w.V)]
+    at = [(0, 17), (1, 150 + new // 2), (2, 200 + new - 1)]          # seen by all rows, by half of them, by the last
+    for b, place in at:
+        _spoil(w, ("v", "nan"), b, place, 0)
+        page, slot = int(w.table[b, place // w.page]), place % w.page
+        w.k[page, 1, slot], w.ks[page, 1, slot] = -127, 1.0
+        clean[0][b][place, 1] = -127.0
+    out = attend(A, w, q).double().reshape(w.n_rows, w.shape.n_heads, hd)
+    w.K, w.V = clean
+    ref, bound = (t.reshape(out.shape) for t in attend64(w, q))
+    r = 0
+    for b, (n, l) in enumerate(w.seqs):
+        for i in range(n):
+            hit = l - n + i >= at[b][1]
+            want = torch.ones(w.shape.n_heads, hd, dtype=torch.bool, device="cuda")
+            if hit:
+                want[G:2 * G] = False
+            assert torch.equal(torch.isfinite(out[r]), want), (b, i)
+            assert ((out[r] - ref[r]).abs()[want] <= bound[r][want]).all(), (b, i)
+            r += 1
