@@ -1623,7 +1623,8 @@ static adadsf_status paged_view(const adadsf_model_cfg* cfg, const adadsf_paged_
   p->i8 = c->store == ADADSF_KV_I8;
   p->starts = b->starts; p->lens = b->lens; p->table = b->table;
   p->n_rows = b->n_rows;
-  p->B = b->B; p->max_new = b->max_new; p->max_pages = b->max_pages;
+  p->B = b->B; p->max_pages = b->max_pages;
+  p->max_new = (int)std::min<int64_t>(b->max_new, b->n_rows);   // no sequence has more
   p->Hq = cfg->n_heads; p->Hkv = cfg->n_kv_heads; p->hd = cfg->head_dim;
   return ADADSF_OK;
 }

@@ -875,7 +875,7 @@ cudaError_t launch_tc(const Paged& p, const void* q, int64_t ld_q, void* out, in
   if (!make_tmap_pages(&tk, p.k, p, I8, box) || !make_tmap_pages(&tv, p.v, p, I8, box)) return cudaErrorInvalidValue;
   // no more CTAs than pieces of the least size that any counts could make
   const int64_t span = ((int64_t)p.max_pages << p.page_log2) / kPtKB + 1;
-  const int64_t groups = std::min<int64_t>((int64_t)p.B * ((p.max_new + 2 * R - 1) / (2 * R)), p.n_rows);
+  const int64_t groups = std::min<int64_t>(p.B * (((int64_t)p.max_new + 2 * R - 1) / (2 * R)), p.n_rows);
   const int64_t most = std::max<int64_t>(1, (groups * p.Hkv * (span + kPtPad) + kPtPad) / (kPtPad + 1));
   return launch_pdl(paged_tc_kernel<HD, I8>, dim3((unsigned)std::min<int64_t>(most, std::min(dev.num_sms, kPtMaxCtas))),
                     dim3(C::THREADS), (size_t)C::SMEM, dev.stream, tq, tk, tv, p, static_cast<bf16*>(out),

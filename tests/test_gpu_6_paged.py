@@ -626,3 +626,20 @@ def test_attention_nan_scale_of_no_weight(A, heads, new):
             assert torch.equal(torch.isfinite(out[r]), want), (b, i)
             assert ((out[r] - ref[r]).abs()[want] <= bound[r][want]).all(), (b, i)
             r += 1
+
+
+@pytest.mark.parametrize("heads,store,seqs", [((28, 4, 128, "bf16"), "same", [(300, 2000), (90, 700)]), ((12, 2, 128, "bf16"), "i8", [(250, 1500)]),
+                                              ((12, 12, 64, "bf16"), "same", [(200, 900)]), ((8, 8, 64, "f32"), "same", [(70, 300)]),
+                                              ((28, 4, 128, "bf16"), "same", [(1, 900), (2, 70)])], ids=str)
+def test_attention_loose_bound_of_new_tokens(A, heads, store, seqs):
+    """max_new is a bound of the host's: one far above the rows that there are, up to the largest int32, gives the bits
+    that the closest one gives (as many CTAs share the work)."""
+    w = World(A, shape_of(*heads), store, 64, seqs, seed=19)
+    q = queries(w)
+    want = None
+    for bound in (w.n_rows, 2 ** 20, 2 ** 31 - 1):
+        w.batch = A.PagedBatch(w.starts, w.lens, w.table, w.n_rows, bound)
+        out = attend(A, w, q)
+        check_attention(A, w, q, out)
+        want = out if want is None else want
+        assert torch.equal(out, want), bound
