@@ -33,9 +33,12 @@ class PagePool:
         self.table = np.zeros((n_layers, batch, max_pages), dtype=np.int32)
         self.held = np.zeros((n_layers, batch), dtype=np.int64)   # pages
 
+    def pages(self, tokens: np.ndarray) -> np.ndarray:
+        return -(-tokens // self.page_size)
+
     def reserve(self, tokens: np.ndarray) -> bool:
         """Room for tokens (n_layers, batch); whether the table changed."""
-        want = -(-tokens // self.page_size)
+        want = self.pages(tokens)
         if (want > self.max_pages).any():
             raise ValueError(f"{int(tokens.max())} tokens of a sequence exceed {self.max_pages} pages of {self.page_size}")
         need = int(np.maximum(want - self.held, 0).sum())
@@ -74,7 +77,10 @@ class Server:
         self.lens = torch.zeros(L, self.B, dtype=torch.int32, device=self.device)
         self.thr = torch.full((L, self.B), float("inf"), device=self.device)
         self.pos = torch.zeros(self.B, dtype=torch.int32, device=self.device)
-        self.known, self.steps, self.longest = np.zeros((L, self.B), dtype=np.int64), 0, 0
+        self.known, self.steps = np.zeros((L, self.B), dtype=np.int64), 0
+        self.grows = np.zeros((L, self.B), dtype=bool)            # where a token can be kept at all
+        self.length = np.zeros(self.B, dtype=np.int64)            # tokens of a sequence; 0: none, or released
+        self.live = torch.zeros(self.B, dtype=torch.int32, device=self.device)
 
     # ------------------------------------------------------------ one layer's block on packed rows
     def _norm(self, x: torch.Tensor, w: dict, name: str) -> torch.Tensor:
@@ -131,7 +137,8 @@ class Server:
         pos = torch.cat([torch.arange(n, dtype=torch.int32, device=self.device) for n in T])
         K = np.array([[int(np.floor(r * n)) for n in T] for r in ratios], dtype=np.int64)
         self._reserve(K)
-        self.known, self.steps, self.longest = K, 0, int(T.max())
+        self.known, self.steps, self.grows, self.length = K, 0, K > 0, T.astype(np.int64)
+        self.live.fill_(1)
         self.lens.copy_(torch.from_numpy(K.astype(np.int32)))
         self.thr.fill_(float("inf"))
         self.pos.copy_(torch.from_numpy(T.astype(np.int32)))
@@ -156,14 +163,14 @@ class Server:
 
     def step(self, tokens: torch.Tensor, kept_out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One token of every sequence (B,): their final hidden states. kept_out:
-        (n_layers, B) bool."""
-        if self.longest >= self.max_len:
+        (n_layers, B) bool. A released sequence's token is of no effect."""
+        if self.length.max(initial=0) >= self.max_len:
             raise ValueError(f"a sequence is longer than {self.max_len}")
-        if (-(-(self.known + self.steps + 1) // self.pool.page_size) > self.pool.held).any():
+        if (self.pool.pages(np.where(self.grows, self.known + self.steps + 1, 0)) > self.pool.held).any():
             self.known, self.steps = self.lens.cpu().numpy().astype(np.int64), 0   # a page may run out: look
-            self._reserve(self.known + 1)
+            self._reserve(np.where(self.grows, self.known + 1, 0))
         self.steps += 1
-        self.longest += 1
+        self.length += self.length > 0
         x = self.extra["embed"][tokens.long()]
         for l, w in enumerate(self.layers):
             keep = self._scores(l, x) > self.thr[l]
@@ -176,7 +183,7 @@ class Server:
             x[rows] = (xr.float() + delta).to(self.dtype)
             if kept_out is not None:
                 kept_out[l] = keep
-        self.pos += 1
+        self.pos += self.live
         return self._norm(x, self.extra, "final")
 
     def sample(self, hidden: torch.Tensor, u: torch.Tensor, logprob: Optional[torch.Tensor] = None, **settings) -> torch.Tensor:
@@ -209,11 +216,13 @@ class Server:
         return list(zip(*[t.split(n.tolist()) for t in out]))
 
     def release(self, b: int):
-        """Gives sequence b's pages back to the pool."""
+        """Gives sequence b's pages back to the pool; it takes none again before the next prompts."""
         self.pool.release(b)
         self.lens[:, b] = 0
         self.thr[:, b] = float("inf")
-        self.known[:, b] = 0
+        self.pos[b] = 0
+        self.live[b] = 0
+        self.known[:, b], self.grows[:, b], self.length[b] = 0, False, 0
 
     def check(self):
         for ws in (self.ws, self.attn_ws):

@@ -149,3 +149,44 @@ def test_refusals(A):
     with pytest.raises(ValueError, match="flags"):
         from paper_2607_21291_gb300 import serve
         serve.Server(A.make_cfg(shape, A.FLAG_GATE_SIGMOID), [], {}, srv.head, 1, 16, 1)
+
+
+def test_a_released_sequence_stays_released(A):
+    """A sequence that is released between steps takes no page again, nor does a layer that keeps nothing; the others go on
+    with the pages that it gave back, past the length where it would have had to stop, and answer as without the release."""
+    shape = NEOX_SMALL
+    ids, prompts = prompts_of(shape)
+    srv, _, _ = make(A, shape, "same", 16, n_pages=14, max_len=75)     # the prompts fill the pool
+    other, _, _ = make(A, shape, "same", 16)
+    assert torch.equal(srv.prefill(prompts, RATIOS), other.prefill(prompts, RATIOS))
+    assert not srv.pool.free
+    srv.release(0)
+    free = len(srv.pool.free)
+    assert free == 7
+    for step in range(12):
+        tok = torch.tensor([int(ids[b, n + step]) for b, n in enumerate(LENS)], dtype=torch.int32, device="cuda")
+        flags = [torch.empty(shape.n_layers, len(LENS), dtype=torch.bool, device="cuda") for _ in range(2)]
+        got, want = srv.step(tok, flags[0]), other.step(tok, flags[1])
+        assert torch.equal(flags[0][:, 1:], flags[1][:, 1:]) and not flags[0][:, 0].any()
+        H.assert_close(H.to_np(got[1:]), H.to_np(want[1:]), H.tol(shape), f"step {step}")
+        assert (srv.pool.held[:, 0] == 0).all() and (srv.pool.held[2] == 0).all() and (other.pool.held[2] == 0).all()
+        assert (srv.lens[:, 0] == 0).all()
+    srv.check()
+    assert len(srv.pool.free) < free                                   # taken by the others
+    # everything released: steps need no page and meet no end
+    for b in range(1, len(LENS)):
+        srv.release(b)
+    for step in range(80):
+        srv.step(tok)
+    srv.check()
+    assert len(srv.pool.free) == 14
+    # the pool and the slots serve the next prompts
+    assert torch.equal(srv.prefill(prompts, RATIOS), other.prefill(prompts, RATIOS))
+    srv.release(3)                                                     # the next step needs a page
+    for step in range(5):
+        srv.step(tok)
+    with pytest.raises(ValueError, match="longer"):                    # 75 tokens
+        srv.step(tok)
+    srv.release(0)
+    srv.step(tok)
+    srv.check()
