@@ -190,3 +190,22 @@ def test_a_released_sequence_stays_released(A):
     srv.release(0)
     srv.step(tok)
     srv.check()
+
+
+def test_kept_numbers_are_the_librarys(A):
+    """Layers keep the numbers that the retention allocation gives, also where r T falls a rounding short of a whole
+    number (0.29 x 100, 0.58 x 50) or r a rounding above 1."""
+    ids = S.token_ids(32, len(LENS), 100, NEOX_SMALL.vocab)
+    lens = [100, 50, 1, 100]
+    srv, _, _ = make(A, NEOX_SMALL, "same", 16)
+    ratios = [0.29, 0.58, 1.0 + 1e-12]
+    kept = []
+    srv.prefill([torch.from_numpy(ids[b, :n].astype(np.int64)) for b, n in enumerate(lens)], ratios, kept)
+    srv.check()
+    want = [[int(O.kept_counts(r, n)) for n in lens] for r in ratios]
+    assert want == [[29, 14, 0, 29], [58, 29, 0, 58], [100, 50, 1, 100]]
+    assert [[len(k) for k in row] for row in kept] == want == srv.lens.tolist()
+    # and no fewer than none, no more than all
+    assert [int(O.kept_counts(r, 10)) for r in (-0.5, 2.0)] == [0, 10]
+    srv.prefill([torch.from_numpy(ids[b, :10].astype(np.int64)) for b in range(4)], [-0.5, 2.0, 0.5])
+    assert srv.lens.tolist() == [[0] * 4, [10] * 4, [5] * 4]
