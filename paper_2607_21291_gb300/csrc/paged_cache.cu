@@ -54,7 +54,8 @@ __device__ __forceinline__ void turned8(const T* head, int e0, int half, const f
 }
 
 // Where a block's rows lie: number of the token's vector of head 0 (-1: no token, or a page that is not),
-// and its place. Whole first warp; then for all.
+// and its place. Whole first warp; then for all. Meanwhile the other warps of the grid's first block look at the
+// counts of all sequences: the rows only lead to those that have some.
 struct PgRows {
   int64_t vec[kPgRows];
   int place[kPgRows];
@@ -76,6 +77,8 @@ __device__ __forceinline__ void pg_rows(const Paged& p, int64_t row0, int n, PgR
       s.vec[lane] = page >= 0 ? paged_vec(p, page, place, 0) : -1;
       s.place[lane] = place;
     }
+  } else if (blockIdx.x == 0 && blockIdx.y == 0) {
+    for (int b = threadIdx.x - 32; b < p.B; b += kPgThreads - 32) paged_seq(p, b, err);
   }
   __syncthreads();
 }

@@ -643,3 +643,48 @@ def test_attention_loose_bound_of_new_tokens(A, heads, store, seqs):
         check_attention(A, w, q, out)
         want = out if want is None else want
         assert torch.equal(out, want), bound
+
+
+@pytest.mark.parametrize("idle", [0, 400])
+@pytest.mark.parametrize("call", ["append", "read", "attention"])
+def test_bad_counts_of_any_sequence_are_reported(A, call, idle):
+    """Each count that breaks the header's rules is reported, also one of a sequence without rows, and the rows of
+    the others are answered."""
+    shape = shape_of(4, 2, 64, "bf16", rotary=0)
+    w = World(A, shape, "same", 16, [(2, 30), (0, 20), (2, 40)] + [(0, 7)] * idle + [(1, 3)], seed=20)
+    qkv = torch.randn(w.n_rows, shape.qkv_dim).to(torch.bfloat16).cuda()
+    q = queries(w)
+    ws = A.workspace(A.adadsf_paged_attention_workspace_size(w.cfg, w.cache, w.batch))
+
+    def run():
+        out = [torch.full((w.n_rows, n), 9.0, dtype=torch.bfloat16, device="cuda") for n in (128, 128, 256)]
+        if call == "append":
+            A.adadsf_paged_append(w.cfg, w.cache, w.batch, qkv, None, None, None, ws=ws)
+        elif call == "read":
+            A.adadsf_paged_read(w.cfg, w.cache, w.batch, *out[:2], ws=ws)
+        else:
+            A.adadsf_paged_attention(w.cfg, w.cache, w.batch, q, out[2], ws=ws)
+        return A.adadsf_sync_check(ws), out
+
+    status, good = run()
+    assert status == A.OK
+    room = w.table.shape[1] * 16
+    last = len(w.seqs) - 1
+    for name, at, wrong in (("lens", 1, -1), ("lens", 1, room + 1), ("lens", 1, 2 ** 31 - 1), ("lens", last - (idle > 0), -5),
+                            ("starts", 0, -1), ("starts", last + 1, w.n_rows + 1), ("starts", 1, 2 ** 31 - 1), ("starts", 2, -2 ** 31)):
+        t = getattr(w, name)
+        keep = t.clone()
+        t[at] = wrong
+        status, out = run()
+        assert status == A.ERR_INVALID_ARG, (name, at, wrong)
+        t.copy_(keep)
+        if name == "lens" and (at == 1 or idle):                      # an idle sequence's: the rows are as they were
+            for a, b in zip(out, good):
+                assert torch.equal(a, b), (name, at, wrong)
+    w.batch = A.PagedBatch(w.starts, w.lens, w.table, w.n_rows, 1)     # more rows of a sequence than the host said
+    assert run()[0] == A.ERR_INVALID_ARG
+    w.batch = A.PagedBatch(w.starts, w.lens, w.table, w.n_rows, 2)
+    status, out = run()
+    assert status == A.OK
+    for a, b in zip(out, good):
+        assert torch.equal(a, b)
