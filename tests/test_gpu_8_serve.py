@@ -209,3 +209,67 @@ def test_kept_numbers_are_the_librarys(A):
     assert [int(O.kept_counts(r, 10)) for r in (-0.5, 2.0)] == [0, 10]
     srv.prefill([torch.from_numpy(ids[b, :10].astype(np.int64)) for b in range(4)], [-0.5, 2.0, 0.5])
     assert srv.lens.tolist() == [[0] * 4, [10] * 4, [5] * 4]
+
+
+def _slope(x, W):
+    """|gradient| of the router's score at rows x, times their rms."""
+    h = x @ W["router_w1"].T + W["router_b1"]
+    s = 1 / (1 + np.exp(-h))
+    g = (W["router_w2"] * s * (1 + h * (1 - s))) @ W["router_w1"]
+    return np.linalg.norm(g, axis=-1) * np.sqrt((x * x).mean(-1))
+
+
+@pytest.mark.parametrize("shape", [QWEN_SMALL, NEOX_SMALL, NEOX_F32], ids=["qwen", "neox", "neox-f32"])
+def test_decisions_with_an_8_bit_cache(A, shape):
+    """Keep decisions over an 8-bit cache, wherever the score is clear of the threshold. The first layer's scores are of
+    embeddings, which no cache changes: 1e-3, as with a cache in the model's type. A later layer's inputs are off by about 2^-7 of
+    their rms in bf16, 2^-6 with 8 bits; six standard deviations of that along the router's gradient, for the score and for the
+    threshold, come on top. At least half of a layer's decisions have to be clear."""
+    srv, W, E = make(A, shape, "i8", 16)
+    ids, prompts = prompts_of(shape)
+    p = O.params_of(shape)
+    kept, states = [], []
+    srv.prefill(prompts, RATIOS, kept)
+    for b, n in enumerate(LENS):
+        force = [k[b].cpu().numpy()[None] for k in kept]
+        states.append(O.sparse_prefill(ids[b:b + 1, :n], E, W, p, [f.shape[1] for f in force], idx_force=force)[1])
+    clear, all_of = np.zeros(2, dtype=int), np.zeros(2, dtype=int)
+    for step in range(18):
+        tok = np.array([ids[b, n + step] for b, n in enumerate(LENS)])
+        flags = torch.empty(shape.n_layers, len(LENS), dtype=torch.bool, device="cuda")
+        srv.step(torch.from_numpy(tok.astype(np.int32)).cuda(), flags)
+        flags = flags.cpu().numpy()
+        for b in range(len(LENS)):
+            thr = [states[b]["thr"][l][0] for l in range(2)]
+            _, own, score = O.decode_step(tok[b:b + 1], E, W, p, states[b], kept_force=flags[:, b:b + 1])
+            for l in range(2):
+                if not np.isfinite(thr[l]):
+                    assert not flags[l, b]
+                    continue
+                margin = 1e-3 + (12 * 2.0 ** -6 * _slope(np.array(states[b]["rows"][l][0]), W[l]).max() if l else 0.0)
+                all_of[l] += 1
+                if abs(score[l, 0] - thr[l]) > margin:
+                    clear[l] += 1
+                    assert flags[l, b] == own[l, 0], (step, b, l)
+    srv.check()
+    assert (2 * clear >= all_of).all() and (all_of > 0).all(), (clear, all_of)
+
+
+def test_greedy_tokens_that_are_compared(A):
+    """Greedy generation against an argmax of the logits in 32 bits, where the two largest are further apart than bf16's
+    rounding of both: that has to be so for half of the tokens at least."""
+    shape = NEOX_SMALL
+    ids, prompts = prompts_of(shape)
+    srv, other = make(A, shape, "same", 16)[0], make(A, shape, "same", 64)[0]
+    n = 12
+    tokens, _ = srv.generate(prompts, RATIOS, n, torch.zeros(n, len(LENS), device="cuda"), temperature=torch.zeros(len(LENS), device="cuda"))
+    hidden, compared = other.prefill(prompts, RATIOS), 0
+    for i in range(n):
+        best = (hidden.float() @ other.head.float().T).topk(2, -1)
+        sure = (best.values[:, 0] - best.values[:, 1]) > 2.0 ** -6 * best.values[:, 0].abs()
+        assert (tokens[i] == best.indices[:, 0])[sure].all()
+        compared += int(sure.sum())
+        if i + 1 < n:
+            hidden = other.step(tokens[i])
+    other.check()
+    assert 2 * compared >= n * len(LENS), compared
