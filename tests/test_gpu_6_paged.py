@@ -688,3 +688,53 @@ def test_bad_counts_of_any_sequence_are_reported(A, call, idle):
     assert status == A.OK
     for a, b in zip(out, good):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("new", [20, 60, 130])
+@pytest.mark.parametrize("heads", [(28, 4, 128, "bf16"), (8, 8, 64, "bf16"), (8, 2, 128, "bf16")], ids=str)
+def test_attention_infinities_under_a_wide_table(A, heads, new, store):
+    """As the test of infinities in later tokens, with tables of 2^20 tokens a sequence: few rows over what could be
+    that many keys are taken as chunks, so the chunk kernel's own way with such values is what runs at these heads."""
+    w = World(A, shape_of(*heads), store, 32, [(new, 300), (new, new), (new, 150), (0, 40)], seed=new)
+    wide = torch.full((4, 2 ** 20 // 32), -1, dtype=torch.int32, device="cuda")
+    wide[:, :w.table.shape[1]] = w.table
+    w.table = wide
+    w.batch = A.PagedBatch(w.starts, w.lens, w.table, w.n_rows, new)
+    clean = [[x.clone() for x in t] for t in (w.K, w.V)]
+    _spoil(w, ("v", "inf"), 0, 299, 5)
+    _spoil(w, ("v", "nan"), 1, new - 1, 63)
+    _spoil(w, ("v", "-inf"), 0, 298, 17)
+    _spoil(w, ("v", "inf"), 1, new // 2, 0)
+    _spoil(w, ("k", "nan"), 2, 150 - new // 3, 9)
+    q = queries(w, scale=0.5)
+    out = attend(A, w, q).double().reshape(w.n_rows, w.shape.n_heads, w.shape.head_dim)
+    bad = [w.K, w.V]
+    w.K, w.V = clean
+    ref, bound = (t.reshape(out.shape) for t in attend64(w, q))
+    G, r = w.shape.n_heads // w.shape.n_kv_heads, 0
+    for b, (n, l) in enumerate(w.seqs):
+        for i in range(n):
+            seen = l - n + i + 1
+            mine = slice(G, 2 * G)
+            want = torch.ones(w.shape.n_heads, w.shape.head_dim, dtype=torch.bool, device="cuda")
+            if not torch.isfinite(bad[0][b][:seen, 1]).all():
+                want[mine] = False
+            else:
+                want[mine] = torch.isfinite(bad[1][b][:seen, 1]).all(0)
+            assert torch.equal(torch.isfinite(out[r]), want), (b, i)
+            assert ((out[r] - ref[r]).abs()[want] <= bound[r][want]).all(), (b, i)
+            r += 1
+
+
+@pytest.mark.parametrize("store", ["same", "i8"])
+@pytest.mark.parametrize("heads", [(28, 4, 128, "bf16"), (12, 12, 64, "bf16"), (12, 2, 128, "bf16"), (16, 1, 64, "bf16")], ids=str)
+def test_attention_under_a_wide_table(A, heads, store):
+    """Few new tokens, some of them on nothing, under a table far wider than the longest sequence."""
+    w = World(A, shape_of(*heads), store, 16, [(17, 300), (33, 33), (5, 1000), (0, 9), (1, 1), (20, 19), (19, 129), (3, 0)], seed=21)
+    wide = torch.full((8, 2 ** 20 // 16), 2 ** 30, dtype=torch.int32, device="cuda")
+    wide[:, :w.table.shape[1]] = w.table
+    w.table = wide
+    w.batch = A.PagedBatch(w.starts, w.lens, w.table, w.n_rows, 33)
+    q = queries(w)
+    check_attention(A, w, q, attend(A, w, q))
