@@ -86,21 +86,6 @@ struct AttnCfg {
   static_assert(TO + 2 * HD <= 512, "TMEM columns");
 };
 
-// 2^x on the SFU (ex2.approx.ftz.f32: relative error ~2^-22, flushes
-// denormal results; P is rounded to bf16 afterwards).
-__device__ __forceinline__ float ex2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// max(a, b, c) in one instruction.
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-
 struct AttnDev {
   int K;                 // kept tokens per sequence
   int pair;              // 1: two query blocks per work item, 0: one

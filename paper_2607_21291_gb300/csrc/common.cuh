@@ -22,6 +22,19 @@ __device__ __forceinline__ void set_device_error(int* err, int bit) {
   if (err) atomicOr(err, bit);
 }
 
+// 2^x on the SFU (ex2.approx.ftz.f32: relative error about 2^-22, denormal results flushed).
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// max(a, b, c) in one instruction.
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // ---------------------------------------------------------------- storage types
 template <typename T> struct Elem;
 template <> struct Elem<float> {

@@ -63,11 +63,6 @@ __host__ __device__ __forceinline__ int kl_owner(int64_t tiles, int G, int64_t t
 struct KlSums {
   float ms, zs, md, zd, x;
 };
-__device__ __forceinline__ float kl_ex2(float x) {   // ex2.approx: relative error ~2^-22, averaged out over the classes
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float2 f2(uint32_t a, uint32_t b) {
   return make_float2(__uint_as_float(a), __uint_as_float(b));
 }
@@ -85,7 +80,7 @@ __device__ __forceinline__ void kl_fold(KlSums& s, const uint32_t* us, const uin
   if (ns > s.ms || nd > s.md) {
     const float ms = fmaxf(s.ms, ns), md = fmaxf(s.md, nd);
     // a maximum that stays where it is (at -inf too) scales by 1; without one so far the sums are 0
-    const float fs = ms == s.ms ? 1.f : kl_ex2((s.ms - ms) * kLog2e), fd = md == s.md ? 1.f : kl_ex2((s.md - md) * kLog2e);
+    const float fs = ms == s.ms ? 1.f : ex2_approx((s.ms - ms) * kLog2e), fd = md == s.md ? 1.f : ex2_approx((s.md - md) * kLog2e);
     s.zs *= fs;
     s.zd *= fd;
     s.x *= fd;
@@ -101,8 +96,8 @@ __device__ __forceinline__ void kl_fold(KlSums& s, const uint32_t* us, const uin
   for (int i = 0; i < 16; ++i) {
     const float2 a = f2(us[2 * i], us[2 * i + 1]), b = f2(ud[2 * i], ud[2 * i + 1]);
     const float2 ta = __fmul2_rn(__fadd2_rn(a, ms2), l2), tb = __fmul2_rn(__fadd2_rn(b, md2), l2);
-    const float2 e = make_float2(kl_ex2(tb.x), kl_ex2(tb.y));
-    zs[i & 1] = __fadd2_rn(zs[i & 1], make_float2(kl_ex2(ta.x), kl_ex2(ta.y)));
+    const float2 e = make_float2(ex2_approx(tb.x), ex2_approx(tb.y));
+    zs[i & 1] = __fadd2_rn(zs[i & 1], make_float2(ex2_approx(ta.x), ex2_approx(ta.y)));
     zd[i & 1] = __fadd2_rn(zd[i & 1], e);
     x[i & 1] = __ffma2_rn(e, __ffma2_rn(a, minus, b), x[i & 1]);
   }

@@ -183,12 +183,6 @@ __device__ __forceinline__ bool paged_wait(uint32_t bar, uint32_t parity, volati
   }
 }
 
-// 2^x on the SFU (relative error about 2^-22, denormal results flushed).
-__device__ __forceinline__ float paged_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // Two 8-bit numbers (the low bytes of t's halves) as bf16, exactly: with b a number's low seven
 // bits and s its top one, (128 + b) - (s ? 256 : 128).
 __device__ __forceinline__ uint32_t bf16_of_i8(uint32_t t) {

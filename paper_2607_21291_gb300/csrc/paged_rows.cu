@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
           const float mn = fmaxf(m_r[r], mx);
           base[r] = mn == -INFINITY ? 0.f : mn;
-          corr[r] = paged_ex2(m_r[r] - base[r]);
+          corr[r] = ex2_approx(m_r[r] - base[r]);
           m_r[r] = mn;
         }
         uint32_t pa[2 * KT], pl[2 * KT];   // weights: bf16, and what that leaves
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
           float sum = 0.f;
 #pragma unroll
           for (int nt = 0; nt < KT; ++nt) {
-            float p0 = paged_ex2(sc[nt][2 * r] - base[r]), p1 = paged_ex2(sc[nt][2 * r + 1] - base[r]);
+            float p0 = ex2_approx(sc[nt][2 * r] - base[r]), p1 = ex2_approx(sc[nt][2 * r + 1] - base[r]);
             sum += p0 + p1;
             if (I8) {
               p0 *= vsc[nt].x;
@@ -460,8 +460,8 @@ __global__ void __launch_bounds__(kPrThreads, kPrPerSm)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float mn = fmaxf(m_r[r], ml[r].x), b = mn == -INFINITY ? 0.f : mn;
-        mine[r] = paged_ex2(m_r[r] - b);
-        theirs[r] = paged_ex2(ml[r].x - b);
+        mine[r] = ex2_approx(m_r[r] - b);
+        theirs[r] = ex2_approx(ml[r].x - b);
         l_r[r] = l_r[r] * mine[r] + ml[r].y * theirs[r];
         m_r[r] = mn;
       }

@@ -112,11 +112,6 @@ __device__ __forceinline__ PtWork pt_work(const PagedItem<PtCut>& it, int64_t ua
   return w;
 }
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* tmap, int c0, int c1, int c2, int c3, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
@@ -535,8 +530,8 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
               const float2 u1 = __fmul2_rn(make_float2(y.z, y.w), make_float2(f.z, f.w));
               y = make_float4(u0.x, u0.y, u1.x, u1.y);
             }
-            mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], y.x, y.y);
-            mx[((k >> 1) + 1) & 3] = max3(mx[((k >> 1) + 1) & 3], y.z, y.w);
+            mx[(k >> 1) & 3] = fmax3(mx[(k >> 1) & 3], y.x, y.y);
+            mx[((k >> 1) + 1) & 3] = fmax3(mx[((k >> 1) + 1) & 3], y.z, y.w);
             if (I8) {
               s[k] = __float_as_uint(y.x); s[k + 1] = __float_as_uint(y.y);
               s[k + 2] = __float_as_uint(y.z); s[k + 3] = __float_as_uint(y.w);
@@ -550,7 +545,7 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
         // O is stable: its last product was issued before S_t(j), which is complete
         const bool grow = top > m + kPtRescale;          // true for the first finite maximum
         if (__any_sync(0xffffffffu, grow && m > -INFINITY)) {
-          const float alpha = grow ? (m > -INFINITY ? paged_ex2(m - top) : 1.f) : 1.f;
+          const float alpha = grow ? (m > -INFINITY ? ex2_approx(m - top) : 1.f) : 1.f;
           l *= alpha;
 #pragma unroll 1
           for (int c = 0; c < HD / 32; ++c) {
@@ -574,7 +569,7 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
           for (int k = 0; k < 16; ++k) {
             float2 y = make_float2(__uint_as_float(z[2 * k]), __uint_as_float(z[2 * k + 1]));
             y = I8 ? __fadd2_rn(y, neg2) : __ffma2_rn(y, scale2, neg2);
-            e[k] = make_float2(paged_ex2(y.x), paged_ex2(y.y));
+            e[k] = make_float2(ex2_approx(y.x), ex2_approx(y.y));
             sum[k & 1] = __fadd2_rn(sum[k & 1], e[k]);
             if (I8) {
               const float4 f = vs4[8 * c + k / 2];
@@ -685,7 +680,7 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
           const float base = mm == -INFINITY ? 0.f : mm;
           for (int c = from; c <= to; c += step) {
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_of(c) + kPtRows * HD) + r);
-            ll += ml.y * paged_ex2(ml.x - base);
+            ll += ml.y * ex2_approx(ml.x - base);
           }
           const float by = out ? 1.f / ll : 1.f;
           if (live) {
@@ -697,7 +692,7 @@ __global__ void __launch_bounds__(PtCfg<HD, I8>::THREADS, 1)
 #pragma unroll(I8 ? 1 : 2)
               for (int c = from; c <= to; c += step) {
                 const float* po = part_of(c);
-                const float f = paged_ex2(__ldcg(reinterpret_cast<const float2*>(po + kPtRows * HD) + r).x - base) * by;
+                const float f = ex2_approx(__ldcg(reinterpret_cast<const float2*>(po + kPtRows * HD) + r).x - base) * by;
                 float4 x[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4*>(po) + (e / 4 + k) * kPtRows + r);

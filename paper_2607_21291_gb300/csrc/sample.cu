@@ -90,7 +90,7 @@ struct SampleShared {
   u64 total[2];                        // this CTA's total
   u64 bins[2][kSmBins];                // sums over the cluster of this CTA's share of the bins, or the gathered keys' indices
   u64 warp[kSmWarps];                  // block scan
-  u64 found_before, found_in, found_all, found_target;
+  u64 found_before, found_in, found_target;
   uint32_t found_bin;
   uint32_t most, least;                // this CTA's largest key, the smallest of its warps' largest ones; read by the cluster
   uint32_t index;                      // written by the CTA that finds it
@@ -183,10 +183,7 @@ __device__ __forceinline__ void find_bin(SampleShared& s, int q, u64 base, u64 t
   u64 all;
   const u64 run = base + block_before(v, s, &all);
   if (frac < 1.0) {
-    if (tid == 0) {
-      s.found_all = all;
-      s.found_target = whole_target(fmax(frac * (double)all, 1.0));
-    }
+    if (tid == 0) s.found_target = whole_target(fmax(frac * (double)all, 1.0));
     __syncthreads();
     target = s.found_target;
   }
