@@ -150,12 +150,14 @@ def _p(t: Optional[torch.Tensor]):
 
 
 def _s(stream) -> int:
-    """The stream's handle; None is the current one (without making a Stream object of it: 2 us of a call's 10)."""
-    if stream is not None:
-        return stream.cuda_stream
-    if not torch.cuda.is_initialized():
-        return torch.cuda.current_stream().cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    """The stream's handle; None is the current one, where torch tells it without making a Stream object (2 us of
+    a call's 10), else from one."""
+    if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None and torch.cuda.is_initialized():
+            return raw(torch.cuda.current_device())
+        stream = torch.cuda.current_stream()
+    return stream.cuda_stream
 
 
 def _dev(t: torch.Tensor, name: str):

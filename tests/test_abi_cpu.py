@@ -182,3 +182,27 @@ def test_decode_argument_errors_precede_launch(A):
     assert lib.adadsf_decode_step(ctypes.byref(cfg), None, None, 2, None, None, None, n, 100, None, 0,
                                   None) == A.ERR_INVALID_ARG
     assert lib.adadsf_decode_workspace_size(ctypes.byref(cfg), 2, 100) > 0
+
+
+def test_current_stream_without_private_names(monkeypatch):
+    """Where torch has no raw handle of the current stream to give, its public stream object is asked; a stream
+    that the caller names is used as it is."""
+    import torch
+    from paper_2607_21291_gb300 import adadsf as A
+
+    class Stream:
+        cuda_stream = 77
+
+    class Other:
+        cuda_stream = 78
+
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream())
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    assert A._s(None) == 77 and A._s(Other()) == 78
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 79 + device, raising=False)
+    assert A._s(None) == 79
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: False)
+    assert A._s(None) == 77
