@@ -738,3 +738,21 @@ def test_attention_under_a_wide_table(A, heads, store):
     w.batch = A.PagedBatch(w.starts, w.lens, w.table, w.n_rows, 33)
     q = queries(w)
     check_attention(A, w, q, attend(A, w, q))
+
+
+@pytest.mark.parametrize("heads,seqs", [((28, 4, 128, "bf16"), [(4, 9000 + 40 * b) for b in range(8)]),
+                                        ((12, 2, 128, "bf16"), [(5, 20000), (1, 3), (0, 50), (3, 2), (5, 30000)]),
+                                        ((12, 12, 64, "bf16"), [(32, 12000 + b) for b in range(4)]),
+                                        ((16, 1, 64, "bf16"), [(2, 40000), (1, 1), (2, 2)])], ids=str)
+def test_attention_two_row_groups_of_8_bits(A, heads, seqs):
+    """17 to 32 packed rows a sequence over long 8-bit caches: two groups of rows a head, cut in pieces; the same under a
+    table far wider than the sequences."""
+    w = World(A, shape_of(*heads), "i8", 64, seqs, seed=22)
+    q = queries(w)
+    got = attend(A, w, q)
+    check_attention(A, w, q, got)
+    wide = torch.full((len(seqs), 2 ** 17), -1, dtype=torch.int32, device="cuda")
+    wide[:, :w.table.shape[1]] = w.table
+    w.table = wide
+    w.batch = A.PagedBatch(w.starts, w.lens, w.table, w.n_rows, max(n for n, _ in seqs))
+    assert torch.equal(attend(A, w, q), got)
