@@ -537,8 +537,12 @@ adadsf_status adadsf_paged_read(const adadsf_model_cfg *cfg, const adadsf_paged_
  * qkv matrix will do); out_dev [n_rows, q]. cfg->dtype. A row without any
  * visible token gets zeros. The new tokens' keys and values must be in the
  * pages (adadsf_paged_append).
+ * Sums and softmax statistics are fp32. bf16: weights enter the products with values as
+ * bf16 and the bf16 of what that leaves, but in chunks of tokens over more than 2048 keys
+ * as one bf16.
  * ws: adadsf_paged_attention_workspace_size bytes, zero-filled before first
- * use; it may serve batches of any smaller workspace size.
+ * use; it may serve batches of any smaller workspace size (the size goes by cfg's type
+ * and head size alone, up to 43 MB, so one workspace serves all batches of a model).
  * ---------------------------------------------------------------------- */
 size_t adadsf_paged_attention_workspace_size(const adadsf_model_cfg *cfg, const adadsf_paged_cache *cache,
                                              const adadsf_paged_batch *batch);

@@ -14,6 +14,7 @@
 // Measured, 8 heads of 64: 4 x 600 tokens on 1000 cached 203 us, 31 TFLOP/s of the 74 that fp32 can (schedulers 65% busy,
 // three quarters of that multiply-adds; two multiply-adds an instruction took 217 us, for the copies that make the
 // weights pairs); 3 x 129 on 511 35 us; 8 single tokens on 4000 36 us, 3.6 TB/s.
+// From 8-bit caches 213, 36 and 38 us.
 #include <math.h>
 
 #include <algorithm>

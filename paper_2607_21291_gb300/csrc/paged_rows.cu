@@ -24,8 +24,8 @@
 // each: one single token on 131071 cached has 77 pieces a head to join (95 us with one warp).
 //
 // Measured, 28 query heads on 4 of 128: 8 single tokens on 32767 cached 89 us, 6.0 TB/s (89% of
-// a plain copy); 8-bit numbers 95 us, 2.9 TB/s, bound by the instructions that make them
-// bf16; 16 on up to 4096 in 8 bits 22 us; one on 131071 69 us; 256 on 300 43 us.
+// a plain copy); 8-bit numbers 94 us, 2.9 TB/s, bound by the instructions that make them
+// bf16; 16 on up to 4096 in 8 bits 22 us; one on 131071 70 us (8 bits 73); 256 on 300 44 us (49).
 #include <math.h>
 
 #include <algorithm>

@@ -17,7 +17,7 @@
 // Few rows are bound by the latency of those rounds (two to eight, 2 us each over the cluster), many
 // rows by the instructions of the passes over the keys, half of them comparisons and logic on a pipe of half
 // rate. Measured: one row of 50304 bf16 5 us greedy, 11 with top-k 50, 15 with top-p 0.9; 16 rows of 152064 fp32 of
-// mixed settings 31 us; 256 of 151936 bf16 173 us (54 greedy, 82 with top-k 50, 272 with top-p 0.9).
+// mixed settings 31 us; 256 of 151936 bf16 173 us (54 greedy, 83 with top-k 50, 277 with top-p 0.9).
 #include <math.h>
 
 #include <type_traits>
