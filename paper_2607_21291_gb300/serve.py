@@ -132,11 +132,14 @@ class Server:
         T = np.array([len(p) for p in prompts])
         if len(T) != self.B or T.min() < 1 or T.max() > self.max_len:
             raise ValueError(f"need {self.B} prompts of 1 to {self.max_len} tokens")
+        ratios = np.asarray(ratios, dtype=np.float64)
+        if ratios.shape != (len(self.layers),) or not np.isfinite(ratios).all():
+            raise ValueError(f"need a finite ratio for each of {len(self.layers)} layers")
         at = np.concatenate([[0], np.cumsum(T)])
         ids = torch.cat([torch.as_tensor(p) for p in prompts]).to(self.device)
         pos = torch.cat([torch.arange(n, dtype=torch.int32, device=self.device) for n in T])
         # as the retention allocation counts them (adadsf_alloc_ratios): 0.29 x 100 falls short of 29 by a rounding
-        K = np.clip(np.floor(np.multiply.outer(np.asarray(ratios, dtype=np.float64), T) + 1e-9), 0, T).astype(np.int64)
+        K = np.clip(np.floor(np.multiply.outer(ratios, T) + 1e-9), 0, T).astype(np.int64)
         self._reserve(K)
         self.known, self.steps, self.grows, self.length = K, 0, K > 0, T.astype(np.int64)
         self.live.fill_(1)

@@ -273,3 +273,17 @@ def test_greedy_tokens_that_are_compared(A):
             hidden = other.step(tokens[i])
     other.check()
     assert 2 * compared >= n * len(LENS), compared
+
+
+def test_ratios_are_checked(A):
+    """A ratio that is no number, or not one for each layer, is refused and changes nothing."""
+    srv, _, _ = make(A, NEOX_SMALL, "same", 16)
+    _, prompts = prompts_of(NEOX_SMALL)
+    srv.prefill(prompts, RATIOS)
+    lens, held = srv.lens.clone(), srv.pool.held.copy()
+    for ratios in ([1.0, 0.5], [1.0] * 4, [1.0, float("nan"), 0.5], [1.0, float("inf"), 0.5], []):
+        with pytest.raises(ValueError, match="ratio"):
+            srv.prefill(prompts, ratios)
+    assert torch.equal(srv.lens, lens) and (srv.pool.held == held).all()
+    srv.step(torch.zeros(len(LENS), dtype=torch.int32, device="cuda"))
+    srv.check()
