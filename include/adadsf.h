@@ -280,6 +280,102 @@ adadsf_status adadsf_router_backward(const adadsf_model_cfg *cfg, const adadsf_l
                                      void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Losses at the LM head, in pieces of the classes: no call stores the logits,
+ * its scratch grows with n_rows n_classes / 16 bytes and a piece's share of
+ * them. h_dev [n_rows, d] and w_head_dev [n_classes, d] in `dtype`; with
+ * l = h w_head^T (fp32):
+ *   adadsf_head_loss: cross entropy of a target a row, loss = lse - l[target],
+ *     lse = log sum_c e^{l_c} (the L_causal of Table 4). target_dev [n_rows]
+ *     int32; below 0: none (a prompt's token, padding).
+ *   adadsf_distill_loss: a teacher's top logits (Eq. 10's KL where only those
+ *     are stored). top_idx_dev [n_rows, top_k] int32 and top_logit_dev fp32: a
+ *     slot with an index below 0 or a logit of -infinity is not in use, the
+ *     same class twice counts twice. With p the softmax of the slots' logits /
+ *     temperature and q that of all of the row's l / temperature,
+ *     loss = temperature^2 sum_j p_j (log p_j - log q_{c_j}), and
+ *     lse = log sum_c e^{l_c / temperature}.
+ * Rows without a target have loss and lse 0 and no gradient; what their h
+ * holds, infinities and NaN among it, reaches nothing. A class >= n_classes
+ * sets the device error word (adadsf_sync_check: ADADSF_ERR_INVALID_ARG) and
+ * counts as none.
+ * loss_dev, lse_dev: fp32 [n_rows] (loss_dev may be NULL without acc_dev);
+ * acc_dev (NULL or 2 doubles): acc[0] += sum of the losses, acc[1] += rows
+ * that have one.
+ * Backward: lse_dev as the forward call left it, grad_loss_dev fp32 [n_rows]
+ * the gradient of each row's loss (NULL: 1). grad_h_dev [n_rows, d] and
+ * grad_w_dev [n_classes, d] in `dtype` (either may be NULL: not computed);
+ * accumulate_w 1 adds to what grad_w_dev holds, before the one rounding.
+ * Logits, exponentials and sums are fp32; the bf16 path rounds the logits'
+ * gradients to bf16 for the tensor cores. Every sum has one order: results
+ * repeat bit for bit.
+ * d % 8 == 0 (bf16) or d % 4 == 0 (fp32); any n_classes up to 2^24; n_rows up
+ * to 2^22; top_k up to 1024. ws: adadsf_head_workspace_size bytes (top_k 1 for
+ * adadsf_head_loss), for either direction.
+ * ---------------------------------------------------------------------- */
+size_t adadsf_head_workspace_size(int64_t n_rows, int d, int n_classes, int dtype, int top_k);
+adadsf_status adadsf_head_loss(const void *h_dev, const void *w_head_dev, const int32_t *target_dev,
+                               int64_t n_rows, int d, int n_classes, int dtype, float *loss_dev,
+                               float *lse_dev, double *acc_dev, void *ws, size_t ws_bytes, void *stream);
+adadsf_status adadsf_head_loss_backward(const void *h_dev, const void *w_head_dev, const int32_t *target_dev,
+                                        int64_t n_rows, int d, int n_classes, int dtype, const float *lse_dev,
+                                        const float *grad_loss_dev, void *grad_h_dev, void *grad_w_dev,
+                                        int accumulate_w, void *ws, size_t ws_bytes, void *stream);
+adadsf_status adadsf_distill_loss(const void *h_dev, const void *w_head_dev, const int32_t *top_idx_dev,
+                                  const float *top_logit_dev, int top_k, float temperature, int64_t n_rows,
+                                  int d, int n_classes, int dtype, float *loss_dev, float *lse_dev,
+                                  double *acc_dev, void *ws, size_t ws_bytes, void *stream);
+adadsf_status adadsf_distill_loss_backward(const void *h_dev, const void *w_head_dev, const int32_t *top_idx_dev,
+                                           const float *top_logit_dev, int top_k, float temperature,
+                                           int64_t n_rows, int d, int n_classes, int dtype, const float *lse_dev,
+                                           const float *grad_loss_dev, void *grad_h_dev, void *grad_w_dev,
+                                           int accumulate_w, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * LayerNorm (is_rms 0) or RMSNorm of rows, with the statistics a backward
+ * pass needs: y = (x - mean) rstd w + b, rstd = 1 / sqrt(var + eps); RMSNorm:
+ * y = x rstd w, rstd = 1 / sqrt(mean x^2 + eps) (b_dev and mean_dev NULL).
+ * x_dev, y_dev [n_rows, d], w_dev, b_dev [d] in `dtype`; mean_dev, rstd_dev
+ * fp32 [n_rows]. y_dev may be x_dev.
+ * Backward, with xhat = (x - mean) rstd and a = grad_y w:
+ *   grad_x = rstd (a - mean(a) - xhat mean(a xhat)) + add
+ * (RMSNorm: without mean(a)); add_dev (NULL or [n_rows, d]): the gradient that
+ * goes around the norm. grad_x_dev may be grad_y_dev or add_dev.
+ * grad_w_dev = sum grad_y xhat, grad_b_dev = sum grad_y over the rows: fp32
+ * [d], either may be NULL; accumulate 1 adds to what they hold. Sums in one
+ * order. d as for the losses above, up to 8192.
+ * ws: adadsf_norm_backward_workspace_size bytes.
+ * ---------------------------------------------------------------------- */
+adadsf_status adadsf_norm_forward(const void *x_dev, const void *w_dev, const void *b_dev, int64_t n_rows,
+                                  int d, int dtype, float eps, int is_rms, void *y_dev, float *mean_dev,
+                                  float *rstd_dev, void *stream);
+size_t adadsf_norm_backward_workspace_size(int64_t n_rows, int d);
+adadsf_status adadsf_norm_backward(const void *grad_y_dev, const void *x_dev, const void *w_dev,
+                                   const float *mean_dev, const float *rstd_dev, const void *add_dev,
+                                   int64_t n_rows, int d, int dtype, int is_rms, void *grad_x_dev,
+                                   float *grad_w_dev, float *grad_b_dev, int accumulate, void *ws,
+                                   size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Embedding rows with a scale, out = scale table[id], and the gradient of the
+ * table, grad_table[v] = scale sum of grad_out_i over ids_i = v, in fp32 and
+ * one order (ascending i), rounded once. ids_dev [n] int32: below 0 is padding
+ * (a row of zeros, no gradient), >= vocab too but sets the device error word.
+ * table_dev, grad_table_dev [vocab, d], out_dev, grad_out_dev [n, d] in
+ * `dtype`. accumulate 0 writes every row of grad_table_dev, 1 adds to the rows
+ * of ids that came and leaves the others (a head that shares the table has its
+ * gradient there). d as for the losses above; n up to 2^30, vocab up to 2^27.
+ * ws: 256 bytes (the device error word) forward,
+ * adadsf_embed_backward_workspace_size bytes backward.
+ * ---------------------------------------------------------------------- */
+adadsf_status adadsf_embed_forward(const int32_t *ids_dev, int64_t n, const void *table_dev, int vocab, int d,
+                                   int dtype, float scale, void *out_dev, void *ws, size_t ws_bytes,
+                                   void *stream);
+size_t adadsf_embed_backward_workspace_size(int64_t n, int vocab, int d);
+adadsf_status adadsf_embed_backward(const int32_t *ids_dev, const void *grad_out_dev, int64_t n, int vocab,
+                                    int d, int dtype, float scale, void *grad_table_dev, int accumulate,
+                                    void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Sec. 4.1 (the normalized FLOPs of Tables 1-2): FLOPs of the depth-sparse
  * forward over those of the dense model, per sequence of T tokens. Host
  * only, pure. Counted per layer l: the router on all T tokens when
@@ -613,6 +709,11 @@ typedef enum {
   ADADSF_KERNEL_PAGED_READ,    /* paged cache read back */
   ADADSF_KERNEL_PAGED_ATTENTION,
   ADADSF_KERNEL_SAMPLE,        /* next tokens from logits */
+  ADADSF_KERNEL_HEAD_LOSS,     /* loss at the LM head: all launches of a call */
+  ADADSF_KERNEL_HEAD_GRAD,     /* its gradients: all launches of a call */
+  ADADSF_KERNEL_NORM,          /* norm of rows, statistics kept */
+  ADADSF_KERNEL_NORM_GRAD,
+  ADADSF_KERNEL_EMBED_GRAD,
   ADADSF_KERNEL_COUNT
 } adadsf_kernel_kind;
 

@@ -89,6 +89,7 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, sz, f64, u32 = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t,
                                       ctypes.c_double, ctypes.c_uint)
+        f32 = ctypes.c_float
         ppc, ppb = ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedBatch)
         pcfg, plw, pmw = ctypes.POINTER(ModelCfg), ctypes.POINTER(LayerWeights), ctypes.POINTER(ModelWeights)
         sig = {
@@ -126,6 +127,17 @@ def lib() -> ctypes.CDLL:
             "adadsf_paged_attention_workspace_size": (sz, [pcfg, ppc, ppb]),
             "adadsf_paged_attention": (i32, [pcfg, ppc, ppb, vp, i64, vp, vp, sz, vp]),
             "adadsf_sample": (i32, [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]),
+            "adadsf_head_workspace_size": (sz, [i64, i32, i32, i32, i32]),
+            "adadsf_head_loss": (i32, [vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp, sz, vp]),
+            "adadsf_head_loss_backward": (i32, [vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp, i32, vp, sz, vp]),
+            "adadsf_distill_loss": (i32, [vp, vp, vp, vp, i32, f32, i64, i32, i32, i32, vp, vp, vp, vp, sz, vp]),
+            "adadsf_distill_loss_backward": (i32, [vp, vp, vp, vp, i32, f32, i64, i32, i32, i32, vp, vp, vp, vp, i32, vp, sz, vp]),
+            "adadsf_norm_forward": (i32, [vp, vp, vp, i64, i32, i32, f32, i32, vp, vp, vp, vp]),
+            "adadsf_norm_backward_workspace_size": (sz, [i64, i32]),
+            "adadsf_norm_backward": (i32, [vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, i32, vp, sz, vp]),
+            "adadsf_embed_forward": (i32, [vp, i64, vp, i32, i32, i32, f32, vp, vp, sz, vp]),
+            "adadsf_embed_backward_workspace_size": (sz, [i64, i32, i32]),
+            "adadsf_embed_backward": (i32, [vp, vp, i64, i32, i32, i32, f32, vp, i32, vp, sz, vp]),
             "adadsf_sync_check": (i32, [vp, sz, vp]),
             "adadsf_selftest_bounded_wait": (i32, [vp, sz, i32, vp]),
             "adadsf_profile_begin": (i32, [i32]),
@@ -642,6 +654,207 @@ def adadsf_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor,
                                ptr(temperature, "temperature"), ptr(top_k, "top_k", torch.int32), ptr(top_p, "top_p"),
                                ptr(min_p, "min_p"), ptr(u, "u"), ptr(token, "token", torch.int32), ptr(logprob, "logprob"),
                                _s(stream)))
+
+
+# --------------------------------------------------------------------- training at the two ends
+def _matrix(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None, dtype=None, like=None):
+    """A contiguous matrix on the current device; rows, cols, type and device as asked."""
+    _dev(t, name)
+    if t.dim() != 2 or t.dtype not in DTYPE_CODE or (rows is not None and t.shape[0] != rows) or \
+            (cols is not None and t.shape[1] != cols) or (dtype is not None and t.dtype is not dtype):
+        want = " x ".join("any" if v is None else str(v) for v in (rows, cols))
+        raise ValueError(f"{name} must be a matrix ({want}) of {dtype or 'float32 or bfloat16'}, not {tuple(t.shape)} of {t.dtype}")
+    _here(t, name)
+
+
+def _here(t: torch.Tensor, name: str):
+    """The library launches on the current device: a tensor of another one is refused."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype: torch.dtype):
+    if t is None:
+        return None
+    _dev(t, name)
+    if t.dtype is not dtype or t.numel() != n:
+        raise ValueError(f"{name} must be {n} values of {dtype}, not {t.numel()} of {t.dtype}")
+    _here(t, name)
+    return t.data_ptr()
+
+
+def _ws(ws: Optional[torch.Tensor], size, device) -> torch.Tensor:
+    if ws is None:
+        return workspace(size(), device)
+    _dev(ws, "ws")
+    if ws.dtype is not torch.uint8:
+        raise ValueError("ws must be bytes (see workspace)")
+    _here(ws, "ws")
+    return ws
+
+
+def adadsf_head_workspace_size(n_rows: int, d: int, n_classes: int, dtype: torch.dtype, top_k: int = 1) -> int:
+    n = lib().adadsf_head_workspace_size(int(n_rows), int(d), int(n_classes), DTYPE_CODE[dtype], int(top_k))
+    if n == 0:
+        raise AdadsfError(ERR_INVALID_ARG, adadsf_last_error())
+    return n
+
+
+def _head(h, w_head, k, ws):
+    _matrix(w_head, "w_head")
+    n_cls, d = w_head.shape
+    _matrix(h, "h", cols=d, dtype=w_head.dtype)
+    n = h.shape[0]
+    ws = _ws(ws, lambda: adadsf_head_workspace_size(n, d, n_cls, h.dtype, k), h.device)
+    return n, d, n_cls, DTYPE_CODE[h.dtype], ws
+
+
+def _teacher(h, top_idx, top_logit):
+    _dev(top_idx, "top_idx")
+    if top_idx.dim() != 2 or top_idx.shape[0] != h.shape[0] or top_idx.shape[1] == 0:
+        raise ValueError(f"top_idx must be ({h.shape[0]}, k), not {tuple(top_idx.shape)}")
+    n = top_idx.numel()
+    return _vector(top_idx, "top_idx", n, torch.int32), _vector(top_logit, "top_logit", n, torch.float32), top_idx.shape[1]
+
+
+def _losses(n, loss, lse, acc):
+    return (_vector(loss, "loss", n, torch.float32), _vector(lse, "lse", n, torch.float32),
+            _vector(acc, "acc", 2, torch.float64))
+
+
+def _head_grads(n, d, n_cls, dtype, grad_h, grad_w):
+    if grad_h is not None:
+        _matrix(grad_h, "grad_h", n, d, dtype)
+    if grad_w is not None:
+        _matrix(grad_w, "grad_w", n_cls, d, dtype)
+    return None if grad_h is None else grad_h.data_ptr(), None if grad_w is None else grad_w.data_ptr()
+
+
+def adadsf_head_loss(h: torch.Tensor, w_head: torch.Tensor, target: torch.Tensor, loss: Optional[torch.Tensor],
+                     lse: torch.Tensor, acc: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                     stream=None):
+    """Cross entropy of each row of h (n, d) with its target (int32, below 0:
+    none) through the head w_head (classes, d), no logit stored: loss and lse
+    (fp32, n) receive the losses and logarithms that the backward call needs;
+    acc (2 doubles) += {sum of losses, rows with a target}."""
+    n, d, n_cls, dtype, ws = _head(h, w_head, 1, ws)
+    out = _losses(n, loss, lse, acc)
+    _check(lib().adadsf_head_loss(h.data_ptr(), w_head.data_ptr(), _vector(target, "target", n, torch.int32), n, d, n_cls,
+                                  dtype, *out, ws.data_ptr(), ws.numel(), _s(stream)))
+
+
+def adadsf_head_loss_backward(h: torch.Tensor, w_head: torch.Tensor, target: torch.Tensor, lse: torch.Tensor,
+                              grad_loss: Optional[torch.Tensor] = None, grad_h: Optional[torch.Tensor] = None,
+                              grad_w: Optional[torch.Tensor] = None, accumulate_w: bool = False,
+                              ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of adadsf_head_loss's losses, each weighted by grad_loss (fp32,
+    n; None: 1): grad_h like h, grad_w like w_head (either may be None;
+    accumulate_w adds to what grad_w holds)."""
+    n, d, n_cls, dtype, ws = _head(h, w_head, 1, ws)
+    grads = _head_grads(n, d, n_cls, h.dtype, grad_h, grad_w)
+    _check(lib().adadsf_head_loss_backward(h.data_ptr(), w_head.data_ptr(), _vector(target, "target", n, torch.int32), n, d,
+                                           n_cls, dtype, _vector(lse, "lse", n, torch.float32),
+                                           _vector(grad_loss, "grad_loss", n, torch.float32), *grads,
+                                           1 if accumulate_w else 0, ws.data_ptr(), ws.numel(), _s(stream)))
+
+
+def adadsf_distill_loss(h: torch.Tensor, w_head: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor,
+                        temperature: float, loss: Optional[torch.Tensor], lse: torch.Tensor,
+                        acc: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """KL of each row's softmax at a temperature from a teacher's top logits:
+    top_idx (int32, n x k; below 0: slot not in use) and top_logit (fp32).
+    Outputs as adadsf_head_loss's."""
+    idx, logit, k = _teacher(h, top_idx, top_logit)
+    n, d, n_cls, dtype, ws = _head(h, w_head, k, ws)
+    out = _losses(n, loss, lse, acc)
+    _check(lib().adadsf_distill_loss(h.data_ptr(), w_head.data_ptr(), idx, logit, k, float(temperature), n, d, n_cls, dtype,
+                                     *out, ws.data_ptr(), ws.numel(), _s(stream)))
+
+
+def adadsf_distill_loss_backward(h: torch.Tensor, w_head: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor,
+                                 lse: torch.Tensor, temperature: float, grad_loss: Optional[torch.Tensor] = None,
+                                 grad_h: Optional[torch.Tensor] = None, grad_w: Optional[torch.Tensor] = None,
+                                 accumulate_w: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of adadsf_distill_loss's losses (see adadsf_head_loss_backward)."""
+    idx, logit, k = _teacher(h, top_idx, top_logit)
+    n, d, n_cls, dtype, ws = _head(h, w_head, k, ws)
+    grads = _head_grads(n, d, n_cls, h.dtype, grad_h, grad_w)
+    _check(lib().adadsf_distill_loss_backward(h.data_ptr(), w_head.data_ptr(), idx, logit, k, float(temperature), n, d, n_cls,
+                                              dtype, _vector(lse, "lse", n, torch.float32),
+                                              _vector(grad_loss, "grad_loss", n, torch.float32), *grads,
+                                              1 if accumulate_w else 0, ws.data_ptr(), ws.numel(), _s(stream)))
+
+
+def adadsf_norm_forward(x: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor], y: torch.Tensor, eps: float,
+                        mean: Optional[torch.Tensor], rstd: torch.Tensor, stream=None):
+    """LayerNorm of the rows of x (n, d) into y, RMSNorm where b and mean are
+    None; mean and rstd (fp32, n) are what the backward call needs."""
+    _matrix(x, "x")
+    n, d = x.shape
+    _matrix(y, "y", n, d, x.dtype)
+    _check(lib().adadsf_norm_forward(x.data_ptr(), _vector(w, "w", d, x.dtype), _vector(b, "b", d, x.dtype), n, d,
+                                     DTYPE_CODE[x.dtype], float(eps), 1 if b is None and mean is None else 0, y.data_ptr(),
+                                     _vector(mean, "mean", n, torch.float32), _vector(rstd, "rstd", n, torch.float32),
+                                     _s(stream)))
+
+
+def adadsf_norm_backward_workspace_size(n_rows: int, d: int) -> int:
+    n = lib().adadsf_norm_backward_workspace_size(int(n_rows), int(d))
+    if n == 0:
+        raise AdadsfError(ERR_INVALID_ARG, f"no workspace for {n_rows} rows of {d}")
+    return n
+
+
+def adadsf_norm_backward(grad_y: torch.Tensor, x: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor, grad_x: torch.Tensor,
+                         mean: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
+                         grad_w: Optional[torch.Tensor] = None, grad_b: Optional[torch.Tensor] = None,
+                         accumulate: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of adadsf_norm_forward (RMSNorm where mean is None): grad_x
+    like x, with add added; grad_w and grad_b (fp32, d) where wanted."""
+    _matrix(x, "x")
+    n, d = x.shape
+    for t, name in ((grad_y, "grad_y"), (grad_x, "grad_x"), (add, "add")):
+        if t is not None or name != "add":
+            _matrix(t, name, n, d, x.dtype)
+    ws = _ws(ws, lambda: adadsf_norm_backward_workspace_size(n, d), x.device)
+    _check(lib().adadsf_norm_backward(grad_y.data_ptr(), x.data_ptr(), _vector(w, "w", d, x.dtype),
+                                      _vector(mean, "mean", n, torch.float32), _vector(rstd, "rstd", n, torch.float32),
+                                      None if add is None else add.data_ptr(), n, d, DTYPE_CODE[x.dtype],
+                                      1 if mean is None else 0, grad_x.data_ptr(), _vector(grad_w, "grad_w", d, torch.float32),
+                                      _vector(grad_b, "grad_b", d, torch.float32), 1 if accumulate else 0, ws.data_ptr(),
+                                      ws.numel(), _s(stream)))
+
+
+def adadsf_embed_forward(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+                         ws: Optional[torch.Tensor] = None, stream=None):
+    """out (n, d) = scale * the rows ids (int32; below 0: zeros) of table (vocab, d)."""
+    _matrix(table, "table")
+    n, (vocab, d) = ids.numel(), table.shape
+    _matrix(out, "out", n, d, table.dtype)
+    ws = _ws(ws, lambda: 256, table.device)
+    _check(lib().adadsf_embed_forward(_vector(ids, "ids", n, torch.int32), n, table.data_ptr(), vocab, d,
+                                      DTYPE_CODE[table.dtype], float(scale), out.data_ptr(), ws.data_ptr(), ws.numel(),
+                                      _s(stream)))
+
+
+def adadsf_embed_backward_workspace_size(n: int, vocab: int, d: int) -> int:
+    size = lib().adadsf_embed_backward_workspace_size(int(n), int(vocab), int(d))
+    if size == 0:
+        raise AdadsfError(ERR_INVALID_ARG, f"no workspace for {n} tokens of {vocab}, rows of {d}")
+    return size
+
+
+def adadsf_embed_backward(ids: torch.Tensor, grad_out: torch.Tensor, grad_table: torch.Tensor, scale: float = 1.0,
+                          accumulate: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
+    """The table's gradient (vocab, d): scale * the sum of grad_out's rows of
+    each id, in one order; accumulate adds to the rows of the ids that came."""
+    _matrix(grad_table, "grad_table")
+    n, (vocab, d) = ids.numel(), grad_table.shape
+    _matrix(grad_out, "grad_out", n, d, grad_table.dtype)
+    ws = _ws(ws, lambda: adadsf_embed_backward_workspace_size(n, vocab, d), grad_table.device)
+    _check(lib().adadsf_embed_backward(_vector(ids, "ids", n, torch.int32), grad_out.data_ptr(), n, vocab, d,
+                                       DTYPE_CODE[grad_table.dtype], float(scale), grad_table.data_ptr(),
+                                       1 if accumulate else 0, ws.data_ptr(), ws.numel(), _s(stream)))
 
 
 def adadsf_sync_check(ws: torch.Tensor, stream=None) -> int:

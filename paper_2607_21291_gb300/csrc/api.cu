@@ -1742,6 +1742,337 @@ adadsf_status adadsf_sample(const void* logits_dev, int64_t ld_logits, int B, in
                 CALL(sample(dtype, a, dev), "sampling"));
 }
 
+// ---------------------------------------------------------------- training at the two ends
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// A vector of one number a row.
+adadsf_status need_row(const void* p, const char* name, bool optional) {
+  if (!p && !optional) return fail(ADADSF_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned4(p)) return fail(ADADSF_ERR_INVALID_ARG, "%s is misaligned", name);
+  return ADADSF_OK;
+}
+
+constexpr int64_t kHeadMaxRows = (int64_t)1 << 22;
+constexpr int kHeadMaxClasses = 1 << 24;
+
+adadsf_status check_head(int64_t n_rows, int d, int n_classes, int dtype, int top_k) {
+  if (dtype != ADADSF_F32 && dtype != ADADSF_BF16) return fail(ADADSF_ERR_INVALID_ARG, "dtype %d unknown", dtype);
+  if (n_rows < 0 || d <= 0 || n_classes <= 0 || top_k <= 0)
+    return fail(ADADSF_ERR_INVALID_ARG, "need n_rows >= 0 and d, n_classes, top_k > 0");
+  const int vec = dtype == ADADSF_BF16 ? 8 : 4;
+  if (d % vec || d > 65536) return fail(ADADSF_ERR_UNSUPPORTED, "d=%d must be a multiple of %d up to 65536", d, vec);
+  if (n_rows > kHeadMaxRows || n_classes > kHeadMaxClasses)
+    return fail(ADADSF_ERR_UNSUPPORTED, "n_rows=%lld exceeds 2^22 or n_classes=%d 2^24", (long long)n_rows, n_classes);
+  if (top_k > kHeadMaxK) return fail(ADADSF_ERR_UNSUPPORTED, "top_k=%d exceeds %d", top_k, kHeadMaxK);
+  return ADADSF_OK;
+}
+
+struct HeadLayout {
+  HeadPlan plan;
+  size_t count, rows, target, cls, p, ent, picked, packed, rec, g[2], acc, total;
+};
+HeadLayout head_layout(int64_t n, int d, int V, int dtype, int k) {
+  HeadLayout l;
+  l.plan = head_plan(dtype, n, d, V);
+  Carver cv;
+  cv.take(kErrBytes);
+  cv.take(kSyncBytes);
+  l.count = cv.take(256);
+  l.rows = cv.take((size_t)l.plan.cap * 4);
+  l.target = cv.take((size_t)n * 4);
+  l.cls = cv.take((size_t)n * k * 4);
+  l.p = cv.take((size_t)n * k * 4);
+  l.ent = cv.take((size_t)n * 4);
+  l.picked = cv.take((size_t)n * k * 4);
+  l.packed = cv.take(l.plan.packed);
+  // the forward pass's records and the backward pass's buffers take turns
+  Carver back = cv;
+  l.rec = cv.take(l.plan.rec);
+  l.g[0] = back.take(l.plan.g);
+  l.g[1] = back.take(l.plan.g);
+  l.acc = back.take(l.plan.acc);
+  l.total = cv.cur > back.cur ? cv.cur : back.cur;
+  return l;
+}
+
+// What both losses and both directions share; target: one a row, or NULL with a teacher's k.
+struct HeadCall {
+  const void *h, *w;
+  const int32_t* target;
+  const int32_t* idx;
+  const float* logit;
+  int k;
+  float temp;
+  int64_t n;
+  int d, V, dtype;
+};
+
+adadsf_status head_prepare(const HeadCall& c, void* ws, size_t ws_bytes, void* stream, HeadLayout* l, Head* a, Dev* dev) {
+  *l = head_layout(c.n, c.d, c.V, c.dtype, c.k);
+  TRY(check_ws(ws, ws_bytes, l->total));
+  NEED_PTR(c.h, "h_dev");
+  NEED_PTR(c.w, "w_head_dev");
+  TRY(device_info(dev, stream, ws));
+  *a = Head();
+  a->h = c.h;
+  a->w = c.w;
+  a->n = c.n;
+  a->d = c.d;
+  a->V = c.V;
+  a->temp = c.temp;
+  a->k = c.k;
+  a->count = at<int32_t>(ws, l->count);
+  a->rows = at<int32_t>(ws, l->rows);
+  a->packed = at<void>(ws, l->packed);
+  a->cap = l->plan.cap;
+  a->picked = at<float>(ws, l->picked);
+  a->rec = at<float2>(ws, l->rec);
+  a->G[0] = at<void>(ws, l->g[0]);
+  a->G[1] = at<void>(ws, l->g[1]);
+  a->dh_acc = at<float>(ws, l->acc);
+  a->piece = l->plan.piece;
+  a->splits = l->plan.splits;
+  if (c.target) {
+    a->target = a->cls = c.target;
+    return ADADSF_OK;
+  }
+  int32_t* target = at<int32_t>(ws, l->target);
+  a->target = target;
+  a->cls = at<int32_t>(ws, l->cls);
+  a->p = at<float>(ws, l->p);
+  a->ent = at<float>(ws, l->ent);
+  CUDA_TRY(head_teacher(c.idx, c.logit, c.n, c.k, c.V, c.temp, at<int32_t>(ws, l->cls), at<float>(ws, l->p),
+                        at<float>(ws, l->ent), target, *dev),
+           "teacher's targets");
+  return ADADSF_OK;
+}
+
+adadsf_status head_loss(const HeadCall& c, float* loss, float* lse, double* acc, void* ws, size_t ws_bytes, void* stream) {
+  TRY(need_row(loss, "loss_dev", !acc || c.n == 0));
+  TRY(need_row(lse, "lse_dev", c.n == 0));
+  if (reinterpret_cast<uintptr_t>(acc) & 7u) return fail(ADADSF_ERR_INVALID_ARG, "acc_dev is not 8-byte aligned");
+  if (c.n == 0) return ADADSF_OK;
+  HeadLayout l;
+  Head a;
+  Dev dev;
+  TRY(head_prepare(c, ws, ws_bytes, stream, &l, &a, &dev));
+  a.loss = loss;
+  a.lse = lse;
+  a.acc = acc;
+  return launch(dev, ADADSF_KERNEL_HEAD_LOSS, c.dtype == ADADSF_BF16, 2.0 * c.n * c.V * c.d,
+                ((double)c.n * c.d + (double)c.V * c.d) * elem_size(c.dtype), CALL(head_forward(c.dtype, a, dev), "head loss"));
+}
+
+adadsf_status head_grad(const HeadCall& c, const float* lse, const float* grad_loss, void* grad_h, void* grad_w, int accumulate_w,
+                        void* ws, size_t ws_bytes, void* stream) {
+  if (accumulate_w != 0 && accumulate_w != 1) return fail(ADADSF_ERR_INVALID_ARG, "accumulate_w must be 0 or 1");
+  if (!grad_h && !grad_w) return fail(ADADSF_ERR_INVALID_ARG, "grad_h_dev and grad_w_dev are both NULL");
+  if (grad_h) NEED_PTR(grad_h, "grad_h_dev");
+  if (grad_w) NEED_PTR(grad_w, "grad_w_dev");
+  if (grad_w && (grad_w == c.w || grad_w == c.h))
+    return fail(ADADSF_ERR_INVALID_ARG, "grad_w_dev is an input's buffer");
+  TRY(need_row(lse, "lse_dev", c.n == 0));
+  TRY(need_row(grad_loss, "grad_loss_dev", true));
+  if (c.n == 0) {
+    if (grad_w && !accumulate_w)
+      CUDA_TRY(cudaMemsetAsync(grad_w, 0, (size_t)c.V * c.d * elem_size(c.dtype), static_cast<cudaStream_t>(stream)), "head gradient");
+    return ADADSF_OK;
+  }
+  HeadLayout l;
+  Head a;
+  Dev dev;
+  TRY(head_prepare(c, ws, ws_bytes, stream, &l, &a, &dev));
+  a.lse = const_cast<float*>(lse);   // read
+  a.g = grad_loss;
+  a.dh = grad_h;
+  a.dw = grad_w;
+  a.add_w = accumulate_w != 0;
+  const double product = 2.0 * c.n * c.V * c.d;
+  return launch(dev, ADADSF_KERNEL_HEAD_GRAD, c.dtype == ADADSF_BF16, product * (1 + (grad_h != nullptr) + (grad_w != nullptr)),
+                ((double)c.n * c.d + (double)c.V * c.d) * 2 * elem_size(c.dtype),
+                CALL(head_backward(c.dtype, a, l.plan, dev), "head gradient"));
+}
+
+adadsf_status check_temperature(float temperature) {
+  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature))
+    return fail(ADADSF_ERR_INVALID_ARG, "temperature must be a positive number");
+  return ADADSF_OK;
+}
+
+}  // namespace
+
+size_t adadsf_head_workspace_size(int64_t n_rows, int d, int n_classes, int dtype, int top_k) {
+  if (check_head(n_rows, d, n_classes, dtype, top_k) != ADADSF_OK) return 0;
+  return head_layout(n_rows, d, n_classes, dtype, top_k).total;
+}
+
+adadsf_status adadsf_head_loss(const void* h_dev, const void* w_head_dev, const int32_t* target_dev, int64_t n_rows, int d,
+                               int n_classes, int dtype, float* loss_dev, float* lse_dev, double* acc_dev, void* ws,
+                               size_t ws_bytes, void* stream) {
+  TRY(check_head(n_rows, d, n_classes, dtype, 1));
+  TRY(need_row(target_dev, "target_dev", n_rows == 0));
+  const HeadCall c = {h_dev, w_head_dev, target_dev, nullptr, nullptr, 1, 1.f, n_rows, d, n_classes, dtype};
+  return head_loss(c, loss_dev, lse_dev, acc_dev, ws, ws_bytes, stream);
+}
+
+adadsf_status adadsf_head_loss_backward(const void* h_dev, const void* w_head_dev, const int32_t* target_dev, int64_t n_rows,
+                                        int d, int n_classes, int dtype, const float* lse_dev, const float* grad_loss_dev,
+                                        void* grad_h_dev, void* grad_w_dev, int accumulate_w, void* ws, size_t ws_bytes,
+                                        void* stream) {
+  TRY(check_head(n_rows, d, n_classes, dtype, 1));
+  TRY(need_row(target_dev, "target_dev", n_rows == 0));
+  const HeadCall c = {h_dev, w_head_dev, target_dev, nullptr, nullptr, 1, 1.f, n_rows, d, n_classes, dtype};
+  return head_grad(c, lse_dev, grad_loss_dev, grad_h_dev, grad_w_dev, accumulate_w, ws, ws_bytes, stream);
+}
+
+adadsf_status adadsf_distill_loss(const void* h_dev, const void* w_head_dev, const int32_t* top_idx_dev,
+                                  const float* top_logit_dev, int top_k, float temperature, int64_t n_rows, int d, int n_classes,
+                                  int dtype, float* loss_dev, float* lse_dev, double* acc_dev, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  TRY(check_head(n_rows, d, n_classes, dtype, top_k));
+  TRY(check_temperature(temperature));
+  TRY(need_row(top_idx_dev, "top_idx_dev", n_rows == 0));
+  TRY(need_row(top_logit_dev, "top_logit_dev", n_rows == 0));
+  const HeadCall c = {h_dev, w_head_dev, nullptr, top_idx_dev, top_logit_dev, top_k, temperature, n_rows, d, n_classes, dtype};
+  return head_loss(c, loss_dev, lse_dev, acc_dev, ws, ws_bytes, stream);
+}
+
+adadsf_status adadsf_distill_loss_backward(const void* h_dev, const void* w_head_dev, const int32_t* top_idx_dev,
+                                           const float* top_logit_dev, int top_k, float temperature, int64_t n_rows, int d,
+                                           int n_classes, int dtype, const float* lse_dev, const float* grad_loss_dev,
+                                           void* grad_h_dev, void* grad_w_dev, int accumulate_w, void* ws, size_t ws_bytes,
+                                           void* stream) {
+  TRY(check_head(n_rows, d, n_classes, dtype, top_k));
+  TRY(check_temperature(temperature));
+  TRY(need_row(top_idx_dev, "top_idx_dev", n_rows == 0));
+  TRY(need_row(top_logit_dev, "top_logit_dev", n_rows == 0));
+  const HeadCall c = {h_dev, w_head_dev, nullptr, top_idx_dev, top_logit_dev, top_k, temperature, n_rows, d, n_classes, dtype};
+  return head_grad(c, lse_dev, grad_loss_dev, grad_h_dev, grad_w_dev, accumulate_w, ws, ws_bytes, stream);
+}
+
+namespace {
+
+adadsf_status check_norm(int64_t n_rows, int d, int dtype) {
+  if (dtype != ADADSF_F32 && dtype != ADADSF_BF16) return fail(ADADSF_ERR_INVALID_ARG, "dtype %d unknown", dtype);
+  if (n_rows < 0 || d <= 0) return fail(ADADSF_ERR_INVALID_ARG, "need n_rows >= 0 and d > 0");
+  const int vec = dtype == ADADSF_BF16 ? 8 : 4;
+  if (d % vec || d > kNormMaxD) return fail(ADADSF_ERR_UNSUPPORTED, "d=%d must be a multiple of %d up to %d", d, vec, kNormMaxD);
+  if (n_rows > (int64_t)INT32_MAX) return fail(ADADSF_ERR_UNSUPPORTED, "n_rows too large");
+  return ADADSF_OK;
+}
+
+adadsf_status check_embed(int64_t n, int vocab, int d, int dtype, float scale) {
+  if (dtype != ADADSF_F32 && dtype != ADADSF_BF16) return fail(ADADSF_ERR_INVALID_ARG, "dtype %d unknown", dtype);
+  if (n < 0 || vocab <= 0 || d <= 0) return fail(ADADSF_ERR_INVALID_ARG, "need n >= 0 and vocab, d > 0");
+  const int vec = dtype == ADADSF_BF16 ? 8 : 4;
+  if (d % vec || d > 65536) return fail(ADADSF_ERR_UNSUPPORTED, "d=%d must be a multiple of %d up to 65536", d, vec);
+  if (n > (int64_t)1 << 30 || vocab > 1 << 27)
+    return fail(ADADSF_ERR_UNSUPPORTED, "n=%lld exceeds 2^30 or vocab=%d 2^27", (long long)n, vocab);
+  if (!isfinite(scale)) return fail(ADADSF_ERR_INVALID_ARG, "scale must be a number");
+  return ADADSF_OK;
+}
+
+}  // namespace
+
+adadsf_status adadsf_norm_forward(const void* x_dev, const void* w_dev, const void* b_dev, int64_t n_rows, int d, int dtype,
+                                  float eps, int is_rms, void* y_dev, float* mean_dev, float* rstd_dev, void* stream) {
+  TRY(check_norm(n_rows, d, dtype));
+  if (!(eps > 0.f) || !isfinite(eps)) return fail(ADADSF_ERR_INVALID_ARG, "eps must be a positive number");
+  if (is_rms && (b_dev || mean_dev)) return fail(ADADSF_ERR_INVALID_ARG, "RMSNorm has neither b_dev nor mean_dev");
+  if (n_rows == 0) return ADADSF_OK;
+  NEED_PTR(x_dev, "x_dev");
+  NEED_PTR(w_dev, "w_dev");
+  if (!is_rms) {
+    NEED_PTR(b_dev, "b_dev");
+    TRY(need_row(mean_dev, "mean_dev", false));
+  }
+  NEED_PTR(y_dev, "y_dev");
+  TRY(need_row(rstd_dev, "rstd_dev", false));
+  Dev dev;
+  TRY(device_info(&dev, stream, nullptr));
+  return launch(dev, ADADSF_KERNEL_NORM, false, 0, 2.0 * n_rows * d * elem_size(dtype),
+                CALL(norm_forward(dtype, x_dev, w_dev, b_dev, n_rows, d, eps, is_rms != 0, y_dev, mean_dev, rstd_dev, dev), "norm"));
+}
+
+size_t adadsf_norm_backward_workspace_size(int64_t n_rows, int d) {
+  if (n_rows < 0 || d <= 0 || d > kNormMaxD) return 0;
+  return kErrBytes + align256(norm_backward_scratch(n_rows, d));
+}
+
+adadsf_status adadsf_norm_backward(const void* grad_y_dev, const void* x_dev, const void* w_dev, const float* mean_dev,
+                                   const float* rstd_dev, const void* add_dev, int64_t n_rows, int d, int dtype, int is_rms,
+                                   void* grad_x_dev, float* grad_w_dev, float* grad_b_dev, int accumulate, void* ws,
+                                   size_t ws_bytes, void* stream) {
+  TRY(check_norm(n_rows, d, dtype));
+  if (accumulate != 0 && accumulate != 1) return fail(ADADSF_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+  if (is_rms && (mean_dev || grad_b_dev)) return fail(ADADSF_ERR_INVALID_ARG, "RMSNorm has neither mean_dev nor grad_b_dev");
+  TRY(need_row(grad_w_dev, "grad_w_dev", true));
+  TRY(need_row(grad_b_dev, "grad_b_dev", true));
+  TRY(check_ws(ws, ws_bytes, adadsf_norm_backward_workspace_size(n_rows, d)));
+  if (n_rows == 0) {
+    for (float* g : {grad_w_dev, grad_b_dev})
+      if (g && !accumulate) CUDA_TRY(cudaMemsetAsync(g, 0, (size_t)d * 4, static_cast<cudaStream_t>(stream)), "norm gradient");
+    return ADADSF_OK;
+  }
+  NEED_PTR(grad_y_dev, "grad_y_dev");
+  NEED_PTR(x_dev, "x_dev");
+  NEED_PTR(w_dev, "w_dev");
+  if (!is_rms) TRY(need_row(mean_dev, "mean_dev", false));
+  TRY(need_row(rstd_dev, "rstd_dev", false));
+  if (add_dev) NEED_PTR(add_dev, "add_dev");
+  NEED_PTR(grad_x_dev, "grad_x_dev");
+  Dev dev;
+  TRY(device_info(&dev, stream, ws));
+  return launch(dev, ADADSF_KERNEL_NORM_GRAD, false, 0, (3.0 + (add_dev != nullptr)) * n_rows * d * elem_size(dtype),
+                CALL(norm_backward(dtype, grad_y_dev, x_dev, w_dev, mean_dev, rstd_dev, add_dev, n_rows, d, grad_x_dev, grad_w_dev,
+                                   grad_b_dev, accumulate != 0, at<float>(ws, kErrBytes), dev),
+                     "norm gradient"));
+}
+
+adadsf_status adadsf_embed_forward(const int32_t* ids_dev, int64_t n, const void* table_dev, int vocab, int d, int dtype,
+                                   float scale, void* out_dev, void* ws, size_t ws_bytes, void* stream) {
+  TRY(check_embed(n, vocab, d, dtype, scale));
+  TRY(check_ws(ws, ws_bytes, kErrBytes));
+  if (n == 0) return ADADSF_OK;
+  TRY(need_row(ids_dev, "ids_dev", false));
+  NEED_PTR(table_dev, "table_dev");
+  NEED_PTR(out_dev, "out_dev");
+  Dev dev;
+  TRY(device_info(&dev, stream, ws));
+  return launch(dev, ADADSF_KERNEL_EMBED, false, 0, 2.0 * n * d * elem_size(dtype),
+                CALL(embed_scale(dtype, ids_dev, n, table_dev, vocab, d, scale, out_dev, dev), "embedding"));
+}
+
+size_t adadsf_embed_backward_workspace_size(int64_t n, int vocab, int d) {
+  if (n < 0 || n > (int64_t)1 << 30 || vocab <= 0 || vocab > 1 << 27 || d <= 0 || d > 65536) return 0;
+  return kErrBytes + embed_backward_scratch(n, vocab, d);
+}
+
+adadsf_status adadsf_embed_backward(const int32_t* ids_dev, const void* grad_out_dev, int64_t n, int vocab, int d, int dtype,
+                                    float scale, void* grad_table_dev, int accumulate, void* ws, size_t ws_bytes, void* stream) {
+  TRY(check_embed(n, vocab, d, dtype, scale));
+  if (accumulate != 0 && accumulate != 1) return fail(ADADSF_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+  NEED_PTR(grad_table_dev, "grad_table_dev");
+  TRY(check_ws(ws, ws_bytes, adadsf_embed_backward_workspace_size(n, vocab, d)));
+  if (n == 0) {
+    if (!accumulate)
+      CUDA_TRY(cudaMemsetAsync(grad_table_dev, 0, (size_t)vocab * d * elem_size(dtype), static_cast<cudaStream_t>(stream)),
+               "embedding gradient");
+    return ADADSF_OK;
+  }
+  TRY(need_row(ids_dev, "ids_dev", false));
+  NEED_PTR(grad_out_dev, "grad_out_dev");
+  if (grad_table_dev == grad_out_dev) return fail(ADADSF_ERR_INVALID_ARG, "grad_table_dev is grad_out_dev");
+  Dev dev;
+  TRY(device_info(&dev, stream, ws));
+  return launch(dev, ADADSF_KERNEL_EMBED_GRAD, false, 0, ((double)n * d + (accumulate ? 0.0 : (double)vocab * d)) * elem_size(dtype),
+                CALL(embed_backward(dtype, ids_dev, grad_out_dev, n, vocab, d, scale, grad_table_dev, accumulate != 0,
+                                    at<uint8_t>(ws, kErrBytes), dev),
+                     "embedding gradient"));
+}
+
 adadsf_status adadsf_sync_check(void* ws, size_t ws_bytes, void* stream) {
   TRY(check_ws(ws, ws_bytes, kErrBytes));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -1810,7 +2141,7 @@ const char* adadsf_kernel_name(int kind) {
       "embed", "router", "topk", "positions", "gather_norm", "gemm_qkv", "rope_table", "rope",
       "attention", "gemm_o", "norm2", "gemm_up", "gemm_down", "stats", "final_norm", "copy",
       "linear", "selftest", "gemm_qkv_up", "gemm_o_down", "topk_gather_norm", "decide", "kv_cache", "align",
-      "paged_append", "paged_read", "paged_attention", "sample"};
+      "paged_append", "paged_read", "paged_attention", "sample", "head_loss", "head_grad", "norm", "norm_grad", "embed_grad"};
   return (kind >= 0 && kind < ADADSF_KERNEL_COUNT) ? names[kind] : "unknown";
 }
 

@@ -1,0 +1,327 @@
+// Losses at the LM head: targets, packing of the rows that have one, and what joins the
+// products of head_tc.cu and head_f32.cu (formulas in head.cuh).
+#include <math.h>
+
+#include <algorithm>
+
+#include "head.cuh"
+
+namespace adadsf {
+namespace {
+
+constexpr int kTeacherThreads = 128;
+
+// A block a row. p = softmax of the slots in use, sorted by class (each slot counts the ones before
+// it: k^2 comparisons, no barriers between them).
+__global__ void __launch_bounds__(kTeacherThreads)
+    head_teacher_kernel(const int32_t* idx, const float* logit, int k, int V, float inv_t, int32_t* cls, float* p, float* ent,
+                        int32_t* target, int* err) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ int32_t c[kHeadMaxK];
+  __shared__ float t[kHeadMaxK];
+  __shared__ float red[2][kTeacherThreads / 32];
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  float top = -INFINITY;
+  bool bad = false;
+  for (int j = tid; j < k; j += kTeacherThreads) {
+    const int32_t id = idx[row * k + j];
+    const float z = logit[row * k + j] * inv_t;
+    const bool in = id >= 0 && id < V && !(z == -INFINITY);
+    bad |= id >= V;
+    c[j] = in ? id : INT_MAX;
+    t[j] = in ? z : -INFINITY;
+    if (in) top = fmaxf(top, z);
+  }
+  if (bad) set_device_error(err, DEVERR_INDEX);
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) red[0][warp] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  float sum = 0.f;
+  for (int j = tid; j < k; j += kTeacherThreads) {
+    if (c[j] != INT_MAX) sum += expf(t[j] - top);
+  }
+  sum = warp_sum(sum);
+  if (lane == 0) red[1][warp] = sum;
+  __syncthreads();
+  sum = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  const float log_sum = logf(sum), inv = 1.f / sum;
+  float e = 0.f;
+  for (int j = tid; j < k; j += kTeacherThreads) {
+    const int32_t mine = c[j];
+    const bool in = mine != INT_MAX;
+    const float w = in ? expf(t[j] - top) * inv : 0.f;
+    if (in && w != 0.f) e += w * ((t[j] - top) - log_sum);
+    int rank = 0;
+    for (int i = 0; i < k; ++i) rank += c[i] < mine || (c[i] == mine && i < j);
+    cls[row * k + rank] = mine;
+    p[row * k + rank] = w;
+    if (rank == 0) target[row] = in ? mine : -1;
+  }
+  e = warp_sum(e);
+  __syncthreads();
+  if (lane == 0) red[0][warp] = e;
+  __syncthreads();
+  if (tid == 0) ent[row] = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
+}
+
+constexpr int kPackThreads = 256;
+
+// Rows with a target, in order: their numbers, their count and a copy of their features. Every block counts all
+// targets by itself (no launch before it, no order between blocks). Rows without one get a loss, a
+// logarithm and a gradient of zero; what they hold is read by nobody. Packed rows past the last one, up to a
+// multiple of kHeadZeroPad, are zero: products over rows run that far.
+template <typename T>
+__global__ void __launch_bounds__(kPackThreads)
+    head_pack_kernel(const int32_t* target, int64_t n, int V, int64_t per_block, const T* h, int d, T* packed, int32_t* rows,
+                     int32_t* count, float* loss, float* lse, T* dh, int* err) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr int W = kPackThreads / 32;
+  __shared__ int red[2][W];
+  __shared__ int at[kPackThreads];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t r0 = blockIdx.x * per_block, r1 = min(n, r0 + per_block);
+  int before = 0, all = 0;
+  for (int64_t i = tid; i < n; i += kPackThreads) {
+    const int32_t t = target[i];
+    const int in = t >= 0 && t < V;
+    all += in;
+    before += in && i < r0;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  all = __reduce_add_sync(0xffffffffu, all);
+  if (lane == 0) {
+    red[0][warp] = before;
+    red[1][warp] = all;
+  }
+  __syncthreads();
+  before = all = 0;
+  for (int i = 0; i < W; ++i) {
+    before += red[0][i];
+    all += red[1][i];
+  }
+  if (blockIdx.x == 0 && tid == 0) *count = all;
+  const int nv = d / Elem<T>::kVec;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  for (int64_t c = r0; c < r1; c += kPackThreads) {
+    const int64_t r = c + tid;
+    const int32_t t = r < r1 ? target[r] : -1;
+    const bool in = t >= 0 && t < V;
+    if (t >= V) set_device_error(err, DEVERR_INDEX);
+    const uint32_t live = __ballot_sync(0xffffffffu, in);
+    __syncthreads();   // the counts and places before are read
+    if (lane == 0) red[0][warp] = __popc(live);
+    __syncthreads();
+    int place = before + __popc(live & ((1u << lane) - 1));
+    for (int i = 0; i < W; ++i) {
+      if (i < warp) place += red[0][i];
+      before += red[0][i];
+    }
+    at[tid] = in ? place : -1;
+    if (in) rows[place] = (int32_t)r;
+    if (r < r1 && !in) {
+      if (loss) loss[r] = 0.f;
+      if (lse) lse[r] = 0.f;
+    }
+    __syncthreads();
+    const int in_chunk = (int)min((int64_t)kPackThreads, r1 - c);
+    for (int i = warp; i < in_chunk; i += W) {
+      const uint4* src = reinterpret_cast<const uint4*>(h + (c + i) * d);
+      if (at[i] >= 0) {
+        uint4* dst = reinterpret_cast<uint4*>(packed + (int64_t)at[i] * d);
+        for (int v = lane; v < nv; v += 32) dst[v] = src[v];
+      } else if (dh) {
+        uint4* dst = reinterpret_cast<uint4*>(dh + (c + i) * d);
+        for (int v = lane; v < nv; v += 32) dst[v] = zero;
+      }
+    }
+  }
+  const int tail = (kHeadZeroPad - all % kHeadZeroPad) % kHeadZeroPad;
+  for (int i = (int)((blockIdx.x + (int64_t)gridDim.x * warp)); i < tail; i += (int)gridDim.x * W) {
+    uint4* dst = reinterpret_cast<uint4*>(packed + ((int64_t)all + i) * d);
+    for (int v = lane; v < nv; v += 32) dst[v] = zero;
+  }
+}
+
+// Losses of 32 packed rows: a lane a row, the warps share the records of its classes and its targets.
+// Every sum runs in one order.
+constexpr int kMergeWarps = 32;
+__global__ void __launch_bounds__(32 * kMergeWarps)
+    head_merge_kernel(const int32_t* count, const int32_t* rows, const float2* rec, int64_t cap, int n_rec, const float* picked,
+                      const float* p, const float* ent, int k, float temp, float* loss, float* lse) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ float s_top[kMergeWarps][32], s_sum[kMergeWarps][32], s_pz[kMergeWarps][32], s_p[kMergeWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int n = *count;
+  const float inv_t = 1.f / temp;
+  for (int64_t m0 = (int64_t)blockIdx.x * 32; m0 < n; m0 += (int64_t)gridDim.x * 32) {
+    const int64_t m = m0 + lane;
+    float top = -INFINITY, sum = 0.f, pz = 0.f, ps = 0.f;
+    int64_t row = 0;
+    if (m < n) {
+      row = rows[m];
+#pragma unroll 4
+      for (int i = warp; i < n_rec; i += kMergeWarps) {
+        const float2 r = rec[(int64_t)i * cap + m];
+        const float now = fmaxf(top, r.x);
+        // a side without a number so far (-inf) adds nothing but its NaN
+        const float a = top == now ? 1.f : expf((top - now) * inv_t), b = r.x == now ? 1.f : expf((r.x - now) * inv_t);
+        sum = sum * a + r.y * b;
+        top = now;
+      }
+      for (int j = warp; j < k; j += kMergeWarps) {
+        const float w = p ? p[row * k + j] : 1.f;
+        if (w != 0.f) {
+          pz += w * (picked[row * k + j] * inv_t);
+          ps += w;
+        }
+      }
+    }
+    s_top[warp][lane] = top;
+    s_sum[warp][lane] = sum;
+    s_pz[warp][lane] = pz;
+    s_p[warp][lane] = ps;
+    __syncthreads();
+    if (warp == 0 && m < n) {
+      for (int i = 1; i < kMergeWarps; ++i) top = fmaxf(top, s_top[i][lane]);
+      sum = 0.f;
+      pz = 0.f;
+      ps = 0.f;
+      for (int i = 0; i < kMergeWarps; ++i) {
+        const float a = s_top[i][lane] == top ? 1.f : expf((s_top[i][lane] - top) * inv_t);
+        sum += s_sum[i][lane] * a;
+        pz += s_pz[i][lane];
+        ps += s_p[i][lane];
+      }
+      const float z = top * inv_t + logf(sum);
+      lse[row] = z;
+      if (loss) loss[row] = temp * temp * ((ent ? ent[row] : 0.f) + (ps * z - pz));
+    }
+    __syncthreads();
+  }
+}
+
+// acc[0] += sum of the losses, acc[1] += rows that have one; one block, in a fixed order.
+__global__ void __launch_bounds__(1024) head_sum_kernel(const float* loss, int64_t n, const int32_t* count, double* acc) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ double red[32];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 1024) s += (double)loss[i];
+  s = warp_sum(s);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 32; ++i) s += red[i];
+    acc[0] += s;
+    acc[1] += (double)*count;
+  }
+}
+
+// The hidden states' gradient: a packed row's partial sums added in order, rounded once, to its row.
+template <typename T>
+__global__ void __launch_bounds__(256)
+    head_finish_kernel(const float* acc, const int32_t* count, const int32_t* rows, int64_t cap, int d, int splits, T* dh) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr int V = Elem<T>::kVec;
+  const int nv = d / V;
+  const int64_t n = (int64_t)*count * nv, stride = cap * d;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t m = i / nv;
+    const int c = (int)(i - m * nv) * V;
+    float s[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = 0.f;
+    for (int q = 0; q < splits; ++q) {
+      const float* a = acc + q * stride + m * d + c;
+#pragma unroll
+      for (int j = 0; j < V; j += 4) {
+        float f[4];
+        load4(a + j, f);
+#pragma unroll
+        for (int l = 0; l < 4; ++l) s[j + l] += f[l];
+      }
+    }
+    store_vec(dh + (int64_t)rows[m] * d + c, s);
+  }
+}
+
+template <typename T>
+cudaError_t pack(const Head& a, bool backward, const Dev& dev) {
+  const int64_t per = std::max<int64_t>(8, (a.n + 511) / 512);
+  return launch_pdl(head_pack_kernel<T>, dim3((unsigned)((a.n + per - 1) / per)), dim3(kPackThreads), 0, dev.stream, a.target,
+                    a.n, a.V, per, static_cast<const T*>(a.h), a.d, static_cast<T*>(a.packed), a.rows, a.count,
+                    backward ? (float*)nullptr : a.loss, backward ? (float*)nullptr : a.lse,
+                    backward ? static_cast<T*>(a.dh) : (T*)nullptr, dev.err);
+}
+
+}  // namespace
+
+// Classes a piece: its G in both buffers is to stay in the L2 with what else is read, but whole where
+// few rows make it small.
+HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
+  const int64_t es = dtype == kBF16 ? 2 : 4, tile = dtype == kBF16 ? 256 : 128;
+  HeadPlan q;
+  q.cap = (n + kHeadRowPad - 1) / kHeadRowPad * kHeadRowPad;
+  const int64_t padded = ((int64_t)V + 255) / 256 * 256;
+  int64_t piece = std::max<int64_t>(2048, (96ll << 20) / std::max<int64_t>(1, q.cap * es));
+  const int64_t pieces = (padded + piece - 1) / piece;
+  piece = ((padded + pieces - 1) / pieces + 255) / 256 * 256;
+  q.piece = (int)piece;
+  q.pieces = (int)((V + piece - 1) / piece);
+  // dH sums over a piece's classes: cut so that its tiles are about as long as the others
+  const int64_t other = std::max<int64_t>(std::max<int64_t>(q.cap, d), 1024);
+  const int64_t tiles = std::max<int64_t>(1, q.cap / tile * ((d + tile - 1) / tile));
+  int64_t splits = std::max<int64_t>(1, (piece + other / 2) / other);
+  splits = std::min<int64_t>(splits, std::max<int64_t>(1, 1024 / tiles));
+  q.splits = (int)std::min<int64_t>(splits, 64);
+  q.packed = (size_t)(q.cap * d * es);
+  q.rec = (size_t)(padded / 128 * q.cap * 8);
+  q.g = (size_t)(q.cap * piece * es);
+  q.acc = (size_t)(q.splits * q.cap * d * 4);
+  return q;
+}
+
+cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int k, int V, float temp, int32_t* cls, float* p,
+                         float* ent, int32_t* target, const Dev& dev) {
+  return launch_pdl(head_teacher_kernel, dim3((unsigned)n), dim3(kTeacherThreads), 0, dev.stream, idx, logit, k, V, 1.f / temp,
+                    cls, p, ent, target, dev.err);
+}
+
+cudaError_t head_forward(int dtype, const Head& a, const Dev& dev) {
+  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, false, dev) : pack<float>(a, false, dev);
+  if (e == cudaSuccess) e = dtype == kBF16 ? head_tc_stats(a, dev) : head_f32_stats(a, dev);
+  if (e != cudaSuccess) return e;
+  const int blocks = (int)std::min<int64_t>((a.n + 31) / 32, 2 * dev.num_sms);
+  e = launch_pdl(head_merge_kernel, dim3((unsigned)blocks), dim3(32 * kMergeWarps), 0, dev.stream, (const int32_t*)a.count,
+                 (const int32_t*)a.rows, (const float2*)a.rec, a.cap, (a.V + 127) / 128, (const float*)a.picked, a.p, a.ent, a.k,
+                 a.temp, a.loss, a.lse);
+  if (e != cudaSuccess || !a.acc) return e;
+  return launch_pdl(head_sum_kernel, dim3(1), dim3(1024), 0, dev.stream, (const float*)a.loss, a.n, (const int32_t*)a.count, a.acc);
+}
+
+cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev) {
+  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, true, dev) : pack<float>(a, true, dev);
+  const auto grad = dtype == kBF16 ? head_tc_grad : head_f32_grad;
+  // launch j: G of piece j, gradients of piece j - 1
+  for (int j = 0; j <= plan.pieces && e == cudaSuccess; ++j) {
+    const int64_t v = (int64_t)j * plan.piece, before = v - plan.piece;
+    const int n_g = j < plan.pieces ? (int)std::min<int64_t>(plan.piece, a.V - v) : 0;
+    const int n_d = j > 0 ? (int)std::min<int64_t>(plan.piece, a.V - before) : 0;
+    e = grad(a, j & 1, v, n_g, before, n_d, j == 1, dev);
+  }
+  if (e != cudaSuccess || !a.dh) return e;
+  const int blocks = (int)std::min<int64_t>((a.n * a.d / 4 + 255) / 256, 8 * dev.num_sms);
+  if (dtype == kBF16)
+    return launch_pdl(head_finish_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, dev.stream, (const float*)a.dh_acc,
+                      (const int32_t*)a.count, (const int32_t*)a.rows, a.cap, a.d, a.splits, static_cast<bf16*>(a.dh));
+  return launch_pdl(head_finish_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, dev.stream, (const float*)a.dh_acc,
+                    (const int32_t*)a.count, (const int32_t*)a.rows, a.cap, a.d, a.splits, static_cast<float*>(a.dh));
+}
+
+}  // namespace adadsf

@@ -304,6 +304,66 @@ cudaError_t paged_tc(const Paged& p, const void* q, int64_t ld_q, void* out, int
 // paged_f32.cu -- fp32 models.
 size_t paged_f32_scratch(const Paged& p);
 cudaError_t paged_f32(const Paged& p, const void* q, int64_t ld_q, void* out, int* sync, void* scratch, const Dev& dev);
+// head.cu -- losses at the LM head on packed rows (see head.cuh).
+struct Head {
+  const void *h, *w;                     // [n][d], [V][d]
+  int64_t n;
+  int d, V;
+  float temp;
+  const int32_t* target;                 // by row: below 0 none (with k slots: the first class)
+  const int32_t* cls; const float* p;    // by row, [k] ascending (p null: 1)
+  const float* ent;                      // by row: sum p log p (null: 0)
+  int k;
+  // packed rows: count, their rows, their copy [cap][d]
+  int32_t *count, *rows;
+  void* packed;
+  int64_t cap;
+  float2* rec;                           // [ceil(V / 256) * 2][cap]
+  float* picked;                         // by row, [k]
+  float *loss, *lse;                     // by row (loss may be null)
+  double* acc;                           // or null
+  // backward
+  const float* g;                        // by row, or null
+  void *dh, *dw;                         // either may be null
+  bool add_w;
+  void* G[2];                            // [cap][piece]
+  int piece, splits;
+  float* dh_acc;                         // [splits][cap][d]
+};
+struct HeadPlan {
+  int64_t cap;
+  int piece, pieces, splits;
+  size_t packed, rec, g, acc;            // bytes
+};
+HeadPlan head_plan(int dtype, int64_t n, int d, int V);
+constexpr int kHeadMaxK = 1024;
+// Teacher's logits [n][k] -> ascending classes, weights, sum p log p and first class of each row.
+cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int k, int V, float temp, int32_t* cls, float* p,
+                         float* ent, int32_t* target, const Dev& dev);
+cudaError_t head_forward(int dtype, const Head& a, const Dev& dev);
+cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev);
+// head_tc.cu (bf16), head_f32.cu: stats of all tiles; one launch of the backward pass -- G of the n_g classes
+// from v_g into G[buf], the gradients of the n_d classes from v_d from the other buffer.
+cudaError_t head_tc_stats(const Head& a, const Dev& dev);
+cudaError_t head_tc_grad(const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev);
+cudaError_t head_f32_stats(const Head& a, const Dev& dev);
+cudaError_t head_f32_grad(const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev);
+
+// norm_grad.cu -- norms of rows with their statistics, and the gradients. scratch: norm_backward_scratch bytes.
+constexpr int kNormMaxD = 8192;
+size_t norm_backward_scratch(int64_t n, int d);
+cudaError_t norm_forward(int dtype, const void* x, const void* w, const void* b, int64_t n, int d, float eps, bool rms, void* y,
+                         float* mean, float* rstd, const Dev& dev);
+cudaError_t norm_backward(int dtype, const void* dy, const void* x, const void* w, const float* mean, const float* rstd,
+                          const void* add, int64_t n, int d, void* dx, float* dw, float* db, bool accumulate, float* scratch,
+                          const Dev& dev);
+// embed_grad.cu
+cudaError_t embed_scale(int dtype, const int32_t* ids, int64_t n, const void* table, int vocab, int d, float scale, void* out,
+                        const Dev& dev);
+size_t embed_backward_scratch(int64_t n, int vocab, int d);
+cudaError_t embed_backward(int dtype, const int32_t* ids, const void* dy, int64_t n, int vocab, int d, float scale, void* out,
+                           bool add, void* scratch, const Dev& dev);
+
 // sample.cu
 struct Sample {
   const void* logits; int64_t ld;

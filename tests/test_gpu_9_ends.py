@@ -1,0 +1,565 @@
+"""GPU parity of training's two ends against 64-bit forms: cross entropy and
+distillation at the LM head, norms and embedding, each with its gradients, and
+a run of them together.
+
+Bounds. u = 2^-24 is half a step of fp32 (one rounding), b = 2^-8 of bf16; a sum
+of m terms in fp32, in any order, is off by at most m 2u of the sum of their
+absolute values (2u a step: the tensor cores do not round their sums to nearest)."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U, B16 = 2.0 ** -24, 2.0 ** -8
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def A():
+    from paper_2607_21291_gb300 import adadsf
+    adadsf.lib()
+    return adadsf
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape, std=1.0):
+    return torch.randn(*shape, generator=g, device="cuda") * std
+
+
+def within(got, ref, bound, what):
+    """Element by element; bound a tensor or a number."""
+    got, ref = got.double(), ref.double()
+    assert torch.isfinite(got).all(), what
+    over = (got - ref).abs() - bound
+    assert float(over.max()) <= 0, (what, float(over.max()), float((got - ref).abs().max()), int((over > 0).sum()))
+
+
+# ------------------------------------------------------------------ losses at the head
+def head_inputs(n, d, V, dtype, seed=0, std=1.0):
+    g = gen(seed * 1000 + n + d + V)
+    h = randn(g, n, d, std=std).to(DT[dtype])
+    w = randn(g, V, d, std=0.3 / math.sqrt(d) * 4).to(DT[dtype])
+    target = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    if n > 2:
+        target[torch.rand(n, generator=g, device="cuda") < 0.3] = -1
+        target[n // 2] = V - 1
+    gl = torch.rand(n, generator=g, device="cuda") + 0.1
+    return h, w, target, gl
+
+
+def want_of(target, V):
+    """Targets as rows of weights over the classes, and whether a row has one."""
+    used = (target >= 0) & (target < V)
+    want = torch.zeros(target.numel(), V, dtype=torch.float64, device="cuda")
+    want[used, target[used].long()] = 1.0
+    return want, used
+
+
+def teacher_want(idx, logit, V, temp):
+    there = (idx >= 0) & (idx < V) & (logit > -math.inf)
+    used = there.any(-1)
+    t = (logit.double() / temp).masked_fill(~there, -math.inf)
+    p = torch.where(used[:, None], torch.softmax(torch.where(used[:, None], t, 0.0), -1), 0.0)
+    want = torch.zeros(idx.shape[0], V, dtype=torch.float64, device="cuda")
+    want.scatter_add_(1, idx.clamp(0, V - 1).long(), torch.where(there, p, 0.0))
+    return want, used, torch.special.xlogy(p, p).sum(-1)
+
+
+class Ref:
+    """The losses and gradients in 64 bits, and how far the kernels may be from them."""
+
+    def __init__(self, h, w, want, used, ent, gl, temp, k):
+        bf = h.dtype == torch.bfloat16
+        h, w, gl = h.double(), w.double(), (torch.ones(h.shape[0], device="cuda") if gl is None else gl).double()
+        h = torch.where(used[:, None], h, 0.0)
+        d, V = w.shape[1], w.shape[0]
+        z = h @ w.T / temp
+        size = (h.abs() @ w.abs().T).amax(-1) / temp
+        self.lse = torch.where(used, torch.logsumexp(z, -1), 0.0)
+        mass = want.sum(-1)
+        self.loss = torch.where(used, temp ** 2 * (ent + mass * self.lse - (want * z).sum(-1)), 0.0)
+        # a logit: a sum of d products, and its scale; an exponential: 2^-22 and its argument's two roundings; the sum of
+        # them: 16 terms a chain, 4 chunks, and the records (V / 128 over 32 threads, then 32)
+        far = z.abs().amax(-1) + self.lse.abs()
+        e_z = (2 * d + 4) * U * size
+        e_lse = e_z + 4 * U + 4 * U * far + 2 * U * (64 + V / 4096 + 32) + 2 * U * self.lse.abs()
+        self.e_lse = torch.where(used, e_lse, 0.0)
+        # targets: a sum of k weights times logits, the entropy's like it
+        self.e_loss = torch.where(used, temp ** 2 * (e_lse + e_z + (2 * k + 16) * U * (far + 2 * ent.abs() + 1)), 0.0)
+        q = torch.exp(z - self.lse[:, None])
+        s = torch.where(used, gl * temp, 0.0)[:, None]
+        G = (q - want) * s
+        e_q = (e_z + e_lse + 4 * U + 4 * U * far)[:, None] * q * s.abs() + 4 * U * (q + want) * s.abs()
+        e_g = e_q + (B16 * (G.abs() + e_q) if bf else 2 * U * G.abs())
+        self.dh, self.dw = G @ w, G.T @ h
+        out = B16 if bf else U
+        n = h.shape[0]
+        self.e_dh = (e_g + 2 * U * (V + 64) * G.abs()) @ w.abs()
+        self.e_dh += out * (self.dh.abs() + self.e_dh)
+        self.e_dw = (e_g + 2 * U * (n + 64) * G.abs()).T @ h.abs()
+        self.e_dw += out * (self.dw.abs() + self.e_dw)
+        # roundings of G are independent: their part of a gradient has a 2-norm of about b / sqrt(3) (sum G^2 W^2)^(1/2);
+        # twice that, and the outputs' own roundings
+        g2 = G * G
+        self.n_dh = out * self.dh.norm() + 2 * out / 3 ** 0.5 * (g2 @ (w * w)).sum().sqrt() + (e_q @ w.abs()).norm() * 0.5
+        self.n_dw = out * self.dw.norm() + 2 * out / 3 ** 0.5 * (g2.T @ (h * h)).sum().sqrt() + (e_q.T @ h.abs()).norm() * 0.5
+        if not bf:   # rounding of long fp32 sums, for which the bound of a chain is all there is
+            self.n_dh += self.e_dh.norm()
+            self.n_dw += self.e_dw.norm()
+        else:
+            self.n_dh += 2 * U * ((V + 64) * (G.abs() @ w.abs())).norm()
+            self.n_dw += 2 * U * ((n + 64) * (G.abs().T @ h.abs())).norm()
+
+    def check(self, loss, lse, dh, dw, base=None):
+        if lse is not None:
+            within(lse, self.lse, self.e_lse, "lse")
+        if loss is not None:
+            within(loss, self.loss, self.e_loss, "loss")
+        if dh is not None:
+            within(dh, self.dh, self.e_dh, "dh")
+            assert float((dh.double() - self.dh).norm()) <= float(self.n_dh), "dh's norm"
+        if dw is not None:
+            b = 0.0 if base is None else base.double()
+            out = B16 if dw.dtype == torch.bfloat16 else U
+            more = 0.0 if base is None else 2 * out * b.abs()
+            within(dw, self.dw + b, self.e_dw + more, "dw")
+            if base is None:
+                assert float((dw.double() - self.dw).norm()) <= float(self.n_dw), "dw's norm"
+
+
+def ce(A, h, w, target, gl=None, grads=True, ws=None, stream=None):
+    n = h.shape[0]
+    loss, lse = torch.full((n,), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")
+    acc = torch.zeros(2, dtype=torch.float64, device="cuda")
+    A.adadsf_head_loss(h, w, target, loss, lse, acc=acc, ws=ws, stream=stream)
+    dh = dw = None
+    if grads:
+        dh, dw = torch.full_like(h, 7.0), torch.full_like(w, 7.0)
+        A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_h=dh, grad_w=dw, ws=ws, stream=stream)
+    return loss, lse, acc, dh, dw
+
+
+HEADS = [(1, 64, 100, "bf16"), (3, 8, 1, "bf16"), (24, 768, 5003, "bf16"), (130, 200, 257, "bf16"), (257, 520, 1000, "bf16"),
+         (300, 768, 1280, "bf16"), (700, 264, 255, "bf16"), (9000, 64, 12001, "bf16"),
+         (1, 4, 1, "f32"), (5, 132, 130, "f32"), (77, 512, 3001, "f32"), (515, 100, 777, "f32"), (9000, 32, 6002, "f32")]
+
+
+@pytest.mark.parametrize("n,d,V,dtype", HEADS)
+def test_head_loss(A, n, d, V, dtype):
+    """Sizes on both sides of tiles, boxes and k blocks; many row tiles and several pieces of the classes in the last of
+    either type. Twice the same bits."""
+    h, w, target, gl = head_inputs(n, d, V, dtype)
+    want, used = want_of(target, V)
+    ref = Ref(h, w, want, used, torch.zeros(n, dtype=torch.float64, device="cuda"), gl, 1.0, 1)
+    loss, lse, acc, dh, dw = ce(A, h, w, target, gl)
+    ref.check(loss, lse, dh, dw)
+    assert float(acc[1]) == int(used.sum())
+    assert float(acc[0]) == pytest.approx(float(loss.double().sum()), rel=1e-12, abs=1e-12)
+    assert (loss[~used] == 0).all() and (lse[~used] == 0).all() and (dh[~used] == 0).all()
+    again = ce(A, h, w, target, gl)
+    for x, y in zip((loss, lse, dh, dw), (again[0], again[1], again[3], again[4])):
+        assert torch.equal(x, y)
+
+
+def distill_inputs(n, d, V, k, dtype, seed=1):
+    h, w, target, gl = head_inputs(n, d, V, dtype, seed)
+    g = gen(n * k + V)
+    idx = torch.randint(0, V, (n, k), generator=g, device="cuda", dtype=torch.int32)   # the same class twice now and then
+    logit = randn(g, n, k, std=3.0)
+    gone = torch.rand(n, k, generator=g, device="cuda") < 0.2
+    idx[gone] = -1
+    logit[torch.rand(n, k, generator=g, device="cuda") < 0.05] = -math.inf
+    idx[target < 0] = -1
+    logit[gone] = math.nan                                                             # of slots not in use
+    return h, w, idx, logit, gl
+
+
+def distill(A, h, w, idx, logit, temp, gl, ws=None):
+    n = h.shape[0]
+    loss, lse = torch.full((n,), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")
+    A.adadsf_distill_loss(h, w, idx, logit, temp, loss, lse, ws=ws)
+    dh, dw = torch.full_like(h, 7.0), torch.full_like(w, 7.0)
+    A.adadsf_distill_loss_backward(h, w, idx, logit, lse, temp, grad_loss=gl, grad_h=dh, grad_w=dw, ws=ws)
+    return loss, lse, dh, dw
+
+
+@pytest.mark.parametrize("n,d,V,k,temp,dtype", [(1, 64, 100, 1, 1.0, "bf16"), (40, 128, 300, 7, 2.0, "bf16"),
+                                                (300, 520, 1000, 64, 0.7, "bf16"), (33, 64, 70, 1024, 1.0, "bf16"),
+                                                (9000, 64, 11000, 20, 4.0, "bf16"), (5, 132, 130, 3, 1.0, "f32"),
+                                                (200, 256, 3001, 129, 2.0, "f32"), (9000, 32, 6002, 5, 1.0, "f32")])
+def test_distill_loss(A, n, d, V, k, temp, dtype):
+    h, w, idx, logit, gl = distill_inputs(n, d, V, k, dtype)
+    want, used, ent = teacher_want(idx, logit, V, temp)
+    ref = Ref(h, w, want, used, ent, gl, temp, k)
+    got = distill(A, h, w, idx, logit, temp, gl)
+    ref.check(*got)
+    again = distill(A, h, w, idx, logit, temp, gl)
+    for x, y in zip(got, again):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_distill_of_one_class_is_cross_entropy(A, dtype):
+    """One slot at temperature 1: weight 1, entropy 0; the same products and sums."""
+    h, w, target, gl = head_inputs(70, 128, 500, dtype)
+    loss, lse, _, dh, dw = ce(A, h, w, target, gl)
+    logit = randn(gen(3), 70, 1)
+    got = distill(A, h, w, target[:, None].contiguous(), logit, 1.0, gl)
+    for x, y in zip(got, (loss, lse, dh, dw)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_without_target_reach_nothing(A, dtype):
+    """Infinities and NaN in rows without a target; the others as without them, bit for bit."""
+    h, w, target, gl = head_inputs(140, 128, 700, dtype)
+    clean = ce(A, h, w, target, gl)
+    dirty = h.clone()
+    dirty[target < 0] = torch.tensor([math.nan, math.inf, -math.inf, 1e30], device="cuda", dtype=h.dtype).repeat(32)
+    gl2 = torch.where(target < 0, math.nan, gl)
+    got = ce(A, dirty, w, target, gl2)
+    for x, y in zip(got, clean):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_row_has_a_target(A, dtype):
+    h, w, target, gl = head_inputs(300, 64, 400, dtype)
+    loss, lse, acc, dh, dw = ce(A, h, w, torch.full_like(target, -100), gl)
+    for x in (loss, lse, acc, dh, dw):
+        assert (x == 0).all()
+    none = ce(A, h[:0], w, target[:0], gl[:0])
+    assert (none[4] == 0).all() and (none[2] == 0).all()
+
+
+def test_classes_out_of_range(A):
+    h, w, target, gl = head_inputs(50, 64, 400, "bf16")
+    ws = A.workspace(A.adadsf_head_workspace_size(50, 64, 400, h.dtype, 4))
+    bad = target.clone()
+    bad[7] = 400
+    got = ce(A, h, w, bad, gl, ws=ws)
+    assert A.adadsf_sync_check(ws) == A.ERR_INVALID_ARG
+    bad[7] = -1
+    for x, y in zip(got, ce(A, h, w, bad, gl, ws=ws)):
+        assert torch.equal(x, y)
+    assert A.adadsf_sync_check(ws) == A.OK
+    _, _, idx, logit, _ = distill_inputs(50, 64, 400, 4, "bf16")
+    idx[9] = torch.tensor([400, 2 ** 31 - 1, 3, -5], device="cuda", dtype=torch.int32)
+    logit[9] = 1.0
+    got = distill(A, h, w, idx, logit, 1.0, gl, ws=ws)
+    assert A.adadsf_sync_check(ws) == A.ERR_INVALID_ARG
+    idx[9, :2] = -1
+    for x, y in zip(got, distill(A, h, w, idx, logit, 1.0, gl, ws=ws)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("n,d,V,dtype", [(300, 128, 700, "bf16"), (9000, 64, 12001, "bf16"), (200, 64, 300, "f32")])
+def test_head_gradients_apart_and_added(A, n, d, V, dtype):
+    """Each gradient by itself is the pair's; the head's added to what is there; no weights are weights of one."""
+    h, w, target, gl = head_inputs(n, d, V, dtype)
+    loss, lse, _, dh, dw = ce(A, h, w, target, gl)
+    one = torch.full_like(h, 7.0)
+    A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_h=one)
+    assert torch.equal(one, dh)
+    two = torch.full_like(w, 7.0)
+    A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_w=two)
+    assert torch.equal(two, dw)
+    want, used = want_of(target, V)
+    zero = torch.zeros(n, dtype=torch.float64, device="cuda")
+    ref = Ref(h, w, want, used, zero, gl, 1.0, 1)
+    base = randn(gen(5), V, d, std=0.2).to(h.dtype)
+    two.copy_(base)
+    A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_w=two, accumulate_w=True)
+    ref.check(None, None, None, two, base=base)
+    A.adadsf_head_loss_backward(h, w, target, lse, grad_h=one, grad_w=two)
+    Ref(h, w, want, used, zero, None, 1.0, 1).check(None, None, one, two)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_wide_logits(A, dtype):
+    """Logits of some thousands: no overflow, a loss of their size, gradients of single classes."""
+    h, w, target, gl = head_inputs(60, 128, 900, dtype, std=1500.0)
+    want, used = want_of(target, 900)
+    ref = Ref(h, w, want, used, torch.zeros(60, dtype=torch.float64, device="cuda"), gl, 1.0, 1)
+    loss, lse, _, dh, dw = ce(A, h, w, target, gl)
+    assert float(ref.lse.max()) > 1000
+    within(lse, ref.lse, ref.e_lse, "lse")
+    within(loss, ref.loss, ref.e_loss, "loss")
+    assert torch.isfinite(dh).all() and torch.isfinite(dw).all()
+
+
+def test_head_gradient_is_the_losses_difference(A):
+    """Against differences of the 64-bit loss, and the kernel against the same formula (fp32)."""
+    n, d, V = 6, 16, 40
+    h, w, target, gl = head_inputs(n, d, V, "f32")
+    idx = torch.randint(0, V, (n, 5), generator=gen(1), device="cuda", dtype=torch.int32)
+    logit, temp = randn(gen(2), n, 5), 1.7
+    for form in ("ce", "distill"):
+        if form == "ce":
+            want, used = want_of(target, V)
+            ent, t = torch.zeros(n, dtype=torch.float64, device="cuda"), 1.0
+            _, _, _, dh, dw = ce(A, h, w, target, gl)
+        else:
+            want, used, ent = teacher_want(idx, logit, V, temp)
+            t = temp
+            _, _, dh, dw = distill(A, h, w, idx, logit, temp, gl)
+
+        def total(hh, ww):
+            z = hh @ ww.T / t
+            row = t * t * (ent + want.sum(-1) * torch.logsumexp(z, -1) - (want * z).sum(-1))
+            return float((torch.where(used, row, 0.0) * gl.double()).sum())
+
+        for x, grad, other in ((h, dh, w), (w, dw, h)):
+            for i, j in ((0, 0), (3, 7), (5, 15)):
+                step = torch.zeros_like(x, dtype=torch.float64)
+                step[i, j] = 1e-4
+                xd, od = x.double(), other.double()
+                hi = total(xd + step, od) if x is h else total(od, xd + step)
+                lo = total(xd - step, od) if x is h else total(od, xd - step)
+                # differences: 1e-8 of the third derivative, and 1e-15 of a loss of tens over 1e-4
+                assert (hi - lo) / 2e-4 == pytest.approx(float(grad[i, j]), rel=2e-5, abs=2e-6)
+
+
+def test_head_captured(A):
+    """A forward and backward call in a graph, replayed on other inputs in the same places; a second graph on the same
+    workspace behind it; calls on another stream."""
+    n, d, V = 200, 128, 3000
+    ws = A.workspace(A.adadsf_head_workspace_size(9000, 64, 12001, torch.bfloat16, 4))
+    h, w, target, gl = head_inputs(n, d, V, "bf16")
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+
+    def step():
+        A.adadsf_head_loss(h, w, target, loss, lse, ws=ws)
+        A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_h=dh, grad_w=dw, ws=ws)
+
+    big = head_inputs(1000, 64, 5000, "bf16", seed=8)
+    big_out = [torch.empty(1000, device="cuda"), torch.empty(1000, device="cuda")]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        A.adadsf_head_loss(big[0], big[1], big[2], *big_out, ws=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0]):
+        step()
+    with torch.cuda.graph(graphs[1]):
+        A.adadsf_head_loss(big[0], big[1], big[2], *big_out, ws=ws)
+    for seed in (3, 4):
+        for dst, src in zip((h, w, target, gl), head_inputs(n, d, V, "bf16", seed=seed)):
+            dst.copy_(src)
+        graphs[0].replay()
+        graphs[1].replay()
+        graphs[0].replay()
+        got = [x.clone() for x in (loss, lse, dh, dw)]
+        want = ce(A, h, w, target, gl)
+        for x, y in zip(got, (want[0], want[1], want[3], want[4])):
+            assert torch.equal(x, y)
+        assert torch.equal(big_out[0], ce(A, *big[:3], grads=False)[0])
+
+
+# ------------------------------------------------------------------ norms
+def norm_inputs(n, d, dtype, rms, res):
+    g = gen(n * 7 + d)
+    x = randn(g, n, d) * torch.exp(randn(g, n, 1, std=0.5)) + randn(g, 1, d, std=0.5)
+    x = x.to(DT[dtype])
+    w = (1 + randn(g, d, std=0.2)).to(x.dtype)
+    b = None if rms else randn(g, d, std=0.2).to(x.dtype)
+    dy = randn(g, n, d).to(x.dtype)
+    add = randn(g, n, d).to(x.dtype) if res else None
+    return x, w, b, dy, add
+
+
+def norm(A, x, w, b, dy, add, eps=1e-5, ws=None, dw=None, db=None, accumulate=False):
+    n, d = x.shape
+    y, dx = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    mean = None if b is None else torch.full((n,), 7.0, device="cuda")
+    rstd = torch.full((n,), 7.0, device="cuda")
+    dw = torch.full((d,), 7.0, device="cuda") if dw is None else dw
+    db = None if b is None else torch.full((d,), 7.0, device="cuda") if db is None else db
+    A.adadsf_norm_forward(x, w, b, y, eps, mean, rstd)
+    A.adadsf_norm_backward(dy, x, w, rstd, dx, mean=mean, add=add, grad_w=dw, grad_b=db, accumulate=accumulate, ws=ws)
+    return y, mean, rstd, dx, dw, db
+
+
+def norm_check(x, w, b, dy, add, got, eps=1e-5, base=(0.0, 0.0)):
+    y, mean, rstd, dx, dw, db = got
+    out = B16 if x.dtype == torch.bfloat16 else U
+    xr = x.double().requires_grad_(True)
+    n, d = x.shape
+    m = xr.mean(-1, keepdim=True) if b is not None else torch.zeros(n, 1, dtype=torch.float64, device="cuda")
+    c = xr - m
+    r = (c.square().mean(-1, keepdim=True) + eps) ** -0.5
+    xh = c * r
+    (ref_dx,) = torch.autograd.grad(xh, xr, dy.double() * w.double())
+    m, c, r, xh = (t.detach() for t in (m, c, r, xh))
+    # a thread adds at most 32 values, then 5 steps of a warp and 16 warps: 64 terms' roundings
+    s = 64 * 2 * U
+    e_m = s * x.double().abs().mean(-1, keepdim=True) if b is not None else torch.zeros_like(m)
+    e_r = (s + 4 * U) * r + e_m * r * r          # of rstd: its sum's, and what the mean's error adds
+    e_xh = e_m * r + c.abs() * e_r + 2 * U * (xh.abs() + x.double().abs() * r)
+    if mean is not None:
+        within(mean, m[:, 0], e_m[:, 0] + U * m[:, 0].abs(), "mean")
+    within(rstd, r[:, 0], e_r[:, 0], "rstd")
+    ref = xh * w.double() + (0.0 if b is None else b.double())
+    within(y, ref, out * ref.abs() + (1 + out) * (w.double().abs() * e_xh + 2 * U * (ref.abs() + (xh * w.double()).abs())), "y")
+    a = dy.double() * w.double()
+    c2 = (a * xh).mean(-1, keepdim=True)
+    e_c1 = s * a.abs().mean(-1, keepdim=True)
+    e_c2 = s * (a * xh).abs().mean(-1, keepdim=True) + (a.abs() * e_xh).mean(-1, keepdim=True)
+    e = r * (e_c1 + xh.abs() * e_c2 + e_xh * c2.abs() + 6 * U * (a.abs() + a.mean(-1, keepdim=True).abs() + (xh * c2).abs())) \
+        + e_r / r * ref_dx.abs()
+    if add is not None:
+        ref_dx = ref_dx + add.double()
+        e = e + 2 * U * (ref_dx.abs() + add.double().abs())
+    within(dx, ref_dx, (1 + out) * e + out * ref_dx.abs(), "dx")
+    # sums over the rows: at most as many steps as rows
+    ref_w = (dy.double() * xh).sum(0)
+    within(dw, ref_w + base[0], 2 * U * (n + 32) * (dy.double() * xh).abs().sum(0) + (dy.double().abs() * e_xh).sum(0)
+           + 2 * U * (ref_w + base[0]).abs() + 1e-30, "dw")
+    if db is not None:
+        ref_b = dy.double().sum(0)
+        within(db, ref_b + base[1], 2 * U * (n + 32) * dy.double().abs().sum(0) + 2 * U * (ref_b + base[1]).abs() + 1e-30, "db")
+
+
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("n,d,dtype", [(1, 8, "bf16"), (24, 768, "bf16"), (3, 256, "bf16"), (400, 264, "bf16"), (2000, 64, "bf16"),
+                                       (5000, 128, "bf16"), (700, 3584, "bf16"), (9, 4096, "bf16"), (310, 4104, "bf16"),
+                                       (5, 8192, "bf16"), (1, 4, "f32"), (2044, 512, "f32"), (33, 132, "f32"), (3000, 100, "f32"),
+                                       (10, 2048, "f32"), (311, 2052, "f32"), (7, 4100, "f32"), (309, 8192, "f32")])
+def test_norm(A, n, d, dtype, rms):
+    """Widths on both sides of every split over threads, few and many rows."""
+    for res in (False, True):
+        args = norm_inputs(n, d, dtype, rms, res)
+        got = norm(A, *args)
+        norm_check(*args, got)
+        for x, y in zip(got, norm(A, *args)):
+            assert x is None or torch.equal(x, y)
+
+
+def test_norm_in_place_and_added(A):
+    x, w, b, dy, add = norm_inputs(500, 768, "bf16", False, True)
+    y, mean, rstd, dx, dw, db = norm(A, x, w, b, dy, add)
+    x2, m2, r2 = x.clone(), torch.empty_like(mean), torch.empty_like(rstd)
+    A.adadsf_norm_forward(x2, w, b, x2, 1e-5, m2, r2)
+    assert torch.equal(x2, y) and torch.equal(m2, mean)
+    for which in (0, 1):
+        g, a = dy.clone(), add.clone()
+        A.adadsf_norm_backward(g, x, w, rstd, (g, a)[which], mean=mean, add=a)
+        assert torch.equal((g, a)[which], dx)
+    base_w, base_b = randn(gen(1), 768, std=30.0), randn(gen(2), 768, std=30.0)
+    got = norm(A, x, w, b, dy, add, dw=base_w.clone(), db=base_b.clone(), accumulate=True)
+    norm_check(x, w, b, dy, add, got, base=(base_w.double(), base_b.double()))
+    dw0, db0 = torch.full((768,), 7.0, device="cuda"), torch.full((768,), 7.0, device="cuda")
+    A.adadsf_norm_backward(dy[:0], x[:0], w, rstd[:0], dx[:0], mean=mean[:0], grad_w=dw0, grad_b=db0)
+    assert (dw0 == 0).all() and (db0 == 0).all()
+
+
+def test_norm_row_of_one_value(A):
+    """A constant row has no spread: rstd = eps^-1/2, xhat 0, and no gradient but what the formula gives."""
+    x, w, b, dy, _ = norm_inputs(40, 512, "f32", False, False)
+    x[7] = 2.0
+    x[8] = 0.0
+    got = norm(A, x, w, b, dy, None)
+    norm_check(x, w, b, dy, None, got)
+    assert torch.equal(got[0][7], b) and torch.equal(got[0][8], b)
+
+
+# ------------------------------------------------------------------ embedding
+def embed_check(A, ids, table, dy, scale, base=None, ws=None):
+    V, d = table.shape
+    out = B16 if table.dtype == torch.bfloat16 else U
+    used = (ids >= 0) & (ids < V)
+    y = torch.full_like(dy, 7.0)
+    A.adadsf_embed_forward(ids, table, y, scale=scale, ws=ws)
+    ref = torch.where(used[:, None], table.double()[ids.clamp(0, V - 1).long()] * scale, 0.0)
+    within(y, ref, (out + 4 * U) * ref.abs(), "y")
+    got = torch.full_like(table, 7.0) if base is None else base.clone()
+    A.adadsf_embed_backward(ids, dy, got, scale=scale, accumulate=base is not None, ws=ws)
+    at, rows = ids[used].long(), dy[used].double()
+    ref = torch.zeros(V, d, dtype=torch.float64, device="cuda").index_add_(0, at, rows)
+    size = torch.zeros_like(ref).index_add_(0, at, rows.abs())
+    count = torch.zeros(V, dtype=torch.float64, device="cuda").index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
+    ref, b = ref * scale, 0.0 if base is None else base.double()
+    err = abs(scale) * 2 * U * (count[:, None] + 2) * size + 4 * U * (ref.abs() + (b if base is None else b.abs()))
+    within(got, ref + b, (1 + out) * err + out * (ref + b).abs(), "dtable")
+    untouched = count == 0
+    if base is None:
+        assert (got[untouched] == 0).all()
+    else:
+        assert torch.equal(got[untouched], base[untouched])
+    again = torch.full_like(table, 3.0) if base is None else base.clone()
+    A.adadsf_embed_backward(ids, dy, again, scale=scale, accumulate=base is not None, ws=ws)
+    assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("n,V,d,dtype", [(1, 1, 8, "bf16"), (31, 50, 64, "bf16"), (33, 5, 264, "bf16"), (100, 50304, 768, "bf16"),
+                                         (4096, 1000, 64, "bf16"), (4097, 1000, 72, "bf16"), (20000, 300, 40, "bf16"),
+                                         (6000, 300000, 8, "bf16"), (700, 100, 8200, "bf16"), (2044, 3000, 512, "f32"),
+                                         (65, 2, 4, "f32"), (70000, 7, 4, "f32"), (5000, 513, 260, "f32")])
+def test_embed(A, n, V, d, dtype):
+    """Both sorts, one to three digits, ids that fill many runs, fewer ids than threads."""
+    g = gen(n + V)
+    table = randn(g, V, d).to(DT[dtype])
+    dy = randn(g, n, d).to(DT[dtype])
+    ids = (torch.rand(n, generator=g, device="cuda") ** 3 * V).to(torch.int32)
+    ids[torch.rand(n, generator=g, device="cuda") < 0.1] = -1
+    embed_check(A, ids, table, dy, 1.0)
+    embed_check(A, ids, table, dy, -2.5, base=randn(g, V, d).to(DT[dtype]))
+
+
+@pytest.mark.parametrize("n", [32, 64, 65, 3000, 9000])
+def test_embed_one_id_and_none(A, n):
+    g = gen(n)
+    table, dy = randn(g, 40, 64).to(torch.bfloat16), randn(g, n, 64).to(torch.bfloat16)
+    dy[1::2] = math.nan
+    ids = torch.full((n,), -1, device="cuda", dtype=torch.int32)
+    got = torch.full_like(table, 7.0)
+    A.adadsf_embed_backward(ids, dy, got)
+    assert (got == 0).all()                                # what padding's rows hold reaches nothing
+    ids[::2] = 39
+    embed_check(A, ids, table, torch.nan_to_num(dy), 1.0)
+    A.adadsf_embed_backward(ids, dy, got)
+    assert torch.isfinite(got).all()
+
+
+def test_embed_out_of_range(A):
+    g = gen(5)
+    table, dy = randn(g, 100, 64), randn(g, 5000, 64)
+    ws = A.workspace(A.adadsf_embed_backward_workspace_size(5000, 100, 64))
+    for n in (50, 5000):
+        ids = torch.randint(0, 100, (n,), generator=g, device="cuda", dtype=torch.int32)
+        ids[3], ids[4] = 100, 2 ** 31 - 1
+        got, y = torch.empty_like(table), torch.empty(n, 64, device="cuda")
+        A.adadsf_embed_backward(ids, dy[:n], got, ws=ws)
+        assert A.adadsf_sync_check(ws) == A.ERR_INVALID_ARG
+        A.adadsf_embed_forward(ids, table, y, ws=ws)
+        assert A.adadsf_sync_check(ws) == A.ERR_INVALID_ARG
+        assert (y[3:5] == 0).all()
+        ids[3:5] = -1
+        want = torch.empty_like(table)
+        A.adadsf_embed_backward(ids, dy[:n], want, ws=ws)
+        assert A.adadsf_sync_check(ws) == A.OK
+        assert torch.equal(got, want)
+
+
+def test_embed_backward_captured(A):
+    g = gen(6)
+    for n in (300, 6000):
+        table, dy = torch.empty(500, 64, device="cuda"), randn(g, n, 64)
+        ids = torch.randint(0, 500, (n,), generator=g, device="cuda", dtype=torch.int32)
+        ws = A.workspace(A.adadsf_embed_backward_workspace_size(n, 500, 64))
+        A.adadsf_embed_backward(ids, dy, table, ws=ws)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            A.adadsf_embed_backward(ids, dy, table, ws=ws)
+        ids.copy_(torch.randint(0, 500, (n,), generator=g, device="cuda", dtype=torch.int32))
+        graph.replay()
+        got = table.clone()
+        A.adadsf_embed_backward(ids, dy, table, ws=ws)
+        assert torch.equal(got, table)
