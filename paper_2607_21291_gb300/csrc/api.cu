@@ -1771,7 +1771,7 @@ adadsf_status check_head(int64_t n_rows, int d, int n_classes, int dtype, int to
 
 struct HeadLayout {
   HeadPlan plan;
-  size_t count, rows, target, cls, p, ent, picked, packed, rec, g[2], acc, total;
+  size_t count, rows, target, cls, p, ent, picked, packed, w_parts, rec, g[2], acc, total;
 };
 HeadLayout head_layout(int64_t n, int d, int V, int dtype, int k) {
   HeadLayout l;
@@ -1787,6 +1787,7 @@ HeadLayout head_layout(int64_t n, int d, int V, int dtype, int k) {
   l.ent = cv.take((size_t)n * 4);
   l.picked = cv.take((size_t)n * k * 4);
   l.packed = cv.take(l.plan.packed);
+  l.w_parts = cv.take(l.plan.w_parts);
   // the forward pass's records and the backward pass's buffers take turns
   Carver back = cv;
   l.rec = cv.take(l.plan.rec);
@@ -1827,6 +1828,10 @@ adadsf_status head_prepare(const HeadCall& c, void* ws, size_t ws_bytes, void* s
   a->rows = at<int32_t>(ws, l->rows);
   a->packed = at<void>(ws, l->packed);
   a->cap = l->plan.cap;
+  a->ld = l->plan.ld;
+  a->Vp = l->plan.Vp;
+  a->w_parts = at<void>(ws, l->w_parts);
+  a->g_ref = at<float>(ws, l->count) + 1;
   a->picked = at<float>(ws, l->picked);
   a->rec = at<float2>(ws, l->rec);
   a->G[0] = at<void>(ws, l->g[0]);
@@ -1849,7 +1854,7 @@ adadsf_status head_prepare(const HeadCall& c, void* ws, size_t ws_bytes, void* s
   return ADADSF_OK;
 }
 
-adadsf_status head_loss(const HeadCall& c, float* loss, float* lse, double* acc, void* ws, size_t ws_bytes, void* stream) {
+adadsf_status run_head_loss(const HeadCall& c, float* loss, float* lse, double* acc, void* ws, size_t ws_bytes, void* stream) {
   TRY(need_row(loss, "loss_dev", !acc || c.n == 0));
   TRY(need_row(lse, "lse_dev", c.n == 0));
   if (reinterpret_cast<uintptr_t>(acc) & 7u) return fail(ADADSF_ERR_INVALID_ARG, "acc_dev is not 8-byte aligned");
@@ -1865,7 +1870,7 @@ adadsf_status head_loss(const HeadCall& c, float* loss, float* lse, double* acc,
                 ((double)c.n * c.d + (double)c.V * c.d) * elem_size(c.dtype), CALL(head_forward(c.dtype, a, dev), "head loss"));
 }
 
-adadsf_status head_grad(const HeadCall& c, const float* lse, const float* grad_loss, void* grad_h, void* grad_w, int accumulate_w,
+adadsf_status run_head_grad(const HeadCall& c, const float* lse, const float* grad_loss, void* grad_h, void* grad_w, int accumulate_w,
                         void* ws, size_t ws_bytes, void* stream) {
   if (accumulate_w != 0 && accumulate_w != 1) return fail(ADADSF_ERR_INVALID_ARG, "accumulate_w must be 0 or 1");
   if (!grad_h && !grad_w) return fail(ADADSF_ERR_INVALID_ARG, "grad_h_dev and grad_w_dev are both NULL");
@@ -1914,7 +1919,7 @@ adadsf_status adadsf_head_loss(const void* h_dev, const void* w_head_dev, const 
   TRY(check_head(n_rows, d, n_classes, dtype, 1));
   TRY(need_row(target_dev, "target_dev", n_rows == 0));
   const HeadCall c = {h_dev, w_head_dev, target_dev, nullptr, nullptr, 1, 1.f, n_rows, d, n_classes, dtype};
-  return head_loss(c, loss_dev, lse_dev, acc_dev, ws, ws_bytes, stream);
+  return run_head_loss(c, loss_dev, lse_dev, acc_dev, ws, ws_bytes, stream);
 }
 
 adadsf_status adadsf_head_loss_backward(const void* h_dev, const void* w_head_dev, const int32_t* target_dev, int64_t n_rows,
@@ -1924,7 +1929,7 @@ adadsf_status adadsf_head_loss_backward(const void* h_dev, const void* w_head_de
   TRY(check_head(n_rows, d, n_classes, dtype, 1));
   TRY(need_row(target_dev, "target_dev", n_rows == 0));
   const HeadCall c = {h_dev, w_head_dev, target_dev, nullptr, nullptr, 1, 1.f, n_rows, d, n_classes, dtype};
-  return head_grad(c, lse_dev, grad_loss_dev, grad_h_dev, grad_w_dev, accumulate_w, ws, ws_bytes, stream);
+  return run_head_grad(c, lse_dev, grad_loss_dev, grad_h_dev, grad_w_dev, accumulate_w, ws, ws_bytes, stream);
 }
 
 adadsf_status adadsf_distill_loss(const void* h_dev, const void* w_head_dev, const int32_t* top_idx_dev,
@@ -1936,7 +1941,7 @@ adadsf_status adadsf_distill_loss(const void* h_dev, const void* w_head_dev, con
   TRY(need_row(top_idx_dev, "top_idx_dev", n_rows == 0));
   TRY(need_row(top_logit_dev, "top_logit_dev", n_rows == 0));
   const HeadCall c = {h_dev, w_head_dev, nullptr, top_idx_dev, top_logit_dev, top_k, temperature, n_rows, d, n_classes, dtype};
-  return head_loss(c, loss_dev, lse_dev, acc_dev, ws, ws_bytes, stream);
+  return run_head_loss(c, loss_dev, lse_dev, acc_dev, ws, ws_bytes, stream);
 }
 
 adadsf_status adadsf_distill_loss_backward(const void* h_dev, const void* w_head_dev, const int32_t* top_idx_dev,
@@ -1949,7 +1954,7 @@ adadsf_status adadsf_distill_loss_backward(const void* h_dev, const void* w_head
   TRY(need_row(top_idx_dev, "top_idx_dev", n_rows == 0));
   TRY(need_row(top_logit_dev, "top_logit_dev", n_rows == 0));
   const HeadCall c = {h_dev, w_head_dev, nullptr, top_idx_dev, top_logit_dev, top_k, temperature, n_rows, d, n_classes, dtype};
-  return head_grad(c, lse_dev, grad_loss_dev, grad_h_dev, grad_w_dev, accumulate_w, ws, ws_bytes, stream);
+  return run_head_grad(c, lse_dev, grad_loss_dev, grad_h_dev, grad_w_dev, accumulate_w, ws, ws_bytes, stream);
 }
 
 namespace {

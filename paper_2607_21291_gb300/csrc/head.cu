@@ -1,5 +1,5 @@
 // Losses at the LM head: targets, packing of the rows that have one, and what joins the
-// products of head_tc.cu and head_f32.cu (formulas in head.cuh).
+// products of head_tc.cu (formulas in head.cuh).
 #include <math.h>
 
 #include <algorithm>
@@ -73,29 +73,58 @@ constexpr int kPackThreads = 256;
 // targets by itself (no launch before it, no order between blocks). Rows without one get a loss, a
 // logarithm and a gradient of zero; what they hold is read by nobody. Packed rows past the last one, up to a
 // multiple of kHeadZeroPad, are zero: products over rows run that far.
+//
+// The copy is bf16 [cap][ld]; of fp32 features three parts (see next_part), each such a matrix, ld features with zeros behind
+// the d-th. Backward: the largest weight of a row's loss as well.
+__device__ __forceinline__ void put_row(const bf16* src, bf16* dst, int64_t, int d, int, int lane) {
+  for (int v = lane; v < d / 8; v += 32) reinterpret_cast<uint4*>(dst)[v] = reinterpret_cast<const uint4*>(src)[v];
+}
+// 4 features of fp32 into the parts, `part` elements apart.
+__device__ __forceinline__ void put4(const float4& f, bf16* dst, int64_t part) {
+  float x[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    uint2 u;
+    u.x = (uint32_t)__bfloat16_as_ushort(next_part(x[0], q == 2)) | (uint32_t)__bfloat16_as_ushort(next_part(x[1], q == 2)) << 16;
+    u.y = (uint32_t)__bfloat16_as_ushort(next_part(x[2], q == 2)) | (uint32_t)__bfloat16_as_ushort(next_part(x[3], q == 2)) << 16;
+    *reinterpret_cast<uint2*>(dst + q * part) = u;
+  }
+}
+__device__ __forceinline__ void put_row(const float* src, bf16* dst, int64_t part, int d, int ld, int lane) {
+  for (int v = lane; v < ld / 4; v += 32)
+    put4(v < d / 4 ? reinterpret_cast<const float4*>(src)[v] : make_float4(0.f, 0.f, 0.f, 0.f), dst + 4 * v, part);
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kPackThreads)
-    head_pack_kernel(const int32_t* target, int64_t n, int V, int64_t per_block, const T* h, int d, T* packed, int32_t* rows,
-                     int32_t* count, float* loss, float* lse, T* dh, int* err) {
+    head_pack_kernel(const int32_t* target, int64_t n, int V, int64_t per_block, const T* h, int d, bf16* packed, int64_t cap,
+                     int ld, int32_t* rows, int32_t* count, const float* g, float* g_ref, float* loss, float* lse, T* dh, int* err) {
   pdl_wait();
   pdl_trigger();
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
   constexpr int W = kPackThreads / 32;
   __shared__ int red[2][W];
   __shared__ int at[kPackThreads];
+  __shared__ float most[W];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t r0 = blockIdx.x * per_block, r1 = min(n, r0 + per_block);
   int before = 0, all = 0;
+  float top = 0.f;
+  const bool weigh = g && blockIdx.x == 0;
   for (int64_t i = tid; i < n; i += kPackThreads) {
     const int32_t t = target[i];
     const int in = t >= 0 && t < V;
     all += in;
     before += in && i < r0;
+    if (weigh && in) top = fmaxf(top, fabsf(g[i]));
   }
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   before = __reduce_add_sync(0xffffffffu, before);
   all = __reduce_add_sync(0xffffffffu, all);
   if (lane == 0) {
     red[0][warp] = before;
     red[1][warp] = all;
+    most[warp] = top;
   }
   __syncthreads();
   before = all = 0;
@@ -103,7 +132,13 @@ __global__ void __launch_bounds__(kPackThreads)
     before += red[0][i];
     all += red[1][i];
   }
-  if (blockIdx.x == 0 && tid == 0) *count = all;
+  if (blockIdx.x == 0 && tid == 0) {
+    *count = all;
+    if (g_ref) {
+      for (int i = 0; i < W; ++i) top = fmaxf(top, most[i]);
+      *g_ref = top > 0.f && top < INFINITY ? top : 1.f;
+    }
+  }
   const int nv = d / Elem<T>::kVec;
   const uint4 zero = make_uint4(0, 0, 0, 0);
   for (int64_t c = r0; c < r1; c += kPackThreads) {
@@ -129,10 +164,8 @@ __global__ void __launch_bounds__(kPackThreads)
     __syncthreads();
     const int in_chunk = (int)min((int64_t)kPackThreads, r1 - c);
     for (int i = warp; i < in_chunk; i += W) {
-      const uint4* src = reinterpret_cast<const uint4*>(h + (c + i) * d);
       if (at[i] >= 0) {
-        uint4* dst = reinterpret_cast<uint4*>(packed + (int64_t)at[i] * d);
-        for (int v = lane; v < nv; v += 32) dst[v] = src[v];
+        put_row(h + (c + i) * d, packed + (int64_t)at[i] * ld, cap * ld, d, ld, lane);
       } else if (dh) {
         uint4* dst = reinterpret_cast<uint4*>(dh + (c + i) * d);
         for (int v = lane; v < nv; v += 32) dst[v] = zero;
@@ -140,9 +173,25 @@ __global__ void __launch_bounds__(kPackThreads)
     }
   }
   const int tail = (kHeadZeroPad - all % kHeadZeroPad) % kHeadZeroPad;
-  for (int i = (int)((blockIdx.x + (int64_t)gridDim.x * warp)); i < tail; i += (int)gridDim.x * W) {
-    uint4* dst = reinterpret_cast<uint4*>(packed + ((int64_t)all + i) * d);
-    for (int v = lane; v < nv; v += 32) dst[v] = zero;
+  for (int i = (int)(blockIdx.x + gridDim.x * warp); i < tail; i += (int)gridDim.x * W) {
+    for (int q = 0; q < PARTS; ++q) {
+      uint4* dst = reinterpret_cast<uint4*>(packed + (q * cap + all + i) * ld);
+      for (int v = lane; v < ld / 8; v += 32) dst[v] = zero;
+    }
+  }
+}
+
+// The head's parts (fp32): [3][Vp][ld], zeros behind the d-th feature and the last class.
+__global__ void __launch_bounds__(256) head_split_kernel(const float* w, int V, int d, int Vp, int ld, bf16* parts) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = (int64_t)Vp * (ld / 4), part = (int64_t)Vp * ld;
+  const int nv = ld / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / nv;
+    const int c = (int)(i - r * nv) * 4;
+    const bool in = r < V && c < d;
+    put4(in ? *reinterpret_cast<const float4*>(w + r * d + c) : make_float4(0.f, 0.f, 0.f, 0.f), parts + r * ld + c, part);
   }
 }
 
@@ -225,9 +274,11 @@ __global__ void __launch_bounds__(1024) head_sum_kernel(const float* loss, int64
 // The hidden states' gradient: a packed row's partial sums added in order, rounded once, to its row.
 template <typename T>
 __global__ void __launch_bounds__(256)
-    head_finish_kernel(const float* acc, const int32_t* count, const int32_t* rows, int64_t cap, int d, int splits, T* dh) {
+    head_finish_kernel(const float* acc, const int32_t* count, const int32_t* rows, int64_t cap, int d, int splits,
+                       const float* g_ref, float temp, T* dh) {
   pdl_wait();
   pdl_trigger();
+  const float scale = *g_ref * temp;
   constexpr int V = Elem<T>::kVec;
   const int nv = d / V;
   const int64_t n = (int64_t)*count * nv, stride = cap * d;
@@ -247,6 +298,8 @@ __global__ void __launch_bounds__(256)
         for (int l = 0; l < 4; ++l) s[j + l] += f[l];
       }
     }
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] *= scale;
     store_vec(dh + (int64_t)rows[m] * d + c, s);
   }
 }
@@ -254,10 +307,15 @@ __global__ void __launch_bounds__(256)
 template <typename T>
 cudaError_t pack(const Head& a, bool backward, const Dev& dev) {
   const int64_t per = std::max<int64_t>(8, (a.n + 511) / 512);
-  return launch_pdl(head_pack_kernel<T>, dim3((unsigned)((a.n + per - 1) / per)), dim3(kPackThreads), 0, dev.stream, a.target,
-                    a.n, a.V, per, static_cast<const T*>(a.h), a.d, static_cast<T*>(a.packed), a.rows, a.count,
-                    backward ? (float*)nullptr : a.loss, backward ? (float*)nullptr : a.lse,
-                    backward ? static_cast<T*>(a.dh) : (T*)nullptr, dev.err);
+  cudaError_t e = launch_pdl(head_pack_kernel<T>, dim3((unsigned)((a.n + per - 1) / per)), dim3(kPackThreads), 0, dev.stream,
+                             a.target, a.n, a.V, per, static_cast<const T*>(a.h), a.d, static_cast<bf16*>(a.packed), a.cap, a.ld,
+                             a.rows, a.count, backward ? a.g : (const float*)nullptr, backward ? a.g_ref : (float*)nullptr,
+                             backward ? (float*)nullptr : a.loss, backward ? (float*)nullptr : a.lse,
+                             backward ? static_cast<T*>(a.dh) : (T*)nullptr, dev.err);
+  if (e != cudaSuccess || sizeof(T) == 2) return e;
+  const int64_t pieces = (int64_t)a.Vp * (a.ld / 4);
+  return launch_pdl(head_split_kernel, dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 8 * dev.num_sms)), dim3(256), 0,
+                    dev.stream, static_cast<const float*>(a.w), a.V, a.d, a.Vp, a.ld, static_cast<bf16*>(a.w_parts));
 }
 
 }  // namespace
@@ -265,11 +323,13 @@ cudaError_t pack(const Head& a, bool backward, const Dev& dev) {
 // Classes a piece: its G in both buffers is to stay in the L2 with what else is read, but whole where
 // few rows make it small.
 HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
-  const int64_t es = dtype == kBF16 ? 2 : 4, tile = dtype == kBF16 ? 256 : 128;
+  const int64_t parts = dtype == kBF16 ? 1 : 3, tile = 256;
   HeadPlan q;
   q.cap = (n + kHeadRowPad - 1) / kHeadRowPad * kHeadRowPad;
+  q.ld = (d + 7) / 8 * 8;
+  q.Vp = (int)(((int64_t)V + 63) / 64 * 64);
   const int64_t padded = ((int64_t)V + 255) / 256 * 256;
-  int64_t piece = std::max<int64_t>(2048, (96ll << 20) / std::max<int64_t>(1, q.cap * es));
+  int64_t piece = std::max<int64_t>(2048, (96ll << 20) / std::max<int64_t>(1, q.cap * 2 * parts));
   const int64_t pieces = (padded + piece - 1) / piece;
   piece = ((padded + pieces - 1) / pieces + 255) / 256 * 256;
   q.piece = (int)piece;
@@ -280,9 +340,10 @@ HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
   int64_t splits = std::max<int64_t>(1, (piece + other / 2) / other);
   splits = std::min<int64_t>(splits, std::max<int64_t>(1, 1024 / tiles));
   q.splits = (int)std::min<int64_t>(splits, 64);
-  q.packed = (size_t)(q.cap * d * es);
+  q.packed = (size_t)(parts * q.cap * q.ld * 2);
+  q.w_parts = dtype == kBF16 ? 0 : (size_t)(parts * q.Vp * q.ld * 2);
   q.rec = (size_t)(padded / 128 * q.cap * 8);
-  q.g = (size_t)(q.cap * piece * es);
+  q.g = (size_t)(parts * q.cap * piece * 2);
   q.acc = (size_t)(q.splits * q.cap * d * 4);
   return q;
 }
@@ -295,7 +356,7 @@ cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int 
 
 cudaError_t head_forward(int dtype, const Head& a, const Dev& dev) {
   cudaError_t e = dtype == kBF16 ? pack<bf16>(a, false, dev) : pack<float>(a, false, dev);
-  if (e == cudaSuccess) e = dtype == kBF16 ? head_tc_stats(a, dev) : head_f32_stats(a, dev);
+  if (e == cudaSuccess) e = head_stats(dtype, a, dev);
   if (e != cudaSuccess) return e;
   const int blocks = (int)std::min<int64_t>((a.n + 31) / 32, 2 * dev.num_sms);
   e = launch_pdl(head_merge_kernel, dim3((unsigned)blocks), dim3(32 * kMergeWarps), 0, dev.stream, (const int32_t*)a.count,
@@ -307,21 +368,22 @@ cudaError_t head_forward(int dtype, const Head& a, const Dev& dev) {
 
 cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev) {
   cudaError_t e = dtype == kBF16 ? pack<bf16>(a, true, dev) : pack<float>(a, true, dev);
-  const auto grad = dtype == kBF16 ? head_tc_grad : head_f32_grad;
   // launch j: G of piece j, gradients of piece j - 1
   for (int j = 0; j <= plan.pieces && e == cudaSuccess; ++j) {
     const int64_t v = (int64_t)j * plan.piece, before = v - plan.piece;
     const int n_g = j < plan.pieces ? (int)std::min<int64_t>(plan.piece, a.V - v) : 0;
     const int n_d = j > 0 ? (int)std::min<int64_t>(plan.piece, a.V - before) : 0;
-    e = grad(a, j & 1, v, n_g, before, n_d, j == 1, dev);
+    e = head_grad(dtype, a, j & 1, v, n_g, before, n_d, j == 1, dev);
   }
   if (e != cudaSuccess || !a.dh) return e;
   const int blocks = (int)std::min<int64_t>((a.n * a.d / 4 + 255) / 256, 8 * dev.num_sms);
   if (dtype == kBF16)
     return launch_pdl(head_finish_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, dev.stream, (const float*)a.dh_acc,
-                      (const int32_t*)a.count, (const int32_t*)a.rows, a.cap, a.d, a.splits, static_cast<bf16*>(a.dh));
+                      (const int32_t*)a.count, (const int32_t*)a.rows, a.cap, a.d, a.splits, (const float*)a.g_ref,
+                      a.temp, static_cast<bf16*>(a.dh));
   return launch_pdl(head_finish_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, dev.stream, (const float*)a.dh_acc,
-                    (const int32_t*)a.count, (const int32_t*)a.rows, a.cap, a.d, a.splits, static_cast<float*>(a.dh));
+                    (const int32_t*)a.count, (const int32_t*)a.rows, a.cap, a.d, a.splits, (const float*)a.g_ref,
+                    a.temp, static_cast<float*>(a.dh));
 }
 
 }  // namespace adadsf

@@ -1,4 +1,4 @@
-// Shared pieces of the losses at the LM head (head.cu, head_tc.cu, head_f32.cu).
+// Shared pieces of the losses at the LM head (head.cu, head_tc.cu).
 //
 // A row's targets are k classes with weights p, classes ascending (distillation) or one class
 // of weight 1 (cross entropy). With z = l / T, l = h W^T, q = softmax(z) over all classes:
@@ -16,6 +16,15 @@ namespace adadsf {
 
 constexpr int kHeadRowPad = 256;   // packed buffers hold whole tiles of rows
 constexpr int kHeadZeroPad = 64;   // rows past the last packed one, up to a multiple of this, are zero in the packed copy
+
+// x as the sum of three bf16 numbers: the next one, and in x what it leaves. Numbers past bf16's largest leave the
+// rest to the next part; NaN stays NaN in the last.
+__device__ __forceinline__ bf16 next_part(float& x, bool last) {
+  constexpr float kMost = 3.3895313892515355e38f;
+  const bf16 h = __float2bfloat16_rn(last ? x : fminf(fmaxf(x, -kMost), kMost));
+  x -= __bfloat162float(h);
+  return h;
+}
 
 // First of a row's k ascending classes that is not below c0.
 __device__ __forceinline__ int first_class(const int32_t* cls, int k, int c0) {

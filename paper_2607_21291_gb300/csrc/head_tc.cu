@@ -1,4 +1,4 @@
-// Products of the losses at the LM head on the 5th-generation tensor cores (bf16).
+// Products of the losses at the LM head on the 5th-generation tensor cores.
 //
 // One persistent kernel, a CTA pair a tile of 256 x 256 (tcgen05.mma cta_group::2, fp32
 // accumulators in TMEM, two of them, so that one tile's epilogue runs under the next one's
@@ -14,8 +14,12 @@
 // has one order: results are the same in every run.
 // Operands lie as they are: rows x features, classes x features and rows x classes are read
 // K-major or MN-major (64 of M or N a 128-byte line), by descriptor, from the same TMA boxes of 64 x 64.
-// G is rounded to bf16 because the tensor cores take it so; its roundings are independent, and
-// the gradients that they enter are rounded to bf16 as well.
+// G is rounded to bf16 because the tensor cores take it so; rows' weights enter it as shares of the largest one,
+// so that equal weights leave its roundings independent (a common factor of 1 / 3580 rounded every target's
+// entry the same way: gradients 2.8e-3 off, now NEWERR), and the gradients that it enters are rounded to bf16 as well.
+//
+// fp32: every operand is three bf16 numbers whose sum it is (8 bits each), and a product of two is six of their nine
+// products, the least first, in the same accumulators; the three that are left out are below 2^-24 of it.
 //   warp 0     TMA: A and B tiles of 64 k, 6 stages of 32 KB (both CTAs)
 //   warp 1     TMEM, MMA issue (one thread of the even CTA)
 //   warps 2-9  epilogue (two per TMEM lane quarter, 128 columns each)
@@ -23,6 +27,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "head.cuh"
 
@@ -44,11 +49,16 @@ constexpr uint32_t kHtDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;   // groups
 
 enum { kStats = 0, kG = 1, kDH = 2, kDW = 3 };
 
+// Parts of A and B of each product of an fp32 operand's parts.
+constexpr int kHtTerms = 6;
+__device__ __forceinline__ int part_a(int term) { return (0x001102 >> (4 * term)) & 3; }   // 2 0 1 1 0 0
+__device__ __forceinline__ int part_b(int term) { return (0x010120 >> (4 * term)) & 3; }   // 0 2 1 0 1 0
+
 struct HtDev {
   const int32_t* count;      // packed rows
   const int32_t* rows;       // their rows
-  int64_t cap;               // rows of the packed buffers
-  int d, V;
+  int64_t cap;               // rows of the packed buffers, and of G
+  int d, V, Vp;              // Vp: rows of a part of the head
   float inv_t;
   const int32_t* cls;        // targets by row, [k]
   const float* p;            // their weights (null: 1)
@@ -59,6 +69,7 @@ struct HtDev {
   // gradients
   const float* lse;          // by row
   const float* g;            // by row (null: 1)
+  const float* g_ref;        // the largest
   float temp;
   int v_g, n_g;              // G tiles: first class, class tiles (0: none)
   int v_d, kb_d;             // dH and dW: first class of the piece, its blocks of 64 classes (0: none)
@@ -66,7 +77,7 @@ struct HtDev {
   int ld_g;
   bf16* G;                   // the piece of the G tiles
   float* acc;                // [splits][cap][d]
-  bf16* dw;
+  void* dw;
   int* err;
   unsigned long long timeout_ns;
 };
@@ -211,66 +222,94 @@ __device__ __forceinline__ void stats_tile(const HtDev& p, const Tile& ti, int m
   if (live) p.rec[(int64_t)(ti.nb * 2 + half) * p.cap + m] = make_float2(top, sum);
 }
 
+template <bool F32>
 __device__ __forceinline__ void g_tile(const HtDev& p, const Tile& ti, int m, int half, bool live, uint32_t tacc, Walk& w,
                                        uint8_t* out, int lane) {
   constexpr float kLog2e = 1.4426950408889634f;
   const int64_t row = live ? p.rows[m] : 0;
   const float lse = live ? p.lse[row] : 0.f;
-  const float g = live ? (p.g ? p.g[row] : 1.f) * p.temp : 0.f;
+  const float g = live ? (p.g ? p.g[row] : 1.f) / *p.g_ref : 0.f;
   const float2 it2 = make_float2(p.inv_t, p.inv_t), ml2 = make_float2(-lse, -lse), e2 = make_float2(kLog2e, kLog2e);
   const float2 g2 = make_float2(g, g);
   const int m0 = m - lane;
   bf16* dst = p.G + (int64_t)m0 * p.ld_g + ti.nb * kHtTile + half * 128;
 #pragma unroll 1
-  for (int c64 = 0; c64 < 2; ++c64) {
+  for (int c32 = 0; c32 < 4; ++c32) {
+    const int cb = p.v_g + ti.nb * kHtTile + half * 128 + c32 * 32;
+    uint32_t r[32];
+    tmem_ld32(tacc + c32 * 32, r);
+    tmem_ld_wait();
+    const bool edge = cb + 32 > p.V;
+    float f[32];
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      const float2 z = __ffma2_rn(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), it2, ml2);
+      const float2 t = __fmul2_rn(z, e2);
+      const float2 v = __fmul2_rn(make_float2(ex2_approx(t.x), ex2_approx(t.y)), g2);
+      f[i] = v.x;
+      f[i + 1] = v.y;
+    }
+    if (edge || !live) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (!live || cb + i >= p.V) f[i] = 0.f;
+    }
+    if (!F32) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(out + out_at(lane, (c32 & 1) * 4 + q)) = pack16(f + 8 * q, bf16());
+    }
+    while (__any_sync(0xffffffffu, w.next < cb + 32)) {
+      const int at = (w.next - cb) & 31;
+      const float l = pick32(r, at);
+      if (w.next < cb + 32) {
+        const int c = w.next;
+        float want = 0.f;
+        do {   // the same class twice: both weights
+          want += p.p ? p.p[row * p.k + w.j] : 1.f;
+          w.step();
+        } while (w.next == c);
+        const float v = (ex2_approx(fmaf(l, p.inv_t, -lse) * kLog2e) - want) * g;
+        if (F32) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i == at) f[i] = v;
+        } else {
+          *reinterpret_cast<bf16*>(out + out_at(lane, (c32 & 1) * 4 + (at >> 3)) + (at & 7) * 2) = __float2bfloat16_rn(v);
+        }
+      }
+    }
+    if (F32) {
 #pragma unroll 1
-    for (int h32 = 0; h32 < 2; ++h32) {
-      const int cb = p.v_g + ti.nb * kHtTile + half * 128 + c64 * 64 + h32 * 32;
-      uint32_t r[32];
-      tmem_ld32(tacc + c64 * 64 + h32 * 32, r);
-      tmem_ld_wait();
-      const bool edge = cb + 32 > p.V;
+      for (int part = 0; part < 3; ++part) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float f[8];
+        for (int q = 0; q < 4; ++q) {
+          uint32_t v[4];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-          const float2 z = __ffma2_rn(make_float2(__uint_as_float(r[8 * q + i]), __uint_as_float(r[8 * q + i + 1])), it2, ml2);
-          const float2 t = __fmul2_rn(z, e2);
-          const float2 v = __fmul2_rn(make_float2(ex2_approx(t.x), ex2_approx(t.y)), g2);
-          f[i] = v.x;
-          f[i + 1] = v.y;
+          for (int i = 0; i < 4; ++i) {
+            const bf16 lo = next_part(f[8 * q + 2 * i], part == 2), hi = next_part(f[8 * q + 2 * i + 1], part == 2);
+            v[i] = (uint32_t)__bfloat16_as_ushort(lo) | (uint32_t)__bfloat16_as_ushort(hi) << 16;
+          }
+          *reinterpret_cast<uint4*>(out + out_at(lane, q)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        if (edge || !live) {
+        __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (!live || cb + 8 * q + i >= p.V) f[i] = 0.f;
+        for (int i = 0; i < 4; ++i) {
+          const int rr = i * 8 + (lane >> 2), piece = lane & 3;
+          const uint4 v = *reinterpret_cast<const uint4*>(out + out_at(rr, piece));
+          *reinterpret_cast<uint4*>(dst + (part * p.cap + rr) * p.ld_g + c32 * 32 + piece * 8) = v;
         }
-        *reinterpret_cast<uint4*>(out + out_at(lane, h32 * 4 + q)) = pack16(f, bf16());
+        __syncwarp();
       }
-      while (__any_sync(0xffffffffu, w.next < cb + 32)) {
-        const int at = (w.next - cb) & 31;
-        const float l = pick32(r, at);
-        if (w.next < cb + 32) {
-          const int c = w.next;
-          float want = 0.f;
-          do {   // the same class twice: both weights
-            want += p.p ? p.p[row * p.k + w.j] : 1.f;
-            w.step();
-          } while (w.next == c);
-          const float q = ex2_approx(fmaf(l, p.inv_t, -lse) * kLog2e);
-          *reinterpret_cast<bf16*>(out + out_at(lane, h32 * 4 + (at >> 3)) + (at & 7) * 2) = __float2bfloat16_rn((q - want) * g);
-        }
-      }
-    }
-    __syncwarp();
+    } else if (c32 & 1) {
+      __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int rr = i * 4 + (lane >> 3), piece = lane & 7;
-      const uint4 v = *reinterpret_cast<const uint4*>(out + out_at(rr, piece));
-      *reinterpret_cast<uint4*>(dst + (int64_t)rr * p.ld_g + c64 * 64 + piece * 8) = v;
+      for (int i = 0; i < 8; ++i) {
+        const int rr = i * 4 + (lane >> 3), piece = lane & 7;
+        const uint4 v = *reinterpret_cast<const uint4*>(out + out_at(rr, piece));
+        *reinterpret_cast<uint4*>(dst + (int64_t)rr * p.ld_g + (c32 - 1) * 32 + piece * 8) = v;
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
 }
 
@@ -303,34 +342,34 @@ __device__ __forceinline__ void dh_tile(const HtDev& p, const Tile& ti, int m0, 
   }
 }
 
+template <bool F32>
 __device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, int half, uint32_t tacc, uint8_t* out, int lane) {
+  using T = typename std::conditional<F32, float, bf16>::type;
+  constexpr int V = Elem<T>::kVec, COLS = 8 * V;   // columns of 128 bytes
+  const float scale = *p.g_ref * p.temp;
   const int c0 = ti.nb * kHtTile + half * 128;
-  bf16* dst = p.dw + (int64_t)v0 * p.d + c0;
+  T* dst = static_cast<T*>(p.dw) + (int64_t)v0 * p.d + c0;
 #pragma unroll 1
-  for (int c64 = 0; c64 < 2; ++c64) {
-    if (c0 + c64 * 64 >= p.d) break;
+  for (int c = 0; c < 128; c += COLS) {
+    if (c0 + c >= p.d) break;
 #pragma unroll 1
-    for (int h32 = 0; h32 < 2; ++h32) {
+    for (int h = 0; h < COLS; h += 32) {
       uint32_t r[32];
-      tmem_ld32(tacc + c64 * 64 + h32 * 32, r);
+      tmem_ld32(tacc + c + h, r);
       tmem_ld_wait();
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float f[8];
+      for (int q = 0; q < 32 / V; ++q) {
+        float f[V];
+        const int col = c + h + q * V;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = ti.nkb ? __uint_as_float(r[8 * q + i]) : 0.f;
-        if (!p.add_w) {
-          *reinterpret_cast<uint4*>(out + out_at(lane, h32 * 4 + q)) = pack16(f, bf16());
-        } else {   // what is there is added before the one rounding
-          const int col = c64 * 64 + h32 * 32 + q * 8;
-          if (v0 + lane < p.V && c0 + col < p.d) {
-            float old[8];
-            load_vec(dst + (int64_t)lane * p.d + col, old);
+        for (int i = 0; i < V; ++i) f[i] = ti.nkb ? __uint_as_float(r[V * q + i]) * scale : 0.f;
+        if (p.add_w && v0 + lane < p.V && c0 + col < p.d) {   // what is there is added before the one rounding
+          float old[V];
+          load_vec(dst + (int64_t)lane * p.d + col, old);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] += old[i];
-          }
-          *reinterpret_cast<uint4*>(out + out_at(lane, h32 * 4 + q)) = pack16(f, bf16());
+          for (int i = 0; i < V; ++i) f[i] += old[i];
         }
+        *reinterpret_cast<uint4*>(out + out_at(lane, h / V + q)) = pack16(f, T());
       }
     }
     __syncwarp();
@@ -338,14 +377,13 @@ __device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, 
     for (int i = 0; i < 8; ++i) {
       const int rr = i * 4 + (lane >> 3), piece = lane & 7;
       const uint4 v = *reinterpret_cast<const uint4*>(out + out_at(rr, piece));
-      if (v0 + rr < p.V && c0 + c64 * 64 + piece * 8 < p.d)
-        *reinterpret_cast<uint4*>(dst + (int64_t)rr * p.d + c64 * 64 + piece * 8) = v;
+      if (v0 + rr < p.V && c0 + c + piece * V < p.d) *reinterpret_cast<uint4*>(dst + (int64_t)rr * p.d + c + piece * V) = v;
     }
     __syncwarp();
   }
 }
 
-template <bool GRAD>
+template <bool GRAD, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
     head_tc_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW,
                    const __grid_constant__ CUtensorMap tmG, const __grid_constant__ HtDev p) {
@@ -397,6 +435,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
   pdl_wait();
   const int count = *p.count;
   const Tiles<GRAD> tiles(p, count);
+  constexpr int TERMS = F32 ? kHtTerms : 1;
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
@@ -408,7 +447,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       for (int t = pair; t < tiles.n && ok; t += num_pairs) {
         const Tile ti = tiles.at(p, count, t);
         const int a0 = ti.mb * kHtTile + (int)rank * 128, b0 = ti.nb * kHtTile + (int)rank * 128;
-        for (int kb = 0; kb < ti.nkb; ++kb) {
+        int kb = 0, term = 0;
+        int64_t pa = 0, pb = 0;   // rows before the parts
+        auto parts = [&] {
+          if (!F32) return;
+          pa = part_a(term) * p.cap;
+          pb = part_b(term) * (!GRAD || ti.kind != kDW ? (int64_t)p.Vp : p.cap);
+        };
+        parts();
+        for (int i = ti.nkb * TERMS; i > 0; --i) {
           if (!mbar_wait_bounded(empty0 + 8 * stage, phase ^ 1, abort_flag, p.err, p.timeout_ns)) {
             ok = false;
             break;
@@ -417,21 +464,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
           if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * stage, 2 * kHtStage);
           const int k0 = (ti.kb0 + kb) * kHtK;
           if (!GRAD || ti.kind == kG) {   // H and W, both K-major: boxes of 64 rows
-            const int c0 = GRAD ? p.v_g + b0 : b0;
-            tma_load_2d_pair(a_s, &tmH, k0, a0, fb);
-            tma_load_2d_pair(a_s + kHtBox, &tmH, k0, a0 + 64, fb);
-            tma_load_2d_pair(b_s, &tmW, k0, c0, fb);
-            tma_load_2d_pair(b_s + kHtBox, &tmW, k0, c0 + 64, fb);
+            const int a = (int)(a0 + pa), b = (int)((GRAD ? p.v_g : 0) + b0 + pb);
+            tma_load_2d_pair(a_s, &tmH, k0, a, fb);
+            tma_load_2d_pair(a_s + kHtBox, &tmH, k0, a + 64, fb);
+            tma_load_2d_pair(b_s, &tmW, k0, b, fb);
+            tma_load_2d_pair(b_s + kHtBox, &tmW, k0, b + 64, fb);
           } else if (ti.kind == kDH) {    // G K-major, W as it lies (N = features)
-            tma_load_2d_pair(a_s, &tmG, k0, a0, fb);
-            tma_load_2d_pair(a_s + kHtBox, &tmG, k0, a0 + 64, fb);
-            tma_load_2d_pair(b_s, &tmW, b0, p.v_d + k0, fb);
-            tma_load_2d_pair(b_s + kHtBox, &tmW, b0 + 64, p.v_d + k0, fb);
+            const int a = (int)(a0 + pa), b = (int)(p.v_d + k0 + pb);
+            tma_load_2d_pair(a_s, &tmG, k0, a, fb);
+            tma_load_2d_pair(a_s + kHtBox, &tmG, k0, a + 64, fb);
+            tma_load_2d_pair(b_s, &tmW, b0, b, fb);
+            tma_load_2d_pair(b_s + kHtBox, &tmW, b0 + 64, b, fb);
           } else {                        // both as they lie (M = classes, N = features, K = rows)
-            tma_load_2d_pair(a_s, &tmG, a0, k0, fb);
-            tma_load_2d_pair(a_s + kHtBox, &tmG, a0 + 64, k0, fb);
-            tma_load_2d_pair(b_s, &tmH, b0, k0, fb);
-            tma_load_2d_pair(b_s + kHtBox, &tmH, b0 + 64, k0, fb);
+            const int a = (int)(k0 + pa), b = (int)(k0 + pb);
+            tma_load_2d_pair(a_s, &tmG, a0, a, fb);
+            tma_load_2d_pair(a_s + kHtBox, &tmG, a0 + 64, a, fb);
+            tma_load_2d_pair(b_s, &tmH, b0, b, fb);
+            tma_load_2d_pair(b_s + kHtBox, &tmH, b0 + 64, b, fb);
+          }
+          if (++kb == ti.nkb) {
+            kb = 0;
+            ++term;
+            parts();
           }
           ++issued;
           if (++stage == kHtStages) { stage = 0; phase ^= 1; }
@@ -465,7 +519,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
         const uint32_t id = idesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
         const uint32_t a_hi = a_mn ? kMajorMN : kMajorK, b_hi = b_mn ? kMajorMN : kMajorK;
         const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 k on, in 16 bytes
-        for (int kb = 0; kb < ti.nkb; ++kb) {
+        for (int kb = 0; kb < ti.nkb * TERMS; ++kb) {
           if (!mbar_wait_bounded(full0 + 8 * stage, phase, abort_flag, p.err, p.timeout_ns)) {
             ok = false;
             break;
@@ -505,9 +559,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       tc_fence_after();
       const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * 256 + half * 128;
       if (!GRAD) stats_tile(p, ti, m, half, m < count, tacc, w);
-      else if (ti.kind == kG) g_tile(p, ti, m, half, m < count, tacc, w, out, lane);
+      else if (ti.kind == kG) g_tile<F32>(p, ti, m, half, m < count, tacc, w, out, lane);
       else if (ti.kind == kDH) dh_tile(p, ti, m0, count, half, tacc, out, lane);
-      else dw_tile(p, ti, p.v_d + m0, half, tacc, out, lane);
+      else dw_tile<F32>(p, ti, p.v_d + m0, half, tacc, out, lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(tempty_lead + 8 * acc);
@@ -524,9 +578,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
   }
 }
 
-bool head_maps(const Head& a, CUtensorMap* th, CUtensorMap* tw) {
-  return make_tmap_bf16(th, a.packed, (uint64_t)a.cap, (uint64_t)a.d, (uint64_t)a.d, 64, 64) &&
-         make_tmap_bf16(tw, a.w, (uint64_t)a.V, (uint64_t)a.d, (uint64_t)a.d, 64, 64);
+bool head_maps(bool f32, const Head& a, CUtensorMap* th, CUtensorMap* tw) {
+  const uint64_t parts = f32 ? 3 : 1, ld = (uint64_t)a.ld;
+  return make_tmap_bf16(th, a.packed, parts * (uint64_t)a.cap, ld, ld, 64, 64) &&
+         make_tmap_bf16(tw, f32 ? a.w_parts : a.w, f32 ? parts * (uint64_t)a.Vp : (uint64_t)a.V, ld, ld, 64, 64);
 }
 
 HtDev head_dev(const Head& a, const Dev& dev) {
@@ -536,6 +591,7 @@ HtDev head_dev(const Head& a, const Dev& dev) {
   p.cap = a.cap;
   p.d = a.d;
   p.V = a.V;
+  p.Vp = a.Vp;
   p.inv_t = 1.f / a.temp;
   p.temp = a.temp;
   p.cls = a.cls;
@@ -545,6 +601,7 @@ HtDev head_dev(const Head& a, const Dev& dev) {
   p.picked = a.picked;
   p.lse = a.lse;
   p.g = a.g;
+  p.g_ref = a.g_ref;
   p.err = dev.err;
   p.timeout_ns = kWaitTimeoutNs;
   return p;
@@ -552,26 +609,28 @@ HtDev head_dev(const Head& a, const Dev& dev) {
 
 int ceil_to(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
-}  // namespace
-
-cudaError_t head_tc_stats(const Head& a, const Dev& dev) {
-  cudaError_t e = allow_smem<head_tc_kernel<false>, kHtSmem>();
-  if (e != cudaSuccess) return e;
+template <bool GRAD, bool F32>
+cudaError_t launch_tiles(int64_t tiles, const Head& a, const CUtensorMap& tg, const HtDev& p, const Dev& dev) {
+  const cudaError_t e = allow_smem<head_tc_kernel<GRAD, F32>, kHtSmem>();
+  if (e != cudaSuccess || tiles == 0) return e;
   CUtensorMap th, tw;
-  if (!head_maps(a, &th, &tw)) return cudaErrorInvalidValue;
-  const int64_t tiles = (int64_t)ceil_to(a.n, kHtTile) * ceil_to(a.V, kHtTile);
+  if (!head_maps(F32, a, &th, &tw)) return cudaErrorInvalidValue;
   const int pairs = (int)std::min<int64_t>(tiles, dev.num_sms / 2);
-  return launch_pdl(head_tc_kernel<false>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, tw, tw, head_dev(a, dev));
+  return launch_pdl(head_tc_kernel<GRAD, F32>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, tw, tg, p);
 }
 
-// One launch of the backward pass: G of the piece at v_g (n_g classes, 0: none) and the gradients of the
-// piece at v_d (n_d classes, 0: none), whose G lies in the other buffer.
-cudaError_t head_tc_grad(const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev) {
-  cudaError_t e = allow_smem<head_tc_kernel<true>, kHtSmem>();
-  if (e != cudaSuccess) return e;
-  CUtensorMap th, tw, tg;
-  void* other = a.G[buf ^ 1];
-  if (!head_maps(a, &th, &tw) || !make_tmap_bf16(&tg, other, (uint64_t)a.cap, (uint64_t)a.piece, (uint64_t)a.piece, 64, 64))
+}  // namespace
+
+cudaError_t head_stats(int dtype, const Head& a, const Dev& dev) {
+  const int64_t tiles = (int64_t)ceil_to(a.n, kHtTile) * ceil_to(a.V, kHtTile);
+  const CUtensorMap none = {};
+  return dtype == kBF16 ? launch_tiles<false, false>(tiles, a, none, head_dev(a, dev), dev)
+                        : launch_tiles<false, true>(tiles, a, none, head_dev(a, dev), dev);
+}
+
+cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev) {
+  CUtensorMap tg;
+  if (!make_tmap_bf16(&tg, a.G[buf ^ 1], (uint64_t)a.cap * (dtype == kBF16 ? 1 : 3), (uint64_t)a.piece, (uint64_t)a.piece, 64, 64))
     return cudaErrorInvalidValue;
   HtDev p = head_dev(a, dev);
   p.v_g = (int)v_g;
@@ -586,12 +645,10 @@ cudaError_t head_tc_grad(const Head& a, int buf, int64_t v_g, int n_g, int64_t v
   p.ld_g = a.piece;
   p.G = static_cast<bf16*>(a.G[buf]);
   p.acc = a.dh_acc;
-  p.dw = static_cast<bf16*>(a.dw);
+  p.dw = a.dw;
   const int64_t mbs = ceil_to(a.n, kHtTile), nbd = ceil_to(a.d, kHtTile);
   const int64_t tiles = mbs * p.n_g + (p.want_h && n_d ? mbs * nbd * p.splits : 0) + (p.want_w ? ceil_to(n_d, kHtTile) * nbd : 0);
-  if (tiles == 0) return cudaSuccess;
-  const int pairs = (int)std::min<int64_t>(tiles, dev.num_sms / 2);
-  return launch_pdl(head_tc_kernel<true>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, tw, tg, p);
+  return dtype == kBF16 ? launch_tiles<true, false>(tiles, a, tg, p, dev) : launch_tiles<true, true>(tiles, a, tg, p, dev);
 }
 
 }  // namespace adadsf

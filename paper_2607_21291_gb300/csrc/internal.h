@@ -316,24 +316,27 @@ struct Head {
   int k;
   // packed rows: count, their rows, their copy [cap][d]
   int32_t *count, *rows;
-  void* packed;
+  void* packed;                          // bf16 [cap][ld]; fp32: three parts of it
   int64_t cap;
+  int ld, Vp;                            // features of a packed row, rows of a part of the head
+  void* w_parts;                         // fp32: the head's parts [3][Vp][ld]
   float2* rec;                           // [ceil(V / 256) * 2][cap]
   float* picked;                         // by row, [k]
   float *loss, *lse;                     // by row (loss may be null)
   double* acc;                           // or null
   // backward
   const float* g;                        // by row, or null
+  float* g_ref;                          // the largest of a row with a target
   void *dh, *dw;                         // either may be null
   bool add_w;
-  void* G[2];                            // [cap][piece]
+  void* G[2];                            // bf16 [cap][piece]; fp32: three parts
   int piece, splits;
   float* dh_acc;                         // [splits][cap][d]
 };
 struct HeadPlan {
   int64_t cap;
-  int piece, pieces, splits;
-  size_t packed, rec, g, acc;            // bytes
+  int ld, Vp, piece, pieces, splits;
+  size_t packed, w_parts, rec, g, acc;   // bytes
 };
 HeadPlan head_plan(int dtype, int64_t n, int d, int V);
 constexpr int kHeadMaxK = 1024;
@@ -342,12 +345,10 @@ cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int 
                          float* ent, int32_t* target, const Dev& dev);
 cudaError_t head_forward(int dtype, const Head& a, const Dev& dev);
 cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev);
-// head_tc.cu (bf16), head_f32.cu: stats of all tiles; one launch of the backward pass -- G of the n_g classes
-// from v_g into G[buf], the gradients of the n_d classes from v_d from the other buffer.
-cudaError_t head_tc_stats(const Head& a, const Dev& dev);
-cudaError_t head_tc_grad(const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev);
-cudaError_t head_f32_stats(const Head& a, const Dev& dev);
-cudaError_t head_f32_grad(const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev);
+// head_tc.cu: stats of all tiles; one launch of the backward pass -- G of the n_g classes from v_g into G[buf], the
+// gradients of the n_d classes from v_d from the other buffer.
+cudaError_t head_stats(int dtype, const Head& a, const Dev& dev);
+cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev);
 
 // norm_grad.cu -- norms of rows with their statistics, and the gradients. scratch: norm_backward_scratch bytes.
 constexpr int kNormMaxD = 8192;
