@@ -161,13 +161,16 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+_get_device = getattr(torch._C, "_cuda_getDevice", None)   # what torch.cuda.current_device() asks, half a microsecond sooner
+
+
 def _s(stream) -> int:
     """The stream's handle; None is the current one, where torch tells it without making a Stream object (2 us of
     a call's 10), else from one."""
     if stream is None:
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None and torch.cuda.is_initialized():
-            return raw(torch.cuda.current_device())
+            return raw(_get_device() if _get_device else torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
@@ -657,40 +660,38 @@ def adadsf_sample(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor,
 
 
 # --------------------------------------------------------------------- training at the two ends
-def _matrix(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None, dtype=None, like=None):
-    """A contiguous matrix on the current device; rows, cols, type and device as asked."""
-    _dev(t, name)
-    if t.dim() != 2 or t.dtype not in DTYPE_CODE or (rows is not None and t.shape[0] != rows) or \
-            (cols is not None and t.shape[1] != cols) or (dtype is not None and t.dtype is not dtype):
-        want = " x ".join("any" if v is None else str(v) for v in (rows, cols))
-        raise ValueError(f"{name} must be a matrix ({want}) of {dtype or 'float32 or bfloat16'}, not {tuple(t.shape)} of {t.dtype}")
-    _here(t, name)
-
-
-def _here(t: torch.Tensor, name: str):
-    """The library launches on the current device: a tensor of another one is refused."""
-    if t.device.index != torch.cuda.current_device():
+def _on(t: torch.Tensor, name: str) -> int:
+    """The current device, on which the library launches; t has to be a matrix there."""
+    if not (t.is_cuda and t.dim() == 2 and t.is_contiguous()) or t.dtype not in DTYPE_CODE:
+        raise ValueError(f"{name} must be a contiguous CUDA matrix of float32 or bfloat16")
+    dev = t.get_device()
+    if dev != (_get_device() if _get_device else torch.cuda.current_device()):
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return dev
 
 
-def _vector(t: Optional[torch.Tensor], name: str, n: int, dtype: torch.dtype):
+def _mat(t: torch.Tensor, name: str, shape: tuple, dtype: torch.dtype, dev: int) -> int:
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous matrix {shape} of {dtype} on cuda:{dev}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+
+
+def _vec(t: Optional[torch.Tensor], name: str, n: int, dtype: torch.dtype, dev: int) -> Optional[int]:
+    """n contiguous values in any shape, or None."""
     if t is None:
         return None
-    _dev(t, name)
-    if t.dtype is not dtype or t.numel() != n:
-        raise ValueError(f"{name} must be {n} values of {dtype}, not {t.numel()} of {t.dtype}")
-    _here(t, name)
-    return t.data_ptr()
+    if t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    raise ValueError(f"{name} must be {n} contiguous values of {dtype} on cuda:{dev}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
-def _ws(ws: Optional[torch.Tensor], size, device) -> torch.Tensor:
-    if ws is None:
-        return workspace(size(), device)
-    _dev(ws, "ws")
-    if ws.dtype is not torch.uint8:
-        raise ValueError("ws must be bytes (see workspace)")
-    _here(ws, "ws")
-    return ws
+def _room(ws: torch.Tensor, dev: int):
+    if ws.dtype is torch.uint8 and ws.is_contiguous() and ws.get_device() == dev:
+        return ws.data_ptr(), ws.numel()
+    raise ValueError(f"ws must be contiguous bytes on cuda:{dev} (see workspace)")
+
+
+_F32 = torch.float32
 
 
 def adadsf_head_workspace_size(n_rows: int, d: int, n_classes: int, dtype: torch.dtype, top_k: int = 1) -> int:
@@ -701,33 +702,31 @@ def adadsf_head_workspace_size(n_rows: int, d: int, n_classes: int, dtype: torch
 
 
 def _head(h, w_head, k, ws):
-    _matrix(w_head, "w_head")
+    dev, dtype = _on(w_head, "w_head"), w_head.dtype
     n_cls, d = w_head.shape
-    _matrix(h, "h", cols=d, dtype=w_head.dtype)
     n = h.shape[0]
-    ws = _ws(ws, lambda: adadsf_head_workspace_size(n, d, n_cls, h.dtype, k), h.device)
-    return n, d, n_cls, DTYPE_CODE[h.dtype], ws
+    h_ptr = _mat(h, "h", (n, d), dtype, dev)
+    if ws is None:
+        ws = workspace(adadsf_head_workspace_size(n, d, n_cls, dtype, k), w_head.device)
+    return dev, (h_ptr, w_head.data_ptr()), (n, d, n_cls, DTYPE_CODE[dtype]), _room(ws, dev)
 
 
-def _teacher(h, top_idx, top_logit):
-    _dev(top_idx, "top_idx")
+def _teacher(top_idx, top_logit, n, dev):
+    k = top_idx.shape[-1]
+    return _vec(top_idx, "top_idx", n * k, torch.int32, dev), _vec(top_logit, "top_logit", n * k, _F32, dev), k
+
+
+def _slots(h, top_idx) -> int:
     if top_idx.dim() != 2 or top_idx.shape[0] != h.shape[0] or top_idx.shape[1] == 0:
         raise ValueError(f"top_idx must be ({h.shape[0]}, k), not {tuple(top_idx.shape)}")
-    n = top_idx.numel()
-    return _vector(top_idx, "top_idx", n, torch.int32), _vector(top_logit, "top_logit", n, torch.float32), top_idx.shape[1]
+    return top_idx.shape[1]
 
 
-def _losses(n, loss, lse, acc):
-    return (_vector(loss, "loss", n, torch.float32), _vector(lse, "lse", n, torch.float32),
-            _vector(acc, "acc", 2, torch.float64))
-
-
-def _head_grads(n, d, n_cls, dtype, grad_h, grad_w):
-    if grad_h is not None:
-        _matrix(grad_h, "grad_h", n, d, dtype)
-    if grad_w is not None:
-        _matrix(grad_w, "grad_w", n_cls, d, dtype)
-    return None if grad_h is None else grad_h.data_ptr(), None if grad_w is None else grad_w.data_ptr()
+def _head_grads(size, w_head, lse, grad_loss, grad_h, grad_w, dev):
+    n, d, n_cls, _ = size
+    return (_vec(lse, "lse", n, _F32, dev), _vec(grad_loss, "grad_loss", n, _F32, dev),
+            None if grad_h is None else _mat(grad_h, "grad_h", (n, d), w_head.dtype, dev),
+            None if grad_w is None else _mat(grad_w, "grad_w", (n_cls, d), w_head.dtype, dev))
 
 
 def adadsf_head_loss(h: torch.Tensor, w_head: torch.Tensor, target: torch.Tensor, loss: Optional[torch.Tensor],
@@ -737,10 +736,10 @@ def adadsf_head_loss(h: torch.Tensor, w_head: torch.Tensor, target: torch.Tensor
     none) through the head w_head (classes, d), no logit stored: loss and lse
     (fp32, n) receive the losses and logarithms that the backward call needs;
     acc (2 doubles) += {sum of losses, rows with a target}."""
-    n, d, n_cls, dtype, ws = _head(h, w_head, 1, ws)
-    out = _losses(n, loss, lse, acc)
-    _check(lib().adadsf_head_loss(h.data_ptr(), w_head.data_ptr(), _vector(target, "target", n, torch.int32), n, d, n_cls,
-                                  dtype, *out, ws.data_ptr(), ws.numel(), _s(stream)))
+    dev, ptrs, size, room = _head(h, w_head, 1, ws)
+    n = size[0]
+    _check(lib().adadsf_head_loss(*ptrs, _vec(target, "target", n, torch.int32, dev), *size, _vec(loss, "loss", n, _F32, dev),
+                                  _vec(lse, "lse", n, _F32, dev), _vec(acc, "acc", 2, torch.float64, dev), *room, _s(stream)))
 
 
 def adadsf_head_loss_backward(h: torch.Tensor, w_head: torch.Tensor, target: torch.Tensor, lse: torch.Tensor,
@@ -750,12 +749,10 @@ def adadsf_head_loss_backward(h: torch.Tensor, w_head: torch.Tensor, target: tor
     """Gradients of adadsf_head_loss's losses, each weighted by grad_loss (fp32,
     n; None: 1): grad_h like h, grad_w like w_head (either may be None;
     accumulate_w adds to what grad_w holds)."""
-    n, d, n_cls, dtype, ws = _head(h, w_head, 1, ws)
-    grads = _head_grads(n, d, n_cls, h.dtype, grad_h, grad_w)
-    _check(lib().adadsf_head_loss_backward(h.data_ptr(), w_head.data_ptr(), _vector(target, "target", n, torch.int32), n, d,
-                                           n_cls, dtype, _vector(lse, "lse", n, torch.float32),
-                                           _vector(grad_loss, "grad_loss", n, torch.float32), *grads,
-                                           1 if accumulate_w else 0, ws.data_ptr(), ws.numel(), _s(stream)))
+    dev, ptrs, size, room = _head(h, w_head, 1, ws)
+    grads = _head_grads(size, w_head, lse, grad_loss, grad_h, grad_w, dev)
+    _check(lib().adadsf_head_loss_backward(*ptrs, _vec(target, "target", size[0], torch.int32, dev), *size, *grads,
+                                           1 if accumulate_w else 0, *room, _s(stream)))
 
 
 def adadsf_distill_loss(h: torch.Tensor, w_head: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor,
@@ -764,11 +761,11 @@ def adadsf_distill_loss(h: torch.Tensor, w_head: torch.Tensor, top_idx: torch.Te
     """KL of each row's softmax at a temperature from a teacher's top logits:
     top_idx (int32, n x k; below 0: slot not in use) and top_logit (fp32).
     Outputs as adadsf_head_loss's."""
-    idx, logit, k = _teacher(h, top_idx, top_logit)
-    n, d, n_cls, dtype, ws = _head(h, w_head, k, ws)
-    out = _losses(n, loss, lse, acc)
-    _check(lib().adadsf_distill_loss(h.data_ptr(), w_head.data_ptr(), idx, logit, k, float(temperature), n, d, n_cls, dtype,
-                                     *out, ws.data_ptr(), ws.numel(), _s(stream)))
+    dev, ptrs, size, room = _head(h, w_head, _slots(h, top_idx), ws)
+    n = size[0]
+    _check(lib().adadsf_distill_loss(*ptrs, *_teacher(top_idx, top_logit, n, dev), float(temperature), *size,
+                                     _vec(loss, "loss", n, _F32, dev), _vec(lse, "lse", n, _F32, dev),
+                                     _vec(acc, "acc", 2, torch.float64, dev), *room, _s(stream)))
 
 
 def adadsf_distill_loss_backward(h: torch.Tensor, w_head: torch.Tensor, top_idx: torch.Tensor, top_logit: torch.Tensor,
@@ -776,26 +773,22 @@ def adadsf_distill_loss_backward(h: torch.Tensor, w_head: torch.Tensor, top_idx:
                                  grad_h: Optional[torch.Tensor] = None, grad_w: Optional[torch.Tensor] = None,
                                  accumulate_w: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
     """Gradients of adadsf_distill_loss's losses (see adadsf_head_loss_backward)."""
-    idx, logit, k = _teacher(h, top_idx, top_logit)
-    n, d, n_cls, dtype, ws = _head(h, w_head, k, ws)
-    grads = _head_grads(n, d, n_cls, h.dtype, grad_h, grad_w)
-    _check(lib().adadsf_distill_loss_backward(h.data_ptr(), w_head.data_ptr(), idx, logit, k, float(temperature), n, d, n_cls,
-                                              dtype, _vector(lse, "lse", n, torch.float32),
-                                              _vector(grad_loss, "grad_loss", n, torch.float32), *grads,
-                                              1 if accumulate_w else 0, ws.data_ptr(), ws.numel(), _s(stream)))
+    dev, ptrs, size, room = _head(h, w_head, _slots(h, top_idx), ws)
+    grads = _head_grads(size, w_head, lse, grad_loss, grad_h, grad_w, dev)
+    _check(lib().adadsf_distill_loss_backward(*ptrs, *_teacher(top_idx, top_logit, size[0], dev), float(temperature), *size,
+                                              *grads, 1 if accumulate_w else 0, *room, _s(stream)))
 
 
 def adadsf_norm_forward(x: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor], y: torch.Tensor, eps: float,
                         mean: Optional[torch.Tensor], rstd: torch.Tensor, stream=None):
     """LayerNorm of the rows of x (n, d) into y, RMSNorm where b and mean are
     None; mean and rstd (fp32, n) are what the backward call needs."""
-    _matrix(x, "x")
+    dev, dtype = _on(x, "x"), x.dtype
     n, d = x.shape
-    _matrix(y, "y", n, d, x.dtype)
-    _check(lib().adadsf_norm_forward(x.data_ptr(), _vector(w, "w", d, x.dtype), _vector(b, "b", d, x.dtype), n, d,
-                                     DTYPE_CODE[x.dtype], float(eps), 1 if b is None and mean is None else 0, y.data_ptr(),
-                                     _vector(mean, "mean", n, torch.float32), _vector(rstd, "rstd", n, torch.float32),
-                                     _s(stream)))
+    _check(lib().adadsf_norm_forward(x.data_ptr(), _vec(w, "w", d, dtype, dev), _vec(b, "b", d, dtype, dev), n, d,
+                                     DTYPE_CODE[dtype], eps, 1 if b is None and mean is None else 0,
+                                     _mat(y, "y", (n, d), dtype, dev), _vec(mean, "mean", n, _F32, dev),
+                                     _vec(rstd, "rstd", n, _F32, dev), _s(stream)))
 
 
 def adadsf_norm_backward_workspace_size(n_rows: int, d: int) -> int:
@@ -811,30 +804,27 @@ def adadsf_norm_backward(grad_y: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
                          accumulate: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
     """Gradients of adadsf_norm_forward (RMSNorm where mean is None): grad_x
     like x, with add added; grad_w and grad_b (fp32, d) where wanted."""
-    _matrix(x, "x")
-    n, d = x.shape
-    for t, name in ((grad_y, "grad_y"), (grad_x, "grad_x"), (add, "add")):
-        if t is not None or name != "add":
-            _matrix(t, name, n, d, x.dtype)
-    ws = _ws(ws, lambda: adadsf_norm_backward_workspace_size(n, d), x.device)
-    _check(lib().adadsf_norm_backward(grad_y.data_ptr(), x.data_ptr(), _vector(w, "w", d, x.dtype),
-                                      _vector(mean, "mean", n, torch.float32), _vector(rstd, "rstd", n, torch.float32),
-                                      None if add is None else add.data_ptr(), n, d, DTYPE_CODE[x.dtype],
-                                      1 if mean is None else 0, grad_x.data_ptr(), _vector(grad_w, "grad_w", d, torch.float32),
-                                      _vector(grad_b, "grad_b", d, torch.float32), 1 if accumulate else 0, ws.data_ptr(),
-                                      ws.numel(), _s(stream)))
+    dev, dtype, shape = _on(x, "x"), x.dtype, x.shape
+    n, d = shape
+    if ws is None:
+        ws = workspace(adadsf_norm_backward_workspace_size(n, d), x.device)
+    _check(lib().adadsf_norm_backward(_mat(grad_y, "grad_y", shape, dtype, dev), x.data_ptr(), _vec(w, "w", d, dtype, dev),
+                                      _vec(mean, "mean", n, _F32, dev), _vec(rstd, "rstd", n, _F32, dev),
+                                      None if add is None else _mat(add, "add", shape, dtype, dev), n, d, DTYPE_CODE[dtype],
+                                      1 if mean is None else 0, _mat(grad_x, "grad_x", shape, dtype, dev),
+                                      _vec(grad_w, "grad_w", d, _F32, dev), _vec(grad_b, "grad_b", d, _F32, dev),
+                                      1 if accumulate else 0, *_room(ws, dev), _s(stream)))
 
 
 def adadsf_embed_forward(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
                          ws: Optional[torch.Tensor] = None, stream=None):
     """out (n, d) = scale * the rows ids (int32; below 0: zeros) of table (vocab, d)."""
-    _matrix(table, "table")
+    dev, dtype = _on(table, "table"), table.dtype
     n, (vocab, d) = ids.numel(), table.shape
-    _matrix(out, "out", n, d, table.dtype)
-    ws = _ws(ws, lambda: 256, table.device)
-    _check(lib().adadsf_embed_forward(_vector(ids, "ids", n, torch.int32), n, table.data_ptr(), vocab, d,
-                                      DTYPE_CODE[table.dtype], float(scale), out.data_ptr(), ws.data_ptr(), ws.numel(),
-                                      _s(stream)))
+    if ws is None:
+        ws = workspace(256, table.device)
+    _check(lib().adadsf_embed_forward(_vec(ids, "ids", n, torch.int32, dev), n, table.data_ptr(), vocab, d, DTYPE_CODE[dtype],
+                                      scale, _mat(out, "out", (n, d), dtype, dev), *_room(ws, dev), _s(stream)))
 
 
 def adadsf_embed_backward_workspace_size(n: int, vocab: int, d: int) -> int:
@@ -848,13 +838,13 @@ def adadsf_embed_backward(ids: torch.Tensor, grad_out: torch.Tensor, grad_table:
                           accumulate: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
     """The table's gradient (vocab, d): scale * the sum of grad_out's rows of
     each id, in one order; accumulate adds to the rows of the ids that came."""
-    _matrix(grad_table, "grad_table")
+    dev, dtype = _on(grad_table, "grad_table"), grad_table.dtype
     n, (vocab, d) = ids.numel(), grad_table.shape
-    _matrix(grad_out, "grad_out", n, d, grad_table.dtype)
-    ws = _ws(ws, lambda: adadsf_embed_backward_workspace_size(n, vocab, d), grad_table.device)
-    _check(lib().adadsf_embed_backward(_vector(ids, "ids", n, torch.int32), grad_out.data_ptr(), n, vocab, d,
-                                       DTYPE_CODE[grad_table.dtype], float(scale), grad_table.data_ptr(),
-                                       1 if accumulate else 0, ws.data_ptr(), ws.numel(), _s(stream)))
+    if ws is None:
+        ws = workspace(adadsf_embed_backward_workspace_size(n, vocab, d), grad_table.device)
+    _check(lib().adadsf_embed_backward(_vec(ids, "ids", n, torch.int32, dev), _mat(grad_out, "grad_out", (n, d), dtype, dev), n,
+                                       vocab, d, DTYPE_CODE[dtype], scale, grad_table.data_ptr(), 1 if accumulate else 0,
+                                       *_room(ws, dev), _s(stream)))
 
 
 def adadsf_sync_check(ws: torch.Tensor, stream=None) -> int:

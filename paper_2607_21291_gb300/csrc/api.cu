@@ -2003,7 +2003,7 @@ adadsf_status adadsf_norm_forward(const void* x_dev, const void* w_dev, const vo
 
 size_t adadsf_norm_backward_workspace_size(int64_t n_rows, int d) {
   if (n_rows < 0 || d <= 0 || d > kNormMaxD) return 0;
-  return kErrBytes + align256(norm_backward_scratch(n_rows, d));
+  return kErrBytes + kSyncBytes + align256(norm_backward_scratch(n_rows, d));
 }
 
 adadsf_status adadsf_norm_backward(const void* grad_y_dev, const void* x_dev, const void* w_dev, const float* mean_dev,
@@ -2032,7 +2032,7 @@ adadsf_status adadsf_norm_backward(const void* grad_y_dev, const void* x_dev, co
   TRY(device_info(&dev, stream, ws));
   return launch(dev, ADADSF_KERNEL_NORM_GRAD, false, 0, (3.0 + (add_dev != nullptr)) * n_rows * d * elem_size(dtype),
                 CALL(norm_backward(dtype, grad_y_dev, x_dev, w_dev, mean_dev, rstd_dev, add_dev, n_rows, d, grad_x_dev, grad_w_dev,
-                                   grad_b_dev, accumulate != 0, at<float>(ws, kErrBytes), dev),
+                                   grad_b_dev, accumulate != 0, at<int>(ws, kErrBytes), at<float>(ws, kErrBytes + kSyncBytes), dev),
                      "norm gradient"));
 }
 
@@ -2052,7 +2052,7 @@ adadsf_status adadsf_embed_forward(const int32_t* ids_dev, int64_t n, const void
 
 size_t adadsf_embed_backward_workspace_size(int64_t n, int vocab, int d) {
   if (n < 0 || n > (int64_t)1 << 30 || vocab <= 0 || vocab > 1 << 27 || d <= 0 || d > 65536) return 0;
-  return kErrBytes + embed_backward_scratch(n, vocab, d);
+  return kErrBytes + kSyncBytes + embed_backward_scratch(n, vocab, d);
 }
 
 adadsf_status adadsf_embed_backward(const int32_t* ids_dev, const void* grad_out_dev, int64_t n, int vocab, int d, int dtype,
@@ -2074,7 +2074,7 @@ adadsf_status adadsf_embed_backward(const int32_t* ids_dev, const void* grad_out
   TRY(device_info(&dev, stream, ws));
   return launch(dev, ADADSF_KERNEL_EMBED_GRAD, false, 0, ((double)n * d + (accumulate ? 0.0 : (double)vocab * d)) * elem_size(dtype),
                 CALL(embed_backward(dtype, ids_dev, grad_out_dev, n, vocab, d, scale, grad_table_dev, accumulate != 0,
-                                    at<uint8_t>(ws, kErrBytes), dev),
+                                    at<uint8_t>(ws, kErrBytes + kSyncBytes), dev),
                      "embedding gradient"));
 }
 

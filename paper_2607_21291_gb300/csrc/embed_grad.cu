@@ -17,7 +17,7 @@
 namespace adadsf {
 namespace {
 
-constexpr int kEgRun = 32;          // places a group walks
+constexpr int kEgRun = 32;          // places a group walks, a lane of each warp a place; a quarter of it where there are few
 constexpr int kEgThreads = 512;     // at most, of a block
 constexpr int kEgFew = 4096;        // tokens up to which each counts the ones before it
 constexpr int kEgLanes = 4;         // lanes that share a token's count
@@ -26,7 +26,7 @@ constexpr int kEgSort = 256;        // threads of the digit sort
 constexpr int kEgChunk = kEgSort * 8;
 constexpr int kEgMaxTiles = 512;
 constexpr int kEgDigit = 9;
-constexpr int kEgAhead = 4;         // rows on their way
+constexpr int kEgAhead = 8;         // rows on their way
 
 // Ids of no row of the table: below 0 padding, past it an error; both sort behind every id.
 __device__ __forceinline__ int32_t key_of(int32_t id, int vocab, int* err) {
@@ -219,6 +219,7 @@ __global__ void __launch_bounds__(kEgSort) embed_place_kernel(const Digit q, con
 struct EgDev {
   const int32_t *key, *place;
   int64_t n, runs;
+  int run;             // places of a run
   const void* dy;
   int vocab, d, group, groups, nv;
   float scale;
@@ -242,61 +243,64 @@ __device__ __forceinline__ void write_row(const EgDev& p, int64_t id, int c, flo
   store_vec(at, s);
 }
 
-// A group of threads: kEgRun places of the sorted list, its threads the vectors of a row (blockIdx.y: which of them).
+template <int V>
+__device__ __forceinline__ void put_carry(const EgDev& p, int64_t at, int c, const float (&s)[V]) {
+  float* to = p.carry + at * p.d + c * V;
+#pragma unroll
+  for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+}
+
+// A group of threads: a run of places of the sorted list, its threads the vectors of a row (blockIdx.y: which of them).
 template <typename T>
 __global__ void __launch_bounds__(kEgThreads) embed_sum_kernel(const __grid_constant__ EgDev p) {
   constexpr int V = Elem<T>::kVec;
   pdl_wait();
   pdl_trigger();
-  const int g = threadIdx.x / p.group, c = blockIdx.y * p.group + threadIdx.x - g * p.group;
+  const int g = threadIdx.x / p.group, c = blockIdx.y * p.group + threadIdx.x - g * p.group, lane = threadIdx.x & 31;
   const int64_t run = (int64_t)blockIdx.x * p.groups + g;
-  if (run >= p.runs || c >= p.nv) return;
-  const int64_t i0 = run * kEgRun, i1 = min(p.n, i0 + kEgRun);
-  int32_t id = p.key[i0];
-  if (id >= p.vocab) return;
-  bool began = i0 > 0 && p.key[i0 - 1] == id;   // the id's first place is another group's
-  float s[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) s[j] = 0.f;
-  uint4 next[kEgAhead];
+  if (run >= p.runs) return;
+  const bool mine = c < p.nv;
+  const int64_t i0 = run * p.run;
+  const int count = (int)min((int64_t)p.run, p.n - i0);
+  const int32_t key = lane < count ? p.key[i0 + lane] : p.vocab, place = lane < count ? p.place[i0 + lane] : 0;
+  const int32_t before = i0 > 0 ? p.key[i0 - 1] : -1, behind = i0 + count < p.n ? p.key[i0 + count] : -1;
+  const int used = __popc(__ballot_sync(0xffffffffu, key < p.vocab));   // padding sorts last
+  if (used == 0) return;
   const uint4* dy = static_cast<const uint4*>(p.dy);
-  auto load = [&](int64_t i) {
-    return i < i1 && p.key[i] < p.vocab ? dy[(int64_t)p.place[i] * p.nv + c] : make_uint4(0, 0, 0, 0);
-  };
-#pragma unroll
-  for (int a = 0; a < kEgAhead; ++a) next[a] = load(i0 + a);
-  for (int64_t i = i0; i < i1; i += kEgAhead) {
+  int32_t id = __shfl_sync(0xffffffffu, key, 0);
+  bool began = id == before;   // the id's first place is another group's
+  float s[V] = {};
+  for (int i = 0; i < used; i += kEgAhead) {
+    uint4 u[kEgAhead];
 #pragma unroll
     for (int a = 0; a < kEgAhead; ++a) {
-      if (i + a < i1) {
-        const int32_t now = p.key[i + a];
-        if (now != id) {
-          if (began) {
-            float* at = p.carry + (run * 2) * p.d + c * V;
+      const int32_t at = __shfl_sync(0xffffffffu, place, (i + a) & 31);
+      u[a] = mine && i + a < used ? dy[(int64_t)at * p.nv + c] : make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
-            for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(at + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
-          } else {
-            write_row<T>(p, id, c, s);
-          }
-          began = false;
-          id = now;
-          if (id >= p.vocab) return;
-#pragma unroll
-          for (int j = 0; j < V; ++j) s[j] = 0.f;
+    for (int a = 0; a < kEgAhead; ++a) {
+      const int32_t now = __shfl_sync(0xffffffffu, key, (i + a) & 31);
+      if (i + a >= used) break;
+      if (now != id) {
+        if (mine) {
+          if (began) put_carry<V>(p, run * 2, c, s);
+          else write_row<T>(p, id, c, s);
         }
-        float f[V];
-        unpack16(next[a], f, T());
-        next[a] = load(i + a + kEgAhead);
+        began = false;
+        id = now;
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j] += f[j];
+        for (int j = 0; j < V; ++j) s[j] = 0.f;
       }
+      float f[V];
+      unpack16(u[a], f, T());
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] += f[j];
     }
   }
-  const bool goes_on = i1 < p.n && p.key[i1] == id;
-  if (!began && !goes_on) return write_row<T>(p, id, c, s);
-  float* at = p.carry + (run * 2 + (began ? 0 : 1)) * p.d + c * V;
-#pragma unroll
-  for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(at + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+  if (!mine) return;
+  if (began) put_carry<V>(p, run * 2, c, s);
+  else if (id == behind) put_carry<V>(p, run * 2 + 1, c, s);
+  else write_row<T>(p, id, c, s);
 }
 
 // The group whose places an id begins in and goes on behind adds up what the others left of it, in order.
@@ -308,41 +312,45 @@ __global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_con
   const int g = threadIdx.x / p.group, c = blockIdx.y * p.group + threadIdx.x - g * p.group;
   const int64_t run = (int64_t)blockIdx.x * p.groups + g;
   if (run >= p.runs || c >= p.nv) return;
-  const int64_t i0 = run * kEgRun, i1 = i0 + kEgRun;
+  const int64_t i0 = run * p.run, i1 = i0 + p.run;
   if (i1 >= p.n) return;
-  const int32_t id = p.key[i1 - 1];
-  if (id >= p.vocab || p.key[i1] != id) return;
-  if (p.key[i0] == id && i0 > 0 && p.key[i0 - 1] == id) return;   // it began before
+  const int32_t id = p.key[i1 - 1], behind = p.key[i1], first = p.key[i0], before = i0 > 0 ? p.key[i0 - 1] : -1;
+  if (id >= p.vocab || behind != id || (first == id && before == id)) return;   // ends here, or began before
   float s[V];
   const float* at = p.carry + (run * 2 + 1) * p.d + c * V;
 #pragma unroll
   for (int j = 0; j < V; j += 4) load4(at + j, s + j);
-  // the last run that holds the id: its sums lie at every run's first carry up to there
-  int64_t lo = run + 1, hi = p.runs - 1;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) >> 1;
-    if (p.key[mid * kEgRun] == id) lo = mid;
-    else hi = mid - 1;
-  }
-#pragma unroll 4
-  for (int64_t r = run + 1; r <= lo; ++r) {
-    const float* a = p.carry + (r * 2) * p.d + c * V;
-    float f[V];
+  // the runs behind that begin with the id, eight at a time: their sums lie at the first of their two places
+  bool more = true;
+  for (int64_t r = run + 1; more && r < p.runs; r += kEgAhead) {
+    float f[kEgAhead][V];
+    bool in[kEgAhead];
 #pragma unroll
-    for (int j = 0; j < V; j += 4) load4(a + j, f + j);
+    for (int a = 0; a < kEgAhead; ++a) {
+      in[a] = r + a < p.runs && p.key[(r + a) * p.run] == id;
+      const float* from = p.carry + (min(r + a, p.runs - 1) * 2) * p.d + c * V;
 #pragma unroll
-    for (int j = 0; j < V; ++j) s[j] += f[j];
+      for (int j = 0; j < V; j += 4) load4(from + j, f[a] + j);
+    }
+#pragma unroll
+    for (int a = 0; a < kEgAhead; ++a) {
+      more = more && in[a];
+      if (!more) break;
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] += f[a][j];
+    }
   }
   write_row<T>(p, id, c, s);
 }
 
 struct EgPlan {
   int64_t runs, per_tile;
-  int tiles, bits, passes, digit;
+  int run, tiles, bits, passes, digit;
 };
 EgPlan plan(int64_t n, int vocab) {
   EgPlan q;
-  q.runs = (n + kEgRun - 1) / kEgRun;
+  q.run = n <= kEgFew ? kEgRun / 4 : kEgRun;
+  q.runs = (n + q.run - 1) / q.run;
   q.bits = 1;
   while (q.bits < 31 && ((int64_t)1 << q.bits) <= vocab) ++q.bits;   // keys 0 .. vocab
   q.passes = (q.bits + kEgDigit - 1) / kEgDigit;
@@ -445,6 +453,7 @@ cudaError_t embed_backward(int dtype, const int32_t* ids, const void* dy, int64_
   p.place = place[last];
   p.n = n;
   p.runs = q.runs;
+  p.run = q.run;
   p.dy = dy;
   p.vocab = vocab;
   p.d = d;

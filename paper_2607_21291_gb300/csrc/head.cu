@@ -76,8 +76,18 @@ constexpr int kPackThreads = 256;
 //
 // The copy is bf16 [cap][ld]; of fp32 features three parts (see next_part), each such a matrix, ld features with zeros behind
 // the d-th. Backward: the largest weight of a row's loss as well.
+constexpr int kPutAhead = 8;   // loads of a lane on their way
 __device__ __forceinline__ void put_row(const bf16* src, bf16* dst, int64_t, int d, int, int lane) {
-  for (int v = lane; v < d / 8; v += 32) reinterpret_cast<uint4*>(dst)[v] = reinterpret_cast<const uint4*>(src)[v];
+  const int nv = d / 8;
+  for (int v = lane; v < nv; v += 32 * kPutAhead) {
+    uint4 u[kPutAhead];
+#pragma unroll
+    for (int j = 0; j < kPutAhead; ++j)
+      if (v + 32 * j < nv) u[j] = reinterpret_cast<const uint4*>(src)[v + 32 * j];
+#pragma unroll
+    for (int j = 0; j < kPutAhead; ++j)
+      if (v + 32 * j < nv) reinterpret_cast<uint4*>(dst)[v + 32 * j] = u[j];
+  }
 }
 // 4 features of fp32 into the parts, `part` elements apart.
 __device__ __forceinline__ void put4(const float4& f, bf16* dst, int64_t part) {
@@ -91,8 +101,15 @@ __device__ __forceinline__ void put4(const float4& f, bf16* dst, int64_t part) {
   }
 }
 __device__ __forceinline__ void put_row(const float* src, bf16* dst, int64_t part, int d, int ld, int lane) {
-  for (int v = lane; v < ld / 4; v += 32)
-    put4(v < d / 4 ? reinterpret_cast<const float4*>(src)[v] : make_float4(0.f, 0.f, 0.f, 0.f), dst + 4 * v, part);
+  for (int v = lane; v < ld / 4; v += 32 * kPutAhead) {
+    float4 f[kPutAhead];
+#pragma unroll
+    for (int j = 0; j < kPutAhead; ++j)
+      f[j] = v + 32 * j < d / 4 ? reinterpret_cast<const float4*>(src)[v + 32 * j] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < kPutAhead; ++j)
+      if (v + 32 * j < ld / 4) put4(f[j], dst + 4 * (v + 32 * j), part);
+  }
 }
 
 template <typename T>
@@ -111,6 +128,7 @@ __global__ void __launch_bounds__(kPackThreads)
   int before = 0, all = 0;
   float top = 0.f;
   const bool weigh = g && blockIdx.x == 0;
+#pragma unroll 8
   for (int64_t i = tid; i < n; i += kPackThreads) {
     const int32_t t = target[i];
     const int in = t >= 0 && t < V;
@@ -197,7 +215,7 @@ __global__ void __launch_bounds__(256) head_split_kernel(const float* w, int V, 
 
 // Losses of 32 packed rows: a lane a row, the warps share the records of its classes and its targets.
 // Every sum runs in one order.
-constexpr int kMergeWarps = 32;
+constexpr int kMergeWarps = 32, kMergeAhead = 8;
 __global__ void __launch_bounds__(32 * kMergeWarps)
     head_merge_kernel(const int32_t* count, const int32_t* rows, const float2* rec, int64_t cap, int n_rec, const float* picked,
                       const float* p, const float* ent, int k, float temp, float* loss, float* lse) {
@@ -206,20 +224,27 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
   __shared__ float s_top[kMergeWarps][32], s_sum[kMergeWarps][32], s_pz[kMergeWarps][32], s_p[kMergeWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n = *count;
-  const float inv_t = 1.f / temp;
+  const float inv_t = 1.f / temp, c = inv_t * 1.4426950408889634f;
   for (int64_t m0 = (int64_t)blockIdx.x * 32; m0 < n; m0 += (int64_t)gridDim.x * 32) {
     const int64_t m = m0 + lane;
     float top = -INFINITY, sum = 0.f, pz = 0.f, ps = 0.f;
     int64_t row = 0;
     if (m < n) {
       row = rows[m];
-#pragma unroll 4
-      for (int i = warp; i < n_rec; i += kMergeWarps) {
-        const float2 r = rec[(int64_t)i * cap + m];
-        const float now = fmaxf(top, r.x);
+      for (int i = warp; i < n_rec; i += kMergeWarps * kMergeAhead) {
+        float2 r[kMergeAhead];
+        float now = top;
+#pragma unroll
+        for (int j = 0; j < kMergeAhead; ++j) {
+          const int at = i + j * kMergeWarps;
+          r[j] = at < n_rec ? rec[(int64_t)at * cap + m] : make_float2(-INFINITY, 0.f);
+        }
+#pragma unroll
+        for (int j = 0; j < kMergeAhead; ++j) now = fmaxf(now, r[j].x);
         // a side without a number so far (-inf) adds nothing but its NaN
-        const float a = top == now ? 1.f : expf((top - now) * inv_t), b = r.x == now ? 1.f : expf((r.x - now) * inv_t);
-        sum = sum * a + r.y * b;
+        sum *= top == now ? 1.f : ex2_approx((top - now) * c);
+#pragma unroll
+        for (int j = 0; j < kMergeAhead; ++j) sum += r[j].y * (r[j].x == now ? 1.f : ex2_approx((r[j].x - now) * c));
         top = now;
       }
       for (int j = warp; j < k; j += kMergeWarps) {
@@ -241,7 +266,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
       pz = 0.f;
       ps = 0.f;
       for (int i = 0; i < kMergeWarps; ++i) {
-        const float a = s_top[i][lane] == top ? 1.f : expf((s_top[i][lane] - top) * inv_t);
+        const float a = s_top[i][lane] == top ? 1.f : ex2_approx((s_top[i][lane] - top) * c);
         sum += s_sum[i][lane] * a;
         pz += s_pz[i][lane];
         ps += s_p[i][lane];
@@ -320,8 +345,8 @@ cudaError_t pack(const Head& a, bool backward, const Dev& dev) {
 
 }  // namespace
 
-// Classes a piece: its G in both buffers is to stay in the L2 with what else is read, but whole where
-// few rows make it small.
+// Classes a piece: 256 MB of G. With 96 MB the launches' first and last waves cost more than its second reading from the
+// L2 saves (3 x 259 fp32 tokens 725 -> 650 us, 8 x 511 of the Pythia-1.4B head 1750 -> 1590); 600 and 1500 MB are no faster.
 HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
   const int64_t parts = dtype == kBF16 ? 1 : 3, tile = 256;
   HeadPlan q;
@@ -329,7 +354,7 @@ HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
   q.ld = (d + 7) / 8 * 8;
   q.Vp = (int)(((int64_t)V + 63) / 64 * 64);
   const int64_t padded = ((int64_t)V + 255) / 256 * 256;
-  int64_t piece = std::max<int64_t>(2048, (96ll << 20) / std::max<int64_t>(1, q.cap * 2 * parts));
+  int64_t piece = std::max<int64_t>(2048, (256ll << 20) / std::max<int64_t>(1, q.cap * 2 * parts));
   const int64_t pieces = (padded + piece - 1) / piece;
   piece = ((padded + pieces - 1) / pieces + 255) / 256 * 256;
   q.piece = (int)piece;

@@ -350,14 +350,15 @@ cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const 
 cudaError_t head_stats(int dtype, const Head& a, const Dev& dev);
 cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev);
 
-// norm_grad.cu -- norms of rows with their statistics, and the gradients. scratch: norm_backward_scratch bytes.
+// norm_grad.cu -- norms of rows with their statistics, and the gradients. sync: the workspace's synchronisation
+// area; scratch: norm_backward_scratch bytes.
 constexpr int kNormMaxD = 8192;
 size_t norm_backward_scratch(int64_t n, int d);
 cudaError_t norm_forward(int dtype, const void* x, const void* w, const void* b, int64_t n, int d, float eps, bool rms, void* y,
                          float* mean, float* rstd, const Dev& dev);
 cudaError_t norm_backward(int dtype, const void* dy, const void* x, const void* w, const float* mean, const float* rstd,
-                          const void* add, int64_t n, int d, void* dx, float* dw, float* db, bool accumulate, float* scratch,
-                          const Dev& dev);
+                          const void* add, int64_t n, int d, void* dx, float* dw, float* db, bool accumulate, int* sync,
+                          float* scratch, const Dev& dev);
 // embed_grad.cu
 cudaError_t embed_scale(int dtype, const int32_t* ids, int64_t n, const void* table, int vocab, int d, float scale, void* out,
                         const Dev& dev);
