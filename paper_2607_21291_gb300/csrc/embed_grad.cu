@@ -326,9 +326,11 @@ __global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_con
     float f[kEgAhead][V];
     bool in[kEgAhead];
 #pragma unroll
+    for (int a = 0; a < kEgAhead; ++a) in[a] = r + a < p.runs && p.key[(r + a) * p.run] == id;
+#pragma unroll
     for (int a = 0; a < kEgAhead; ++a) {
-      in[a] = r + a < p.runs && p.key[(r + a) * p.run] == id;
-      const float* from = p.carry + (min(r + a, p.runs - 1) * 2) * p.d + c * V;
+      if (!in[a]) continue;   // most ids go over one border: eight rows for each would be read for nothing
+      const float* from = p.carry + (r + a) * 2 * p.d + c * V;
 #pragma unroll
       for (int j = 0; j < V; j += 4) load4(from + j, f[a] + j);
     }

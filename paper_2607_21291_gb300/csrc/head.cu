@@ -74,7 +74,7 @@ constexpr int kPackThreads = 256;
 // logarithm and a gradient of zero; what they hold is read by nobody. Packed rows past the last one, up to a
 // multiple of kHeadZeroPad, are zero: products over rows run that far.
 //
-// The copy is bf16 [cap][ld]; of fp32 features three parts (see next_part), each such a matrix, ld features with zeros behind
+// The copy is bf16 [cap][ld]; of fp32 features three parts (see next_parts), each such a matrix, ld features with zeros behind
 // the d-th. Backward: the largest weight of a row's loss as well.
 constexpr int kPutAhead = 8;   // loads of a lane on their way
 __device__ __forceinline__ void put_row(const bf16* src, bf16* dst, int64_t, int d, int, int lane) {
@@ -95,8 +95,8 @@ __device__ __forceinline__ void put4(const float4& f, bf16* dst, int64_t part) {
 #pragma unroll
   for (int q = 0; q < 3; ++q) {
     uint2 u;
-    u.x = (uint32_t)__bfloat16_as_ushort(next_part(x[0], q == 2)) | (uint32_t)__bfloat16_as_ushort(next_part(x[1], q == 2)) << 16;
-    u.y = (uint32_t)__bfloat16_as_ushort(next_part(x[2], q == 2)) | (uint32_t)__bfloat16_as_ushort(next_part(x[3], q == 2)) << 16;
+    u.x = next_parts(x[0], x[1]);
+    u.y = next_parts(x[2], x[3]);
     *reinterpret_cast<uint2*>(dst + q * part) = u;
   }
 }
@@ -330,14 +330,14 @@ __global__ void __launch_bounds__(256)
 }
 
 template <typename T>
-cudaError_t pack(const Head& a, bool backward, const Dev& dev) {
+cudaError_t pack(const Head& a, bool backward, bool split, const Dev& dev) {
   const int64_t per = std::max<int64_t>(8, (a.n + 511) / 512);
   cudaError_t e = launch_pdl(head_pack_kernel<T>, dim3((unsigned)((a.n + per - 1) / per)), dim3(kPackThreads), 0, dev.stream,
                              a.target, a.n, a.V, per, static_cast<const T*>(a.h), a.d, static_cast<bf16*>(a.packed), a.cap, a.ld,
                              a.rows, a.count, backward ? a.g : (const float*)nullptr, backward ? a.g_ref : (float*)nullptr,
                              backward ? (float*)nullptr : a.loss, backward ? (float*)nullptr : a.lse,
                              backward ? static_cast<T*>(a.dh) : (T*)nullptr, dev.err);
-  if (e != cudaSuccess || sizeof(T) == 2) return e;
+  if (e != cudaSuccess || !split || sizeof(T) == 2) return e;
   const int64_t pieces = (int64_t)a.Vp * (a.ld / 4);
   return launch_pdl(head_split_kernel, dim3((unsigned)std::min<int64_t>((pieces + 255) / 256, 8 * dev.num_sms)), dim3(256), 0,
                     dev.stream, static_cast<const float*>(a.w), a.V, a.d, a.Vp, a.ld, static_cast<bf16*>(a.w_parts));
@@ -367,7 +367,7 @@ HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
   q.splits = (int)std::min<int64_t>(splits, 64);
   q.packed = (size_t)(parts * q.cap * q.ld * 2);
   q.w_parts = dtype == kBF16 ? 0 : (size_t)(parts * q.Vp * q.ld * 2);
-  q.rec = (size_t)(padded / 128 * q.cap * 8);
+  q.rec = (size_t)(std::max<int64_t>(padded / 128, kHeadFewCtas) * q.cap * 8);
   q.g = (size_t)(parts * q.cap * piece * 2);
   q.acc = (size_t)(q.splits * q.cap * d * 4);
   return q;
@@ -380,19 +380,21 @@ cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int 
 }
 
 cudaError_t head_forward(int dtype, const Head& a, const Dev& dev) {
-  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, false, dev) : pack<float>(a, false, dev);
-  if (e == cudaSuccess) e = head_stats(dtype, a, dev);
+  const bool few = a.n <= kHeadFewRows;
+  int records = (a.V + 127) / 128;
+  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, false, !few, dev) : pack<float>(a, false, !few, dev);
+  if (e == cudaSuccess) e = few ? head_few(dtype, a, dev, &records) : head_stats(dtype, a, dev);
   if (e != cudaSuccess) return e;
   const int blocks = (int)std::min<int64_t>((a.n + 31) / 32, 2 * dev.num_sms);
   e = launch_pdl(head_merge_kernel, dim3((unsigned)blocks), dim3(32 * kMergeWarps), 0, dev.stream, (const int32_t*)a.count,
-                 (const int32_t*)a.rows, (const float2*)a.rec, a.cap, (a.V + 127) / 128, (const float*)a.picked, a.p, a.ent, a.k,
+                 (const int32_t*)a.rows, (const float2*)a.rec, a.cap, records, (const float*)a.picked, a.p, a.ent, a.k,
                  a.temp, a.loss, a.lse);
   if (e != cudaSuccess || !a.acc) return e;
   return launch_pdl(head_sum_kernel, dim3(1), dim3(1024), 0, dev.stream, (const float*)a.loss, a.n, (const int32_t*)a.count, a.acc);
 }
 
 cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev) {
-  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, true, dev) : pack<float>(a, true, dev);
+  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, true, true, dev) : pack<float>(a, true, true, dev);
   // launch j: G of piece j, gradients of piece j - 1
   for (int j = 0; j <= plan.pieces && e == cudaSuccess; ++j) {
     const int64_t v = (int64_t)j * plan.piece, before = v - plan.piece;

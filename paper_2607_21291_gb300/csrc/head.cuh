@@ -17,14 +17,19 @@ namespace adadsf {
 constexpr int kHeadRowPad = 256;   // packed buffers hold whole tiles of rows
 constexpr int kHeadZeroPad = 64;   // rows past the last packed one, up to a multiple of this, are zero in the packed copy
 
-// x as the sum of three bf16 numbers: the next one, and in x what it leaves. Numbers past bf16's largest leave the
-// rest to the next part; NaN stays NaN in the last.
-__device__ __forceinline__ bf16 next_part(float& x, bool last) {
-  constexpr float kMost = 3.3895313892515355e38f;
-  const bf16 h = __float2bfloat16_rn(last ? x : fminf(fmaxf(x, -kMost), kMost));
-  x -= __bfloat162float(h);
-  return h;
+// fp32 numbers as sums of three bf16 numbers, their leading 8 bits, the next 8 and the last: the next part of a (low
+// half) and b (high half), which keep what it leaves. Exact; an infinity becomes NaN.
+__device__ __forceinline__ uint32_t next_parts(float& a, float& b) {
+  const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+  a -= __uint_as_float(ua & 0xffff0000u);
+  b -= __uint_as_float(ub & 0xffff0000u);
+  return __byte_perm(ua, ub, 0x7632);
 }
+
+// Parts of the two operands of each product of an fp32 product's parts.
+constexpr int kHeadTerms = 6;
+__device__ __forceinline__ int head_part_a(int term) { return (0x001102 >> (4 * term)) & 3; }   // 2 0 1 1 0 0
+__device__ __forceinline__ int head_part_b(int term) { return (0x010120 >> (4 * term)) & 3; }   // 0 2 1 0 1 0
 
 // First of a row's k ascending classes that is not below c0.
 __device__ __forceinline__ int first_class(const int32_t* cls, int k, int c0) {

@@ -1,0 +1,414 @@
+// The losses' forward pass for few rows (at most kHeadFewRows): what bounds it is reading the head once.
+//
+// The operands change places against head_tc.cu: 128 classes are the M of a product and the packed rows, up to
+// 128 in steps of 16, its N, so that the tensor cores spend on a block of classes what its rows need (with 256 rows
+// a tile, 24 rows took as long as 256: 20 us for the Pythia-160M head, now FEWUS). A CTA takes one range of
+// classes, in units of 32, and keeps a running maximum and sum of exponentials a row: one record a CTA and row.
+// fp32: the head's numbers are split into their three bf16 parts (see next_parts) on the way into shared
+// memory, by warps that read them a block ahead; a pass of its own wrote and read again 4.5 times the head's bytes.
+//   warp 0       TMA: the rows' blocks of 64 k (fp32: three parts), the head's blocks (bf16)
+//   warp 1       TMEM, MMA issue (one thread), accumulators double-buffered
+//   warps 2-9    epilogue: four warps take 32 rows of a tile through shared memory, which turns classes into columns
+//   warps 10-17  fp32: the head's parts
+// Every wait is bounded in time (device error word on give-up).
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "head.cuh"
+
+namespace adadsf {
+namespace {
+
+constexpr int kHfM = 128;                        // classes of a tile
+constexpr int kHfUnit = 32;                      // classes of a box
+constexpr int kHfK = 64;
+constexpr int kHfPart = kHfM * kHfK * 2;         // bytes of a block of classes (one part)
+constexpr int kHfEpiWarps = 8, kHfConvWarps = 8;
+constexpr int kHfOutLd = kHfM + 4;               // floats of a staged row
+constexpr int kHfOut = 32 * kHfOutLd * 4;        // 32 rows of a tile
+constexpr int kHfMaxStages = 8;
+constexpr int kHfBars = 2 * kHfMaxStages + 5;
+constexpr int kHfRing = 196608;
+constexpr int kHfSmem = 1024 + kHfRing + 2 * kHfOut + kHfBars * 8 + 16;
+constexpr uint32_t kHfDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+
+template <bool F32>
+struct HfCfg {
+  static constexpr int PARTS = F32 ? 3 : 1;
+  static constexpr int TERMS = F32 ? kHeadTerms : 1;
+  static constexpr int THREADS = 64 + 32 * kHfEpiWarps + (F32 ? 32 * kHfConvWarps : 0);
+  __host__ __device__ static int stage(int n) { return PARTS * (kHfPart + n * 128); }
+  __host__ __device__ static int stages(int n) {
+    const int s = kHfRing / stage(n);
+    return s < kHfMaxStages ? s : kHfMaxStages;
+  }
+};
+
+struct HfDev {
+  const int32_t *count, *rows;
+  const float* w;            // fp32 head
+  int64_t cap;
+  int d, V, n;               // n: rows, a multiple of 16
+  float inv_t;
+  const int32_t* cls;
+  int k;
+  float2* rec;               // [CTA][cap]
+  float* picked;
+  int* err;
+  unsigned long long timeout_ns;
+};
+
+// A product, and the arrival when all so far are done, issued by the lane with lead != 0 of a warp that comes along.
+__device__ __forceinline__ void few_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %6};\n\tmov.b64 db, {%2, %6};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(lead), "r"(kHfDescHigh)
+      : "memory");
+}
+__device__ __forceinline__ void few_commit(uint32_t bar, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(lead)
+      : "memory");
+}
+
+// Whether ok holds in all 128 threads of a barrier.
+__device__ __forceinline__ bool group_agrees(int id, bool ok) {
+  int all;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\t"
+      "bar.red.and.pred q, %1, 128, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(id), "r"((int)ok)
+      : "memory");
+  return all != 0;
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
+    head_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW,
+                    const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ HfDev p) {
+  using C = HfCfg<F32>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const uint32_t ring = smem_u32(smem);
+  float* outs = reinterpret_cast<float*>(smem + kHfRing);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kHfRing + 2 * kHfOut);
+  const uint32_t full0 = smem_u32(bars);
+  const uint32_t empty0 = full0 + 8 * kHfMaxStages;
+  const uint32_t tfull0 = empty0 + 8 * kHfMaxStages;
+  const uint32_t tempty0 = tfull0 + 16;
+  const uint32_t drain = tempty0 + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kHfBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int stage_bytes = C::stage(p.n), stages = C::stages(p.n);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // this CTA's classes, in tiles of 128 of which the last may be short
+  const int units = (p.V + kHfUnit - 1) / kHfUnit;
+  const int c_begin = (int)((int64_t)units * blockIdx.x / gridDim.x) * kHfUnit;
+  const int c_end = min(p.V, (int)((int64_t)units * (blockIdx.x + 1) / gridDim.x) * kHfUnit);
+  const int tiles = (c_end - c_begin + kHfM - 1) / kHfM, nkb = (p.d + kHfK - 1) / kHfK;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(full0 + 8 * s, 1 + (F32 ? kHfConvWarps : 0));
+      mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(tfull0 + 8 * a, 1);
+      mbar_init(tempty0 + 8 * a, kHfEpiWarps);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 0 && lane == 0) {
+    tma_prefetch_desc(&tmH);
+    if (!F32) tma_prefetch_desc(&tmW);   // boxes of a whole tile; tmW1: of a unit
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 256);
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      int64_t issued = 0;
+      bool ok = true;
+      const int total = tiles * nkb;
+      // bf16: the head's next block (weights: an earlier launch of this call waited for whatever wrote them)
+      int c0 = c_begin, w_k = 0;
+      auto head = [&](int s) {
+        const uint32_t bar = full0 + 8 * s, to = ring + s * stage_bytes;
+        const int classes = c_end - c0;
+        if (classes >= kHfM) {
+          mbar_arrive_expect_tx(bar, kHfPart + p.n * 128);
+          tma_load_2d(to, &tmW, w_k, c0, bar);
+        } else {
+          const int boxes = (classes + kHfUnit - 1) / kHfUnit;
+          mbar_arrive_expect_tx(bar, boxes * kHfUnit * 128 + p.n * 128);
+          for (int b = 0; b < boxes; ++b) tma_load_2d(to + b * kHfUnit * 128, &tmW1, w_k, c0 + b * kHfUnit, bar);
+        }
+        w_k += kHfK;
+        if (w_k >= p.d) {
+          w_k = 0;
+          c0 += kHfM;
+        }
+      };
+      const int pre = F32 ? 0 : min(total, stages);
+      for (int i = 0; i < pre; ++i) head(i);
+      pdl_wait();
+      int k = 0;
+      for (int i = 0; i < total && ok; ++i) {
+        if (i >= pre) {
+          if (!mbar_wait_bounded(empty0 + 8 * stage, phase ^ 1, abort_flag, p.err, p.timeout_ns)) {
+            ok = false;
+            break;
+          }
+          if (F32) mbar_arrive_expect_tx(full0 + 8 * stage, 3 * p.n * 128);
+          else head(stage);
+        }
+#pragma unroll
+        for (int q = 0; q < C::PARTS; ++q)
+          tma_load_2d(ring + stage * stage_bytes + C::PARTS * kHfPart + q * p.n * 128, &tmH, k, (int)(q * p.cap), full0 + 8 * stage);
+        k += kHfK;
+        if (k >= p.d) k = 0;
+        ++issued;
+        if (++stage == stages) { stage = 0; phase ^= 1; }
+      }
+      pdl_trigger();
+      for (int s = 0; s < stages; ++s) {   // drain: the copies issued last have landed
+        if (issued <= s) break;
+        const int64_t last = s + ((issued - 1 - s) / stages) * stages;
+        mbar_wait_drain(full0 + 8 * s, (uint32_t)((last / stages) & 1), p.timeout_ns);
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    // all lanes come along, one of them issues: with warp-uniform operands a product takes no moves between
+    // register files, which took longer than a product of few columns
+    const uint32_t idesc = idesc_bf16_f32(kHfM, p.n), lead = lane == 0;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      int got = 0;
+      if (lane == 0) got = mbar_wait_bounded(bar, parity, abort_flag, p.err, p.timeout_ns);
+      return __shfl_sync(0xffffffffu, got, 0) != 0;
+    };
+    for (int it = 0; it < tiles && ok; ++it) {
+      const int acc = it & 1;
+      if (!wait(tempty0 + 8 * acc, ((it >> 1) & 1) ^ 1)) break;
+      tc_fence_after();
+      const uint32_t d = tmem_base + acc * 128;
+      for (int kb = 0; kb < nkb; ++kb) {
+        if (!wait(full0 + 8 * stage, phase)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t w_s = ring + stage * stage_bytes, h_s = w_s + C::PARTS * kHfPart;
+#pragma unroll
+        for (int term = 0; term < C::TERMS; ++term) {
+          // the head is A here, the rows B
+          const uint32_t a = ((w_s + (F32 ? head_part_b(term) * kHfPart : 0)) & 0x3FFFFu) >> 4 | 1u << 16;
+          const uint32_t b = ((h_s + (F32 ? head_part_a(term) * p.n * 128 : 0)) & 0x3FFFFu) >> 4 | 1u << 16;
+#pragma unroll
+          for (int k = 0; k < kHfK / 16; ++k) few_mma(d, a + 2 * k, b + 2 * k, idesc, kb > 0 || term > 0 || k > 0 ? 1u : 0u, lead);
+        }
+        few_commit(empty0 + 8 * stage, lead);
+        if (++stage == stages) { stage = 0; phase ^= 1; }
+      }
+      if (ok) few_commit(tfull0 + 8 * acc, lead);
+    }
+    few_commit(drain, lead);
+    if (lane == 0) mbar_wait_drain(drain, 0, p.timeout_ns);
+  } else if (warp < 2 + kHfEpiWarps) {
+    // ------------------------------------------------------------ epilogue
+    pdl_wait();
+    const int count = *p.count;
+    const int quarter = warp & 3, group = (warp - 2) >> 2;
+    const int t = quarter * 32 + lane, r = t >> 2, q = t & 3;   // thread of the group; its row of 32, its quarter of the classes
+    const float c = p.inv_t * 1.4426950408889634f;
+    float* out = outs + group * (kHfOut / 4);
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+    int next[2] = {0, 0};
+    const int chunks = (min(count, p.n) + 31) / 32;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int m = (group + 2 * u) * 32 + r;
+      next[u] = q == 0 && m < count ? first_class(p.cls + (int64_t)p.rows[m] * p.k, p.k, c_begin) : p.k;
+    }
+    bool ok = true;
+    for (int it = 0; it < tiles; ++it) {
+      const int acc = it & 1, c0 = c_begin + it * kHfM, c1 = min(c_end, c0 + kHfM);
+      int got = 0;
+      if (lane == 0) got = mbar_wait_bounded(tfull0 + 8 * acc, (it >> 1) & 1, abort_flag, p.err, p.timeout_ns);
+      ok = __shfl_sync(0xffffffffu, got, 0) != 0;
+      // the four warps of a group go on or leave together: they share barriers
+      if (!group_agrees(1 + group, ok)) break;
+      tc_fence_after();
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int chunk = group + 2 * u;
+        if (chunk >= chunks) continue;
+        uint32_t v[32];
+        tmem_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * 128 + chunk * 32, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) out[j * kHfOutLd + t] = __uint_as_float(v[j]);
+        named_bar_sync(1 + group, 128);
+        const int m = chunk * 32 + r;
+        const float* row = out + r * kHfOutLd;
+        float f[32], now = top[u];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          f[i] = c0 + 4 * i + q < c1 ? row[4 * i + q] : -INFINITY;
+          now = fmaxf(now, f[i]);
+        }
+        // NaN logits leave the maximum but reach the sum; a maximum of -inf subtracts nothing
+        if (now > top[u]) {
+          sum[u] *= top[u] == -INFINITY ? 0.f : ex2_approx((top[u] - now) * c);
+          top[u] = now;
+        }
+        const float base = now == -INFINITY ? 0.f : now;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i & 3] += ex2_approx((f[i] - base) * c);
+        sum[u] += (s[0] + s[1]) + (s[2] + s[3]);
+        if (q == 0 && m < count) {
+          const int64_t line = (int64_t)p.rows[m] * p.k;
+          for (; next[u] < p.k; ++next[u]) {
+            const int cl = p.cls[line + next[u]];
+            if (cl >= c1) break;
+            p.picked[line + next[u]] = row[cl - c0];
+          }
+        }
+        named_bar_sync(1 + group, 128);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int m = (group + 2 * u) * 32 + r;
+      float most = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      float s = sum[u] * (top[u] == most ? 1.f : ex2_approx((top[u] - most) * c));
+      s += __shfl_xor_sync(0xffffffffu, s, 1);
+      s += __shfl_xor_sync(0xffffffffu, s, 2);
+      if (q == 0 && m < count) p.rec[(int64_t)blockIdx.x * p.cap + m] = make_float2(most, s);
+    }
+  } else if (F32) {
+    // ------------------------------------------------------------ the head's parts
+    const int w = warp - 2 - kHfEpiWarps, k4 = lane & 15, r0 = w * 16 + (lane >> 4);
+    int stage = 0;
+    uint32_t phase = 0;
+    const int total = tiles * nkb;
+    float4 f[2][8];
+    int c0 = c_begin, k0 = 0;   // of the block that is loaded next
+    auto load = [&](float4 (&g)[8]) {
+      const int k = k0 + 4 * k4;
+      const float* src = p.w + (int64_t)(c0 + r0) * p.d + k;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        g[j] = c0 + r0 + 2 * j < c_end && k < p.d ? *reinterpret_cast<const float4*>(src + (int64_t)(2 * j) * p.d) : make_float4(0.f, 0.f, 0.f, 0.f);
+      k0 += kHfK;
+      if (k0 >= p.d) {
+        k0 = 0;
+        c0 += kHfM;
+      }
+    };
+    auto put = [&](const float4 (&g)[8]) {
+      int got = 0;
+      if (lane == 0) got = mbar_wait_bounded(empty0 + 8 * stage, phase ^ 1, abort_flag, p.err, p.timeout_ns);
+      if (!__shfl_sync(0xffffffffu, got, 0)) return false;
+      uint8_t* at = smem + stage * stage_bytes;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int row = r0 + 2 * j;
+        float x[4] = {g[j].x, g[j].y, g[j].z, g[j].w};
+        uint8_t* to = at + row * 128 + (((k4 >> 1) ^ (row & 7)) << 4) + (k4 & 1) * 8;
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+          uint2 u;
+          u.x = next_parts(x[0], x[1]);
+          u.y = next_parts(x[2], x[3]);
+          *reinterpret_cast<uint2*>(to + q * kHfPart) = u;
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full0 + 8 * stage);
+      if (++stage == stages) { stage = 0; phase ^= 1; }
+      return true;
+    };
+    load(f[0]);
+    load(f[1]);
+    for (int i = 0; i < total; i += 2) {
+      if (!put(f[0])) break;
+      load(f[0]);
+      if (i + 1 >= total || !put(f[1])) break;
+      load(f[1]);
+    }
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 256);
+  }
+}
+
+template <bool F32>
+cudaError_t launch_few(const Head& a, const Dev& dev, int* records) {
+  const cudaError_t e = allow_smem<head_few_kernel<F32>, kHfSmem>();
+  if (e != cudaSuccess) return e;
+  HfDev p = {};
+  p.n = (int)((a.n + 15) / 16 * 16);
+  CUtensorMap th, tw = {}, tw1 = {};
+  if (!make_tmap_bf16(&th, a.packed, (uint64_t)a.cap * (F32 ? 3 : 1), (uint64_t)a.ld, (uint64_t)a.ld, kHfK, (uint32_t)p.n))
+    return cudaErrorInvalidValue;
+  if (!F32 && (!make_tmap_bf16(&tw, a.w, (uint64_t)a.V, (uint64_t)a.d, (uint64_t)a.d, kHfK, kHfM) ||
+               !make_tmap_bf16(&tw1, a.w, (uint64_t)a.V, (uint64_t)a.d, (uint64_t)a.d, kHfK, kHfUnit)))
+    return cudaErrorInvalidValue;
+  p.count = a.count;
+  p.rows = a.rows;
+  p.w = static_cast<const float*>(a.w);
+  p.cap = a.cap;
+  p.d = a.d;
+  p.V = a.V;
+  p.inv_t = 1.f / a.temp;
+  p.cls = a.cls;
+  p.k = a.k;
+  p.rec = a.rec;
+  p.picked = a.picked;
+  p.err = dev.err;
+  p.timeout_ns = kWaitTimeoutNs;
+  *records = (int)std::min<int64_t>(std::min(dev.num_sms, kHeadFewCtas), ((int64_t)a.V + kHfUnit - 1) / kHfUnit);
+  return launch_pdl(head_few_kernel<F32>, dim3((unsigned)*records), dim3(HfCfg<F32>::THREADS), kHfSmem, dev.stream, th, tw, tw1, p);
+}
+
+}  // namespace
+
+cudaError_t head_few(int dtype, const Head& a, const Dev& dev, int* records) {
+  return dtype == kBF16 ? launch_few<false>(a, dev, records) : launch_few<true>(a, dev, records);
+}
+
+}  // namespace adadsf

@@ -18,7 +18,7 @@
 // so that equal weights leave its roundings independent (a common factor of 1 / 3580 rounded every target's
 // entry the same way: gradients 2.8e-3 off, now NEWERR), and the gradients that it enters are rounded to bf16 as well.
 //
-// fp32: every operand is three bf16 numbers whose sum it is (8 bits each), and a product of two is six of their nine
+// fp32: every operand is three bf16 numbers whose sum it is (8 bits each, next_parts), and a product of two is six of their nine
 // products, the least first, in the same accumulators; the three that are left out are below 2^-24 of it.
 //   warp 0     TMA: A and B tiles of 64 k, 6 stages of 32 KB (both CTAs)
 //   warp 1     TMEM, MMA issue (one thread of the even CTA)
@@ -48,11 +48,6 @@ constexpr int kHtSmem = 1024 + kHtStages * kHtStage + kHtEpiWarps * kHtOut + kHt
 constexpr uint32_t kHtDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;   // groups of 8 lines 1024 bytes apart, 128-byte swizzle
 
 enum { kStats = 0, kG = 1, kDH = 2, kDW = 3 };
-
-// Parts of A and B of each product of an fp32 operand's parts.
-constexpr int kHtTerms = 6;
-__device__ __forceinline__ int part_a(int term) { return (0x001102 >> (4 * term)) & 3; }   // 2 0 1 1 0 0
-__device__ __forceinline__ int part_b(int term) { return (0x010120 >> (4 * term)) & 3; }   // 0 2 1 0 1 0
 
 struct HtDev {
   const int32_t* count;      // packed rows
@@ -286,8 +281,7 @@ __device__ __forceinline__ void g_tile(const HtDev& p, const Tile& ti, int m, in
           uint32_t v[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const bf16 lo = next_part(f[8 * q + 2 * i], part == 2), hi = next_part(f[8 * q + 2 * i + 1], part == 2);
-            v[i] = (uint32_t)__bfloat16_as_ushort(lo) | (uint32_t)__bfloat16_as_ushort(hi) << 16;
+            v[i] = next_parts(f[8 * q + 2 * i], f[8 * q + 2 * i + 1]);
           }
           *reinterpret_cast<uint4*>(out + out_at(lane, q)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
@@ -435,7 +429,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
   pdl_wait();
   const int count = *p.count;
   const Tiles<GRAD> tiles(p, count);
-  constexpr int TERMS = F32 ? kHtTerms : 1;
+  constexpr int TERMS = F32 ? kHeadTerms : 1;
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
@@ -451,8 +445,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
         int64_t pa = 0, pb = 0;   // rows before the parts
         auto parts = [&] {
           if (!F32) return;
-          pa = part_a(term) * p.cap;
-          pb = part_b(term) * (!GRAD || ti.kind != kDW ? (int64_t)p.Vp : p.cap);
+          pa = head_part_a(term) * p.cap;
+          pb = head_part_b(term) * (!GRAD || ti.kind != kDW ? (int64_t)p.Vp : p.cap);
         };
         parts();
         for (int i = ti.nkb * TERMS; i > 0; --i) {

@@ -320,7 +320,7 @@ struct Head {
   int64_t cap;
   int ld, Vp;                            // features of a packed row, rows of a part of the head
   void* w_parts;                         // fp32: the head's parts [3][Vp][ld]
-  float2* rec;                           // [ceil(V / 256) * 2][cap]
+  float2* rec;                           // [head_plan's][cap]
   float* picked;                         // by row, [k]
   float *loss, *lse;                     // by row (loss may be null)
   double* acc;                           // or null
@@ -345,6 +345,9 @@ cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int 
                          float* ent, int32_t* target, const Dev& dev);
 cudaError_t head_forward(int dtype, const Head& a, const Dev& dev);
 cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev);
+// head_few.cu: stats for at most kHeadFewRows rows, one record a CTA (their number in *records).
+constexpr int kHeadFewRows = 128, kHeadFewCtas = 160;
+cudaError_t head_few(int dtype, const Head& a, const Dev& dev, int* records);
 // head_tc.cu: stats of all tiles; one launch of the backward pass -- G of the n_g classes from v_g into G[buf], the
 // gradients of the n_d classes from v_d from the other buffer.
 cudaError_t head_stats(int dtype, const Head& a, const Dev& dev);

@@ -145,6 +145,8 @@ def ce(A, h, w, target, gl=None, grads=True, ws=None, stream=None):
 
 HEADS = [(1, 64, 100, "bf16"), (3, 8, 1, "bf16"), (24, 768, 5003, "bf16"), (130, 200, 257, "bf16"), (257, 520, 1000, "bf16"),
          (300, 768, 1280, "bf16"), (700, 264, 255, "bf16"), (9000, 64, 12001, "bf16"),
+         (65, 64, 31, "bf16"), (97, 136, 33, "bf16"), (128, 136, 20011, "bf16"), (129, 72, 300, "bf16"),
+         (33, 4, 5000, "f32"), (128, 100, 20011, "f32"), (129, 68, 300, "f32"),
          (1, 4, 1, "f32"), (5, 132, 130, "f32"), (77, 512, 3001, "f32"), (515, 100, 777, "f32"), (9000, 32, 6002, "f32")]
 
 
@@ -189,7 +191,8 @@ def distill(A, h, w, idx, logit, temp, gl, ws=None):
 
 @pytest.mark.parametrize("n,d,V,k,temp,dtype", [(1, 64, 100, 1, 1.0, "bf16"), (40, 128, 300, 7, 2.0, "bf16"),
                                                 (300, 520, 1000, 64, 0.7, "bf16"), (33, 64, 70, 1024, 1.0, "bf16"),
-                                                (9000, 64, 11000, 20, 4.0, "bf16"), (5, 132, 130, 3, 1.0, "f32"),
+                                                (9000, 64, 11000, 20, 4.0, "bf16"), (128, 64, 9000, 33, 1.5, "bf16"),
+                                                (100, 68, 9000, 9, 1.0, "f32"), (5, 132, 130, 3, 1.0, "f32"),
                                                 (200, 256, 3001, 129, 2.0, "f32"), (9000, 32, 6002, 5, 1.0, "f32")])
 def test_distill_loss(A, n, d, V, k, temp, dtype):
     h, w, idx, logit, gl = distill_inputs(n, d, V, k, dtype)
