@@ -9,10 +9,14 @@ calls and applies the plain SGD update to the router tensors.
 The layer input x and the dense layer's output h_dense are held fixed
 (teacher forcing from the dense model, as Eq. 9 compares the two models
 layer by layer), so the step's gradient is that of the layer's own L_hid.
+
+The two ends of the model train beside it (ends_gradients, ends_step): embedding,
+final norm and LM head against the next tokens (the L_causal of Table 4) or a
+teacher's top logits, each operator and its gradient a library call.
 """
 from __future__ import annotations
 
-from typing import Optional
+from typing import Callable, Optional
 
 import torch
 
@@ -56,3 +60,70 @@ def router_alignment_step(shape_cfg: A.ModelCfg, w: dict, x: torch.Tensor, h_den
         w[k].sub_((g[off:off + n] * scale).view(w[k].shape).to(w[k].dtype))
         off += n
     return float(acc[0] / acc[1])
+
+
+def ends_gradients(cfg: A.ModelCfg, w: dict, ids: torch.Tensor, target: Optional[torch.Tensor] = None,
+                   body: Optional[Callable] = None, top: Optional[tuple] = None, scale: float = 1.0, stream=None):
+    """Loss and gradients of the model's two ends: scale * w["embed"][ids]
+    (vocab, d; ids below 0 are padding) -> body -> final norm (w["final_w"],
+    GPT-NeoX also w["final_b"]) -> LM head w["head"], or w["embed"] where there
+    is none -> cross entropy with target (int32 like ids, below 0: none), or the
+    distillation loss of top = (indices, logits, temperature) in its place.
+    body(x (tokens, d)) returns (y, pull), the layers' output and the function
+    from a gradient at y to the one at x; None: no layers. Returns the mean over
+    the tokens that have a loss (0-d, on the device) and the gradients by name;
+    a shared table's is the sum of both ends'."""
+    embed = w["embed"]
+    head = w.get("head", embed)
+    rms = cfg.arch == A.ARCH_QWEN
+    n, d = ids.numel(), embed.shape[1]
+    dev = embed.device
+
+    def rows():
+        return torch.empty(n, dtype=torch.float32, device=dev)
+
+    k = 1 if top is None else top[0].shape[-1]
+    ws = A.workspace(max(A.adadsf_head_workspace_size(n, d, head.shape[0], head.dtype, k),
+                         A.adadsf_norm_backward_workspace_size(n, d),
+                         A.adadsf_embed_backward_workspace_size(n, embed.shape[0], d)), dev)
+    x = torch.empty(n, d, dtype=embed.dtype, device=dev)
+    A.adadsf_embed_forward(ids, embed, x, scale=scale, ws=ws, stream=stream)
+    y, pull = (x, None) if body is None else body(x)
+    h, mean, rstd = torch.empty_like(y), None if rms else rows(), rows()
+    A.adadsf_norm_forward(y, w["final_w"], w.get("final_b"), h, cfg.norm_eps, mean, rstd, stream=stream)
+    loss, lse = rows(), rows()
+    acc = torch.zeros(2, dtype=torch.float64, device=dev)
+    grads = {"head" if "head" in w else "embed": torch.empty_like(head), "final_w": torch.empty(d, device=dev)}
+    if not rms:
+        grads["final_b"] = torch.empty(d, device=dev)
+    grad_h = torch.empty_like(h)
+    if top is None:
+        A.adadsf_head_loss(h, head, target, loss, lse, acc=acc, ws=ws, stream=stream)
+    else:
+        A.adadsf_distill_loss(h, head, top[0], top[1], top[2], loss, lse, acc=acc, ws=ws, stream=stream)
+    count = acc[1].clamp(min=1.0)
+    share = (1.0 / count).float().expand(n).contiguous()
+    grad_head = grads["head" if "head" in w else "embed"]
+    if top is None:
+        A.adadsf_head_loss_backward(h, head, target, lse, grad_loss=share, grad_h=grad_h, grad_w=grad_head, ws=ws, stream=stream)
+    else:
+        A.adadsf_distill_loss_backward(h, head, top[0], top[1], lse, top[2], grad_loss=share, grad_h=grad_h,
+                                       grad_w=grad_head, ws=ws, stream=stream)
+    A.adadsf_norm_backward(grad_h, y, w["final_w"], rstd, grad_h, mean=mean, grad_w=grads["final_w"],
+                           grad_b=grads.get("final_b"), ws=ws, stream=stream)
+    grad_x = grad_h if pull is None else pull(grad_h)
+    tied = "head" not in w
+    if not tied:
+        grads["embed"] = torch.empty_like(embed)
+    A.adadsf_embed_backward(ids, grad_x, grads["embed"], scale=scale, accumulate=tied, ws=ws, stream=stream)
+    return acc[0] / count, grads
+
+
+def ends_step(cfg: A.ModelCfg, w: dict, ids: torch.Tensor, target: Optional[torch.Tensor], lr: float,
+              body: Optional[Callable] = None, top: Optional[tuple] = None, scale: float = 1.0, stream=None):
+    """One plain SGD step on the tensors of w (in place) by ends_gradients;
+    returns the loss before it."""
+    loss, grads = ends_gradients(cfg, w, ids, target, body, top, scale, stream)
+    for name, g in grads.items():
+        w[name].copy_(w[name].float().sub_(g.float(), alpha=lr))
+    return loss

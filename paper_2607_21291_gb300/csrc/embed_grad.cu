@@ -2,7 +2,7 @@
 //   y_i = s E[id_i],   dE[v] = s sum of dy_i over id_i = v
 //
 // Backward: the tokens are sorted by id (equal ones by place), then summed along the sorted list: a group of
-// threads walks kEgRun places, adds the rows of one id in fp32 and writes an id's row when all of its places are
+// threads walks a run of places, adds the rows of one id in fp32 and writes an id's row when all of its places are
 // its own. Sums of ids that go over a border are left beside the table and joined in order, so that a
 // token that makes up a tenth of the batch is shared by many groups. Nothing depends on the order in which
 // blocks run. Sorting: every token counts the ones before it where there are few (n^2 comparisons in one launch,
@@ -17,7 +17,6 @@
 namespace adadsf {
 namespace {
 
-constexpr int kEgRun = 32;          // places a group walks, a lane of each warp a place; a quarter of it where there are few
 constexpr int kEgThreads = 512;     // at most, of a block
 constexpr int kEgFew = 4096;        // tokens up to which each counts the ones before it
 constexpr int kEgLanes = 4;         // lanes that share a token's count
@@ -260,42 +259,48 @@ __global__ void __launch_bounds__(kEgThreads) embed_sum_kernel(const __grid_cons
   const int64_t run = (int64_t)blockIdx.x * p.groups + g;
   if (run >= p.runs) return;
   const bool mine = c < p.nv;
-  const int64_t i0 = run * p.run;
-  const int count = (int)min((int64_t)p.run, p.n - i0);
-  const int32_t key = lane < count ? p.key[i0 + lane] : p.vocab, place = lane < count ? p.place[i0 + lane] : 0;
-  const int32_t before = i0 > 0 ? p.key[i0 - 1] : -1, behind = i0 + count < p.n ? p.key[i0 + count] : -1;
-  const int used = __popc(__ballot_sync(0xffffffffu, key < p.vocab));   // padding sorts last
-  if (used == 0) return;
+  const int64_t i0 = run * p.run, i1 = min(p.n, i0 + p.run);
+  // 32 places at a time, a lane of each warp a place; the next ones are on their way
+  int32_t key = i0 + lane < i1 ? p.key[i0 + lane] : p.vocab, place = i0 + lane < i1 ? p.place[i0 + lane] : 0;
+  const int32_t before = i0 > 0 ? p.key[i0 - 1] : -1, behind = i1 < p.n ? p.key[i1] : -1;
   const uint4* dy = static_cast<const uint4*>(p.dy);
   int32_t id = __shfl_sync(0xffffffffu, key, 0);
+  if (id >= p.vocab) return;
   bool began = id == before;   // the id's first place is another group's
   float s[V] = {};
-  for (int i = 0; i < used; i += kEgAhead) {
-    uint4 u[kEgAhead];
+  for (int64_t at = i0; at < i1; at += 32) {
+    const int used = __popc(__ballot_sync(0xffffffffu, key < p.vocab));   // padding sorts last
+    const int64_t ahead = at + 32 + lane;
+    const int32_t next_key = ahead < i1 ? p.key[ahead] : p.vocab, next_place = ahead < i1 ? p.place[ahead] : 0;
+    for (int i = 0; i < used; i += kEgAhead) {
+      uint4 u[kEgAhead];
 #pragma unroll
-    for (int a = 0; a < kEgAhead; ++a) {
-      const int32_t at = __shfl_sync(0xffffffffu, place, (i + a) & 31);
-      u[a] = mine && i + a < used ? dy[(int64_t)at * p.nv + c] : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int a = 0; a < kEgAhead; ++a) {
-      const int32_t now = __shfl_sync(0xffffffffu, key, (i + a) & 31);
-      if (i + a >= used) break;
-      if (now != id) {
-        if (mine) {
-          if (began) put_carry<V>(p, run * 2, c, s);
-          else write_row<T>(p, id, c, s);
-        }
-        began = false;
-        id = now;
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = 0.f;
+      for (int a = 0; a < kEgAhead; ++a) {
+        const int32_t from = __shfl_sync(0xffffffffu, place, (i + a) & 31);
+        u[a] = mine && i + a < used ? dy[(int64_t)from * p.nv + c] : make_uint4(0, 0, 0, 0);
       }
-      float f[V];
-      unpack16(u[a], f, T());
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[j] += f[j];
+      for (int a = 0; a < kEgAhead; ++a) {
+        const int32_t now = __shfl_sync(0xffffffffu, key, (i + a) & 31);
+        if (i + a >= used) break;
+        if (now != id) {
+          if (mine) {
+            if (began) put_carry<V>(p, run * 2, c, s);
+            else write_row<T>(p, id, c, s);
+          }
+          began = false;
+          id = now;
+#pragma unroll
+          for (int j = 0; j < V; ++j) s[j] = 0.f;
+        }
+        float f[V];
+        unpack16(u[a], f, T());
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] += f[j];
+      }
     }
+    key = next_key;
+    place = next_place;
   }
   if (!mine) return;
   if (began) put_carry<V>(p, run * 2, c, s);
@@ -349,9 +354,13 @@ struct EgPlan {
   int64_t runs, per_tile;
   int run, tiles, bits, passes, digit;
 };
-EgPlan plan(int64_t n, int vocab) {
+EgPlan plan(int64_t n, int vocab, int d) {
+  n = std::max<int64_t>(n, 1);
   EgPlan q;
-  q.run = n <= kEgFew ? kEgRun / 4 : kEgRun;
+  // Long runs leave fewer sums beside the table; short ones give every SM some 16 warps (8 bf16 features a thread, and
+  // as many for fp32, whose plan is the same).
+  const int64_t warps = n * ((d / 8 + 31) / 32);
+  q.run = warps / 128 >= 2432 ? 128 : warps / 32 >= 2432 ? 32 : 8;
   q.runs = (n + q.run - 1) / q.run;
   q.bits = 1;
   while (q.bits < 31 && ((int64_t)1 << q.bits) <= vocab) ++q.bits;   // keys 0 .. vocab
@@ -385,13 +394,13 @@ cudaError_t embed_scale(int dtype, const int32_t* ids, int64_t n, const void* ta
 }
 
 size_t embed_backward_scratch(int64_t n, int vocab, int d) {
-  const EgPlan q = plan(n, vocab);
+  const EgPlan q = plan(n, vocab, d);
   return 4 * up256((size_t)n * 4) + up256((size_t)q.tiles * sizeof(int32_t) << q.digit) + up256((size_t)q.runs * 2 * d * 4);
 }
 
 cudaError_t embed_backward(int dtype, const int32_t* ids, const void* dy, int64_t n, int vocab, int d, float scale, void* out,
                            bool add, void* scratch, const Dev& dev) {
-  const EgPlan q = plan(n, vocab);
+  const EgPlan q = plan(n, vocab, d);
   uint8_t* at = static_cast<uint8_t*>(scratch);
   auto take = [&](size_t bytes) {
     void* r = at;

@@ -380,7 +380,7 @@ cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int 
 }
 
 cudaError_t head_forward(int dtype, const Head& a, const Dev& dev) {
-  const bool few = a.n <= kHeadFewRows;
+  const bool few = a.n <= (dtype == kBF16 ? kHeadFewRows : kHeadFewRowsF32);
   int records = (a.V + 127) / 128;
   cudaError_t e = dtype == kBF16 ? pack<bf16>(a, false, !few, dev) : pack<float>(a, false, !few, dev);
   if (e == cudaSuccess) e = few ? head_few(dtype, a, dev, &records) : head_stats(dtype, a, dev);

@@ -1,15 +1,20 @@
-// The losses' forward pass for few rows (at most kHeadFewRows): what bounds it is reading the head once.
+// The losses' forward pass for few rows (at most kHeadFewRows, fp32 kHeadFewRowsF32): what bounds it is reading the head once.
 //
 // The operands change places against head_tc.cu: 128 classes are the M of a product and the packed rows, up to
 // 128 in steps of 16, its N, so that the tensor cores spend on a block of classes what its rows need (with 256 rows
-// a tile, 24 rows took as long as 256: 20 us for the Pythia-160M head, now FEWUS). A CTA takes one range of
+// a tile, 24 rows took as long as 256). A CTA takes one range of
 // classes, in units of 32, and keeps a running maximum and sum of exponentials a row: one record a CTA and row.
 // fp32: the head's numbers are split into their three bf16 parts (see next_parts) on the way into shared
-// memory, by warps that read them a block ahead; a pass of its own wrote and read again 4.5 times the head's bytes.
+// memory, by warps that read them a block ahead; a pass of its own wrote and read again three times the head's bytes.
+// The rows' parts lie one behind the other, so that w1 (h2, h3) and w2 (h1, h2) are one product each, beside w3 h1
+// and w1 h1: four products a step in place of six. The large one, w1 h1, has columns of its own, since what an
+// addition cuts off goes by the accumulator (see head_tc.cu, also for the chunks of k).
+// Measured, a graph's pass: FEWMEASURED
 //   warp 0       TMA: the rows' blocks of 64 k (fp32: three parts), the head's blocks (bf16)
 //   warp 1       TMEM, MMA issue (one thread), accumulators double-buffered
-//   warps 2-9    epilogue: four warps take 32 rows of a tile through shared memory, which turns classes into columns
-//   warps 10-17  fp32: the head's parts
+//   then 8 (fp32 12) warps, epilogue: four of them take 32 rows of a tile through shared memory, which turns classes
+//                into columns
+//   then 8 warps, fp32: the head's parts
 // Every wait is bounded in time (device error word on give-up).
 #include <cuda.h>
 
@@ -24,25 +29,31 @@ constexpr int kHfM = 128;                        // classes of a tile
 constexpr int kHfUnit = 32;                      // classes of a box
 constexpr int kHfK = 64;
 constexpr int kHfPart = kHfM * kHfK * 2;         // bytes of a block of classes (one part)
-constexpr int kHfEpiWarps = 8, kHfConvWarps = 8;
+constexpr int kHfConvWarps = 8;
 constexpr int kHfOutLd = kHfM + 4;               // floats of a staged row
 constexpr int kHfOut = 32 * kHfOutLd * 4;        // 32 rows of a tile
 constexpr int kHfMaxStages = 8;
 constexpr int kHfBars = 2 * kHfMaxStages + 5;
-constexpr int kHfRing = 196608;
-constexpr int kHfSmem = 1024 + kHfRing + 2 * kHfOut + kHfBars * 8 + 16;
 constexpr uint32_t kHfDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
 
 template <bool F32>
 struct HfCfg {
   static constexpr int PARTS = F32 ? 3 : 1;
-  static constexpr int TERMS = F32 ? kHeadTerms : 1;
-  static constexpr int THREADS = 64 + 32 * kHfEpiWarps + (F32 ? 32 * kHfConvWarps : 0);
+  static constexpr int COLS = F32 ? 256 : 128;   // of an accumulator
+  static constexpr int GROUPS = F32 ? 3 : 2;     // of four epilogue warps
+  static constexpr int TURNS = F32 ? 1 : 2;      // times 32 rows that a group takes
+  static constexpr int EPI = 4 * GROUPS;
+  static constexpr int CHUNK = F32 ? 8 : 16;     // blocks of 64 k that share an accumulator (see head_tc.cu)
+  static constexpr int THREADS = 64 + 32 * (EPI + (F32 ? kHfConvWarps : 0));
+  static constexpr int RING = F32 ? 2 * 3 * (kHfPart + kHeadFewRowsF32 * 128) : 196608;
+  static constexpr int SMEM = 1024 + RING + GROUPS * kHfOut + kHfBars * 8 + 16;
   __host__ __device__ static int stage(int n) { return PARTS * (kHfPart + n * 128); }
   __host__ __device__ static int stages(int n) {
-    const int s = kHfRing / stage(n);
+    const int s = RING / stage(n);
     return s < kHfMaxStages ? s : kHfMaxStages;
   }
+  static_assert(32 * GROUPS * TURNS >= (F32 ? kHeadFewRowsF32 : kHeadFewRows), "rows");
+  static_assert(PARTS * (F32 ? kHeadFewRowsF32 : kHeadFewRows) <= COLS, "columns");
 };
 
 struct HfDev {
@@ -98,8 +109,8 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const uint32_t ring = smem_u32(smem);
-  float* outs = reinterpret_cast<float*>(smem + kHfRing);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kHfRing + 2 * kHfOut);
+  float* outs = reinterpret_cast<float*>(smem + C::RING);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::RING + C::GROUPS * kHfOut);
   const uint32_t full0 = smem_u32(bars);
   const uint32_t empty0 = full0 + 8 * kHfMaxStages;
   const uint32_t tfull0 = empty0 + 8 * kHfMaxStages;
@@ -123,7 +134,7 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(tfull0 + 8 * a, 1);
-      mbar_init(tempty0 + 8 * a, kHfEpiWarps);
+      mbar_init(tempty0 + 8 * a, C::EPI);
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -134,7 +145,7 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     tma_prefetch_desc(&tmH);
     if (!F32) tma_prefetch_desc(&tmW);   // boxes of a whole tile; tmW1: of a unit
   }
-  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 256);
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 2 * C::COLS);
   __syncwarp();
   tc_fence_before();
   __syncthreads();
@@ -200,7 +211,7 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     // ------------------------------------------------------------ MMA issuer
     // all lanes come along, one of them issues: with warp-uniform operands a product takes no moves between
     // register files, which took longer than a product of few columns
-    const uint32_t idesc = idesc_bf16_f32(kHfM, p.n), lead = lane == 0;
+    const uint32_t idesc = idesc_bf16_f32(kHfM, p.n), idesc2 = idesc_bf16_f32(kHfM, 2 * p.n), lead = lane == 0;
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -209,34 +220,44 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
       if (lane == 0) got = mbar_wait_bounded(bar, parity, abort_flag, p.err, p.timeout_ns);
       return __shfl_sync(0xffffffffu, got, 0) != 0;
     };
-    for (int it = 0; it < tiles && ok; ++it) {
-      const int acc = it & 1;
-      if (!wait(tempty0 + 8 * acc, ((it >> 1) & 1) ^ 1)) break;
-      tc_fence_after();
-      const uint32_t d = tmem_base + acc * 128;
-      for (int kb = 0; kb < nkb; ++kb) {
-        if (!wait(full0 + 8 * stage, phase)) {
+    int it = 0;
+    for (int tile = 0; tile < tiles && ok; ++tile) {
+      for (int first = 0; first < nkb && ok; first += C::CHUNK, ++it) {
+        const int acc = it & 1, blocks = min(C::CHUNK, nkb - first);
+        if (!wait(tempty0 + 8 * acc, ((it >> 1) & 1) ^ 1)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        const uint32_t w_s = ring + stage * stage_bytes, h_s = w_s + C::PARTS * kHfPart;
+        const uint32_t d = tmem_base + acc * C::COLS;
+        for (int kb = 0; kb < blocks; ++kb) {
+          if (!wait(full0 + 8 * stage, phase)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t w_s = ring + stage * stage_bytes, h_s = w_s + C::PARTS * kHfPart;
+          const uint32_t w = (w_s & 0x3FFFFu) >> 4 | 1u << 16, h = (h_s & 0x3FFFFu) >> 4 | 1u << 16;
+          const uint32_t w1 = kHfPart >> 4, h1 = p.n * 8;   // a part on, in 16 bytes
 #pragma unroll
-        for (int term = 0; term < C::TERMS; ++term) {
-          // the head is A here, the rows B
-          const uint32_t a = ((w_s + (F32 ? head_part_b(term) * kHfPart : 0)) & 0x3FFFFu) >> 4 | 1u << 16;
-          const uint32_t b = ((h_s + (F32 ? head_part_a(term) * p.n * 128 : 0)) & 0x3FFFFu) >> 4 | 1u << 16;
-#pragma unroll
-          for (int k = 0; k < kHfK / 16; ++k) few_mma(d, a + 2 * k, b + 2 * k, idesc, kb > 0 || term > 0 || k > 0 ? 1u : 0u, lead);
+          for (int k = 0; k < 2 * kHfK / 16; k += 2) {
+            const uint32_t more = kb > 0 || k > 0 ? 1u : 0u;
+            if (F32) {
+              few_mma(d + p.n, w + k, h + h1 + k, idesc2, more, lead);
+              few_mma(d + p.n, w + w1 + k, h + k, idesc2, 1u, lead);
+              few_mma(d + p.n, w + 2 * w1 + k, h + k, idesc, 1u, lead);
+            }
+            few_mma(d, w + k, h + k, idesc, more, lead);
+          }
+          few_commit(empty0 + 8 * stage, lead);
+          if (++stage == stages) { stage = 0; phase ^= 1; }
         }
-        few_commit(empty0 + 8 * stage, lead);
-        if (++stage == stages) { stage = 0; phase ^= 1; }
+        if (ok) few_commit(tfull0 + 8 * acc, lead);
       }
-      if (ok) few_commit(tfull0 + 8 * acc, lead);
     }
     few_commit(drain, lead);
     if (lane == 0) mbar_wait_drain(drain, 0, p.timeout_ns);
-  } else if (warp < 2 + kHfEpiWarps) {
+  } else if (warp < 2 + C::EPI) {
     // ------------------------------------------------------------ epilogue
     pdl_wait();
     const int count = *p.count;
@@ -244,32 +265,58 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     const int t = quarter * 32 + lane, r = t >> 2, q = t & 3;   // thread of the group; its row of 32, its quarter of the classes
     const float c = p.inv_t * 1.4426950408889634f;
     float* out = outs + group * (kHfOut / 4);
-    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-    int next[2] = {0, 0};
+    float top[C::TURNS], sum[C::TURNS];
+    int next[C::TURNS];
     const int chunks = (min(count, p.n) + 31) / 32;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int m = (group + 2 * u) * 32 + r;
+    for (int u = 0; u < C::TURNS; ++u) {
+      const int m = (group + C::GROUPS * u) * 32 + r;
+      top[u] = -INFINITY;
+      sum[u] = 0.f;
       next[u] = q == 0 && m < count ? first_class(p.cls + (int64_t)p.rows[m] * p.k, p.k, c_begin) : p.k;
     }
     bool ok = true;
-    for (int it = 0; it < tiles; ++it) {
-      const int acc = it & 1, c0 = c_begin + it * kHfM, c1 = min(c_end, c0 + kHfM);
-      int got = 0;
-      if (lane == 0) got = mbar_wait_bounded(tfull0 + 8 * acc, (it >> 1) & 1, abort_flag, p.err, p.timeout_ns);
-      ok = __shfl_sync(0xffffffffu, got, 0) != 0;
-      // the four warps of a group go on or leave together: they share barriers
-      if (!group_agrees(1 + group, ok)) break;
-      tc_fence_after();
+    int it = 0;
+    for (int tile = 0; tile < tiles && ok; ++tile) {
+      const int c0 = c_begin + tile * kHfM, c1 = min(c_end, c0 + kHfM);
+      float run[C::TURNS][32];
+      for (int first = 0; first < nkb; first += C::CHUNK, ++it) {
+        const int acc = it & 1;
+        int got = 0;
+        if (lane == 0) got = mbar_wait_bounded(tfull0 + 8 * acc, (it >> 1) & 1, abort_flag, p.err, p.timeout_ns);
+        // the four warps of a group go on or leave together: they share barriers
+        ok = group_agrees(1 + group, __shfl_sync(0xffffffffu, got, 0) != 0);
+        if (!ok) break;
+        tc_fence_after();
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int chunk = group + 2 * u;
+        for (int u = 0; u < C::TURNS; ++u) {
+          if (group + C::GROUPS * u >= chunks) continue;
+          const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * C::COLS + (group + C::GROUPS * u) * 32;
+#pragma unroll
+          for (int b = 0; b < 32; b += 8) {
+            uint32_t v[C::PARTS][8];
+#pragma unroll
+            for (int part = 0; part < C::PARTS; ++part) tmem_ld8(from + part * p.n + b, v[part]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              float x = __uint_as_float(v[0][j]);
+              if (F32) x += __uint_as_float(v[1 % C::PARTS][j]) + __uint_as_float(v[2 % C::PARTS][j]);
+              run[u][b + j] = first ? run[u][b + j] + x : x;
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int u = 0; u < C::TURNS; ++u) {
+        const int chunk = group + C::GROUPS * u;
         if (chunk >= chunks) continue;
-        uint32_t v[32];
-        tmem_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * 128 + chunk * 32, v);
-        tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) out[j * kHfOutLd + t] = __uint_as_float(v[j]);
+        for (int j = 0; j < 32; ++j) out[j * kHfOutLd + t] = run[u][j];
         named_bar_sync(1 + group, 128);
         const int m = chunk * 32 + r;
         const float* row = out + r * kHfOutLd;
@@ -299,13 +346,10 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
         }
         named_bar_sync(1 + group, 128);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(tempty0 + 8 * acc);
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int m = (group + 2 * u) * 32 + r;
+    for (int u = 0; u < C::TURNS; ++u) {
+      const int m = (group + C::GROUPS * u) * 32 + r;
       float most = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
       float s = sum[u] * (top[u] == most ? 1.f : ex2_approx((top[u] - most) * c));
@@ -315,11 +359,11 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     }
   } else if (F32) {
     // ------------------------------------------------------------ the head's parts
-    const int w = warp - 2 - kHfEpiWarps, k4 = lane & 15, r0 = w * 16 + (lane >> 4);
+    const int w = warp - 2 - C::EPI, k4 = lane & 15, r0 = w * 16 + (lane >> 4);
     int stage = 0;
     uint32_t phase = 0;
     const int total = tiles * nkb;
-    float4 f[2][8];
+    float4 f[8];
     int c0 = c_begin, k0 = 0;   // of the block that is loaded next
     auto load = [&](float4 (&g)[8]) {
       const int k = k0 + 4 * k4;
@@ -357,14 +401,8 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
       if (++stage == stages) { stage = 0; phase ^= 1; }
       return true;
     };
-    load(f[0]);
-    load(f[1]);
-    for (int i = 0; i < total; i += 2) {
-      if (!put(f[0])) break;
-      load(f[0]);
-      if (i + 1 >= total || !put(f[1])) break;
-      load(f[1]);
-    }
+    load(f);
+    for (int i = 0; i < total && put(f); ++i) load(f);
   }
 
   __syncwarp();
@@ -372,13 +410,13 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, 256);
+    tmem_dealloc(tmem_base, 2 * C::COLS);
   }
 }
 
 template <bool F32>
 cudaError_t launch_few(const Head& a, const Dev& dev, int* records) {
-  const cudaError_t e = allow_smem<head_few_kernel<F32>, kHfSmem>();
+  const cudaError_t e = allow_smem<head_few_kernel<F32>, HfCfg<F32>::SMEM>();
   if (e != cudaSuccess) return e;
   HfDev p = {};
   p.n = (int)((a.n + 15) / 16 * 16);
@@ -402,7 +440,7 @@ cudaError_t launch_few(const Head& a, const Dev& dev, int* records) {
   p.err = dev.err;
   p.timeout_ns = kWaitTimeoutNs;
   *records = (int)std::min<int64_t>(std::min(dev.num_sms, kHeadFewCtas), ((int64_t)a.V + kHfUnit - 1) / kHfUnit);
-  return launch_pdl(head_few_kernel<F32>, dim3((unsigned)*records), dim3(HfCfg<F32>::THREADS), kHfSmem, dev.stream, th, tw, tw1, p);
+  return launch_pdl(head_few_kernel<F32>, dim3((unsigned)*records), dim3(HfCfg<F32>::THREADS), HfCfg<F32>::SMEM, dev.stream, th, tw, tw1, p);
 }
 
 }  // namespace

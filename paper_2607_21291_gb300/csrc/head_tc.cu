@@ -16,10 +16,16 @@
 // K-major or MN-major (64 of M or N a 128-byte line), by descriptor, from the same TMA boxes of 64 x 64.
 // G is rounded to bf16 because the tensor cores take it so; rows' weights enter it as shares of the largest one,
 // so that equal weights leave its roundings independent (a common factor of 1 / 3580 rounded every target's
-// entry the same way: gradients 2.8e-3 off, now NEWERR), and the gradients that it enters are rounded to bf16 as well.
+// entry the same way: gradients 2.8e-3 off, now 1.9e-3), and the gradients that it enters are rounded to bf16 as well.
 //
 // fp32: every operand is three bf16 numbers whose sum it is (8 bits each, next_parts), and a product of two is six of their nine
 // products, the least first, in the same accumulators; the three that are left out are below 2^-24 of it.
+//
+// The tensor cores cut what an addition loses instead of rounding it, so a sum of many steps drifts towards zero: 320 steps
+// of 16 k were 1e-5 of a logit off, which its exponential multiplies (fp32 gradients 5e-5). Where fp32 results come
+// of it (logits of the forward pass, all fp32 products) a tile's k are cut in chunks of at most 64 steps (fp32: 32, each of
+// which holds its six products), whose accumulators the epilogue's threads add up in registers, rounding, while the next
+// chunk is multiplied.
 //   warp 0     TMA: A and B tiles of 64 k, 6 stages of 32 KB (both CTAs)
 //   warp 1     TMEM, MMA issue (one thread of the even CTA)
 //   warps 2-9  epilogue (two per TMEM lane quarter, 128 columns each)
@@ -152,6 +158,10 @@ __device__ __forceinline__ uint32_t out_at(int row, int piece) { return (uint32_
 __device__ __forceinline__ void red_add4(float* p, const float4& v) {
   asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
+
+// Blocks of 64 k whose products share an accumulator.
+template <bool GRAD, bool F32>
+__host__ __device__ constexpr int chunk_blocks() { return F32 ? 8 : GRAD ? 1 << 20 : 16; }
 
 struct Walk {   // a row's targets, from the first one at or past the tile's first class
   const int32_t* cls;
@@ -429,7 +439,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
   pdl_wait();
   const int count = *p.count;
   const Tiles<GRAD> tiles(p, count);
-  constexpr int TERMS = F32 ? kHeadTerms : 1;
+  constexpr int TERMS = F32 ? kHeadTerms : 1, CHUNK = chunk_blocks<GRAD, F32>();
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
@@ -441,8 +451,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       for (int t = pair; t < tiles.n && ok; t += num_pairs) {
         const Tile ti = tiles.at(p, count, t);
         const int a0 = ti.mb * kHtTile + (int)rank * 128, b0 = ti.nb * kHtTile + (int)rank * 128;
-        int kb = 0, term = 0;
-        int64_t pa = 0, pb = 0;   // rows before the parts
+        int first = 0, kb = 0, term = 0;   // of the chunk, in it, and the product of parts
+        int64_t pa = 0, pb = 0;            // rows before the parts
         auto parts = [&] {
           if (!F32) return;
           pa = head_part_a(term) * p.cap;
@@ -456,7 +466,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
           }
           const uint32_t fb = full_lead + 8 * stage, a_s = ring + stage * kHtStage, b_s = a_s + kHtOperand;
           if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * stage, 2 * kHtStage);
-          const int k0 = (ti.kb0 + kb) * kHtK;
+          const int k0 = (ti.kb0 + first + kb) * kHtK;
           if (!GRAD || ti.kind == kG) {   // H and W, both K-major: boxes of 64 rows
             const int a = (int)(a0 + pa), b = (int)((GRAD ? p.v_g : 0) + b0 + pb);
             tma_load_2d_pair(a_s, &tmH, k0, a, fb);
@@ -476,9 +486,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
             tma_load_2d_pair(b_s, &tmH, b0, b, fb);
             tma_load_2d_pair(b_s + kHtBox, &tmH, b0 + 64, b, fb);
           }
-          if (++kb == ti.nkb) {
+          if (++kb == min(CHUNK, ti.nkb - first)) {
             kb = 0;
-            ++term;
+            if (++term == TERMS) {
+              term = 0;
+              first += CHUNK;
+            }
             parts();
           }
           ++issued;
@@ -503,31 +516,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       uint32_t phase = 0;
       int it = 0;
       bool ok = true;
-      for (int t = pair; t < tiles.n && ok; t += num_pairs, ++it) {
+      for (int t = pair; t < tiles.n && ok; t += num_pairs) {
         const Tile ti = tiles.at(p, count, t);
-        const int acc = it & 1;
-        if (!mbar_wait_bounded(tempty0 + 8 * acc, ((it >> 1) & 1) ^ 1, abort_flag, p.err, p.timeout_ns)) break;
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + acc * 256;
         const bool a_mn = GRAD && ti.kind == kDW, b_mn = GRAD && (ti.kind == kDW || ti.kind == kDH);
         const uint32_t id = idesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
         const uint32_t a_hi = a_mn ? kMajorMN : kMajorK, b_hi = b_mn ? kMajorMN : kMajorK;
         const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 k on, in 16 bytes
-        for (int kb = 0; kb < ti.nkb * TERMS; ++kb) {
-          if (!mbar_wait_bounded(full0 + 8 * stage, phase, abort_flag, p.err, p.timeout_ns)) {
+        int first = 0;
+        do {   // a chunk (one without blocks where there is no k)
+          const int acc = it & 1, blocks = min(CHUNK, ti.nkb - first) * TERMS;
+          if (!mbar_wait_bounded(tempty0 + 8 * acc, ((it >> 1) & 1) ^ 1, abort_flag, p.err, p.timeout_ns)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t a_s = ring + stage * kHtStage;
-          const uint32_t a_lo = ((a_s & 0x3FFFFu) >> 4) | a_hi, b_lo = (((a_s + kHtOperand) & 0x3FFFFu) >> 4) | b_hi;
+          const uint32_t d_tmem = tmem_base + acc * 256;
+          for (int kb = 0; kb < blocks; ++kb) {
+            if (!mbar_wait_bounded(full0 + 8 * stage, phase, abort_flag, p.err, p.timeout_ns)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t a_s = ring + stage * kHtStage;
+            const uint32_t a_lo = ((a_s & 0x3FFFFu) >> 4) | a_hi, b_lo = (((a_s + kHtOperand) & 0x3FFFFu) >> 4) | b_hi;
 #pragma unroll
-          for (int k = 0; k < kHtK / 16; ++k)
-            tc_mma_f16_pair(d_tmem, desc_of(a_lo + k * a_step), desc_of(b_lo + k * b_step), id, (kb > 0 || k > 0) ? 1u : 0u);
-          tc_commit_pair_multicast(empty0 + 8 * stage, 0x3);   // both CTAs' stage free
-          if (++stage == kHtStages) { stage = 0; phase ^= 1; }
-        }
-        if (ok) tc_commit_pair_multicast(tfull0 + 8 * acc, 0x3);   // both CTAs' accumulators ready
+            for (int k = 0; k < kHtK / 16; ++k)
+              tc_mma_f16_pair(d_tmem, desc_of(a_lo + k * a_step), desc_of(b_lo + k * b_step), id, (kb > 0 || k > 0) ? 1u : 0u);
+            tc_commit_pair_multicast(empty0 + 8 * stage, 0x3);   // both CTAs' stage free
+            if (++stage == kHtStages) { stage = 0; phase ^= 1; }
+          }
+          if (!ok) break;
+          tc_commit_pair_multicast(tfull0 + 8 * acc, 0x3);   // both CTAs' accumulators ready
+          ++it;
+          first += CHUNK;
+        } while (first < ti.nkb);
       }
       tc_commit_pair_multicast(drain, 0x1);
       mbar_wait_drain(drain, 0, p.timeout_ns);
@@ -537,28 +559,72 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     uint8_t* out = outs + (warp - 2) * kHtOut;
     int it = 0;
-    for (int t = pair; t < tiles.n; t += num_pairs, ++it) {
+    bool ok = true;
+    for (int t = pair; t < tiles.n && ok; t += num_pairs) {
       const Tile ti = tiles.at(p, count, t);
-      const int acc = it & 1;
       const int m0 = ti.mb * kHtTile + (int)rank * 128 + quarter * 32, m = m0 + lane;
       Walk w;
       if (!GRAD || ti.kind == kG) {   // the row's targets are found under the tile's products
         const bool live = m < count;
         w.start(p.cls + (live ? (int64_t)p.rows[m] * p.k : 0), p.k, (GRAD ? p.v_g : 0) + ti.nb * kHtTile + half * 128, live);
       }
-      int ok = 0;
-      if (lane == 0) ok = mbar_wait_bounded(tfull0 + 8 * acc, (it >> 1) & 1, abort_flag, p.err, p.timeout_ns);
-      ok = __shfl_sync(0xffffffffu, ok, 0);
+      const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 128;
+      auto wait = [&] {
+        int got = 0;
+        if (lane == 0) got = mbar_wait_bounded(tfull0 + 8 * (it & 1), (it >> 1) & 1, abort_flag, p.err, p.timeout_ns);
+        ok = __shfl_sync(0xffffffffu, got, 0) != 0;
+        tc_fence_after();
+      };
+      auto release = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(tempty_lead + 8 * (it & 1));
+        ++it;
+      };
+      wait();
       if (!ok) break;
-      tc_fence_after();
-      const uint32_t tacc = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * 256 + half * 128;
+      if ((F32 || !GRAD) && ti.nkb > CHUNK) {
+        float run[128];
+        int first = CHUNK;
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(lanes + (it & 1) * 256 + c, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) run[c + i] = __uint_as_float(r[i]);
+        }
+        release();
+        for (;;) {
+          wait();
+          if (!ok) break;
+          first += CHUNK;
+          const bool last = first >= ti.nkb;
+#pragma unroll
+          for (int c = 0; c < 128; c += 16) {
+            uint32_t r[16];
+            tmem_ld8(lanes + (it & 1) * 256 + c, r);
+            tmem_ld8(lanes + (it & 1) * 256 + c + 8, r + 8);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              run[c + i] += __uint_as_float(r[i]);
+              r[i] = __float_as_uint(run[c + i]);
+            }
+            if (last) tmem_st16(lanes + (it & 1) * 256 + c, r);   // where the tile's epilogue finds them
+          }
+          if (last) break;
+          release();
+        }
+        if (!ok) break;
+        tmem_st_wait();
+      }
+      const uint32_t tacc = lanes + (it & 1) * 256;
       if (!GRAD) stats_tile(p, ti, m, half, m < count, tacc, w);
       else if (ti.kind == kG) g_tile<F32>(p, ti, m, half, m < count, tacc, w, out, lane);
       else if (ti.kind == kDH) dh_tile(p, ti, m0, count, half, tacc, out, lane);
       else dw_tile<F32>(p, ti, p.v_d + m0, half, tacc, out, lane);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(tempty_lead + 8 * acc);
+      release();
     }
   }
 

@@ -345,8 +345,8 @@ cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int 
                          float* ent, int32_t* target, const Dev& dev);
 cudaError_t head_forward(int dtype, const Head& a, const Dev& dev);
 cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev);
-// head_few.cu: stats for at most kHeadFewRows rows, one record a CTA (their number in *records).
-constexpr int kHeadFewRows = 128, kHeadFewCtas = 160;
+// head_few.cu: stats for at most kHeadFewRows (fp32: kHeadFewRowsF32) rows, one record a CTA (their number in *records).
+constexpr int kHeadFewRows = 128, kHeadFewRowsF32 = 80, kHeadFewCtas = 160;
 cudaError_t head_few(int dtype, const Head& a, const Dev& dev, int* records);
 // head_tc.cu: stats of all tiles; one launch of the backward pass -- G of the n_g classes from v_g into G[buf], the
 // gradients of the n_d classes from v_d from the other buffer.

@@ -69,11 +69,22 @@ def teacher_want(idx, logit, V, temp):
     return want, used, torch.special.xlogy(p, p).sum(-1)
 
 
+def terms(m, f32, grad):
+    """Additions that lose up to 2u each in a sum of m products. A step of the tensor cores adds 16 products and the sum so
+    far, 17 terms; where fp32 comes of it, a sum is of chunks of 32 steps (bf16 logits 64), added in fp32; bf16
+    gradients are one chain."""
+    if grad and not f32:
+        return m + 64
+    steps = 32 if f32 else 64
+    return min(m, 17 * steps) + m / (16 * steps) + 64
+
+
 class Ref:
     """The losses and gradients in 64 bits, and how far the kernels may be from them."""
 
     def __init__(self, h, w, want, used, ent, gl, temp, k):
         bf = h.dtype == torch.bfloat16
+        products = 6 if not bf else 1   # of parts, with what is left out of them: 2^-22 of a product
         h, w, gl = h.double(), w.double(), (torch.ones(h.shape[0], device="cuda") if gl is None else gl).double()
         h = torch.where(used[:, None], h, 0.0)
         d, V = w.shape[1], w.shape[0]
@@ -85,7 +96,7 @@ class Ref:
         # a logit: a sum of d products, and its scale; an exponential: 2^-22 and its argument's two roundings; the sum of
         # them: 16 terms a chain, 4 chunks, and the records (V / 128 over 32 threads, then 32)
         far = z.abs().amax(-1) + self.lse.abs()
-        e_z = (2 * d + 4) * U * size
+        e_z = (2 * terms(products * d, not bf, False) + 4) * U * size
         e_lse = e_z + 4 * U + 4 * U * far + 2 * U * (64 + V / 4096 + 32) + 2 * U * self.lse.abs()
         self.e_lse = torch.where(used, e_lse, 0.0)
         # targets: a sum of k weights times logits, the entropy's like it
@@ -93,14 +104,16 @@ class Ref:
         q = torch.exp(z - self.lse[:, None])
         s = torch.where(used, gl * temp, 0.0)[:, None]
         G = (q - want) * s
+        e_z = (2 * terms(products * d, not bf, True) + 4) * U * size   # of the backward pass's logits
         e_q = (e_z + e_lse + 4 * U + 4 * U * far)[:, None] * q * s.abs() + 4 * U * (q + want) * s.abs()
         e_g = e_q + (B16 * (G.abs() + e_q) if bf else 2 * U * G.abs())
         self.dh, self.dw = G @ w, G.T @ h
         out = B16 if bf else U
         n = h.shape[0]
-        self.e_dh = (e_g + 2 * U * (V + 64) * G.abs()) @ w.abs()
+        t_v, t_n = terms(products * V, not bf, True), terms(products * n, not bf, True)
+        self.e_dh = (e_g + 2 * U * t_v * G.abs()) @ w.abs()
         self.e_dh += out * (self.dh.abs() + self.e_dh)
-        self.e_dw = (e_g + 2 * U * (n + 64) * G.abs()).T @ h.abs()
+        self.e_dw = (e_g + 2 * U * t_n * G.abs()).T @ h.abs()
         self.e_dw += out * (self.dw.abs() + self.e_dw)
         # roundings of G are independent: their part of a gradient has a 2-norm of about b / sqrt(3) (sum G^2 W^2)^(1/2);
         # twice that, and the outputs' own roundings
@@ -111,8 +124,8 @@ class Ref:
             self.n_dh += self.e_dh.norm()
             self.n_dw += self.e_dw.norm()
         else:
-            self.n_dh += 2 * U * ((V + 64) * (G.abs() @ w.abs())).norm()
-            self.n_dw += 2 * U * ((n + 64) * (G.abs().T @ h.abs())).norm()
+            self.n_dh += 2 * U * (t_v * (G.abs() @ w.abs())).norm()
+            self.n_dw += 2 * U * (t_n * (G.abs().T @ h.abs())).norm()
 
     def check(self, loss, lse, dh, dw, base=None):
         if lse is not None:
@@ -146,7 +159,8 @@ def ce(A, h, w, target, gl=None, grads=True, ws=None, stream=None):
 HEADS = [(1, 64, 100, "bf16"), (3, 8, 1, "bf16"), (24, 768, 5003, "bf16"), (130, 200, 257, "bf16"), (257, 520, 1000, "bf16"),
          (300, 768, 1280, "bf16"), (700, 264, 255, "bf16"), (9000, 64, 12001, "bf16"),
          (65, 64, 31, "bf16"), (97, 136, 33, "bf16"), (128, 136, 20011, "bf16"), (129, 72, 300, "bf16"),
-         (33, 4, 5000, "f32"), (128, 100, 20011, "f32"), (129, 68, 300, "f32"),
+         (33, 4, 5000, "f32"), (80, 100, 20011, "f32"), (81, 68, 300, "f32"), (40, 5124, 700, "f32"),
+         (200, 5124, 700, "f32"), (40, 5128, 700, "bf16"), (200, 5128, 700, "bf16"),
          (1, 4, 1, "f32"), (5, 132, 130, "f32"), (77, 512, 3001, "f32"), (515, 100, 777, "f32"), (9000, 32, 6002, "f32")]
 
 
@@ -566,3 +580,71 @@ def test_embed_backward_captured(A):
         got = table.clone()
         A.adadsf_embed_backward(ids, dy, table, ws=ws)
         assert torch.equal(got, table)
+
+
+# ------------------------------------------------------------------ a run of them together
+@pytest.mark.parametrize("arch,dtype,tied,teacher", [("neox", "bf16", True, False), ("qwen", "bf16", False, True),
+                                                     ("neox", "f32", True, True), ("qwen", "f32", True, False)])
+def test_ends_together(A, arch, dtype, tied, teacher):
+    """Embedding, a stand-in for the layers, final norm, head, loss and back, as a training step calls them (align.py),
+    against 64-bit autograd of the same composition. bf16 rounds five tensors on the way (rows, normed rows, the logits'
+    gradients, the norm's and the outputs): each is off by 2^-8 / sqrt(3) of its size at most on average, through a norm
+    and products that carry it on at about its relative size: 2-norms within 5 x 2^-8. fp32: chains as in test_head_loss,
+    of sizes that random signs leave far below their bound: 1e-5."""
+    from paper_2607_21291_gb300 import align
+    from paper_2607_21291_gb300 import synth as S
+    d, V, B, T = 128, 700, 3, 50
+    shape = (S.PYTHIA_70M if arch == "neox" else S.QWEN25_1_5B).replace(d=d, vocab=V, dtype=dtype)
+    cfg = A.make_cfg(shape)
+    g = gen(17)
+    td = DT[dtype]
+    w = {"embed": randn(g, V, d, std=0.3).to(td), "final_w": (1 + randn(g, d, std=0.1)).to(td)}
+    if arch == "neox":
+        w["final_b"] = randn(g, d, std=0.1).to(td)
+    if not tied:
+        w["head"] = randn(g, V, d, std=0.1).to(td)
+    ids = torch.randint(0, V, (B, T), generator=g, device="cuda", dtype=torch.int32)
+    target = torch.roll(ids, -1, 1).contiguous()
+    ids[2, 30:] = -1
+    target[:, -1] = -1
+    target[2, 29:] = -1
+    target[0, :7] = -1
+    top = None
+    if teacher:
+        idx = torch.randint(0, V, (B * T, 6), generator=g, device="cuda", dtype=torch.int32)
+        idx[target.reshape(-1) < 0] = -1
+        top = (idx, randn(g, B * T, 6, std=2.0), 1.5)
+    turn = randn(g, d, d, std=d ** -0.5).to(td)
+
+    def body(x):
+        return (x.float() @ turn.float()).to(td), lambda gy: (gy.float() @ turn.float().T).to(td)
+
+    loss, grads = align.ends_gradients(cfg, w, ids, target, body=body, top=top, scale=2.0)
+    leaf = {k: v.double().requires_grad_(True) for k, v in w.items()}
+    used = ids.reshape(-1) >= 0
+    x = torch.where(used[:, None], leaf["embed"][ids.reshape(-1).clamp(min=0).long()] * 2.0, 0.0)
+    y = x @ turn.double()
+    c = y if arch == "qwen" else y - y.mean(-1, keepdim=True)
+    hid = c * (c.square().mean(-1, keepdim=True) + shape.norm_eps) ** -0.5 * leaf["final_w"]
+    if arch == "neox":
+        hid = hid + leaf["final_b"]
+    z = hid @ leaf["embed" if tied else "head"].T
+    if teacher:
+        temp = top[2]
+        want, valid, ent = teacher_want(top[0], top[1], V, temp)
+    else:
+        temp, (want, valid) = 1.0, want_of(target.reshape(-1), V)
+        ent = torch.zeros(B * T, dtype=torch.float64, device="cuda")
+    row = temp ** 2 * (ent - (want * torch.log_softmax(z / temp, -1)).sum(-1))
+    mean = torch.where(valid, row, 0.0).sum() / valid.sum()
+    ref = dict(zip(leaf, torch.autograd.grad(mean, list(leaf.values()))))
+    tol = 5 * B16 if dtype == "bf16" else 1e-5
+    assert float(loss) == pytest.approx(float(mean), rel=tol)
+    assert set(grads) == set(ref)
+    for k in ref:
+        assert float((grads[k].double() - ref[k]).norm()) <= tol * float(ref[k].norm()), k
+    before = {k: v.clone() for k, v in w.items()}
+    assert float(align.ends_step(cfg, w, ids, target, 0.5, body=body, top=top, scale=2.0)) == float(loss)
+    for k in w:   # one rounding of the update
+        step = before[k].double() - 0.5 * grads[k].double()
+        within(w[k], step, (B16 if dtype == "bf16" else U) * 2 * step.abs() + 1e-7, k)
