@@ -1839,6 +1839,7 @@ adadsf_status head_prepare(const HeadCall& c, void* ws, size_t ws_bytes, void* s
   a->dh_acc = at<float>(ws, l->acc);
   a->piece = l->plan.piece;
   a->splits = l->plan.splits;
+  a->dh_whole = l->plan.pieces == 1 && l->plan.splits == 1;
   if (c.target) {
     a->target = a->cls = c.target;
     return ADADSF_OK;
@@ -1876,8 +1877,8 @@ adadsf_status run_head_grad(const HeadCall& c, const float* lse, const float* gr
   if (!grad_h && !grad_w) return fail(ADADSF_ERR_INVALID_ARG, "grad_h_dev and grad_w_dev are both NULL");
   if (grad_h) NEED_PTR(grad_h, "grad_h_dev");
   if (grad_w) NEED_PTR(grad_w, "grad_w_dev");
-  if (grad_w && (grad_w == c.w || grad_w == c.h))
-    return fail(ADADSF_ERR_INVALID_ARG, "grad_w_dev is an input's buffer");
+  for (const void* g : {grad_h, grad_w})
+    if (g && (g == c.w || g == c.h)) return fail(ADADSF_ERR_INVALID_ARG, "a gradient's buffer is h_dev or w_head_dev");
   TRY(need_row(lse, "lse_dev", c.n == 0));
   TRY(need_row(grad_loss, "grad_loss_dev", true));
   if (c.n == 0) {

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kTeacherThreads)
 
 constexpr int kPackThreads = 256;
 
-// Rows with a target, in order: their numbers, their count and a copy of their features. Every block counts all
+// Rows with a target, in order: their numbers, their count and a copy of their features (of bf16 rows that all have one none). Every block counts all
 // targets by itself (no launch before it, no order between blocks). Rows without one get a loss, a
 // logarithm and a gradient of zero; what they hold is read by nobody. Packed rows past the last one, up to a
 // multiple of kHeadZeroPad, are zero: products over rows run that far.
@@ -182,6 +182,7 @@ __global__ void __launch_bounds__(kPackThreads)
     __syncthreads();
     const int in_chunk = (int)min((int64_t)kPackThreads, r1 - c);
     for (int i = warp; i < in_chunk; i += W) {
+      if (PARTS == 1 && all == n) break;   // the products read the rows where they are
       if (at[i] >= 0) {
         put_row(h + (c + i) * d, packed + (int64_t)at[i] * ld, cap * ld, d, ld, lane);
       } else if (dh) {
@@ -190,6 +191,7 @@ __global__ void __launch_bounds__(kPackThreads)
       }
     }
   }
+  if (PARTS == 1 && all == n) return;
   const int tail = (kHeadZeroPad - all % kHeadZeroPad) % kHeadZeroPad;
   for (int i = (int)(blockIdx.x + gridDim.x * warp); i < tail; i += (int)gridDim.x * W) {
     for (int q = 0; q < PARTS; ++q) {
@@ -313,6 +315,7 @@ __global__ void __launch_bounds__(256)
     float s[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = 0.f;
+#pragma unroll 8
     for (int q = 0; q < splits; ++q) {
       const float* a = acc + q * stride + m * d + c;
 #pragma unroll
@@ -359,12 +362,12 @@ HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
   piece = ((padded + pieces - 1) / pieces + 255) / 256 * 256;
   q.piece = (int)piece;
   q.pieces = (int)((V + piece - 1) / piece);
-  // dH sums over a piece's classes: cut so that its tiles are about as long as the others
+  // dH sums over a piece's classes: cut so that its tiles are about as long as the others, into no more than four, or what
+  // gives every pair of SMs two tiles where there are few rows (their parts are added up again)
   const int64_t other = std::max<int64_t>(std::max<int64_t>(q.cap, d), 1024);
   const int64_t tiles = std::max<int64_t>(1, q.cap / tile * ((d + tile - 1) / tile));
   int64_t splits = std::max<int64_t>(1, (piece + other / 2) / other);
-  splits = std::min<int64_t>(splits, std::max<int64_t>(1, 1024 / tiles));
-  q.splits = (int)std::min<int64_t>(splits, 64);
+  q.splits = (int)std::min<int64_t>(splits, std::max<int64_t>(4, (160 + tiles - 1) / tiles));
   q.packed = (size_t)(parts * q.cap * q.ld * 2);
   q.w_parts = dtype == kBF16 ? 0 : (size_t)(parts * q.Vp * q.ld * 2);
   q.rec = (size_t)(std::max<int64_t>(padded / 128, kHeadFewCtas) * q.cap * 8);
@@ -402,7 +405,7 @@ cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const 
     const int n_d = j > 0 ? (int)std::min<int64_t>(plan.piece, a.V - before) : 0;
     e = head_grad(dtype, a, j & 1, v, n_g, before, n_d, j == 1, dev);
   }
-  if (e != cudaSuccess || !a.dh) return e;
+  if (e != cudaSuccess || !a.dh || a.dh_whole) return e;
   const int blocks = (int)std::min<int64_t>((a.n * a.d / 4 + 255) / 256, 8 * dev.num_sms);
   if (dtype == kBF16)
     return launch_pdl(head_finish_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, dev.stream, (const float*)a.dh_acc,

@@ -60,7 +60,7 @@ struct HfDev {
   const int32_t *count, *rows;
   const float* w;            // fp32 head
   int64_t cap;
-  int d, V, n;               // n: rows, a multiple of 16
+  int d, V, n, n_rows;       // n: rows, to a multiple of 16
   float inv_t;
   const int32_t* cls;
   int k;
@@ -103,7 +103,7 @@ __device__ __forceinline__ bool group_agrees(int id, bool ok) {
 
 template <bool F32>
 __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
-    head_few_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW,
+    head_few_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                     const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ HfDev p) {
   using C = HfCfg<F32>;
   extern __shared__ uint8_t smem_raw[];
@@ -142,7 +142,8 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     fence_proxy_async_smem();
   }
   if (warp == 0 && lane == 0) {
-    tma_prefetch_desc(&tmH);
+    tma_prefetch_desc(&tmP);
+    if (!F32) tma_prefetch_desc(&tmA);
     if (!F32) tma_prefetch_desc(&tmW);   // boxes of a whole tile; tmW1: of a unit
   }
   if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 2 * C::COLS);
@@ -182,6 +183,7 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
       const int pre = F32 ? 0 : min(total, stages);
       for (int i = 0; i < pre; ++i) head(i);
       pdl_wait();
+      const CUtensorMap& tmH = !F32 && *p.count == p.n_rows ? tmA : tmP;   // bf16 rows that all count were not packed
       int k = 0;
       for (int i = 0; i < total && ok; ++i) {
         if (i >= pre) {
@@ -420,10 +422,12 @@ cudaError_t launch_few(const Head& a, const Dev& dev, int* records) {
   if (e != cudaSuccess) return e;
   HfDev p = {};
   p.n = (int)((a.n + 15) / 16 * 16);
-  CUtensorMap th, tw = {}, tw1 = {};
+  p.n_rows = (int)a.n;
+  CUtensorMap th, ta = {}, tw = {}, tw1 = {};
   if (!make_tmap_bf16(&th, a.packed, (uint64_t)a.cap * (F32 ? 3 : 1), (uint64_t)a.ld, (uint64_t)a.ld, kHfK, (uint32_t)p.n))
     return cudaErrorInvalidValue;
-  if (!F32 && (!make_tmap_bf16(&tw, a.w, (uint64_t)a.V, (uint64_t)a.d, (uint64_t)a.d, kHfK, kHfM) ||
+  if (!F32 && (!make_tmap_bf16(&ta, a.h, (uint64_t)a.n, (uint64_t)a.d, (uint64_t)a.d, kHfK, (uint32_t)p.n) ||
+               !make_tmap_bf16(&tw, a.w, (uint64_t)a.V, (uint64_t)a.d, (uint64_t)a.d, kHfK, kHfM) ||
                !make_tmap_bf16(&tw1, a.w, (uint64_t)a.V, (uint64_t)a.d, (uint64_t)a.d, kHfK, kHfUnit)))
     return cudaErrorInvalidValue;
   p.count = a.count;
@@ -440,7 +444,7 @@ cudaError_t launch_few(const Head& a, const Dev& dev, int* records) {
   p.err = dev.err;
   p.timeout_ns = kWaitTimeoutNs;
   *records = (int)std::min<int64_t>(std::min(dev.num_sms, kHeadFewCtas), ((int64_t)a.V + kHfUnit - 1) / kHfUnit);
-  return launch_pdl(head_few_kernel<F32>, dim3((unsigned)*records), dim3(HfCfg<F32>::THREADS), HfCfg<F32>::SMEM, dev.stream, th, tw, tw1, p);
+  return launch_pdl(head_few_kernel<F32>, dim3((unsigned)*records), dim3(HfCfg<F32>::THREADS), HfCfg<F32>::SMEM, dev.stream, th, ta, tw, tw1, p);
 }
 
 }  // namespace

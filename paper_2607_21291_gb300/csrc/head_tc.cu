@@ -58,6 +58,7 @@ enum { kStats = 0, kG = 1, kDH = 2, kDW = 3 };
 struct HtDev {
   const int32_t* count;      // packed rows
   const int32_t* rows;       // their rows
+  int n;                     // rows
   int64_t cap;               // rows of the packed buffers, and of G
   int d, V, Vp;              // Vp: rows of a part of the head
   float inv_t;
@@ -77,6 +78,7 @@ struct HtDev {
   int splits, want_h, want_w, first, add_w;
   int ld_g;
   bf16* G;                   // the piece of the G tiles
+  void* dh;                  // where a row's gradient is one sum; else null and its parts go to
   float* acc;                // [splits][cap][d]
   void* dw;
   int* err;
@@ -162,6 +164,12 @@ __device__ __forceinline__ void red_add4(float* p, const float4& v) {
 // Blocks of 64 k whose products share an accumulator.
 template <bool GRAD, bool F32>
 __host__ __device__ constexpr int chunk_blocks() { return F32 ? 8 : GRAD ? 1 << 20 : 16; }
+
+// A warp's loads from TMEM are done (tcgen05.wait::ld): only that is told, so the arrival is relaxed. Released, it waits
+// until the warp's stores to global memory are performed (gradients of 500 tokens at the Qwen2.5-7B head 1104 -> 1079 us).
+__device__ __forceinline__ void arrive_read(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
 
 struct Walk {   // a row's targets, from the first one at or past the tile's first class
   const int32_t* cls;
@@ -317,9 +325,44 @@ __device__ __forceinline__ void g_tile(const HtDev& p, const Tile& ti, int m, in
   }
 }
 
+template <bool F32>
 __device__ __forceinline__ void dh_tile(const HtDev& p, const Tile& ti, int m0, int count, int half, uint32_t tacc, uint8_t* out,
                                         int lane) {
   const int c0 = ti.nb * kHtTile + half * 128;
+  if (p.dh) {   // all classes in one sum: no partial sums to be joined
+    using T = typename std::conditional<F32, float, bf16>::type;
+    constexpr int V = Elem<T>::kVec, COLS = 8 * V;
+    const float scale = *p.g_ref * p.temp;
+    const int64_t row = m0 + lane < count ? p.rows[m0 + lane] : -1;
+#pragma unroll 1
+    for (int c = 0; c < 128; c += COLS) {
+      if (c0 + c >= p.d) break;
+#pragma unroll
+      for (int h = 0; h < COLS; h += 32) {
+        uint32_t r[32];
+        tmem_ld32(tacc + c + h, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < 32 / V; ++q) {
+          float f[V];
+#pragma unroll
+          for (int i = 0; i < V; ++i) f[i] = __uint_as_float(r[V * q + i]) * scale;
+          *reinterpret_cast<uint4*>(out + out_at(lane, h / V + q)) = pack16(f, T());
+        }
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int rr = i * 4 + (lane >> 3), piece = lane & 7;
+        const uint4 v = *reinterpret_cast<const uint4*>(out + out_at(rr, piece));
+        const int64_t to = __shfl_sync(0xffffffffu, row, rr);
+        if (to >= 0 && c0 + c + piece * V < p.d)
+          *reinterpret_cast<uint4*>(static_cast<T*>(p.dh) + to * p.d + c0 + c + piece * V) = v;
+      }
+      __syncwarp();
+    }
+    return;
+  }
   float* dst = p.acc + ((int64_t)ti.slot * p.cap + m0) * p.d + c0;
 #pragma unroll 1
   for (int ch = 0; ch < 4; ++ch) {
@@ -346,36 +389,53 @@ __device__ __forceinline__ void dh_tile(const HtDev& p, const Tile& ti, int m0, 
   }
 }
 
-template <bool F32>
-__device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, int half, uint32_t tacc, uint8_t* out, int lane) {
+// 32 columns of the accumulator as this thread's part of the head's gradient, in vectors.
+template <typename T>
+__device__ __forceinline__ void dw_columns(const HtDev& p, const Tile& ti, uint32_t tacc, float scale, const T* old_row, bool in_row,
+                                           int cols, uint4* held) {
+  constexpr int V = Elem<T>::kVec;
+  uint32_t r[32];
+  tmem_ld32(tacc, r);
+  tmem_ld_wait();
+#pragma unroll
+  for (int q = 0; q < 32 / V; ++q) {
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = ti.nkb ? __uint_as_float(r[V * q + i]) * scale : 0.f;
+    if (p.add_w && in_row && q * V < cols) {   // what is there is added before the one rounding
+      float old[V];
+      load_vec(old_row + q * V, old);
+#pragma unroll
+      for (int i = 0; i < V; ++i) f[i] += old[i];
+    }
+    held[q] = pack16(f, T());
+  }
+}
+
+// Rows of the head's gradient. bf16: the accumulator is free again (release) before the stores: with few rows a
+// tile has one block of products, and its stores are what there is to do. (fp32 has no registers for that.)
+template <bool F32, typename Release>
+__device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, int half, uint32_t tacc, uint8_t* out, int lane,
+                                        Release release) {
   using T = typename std::conditional<F32, float, bf16>::type;
   constexpr int V = Elem<T>::kVec, COLS = 8 * V;   // columns of 128 bytes
   const float scale = *p.g_ref * p.temp;
   const int c0 = ti.nb * kHtTile + half * 128;
   T* dst = static_cast<T*>(p.dw) + (int64_t)v0 * p.d + c0;
-#pragma unroll 1
+  const bool in_row = v0 + lane < p.V;
+  uint4 held[F32 ? 8 : 16];
+  if (!F32) {
+#pragma unroll
+    for (int c = 0; c < 128; c += 32)
+      dw_columns<T>(p, ti, tacc + c, scale, dst + (int64_t)lane * p.d + c, in_row, p.d - c0 - c, held + (F32 ? 0 : c / V));
+    release();
+  }
+#pragma unroll
   for (int c = 0; c < 128; c += COLS) {
     if (c0 + c >= p.d) break;
-#pragma unroll 1
-    for (int h = 0; h < COLS; h += 32) {
-      uint32_t r[32];
-      tmem_ld32(tacc + c + h, r);
-      tmem_ld_wait();
+    if (F32) dw_columns<T>(p, ti, tacc + c, scale, dst + (int64_t)lane * p.d + c, in_row, p.d - c0 - c, held);
 #pragma unroll
-      for (int q = 0; q < 32 / V; ++q) {
-        float f[V];
-        const int col = c + h + q * V;
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = ti.nkb ? __uint_as_float(r[V * q + i]) * scale : 0.f;
-        if (p.add_w && v0 + lane < p.V && c0 + col < p.d) {   // what is there is added before the one rounding
-          float old[V];
-          load_vec(dst + (int64_t)lane * p.d + col, old);
-#pragma unroll
-          for (int i = 0; i < V; ++i) f[i] += old[i];
-        }
-        *reinterpret_cast<uint4*>(out + out_at(lane, h / V + q)) = pack16(f, T());
-      }
-    }
+    for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(out + out_at(lane, q)) = held[F32 ? q : c / V + q];
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -385,11 +445,12 @@ __device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, 
     }
     __syncwarp();
   }
+  if (F32) release();
 }
 
 template <bool GRAD, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
-    head_tc_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW,
+    head_tc_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                    const __grid_constant__ CUtensorMap tmG, const __grid_constant__ HtDev p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -424,7 +485,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
     fence_barrier_init();
   }
   if (warp == 0 && lane == 0) {
-    tma_prefetch_desc(&tmH);
+    tma_prefetch_desc(&tmP);
+    if (!F32) tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmW);
     if (GRAD) tma_prefetch_desc(&tmG);
   }
@@ -438,6 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
   const uint32_t tempty_lead = map_to_cta(tempty0, 0);
   pdl_wait();
   const int count = *p.count;
+  const CUtensorMap& tmH = !F32 && count == p.n ? tmA : tmP;   // bf16 rows that all count were not packed
   const Tiles<GRAD> tiles(p, count);
   constexpr int TERMS = F32 ? kHeadTerms : 1, CHUNK = chunk_blocks<GRAD, F32>();
 
@@ -578,7 +641,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       auto release = [&] {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(tempty_lead + 8 * (it & 1));
+        if (lane == 0) arrive_read(tempty_lead + 8 * (it & 1));
         ++it;
       };
       wait();
@@ -622,9 +685,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       const uint32_t tacc = lanes + (it & 1) * 256;
       if (!GRAD) stats_tile(p, ti, m, half, m < count, tacc, w);
       else if (ti.kind == kG) g_tile<F32>(p, ti, m, half, m < count, tacc, w, out, lane);
-      else if (ti.kind == kDH) dh_tile(p, ti, m0, count, half, tacc, out, lane);
-      else dw_tile<F32>(p, ti, p.v_d + m0, half, tacc, out, lane);
-      release();
+      else if (ti.kind == kDH) dh_tile<F32>(p, ti, m0, count, half, tacc, out, lane);
+      else dw_tile<F32>(p, ti, p.v_d + m0, half, tacc, out, lane, release);
+      if (!GRAD || ti.kind != kDW) release();
     }
   }
 
@@ -648,6 +711,7 @@ HtDev head_dev(const Head& a, const Dev& dev) {
   HtDev p = {};
   p.count = a.count;
   p.rows = a.rows;
+  p.n = (int)a.n;
   p.cap = a.cap;
   p.d = a.d;
   p.V = a.V;
@@ -673,10 +737,11 @@ template <bool GRAD, bool F32>
 cudaError_t launch_tiles(int64_t tiles, const Head& a, const CUtensorMap& tg, const HtDev& p, const Dev& dev) {
   const cudaError_t e = allow_smem<head_tc_kernel<GRAD, F32>, kHtSmem>();
   if (e != cudaSuccess || tiles == 0) return e;
-  CUtensorMap th, tw;
+  CUtensorMap th, ta = {}, tw;
   if (!head_maps(F32, a, &th, &tw)) return cudaErrorInvalidValue;
+  if (!F32 && !make_tmap_bf16(&ta, a.h, (uint64_t)a.n, (uint64_t)a.d, (uint64_t)a.d, 64, 64)) return cudaErrorInvalidValue;
   const int pairs = (int)std::min<int64_t>(tiles, dev.num_sms / 2);
-  return launch_pdl(head_tc_kernel<GRAD, F32>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, tw, tg, p);
+  return launch_pdl(head_tc_kernel<GRAD, F32>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, ta, tw, tg, p);
 }
 
 }  // namespace
@@ -704,6 +769,7 @@ cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, i
   p.add_w = a.add_w;
   p.ld_g = a.piece;
   p.G = static_cast<bf16*>(a.G[buf]);
+  p.dh = a.dh_whole ? a.dh : nullptr;
   p.acc = a.dh_acc;
   p.dw = a.dw;
   const int64_t mbs = ceil_to(a.n, kHtTile), nbd = ceil_to(a.d, kHtTile);

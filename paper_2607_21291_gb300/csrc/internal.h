@@ -331,6 +331,7 @@ struct Head {
   bool add_w;
   void* G[2];                            // bf16 [cap][piece]; fp32: three parts
   int piece, splits;
+  bool dh_whole;                         // one piece, one split
   float* dh_acc;                         // [splits][cap][d]
 };
 struct HeadPlan {

@@ -23,7 +23,7 @@ BF, F = 1, 0
 
 
 def head(A, backward=False, **kw):
-    a = dict(h=P, w=2 * P, target=P, n=10, d=64, V=100, dtype=BF, loss=P, lse=P, acc=None, g=None, dh=P, dw=3 * P, add=0, ws=P,
+    a = dict(h=P, w=2 * P, target=P, n=10, d=64, V=100, dtype=BF, loss=P, lse=P, acc=None, g=None, dh=4 * P, dw=3 * P, add=0, ws=P,
              ws_bytes=WS)
     a.update(kw)
     base = (a["h"], a["w"], a["target"], a["n"], a["d"], a["V"], a["dtype"])
@@ -33,7 +33,7 @@ def head(A, backward=False, **kw):
 
 
 def distill(A, backward=False, **kw):
-    a = dict(h=P, w=2 * P, idx=P, logit=P, k=4, temp=1.0, n=10, d=64, V=100, dtype=BF, loss=P, lse=P, acc=None, g=None, dh=P,
+    a = dict(h=P, w=2 * P, idx=P, logit=P, k=4, temp=1.0, n=10, d=64, V=100, dtype=BF, loss=P, lse=P, acc=None, g=None, dh=4 * P,
              dw=3 * P, add=0, ws=P, ws_bytes=WS)
     a.update(kw)
     base = (a["h"], a["w"], a["idx"], a["logit"], a["k"], a["temp"], a["n"], a["d"], a["V"], a["dtype"])
@@ -57,7 +57,8 @@ def test_head_refusals(A):
         for kw, status in [(dict(loss=P + 2), bad), (dict(acc=P + 4), bad), (dict(loss=None, acc=P), bad)]:
             assert call(A, False, **kw) == status, kw
         for kw, status in [(dict(dh=None, dw=None), bad), (dict(dh=P + 8), bad), (dict(dw=P + 2), bad), (dict(add=2), bad),
-                           (dict(g=P + 1), bad), (dict(dw=2 * P), bad)]:
+                           (dict(g=P + 1), bad), (dict(dw=2 * P), bad), (dict(dw=P), bad), (dict(dh=P), bad),
+                           (dict(dh=2 * P), bad)]:
             assert call(A, True, **kw) == status, kw
         assert call(A, False, n=0) == A.OK
     for backward in (False, True):

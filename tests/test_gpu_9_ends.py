@@ -181,6 +181,19 @@ def test_head_loss(A, n, d, V, dtype):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("n,d,V,dtype", [(5, 136, 3000, "bf16"), (128, 64, 700, "bf16"), (130, 200, 900, "bf16"), (513, 72, 5000, "bf16"),
+                                         (3000, 64, 500, "bf16"), (9000, 64, 12001, "bf16"), (81, 64, 700, "f32")])
+def test_every_row_has_a_target(A, n, d, V, dtype):
+    """bf16 rows are then read where they are; they may be the last of their memory."""
+    h, w, target, gl = head_inputs(n, d, V, dtype)
+    target = torch.randint(0, V, (n,), generator=gen(n), device="cuda", dtype=torch.int32)
+    want, used = want_of(target, V)
+    ref = Ref(h, w, want, used, torch.zeros(n, dtype=torch.float64, device="cuda"), gl, 1.0, 1)
+    loss, lse, acc, dh, dw = ce(A, h, w, target, gl)
+    ref.check(loss, lse, dh, dw)
+    assert float(acc[1]) == n
+
+
 def distill_inputs(n, d, V, k, dtype, seed=1):
     h, w, target, gl = head_inputs(n, d, V, dtype, seed)
     g = gen(n * k + V)
