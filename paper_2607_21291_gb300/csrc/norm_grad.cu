@@ -21,7 +21,8 @@ namespace adadsf {
 namespace {
 
 // Threads of a block, at most. Of one vector a thread two blocks share an SM, with 72 registers a thread: with 64 the
-// next rows' statistics were spilled, which waits for them (388 -> 711 us at 65536 x 3584).
+// next rows' statistics were spilled, which waits for them (388 -> 711 us at 65536 x 3584). LayerNorm's gradient of bf16 rows takes
+// one row at a time for the same reason (two: 484 us, one: 328).
 constexpr int ng_threads(int nv) { return nv == 1 ? 448 : 512; }
 constexpr int kNgOneLaunch = 32;   // blocks up to which the last one adds the weights' gradients
 constexpr int ng_rows(int nv) { return nv <= 2 ? 2 : 1; }   // a group works on at a time: their sums share a barrier
@@ -60,28 +61,56 @@ __device__ __forceinline__ uint4 unpairs(const float2 (&f)[P]) {
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
+// Sums of S (1, 2 or 4) values over a warp: lanes halve their values before they halve their distance, so that four sums
+// take 6 shuffles in place of 20. The lane gets the sum of value lane * S / 32.
+template <int S>
+__device__ __forceinline__ float warp_sums(const float (&v)[S], int lane) {
+  float k[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) k[s] = v[s];
+  int distance = 16;
+#pragma unroll
+  for (int n = S; n > 1; n >>= 1, distance >>= 1) {
+    const bool upper = lane & distance;
+#pragma unroll
+    for (int i = 0; i < n / 2; ++i) {
+      const float send = upper ? k[i] : k[i + n / 2], keep = upper ? k[i + n / 2] : k[i];
+      k[i] = keep + __shfl_xor_sync(0xffffffffu, send, distance);
+    }
+  }
+#pragma unroll
+  for (int o = 16 / S; o > 0; o >>= 1) k[0] += __shfl_xor_sync(0xffffffffu, k[0], o);
+  return k[0];
+}
+
 // Sums of S values over a group, in a fixed order; every thread gets them. `turn` alternates, so that one
 // barrier a sum is enough.
 template <int S>
 __device__ __forceinline__ void group_sum(float (&v)[S], float* red, int turn, int group, int g, int warp_in_group, int lane) {
+  constexpr int LANES = 32 / S;   // of a value
+  float mine = warp_sums(v, lane);
+  const int warps = group >> 5, value = lane / LANES, w = lane % LANES;
+  if (warps > 1) {
+    float* r = red + ((turn & 1) * 16 + g * warps) * S;   // at most 16 warps a block
+    if (w == 0) r[warp_in_group * S + value] = mine;
+    named_bar_sync(1 + g, group);
+    mine = w < warps ? r[w * S + value] : 0.f;
+    if (LANES < 16 && w + LANES < warps) mine += r[(w + LANES) * S + value];
 #pragma unroll
-  for (int s = 0; s < S; ++s) v[s] = warp_sum(v[s]);
-  if (group == 32) return;
-  const int warps = group >> 5;   // at most 16 a block
-  float* r = red + ((turn & 1) * 16 + g * warps) * S;
-  if (lane == 0) {
-#pragma unroll
-    for (int s = 0; s < S; ++s) r[warp_in_group * S + s] = v[s];
+    for (int o = (LANES < 16 ? LANES : 16) / 2; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
   }
-  named_bar_sync(1 + g, group);
-  const int w = lane & 15;
 #pragma unroll
-  for (int s = 0; s < S; ++s) v[s] = sum16(w < warps ? r[w * S + s] : 0.f);
+  for (int s = 0; s < S; ++s) v[s] = __shfl_sync(0xffffffffu, mine, s * LANES);
 }
 
 // A thread's ring: N tensors' vectors of ng_depth rows, of which the ones ahead are on their way.
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ float ring_float(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
 }
 template <int N, int NV>
 struct NgRing {
@@ -197,7 +226,7 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_forward_
 
 template <typename T, int NV, bool ADD, bool MEAN>
 __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward_kernel(const __grid_constant__ NgDev p) {
-  constexpr int V = Elem<T>::kVec, N = ADD ? 3 : 2, DEPTH = ng_depth(N, NV), ROWS = ng_rows(NV);
+  constexpr int V = Elem<T>::kVec, N = ADD ? 3 : 2, DEPTH = ng_depth(N, NV), ROWS = MEAN && V == 8 ? 1 : ng_rows(NV);
   extern __shared__ __align__(16) uint8_t ring_smem[];
   __shared__ float red[2 * 16 * 2 * ROWS];
   pdl_wait();
@@ -207,8 +236,9 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
   const int64_t step = (int64_t)gridDim.x * p.groups;
   const float inv_d = 1.f / (float)p.d;
   const NgRing<N, NV> ring = {smem_u32(ring_smem) + 16u * threadIdx.x, (int)blockDim.x};
-  // the rows' statistics, this thread's own copy: [slot][mean, rstd][thread]
-  volatile float* stats = reinterpret_cast<float*>(ring_smem + (size_t)16 * DEPTH * N * NV * blockDim.x) + threadIdx.x;
+  // the rows' statistics [slot][mean, rstd]: a copy a warp, RMSNorm's one number a copy a thread (302 against 325 us at
+  // 65536 x 3584)
+  const uint32_t stats = smem_u32(ring_smem) + 16u * DEPTH * N * NV * blockDim.x + 8u * DEPTH * (MEAN ? threadIdx.x >> 5 : threadIdx.x);
   const uint4 *x_all = static_cast<const uint4*>(p.x), *y_all = static_cast<const uint4*>(p.dy),
               *a_all = static_cast<const uint4*>(p.add);
   auto fetch = [&](int64_t r, int slot) {
@@ -222,9 +252,10 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
       if (ADD) cp_async16(ring.at(slot, N - 1, i), a_all + at, in);
     }
     const bool row_in = r < p.n;
-    const uint32_t st = smem_u32(const_cast<const float*>(stats)) + 4u * (slot * 2 * blockDim.x);
-    if (MEAN) cp_async4(st, p.mean + (row_in ? r : 0), row_in);
-    cp_async4(st + 4u * blockDim.x, p.rstd + (row_in ? r : 0), row_in);
+    if (!MEAN || lane == 0) {
+      if (MEAN) cp_async4(stats + 8u * slot, p.mean + (row_in ? r : 0), row_in);
+      cp_async4(stats + 8u * slot + 4, p.rstd + (row_in ? r : 0), row_in);
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   int64_t row = (int64_t)blockIdx.x * p.groups + g;
@@ -246,12 +277,14 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) fetch(row + (AHEAD + k) * step, (slot + AHEAD + k) % DEPTH);
     asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+    if (MEAN) __syncwarp();   // lane 0's copies of the statistics
     constexpr int S = MEAN ? 2 : 1;
-    float mean[ROWS], rstd[ROWS], s[S * ROWS];
+    float shift[ROWS], rstd[ROWS], s[S * ROWS];   // xhat = x rstd + shift
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) {
-      mean[k] = MEAN ? stats[(slot + k) % DEPTH * 2 * blockDim.x] : 0.f;
-      rstd[k] = stats[((slot + k) % DEPTH * 2 + 1) * blockDim.x];
+      const uint32_t st = stats + 8u * ((slot + k) % DEPTH);
+      rstd[k] = ring_float(st + 4);
+      shift[k] = MEAN ? -ring_float(st) * rstd[k] : 0.f;
       float2 sa = both(0.f), sx = both(0.f);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -262,7 +295,7 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
         pairs(wv[i], w);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-          const float2 xh = __fmul2_rn(MEAN ? __fadd2_rn(x[j], both(-mean[k])) : x[j], both(rstd[k]));
+          const float2 xh = MEAN ? __ffma2_rn(x[j], both(rstd[k]), both(shift[k])) : __fmul2_rn(x[j], both(rstd[k]));
           const float2 a = __fmul2_rn(y[j], w[j]);
           if (MEAN) sa = __fadd2_rn(sa, a);
           sx = __ffma2_rn(a, xh, sx);
@@ -278,8 +311,9 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
     for (int k = 0; k < ROWS; ++k) {
       const int64_t r = row + k * step;
       if (r < p.n) {
-        // dx = rstd a + ((x - mean) by + c1), by = -rstd^2 mean(a xhat), c1 = -rstd mean(a)
-        const float by = -(s[S * k] * inv_d) * rstd[k] * rstd[k], c1 = MEAN ? -(s[S * k + S - 1] * inv_d) * rstd[k] : 0.f;
+        // dx = rstd a + (x by + c1): by = -rstd^2 mean(a xhat), c1 = -rstd (shift mean(a xhat) + mean(a))
+        const float c2 = -(s[S * k] * inv_d) * rstd[k], by = c2 * rstd[k];
+        const float c1 = MEAN ? fmaf(c2, shift[k], -(s[S * k + S - 1] * inv_d) * rstd[k]) : 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const int c = t + i * p.group;
@@ -290,8 +324,7 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
           if (ADD) pairs(ring.read((slot + k) % DEPTH, N - 1, i), o);
 #pragma unroll
           for (int j = 0; j < P; ++j) {
-            const float2 xc = MEAN ? __fadd2_rn(x[j], both(-mean[k])) : x[j];
-            const float2 rest = MEAN ? __ffma2_rn(xc, both(by), both(c1)) : __fmul2_rn(xc, both(by));
+            const float2 rest = MEAN ? __ffma2_rn(x[j], both(by), both(c1)) : __fmul2_rn(x[j], both(by));
             const float2 dx = __ffma2_rn(__fmul2_rn(y[j], w[j]), both(rstd[k]), rest);
             o[j] = ADD ? __fadd2_rn(dx, o[j]) : dx;
           }
@@ -395,7 +428,7 @@ __global__ void __launch_bounds__(1024)
 struct NgPlan {
   int group, groups, nv, blocks;
 };
-constexpr int kNgMaxBlocks = 2 * 152;
+constexpr int kNgMaxBlocks = 3 * 152;
 
 NgPlan plan(int dtype, int64_t n, int d) {
   const int vecs = d / (dtype == kBF16 ? 8 : 4);
@@ -406,14 +439,16 @@ NgPlan plan(int dtype, int64_t n, int d) {
   q.groups = ng_threads(q.nv) / q.group;
   // few rows: a block a row, so that more SMs share them
   while (q.groups > 1 && (n + q.groups - 1) / q.groups < 152) q.groups /= 2;
-  q.blocks = (int)std::min<int64_t>((n + q.groups - 1) / q.groups, kNgMaxBlocks);
+  // what an SM has registers for (72 a thread of one vector)
+  const int per_sm = q.nv == 1 ? std::max(2, 896 / (q.group * q.groups)) : 1;
+  q.blocks = (int)std::min<int64_t>((n + q.groups - 1) / q.groups, 152 * per_sm);
   return q;
 }
 
 // KERNEL with the rings of its threads: N tensors of NV vectors.
 template <auto KERNEL, int N, int NV>
 cudaError_t start(const NgPlan& q, const NgDev& p, const Dev& dev) {
-  constexpr int kThread = ng_depth(N, NV) * (N * NV * 16 + (N > 1 ? 8 : 0));
+  constexpr int kThread = ng_depth(N, NV) * (N * NV * 16 + (N > 1 ? 8 : 0));   // with the rows' statistics
   static_assert(N == 1 || kThread >= NV * 8 * 4, "a ring holds its thread's weight gradients");
   const cudaError_t e = allow_smem<KERNEL, ng_threads(NV) * kThread>();
   const int threads = q.group * q.groups;
