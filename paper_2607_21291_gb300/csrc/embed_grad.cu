@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kEgThreads = 512;     // at most, of a block
 constexpr int kEgFew = 4096;        // tokens up to which each counts the ones before it
-constexpr int kEgLanes = 4;         // lanes that share a token's count
+constexpr int kEgLanes = 16;        // lanes that share a token's count
 constexpr int kEgFewThreads = 128;
 constexpr int kEgSort = 256;        // threads of the digit sort
 constexpr int kEgChunk = kEgSort * 8;
