@@ -171,6 +171,23 @@ __device__ __forceinline__ void arrive_read(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
+// A warp's 32 staged rows of 64 bf16 (swizzled as out_at does) to a matrix of global memory, which cuts them at its edges. The
+// stage is free again after out_free().
+__device__ __forceinline__ void out_store(const CUtensorMap& tm, const uint8_t* out, int col, int row, int lane) {
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(&tm)),
+                 "r"(col), "r"(row), "r"(smem_u32(out))
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+}
+__device__ __forceinline__ void out_free(int lane) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  __syncwarp();
+}
+
 struct Walk {   // a row's targets, from the first one at or past the tile's first class
   const int32_t* cls;
   int j, k, next;
@@ -236,8 +253,8 @@ __device__ __forceinline__ void stats_tile(const HtDev& p, const Tile& ti, int m
 }
 
 template <bool F32>
-__device__ __forceinline__ void g_tile(const HtDev& p, const Tile& ti, int m, int half, bool live, uint32_t tacc, Walk& w,
-                                       uint8_t* out, int lane) {
+__device__ __forceinline__ void g_tile(const HtDev& p, const CUtensorMap& tm, const Tile& ti, int m, int half, bool live, uint32_t tacc,
+                                       Walk& w, uint8_t* out, int lane) {
   constexpr float kLog2e = 1.4426950408889634f;
   const int64_t row = live ? p.rows[m] : 0;
   const float lse = live ? p.lse[row] : 0.f;
@@ -268,6 +285,7 @@ __device__ __forceinline__ void g_tile(const HtDev& p, const Tile& ti, int m, in
         if (!live || cb + i >= p.V) f[i] = 0.f;
     }
     if (!F32) {
+      if (!(c32 & 1)) out_free(lane);
 #pragma unroll
       for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(out + out_at(lane, (c32 & 1) * 4 + q)) = pack16(f + 8 * q, bf16());
     }
@@ -313,14 +331,7 @@ __device__ __forceinline__ void g_tile(const HtDev& p, const Tile& ti, int m, in
         __syncwarp();
       }
     } else if (c32 & 1) {
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int rr = i * 4 + (lane >> 3), piece = lane & 7;
-        const uint4 v = *reinterpret_cast<const uint4*>(out + out_at(rr, piece));
-        *reinterpret_cast<uint4*>(dst + (int64_t)rr * p.ld_g + (c32 - 1) * 32 + piece * 8) = v;
-      }
-      __syncwarp();
+      out_store(tm, out, ti.nb * kHtTile + half * 128 + (c32 - 1) * 32, m0, lane);
     }
   }
 }
@@ -329,6 +340,7 @@ template <bool F32>
 __device__ __forceinline__ void dh_tile(const HtDev& p, const Tile& ti, int m0, int count, int half, uint32_t tacc, uint8_t* out,
                                         int lane) {
   const int c0 = ti.nb * kHtTile + half * 128;
+  if (!F32) out_free(lane);
   if (p.dh) {   // all classes in one sum: no partial sums to be joined
     using T = typename std::conditional<F32, float, bf16>::type;
     constexpr int V = Elem<T>::kVec, COLS = 8 * V;
@@ -415,8 +427,8 @@ __device__ __forceinline__ void dw_columns(const HtDev& p, const Tile& ti, uint3
 // Rows of the head's gradient. bf16: the accumulator is free again (release) before the stores: with few rows a
 // tile has one block of products, and its stores are what there is to do. (fp32 has no registers for that.)
 template <bool F32, typename Release>
-__device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, int half, uint32_t tacc, uint8_t* out, int lane,
-                                        Release release) {
+__device__ __forceinline__ void dw_tile(const HtDev& p, const CUtensorMap& tm, const Tile& ti, int v0, int half, uint32_t tacc,
+                                        uint8_t* out, int lane, Release release) {
   using T = typename std::conditional<F32, float, bf16>::type;
   constexpr int V = Elem<T>::kVec, COLS = 8 * V;   // columns of 128 bytes
   const float scale = *p.g_ref * p.temp;
@@ -434,8 +446,13 @@ __device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, 
   for (int c = 0; c < 128; c += COLS) {
     if (c0 + c >= p.d) break;
     if (F32) dw_columns<T>(p, ti, tacc + c, scale, dst + (int64_t)lane * p.d + c, in_row, p.d - c0 - c, held);
+    if (!F32) out_free(lane);
 #pragma unroll
     for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(out + out_at(lane, q)) = held[F32 ? q : c / V + q];
+    if (!F32) {
+      if (v0 < p.V) out_store(tm, out, c0 + c, v0, lane);
+      continue;
+    }
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -451,7 +468,8 @@ __device__ __forceinline__ void dw_tile(const HtDev& p, const Tile& ti, int v0, 
 template <bool GRAD, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
     head_tc_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
-                   const __grid_constant__ CUtensorMap tmG, const __grid_constant__ HtDev p) {
+                   const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmGo,
+                   const __grid_constant__ CUtensorMap tmDw, const __grid_constant__ HtDev p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const uint32_t ring = smem_u32(smem);
@@ -489,6 +507,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
     if (!F32) tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmW);
     if (GRAD) tma_prefetch_desc(&tmG);
+    if (GRAD && !F32) {
+      tma_prefetch_desc(&tmGo);
+      tma_prefetch_desc(&tmDw);
+    }
   }
   if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), 512);
   __syncwarp();
@@ -684,11 +706,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       }
       const uint32_t tacc = lanes + (it & 1) * 256;
       if (!GRAD) stats_tile(p, ti, m, half, m < count, tacc, w);
-      else if (ti.kind == kG) g_tile<F32>(p, ti, m, half, m < count, tacc, w, out, lane);
+      else if (ti.kind == kG) g_tile<F32>(p, tmGo, ti, m, half, m < count, tacc, w, out, lane);
       else if (ti.kind == kDH) dh_tile<F32>(p, ti, m0, count, half, tacc, out, lane);
-      else dw_tile<F32>(p, ti, p.v_d + m0, half, tacc, out, lane, release);
+      else dw_tile<F32>(p, tmDw, ti, p.v_d + m0, half, tacc, out, lane, release);
       if (!GRAD || ti.kind != kDW) release();
     }
+    if (GRAD && !F32 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // this warp's stores are done
   }
 
   __syncwarp();
@@ -734,14 +757,16 @@ HtDev head_dev(const Head& a, const Dev& dev) {
 int ceil_to(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
 template <bool GRAD, bool F32>
-cudaError_t launch_tiles(int64_t tiles, const Head& a, const CUtensorMap& tg, const HtDev& p, const Dev& dev) {
+cudaError_t launch_tiles(int64_t tiles, const Head& a, const CUtensorMap& tg, const CUtensorMap& tgo, const CUtensorMap& tdw,
+                         const HtDev& p, const Dev& dev) {
   const cudaError_t e = allow_smem<head_tc_kernel<GRAD, F32>, kHtSmem>();
   if (e != cudaSuccess || tiles == 0) return e;
   CUtensorMap th, ta = {}, tw;
   if (!head_maps(F32, a, &th, &tw)) return cudaErrorInvalidValue;
   if (!F32 && !make_tmap_bf16(&ta, a.h, (uint64_t)a.n, (uint64_t)a.d, (uint64_t)a.d, 64, 64)) return cudaErrorInvalidValue;
   const int pairs = (int)std::min<int64_t>(tiles, dev.num_sms / 2);
-  return launch_pdl(head_tc_kernel<GRAD, F32>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, ta, tw, tg, p);
+  return launch_pdl(head_tc_kernel<GRAD, F32>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, ta, tw, tg, tgo, tdw,
+                    p);
 }
 
 }  // namespace
@@ -749,12 +774,16 @@ cudaError_t launch_tiles(int64_t tiles, const Head& a, const CUtensorMap& tg, co
 cudaError_t head_stats(int dtype, const Head& a, const Dev& dev) {
   const int64_t tiles = (int64_t)ceil_to(a.n, kHtTile) * ceil_to(a.V, kHtTile);
   const CUtensorMap none = {};
-  return dtype == kBF16 ? launch_tiles<false, false>(tiles, a, none, head_dev(a, dev), dev)
-                        : launch_tiles<false, true>(tiles, a, none, head_dev(a, dev), dev);
+  return dtype == kBF16 ? launch_tiles<false, false>(tiles, a, none, none, none, head_dev(a, dev), dev)
+                        : launch_tiles<false, true>(tiles, a, none, none, none, head_dev(a, dev), dev);
 }
 
 cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, int64_t v_d, int n_d, bool first, const Dev& dev) {
-  CUtensorMap tg;
+  CUtensorMap tg, tgo = {}, tdw = {};
+  if (dtype == kBF16 &&
+      (!make_tmap_bf16(&tgo, a.G[buf], (uint64_t)a.cap, (uint64_t)a.piece, (uint64_t)a.piece, 64, 32) ||
+       (a.dw && !make_tmap_bf16(&tdw, a.dw, (uint64_t)a.V, (uint64_t)a.d, (uint64_t)a.d, 64, 32))))
+    return cudaErrorInvalidValue;
   if (!make_tmap_bf16(&tg, a.G[buf ^ 1], (uint64_t)a.cap * (dtype == kBF16 ? 1 : 3), (uint64_t)a.piece, (uint64_t)a.piece, 64, 64))
     return cudaErrorInvalidValue;
   HtDev p = head_dev(a, dev);
@@ -774,7 +803,8 @@ cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, i
   p.dw = a.dw;
   const int64_t mbs = ceil_to(a.n, kHtTile), nbd = ceil_to(a.d, kHtTile);
   const int64_t tiles = mbs * p.n_g + (p.want_h && n_d ? mbs * nbd * p.splits : 0) + (p.want_w ? ceil_to(n_d, kHtTile) * nbd : 0);
-  return dtype == kBF16 ? launch_tiles<true, false>(tiles, a, tg, p, dev) : launch_tiles<true, true>(tiles, a, tg, p, dev);
+  return dtype == kBF16 ? launch_tiles<true, false>(tiles, a, tg, tgo, tdw, p, dev)
+                        : launch_tiles<true, true>(tiles, a, tg, tgo, tdw, p, dev);
 }
 
 }  // namespace adadsf
