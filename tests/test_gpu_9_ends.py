@@ -393,6 +393,128 @@ def test_head_captured(A):
         assert torch.equal(big_out[0], ce(A, *big[:3], grads=False)[0])
 
 
+@pytest.mark.parametrize("n,dtype", [(6, "bf16"), (130, "bf16"), (6, "f32"), (130, "f32")])
+def test_head_of_more_than_2_31_numbers(A, n, dtype):
+    """The head and its gradient pass 2^31 elements; the classes at its end, and around the border, as the first ones."""
+    d, V = 2048, 1_100_000
+    g = gen(n)
+    h = randn(g, n, d).to(DT[dtype])
+    w = torch.empty(V, d, dtype=DT[dtype], device="cuda").normal_(0.0, 0.05, generator=g)
+    target = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    border = 2 ** 31 // d
+    target[:4] = torch.tensor([0, border - 1, border, V - 1], device="cuda", dtype=torch.int32)
+    loss, lse, _, dh, dw = ce(A, h, w, target)
+    hd, step = h.double(), 100_000
+    z = torch.cat([hd @ w[c:c + step].double().T for c in range(0, V, step)], 1)
+    size = torch.stack([(hd.abs() @ w[c:c + step].double().abs().T).amax(-1) for c in range(0, V, step)]).amax(0)
+    ref = torch.logsumexp(z, -1)
+    products = 1 if dtype == "bf16" else 6
+    # as Ref's bounds
+    far = z.abs().amax(-1) + ref.abs()
+    e_z = (2 * terms(products * d, dtype == "f32", False) + 4) * U * size
+    e_lse = e_z + 4 * U + 4 * U * far + 2 * U * (64 + V / 4096 + 32) + 2 * U * ref.abs()
+    within(lse, ref, e_lse, "lse")
+    within(loss, ref - z.gather(1, target[:, None].long())[:, 0], e_lse + e_z + 18 * U * (far + 1), "loss")
+    G = torch.exp(z - ref[:, None])
+    e_z = (2 * terms(products * d, dtype == "f32", True) + 4) * U * size
+    e_g = G * (e_z + e_lse + 8 * U + 4 * U * far)[:, None]
+    G[torch.arange(n), target.long()] -= 1
+    out = B16 if dtype == "bf16" else U
+    e_g += 4 * U * (G.abs() + 2 * (G < 0)) + (B16 if dtype == "bf16" else 2 * U) * (G.abs() + e_g)
+    t_v, t_n = terms(products * V, dtype == "f32", True), terms(products * n, dtype == "f32", True)
+    ref_h, e_h = torch.zeros_like(hd), torch.zeros_like(hd)
+    for c in range(0, V, step):
+        wd = w[c:c + step].double()
+        ref_h += G[:, c:c + step] @ wd
+        e_h += (e_g[:, c:c + step] + 2 * U * t_v * G[:, c:c + step].abs()) @ wd.abs()
+    within(dh, ref_h, e_h + out * (ref_h.abs() + e_h), "dh")
+    for c in (0, border - 256, V - 512):
+        at = slice(c, c + 512)
+        ref_w, e_w = G[:, at].T @ hd, (e_g[:, at] + 2 * U * t_n * G[:, at].abs()).T @ hd.abs()
+        within(dw[at], ref_w, e_w + out * (ref_w.abs() + e_w), "dw")
+
+
+def test_head_of_a_million_rows(A):
+    """Rows times classes of a piece pass 2^31; rows without a target among them."""
+    n, d, V = 1_100_000, 64, 2100
+    g = gen(11)
+    h, w = randn(g, n, d).to(torch.bfloat16), randn(g, V, d, std=0.1).to(torch.bfloat16)
+    target = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    target[torch.rand(n, generator=g, device="cuda") < 0.01] = -1
+    loss, lse, acc, dh, _ = ce(A, h, w, target)
+    assert float(acc[1]) == int((target >= 0).sum())
+    for rows in (slice(0, 300), slice(n // 2, n // 2 + 300), slice(n - 300, n)):
+        want, used = want_of(target[rows], V)
+        ref = Ref(h[rows], w, want, used, torch.zeros(300, dtype=torch.float64, device="cuda"), None, 1.0, 1)
+        ref.check(loss[rows], lse[rows], dh[rows], None)
+
+
+@pytest.mark.parametrize("n,dtype", [(20, "bf16"), (300, "bf16"), (20, "f32"), (300, "f32")])
+def test_head_row_of_nan_stays_in_its_row(A, n, dtype):
+    """A NaN or infinity in a row with a target: its own loss and hidden gradient, the others' bits as before."""
+    h, w, target, gl = head_inputs(n, 128, 700, dtype)
+    target[3], target[9] = 5, 6
+    clean = ce(A, h, w, target, gl)
+    h[3, 7], h[9, 11] = math.nan, math.inf
+    got = ce(A, h, w, target, gl)
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[3] = keep[9] = False
+    for i in (0, 1, 3):
+        assert torch.equal(got[i][keep], clean[i][keep])
+    assert not torch.isfinite(got[0][~keep]).any() and torch.isnan(got[3][3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_head_weights_of_rows(A, dtype):
+    """Weights below zero and of zero; what they hold in rows without a target; all of them zero."""
+    n, V = 200, 700
+    h, w, target, gl = head_inputs(n, 128, V, dtype)
+    gl = gl - 0.6
+    gl[5], target[5] = 0.0, 3
+    want, used = want_of(target, V)
+    ref = Ref(h, w, want, used, torch.zeros(n, dtype=torch.float64, device="cuda"), gl, 1.0, 1)
+    clean = ce(A, h, w, target, gl)
+    ref.check(clean[0], clean[1], clean[3], clean[4])
+    odd = gl.clone()
+    odd[~used] = math.inf
+    odd[(~used).nonzero()[0]] = math.nan
+    got = ce(A, h, w, target, odd)
+    assert torch.equal(got[3], clean[3]) and torch.equal(got[4], clean[4])
+    got = ce(A, h, w, target, torch.zeros_like(gl))
+    assert (got[3] == 0).all() and (got[4] == 0).all()
+
+
+def test_calls_at_once(A):
+    """Two streams, a workspace each, calls of different kernels of every operator in flight together."""
+    def work(n, d, V, dtype):
+        h, w, target, gl = head_inputs(n, d, V, dtype)
+        x, wn, b, dy, _ = norm_inputs(n, d, dtype, False, False)
+        size = max(A.adadsf_head_workspace_size(n, d, V, h.dtype), A.adadsf_norm_backward_workspace_size(n, d),
+                   A.adadsf_embed_backward_workspace_size(n, V, d))
+        ws, ids = A.workspace(size), torch.randint(0, V, (n,), device="cuda", dtype=torch.int32)
+
+        def run():
+            table = torch.full_like(w, 7.0)
+            A.adadsf_embed_backward(ids, h, table, ws=ws)
+            return [*ce(A, h, w, target, gl, ws=ws), *norm(A, x, wn, b, dy, None, ws=ws), table]
+        return run
+
+    calls = [work(100, 256, 30000, "bf16"), work(700, 512, 9000, "f32")]
+    want = [c() for c in calls]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(calls[i]())
+    torch.cuda.synchronize()
+    for i in range(2):
+        for outs in got[i]:
+            for x, y in zip(outs, want[i]):
+                assert torch.equal(x, y)
+
+
 # ------------------------------------------------------------------ norms
 def norm_inputs(n, d, dtype, rms, res):
     g = gen(n * 7 + d)
@@ -500,6 +622,35 @@ def test_norm_row_of_one_value(A):
     assert torch.equal(got[0][7], b) and torch.equal(got[0][8], b)
 
 
+@pytest.mark.parametrize("rms", [False, True])
+def test_norm_of_more_than_2_31_numbers(A, rms):
+    n, d = 1_060_000, 2048
+    g = gen(5)
+    x = torch.empty(n, d, dtype=torch.bfloat16, device="cuda").normal_(0.0, 1.0, generator=g)
+    dy = torch.empty_like(x).normal_(0.0, 1.0, generator=g)
+    w = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    b = None if rms else torch.zeros_like(w)
+    y, mean, rstd, dx, dw, db = norm(A, x, w, b, dy, None)
+    rows = slice(n - 400, n)   # their part of the sums: the same rows by themselves
+    part = norm(A, x[rows], w, b, dy[rows], None)
+    norm_check(x[rows], w, b, dy[rows], None, (y[rows], None if rms else mean[rows], rstd[rows], dx[rows], part[4], part[5]))
+    ref_w, ref_b, size, size_b = (torch.zeros(d, dtype=torch.float64, device="cuda") for _ in range(4))
+    for c in range(0, n, 100_000):
+        at = slice(c, c + 100_000)
+        xh = x[at].double() * rstd[at, None].double()
+        if not rms:
+            xh = xh - (mean[at].double() * rstd[at].double())[:, None]
+        ref_w += (dy[at].double() * xh).sum(0)
+        ref_b += dy[at].double().sum(0)
+        size += (dy[at].double() * xh).abs().sum(0)
+        size_b += dy[at].double().abs().sum(0)
+    # a chain has at most the rows of a block (304 blocks of this width), their sums 16 and 32 more; xhat is off by at most
+    # 3 roundings of |x| rstd + |mean| rstd < 8
+    within(dw, ref_w, 2 * U * (n / 304 + 64) * size + 3 * U * 8 * size_b, "dw")
+    if not rms:
+        within(db, ref_b, 2 * U * (n / 304 + 64) * size_b, "db")
+
+
 # ------------------------------------------------------------------ embedding
 def embed_check(A, ids, table, dy, scale, base=None, ws=None):
     V, d = table.shape
@@ -541,6 +692,35 @@ def test_embed(A, n, V, d, dtype):
     ids[torch.rand(n, generator=g, device="cuda") < 0.1] = -1
     embed_check(A, ids, table, dy, 1.0)
     embed_check(A, ids, table, dy, -2.5, base=randn(g, V, d).to(DT[dtype]))
+
+
+@pytest.mark.parametrize("n", [200, 6000])
+def test_embed_of_more_than_2_31_numbers(A, n):
+    """Rows of a table past 2^31 elements: the last one, the ones at the border, the others left or cleared."""
+    V, d = 1_100_000, 2048
+    g = gen(n)
+    table = torch.empty(V, d, dtype=torch.bfloat16, device="cuda").normal_(0.0, 1.0, generator=g)
+    dy = randn(g, n, d).to(torch.bfloat16)
+    border = 2 ** 31 // d
+    ids = torch.randint(border - 3, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ids[:5] = torch.tensor([V - 1, 0, border, border - 1, V - 1], device="cuda", dtype=torch.int32)
+    y = torch.full_like(dy, 7.0)
+    A.adadsf_embed_forward(ids, table, y)
+    assert torch.equal(y, table[ids.long()])
+    before = table[5:9].clone()
+    A.adadsf_embed_backward(ids, dy, table)
+    there, slot = ids.long().unique(return_inverse=True)
+    ref = torch.zeros(there.numel(), d, dtype=torch.float64, device="cuda").index_add_(0, slot, dy.double())
+    size = torch.zeros_like(ref).index_add_(0, slot, dy.double().abs())
+    # an id comes n times at most; a sum of its rows, rounded once
+    within(table[there], ref, 2 * U * n * size * (1 + B16) + B16 * ref.abs(), "dtable")
+    left = torch.ones(V, dtype=torch.bool, device="cuda")
+    left[there] = False
+    for c in range(0, V, 100_000):
+        assert (table[c:c + 100_000][left[c:c + 100_000]] == 0).all()
+    table[5:9] = before
+    A.adadsf_embed_backward(ids, dy, table, accumulate=True)
+    assert torch.equal(table[5:9], before)
 
 
 @pytest.mark.parametrize("n", [32, 64, 65, 3000, 9000])
@@ -652,7 +832,7 @@ def test_ends_together(A, arch, dtype, tied, teacher):
     mean = torch.where(valid, row, 0.0).sum() / valid.sum()
     ref = dict(zip(leaf, torch.autograd.grad(mean, list(leaf.values()))))
     tol = 5 * B16 if dtype == "bf16" else 1e-5
-    assert float(loss) == pytest.approx(float(mean), rel=tol)
+    assert float(loss) == pytest.approx(float(mean.detach()), rel=tol)
     assert set(grads) == set(ref)
     for k in ref:
         assert float((grads[k].double() - ref[k]).norm()) <= tol * float(ref[k].norm()), k
