@@ -161,9 +161,12 @@ __device__ __forceinline__ void red_add4(float* p, const float4& v) {
   asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
-// Blocks of 64 k whose products share an accumulator.
-template <bool GRAD, bool F32>
-__host__ __device__ constexpr int chunk_blocks() { return F32 ? 8 : GRAD ? 1 << 20 : 16; }
+// Blocks of 64 k whose products share an accumulator. bf16 gradients: LONG cuts sums of more than 65536 rows (or classes, or
+// features), below which the loss does not show: one of 4 million rows was 3.6e-3 short (head gradients 4.4e-3 off, of which
+// roundings are 1.8e-3). A kernel of its own: its registers cost gradients of 27 tokens at a 151936 x 1536 head 341 -> 346 us.
+constexpr int kHtLong = 1024;
+template <bool GRAD, bool F32, bool LONG>
+__host__ __device__ constexpr int chunk_blocks() { return F32 ? 8 : LONG ? kHtLong : GRAD ? 1 << 20 : 16; }
 
 // A warp's loads from TMEM are done (tcgen05.wait::ld): only that is told, so the arrival is relaxed. Released, it waits
 // until the warp's stores to global memory are performed (gradients of 500 tokens at the Qwen2.5-7B head 1104 -> 1079 us).
@@ -465,7 +468,7 @@ __device__ __forceinline__ void dw_tile(const HtDev& p, const CUtensorMap& tm, c
   if (F32) release();
 }
 
-template <bool GRAD, bool F32>
+template <bool GRAD, bool F32, bool LONG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
     head_tc_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                    const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmGo,
@@ -524,7 +527,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
   const int count = *p.count;
   const CUtensorMap& tmH = !F32 && count == p.n ? tmA : tmP;   // bf16 rows that all count were not packed
   const Tiles<GRAD> tiles(p, count);
-  constexpr int TERMS = F32 ? kHeadTerms : 1, CHUNK = chunk_blocks<GRAD, F32>();
+  constexpr int TERMS = F32 ? kHeadTerms : 1, CHUNK = chunk_blocks<GRAD, F32, LONG>();
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
@@ -668,7 +671,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       };
       wait();
       if (!ok) break;
-      if ((F32 || !GRAD) && ti.nkb > CHUNK) {
+      if ((F32 || LONG || !GRAD) && ti.nkb > CHUNK) {
         float run[128];
         int first = CHUNK;
 #pragma unroll
@@ -756,16 +759,16 @@ HtDev head_dev(const Head& a, const Dev& dev) {
 
 int ceil_to(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
-template <bool GRAD, bool F32>
+template <bool GRAD, bool F32, bool LONG = false>
 cudaError_t launch_tiles(int64_t tiles, const Head& a, const CUtensorMap& tg, const CUtensorMap& tgo, const CUtensorMap& tdw,
                          const HtDev& p, const Dev& dev) {
-  const cudaError_t e = allow_smem<head_tc_kernel<GRAD, F32>, kHtSmem>();
+  const cudaError_t e = allow_smem<head_tc_kernel<GRAD, F32, LONG>, kHtSmem>();
   if (e != cudaSuccess || tiles == 0) return e;
   CUtensorMap th, ta = {}, tw;
   if (!head_maps(F32, a, &th, &tw)) return cudaErrorInvalidValue;
   if (!F32 && !make_tmap_bf16(&ta, a.h, (uint64_t)a.n, (uint64_t)a.d, (uint64_t)a.d, 64, 64)) return cudaErrorInvalidValue;
   const int pairs = (int)std::min<int64_t>(tiles, dev.num_sms / 2);
-  return launch_pdl(head_tc_kernel<GRAD, F32>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, ta, tw, tg, tgo, tdw,
+  return launch_pdl(head_tc_kernel<GRAD, F32, LONG>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, ta, tw, tg, tgo, tdw,
                     p);
 }
 
@@ -803,8 +806,10 @@ cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, i
   p.dw = a.dw;
   const int64_t mbs = ceil_to(a.n, kHtTile), nbd = ceil_to(a.d, kHtTile);
   const int64_t tiles = mbs * p.n_g + (p.want_h && n_d ? mbs * nbd * p.splits : 0) + (p.want_w ? ceil_to(n_d, kHtTile) * nbd : 0);
-  return dtype == kBF16 ? launch_tiles<true, false>(tiles, a, tg, tgo, tdw, p, dev)
-                        : launch_tiles<true, true>(tiles, a, tg, tgo, tdw, p, dev);
+  if (dtype != kBF16) return launch_tiles<true, true>(tiles, a, tg, tgo, tdw, p, dev);
+  const bool long_sums = std::max({(int64_t)ceil_to(a.n, kHtK), (int64_t)ceil_to(p.kb_d, p.splits), (int64_t)ceil_to(a.d, kHtK)}) > kHtLong;
+  return long_sums ? launch_tiles<true, false, true>(tiles, a, tg, tgo, tdw, p, dev)
+                   : launch_tiles<true, false>(tiles, a, tg, tgo, tdw, p, dev);
 }
 
 }  // namespace adadsf

@@ -441,12 +441,22 @@ def test_head_of_a_million_rows(A):
     h, w = randn(g, n, d).to(torch.bfloat16), randn(g, V, d, std=0.1).to(torch.bfloat16)
     target = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
     target[torch.rand(n, generator=g, device="cuda") < 0.01] = -1
-    loss, lse, acc, dh, _ = ce(A, h, w, target)
+    loss, lse, acc, dh, dw = ce(A, h, w, target)
     assert float(acc[1]) == int((target >= 0).sum())
     for rows in (slice(0, 300), slice(n // 2, n // 2 + 300), slice(n - 300, n)):
         want, used = want_of(target[rows], V)
         ref = Ref(h[rows], w, want, used, torch.zeros(300, dtype=torch.float64, device="cuda"), None, 1.0, 1)
         ref.check(loss[rows], lse[rows], dh[rows], None)
+    total = torch.zeros(V, d, dtype=torch.float64, device="cuda")
+    for c in range(0, n, 50_000):
+        at = slice(c, c + 50_000)
+        z, (want, used) = h[at].double() @ w.double().T, want_of(target[at], V)
+        total += ((torch.softmax(z, -1) - want) * used[:, None]).T @ h[at].double()
+    # a chain of 65536 rows is 4096 steps, each of which cuts at most 2u of the sum so far; entries of either sign make the
+    # sum a walk, of which the final sum holds half at a step's mean: 4096 u of it, twice that with the 17 chains' sums and
+    # 2e-3 of independent roundings over 134400 entries
+    short = float(((dw.double() - total) * total).sum() / total.square().sum())
+    assert abs(short) <= 4096 * 2 * U, short
 
 
 @pytest.mark.parametrize("n,dtype", [(20, "bf16"), (300, "bf16"), (20, "f32"), (300, "f32")])
