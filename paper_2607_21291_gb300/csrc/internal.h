@@ -325,6 +325,7 @@ struct Head {
   float *loss, *lse;                     // by row (loss may be null)
   double* acc;                           // or null
   // backward
+  float* own_lse;                        // by row: room for the backward pass's own
   const float* g;                        // by row, or null
   float* g_ref;                          // the largest of a row with a target
   void *dh, *dw;                         // either may be null

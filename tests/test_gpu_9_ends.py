@@ -474,6 +474,43 @@ def test_head_row_of_nan_stays_in_its_row(A, n, dtype):
     assert not torch.isfinite(got[0][~keep]).any() and torch.isnan(got[3][3]).all()
 
 
+@pytest.mark.parametrize("n,d", [(1, 256), (20, 256), (80, 256), (81, 256), (300, 512)])
+def test_head_gradients_of_sure_rows(A, n, d):
+    """fp32 rows that are nearly sure of their target, at logits of a hundred: q - 1 there is a difference of numbers near 1,
+    so both passes have to see the same logits. A column of ones in the head sums a row's G, which is 0 but for rounding."""
+    V = 300
+    g = gen(n + d)
+    w = randn(g, V, d).abs() * 0.5
+    h = randn(g, n, d).abs()
+    target = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    w[:, 7] = 1.0
+    h[:, 7] = 0.0
+    z = h.double() @ w.double().T
+    lift = (z.amax(-1) - z[torch.arange(n), target.long()] + 6.0) / (w[target.long()].double() ** 2).sum(-1)
+    h += (lift[:, None] * w[target.long()]).float()
+    h[:, 7] = 0.0
+    loss, lse, _, dh, _ = ce(A, h, w, target)
+    z = h.double() @ w.double().T
+    ref = torch.logsumexp(z, -1)
+    q = torch.exp(z - ref[:, None])
+    spread = (q * (z.amax(-1, keepdim=True) - z)).sum(-1) + (q * (z - ref[:, None]).abs()).sum(-1)
+    size = 2 * (1 - q[torch.arange(n), target.long()])   # the sum of |G|
+    # for logits that are the same in both passes: the logarithm's rounding; arguments of the exponentials (3 roundings of either
+    # pass), the exponentials (2^-22), their sums (V / 128 records of 128), logf and G's own; the sum of G in a chain
+    bound = U * ref.abs() + 3 * U * spread + (4 + 4 + 8 + 8) * U + 2 * U * (64 + 32) * size + 2 * U * terms(6 * V, True, True) * size
+    within(dh[:, 7], torch.zeros(n, device="cuda"), bound, "sum of G")
+
+
+@pytest.mark.parametrize("n,d,V", [(1, 64, 300), (20, 256, 5000), (80, 132, 2480)])
+def test_head_gradient_of_a_row_in_company(A, n, d, V):
+    """fp32: few rows and many have different forward passes; a row's hidden gradient is the same bits in either, since its
+    logarithm is of the logits that the gradient is made of."""
+    h, w, _, _ = head_inputs(200, d, V, "f32")
+    target = torch.randint(0, V, (200,), generator=gen(n), device="cuda", dtype=torch.int32)
+    many, few = ce(A, h, w, target), ce(A, h[:n], w, target[:n])
+    assert torch.equal(few[3], many[3][:n])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_head_weights_of_rows(A, dtype):
     """Weights below zero and of zero; what they hold in rows without a target; all of them zero."""
