@@ -161,7 +161,11 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-_get_device = getattr(torch._C, "_cuda_getDevice", None)   # what torch.cuda.current_device() asks, half a microsecond sooner
+def _current_device() -> int:
+    """torch.cuda.current_device(), asked where torch asks, if it has that name, without its check of the context (half a
+    microsecond)."""
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    return torch.cuda.current_device() if get is None else get()
 
 
 def _s(stream) -> int:
@@ -170,7 +174,7 @@ def _s(stream) -> int:
     if stream is None:
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None and torch.cuda.is_initialized():
-            return raw(_get_device() if _get_device else torch.cuda.current_device())
+            return raw(_current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
@@ -665,7 +669,7 @@ def _on(t: torch.Tensor, name: str) -> int:
     if not (t.is_cuda and t.dim() == 2 and t.is_contiguous()) or t.dtype not in DTYPE_CODE:
         raise ValueError(f"{name} must be a contiguous CUDA matrix of float32 or bfloat16")
     dev = t.get_device()
-    if dev != (_get_device() if _get_device else torch.cuda.current_device()):
+    if dev != _current_device():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     return dev
 
