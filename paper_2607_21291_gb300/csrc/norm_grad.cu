@@ -9,6 +9,8 @@
 // (asynchronous copies, ng_depth rows in all: nobody else reads it, so no barrier guards it), which keeps enough
 // bytes on their way whatever the registers allow. Every block leaves its weight gradients,
 // which a second kernel adds in order: results are the same in every run.
+// 65536 x 3584 bf16 with a sum: RMSNorm 160 us forward, 308 backward (5.9 and 6.1 TB/s); LayerNorm 190 and 328, whose forward pass has two
+// sums one after the other; 24 x 768 11 us for both, two launches.
 #include <math.h>
 
 #include <algorithm>
