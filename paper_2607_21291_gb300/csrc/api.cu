@@ -1771,7 +1771,7 @@ adadsf_status check_head(int64_t n_rows, int d, int n_classes, int dtype, int to
 
 struct HeadLayout {
   HeadPlan plan;
-  size_t count, rows, target, cls, p, ent, picked, lse, packed, w_parts, rec, g[2], acc, total;
+  size_t count, rows, target, cls, p, ent, picked, packed, w_parts, rec, g[2], acc, total;
 };
 HeadLayout head_layout(int64_t n, int d, int V, int dtype, int k) {
   HeadLayout l;
@@ -1786,7 +1786,6 @@ HeadLayout head_layout(int64_t n, int d, int V, int dtype, int k) {
   l.p = cv.take((size_t)n * k * 4);
   l.ent = cv.take((size_t)n * 4);
   l.picked = cv.take((size_t)n * k * 4);
-  l.lse = cv.take((size_t)n * 4);
   l.packed = cv.take(l.plan.packed);
   l.w_parts = cv.take(l.plan.w_parts);
   // the forward pass's records and the backward pass's buffers take turns
@@ -1834,7 +1833,6 @@ adadsf_status head_prepare(const HeadCall& c, void* ws, size_t ws_bytes, void* s
   a->w_parts = at<void>(ws, l->w_parts);
   a->g_ref = at<float>(ws, l->count) + 1;
   a->picked = at<float>(ws, l->picked);
-  a->own_lse = at<float>(ws, l->lse);
   a->rec = at<float2>(ws, l->rec);
   a->G[0] = at<void>(ws, l->g[0]);
   a->G[1] = at<void>(ws, l->g[1]);

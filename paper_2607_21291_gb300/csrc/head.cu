@@ -385,40 +385,35 @@ cudaError_t head_teacher(const int32_t* idx, const float* logit, int64_t n, int 
                     cls, p, ent, target, dev.err);
 }
 
-namespace {
-cudaError_t merge(const Head& a, int records, float* loss, float* lse, const Dev& dev) {
-  const int blocks = (int)std::min<int64_t>((a.n + 31) / 32, 2 * dev.num_sms);
-  return launch_pdl(head_merge_kernel, dim3((unsigned)blocks), dim3(32 * kMergeWarps), 0, dev.stream, (const int32_t*)a.count,
-                    (const int32_t*)a.rows, (const float2*)a.rec, a.cap, records, (const float*)a.picked, a.p, a.ent, a.k,
-                    a.temp, loss, lse);
-}
-}  // namespace
-
 cudaError_t head_forward(int dtype, const Head& a, const Dev& dev) {
   const bool few = a.n <= (dtype == kBF16 ? kHeadFewRows : kHeadFewRowsF32);
   int records = (a.V + 127) / 128;
   cudaError_t e = dtype == kBF16 ? pack<bf16>(a, false, !few, dev) : pack<float>(a, false, !few, dev);
   if (e == cudaSuccess) e = few ? head_few(dtype, a, dev, &records) : head_stats(dtype, a, dev);
   if (e != cudaSuccess) return e;
-  e = merge(a, records, a.loss, a.lse, dev);
+  const int blocks = (int)std::min<int64_t>((a.n + 31) / 32, 2 * dev.num_sms);
+  e = launch_pdl(head_merge_kernel, dim3((unsigned)blocks), dim3(32 * kMergeWarps), 0, dev.stream, (const int32_t*)a.count,
+                 (const int32_t*)a.rows, (const float2*)a.rec, a.cap, records, (const float*)a.picked, a.p, a.ent, a.k,
+                 a.temp, a.loss, a.lse);
   if (e != cudaSuccess || !a.acc) return e;
   return launch_pdl(head_sum_kernel, dim3(1), dim3(1024), 0, dev.stream, (const float*)a.loss, a.n, (const int32_t*)a.count, a.acc);
 }
 
-cudaError_t head_backward(int dtype, const Head& call, const HeadPlan& plan, const Dev& dev) {
-  Head a = call;
-  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, true, true, dev) : pack<float>(a, true, true, dev);
-  // The forward pass of few fp32 rows adds logits up in another order (head_few.cu). At a target of nearly all the weight q - 1 is
-  // a difference of such logits, which leaves their roundings: 20 rows of 256 features and 5000 classes: head gradient
-  // 3.0e-6 off, with a logarithm of the same logits 1.5e-6 (77 rows at a 50304 x 512 head, loss and gradients: 285 -> 341 us). bf16
-  // gradients round far above that.
-  if (e == cudaSuccess && dtype != kBF16 && a.n <= kHeadFewRowsF32) {
-    e = head_stats(dtype, a, dev);
-    if (e == cudaSuccess) e = merge(a, (a.V + 127) / 128, nullptr, a.own_lse, dev);
-    a.lse = a.own_lse;
+cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const Dev& dev) {
+  // The gradient's logits of few fp32 rows come from the kernel of their forward pass: at a target of nearly all the weight q - 1
+  // is a difference of logits of both passes, and those of the other kernel, added up in another order, leave their
+  // roundings (20 rows of 256 features, 5000 classes: head gradient 3.0e-6 off, so 1.4e-6). It is quicker as well: loss and
+  // gradients of 77 rows at a 50304 x 512 head 285 -> 267 us. bf16 gradients round far above that.
+  const bool few = dtype != kBF16 && a.n <= kHeadFewRowsF32;
+  cudaError_t e = dtype == kBF16 ? pack<bf16>(a, true, true, dev) : pack<float>(a, true, !few || a.dh, dev);
+  for (int j = 0; few && j < plan.pieces && e == cudaSuccess; ++j) {
+    const int64_t v = (int64_t)j * plan.piece;
+    const int n_v = (int)std::min<int64_t>(plan.piece, a.V - v);
+    e = head_few_grad(a, v, n_v, dev);
+    if (e == cudaSuccess) e = head_grad(dtype, a, 1, 0, 0, v, n_v, j == 0, dev);
   }
   // launch j: G of piece j, gradients of piece j - 1
-  for (int j = 0; j <= plan.pieces && e == cudaSuccess; ++j) {
+  for (int j = 0; !few && j <= plan.pieces && e == cudaSuccess; ++j) {
     const int64_t v = (int64_t)j * plan.piece, before = v - plan.piece;
     const int n_g = j < plan.pieces ? (int)std::min<int64_t>(plan.piece, a.V - v) : 0;
     const int n_d = j > 0 ? (int)std::min<int64_t>(plan.piece, a.V - before) : 0;

@@ -1,4 +1,5 @@
-// The losses' forward pass for few rows (at most kHeadFewRows, fp32 kHeadFewRowsF32): what bounds it is reading the head once.
+// The losses' forward pass for few rows (at most kHeadFewRows, fp32 kHeadFewRowsF32), and G of few fp32 rows from the same logits: what
+// bounds them is reading the head once.
 //
 // The operands change places against head_tc.cu: 128 classes are the M of a product and the packed rows, up to
 // 128 in steps of 16, its N, so that the tensor cores spend on a block of classes what its rows need (with 256 rows
@@ -67,6 +68,11 @@ struct HfDev {
   int k;
   float2* rec;               // [CTA][cap]
   float* picked;
+  int v0, v1;                // the classes: all of them, or a piece
+  // G of a piece
+  const float *pw, *lse, *g, *g_ref;   // weights of the targets [row][k]; by row
+  bf16* G;                   // three parts of [cap][ld_g]
+  int ld_g;
   int* err;
   unsigned long long timeout_ns;
 };
@@ -102,7 +108,48 @@ __device__ __forceinline__ bool group_agrees(int id, bool ok) {
   return all != 0;
 }
 
-template <bool F32>
+// 32 classes of a row's gradient from its logits (staged), in three parts; zeros for a row behind the last one. Classes from c1 on
+// are another CTA's.
+__device__ __forceinline__ void g_vector(const HfDev& p, const float* l, int cb, int c1, int m, bool live) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  if (cb >= c1) return;
+  bf16* dst = p.G + (int64_t)m * p.ld_g + (cb - p.v0);
+  const int64_t line = live ? (int64_t)p.rows[m] : 0;
+  const float lse = live ? p.lse[line] : 0.f, g = live ? (p.g ? p.g[line] : 1.f) / *p.g_ref : 0.f;
+  int j = live ? first_class(p.cls + line * p.k, p.k, cb) : p.k;
+  int next = j < p.k ? p.cls[line * p.k + j] : INT_MAX;
+#pragma unroll 1
+  for (int b = 0; b < 32; b += 8) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = cb + b + i;
+      float v = 0.f;
+      if (live && c < p.V) {
+        v = ex2_approx(fmaf(l[b + i], p.inv_t, -lse) * kLog2e);
+        if (c == next) {
+          float want = 0.f;
+          do {   // the same class twice: both weights
+            want += p.pw ? p.pw[line * p.k + j] : 1.f;
+            next = ++j < p.k ? p.cls[line * p.k + j] : INT_MAX;
+          } while (next == c);
+          v -= want;
+        }
+        v *= g;
+      }
+      f[i] = v;
+    }
+#pragma unroll
+    for (int part = 0; part < 3; ++part) {
+      uint32_t u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = next_parts(f[2 * i], f[2 * i + 1]);
+      *reinterpret_cast<uint4*>(dst + part * p.cap * p.ld_g + b) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+  }
+}
+
+template <bool F32, bool GRAD>
 __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     head_few_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                     const __grid_constant__ CUtensorMap tmW1, const __grid_constant__ HfDev p) {
@@ -123,9 +170,9 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // this CTA's classes, in tiles of 128 of which the last may be short
-  const int units = (p.V + kHfUnit - 1) / kHfUnit;
-  const int c_begin = (int)((int64_t)units * blockIdx.x / gridDim.x) * kHfUnit;
-  const int c_end = min(p.V, (int)((int64_t)units * (blockIdx.x + 1) / gridDim.x) * kHfUnit);
+  const int units = (p.v1 - p.v0 + kHfUnit - 1) / kHfUnit;
+  const int c_begin = p.v0 + (int)((int64_t)units * blockIdx.x / gridDim.x) * kHfUnit;
+  const int c_end = min(p.v1, p.v0 + (int)((int64_t)units * (blockIdx.x + 1) / gridDim.x) * kHfUnit);
   const int tiles = (c_end - c_begin + kHfM - 1) / kHfM, nkb = (p.d + kHfK - 1) / kHfK;
 
   if (threadIdx.x == 0) {
@@ -271,12 +318,13 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     float top[C::TURNS], sum[C::TURNS];
     int next[C::TURNS];
     const int chunks = (min(count, p.n) + 31) / 32;
+    const int rows_zero = (count + kHeadZeroPad - 1) / kHeadZeroPad * kHeadZeroPad;   // G's rows past the last one are zero as far
 #pragma unroll
     for (int u = 0; u < C::TURNS; ++u) {
       const int m = (group + C::GROUPS * u) * 32 + r;
       top[u] = -INFINITY;
       sum[u] = 0.f;
-      next[u] = q == 0 && m < count ? first_class(p.cls + (int64_t)p.rows[m] * p.k, p.k, c_begin) : p.k;
+      next[u] = !GRAD && q == 0 && m < count ? first_class(p.cls + (int64_t)p.rows[m] * p.k, p.k, c_begin) : p.k;
     }
     bool ok = true;
     int it = 0;
@@ -317,12 +365,21 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
 #pragma unroll
       for (int u = 0; u < C::TURNS; ++u) {
         const int chunk = group + C::GROUPS * u;
-        if (chunk >= chunks) continue;
+        if (GRAD && chunk == C::GROUPS - 1 && rows_zero > C::GROUPS * 32) g_vector(p, out, c0 + 32 * q, c1, C::GROUPS * 32 + r, false);
+        if (chunk >= chunks) {
+          if (GRAD && chunk * 32 < rows_zero) g_vector(p, out, c0 + 32 * q, c1, chunk * 32 + r, false);
+          continue;
+        }
 #pragma unroll
         for (int j = 0; j < 32; ++j) out[j * kHfOutLd + t] = run[u][j];
         named_bar_sync(1 + group, 128);
         const int m = chunk * 32 + r;
         const float* row = out + r * kHfOutLd;
+        if (GRAD) {
+          g_vector(p, row + 32 * q, c0 + 32 * q, c1, m, m < count);
+          named_bar_sync(1 + group, 128);
+          continue;
+        }
         float f[32], now = top[u];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -351,7 +408,7 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
       }
     }
 #pragma unroll
-    for (int u = 0; u < C::TURNS; ++u) {
+    for (int u = 0; u < (GRAD ? 0 : C::TURNS); ++u) {
       const int m = (group + C::GROUPS * u) * 32 + r;
       float most = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
@@ -368,12 +425,13 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
     const int total = tiles * nkb;
     float4 f[8];
     int c0 = c_begin, k0 = 0;   // of the block that is loaded next
+    const int last = GRAD ? min(c_end, p.V) : c_end;
     auto load = [&](float4 (&g)[8]) {
       const int k = k0 + 4 * k4;
       const float* src = p.w + (int64_t)(c0 + r0) * p.d + k;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        g[j] = c0 + r0 + 2 * j < c_end && k < p.d ? *reinterpret_cast<const float4*>(src + (int64_t)(2 * j) * p.d) : make_float4(0.f, 0.f, 0.f, 0.f);
+        g[j] = c0 + r0 + 2 * j < last && k < p.d ? *reinterpret_cast<const float4*>(src + (int64_t)(2 * j) * p.d) : make_float4(0.f, 0.f, 0.f, 0.f);
       k0 += kHfK;
       if (k0 >= p.d) {
         k0 = 0;
@@ -417,9 +475,10 @@ __global__ void __launch_bounds__(HfCfg<F32>::THREADS, 1)
   }
 }
 
-template <bool F32>
-cudaError_t launch_few(const Head& a, const Dev& dev, int* records) {
-  const cudaError_t e = allow_smem<head_few_kernel<F32>, HfCfg<F32>::SMEM>();
+// G of the n_g classes from v_g (0: a forward pass over all).
+template <bool F32, bool GRAD>
+cudaError_t launch_few(const Head& a, int64_t v_g, int n_g, const Dev& dev, int* records) {
+  const cudaError_t e = allow_smem<head_few_kernel<F32, GRAD>, HfCfg<F32>::SMEM>();
   if (e != cudaSuccess) return e;
   HfDev p = {};
   p.n = (int)((a.n + 15) / 16 * 16);
@@ -444,14 +503,27 @@ cudaError_t launch_few(const Head& a, const Dev& dev, int* records) {
   p.picked = a.picked;
   p.err = dev.err;
   p.timeout_ns = kWaitTimeoutNs;
-  *records = (int)std::min<int64_t>(std::min(dev.num_sms, kHeadFewCtas), ((int64_t)a.V + kHfUnit - 1) / kHfUnit);
-  return launch_pdl(head_few_kernel<F32>, dim3((unsigned)*records), dim3(HfCfg<F32>::THREADS), HfCfg<F32>::SMEM, dev.stream, th, ta, tw, tw1, p);
+  p.v0 = (int)v_g;
+  p.v1 = GRAD ? (int)(v_g + (n_g + 63) / 64 * 64) : a.V;   // the products of G take 64 classes at a time
+  p.pw = a.p;
+  p.lse = a.lse;
+  p.g = a.g;
+  p.g_ref = a.g_ref;
+  p.G = static_cast<bf16*>(a.G[0]);
+  p.ld_g = a.piece;
+  *records = (int)std::min<int64_t>(std::min(dev.num_sms, kHeadFewCtas), ((int64_t)(p.v1 - p.v0) + kHfUnit - 1) / kHfUnit);
+  return launch_pdl(head_few_kernel<F32, GRAD>, dim3((unsigned)*records), dim3(HfCfg<F32>::THREADS), HfCfg<F32>::SMEM, dev.stream, th, ta, tw, tw1, p);
 }
 
 }  // namespace
 
 cudaError_t head_few(int dtype, const Head& a, const Dev& dev, int* records) {
-  return dtype == kBF16 ? launch_few<false>(a, dev, records) : launch_few<true>(a, dev, records);
+  return dtype == kBF16 ? launch_few<false, false>(a, 0, 0, dev, records) : launch_few<true, false>(a, 0, 0, dev, records);
+}
+
+cudaError_t head_few_grad(const Head& a, int64_t v_g, int n_g, const Dev& dev) {
+  int ctas;
+  return launch_few<true, true>(a, v_g, n_g, dev, &ctas);
 }
 
 }  // namespace adadsf

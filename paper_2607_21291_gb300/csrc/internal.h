@@ -325,7 +325,6 @@ struct Head {
   float *loss, *lse;                     // by row (loss may be null)
   double* acc;                           // or null
   // backward
-  float* own_lse;                        // by row: room for the backward pass's own
   const float* g;                        // by row, or null
   float* g_ref;                          // the largest of a row with a target
   void *dh, *dw;                         // either may be null
@@ -350,6 +349,8 @@ cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const 
 // head_few.cu: stats for at most kHeadFewRows (fp32: kHeadFewRowsF32) rows, one record a CTA (their number in *records).
 constexpr int kHeadFewRows = 128, kHeadFewRowsF32 = 80, kHeadFewCtas = 160;
 cudaError_t head_few(int dtype, const Head& a, const Dev& dev, int* records);
+// G of the n_g classes from v_g into G[0] for at most kHeadFewRowsF32 fp32 rows.
+cudaError_t head_few_grad(const Head& a, int64_t v_g, int n_g, const Dev& dev);
 // head_tc.cu: stats of all tiles; one launch of the backward pass -- G of the n_g classes from v_g into G[buf], the
 // gradients of the n_d classes from v_d from the other buffer.
 cudaError_t head_stats(int dtype, const Head& a, const Dev& dev);

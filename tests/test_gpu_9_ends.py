@@ -501,14 +501,35 @@ def test_head_gradients_of_sure_rows(A, n, d):
     within(dh[:, 7], torch.zeros(n, device="cuda"), bound, "sum of G")
 
 
-@pytest.mark.parametrize("n,d,V", [(1, 64, 300), (20, 256, 5000), (80, 132, 2480)])
-def test_head_gradient_of_a_row_in_company(A, n, d, V):
-    """fp32: few rows and many have different forward passes; a row's hidden gradient is the same bits in either, since its
-    logarithm is of the logits that the gradient is made of."""
-    h, w, _, _ = head_inputs(200, d, V, "f32")
-    target = torch.randint(0, V, (200,), generator=gen(n), device="cuda", dtype=torch.int32)
-    many, few = ce(A, h, w, target), ce(A, h[:n], w, target[:n])
-    assert torch.equal(few[3], many[3][:n])
+@pytest.mark.parametrize("n", [1, 20, 33, 64, 65, 80, 81, 200])
+@pytest.mark.parametrize("d", [64, 132, 1028])
+def test_head_of_one_class_has_no_gradient(A, n, d):
+    """fp32: the logarithm of one class is its logit, so that q - 1 is 0 where both passes have the same logits, however these
+    are added up, and nothing else where they differ by a rounding."""
+    h, w, _, _ = head_inputs(n, d, 1, "f32")
+    loss, lse, _, dh, dw = ce(A, h, w, torch.zeros(n, dtype=torch.int32, device="cuda"))
+    for x in (loss, dh, dw):
+        assert (x == 0).all()
+
+
+@pytest.mark.parametrize("n,V", [(1, 31), (32, 33), (33, 64), (64, 65), (65, 4900), (80, 5000), (50, 180000)])
+def test_head_gradients_of_few_rows(A, n, V):
+    """fp32 rows on both sides of the zeros that products over rows need, classes on both sides of their blocks and more than a
+    piece has, some rows without a target; distillation as well; each gradient by itself."""
+    d = 100
+    h, w, target, gl = head_inputs(n, d, V, "f32")
+    want, used = want_of(target, V)
+    zero = torch.zeros(n, dtype=torch.float64, device="cuda")
+    ref = Ref(h, w, want, used, zero, gl, 1.0, 1)
+    loss, lse, _, dh, dw = ce(A, h, w, target, gl)
+    ref.check(loss, lse, dh, dw)
+    one, two = torch.full_like(h, 7.0), torch.full_like(w, 7.0)
+    A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_h=one)
+    A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_w=two)
+    assert torch.equal(one, dh) and torch.equal(two, dw)
+    h, w, idx, logit, gl = distill_inputs(n, d, V, 9, "f32")
+    want, used, ent = teacher_want(idx, logit, V, 2.0)
+    Ref(h, w, want, used, ent, gl, 2.0, 9).check(*distill(A, h, w, idx, logit, 2.0, gl))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
