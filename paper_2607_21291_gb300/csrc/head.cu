@@ -275,9 +275,10 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
         pz += s_pz[i][lane];
         ps += s_p[i][lane];
       }
-      const float z = top * inv_t + logf(sum);
-      lse[row] = z;
-      if (loss) loss[row] = temp * temp * ((ent ? ent[row] : 0.f) + (ps * z - pz));
+      const float most = top * inv_t, rest = logf(sum);
+      lse[row] = most + rest;
+      // targets against the largest logit first: a target that is the largest leaves the sum's logarithm alone
+      if (loss) loss[row] = temp * temp * ((ent ? ent[row] : 0.f) + ((ps * most - pz) + ps * rest));
     }
     __syncthreads();
   }

@@ -10,7 +10,7 @@
 // The rows' parts lie one behind the other, so that w1 (h2, h3) and w2 (h1, h2) are one product each, beside w3 h1
 // and w1 h1: four products a step in place of six. The large one, w1 h1, has columns of its own, since what an
 // addition cuts off goes by the accumulator (see head_tc.cu, also for the chunks of k).
-// Measured, a graph's pass: 24 tokens of the Pythia-160M head 23.7 us with packing and joining (its bytes: 11.4), 77 fp32 tokens of
+// Measured, a graph's pass: 24 tokens of the Pythia-160M head 24.2 us with packing and joining (its bytes: 11.4), 77 fp32 tokens of
 // the Pythia-70M head 53.7 (15; chunks of 32 steps 52.4, at twice the error).
 //   warp 0       TMA: the rows' blocks of 64 k (fp32: three parts), the head's blocks (bf16)
 //   warp 1       TMEM, MMA issue (one thread), accumulators double-buffered
@@ -45,7 +45,7 @@ struct HfCfg {
   static constexpr int GROUPS = F32 ? 3 : 2;     // of four epilogue warps
   static constexpr int TURNS = F32 ? 1 : 2;      // times 32 rows that a group takes
   static constexpr int EPI = 4 * GROUPS;
-  static constexpr int CHUNK = F32 ? 4 : 16;     // blocks of 64 k that share an accumulator (see head_tc.cu)
+  static constexpr int CHUNK = F32 ? 4 : 8;     // blocks of 64 k that share an accumulator (see head_tc.cu)
   static constexpr int THREADS = 64 + 32 * (EPI + (F32 ? kHfConvWarps : 0));
   static constexpr int RING = F32 ? 2 * 3 * (kHfPart + kHeadFewRowsF32 * 128) : 196608;
   static constexpr int SMEM = 1024 + RING + GROUPS * kHfOut + kHfBars * 8 + 16;

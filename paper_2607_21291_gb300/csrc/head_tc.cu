@@ -23,10 +23,11 @@
 //
 // The tensor cores cut what an addition loses instead of rounding it, so a sum of many steps drifts towards zero: 320 steps
 // of 16 k were 1e-5 of a logit off, which its exponential multiplies (fp32 gradients 5e-5). Where fp32 results come
-// of it (logits of the forward pass, all fp32 products) a tile's k are cut in chunks of at most 64 steps (fp32: 16, each of
+// of it (logits of the forward pass, all fp32 products) a tile's k are cut in chunks of at most 32 steps (fp32: 16, each of
 // which holds its six products), whose accumulators the epilogue's threads add up in registers, rounding, while the next
 // chunk is multiplied. Chunks of 32, 16 and 8 steps: 700 fp32 rows of 512 features, 50304 classes, head gradient 1.2e-6, 7e-7 and
-// 5e-7 off; loss and gradients of 645 such rows 671, 674 and 694 us.
+// 5e-7 off; loss and gradients of 645 such rows 671, 674 and 694 us. bf16, 64, 32 and 16 steps: losses of 400 rows of 5120 features 6e-7,
+// 3e-7 and 2e-7 off; of 3331 rows of the Pythia-1.4B head 362, 378 and 415 us.
 // The tensor cores bound it: 4096 bf16 rows, 32768 classes of 3584: stats 471 us (2.04 PFLOP/s), G 486, dH and dW 1020 (1.89
 // PFLOP/s), the pipe 90 to 94% active. 768 fp32 rows, 50304 classes of 512: 124, 148 and 312 us (320 to 255 TFLOP/s of fp32 products, the pipe 87,
 // 72 and 68% active: epilogues of short sums).
@@ -170,7 +171,7 @@ __device__ __forceinline__ void red_add4(float* p, const float4& v) {
 // roundings are 1.8e-3). A kernel of its own: its registers cost gradients of 27 tokens at a 151936 x 1536 head 341 -> 346 us.
 constexpr int kHtLong = 1024;
 template <bool GRAD, bool F32, bool LONG>
-__host__ __device__ constexpr int chunk_blocks() { return F32 ? 4 : LONG ? kHtLong : GRAD ? 1 << 20 : 16; }
+__host__ __device__ constexpr int chunk_blocks() { return F32 ? 4 : LONG ? kHtLong : GRAD ? 1 << 20 : 8; }
 
 // A warp's loads from TMEM are done (tcgen05.wait::ld): only that is told, so the arrival is relaxed. Released, it waits
 // until the warp's stores to global memory are performed (gradients of 500 tokens at the Qwen2.5-7B head 1104 -> 1079 us).

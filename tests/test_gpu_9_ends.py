@@ -71,7 +71,7 @@ def teacher_want(idx, logit, V, temp):
 
 def terms(m, f32, grad):
     """Additions that lose up to 2u each in a sum of m products. A step of the tensor cores adds 16 products and the sum so
-    far, 17 terms; where fp32 comes of it, a sum is of chunks of 32 steps (bf16 logits 64), added in fp32; bf16
+    far, 17 terms; where fp32 comes of it, a sum is of chunks of at most 32 steps (bf16 logits 64), added in fp32; bf16
     gradients are one chain."""
     if grad and not f32:
         return m + 64
