@@ -8,6 +8,7 @@ The library is loaded from this package directory; if it is missing every call
 raises (there is no fallback path)."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -184,9 +185,17 @@ def _dev(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be a contiguous CUDA tensor")
 
 
-def workspace(nbytes: int, device=None) -> torch.Tensor:
-    """Zero-initialised device workspace (its first 256 bytes are the error word)."""
-    return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device or "cuda")
+def _torch_on(stream):
+    """Torch's own work of a call on the call's stream (None: the current one): what is made there is cleared in order with
+    the kernels that use it, and its memory goes back to that stream's pool."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def workspace(nbytes: int, device=None, stream=None) -> torch.Tensor:
+    """Zero-initialised device workspace (its first 256 bytes are the error word), cleared on the stream (None: the current
+    one). Calls on other streams have to wait for that."""
+    with _torch_on(stream):
+        return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device or "cuda")
 
 
 # --------------------------------------------------------------------- config
@@ -249,7 +258,7 @@ def adadsf_layer_stats(x_in: torch.Tensor, x_out: torch.Tensor, acc: torch.Tenso
     d = x_in.shape[-1]
     n = x_in.numel() // d
     if ws is None:
-        ws = workspace(adadsf_stats_workspace_size(n), x_in.device)
+        ws = workspace(adadsf_stats_workspace_size(n), x_in.device, stream)
     _check(lib().adadsf_layer_stats(_p(x_in), _p(x_out), n, d, DTYPE_CODE[x_in.dtype], mode,
                                     _p(acc), _p(ws), ws.numel(), _s(stream)))
 
@@ -299,7 +308,7 @@ def adadsf_align_hidden(hs: torch.Tensor, hd: torch.Tensor, acc: torch.Tensor,
     d = hs.shape[-1]
     n = hs.numel() // d
     if ws is None:
-        ws = workspace(lib().adadsf_align_workspace_size(n, 0), hs.device)
+        ws = workspace(lib().adadsf_align_workspace_size(n, 0), hs.device, stream)
     _check(lib().adadsf_align_hidden(_p(hs), _p(hd), n, d, DTYPE_CODE[hs.dtype], _p(acc), _p(grad), _p(ws),
                                      ws.numel(), _s(stream)))
 
@@ -311,7 +320,7 @@ def adadsf_align_output(hs: torch.Tensor, hd: torch.Tensor, w_head: torch.Tensor
     n_cls, d = w_head.shape
     n = hs.numel() // d
     if ws is None:
-        ws = workspace(lib().adadsf_align_workspace_size(n, n_cls), hs.device)
+        ws = workspace(lib().adadsf_align_workspace_size(n, n_cls), hs.device, stream)
     _check(lib().adadsf_align_output(_p(hs), _p(hd), _p(w_head), n, d, n_cls, DTYPE_CODE[hs.dtype], _p(acc),
                                      _p(ws), ws.numel(), _s(stream)))
 
@@ -323,9 +332,10 @@ def adadsf_router_backward(cfg: ModelCfg, w: dict, x: torch.Tensor, y_plain: tor
     _dev(x, "x"); _dev(y_plain, "y_plain"); _dev(rows, "rows"); _dev(grad_y, "grad_y")
     n = rows.numel()
     h = cfg.router_hidden
-    out = torch.empty(h * cfg.d + 2 * h + 1, dtype=torch.float32, device=x.device)
+    with _torch_on(stream):
+        out = torch.empty(h * cfg.d + 2 * h + 1, dtype=torch.float32, device=x.device)
     if ws is None:
-        ws = workspace(lib().adadsf_router_backward_workspace_size(ctypes.byref(cfg), n), x.device)
+        ws = workspace(lib().adadsf_router_backward_workspace_size(ctypes.byref(cfg), n), x.device, stream)
     lw = layer_struct(w)
     _check(lib().adadsf_router_backward(ctypes.byref(cfg), ctypes.byref(lw), _p(x), _p(y_plain), _p(rows), n,
                                         _p(grad_y), _p(out), _p(ws), ws.numel(), _s(stream)))
@@ -359,7 +369,7 @@ def adadsf_router_scores(cfg: ModelCfg, w: dict, x: torch.Tensor, scores: torch.
     _dev(x, "x"); _dev(scores, "scores")
     n = x.numel() // cfg.d
     if ws is None:
-        ws = workspace(256, x.device)
+        ws = workspace(256, x.device, stream)
     lw = layer_struct(w)
     _check(lib().adadsf_router_scores(ctypes.byref(cfg), ctypes.byref(lw), _p(x), n, _p(scores),
                                       _p(ws), ws.numel(), _s(stream)))
@@ -381,7 +391,7 @@ def adadsf_router_select(cfg: ModelCfg, w: dict, x: torch.Tensor, B: int, T: int
                          ws: Optional[torch.Tensor] = None, stream=None):
     _dev(x, "x"); _dev(scores, "scores"); _dev(idx, "idx")
     if ws is None:
-        ws = workspace(adadsf_router_select_workspace_size(cfg, B, T), x.device)
+        ws = workspace(adadsf_router_select_workspace_size(cfg, B, T), x.device, stream)
     lw = layer_struct(w)
     _check(lib().adadsf_router_select(ctypes.byref(cfg), ctypes.byref(lw), _p(x), int(B), int(T), int(K),
                                       _p(scores), _p(idx), _p(rows), _p(ws), ws.numel(), _s(stream)))
@@ -393,7 +403,7 @@ def adadsf_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
     n_out, k_in = w.shape
     M = x.numel() // k_in
     if ws is None:
-        ws = workspace(256, x.device)
+        ws = workspace(256, x.device, stream)
     _check(lib().adadsf_linear(_p(x), _p(w), _p(bias), M, n_out, k_in, DTYPE_CODE[x.dtype], act,
                                _p(out), _p(ws), ws.numel(), _s(stream)))
 
@@ -409,7 +419,7 @@ def adadsf_causal_attention(cfg: ModelCfg, qkv: torch.Tensor, B: int, K: int, ou
                             ws: Optional[torch.Tensor] = None, stream=None):
     _dev(qkv, "qkv"); _dev(out, "out")
     if ws is None:
-        ws = workspace(adadsf_attention_workspace_size(cfg, B, K), qkv.device)
+        ws = workspace(adadsf_attention_workspace_size(cfg, B, K), qkv.device, stream)
     _check(lib().adadsf_causal_attention(ctypes.byref(cfg), _p(qkv), B, K, _p(out), _p(ws), ws.numel(),
                                          _s(stream)))
 
@@ -422,7 +432,7 @@ def adadsf_sparse_layer_forward(cfg: ModelCfg, w: dict, x: torch.Tensor, K: int,
     _dev(x, "x")
     B, T, _ = x.shape
     if ws is None:
-        ws = workspace(adadsf_layer_workspace_size(cfg, B, T, K), x.device)
+        ws = workspace(adadsf_layer_workspace_size(cfg, B, T, K), x.device, stream)
     lw = layer_struct(w)
     _check(lib().adadsf_sparse_layer_forward(ctypes.byref(cfg), ctypes.byref(lw), _p(x), B, T, int(K),
                                              _p(idx_out), _p(scores_out), _p(ws), ws.numel(),
@@ -450,7 +460,7 @@ def adadsf_sparse_model_forward(model: DeviceModel, ids: torch.Tensor, K: Sequen
     B, T = ids.shape
     Karr = (ctypes.c_int32 * len(K))(*[int(k) for k in K])
     if ws is None:
-        ws = workspace(adadsf_model_workspace_size(model.cfg, B, T, K, stats_acc is not None), ids.device)
+        ws = workspace(adadsf_model_workspace_size(model.cfg, B, T, K, stats_acc is not None), ids.device, stream)
     _check(lib().adadsf_sparse_model_forward(ctypes.byref(model.cfg), ctypes.byref(model.struct),
                                              _p(ids), B, T, ctypes.cast(Karr, ctypes.c_void_p),
                                              _p(hidden_out), _p(stats_acc), _p(idx_out), _p(ws),
@@ -484,7 +494,7 @@ def adadsf_prefill(model: DeviceModel, ids: torch.Tensor, K: Sequence[int], hidd
     B, T = ids.shape
     Karr = (ctypes.c_int32 * len(K))(*[int(k) for k in K])
     if ws is None:
-        ws = workspace(adadsf_model_workspace_size(model.cfg, B, T, K, False), ids.device)
+        ws = workspace(adadsf_model_workspace_size(model.cfg, B, T, K, False), ids.device, stream)
     _check(lib().adadsf_prefill(ctypes.byref(model.cfg), ctypes.byref(model.struct), _p(ids), B, T,
                                 ctypes.cast(Karr, ctypes.c_void_p), _p(hidden_out), _p(idx_out), _p(cache),
                                 cache.numel(),
@@ -498,7 +508,7 @@ def adadsf_decode_step(model: DeviceModel, ids: torch.Tensor, hidden_out: torch.
     _dev(ids, "ids"); _dev(hidden_out, "hidden_out"); _dev(cache, "cache")
     B = ids.numel()
     if ws is None:
-        ws = workspace(adadsf_decode_workspace_size(model.cfg, B, C_max), ids.device)
+        ws = workspace(adadsf_decode_workspace_size(model.cfg, B, C_max), ids.device, stream)
     _check(lib().adadsf_decode_step(ctypes.byref(model.cfg), ctypes.byref(model.struct), _p(ids), B,
                                     _p(hidden_out), _p(kept_out), _p(cache), cache.numel(), int(C_max), _p(ws),
                                     ws.numel(), _s(stream)))
@@ -577,7 +587,8 @@ def _fits(cfg: ModelCfg, cache: PagedCache):
 
 def adadsf_rope_table(cfg: ModelCfg, n_pos: int, device=None, stream=None) -> torch.Tensor:
     """(cos, sin) of positions 0 .. n_pos - 1: fp32 (n_pos, rotary_dim / 2, 2)."""
-    tab = torch.empty(int(n_pos), cfg.rotary_dim // 2, 2, dtype=torch.float32, device=device or "cuda")
+    with _torch_on(stream):
+        tab = torch.empty(int(n_pos), cfg.rotary_dim // 2, 2, dtype=torch.float32, device=device or "cuda")
     _check(lib().adadsf_rope_table(ctypes.byref(cfg), int(n_pos), tab.data_ptr(), _s(stream)))
     return tab
 
@@ -598,7 +609,7 @@ def adadsf_paged_append(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, qkv
     if tab is not None:
         _rows(tab, "tab", tab.shape[0], cfg.rotary_dim, torch.float32)
     if ws is None:
-        ws = workspace(256, qkv.device)
+        ws = workspace(256, qkv.device, stream)
     _check(lib().adadsf_paged_append(ctypes.byref(cfg), cache.ref, batch.ref, qkv.data_ptr(),
                                      None if tab is None else tab.data_ptr(), 0 if tab is None else tab.shape[0],
                                      None if pos is None else pos.data_ptr(),
@@ -613,7 +624,7 @@ def adadsf_paged_read(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, k_out
     _rows(k_out, "k_out", batch.n_rows, kv, dtype)
     _rows(v_out, "v_out", batch.n_rows, kv, dtype)
     if ws is None:
-        ws = workspace(256, k_out.device)
+        ws = workspace(256, k_out.device, stream)
     _check(lib().adadsf_paged_read(ctypes.byref(cfg), cache.ref, batch.ref, k_out.data_ptr(), v_out.data_ptr(),
                                    ws.data_ptr(), ws.numel(), _s(stream)))
 
@@ -635,7 +646,7 @@ def adadsf_paged_attention(cfg: ModelCfg, cache: PagedCache, batch: PagedBatch, 
         raise ValueError(f"q must be a CUDA tensor ({n}, {width}) of {dtype} with unit stride along a row")
     _rows(out, "out", n, width, dtype)
     if ws is None:
-        ws = workspace(adadsf_paged_attention_workspace_size(cfg, cache, batch), q.device)
+        ws = workspace(adadsf_paged_attention_workspace_size(cfg, cache, batch), q.device, stream)
     _check(lib().adadsf_paged_attention(ctypes.byref(cfg), cache.ref, batch.ref, q.data_ptr(),
                                         q.stride(0) if n > 1 else width, out.data_ptr(), ws.data_ptr(), ws.numel(),
                                         _s(stream)))
@@ -705,13 +716,13 @@ def adadsf_head_workspace_size(n_rows: int, d: int, n_classes: int, dtype: torch
     return n
 
 
-def _head(h, w_head, k, ws):
+def _head(h, w_head, k, ws, stream):
     dev, dtype = _on(w_head, "w_head"), w_head.dtype
     n_cls, d = w_head.shape
     n = h.shape[0]
     h_ptr = _mat(h, "h", (n, d), dtype, dev)
     if ws is None:
-        ws = workspace(adadsf_head_workspace_size(n, d, n_cls, dtype, k), w_head.device)
+        ws = workspace(adadsf_head_workspace_size(n, d, n_cls, dtype, k), w_head.device, stream)
     return dev, (h_ptr, w_head.data_ptr()), (n, d, n_cls, DTYPE_CODE[dtype]), _room(ws, dev)
 
 
@@ -740,7 +751,7 @@ def adadsf_head_loss(h: torch.Tensor, w_head: torch.Tensor, target: torch.Tensor
     none) through the head w_head (classes, d), no logit stored: loss and lse
     (fp32, n) receive the losses and logarithms that the backward call needs;
     acc (2 doubles) += {sum of losses, rows with a target}."""
-    dev, ptrs, size, room = _head(h, w_head, 1, ws)
+    dev, ptrs, size, room = _head(h, w_head, 1, ws, stream)
     n = size[0]
     _check(lib().adadsf_head_loss(*ptrs, _vec(target, "target", n, torch.int32, dev), *size, _vec(loss, "loss", n, _F32, dev),
                                   _vec(lse, "lse", n, _F32, dev), _vec(acc, "acc", 2, torch.float64, dev), *room, _s(stream)))
@@ -753,7 +764,7 @@ def adadsf_head_loss_backward(h: torch.Tensor, w_head: torch.Tensor, target: tor
     """Gradients of adadsf_head_loss's losses, each weighted by grad_loss (fp32,
     n; None: 1): grad_h like h, grad_w like w_head (either may be None;
     accumulate_w adds to what grad_w holds)."""
-    dev, ptrs, size, room = _head(h, w_head, 1, ws)
+    dev, ptrs, size, room = _head(h, w_head, 1, ws, stream)
     grads = _head_grads(size, w_head, lse, grad_loss, grad_h, grad_w, dev)
     _check(lib().adadsf_head_loss_backward(*ptrs, _vec(target, "target", size[0], torch.int32, dev), *size, *grads,
                                            1 if accumulate_w else 0, *room, _s(stream)))
@@ -765,7 +776,7 @@ def adadsf_distill_loss(h: torch.Tensor, w_head: torch.Tensor, top_idx: torch.Te
     """KL of each row's softmax at a temperature from a teacher's top logits:
     top_idx (int32, n x k; below 0: slot not in use) and top_logit (fp32).
     Outputs as adadsf_head_loss's."""
-    dev, ptrs, size, room = _head(h, w_head, _slots(h, top_idx), ws)
+    dev, ptrs, size, room = _head(h, w_head, _slots(h, top_idx), ws, stream)
     n = size[0]
     _check(lib().adadsf_distill_loss(*ptrs, *_teacher(top_idx, top_logit, n, dev), float(temperature), *size,
                                      _vec(loss, "loss", n, _F32, dev), _vec(lse, "lse", n, _F32, dev),
@@ -777,7 +788,7 @@ def adadsf_distill_loss_backward(h: torch.Tensor, w_head: torch.Tensor, top_idx:
                                  grad_h: Optional[torch.Tensor] = None, grad_w: Optional[torch.Tensor] = None,
                                  accumulate_w: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
     """Gradients of adadsf_distill_loss's losses (see adadsf_head_loss_backward)."""
-    dev, ptrs, size, room = _head(h, w_head, _slots(h, top_idx), ws)
+    dev, ptrs, size, room = _head(h, w_head, _slots(h, top_idx), ws, stream)
     grads = _head_grads(size, w_head, lse, grad_loss, grad_h, grad_w, dev)
     _check(lib().adadsf_distill_loss_backward(*ptrs, *_teacher(top_idx, top_logit, size[0], dev), float(temperature), *size,
                                               *grads, 1 if accumulate_w else 0, *room, _s(stream)))
@@ -811,7 +822,7 @@ def adadsf_norm_backward(grad_y: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     dev, dtype, shape = _on(x, "x"), x.dtype, x.shape
     n, d = shape
     if ws is None:
-        ws = workspace(adadsf_norm_backward_workspace_size(n, d), x.device)
+        ws = workspace(adadsf_norm_backward_workspace_size(n, d), x.device, stream)
     _check(lib().adadsf_norm_backward(_mat(grad_y, "grad_y", shape, dtype, dev), x.data_ptr(), _vec(w, "w", d, dtype, dev),
                                       _vec(mean, "mean", n, _F32, dev), _vec(rstd, "rstd", n, _F32, dev),
                                       None if add is None else _mat(add, "add", shape, dtype, dev), n, d, DTYPE_CODE[dtype],
@@ -826,7 +837,7 @@ def adadsf_embed_forward(ids: torch.Tensor, table: torch.Tensor, out: torch.Tens
     dev, dtype = _on(table, "table"), table.dtype
     n, (vocab, d) = ids.numel(), table.shape
     if ws is None:
-        ws = workspace(256, table.device)
+        ws = workspace(256, table.device, stream)
     _check(lib().adadsf_embed_forward(_vec(ids, "ids", n, torch.int32, dev), n, table.data_ptr(), vocab, d, DTYPE_CODE[dtype],
                                       scale, _mat(out, "out", (n, d), dtype, dev), *_room(ws, dev), _s(stream)))
 
@@ -845,7 +856,7 @@ def adadsf_embed_backward(ids: torch.Tensor, grad_out: torch.Tensor, grad_table:
     dev, dtype = _on(grad_table, "grad_table"), grad_table.dtype
     n, (vocab, d) = ids.numel(), grad_table.shape
     if ws is None:
-        ws = workspace(adadsf_embed_backward_workspace_size(n, vocab, d), grad_table.device)
+        ws = workspace(adadsf_embed_backward_workspace_size(n, vocab, d), grad_table.device, stream)
     _check(lib().adadsf_embed_backward(_vec(ids, "ids", n, torch.int32, dev), _mat(grad_out, "grad_out", (n, d), dtype, dev), n,
                                        vocab, d, DTYPE_CODE[dtype], scale, grad_table.data_ptr(), 1 if accumulate else 0,
                                        *_room(ws, dev), _s(stream)))

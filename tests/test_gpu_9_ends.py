@@ -583,6 +583,44 @@ def test_calls_at_once(A):
                 assert torch.equal(x, y)
 
 
+def test_scratch_of_calls_on_another_stream(A):
+    """Calls on a side stream without a workspace, while the current stream is busy: what they make by themselves comes from
+    memory that held ones, cleared in order with their kernels."""
+    n, d, V = 24, 256, 3000
+    h, w, target, gl = head_inputs(n, d, V, "bf16")
+    x, wn, b, dy, _ = norm_inputs(n, d, "bf16", False, False)
+    ids = torch.randint(0, V, (n,), generator=gen(4), device="cuda", dtype=torch.int32)
+    vectors, rows = [torch.empty(n, device="cuda") for _ in range(4)], [torch.empty_like(x) for _ in range(4)]
+    dw, db, head, table = torch.empty(d, device="cuda"), torch.empty(d, device="cuda"), torch.empty_like(w), torch.empty_like(w)
+    outs = [*vectors, *rows, dw, db, head, table]
+
+    def run(stream):
+        loss, lse, mean, rstd = vectors
+        y, dx, out, dh = rows
+        A.adadsf_embed_forward(ids, w, out, stream=stream)
+        A.adadsf_norm_forward(x, wn, b, y, 1e-5, mean, rstd, stream=stream)
+        A.adadsf_head_loss(h, w, target, loss, lse, stream=stream)
+        A.adadsf_head_loss_backward(h, w, target, lse, grad_loss=gl, grad_h=dh, grad_w=head, stream=stream)
+        A.adadsf_norm_backward(dy, x, wn, rstd, dx, mean=mean, grad_w=dw, grad_b=db, stream=stream)
+        A.adadsf_embed_backward(ids, dy, table, stream=stream)
+
+    run(None)
+    want = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        held = [torch.full((m,), 255, dtype=torch.uint8, device="cuda") for m in (1 << 28, 1 << 20, 1 << 20, 256, 256)]
+        del held
+    for t in outs:
+        t.fill_(7)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        torch.cuda._sleep(100_000_000)
+        run(side)
+    torch.cuda.synchronize()
+    for got, ref in zip(outs, want):
+        assert torch.equal(got, ref)
+
+
 # ------------------------------------------------------------------ norms
 def norm_inputs(n, d, dtype, rms, res):
     g = gen(n * 7 + d)
