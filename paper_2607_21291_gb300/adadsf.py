@@ -191,6 +191,28 @@ def _torch_on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
+@contextlib.contextmanager
+def in_order(stream):
+    """A step's torch work and library calls in one order, on `stream`: it waits for what the current stream was given
+    before, and the current stream for the step, also where that fails halfway. Yields a function that tells the allocator
+    of results which the caller reads on the current stream. None, or the current stream: nothing to do."""
+    outer = None if stream is None else torch.cuda.current_stream()
+    if stream is None or stream == outer:
+        yield lambda *results: None
+        return
+
+    def read_outside(*results):
+        for t in results:
+            t.record_stream(outer)
+
+    stream.wait_stream(outer)
+    try:
+        with torch.cuda.stream(stream):
+            yield read_outside
+    finally:
+        outer.wait_stream(stream)
+
+
 def workspace(nbytes: int, device=None, stream=None) -> torch.Tensor:
     """Zero-initialised device workspace (its first 256 bytes are the error word), cleared on the stream (None: the current
     one). Calls on other streams have to wait for that."""

@@ -32,6 +32,11 @@ def router_alignment_step(shape_cfg: A.ModelCfg, w: dict, x: torch.Tensor, h_den
     gated sparse layer's output on x (B, T, d) and h_dense (B, T, d).
     shape_cfg: the layer's config (the gate flag is set here). Returns the
     layer's L_hid before the step (mean over the B T tokens)."""
+    with A.in_order(stream):
+        return _router_step(shape_cfg, w, x, h_dense, K, lr, stream, ws)
+
+
+def _router_step(shape_cfg, w, x, h_dense, K, lr, stream, ws):
     B, T, d = x.shape
     cfg_g = A.ModelCfg.from_buffer_copy(shape_cfg)
     cfg_g.flags = int(cfg_g.flags) | A.FLAG_GATE_SIGMOID
@@ -72,7 +77,17 @@ def ends_gradients(cfg: A.ModelCfg, w: dict, ids: torch.Tensor, target: Optional
     body(x (tokens, d)) returns (y, pull), the layers' output and the function
     from a gradient at y to the one at x; None: no layers. Returns the mean over
     the tokens that have a loss (0-d, on the device) and the gradients by name;
-    a shared table's is the sum of both ends'."""
+    a shared table's is the sum of both ends' (rounded to its type after either).
+    stream: where all of it runs, body and pull as well (torch's current stream
+    inside them); the current stream is waited for before, and waits for the
+    results."""
+    with A.in_order(stream) as read_outside:
+        loss, grads = _ends(cfg, w, ids, target, body, top, scale, stream)
+        read_outside(loss, *grads.values())
+    return loss, grads
+
+
+def _ends(cfg, w, ids, target, body, top, scale, stream):
     embed = w["embed"]
     head = w.get("head", embed)
     rms = cfg.arch == A.ARCH_QWEN
@@ -123,7 +138,9 @@ def ends_step(cfg: A.ModelCfg, w: dict, ids: torch.Tensor, target: Optional[torc
               body: Optional[Callable] = None, top: Optional[tuple] = None, scale: float = 1.0, stream=None):
     """One plain SGD step on the tensors of w (in place) by ends_gradients;
     returns the loss before it."""
-    loss, grads = ends_gradients(cfg, w, ids, target, body, top, scale, stream)
-    for name, g in grads.items():
-        w[name].copy_(w[name].float().sub_(g.float(), alpha=lr))
+    with A.in_order(stream) as read_outside:
+        loss, grads = _ends(cfg, w, ids, target, body, top, scale, stream)
+        for name, g in grads.items():
+            w[name].copy_(w[name].float().sub_(g.float(), alpha=lr))
+        read_outside(loss)
     return loss

@@ -49,11 +49,12 @@ def calibrate(model: "A.DeviceModel", ids: torch.Tensor, t: float, tau: float = 
               group: Optional[dist.ProcessGroup] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Dense forward with statistics on this replica's calibration ids, sum over
     replicas, allocation. Returns (s, r, K) -- identical on every replica."""
-    B, T = ids.shape
-    L = model.cfg.n_layers
-    acc = torch.zeros(2 * L, dtype=torch.float64, device=ids.device)
-    out = torch.empty((B, T, model.cfg.d), device=ids.device,
-                      dtype=torch.bfloat16 if model.cfg.dtype == A.BF16 else torch.float32)
-    A.adadsf_sparse_model_forward(model, ids, [T] * L, out, stats_acc=acc, ws=ws, stream=stream)
-    acc = allreduce_stats(acc, group)
-    return retention_plan(acc, T, t, tau, beta)
+    with A.in_order(stream):
+        B, T = ids.shape
+        L = model.cfg.n_layers
+        acc = torch.zeros(2 * L, dtype=torch.float64, device=ids.device)
+        out = torch.empty((B, T, model.cfg.d), device=ids.device,
+                          dtype=torch.bfloat16 if model.cfg.dtype == A.BF16 else torch.float32)
+        A.adadsf_sparse_model_forward(model, ids, [T] * L, out, stats_acc=acc, ws=ws, stream=stream)
+        acc = allreduce_stats(acc, group)
+        return retention_plan(acc, T, t, tau, beta)

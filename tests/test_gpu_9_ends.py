@@ -947,3 +947,51 @@ def test_ends_together(A, arch, dtype, tied, teacher):
     for k in w:   # one rounding of the update
         step = before[k].double() - 0.5 * grads[k].double()
         within(w[k], step, (B16 if dtype == "bf16" else U) * 2 * step.abs() + 1e-7, k)
+
+
+@pytest.mark.parametrize("dtype,tied", [("bf16", True), ("f32", False)])
+def test_ends_on_another_stream(A, dtype, tied):
+    """A step on a stream of the caller's while the current one is busy and writes the ids behind that: the same bits as on
+    the current stream, results read on the current one without more ado, and freed there."""
+    from paper_2607_21291_gb300 import align
+    from paper_2607_21291_gb300 import synth as S
+    d, V, n = 128, 700, 150
+    cfg = A.make_cfg(S.PYTHIA_70M.replace(d=d, vocab=V, dtype=dtype))
+    g = gen(19)
+    w = {"embed": randn(g, V, d, std=0.3).to(DT[dtype]), "final_w": (1 + randn(g, d, std=0.1)).to(DT[dtype]),
+         "final_b": randn(g, d, std=0.1).to(DT[dtype])}
+    if not tied:
+        w["head"] = randn(g, V, d, std=0.1).to(DT[dtype])
+    real = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    target = torch.roll(real, -1).contiguous()
+    target[:40] = -1
+    turn = randn(g, d)
+    on = []
+
+    def body(x):
+        on.append(torch.cuda.current_stream())
+        return (x.float() * turn).to(x.dtype), lambda gy: (gy.float() * turn).to(gy.dtype)
+
+    want_loss, want = align.ends_gradients(cfg, w, real, target, body=body)
+    want_w = {k: v.clone() for k, v in w.items()}
+    align.ends_step(cfg, want_w, real, target, 0.5, body=body)
+    side, ids = torch.cuda.Stream(), torch.empty_like(real)
+    with torch.cuda.stream(side):
+        held = [torch.full((m,), 255, dtype=torch.uint8, device="cuda") for m in (1 << 28, *[1 << 20] * 8, *[1024] * 8)]
+        del held
+    torch.cuda.synchronize()
+    for _ in range(3):
+        ids.fill_(-1)
+        torch.cuda._sleep(50_000_000)
+        ids.copy_(real)
+        loss, grads = align.ends_gradients(cfg, w, ids, target, body=body, stream=side)
+        mine = {k: v.clone() for k, v in w.items()}
+        step_loss = align.ends_step(cfg, mine, ids, target, 0.5, body=body, stream=side)
+        assert on[-1] == side and torch.cuda.current_stream() != side
+        got = {k: v + 0 for k, v in grads.items()}
+        assert torch.equal(loss, want_loss) and torch.equal(step_loss, want_loss)
+        del grads, loss, step_loss
+        with torch.cuda.stream(side):
+            torch.full((1 << 22,), 7.0, device="cuda")
+        for k in want:
+            assert torch.equal(got[k], want[k]) and torch.equal(mine[k], want_w[k]), k

@@ -67,3 +67,77 @@ def test_a_function_without_that_is_found():
             m.setattr(inspect, "getsource", lambda _: source)
             with pytest.raises(AssertionError):
                 test_the_binding_makes_tensors_on_the_calls_stream()
+
+
+class Stream:
+    def __init__(self, name, log):
+        self.name, self.log = name, log
+
+    def wait_stream(self, other):
+        self.log.append((self.name, "waits for", other.name))
+
+
+class Result:
+    def __init__(self, log):
+        self.log = log
+
+    def record_stream(self, stream):
+        self.log.append(("result read on", stream.name))
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    log = []
+    now = [Stream("current", log)]
+
+    @contextlib.contextmanager
+    def on(stream):
+        now.append(stream)
+        log.append(("on", stream.name))
+        yield
+        log.append(("off", stream.name))
+        now.pop()
+
+    monkeypatch.setattr(A.torch.cuda, "stream", on)
+    monkeypatch.setattr(A.torch.cuda, "current_stream", lambda: now[-1])
+    return log, now[0], Stream("side", log)
+
+
+def test_a_step_on_another_stream_is_in_order_with_the_current_one(streams):
+    log, _, side = streams
+    with A.in_order(side) as read_outside:
+        log.append("work")
+        read_outside(Result(log))
+    assert log == [("side", "waits for", "current"), ("on", "side"), "work", ("result read on", "current"), ("off", "side"),
+                   ("current", "waits for", "side")]
+
+
+def test_a_step_that_fails_is_waited_for_too(streams):
+    log, _, side = streams
+    with pytest.raises(ValueError):
+        with A.in_order(side):
+            raise ValueError
+    assert log[-1] == ("current", "waits for", "side")
+
+
+def test_a_step_on_the_current_stream_waits_for_nothing(streams):
+    log, current, _ = streams
+    for stream in (None, current):
+        with A.in_order(stream) as read_outside:
+            read_outside(Result(log))
+    assert log == []
+
+
+@pytest.mark.parametrize("module", ["align", "calibrate"])
+def test_steps_run_in_order(module):
+    """Functions of torch work between library calls: all of what takes a caller's stream is under in_order(stream)."""
+    from importlib import import_module
+    source = ast.parse(inspect.getsource(import_module(f"paper_2607_21291_gb300.{module}")))
+    seen = 0
+    for f in source.body:
+        if isinstance(f, ast.FunctionDef) and "stream" in [a.arg for a in f.args.args[len(f.args.args) - len(f.args.defaults):]]:
+            work = [s for s in f.body if not (isinstance(s, ast.Expr) and isinstance(s.value, ast.Constant))]
+            assert isinstance(work[0], ast.With) and ast.unparse(work[0].items[0].context_expr) == "A.in_order(stream)", f.name
+            assert all(isinstance(s, ast.Return) for s in work[1:]), f.name
+            seen += 1
+    assert seen == {"align": 3, "calibrate": 1}[module]
