@@ -404,7 +404,8 @@ cudaError_t head_backward(int dtype, const Head& a, const HeadPlan& plan, const 
   // The gradient's logits of few fp32 rows come from the kernel of their forward pass: at a target of nearly all the weight q - 1
   // is a difference of logits of both passes, and those of the other kernel, added up in another order, leave their
   // roundings (20 rows of 256 features, 5000 classes: head gradient 3.0e-6 off, so 1.4e-6). It is quicker as well: loss and
-  // gradients of 77 rows at a 50304 x 512 head 285 -> 267 us. bf16 gradients round far above that.
+  // gradients of 77 rows at a 50304 x 512 head 285 -> 267 us. bf16 logits are one product a step, which both kernels add up in
+  // the same chunks and order: the same bits.
   const bool few = dtype != kBF16 && a.n <= kHeadFewRowsF32;
   cudaError_t e = dtype == kBF16 ? pack<bf16>(a, true, true, dev) : pack<float>(a, true, !few || a.dh, dev);
   for (int j = 0; few && j < plan.pieces && e == cudaSuccess; ++j) {

@@ -23,7 +23,7 @@
 //
 // The tensor cores cut what an addition loses instead of rounding it, so a sum of many steps drifts towards zero: 320 steps
 // of 16 k were 1e-5 of a logit off, which its exponential multiplies (fp32 gradients 5e-5). Where fp32 results come
-// of it (logits of the forward pass, all fp32 products) a tile's k are cut in chunks of at most 32 steps (fp32: 16, each of
+// of it (logits, all fp32 products) a tile's k are cut in chunks of at most 32 steps (fp32: 16, each of
 // which holds its six products), whose accumulators the epilogue's threads add up in registers, rounding, while the next
 // chunk is multiplied. Chunks of 32, 16 and 8 steps: 700 fp32 rows of 512 features, 50304 classes, head gradient 1.2e-6, 7e-7 and
 // 5e-7 off; loss and gradients of 645 such rows 671, 674 and 694 us. bf16, 64, 32 and 16 steps: losses of 400 rows of 5120 features 6e-7,
@@ -166,12 +166,15 @@ __device__ __forceinline__ void red_add4(float* p, const float4& v) {
   asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
-// Blocks of 64 k whose products share an accumulator. bf16 gradients: LONG cuts sums of more than 65536 rows (or classes, or
-// features), below which the loss does not show: one of 4 million rows was 3.6e-3 short (head gradients 4.4e-3 off, of which
-// roundings are 1.8e-3). A kernel of its own: its registers cost gradients of 27 tokens at a 151936 x 1536 head 341 -> 346 us.
-constexpr int kHtLong = 1024;
-template <bool GRAD, bool F32, bool LONG>
-__host__ __device__ constexpr int chunk_blocks() { return F32 ? 4 : LONG ? kHtLong : GRAD ? 1 << 20 : 8; }
+// Blocks of 64 k whose products share an accumulator. G's logits are added up as those of the forward pass are, so that both passes
+// have the same ones: q - 1 of a target of nearly all the weight is a difference of the two, and of one chain of 320
+// steps beside chunks of 32 it was 6e-4 off where it is 3e-4 itself. bf16 gradients: sums of more than 65536 rows (or
+// classes) are cut, below which the loss does not show: one of 4 million rows was 3.6e-3 short (head gradients 4.4e-3 off, of
+// which roundings are 1.8e-3). Without the chunks of G's logits gradients of 27 rows at a 151936 x 1536 head took 338 us (346 with them), of
+// 3330 at the Pythia-1.4B head 1361 (1412), of 3450 at the Qwen2.5-7B head 6950 (7090).
+constexpr int kHtLogits = 8, kHtLong = 1024;
+template <bool F32>
+__device__ __forceinline__ int chunk_blocks(int kind) { return F32 ? 4 : kind == kStats || kind == kG ? kHtLogits : kHtLong; }
 
 // A warp's loads from TMEM are done (tcgen05.wait::ld): only that is told, so the arrival is relaxed. Released, it waits
 // until the warp's stores to global memory are performed (gradients of 500 tokens at the Qwen2.5-7B head 1104 -> 1079 us).
@@ -474,7 +477,7 @@ __device__ __forceinline__ void dw_tile(const HtDev& p, const CUtensorMap& tm, c
   if (F32) release();
 }
 
-template <bool GRAD, bool F32, bool LONG>
+template <bool GRAD, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
     head_tc_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                    const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmGo,
@@ -533,7 +536,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
   const int count = *p.count;
   const CUtensorMap& tmH = !F32 && count == p.n ? tmA : tmP;   // bf16 rows that all count were not packed
   const Tiles<GRAD> tiles(p, count);
-  constexpr int TERMS = F32 ? kHeadTerms : 1, CHUNK = chunk_blocks<GRAD, F32, LONG>();
+  constexpr int TERMS = F32 ? kHeadTerms : 1;
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (both CTAs)
@@ -545,6 +548,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       for (int t = pair; t < tiles.n && ok; t += num_pairs) {
         const Tile ti = tiles.at(p, count, t);
         const int a0 = ti.mb * kHtTile + (int)rank * 128, b0 = ti.nb * kHtTile + (int)rank * 128;
+        const int chunk = chunk_blocks<F32>(ti.kind);
         int first = 0, kb = 0, term = 0;   // of the chunk, in it, and the product of parts
         int64_t pa = 0, pb = 0;            // rows before the parts
         auto parts = [&] {
@@ -580,11 +584,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
             tma_load_2d_pair(b_s, &tmH, b0, b, fb);
             tma_load_2d_pair(b_s + kHtBox, &tmH, b0 + 64, b, fb);
           }
-          if (++kb == min(CHUNK, ti.nkb - first)) {
+          if (++kb == min(chunk, ti.nkb - first)) {
             kb = 0;
             if (++term == TERMS) {
               term = 0;
-              first += CHUNK;
+              first += chunk;
             }
             parts();
           }
@@ -616,9 +620,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
         const uint32_t id = idesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
         const uint32_t a_hi = a_mn ? kMajorMN : kMajorK, b_hi = b_mn ? kMajorMN : kMajorK;
         const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;   // 16 k on, in 16 bytes
+        const int chunk = chunk_blocks<F32>(ti.kind);
         int first = 0;
         do {   // a chunk (one without blocks where there is no k)
-          const int acc = it & 1, blocks = min(CHUNK, ti.nkb - first) * TERMS;
+          const int acc = it & 1, blocks = min(chunk, ti.nkb - first) * TERMS;
           if (!mbar_wait_bounded(tempty0 + 8 * acc, ((it >> 1) & 1) ^ 1, abort_flag, p.err, p.timeout_ns)) {
             ok = false;
             break;
@@ -642,7 +647,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
           if (!ok) break;
           tc_commit_pair_multicast(tfull0 + 8 * acc, 0x3);   // both CTAs' accumulators ready
           ++it;
-          first += CHUNK;
+          first += chunk;
         } while (first < ti.nkb);
       }
       tc_commit_pair_multicast(drain, 0x1);
@@ -677,9 +682,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
       };
       wait();
       if (!ok) break;
-      if ((F32 || LONG || !GRAD) && ti.nkb > CHUNK) {
+      const int chunk = chunk_blocks<F32>(ti.kind);
+      if (ti.nkb > chunk) {
         float run[128];
-        int first = CHUNK;
+        int first = chunk;
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
           uint32_t r[32];
@@ -692,7 +698,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHtThreads, 1)
         for (;;) {
           wait();
           if (!ok) break;
-          first += CHUNK;
+          first += chunk;
           const bool last = first >= ti.nkb;
 #pragma unroll
           for (int c = 0; c < 128; c += 16) {
@@ -765,16 +771,16 @@ HtDev head_dev(const Head& a, const Dev& dev) {
 
 int ceil_to(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
-template <bool GRAD, bool F32, bool LONG = false>
+template <bool GRAD, bool F32>
 cudaError_t launch_tiles(int64_t tiles, const Head& a, const CUtensorMap& tg, const CUtensorMap& tgo, const CUtensorMap& tdw,
                          const HtDev& p, const Dev& dev) {
-  const cudaError_t e = allow_smem<head_tc_kernel<GRAD, F32, LONG>, kHtSmem>();
+  const cudaError_t e = allow_smem<head_tc_kernel<GRAD, F32>, kHtSmem>();
   if (e != cudaSuccess || tiles == 0) return e;
   CUtensorMap th, ta = {}, tw;
   if (!head_maps(F32, a, &th, &tw)) return cudaErrorInvalidValue;
   if (!F32 && !make_tmap_bf16(&ta, a.h, (uint64_t)a.n, (uint64_t)a.d, (uint64_t)a.d, 64, 64)) return cudaErrorInvalidValue;
   const int pairs = (int)std::min<int64_t>(tiles, dev.num_sms / 2);
-  return launch_pdl(head_tc_kernel<GRAD, F32, LONG>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, ta, tw, tg, tgo, tdw,
+  return launch_pdl(head_tc_kernel<GRAD, F32>, dim3(2 * pairs), dim3(kHtThreads), kHtSmem, dev.stream, th, ta, tw, tg, tgo, tdw,
                     p);
 }
 
@@ -813,9 +819,7 @@ cudaError_t head_grad(int dtype, const Head& a, int buf, int64_t v_g, int n_g, i
   const int64_t mbs = ceil_to(a.n, kHtTile), nbd = ceil_to(a.d, kHtTile);
   const int64_t tiles = mbs * p.n_g + (p.want_h && n_d ? mbs * nbd * p.splits : 0) + (p.want_w ? ceil_to(n_d, kHtTile) * nbd : 0);
   if (dtype != kBF16) return launch_tiles<true, true>(tiles, a, tg, tgo, tdw, p, dev);
-  const bool long_sums = std::max({(int64_t)ceil_to(a.n, kHtK), (int64_t)ceil_to(p.kb_d, p.splits), (int64_t)ceil_to(a.d, kHtK)}) > kHtLong;
-  return long_sums ? launch_tiles<true, false, true>(tiles, a, tg, tgo, tdw, p, dev)
-                   : launch_tiles<true, false>(tiles, a, tg, tgo, tdw, p, dev);
+  return launch_tiles<true, false>(tiles, a, tg, tgo, tdw, p, dev);
 }
 
 }  // namespace adadsf

@@ -512,6 +512,75 @@ def test_head_of_one_class_has_no_gradient(A, n, d):
         assert (x == 0).all()
 
 
+@pytest.mark.parametrize("n", [1, 20, 127, 128, 129, 300])
+@pytest.mark.parametrize("d", [64, 520, 1000, 5128])
+def test_bf16_head_of_one_class_has_no_gradient(A, n, d):
+    """As for fp32 above: both passes have the same bf16 logits, also where few rows' losses come from another kernel."""
+    h, w, target, _ = head_inputs(n, d, 1, "bf16")
+    for t in (torch.zeros_like(target), target):
+        loss, lse, _, dh, dw = ce(A, h, w, t)
+        for x in (loss, dh, dw):
+            assert (x == 0).all()
+
+
+@pytest.mark.parametrize("n", [1, 20, 128, 129, 300])
+@pytest.mark.parametrize("d", [520, 2048, 5128])
+def test_bf16_head_gradients_of_sure_rows(A, n, d):
+    """bf16 rows that are all but sure of class 5, by products of one sign that add up to logits of some 60: q - 1 there, of
+    some 1e-4, is a difference of numbers near 1. A column of ones in the head sums a row's G, which is 0 but for
+    roundings; a column that only class 5 has picks its entry."""
+    V = 300
+    g = gen(n * 3 + d)
+    w = (randn(g, V, d).abs() * (60 / (0.64 * d))).to(torch.bfloat16)
+    h = randn(g, n, d).abs()
+    w[:, 7], w[:, 8] = 1.0, 0.0
+    w[5, 8] = 1.0
+    h[:, 7:9] = 0.0
+    z = h.double() @ w.double().T
+    along = w[5].double().clone()
+    along[7:9] = 0.0
+    gap = along @ (along - w.double()).T      # by how much a step along class 5's row raises its logit over another's
+    gap[5] = math.inf
+    assert float(gap.min()) > 0
+    lift = ((z - z[:, 5:6] + 12.0) / gap).amax(-1).clamp(min=0.0)
+    h = (h + (lift[:, None] * along).float()).to(torch.bfloat16)
+    h[:, 7:9] = 0.0
+    loss, lse, _, dh, _ = ce(A, h, w, torch.full((n,), 5, dtype=torch.int32, device="cuda"))
+    z = h.double() @ w.double().T
+    ref = torch.logsumexp(z, -1)
+    q = torch.exp(z - ref[:, None])
+    rest = q.clone()
+    rest[:, 5] = 0.0
+    rest = rest.sum(-1)                       # 1 - q of class 5; the sum of |G| is twice that
+    assert float(rest.max()) < 2e-3
+    spread = (q * (z.amax(-1, keepdim=True) - z)).sum(-1) + (q * (z - ref[:, None]).abs()).sum(-1)
+    # the same logits in both passes: as in test_head_gradients_of_sure_rows, and G's rounding to bf16
+    one = U * ref.abs() + 3 * U * spread + (4 + 4 + 8 + 8) * U + 2 * U * (64 + 32) * 2 * rest
+    bound = one + B16 * 2 * rest + 2 * U * terms(V, False, True) * 2 * rest
+    within(dh[:, 7], torch.zeros(n, device="cuda"), (1 + B16) * bound, "sum of G")
+    # the others' shares go by the logits' differences
+    e_z = 2 * (2 * terms(d, False, False) + 4) * U * (h.double().abs() @ w.double().abs().T).amax(-1)
+    bound = one + e_z * rest
+    within(dh[:, 8], -rest, bound + 2 * B16 * (rest + bound), "G of the target")
+
+
+@pytest.mark.parametrize("n", [60, 200])
+@pytest.mark.parametrize("d,dtype", [(128, "bf16"), (5128, "bf16"), (128, "f32"), (1028, "f32")])
+def test_wide_logits_gradients(A, n, d, dtype):
+    """Logits of thousands: the gradients too are as near as their sums' bounds."""
+    h, w, target, gl = head_inputs(n, d, 900, dtype, std=1500.0)
+    want, used = want_of(target, 900)
+    ref = Ref(h, w, want, used, torch.zeros(n, dtype=torch.float64, device="cuda"), gl, 1.0, 1)
+    # most entries of G lie below fp32's normal numbers, where exponentials, their shares and products are zeros: each by
+    # less than 2^-126, which meets the other operand
+    hd = torch.where(used[:, None], h.double().abs(), 0.0)
+    ref.e_dh += 3 * 2.0 ** -126 * w.double().abs().sum(0)
+    ref.e_dw += 3 * 2.0 ** -126 * hd.sum(0)
+    loss, lse, _, dh, dw = ce(A, h, w, target, gl)
+    assert float(ref.lse.max()) > 1000
+    ref.check(loss, lse, dh, dw)
+
+
 @pytest.mark.parametrize("n,V", [(1, 31), (32, 33), (33, 64), (64, 65), (65, 4900), (80, 5000), (50, 180000)])
 def test_head_gradients_of_few_rows(A, n, V):
     """fp32 rows on both sides of the zeros that products over rows need, classes on both sides of their blocks and more than a
