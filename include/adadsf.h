@@ -280,9 +280,12 @@ adadsf_status adadsf_router_backward(const adadsf_model_cfg *cfg, const adadsf_l
                                      void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
- * Losses at the LM head, in pieces of the classes: no call stores the logits,
- * its scratch grows with n_rows n_classes / 16 bytes and a piece's share of
- * them. h_dev [n_rows, d] and w_head_dev [n_classes, d] in `dtype`; with
+ * Losses at the LM head, in pieces of the classes: no call stores the logits.
+ * Its scratch holds a copy of the rows (fp32: three of rows and head in bf16)
+ * and, for the forward call, 8 bytes for each row and 128 classes, for the
+ * backward call in the same place two pieces of the logits' gradients (some
+ * 256 MB each, or 2048 classes of all rows where that is more) and up to four
+ * fp32 sums of grad_h_dev (few rows: up to some 42 MB of them). h_dev [n_rows, d] and w_head_dev [n_classes, d] in `dtype`; with
  * l = h w_head^T (fp32):
  *   adadsf_head_loss: cross entropy of a target a row, loss = lse - l[target],
  *     lse = log sum_c e^{l_c} (the L_causal of Table 4). target_dev [n_rows]
@@ -311,7 +314,7 @@ adadsf_status adadsf_router_backward(const adadsf_model_cfg *cfg, const adadsf_l
  * repeat bit for bit.
  * d % 8 == 0 (bf16) or d % 4 == 0 (fp32); any n_classes up to 2^24; n_rows up
  * to 2^22; top_k up to 1024. ws: adadsf_head_workspace_size bytes (top_k 1 for
- * adadsf_head_loss), for either direction.
+ * adadsf_head_loss), for either direction and for fewer rows or slots as well.
  * ---------------------------------------------------------------------- */
 size_t adadsf_head_workspace_size(int64_t n_rows, int d, int n_classes, int dtype, int top_k);
 adadsf_status adadsf_head_loss(const void *h_dev, const void *w_head_dev, const int32_t *target_dev,

@@ -1911,7 +1911,13 @@ adadsf_status check_temperature(float temperature) {
 
 size_t adadsf_head_workspace_size(int64_t n_rows, int d, int n_classes, int dtype, int top_k) {
   if (check_head(n_rows, d, n_classes, dtype, top_k) != ADADSF_OK) return 0;
-  return head_layout(n_rows, d, n_classes, dtype, top_k).total;
+  // more rows may mean smaller pieces, whose buffers take less: the size is what every number of rows up to n_rows needs
+  size_t most = head_layout(n_rows, d, n_classes, dtype, top_k).total;
+  for (int64_t n = kHeadRowPad; n < n_rows; n += kHeadRowPad) {
+    const size_t need = head_layout(n, d, n_classes, dtype, top_k).total;
+    if (need > most) most = need;
+  }
+  return most;
 }
 
 adadsf_status adadsf_head_loss(const void* h_dev, const void* w_head_dev, const int32_t* target_dev, int64_t n_rows, int d,

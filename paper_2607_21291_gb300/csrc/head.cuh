@@ -14,7 +14,6 @@
 
 namespace adadsf {
 
-constexpr int kHeadRowPad = 256;   // packed buffers hold whole tiles of rows
 constexpr int kHeadZeroPad = 64;   // rows past the last packed one, up to a multiple of this, are zero in the packed copy
 
 // fp32 numbers as sums of three bf16 numbers, their leading 8 bits, the next 8 and the last: the next part of a (low

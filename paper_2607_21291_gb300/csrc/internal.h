@@ -339,6 +339,7 @@ struct HeadPlan {
   int ld, Vp, piece, pieces, splits;
   size_t packed, w_parts, rec, g, acc;   // bytes
 };
+constexpr int kHeadRowPad = 256;           // packed buffers hold whole tiles of rows: plans change at its multiples only
 HeadPlan head_plan(int dtype, int64_t n, int d, int V);
 constexpr int kHeadMaxK = 1024;
 // Teacher's logits [n][k] -> ascending classes, weights, sum p log p and first class of each row.

@@ -163,3 +163,18 @@ def test_binding_refuses_tensors(A):
         A.adadsf_embed_forward(t, w, h)
     with pytest.raises(ValueError):
         A.adadsf_embed_backward(t, h, w)
+
+
+@pytest.mark.parametrize("d,V,dtype", [(3584, 152064, "bf16"), (2048, 50304, "bf16"), (512, 50304, "f32"), (64, 300, "bf16"),
+                                       (8, 2 ** 20, "bf16"), (1536, 151936, "f32")])
+def test_head_workspace_serves_fewer_rows(A, d, V, dtype):
+    """A workspace for the longest batch is large enough for every shorter one."""
+    size = A.adadsf_head_workspace_size
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    last = 0
+    for n in sorted({0, 1, 80, 81, 128, 129, *range(255, 20000, 256), *range(256, 20000, 256), *range(257, 20000, 256),
+                     *(r + o for r in (2 ** 15, 2 ** 16, 65537 + 256, 2 ** 18, 2 ** 20, 2 ** 22 - 256) for o in (-1, 0, 1, 256))}):
+        now = size(n, d, V, dt)
+        assert now >= last, (n, now, last)
+        last = now
+    assert size(1000, d, V, dt, 64) <= size(2000, d, V, dt, 64)

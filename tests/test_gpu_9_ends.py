@@ -621,6 +621,17 @@ def test_head_weights_of_rows(A, dtype):
     assert (got[3] == 0).all() and (got[4] == 0).all()
 
 
+def test_head_workspace_of_more_rows(A):
+    """One workspace for the longest batch: a shorter one in it, which takes the classes in fewer and larger pieces."""
+    d, V = 64, 152064
+    ws = A.workspace(A.adadsf_head_workspace_size(800, d, V, torch.bfloat16))
+    for n in (800, 768):
+        h, w, target, gl = head_inputs(n, d, V, "bf16")
+        got, want = ce(A, h, w, target, gl, ws=ws), ce(A, h, w, target, gl)
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+
+
 def test_calls_at_once(A):
     """Two streams, a workspace each, calls of different kernels of every operator in flight together."""
     def work(n, d, V, dtype):
