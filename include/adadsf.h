@@ -347,7 +347,7 @@ adadsf_status adadsf_distill_loss_backward(const void *h_dev, const void *w_head
  * grad_w_dev = sum grad_y xhat, grad_b_dev = sum grad_y over the rows: fp32
  * [d], either may be NULL; accumulate 1 adds to what they hold. Sums in one
  * order. d as for the losses above, up to 8192.
- * ws: adadsf_norm_backward_workspace_size bytes.
+ * ws: adadsf_norm_backward_workspace_size bytes, for fewer rows as well.
  * ---------------------------------------------------------------------- */
 adadsf_status adadsf_norm_forward(const void *x_dev, const void *w_dev, const void *b_dev, int64_t n_rows,
                                   int d, int dtype, float eps, int is_rms, void *y_dev, float *mean_dev,
@@ -369,7 +369,8 @@ adadsf_status adadsf_norm_backward(const void *grad_y_dev, const void *x_dev, co
  * of ids that came and leaves the others (a head that shares the table has its
  * gradient there). d as for the losses above; n up to 2^30, vocab up to 2^27.
  * ws: 256 bytes (the device error word) forward,
- * adadsf_embed_backward_workspace_size bytes backward.
+ * adadsf_embed_backward_workspace_size bytes backward, which serve fewer tokens
+ * as well.
  * ---------------------------------------------------------------------- */
 adadsf_status adadsf_embed_forward(const int32_t *ids_dev, int64_t n, const void *table_dev, int vocab, int d,
                                    int dtype, float scale, void *out_dev, void *ws, size_t ws_bytes,

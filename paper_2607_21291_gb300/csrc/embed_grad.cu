@@ -358,13 +358,14 @@ struct EgPlan {
   int64_t runs, per_tile;
   int run, tiles, bits, passes, digit;
 };
+constexpr int64_t kEgRuns = 32 * 2432, kEgLongRuns = 128 * 2432;   // a row's warps times rows from which runs are 32 and 128 places long
 EgPlan plan(int64_t n, int vocab, int d) {
   n = std::max<int64_t>(n, 1);
   EgPlan q;
   // Long runs leave fewer sums beside the table; short ones give every SM some 16 warps (8 bf16 features a thread, and
   // as many for fp32, whose plan is the same).
   const int64_t warps = n * ((d / 8 + 31) / 32);
-  q.run = warps / 128 >= 2432 ? 128 : warps / 32 >= 2432 ? 32 : 8;
+  q.run = warps >= kEgLongRuns ? 128 : warps >= kEgRuns ? 32 : 8;
   q.runs = (n + q.run - 1) / q.run;
   q.bits = 1;
   while (q.bits < 31 && ((int64_t)1 << q.bits) <= vocab) ++q.bits;   // keys 0 .. vocab
@@ -397,9 +398,15 @@ cudaError_t embed_scale(int dtype, const int32_t* ids, int64_t n, const void* ta
                     scale, static_cast<float*>(out), dev.err);
 }
 
+// What any number of tokens up to n needs: fewer tokens may mean more of the short runs, and more tiles.
 size_t embed_backward_scratch(int64_t n, int vocab, int d) {
   const EgPlan q = plan(n, vocab, d);
-  return 4 * up256((size_t)n * 4) + up256((size_t)q.tiles * sizeof(int32_t) << q.digit) + up256((size_t)q.runs * 2 * d * 4);
+  int64_t runs = q.runs;
+  const int64_t warps = (d / 8 + 31) / 32;   // of a row; a fp32 row of 4 features counts as none
+  for (int64_t from : {kEgRuns, kEgLongRuns})
+    if (warps > 0) runs = std::max(runs, plan(std::min(n, (from - 1) / warps), vocab, d).runs);   // the last ones with shorter runs
+  const int64_t tiles = std::min<int64_t>(kEgMaxTiles, (std::max<int64_t>(n, 1) + kEgChunk - 1) / kEgChunk);
+  return 4 * up256((size_t)n * 4) + up256((size_t)tiles * sizeof(int32_t) << q.digit) + up256((size_t)runs * 2 * d * 4);
 }
 
 cudaError_t embed_backward(int dtype, const int32_t* ids, const void* dy, int64_t n, int vocab, int d, float scale, void* out,

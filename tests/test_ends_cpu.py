@@ -178,3 +178,17 @@ def test_head_workspace_serves_fewer_rows(A, d, V, dtype):
         assert now >= last, (n, now, last)
         last = now
     assert size(1000, d, V, dt, 64) <= size(2000, d, V, dt, 64)
+
+
+@pytest.mark.parametrize("V,d", [(152064, 3584), (50304, 768), (300, 64), (40000, 4), (2 ** 27, 8), (1000, 8200)])
+def test_embed_workspace_serves_fewer_tokens(A, V, d):
+    """A workspace for the longest batch is large enough for every shorter one."""
+    size = A.adadsf_embed_backward_workspace_size
+    last = 0
+    steps = sorted({0, 1, *range(7, 9000, 13), *range(9000, 200000, 511), *(k * 2 ** 20 + o for k in (1, 2, 3, 8, 64) for o in (-1, 0, 1, 2048)),
+                    *(per + o for per in (9, 19, 32, 38, 2432, 4864, 77824, 77824 // 3, 311296, 311296 // 14, 77824 // 14, 9962, 311296 // 33)
+                      for o in (-1, 0, 1, 2))})
+    for n in steps:
+        now = size(n, V, d)
+        assert now >= last, (n, now, last)
+        last = now

@@ -880,6 +880,17 @@ def test_embed(A, n, V, d, dtype):
     embed_check(A, ids, table, dy, -2.5, base=randn(g, V, d).to(DT[dtype]))
 
 
+def test_embed_workspace_of_more_tokens(A):
+    """One workspace for the longest batch: a shorter one in it, of more and shorter runs."""
+    V, d = 3000, 3584
+    ws = A.workspace(A.adadsf_embed_backward_workspace_size(6000, V, d))
+    g = gen(12)
+    table, dy = randn(g, V, d).to(torch.bfloat16), randn(g, 6000, d).to(torch.bfloat16)
+    ids = torch.randint(0, V, (6000,), generator=g, device="cuda", dtype=torch.int32)
+    for n in (6000, 5558, 4096):
+        embed_check(A, ids[:n], table, dy[:n], 1.0, ws=ws)
+
+
 @pytest.mark.parametrize("n", [200, 6000])
 def test_embed_of_more_than_2_31_numbers(A, n):
     """Rows of a table past 2^31 elements: the last one, the ones at the border, the others left or cleared."""
