@@ -306,7 +306,8 @@ adadsf_status adadsf_router_backward(const adadsf_model_cfg *cfg, const adadsf_l
  * that have one.
  * Backward: lse_dev as the forward call left it, grad_loss_dev fp32 [n_rows]
  * the gradient of each row's loss (NULL: 1). grad_h_dev [n_rows, d] and
- * grad_w_dev [n_classes, d] in `dtype` (either may be NULL: not computed);
+ * grad_w_dev [n_classes, d] in `dtype` (either may be NULL: not computed; both
+ * where there are no rows);
  * accumulate_w 1 adds to what grad_w_dev holds, before the one rounding.
  * Gradients may not overlap the inputs.
  * Logits, exponentials and sums are fp32; the bf16 path rounds the logits'

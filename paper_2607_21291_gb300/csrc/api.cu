@@ -1874,7 +1874,8 @@ adadsf_status run_head_loss(const HeadCall& c, float* loss, float* lse, double* 
 adadsf_status run_head_grad(const HeadCall& c, const float* lse, const float* grad_loss, void* grad_h, void* grad_w, int accumulate_w,
                         void* ws, size_t ws_bytes, void* stream) {
   if (accumulate_w != 0 && accumulate_w != 1) return fail(ADADSF_ERR_INVALID_ARG, "accumulate_w must be 0 or 1");
-  if (!grad_h && !grad_w) return fail(ADADSF_ERR_INVALID_ARG, "grad_h_dev and grad_w_dev are both NULL");
+  if (!grad_h && !grad_w && c.n > 0)   // no rows: their gradient may be an empty tensor's NULL
+    return fail(ADADSF_ERR_INVALID_ARG, "grad_h_dev and grad_w_dev are both NULL");
   if (grad_h) NEED_PTR(grad_h, "grad_h_dev");
   if (grad_w) NEED_PTR(grad_w, "grad_w_dev");
   for (const void* g : {grad_h, grad_w})

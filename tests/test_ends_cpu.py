@@ -192,3 +192,11 @@ def test_embed_workspace_serves_fewer_tokens(A, V, d):
         now = size(n, V, d)
         assert now >= last, (n, now, last)
         last = now
+
+
+def test_head_gradients_of_no_rows(A):
+    """An empty batch with a frozen head: the hidden gradient is an empty tensor, whose address is NULL."""
+    for call in (head, distill):
+        assert call(A, True, n=0, dh=None, dw=None) == A.OK
+        assert call(A, True, n=0, dh=None, dw=None, h=None, lse=None) == A.OK
+        assert call(A, True, n=1, dh=None, dw=None) == A.ERR_INVALID_ARG

@@ -266,6 +266,22 @@ def test_no_row_has_a_target(A, dtype):
     assert (none[4] == 0).all() and (none[2] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_rows(A, dtype):
+    """An empty batch, each gradient by itself: the head's is cleared, or left where it is added to."""
+    h, w, target, gl = head_inputs(3, 64, 400, dtype)
+    v, idx, logit = gl[:0], target[:0, None].contiguous(), gl[:0, None].contiguous()
+    calls = [lambda **kw: A.adadsf_head_loss_backward(h[:0], w, target[:0], v, grad_loss=v, **kw),
+             lambda **kw: A.adadsf_distill_loss_backward(h[:0], w, idx, logit, v, 2.0, grad_loss=v, **kw)]
+    for call in calls:
+        call(grad_h=torch.empty_like(h[:0]))
+        dw = torch.full_like(w, 7.0)
+        call(grad_w=dw, accumulate_w=True)
+        assert (dw == 7).all()
+        call(grad_w=dw)
+        assert (dw == 0).all()
+
+
 def test_classes_out_of_range(A):
     h, w, target, gl = head_inputs(50, 64, 400, "bf16")
     ws = A.workspace(A.adadsf_head_workspace_size(50, 64, 400, h.dtype, 4))
