@@ -309,7 +309,8 @@ adadsf_status adadsf_router_backward(const adadsf_model_cfg *cfg, const adadsf_l
  * grad_w_dev [n_classes, d] in `dtype` (either may be NULL: not computed; both
  * where there are no rows);
  * accumulate_w 1 adds to what grad_w_dev holds, before the one rounding.
- * Gradients may not overlap the inputs.
+ * What a call writes may overlap neither its inputs, nor its workspace, nor one
+ * another (ADADSF_ERR_INVALID_ARG).
  * Logits, exponentials and sums are fp32; the bf16 path rounds the logits'
  * gradients to bf16 for the tensor cores. Every sum has one order: results
  * repeat bit for bit.
@@ -340,11 +341,11 @@ adadsf_status adadsf_distill_loss_backward(const void *h_dev, const void *w_head
  * pass needs: y = (x - mean) rstd w + b, rstd = 1 / sqrt(var + eps); RMSNorm:
  * y = x rstd w, rstd = 1 / sqrt(mean x^2 + eps) (b_dev and mean_dev NULL).
  * x_dev, y_dev [n_rows, d], w_dev, b_dev [d] in `dtype`; mean_dev, rstd_dev
- * fp32 [n_rows]. y_dev may be x_dev.
+ * fp32 [n_rows]. y_dev may be x_dev; else outputs overlap nothing, as above.
  * Backward, with xhat = (x - mean) rstd and a = grad_y w:
  *   grad_x = rstd (a - mean(a) - xhat mean(a xhat)) + add
  * (RMSNorm: without mean(a)); add_dev (NULL or [n_rows, d]): the gradient that
- * goes around the norm. grad_x_dev may be grad_y_dev or add_dev.
+ * goes around the norm. grad_x_dev may be grad_y_dev, add_dev or x_dev.
  * grad_w_dev = sum grad_y xhat, grad_b_dev = sum grad_y over the rows: fp32
  * [d], either may be NULL; accumulate 1 adds to what they hold. Sums in one
  * order. d as for the losses above, up to 8192.
@@ -369,6 +370,7 @@ adadsf_status adadsf_norm_backward(const void *grad_y_dev, const void *x_dev, co
  * `dtype`. accumulate 0 writes every row of grad_table_dev, 1 adds to the rows
  * of ids that came and leaves the others (a head that shares the table has its
  * gradient there). d as for the losses above; n up to 2^30, vocab up to 2^27.
+ * Outputs overlap nothing, as above.
  * ws: 256 bytes (the device error word) forward,
  * adadsf_embed_backward_workspace_size bytes backward, which serve fewer tokens
  * as well.

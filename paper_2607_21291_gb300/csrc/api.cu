@@ -6,6 +6,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -1754,6 +1755,33 @@ adadsf_status need_row(const void* p, const char* name, bool optional) {
   return ADADSF_OK;
 }
 
+// The memory of a tensor of a call (none where p is NULL).
+struct Span {
+  const void* p;
+  size_t bytes;
+  const char* name;
+  bool meets(const Span& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    return p && o.p && bytes && o.bytes && a < b + o.bytes && b < a + bytes;
+  }
+  bool is(const Span& o) const { return p == o.p && bytes == o.bytes; }
+};
+
+using Spans = std::initializer_list<Span>;
+
+// What a call writes may not meet what it reads or writes besides. The first output may be one of the first n_same inputs,
+// each of whose numbers is read by the thread that writes in its place.
+adadsf_status check_apart(const Spans& out, const Spans& in, int n_same = 0) {
+  for (const Span* o = out.begin(); o != out.end(); ++o) {
+    for (const Span* i = in.begin(); i != in.end(); ++i)
+      if (o->meets(*i) && !(o == out.begin() && i - in.begin() < n_same && o->is(*i)))
+        return fail(ADADSF_ERR_INVALID_ARG, "%s overlaps %s", o->name, i->name);
+    for (const Span* other = out.begin(); other != o; ++other)
+      if (o->meets(*other)) return fail(ADADSF_ERR_INVALID_ARG, "%s overlaps %s", o->name, other->name);
+  }
+  return ADADSF_OK;
+}
+
 constexpr int64_t kHeadMaxRows = (int64_t)1 << 22;
 constexpr int kHeadMaxClasses = 1 << 24;
 
@@ -1810,11 +1838,23 @@ struct HeadCall {
   int d, V, dtype;
 };
 
-adadsf_status head_prepare(const HeadCall& c, void* ws, size_t ws_bytes, void* stream, HeadLayout* l, Head* a, Dev* dev) {
+// out: what the call writes besides the workspace; read: what it reads by row.
+adadsf_status head_prepare(const HeadCall& c, const Spans& out, const Span& read, const Span& read_too, void* ws, size_t ws_bytes,
+                           void* stream, HeadLayout* l, Head* a, Dev* dev) {
   *l = head_layout(c.n, c.d, c.V, c.dtype, c.k);
   TRY(check_ws(ws, ws_bytes, l->total));
   NEED_PTR(c.h, "h_dev");
   NEED_PTR(c.w, "w_head_dev");
+  const size_t rows = (size_t)c.n, row = (size_t)c.d * elem_size(c.dtype);
+  const Spans in = {{c.h, rows * row, "h_dev"},
+                     {c.w, (size_t)c.V * row, "w_head_dev"},
+                     {c.target, rows * 4, "target_dev"},
+                     {c.idx, rows * c.k * 4, "top_idx_dev"},
+                     {c.logit, rows * c.k * 4, "top_logit_dev"},
+                     read,
+                     read_too,
+                     {ws, l->total, "the workspace"}};
+  TRY(check_apart(out, in));
   TRY(device_info(dev, stream, ws));
   *a = Head();
   a->h = c.h;
@@ -1863,7 +1903,8 @@ adadsf_status run_head_loss(const HeadCall& c, float* loss, float* lse, double* 
   HeadLayout l;
   Head a;
   Dev dev;
-  TRY(head_prepare(c, ws, ws_bytes, stream, &l, &a, &dev));
+  const Spans out = {{loss, (size_t)c.n * 4, "loss_dev"}, {lse, (size_t)c.n * 4, "lse_dev"}, {acc, 16, "acc_dev"}};
+  TRY(head_prepare(c, out, Span(), Span(), ws, ws_bytes, stream, &l, &a, &dev));
   a.loss = loss;
   a.lse = lse;
   a.acc = acc;
@@ -1878,8 +1919,6 @@ adadsf_status run_head_grad(const HeadCall& c, const float* lse, const float* gr
     return fail(ADADSF_ERR_INVALID_ARG, "grad_h_dev and grad_w_dev are both NULL");
   if (grad_h) NEED_PTR(grad_h, "grad_h_dev");
   if (grad_w) NEED_PTR(grad_w, "grad_w_dev");
-  for (const void* g : {grad_h, grad_w})
-    if (g && (g == c.w || g == c.h)) return fail(ADADSF_ERR_INVALID_ARG, "a gradient's buffer is h_dev or w_head_dev");
   TRY(need_row(lse, "lse_dev", c.n == 0));
   TRY(need_row(grad_loss, "grad_loss_dev", true));
   if (c.n == 0) {
@@ -1890,7 +1929,9 @@ adadsf_status run_head_grad(const HeadCall& c, const float* lse, const float* gr
   HeadLayout l;
   Head a;
   Dev dev;
-  TRY(head_prepare(c, ws, ws_bytes, stream, &l, &a, &dev));
+  const size_t row = (size_t)c.d * elem_size(c.dtype), rows = (size_t)c.n * 4;
+  const Spans out = {{grad_h, (size_t)c.n * row, "grad_h_dev"}, {grad_w, (size_t)c.V * row, "grad_w_dev"}};
+  TRY(head_prepare(c, out, {lse, rows, "lse_dev"}, {grad_loss, rows, "grad_loss_dev"}, ws, ws_bytes, stream, &l, &a, &dev));
   a.lse = const_cast<float*>(lse);   // read
   a.g = grad_loss;
   a.dh = grad_h;
@@ -2003,6 +2044,10 @@ adadsf_status adadsf_norm_forward(const void* x_dev, const void* w_dev, const vo
   }
   NEED_PTR(y_dev, "y_dev");
   TRY(need_row(rstd_dev, "rstd_dev", false));
+  const size_t row = (size_t)d * elem_size(dtype), rows = (size_t)n_rows;
+  const Spans out = {{y_dev, rows * row, "y_dev"}, {mean_dev, rows * 4, "mean_dev"}, {rstd_dev, rows * 4, "rstd_dev"}};
+  const Spans in = {{x_dev, rows * row, "x_dev"}, {w_dev, row, "w_dev"}, {b_dev, row, "b_dev"}};
+  TRY(check_apart(out, in, 1));
   Dev dev;
   TRY(device_info(&dev, stream, nullptr));
   return launch(dev, ADADSF_KERNEL_NORM, false, 0, 2.0 * n_rows * d * elem_size(dtype),
@@ -2036,6 +2081,12 @@ adadsf_status adadsf_norm_backward(const void* grad_y_dev, const void* x_dev, co
   TRY(need_row(rstd_dev, "rstd_dev", false));
   if (add_dev) NEED_PTR(add_dev, "add_dev");
   NEED_PTR(grad_x_dev, "grad_x_dev");
+  const size_t row = (size_t)d * elem_size(dtype), rows = (size_t)n_rows;
+  const Spans out = {{grad_x_dev, rows * row, "grad_x_dev"}, {grad_w_dev, (size_t)d * 4, "grad_w_dev"}, {grad_b_dev, (size_t)d * 4, "grad_b_dev"}};
+  const Spans in = {{grad_y_dev, rows * row, "grad_y_dev"}, {add_dev, rows * row, "add_dev"},   {x_dev, rows * row, "x_dev"},
+                     {w_dev, row, "w_dev"},                  {mean_dev, rows * 4, "mean_dev"},   {rstd_dev, rows * 4, "rstd_dev"},
+                     {ws, adadsf_norm_backward_workspace_size(n_rows, d), "the workspace"}};
+  TRY(check_apart(out, in, 3));
   Dev dev;
   TRY(device_info(&dev, stream, ws));
   return launch(dev, ADADSF_KERNEL_NORM_GRAD, false, 0, (3.0 + (add_dev != nullptr)) * n_rows * d * elem_size(dtype),
@@ -2052,6 +2103,10 @@ adadsf_status adadsf_embed_forward(const int32_t* ids_dev, int64_t n, const void
   TRY(need_row(ids_dev, "ids_dev", false));
   NEED_PTR(table_dev, "table_dev");
   NEED_PTR(out_dev, "out_dev");
+  const size_t row = (size_t)d * elem_size(dtype);
+  const Spans out = {{out_dev, (size_t)n * row, "out_dev"}};
+  const Spans in = {{ids_dev, (size_t)n * 4, "ids_dev"}, {table_dev, (size_t)vocab * row, "table_dev"}, {ws, kErrBytes, "the workspace"}};
+  TRY(check_apart(out, in));
   Dev dev;
   TRY(device_info(&dev, stream, ws));
   return launch(dev, ADADSF_KERNEL_EMBED, false, 0, 2.0 * n * d * elem_size(dtype),
@@ -2077,7 +2132,12 @@ adadsf_status adadsf_embed_backward(const int32_t* ids_dev, const void* grad_out
   }
   TRY(need_row(ids_dev, "ids_dev", false));
   NEED_PTR(grad_out_dev, "grad_out_dev");
-  if (grad_table_dev == grad_out_dev) return fail(ADADSF_ERR_INVALID_ARG, "grad_table_dev is grad_out_dev");
+  const size_t row = (size_t)d * elem_size(dtype);
+  const Spans out = {{grad_table_dev, (size_t)vocab * row, "grad_table_dev"}};
+  const Spans in = {{ids_dev, (size_t)n * 4, "ids_dev"},
+                     {grad_out_dev, (size_t)n * row, "grad_out_dev"},
+                     {ws, adadsf_embed_backward_workspace_size(n, vocab, d), "the workspace"}};
+  TRY(check_apart(out, in));
   Dev dev;
   TRY(device_info(&dev, stream, ws));
   return launch(dev, ADADSF_KERNEL_EMBED_GRAD, false, 0, ((double)n * d + (accumulate ? 0.0 : (double)vocab * d)) * elem_size(dtype),

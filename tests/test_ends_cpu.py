@@ -200,3 +200,54 @@ def test_head_gradients_of_no_rows(A):
         assert call(A, True, n=0, dh=None, dw=None) == A.OK
         assert call(A, True, n=0, dh=None, dw=None, h=None, lse=None) == A.OK
         assert call(A, True, n=1, dh=None, dw=None) == A.ERR_INVALID_ARG
+
+
+def apart(sizes):
+    """Addresses of tensors that lie one behind the other, 4096 bytes or more between them."""
+    at, out = 1 << 20, {}
+    for name, size in sizes.items():
+        out[name] = at
+        at += (size // 4096 + 2) * 4096
+    return out
+
+
+def meetings(sizes, outs, allowed=()):
+    """One output moved onto another tensor's first byte, its last 16, and so that its own last 16 meet it."""
+    base = apart(sizes)
+    for o in outs:
+        for other in sizes:
+            if other == o:
+                continue
+            for at in (base[other], base[other] + (sizes[other] - 16) // 16 * 16, base[other] - (sizes[o] - 16) // 16 * 16):
+                if at == base[other] and (o, other) in allowed:
+                    continue
+                yield {**base, o: at}, o, other
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_overlaps_are_refused(A, dtype):
+    n, d, V, k = 10, 64, 100, 4
+    row = d * (2 if dtype == BF else 4)
+    refused = lambda status, o, other: (status == A.ERR_INVALID_ARG and "overlaps" in A.adadsf_last_error(), o, other, A.adadsf_last_error())
+    ws = A.adadsf_head_workspace_size(n, d, V, torch.bfloat16 if dtype == BF else torch.float32, k)
+    kinds = [(head, dict(h=n * row, w=V * row, target=n * 4)), (distill, dict(h=n * row, w=V * row, idx=n * k * 4, logit=n * k * 4))]
+    for call, reads in kinds:
+        for backward, more, outs in ((False, dict(loss=n * 4, lse=n * 4, acc=16), ("loss", "lse", "acc")),
+                                     (True, dict(lse=n * 4, g=n * 4, dh=n * row, dw=V * row), ("dh", "dw"))):
+            for kw, o, other in meetings({**reads, **more, "ws": 4096}, outs):
+                got = refused(call(A, backward, dtype=dtype, ws_bytes=ws, **kw), o, other)
+                assert got[0], got
+    rows = dict(x=n * row, w=row, mean=n * 4, rstd=n * 4)
+    for kw, o, other in meetings({**rows, "b": row, "y": n * row}, ("y", "mean", "rstd"), allowed=[("y", "x")]):
+        got = refused(norm_fw(A, dtype=dtype, **kw), o, other)
+        assert got[0], got
+    sizes = {**rows, "dy": n * row, "add": n * row, "dx": n * row, "dw": d * 4, "db": d * 4, "ws": 4096}
+    for kw, o, other in meetings(sizes, ("dx", "dw", "db"), allowed=[("dx", "dy"), ("dx", "add"), ("dx", "x")]):
+        got = refused(norm_bw(A, dtype=dtype, **kw), o, other)
+        assert got[0], got
+    for kw, o, other in meetings(dict(ids=n * 4, table=V * row, out=n * row, ws=256), ("out",)):
+        got = refused(embed_fw(A, dtype=dtype, **kw), o, other)
+        assert got[0], got
+    for kw, o, other in meetings(dict(ids=n * 4, dy=n * row, table=V * row, ws=4096), ("table",)):
+        got = refused(embed_bw(A, dtype=dtype, **kw), o, other)
+        assert got[0], got

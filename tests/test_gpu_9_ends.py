@@ -648,6 +648,36 @@ def test_head_workspace_of_more_rows(A):
             assert torch.equal(x, y)
 
 
+def test_tensors_side_by_side(A):
+    """All of a call's tensors and its workspace in one buffer, one ending where the next begins; the norm's gradient in
+    place of its input."""
+    n, d, V = 32, 64, 96
+    h, w, target, gl = head_inputs(n, d, V, "bf16")
+    want = ce(A, h, w, target, gl)
+    size = (A.adadsf_head_workspace_size(n, d, V, torch.bfloat16) + 255) // 256 * 256
+    buf, at = torch.zeros(size + (1 << 16), dtype=torch.uint8, device="cuda"), [0]
+
+    def place(t):
+        out = buf[at[0]:at[0] + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+        at[0] += t.numel() * t.element_size()
+        return out.copy_(t)
+
+    h2, dh, w2, dw, t2, loss, g2, lse = (place(t) for t in (h, h, w, w, target, gl, gl, gl))
+    assert at[0] % 256 == 0
+    ws = buf[at[0]:at[0] + size]
+    at[0] += size
+    acc = place(torch.zeros(2, dtype=torch.float64, device="cuda"))
+    A.adadsf_head_loss(h2, w2, t2, loss, lse, acc=acc, ws=ws)
+    A.adadsf_head_loss_backward(h2, w2, t2, lse, grad_loss=g2, grad_h=dh, grad_w=dw, ws=ws)
+    for x, y in zip((loss, lse, acc, dh, dw), want):
+        assert torch.equal(x, y)
+    for dtype, rms in (("bf16", False), ("f32", True)):
+        x, wn, b, dy, add = norm_inputs(500, 768, dtype, rms, True)
+        _, mean, rstd, dx, _, _ = norm(A, x, wn, b, dy, add)
+        A.adadsf_norm_backward(dy, x, wn, rstd, x, mean=mean, add=add)
+        assert torch.equal(x, dx)
+
+
 def test_calls_at_once(A):
     """Two streams, a workspace each, calls of different kernels of every operator in flight together."""
     def work(n, d, V, dtype):
