@@ -281,12 +281,17 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
     asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
     if (MEAN) __syncwarp();   // lane 0's copies of the statistics
     constexpr int S = MEAN ? 2 : 1;
-    float shift[ROWS], rstd[ROWS], s[S * ROWS];   // xhat = x rstd + shift
+    // fp32: xhat = (x - mean) rstd, the difference first as in the forward pass, since x rstd - mean rstd is off by roundings
+    // of the mean's size (rows of a mean of 1000 and a spread of 2: the weights' gradient of one row 3e-5, now 1e-7). bf16: x rstd +
+    // shift, an instruction less a pair (327 us in place of 347 at 65536 x 3584): of rows in 8 bits the mean is some 2^8
+    // spreads at most as a rule, and the gradients of rows are rounded by 2^-8.
+    constexpr bool APART = MEAN && V == 4;
+    float shift[ROWS], rstd[ROWS], s[S * ROWS];
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) {
       const uint32_t st = stats + 8u * ((slot + k) % DEPTH);
       rstd[k] = ring_float(st + 4);
-      shift[k] = MEAN ? -ring_float(st) * rstd[k] : 0.f;
+      shift[k] = !MEAN ? 0.f : APART ? -ring_float(st) : -ring_float(st) * rstd[k];
       float2 sa = both(0.f), sx = both(0.f);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -297,7 +302,8 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
         pairs(wv[i], w);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-          const float2 xh = MEAN ? __ffma2_rn(x[j], both(rstd[k]), both(shift[k])) : __fmul2_rn(x[j], both(rstd[k]));
+          const float2 xh = APART ? __fmul2_rn(__fadd2_rn(x[j], both(shift[k])), both(rstd[k]))
+                            : MEAN ? __ffma2_rn(x[j], both(rstd[k]), both(shift[k])) : __fmul2_rn(x[j], both(rstd[k]));
           const float2 a = __fmul2_rn(y[j], w[j]);
           if (MEAN) sa = __fadd2_rn(sa, a);
           sx = __ffma2_rn(a, xh, sx);
@@ -313,9 +319,10 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
     for (int k = 0; k < ROWS; ++k) {
       const int64_t r = row + k * step;
       if (r < p.n) {
-        // dx = rstd a + (x by + c1): by = -rstd^2 mean(a xhat), c1 = -rstd (shift mean(a xhat) + mean(a))
+        // dx = rstd a + (x by + c1): by = -rstd^2 mean(a xhat), c1 = -rstd (shift mean(a xhat) + mean(a)); apart, x - mean for x
+        // and no shift
         const float c2 = -(s[S * k] * inv_d) * rstd[k], by = c2 * rstd[k];
-        const float c1 = MEAN ? fmaf(c2, shift[k], -(s[S * k + S - 1] * inv_d) * rstd[k]) : 0.f;
+        const float c1 = MEAN ? fmaf(c2, APART ? 0.f : shift[k], -(s[S * k + S - 1] * inv_d) * rstd[k]) : 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const int c = t + i * p.group;
@@ -326,7 +333,8 @@ __global__ void __launch_bounds__(ng_threads(NV), NV == 1 ? 2 : 1) norm_backward
           if (ADD) pairs(ring.read((slot + k) % DEPTH, N - 1, i), o);
 #pragma unroll
           for (int j = 0; j < P; ++j) {
-            const float2 rest = MEAN ? __ffma2_rn(x[j], both(by), both(c1)) : __fmul2_rn(x[j], both(by));
+            const float2 xm = APART ? __fadd2_rn(x[j], both(shift[k])) : x[j];
+            const float2 rest = MEAN ? __ffma2_rn(xm, both(by), both(c1)) : __fmul2_rn(xm, both(by));
             const float2 dx = __ffma2_rn(__fmul2_rn(y[j], w[j]), both(rstd[k]), rest);
             o[j] = ADD ? __fadd2_rn(dx, o[j]) : dx;
           }

@@ -854,6 +854,46 @@ def test_norm_row_of_one_value(A):
     assert torch.equal(got[0][7], b) and torch.equal(got[0][8], b)
 
 
+@pytest.mark.parametrize("n,d,dtype", [(1, 512, "f32"), (1, 2048, "f32"), (1, 4096, "f32"), (40, 512, "f32"),
+                                       (700, 512, "f32"), (1, 1024, "bf16"), (1, 8192, "bf16"), (700, 2048, "bf16")])
+def test_norm_of_rows_far_from_zero(A, n, d, dtype):
+    """Rows whose mean is hundreds of times their spread (bf16: its last places): whole numbers, so that sums, mean and the
+    differences to it are exact and xhat is off by roundings of its own size only, in fp32 in either pass. The bf16
+    gradient's is x rstd - mean rstd: roundings of the mean's size, 2 of them, far below those of bf16."""
+    g = gen(n + d)
+    mean = 1000.0 if dtype == "f32" else 192.0
+    half = torch.randint(1, 4, (n, d // 2), generator=g, device="cuda").float()
+    if dtype == "bf16":
+        half = half.clamp(max=2)
+    off = torch.stack([half, -half], -1).reshape(n, d)[:, torch.randperm(d, generator=g, device="cuda")]
+    x = (mean + off).to(DT[dtype])
+    assert torch.equal(x.float(), mean + off)
+    _, w, b, dy, _ = norm_inputs(n, d, dtype, False, False)
+    y, got_mean, rstd, dx, dw, db = norm(A, x, w, b, dy, None)
+    assert (got_mean == mean).all()
+    out = B16 if dtype == "bf16" else U
+    xd, wd, dyd = off.double(), w.double(), dy.double()
+    r = (xd.square().mean(-1, keepdim=True) + 1e-5) ** -0.5
+    xh = xd * r
+    # the squares' sum is exact; its scale, eps, root and quotient: 4 roundings (2 ulp each at most)
+    within(rstd, r[:, 0], 8 * U * r[:, 0], "rstd")
+    e_xh = 12 * U * xh.abs()
+    ref = xh * wd + b.double()
+    within(y, ref, out * ref.abs() + (1 + out) * (wd.abs() * e_xh + 3 * U * (ref.abs() + (xh * wd).abs())), "y")
+    far = 2 * U * mean * r if dtype == "bf16" else torch.zeros_like(r)
+    a = dyd * wd
+    s = 64 * 2 * U   # as in norm_check
+    m1, m2 = a.mean(-1, keepdim=True), (a * xh).mean(-1, keepdim=True)
+    ref = r * (a - m1 - xh * m2)
+    e = r * (s * a.abs().mean(-1, keepdim=True) + xh.abs() * (s + 12 * U) * (a * xh).abs().mean(-1, keepdim=True)
+             + 6 * U * (a.abs() + m1.abs() + (xh * m2).abs())) + 12 * U * r * (a.abs() + m1.abs() + (xh * m2).abs()) \
+        + r * far * (xh.abs() * a.abs().mean(-1, keepdim=True) + 2 * m2.abs())
+    within(dx, ref, (1 + out) * e + out * ref.abs(), "dx")
+    size = (dyd * xh).abs().sum(0)
+    # a sum of n numbers beside zeros
+    within(dw, (dyd * xh).sum(0), 2 * U * n * size + 14 * U * size + (1 + 2 * U * n) * (dyd.abs() * far).sum(0), "dw")
+
+
 @pytest.mark.parametrize("rms", [False, True])
 def test_norm_of_more_than_2_31_numbers(A, rms):
     n, d = 1_060_000, 2048
