@@ -14,6 +14,7 @@
 
 namespace adadsf {
 
+constexpr int kHeadChunk = 8, kHeadChunkF32 = 4;   // blocks of 64 k of a logit that share an accumulator, in every kernel (see head_tc.cu)
 constexpr int kHeadZeroPad = 64;   // rows past the last packed one, up to a multiple of this, are zero in the packed copy
 
 // fp32 numbers as sums of three bf16 numbers, their leading 8 bits, the next 8 and the last: the next part of a (low

@@ -45,7 +45,7 @@ struct HfCfg {
   static constexpr int GROUPS = F32 ? 3 : 2;     // of four epilogue warps
   static constexpr int TURNS = F32 ? 1 : 2;      // times 32 rows that a group takes
   static constexpr int EPI = 4 * GROUPS;
-  static constexpr int CHUNK = F32 ? 4 : 8;     // blocks of 64 k that share an accumulator (see head_tc.cu)
+  static constexpr int CHUNK = F32 ? kHeadChunkF32 : kHeadChunk;
   static constexpr int THREADS = 64 + 32 * (EPI + (F32 ? kHfConvWarps : 0));
   static constexpr int RING = F32 ? 2 * 3 * (kHfPart + kHeadFewRowsF32 * 128) : 196608;
   static constexpr int SMEM = 1024 + RING + GROUPS * kHfOut + kHfBars * 8 + 16;

@@ -172,9 +172,9 @@ __device__ __forceinline__ void red_add4(float* p, const float4& v) {
 // classes) are cut, below which the loss does not show: one of 4 million rows was 3.6e-3 short (head gradients 4.4e-3 off, of
 // which roundings are 1.8e-3). Without the chunks of G's logits gradients of 27 rows at a 151936 x 1536 head took 338 us (346 with them), of
 // 3330 at the Pythia-1.4B head 1361 (1412), of 3450 at the Qwen2.5-7B head 6950 (7090).
-constexpr int kHtLogits = 8, kHtLong = 1024;
+constexpr int kHtLong = 1024;
 template <bool F32>
-__device__ __forceinline__ int chunk_blocks(int kind) { return F32 ? 4 : kind == kStats || kind == kG ? kHtLogits : kHtLong; }
+__device__ __forceinline__ int chunk_blocks(int kind) { return F32 ? kHeadChunkF32 : kind == kStats || kind == kG ? kHeadChunk : kHtLong; }
 
 // A warp's loads from TMEM are done (tcgen05.wait::ld): only that is told, so the arrival is relaxed. Released, it waits
 // until the warp's stores to global memory are performed (gradients of 500 tokens at the Qwen2.5-7B head 1104 -> 1079 us).

@@ -597,6 +597,52 @@ def test_wide_logits_gradients(A, n, d, dtype):
     ref.check(loss, lse, dh, dw)
 
 
+def cut_of(steps):
+    """How far a long sum of like numbers falls short on average where chunks of `steps` steps of the tensor cores are added
+    up in fp32: at step i a chunk holds i / steps of its sum, of which an addition cuts off less than 2^-23, half of that on
+    average: 2^-24 (steps + 1) / 2 in all. The sums of the chunks are rounded to nearest, which has no mean; one rounding's
+    room for them and the result. (Chunks of twice the length lose 0.7 of their own bound, as sums lie anywhere between two
+    powers of two: more than this.)"""
+    return U * ((steps + 1) / 2 + 1)
+
+
+@pytest.mark.parametrize("n,d,dtype,steps", [(100, 5120, "bf16", 32), (400, 5120, "bf16", 32), (64, 8192, "f32", 16), (200, 8192, "f32", 16)])
+def test_chunks_of_the_logits(A, n, d, dtype, steps):
+    """Logits of products of one sign, which the logarithm of one class is: short by what chunks of this length lose."""
+    g = gen(n + d)
+    h, w = randn(g, n, d).abs().to(DT[dtype]), (randn(g, 1, d).abs() / d).to(DT[dtype])
+    _, lse, _, _, _ = ce(A, h, w, torch.zeros(n, dtype=torch.int32, device="cuda"), grads=False)
+    ref = (h.double() @ w.double().T)[:, 0]
+    short = float(((ref - lse.double()) / ref).mean())
+    more = U if dtype == "f32" else 0.0   # the three products of parts that are left out: 2^-24 of a product at most on average
+    assert -U <= short <= cut_of(steps) + more, short / U
+
+
+@pytest.mark.parametrize("what", ["rows", "classes"])
+def test_chunks_of_the_gradients(A, what):
+    """fp32 gradients as sums of one sign over many rows, and over many classes: every logit is 0, so that G is the same
+    number everywhere but at the target, which meets zeros; a column with a single 1 has that number itself."""
+    d = 64
+    g = gen(3)
+    if what == "rows":
+        n, V = 8192, 2
+        h, w = randn(g, n, d).abs(), torch.zeros(V, d, device="cuda")
+        x = h
+    else:
+        n, V = 100, 8192
+        h, w = torch.zeros(n, d, device="cuda"), randn(g, V, d).abs()
+        w[0] = 0.0
+        x = w
+    x[:, 0] = 0.0
+    x[5, 0] = 1.0
+    _, _, _, dh, dw = ce(A, h, w, torch.zeros(n, dtype=torch.int32, device="cuda"))
+    got = (dw[1:2] if what == "rows" else dh).double()
+    ref = x.double().sum(0) * got[:, :1]
+    assert (got[:, :1] > 0).all()
+    short = float(((ref - got) / ref)[:, 1:].mean())
+    assert -U <= short <= cut_of(16) + 2 * U, short / U   # the products left out, and the single one's rounding
+
+
 @pytest.mark.parametrize("n,V", [(1, 31), (32, 33), (33, 64), (64, 65), (65, 4900), (80, 5000), (50, 180000)])
 def test_head_gradients_of_few_rows(A, n, V):
     """fp32 rows on both sides of the zeros that products over rows need, classes on both sides of their blocks and more than a
