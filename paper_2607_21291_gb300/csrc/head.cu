@@ -352,7 +352,7 @@ cudaError_t pack(const Head& a, bool backward, bool split, const Dev& dev) {
 
 }  // namespace
 
-// Classes a piece: 256 MB of G. With 96 MB the launches' first and last waves cost more than its second reading from the
+// Classes a piece: 256 MB of G, 2048 at least (past 65536 bf16 rows more than that). With 96 MB the launches' first and last waves cost more than its second reading from the
 // L2 saves (3 x 259 fp32 tokens 725 -> 650 us, 8 x 511 of the Pythia-1.4B head 1750 -> 1590); 600 and 1500 MB are no faster.
 HeadPlan head_plan(int dtype, int64_t n, int d, int V) {
   const int64_t parts = dtype == kBF16 ? 1 : 3, tile = 256;

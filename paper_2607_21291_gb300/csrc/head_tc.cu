@@ -28,8 +28,8 @@
 // chunk is multiplied. Chunks of 32, 16 and 8 steps: 700 fp32 rows of 512 features, 50304 classes, head gradient 1.2e-6, 7e-7 and
 // 5e-7 off; loss and gradients of 645 such rows 671, 674 and 694 us. bf16, 64, 32 and 16 steps: losses of 400 rows of 5120 features 6e-7,
 // 3e-7 and 2e-7 off; of 3331 rows of the Pythia-1.4B head 362, 378 and 415 us.
-// The tensor cores bound it: 4096 bf16 rows, 32768 classes of 3584: stats 471 us (2.04 PFLOP/s), G 486, dH and dW 1020 (1.89
-// PFLOP/s), the pipe 90 to 94% active. 768 fp32 rows, 50304 classes of 512: 124, 148 and 312 us (320 to 255 TFLOP/s of fp32 products, the pipe 87,
+// The tensor cores bound it: 4096 bf16 rows, 32768 classes of 3584: stats 473 us (2.03 PFLOP/s), G 504, dH and dW 1017 (1.89
+// PFLOP/s), the pipe 87 to 92% active. 768 fp32 rows, 50304 classes of 512: 124, 148 and 312 us (320 to 255 TFLOP/s of fp32 products, the pipe 87,
 // 72 and 68% active: epilogues of short sums).
 //   warp 0     TMA: A and B tiles of 64 k, 6 stages of 32 KB (both CTAs)
 //   warp 1     TMEM, MMA issue (one thread of the even CTA)

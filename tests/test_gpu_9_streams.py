@@ -67,3 +67,32 @@ def test_calibration(A):
         ids.copy_(real)
         for got, ref in zip(calibrate(model, ids, 0.5, stream=side), want):
             assert (got == ref).all()
+
+
+@pytest.mark.parametrize("inside", [False, True])
+def test_ends_captured(A, inside):
+    """A step in a graph, on the captured stream or (inside) on another one that joins the capture for it; replayed on other
+    ids, beside eager steps on the side stream."""
+    from paper_2607_21291_gb300 import align
+    d, V, n = 128, 700, 90
+    cfg = A.make_cfg(S.PYTHIA_70M.replace(d=d, vocab=V, dtype="bf16"))
+    g = torch.Generator(device="cuda").manual_seed(5)
+    w = {"embed": torch.randn(V, d, generator=g, device="cuda").bfloat16(), "final_w": torch.ones(d, device="cuda").bfloat16(),
+         "final_b": torch.zeros(d, device="cuda").bfloat16()}
+    draws = [torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32) for _ in range(3)]
+    target = torch.roll(draws[0], 3).contiguous()
+    target[:9] = -1
+    want = [align.ends_gradients(cfg, w, ids, target) for ids in draws]
+    side, ids = torch.cuda.Stream(), draws[0].clone()
+    align.ends_gradients(cfg, w, ids, target, stream=side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, grads = align.ends_gradients(cfg, w, ids, target, stream=side if inside else None)
+    for new, (ref_loss, ref) in zip(draws, want):
+        ids.copy_(new)
+        graph.replay()
+        eager_loss, eager = align.ends_gradients(cfg, w, ids, target, stream=side)
+        assert torch.equal(loss, ref_loss) and torch.equal(eager_loss, ref_loss)
+        for k in ref:
+            assert torch.equal(grads[k], ref[k]) and torch.equal(eager[k], ref[k]), k
