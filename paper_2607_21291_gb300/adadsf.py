@@ -185,10 +185,15 @@ def _dev(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be a contiguous CUDA tensor")
 
 
+def _torch_stream(stream):
+    """torch's stream for any object with a stream's handle, which is all that the library's calls take of it."""
+    return stream if hasattr(stream, "wait_stream") else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
 def _torch_on(stream):
     """Torch's own work of a call on the call's stream (None: the current one): what is made there is cleared in order with
     the kernels that use it, and its memory goes back to that stream's pool."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream))
 
 
 @contextlib.contextmanager
@@ -196,8 +201,11 @@ def in_order(stream):
     """A step's torch work and library calls in one order, on `stream`: it waits for what the current stream was given
     before, and the current stream for the step, also where that fails halfway. Yields a function that tells the allocator
     of results which the caller reads on the current stream. None, or the current stream: nothing to do."""
-    outer = None if stream is None else torch.cuda.current_stream()
-    if stream is None or stream == outer:
+    if stream is None:
+        yield lambda *results: None
+        return
+    stream, outer = _torch_stream(stream), torch.cuda.current_stream()
+    if stream == outer:
         yield lambda *results: None
         return
 

@@ -96,3 +96,27 @@ def test_ends_captured(A, inside):
         assert torch.equal(loss, ref_loss) and torch.equal(eager_loss, ref_loss)
         for k in ref:
             assert torch.equal(grads[k], ref[k]) and torch.equal(eager[k], ref[k]), k
+
+
+def test_stream_by_handle(A):
+    """A call and a step on an object that has a stream's handle alone."""
+    from paper_2607_21291_gb300 import align
+    side = used_side()
+
+    class Handle:
+        cuda_stream = side.cuda_stream
+
+    d, V, n = 64, 300, 40
+    cfg = A.make_cfg(S.PYTHIA_70M.replace(d=d, vocab=V, dtype="f32"))
+    g = torch.Generator(device="cuda").manual_seed(6)
+    w = {"embed": torch.randn(V, d, generator=g, device="cuda"), "final_w": torch.ones(d, device="cuda"),
+         "final_b": torch.zeros(d, device="cuda")}
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    want_loss, want = align.ends_gradients(cfg, w, ids, ids)
+    out = torch.empty(n, d, device="cuda")
+    torch.cuda.synchronize()
+    A.adadsf_embed_forward(ids, w["embed"], out, stream=Handle())
+    loss, grads = align.ends_gradients(cfg, w, ids, ids, stream=Handle())
+    assert torch.equal(out, w["embed"][ids.long()]) and torch.equal(loss, want_loss)
+    for k in want:
+        assert torch.equal(grads[k], want[k]), k

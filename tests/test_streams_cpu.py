@@ -55,8 +55,9 @@ def test_workspace_is_cleared_on_its_stream(monkeypatch):
     monkeypatch.setattr(A.torch.cuda, "stream", on)
     monkeypatch.setattr(A.torch, "zeros", zeros)
     assert A.workspace(1000, "cpu").numel() == 1000
-    assert A.workspace(10, "cpu", "side").numel() == 256
-    assert made == [None, "side"]
+    side = Stream("side", [])
+    assert A.workspace(10, "cpu", side).numel() == 256
+    assert made == [None, side]
 
 
 def test_a_function_without_that_is_found():
@@ -141,3 +142,14 @@ def test_steps_run_in_order(module):
             assert all(isinstance(s, ast.Return) for s in work[1:]), f.name
             seen += 1
     assert seen == {"align": 3, "calibrate": 1}[module]
+
+
+def test_streams_by_handle(monkeypatch):
+    """An object with a handle alone, which the library's calls take: torch's own work goes to a stream of that handle."""
+    class Handle:
+        cuda_stream = 4711
+    made = []
+    monkeypatch.setattr(A.torch.cuda, "ExternalStream", lambda handle: made.append(handle) or Stream("external", []))
+    side = Stream("side", [])
+    assert A._torch_stream(side) is side and made == []
+    assert A._torch_stream(Handle()).name == "external" and made == [4711]
